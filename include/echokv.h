@@ -339,6 +339,159 @@ int echokv_full_attention_noalloc(const echokv_config* cfg, const void* k_pool, 
 uint64_t echokv_noalloc_scratch_bytes(void);
 
 /* =====================================================================================================
+ * A serving step over a cache held in 8 bits: plan, rotate, append, attend.
+ *
+ * The calls below need no context: they take the geometry from an echokv_config (n_q_heads, n_kv_heads, head_dim,
+ * page_tokens, max_batch, max_pages_per_seq, n_pages, dtype, softmax_scale, device; n_layers, group_size and the
+ * retained heads are ignored) and everything else as arguments, one layer per call.  In the order in which one step
+ * of a batch of requests uses them:
+ *     echokv_plan_tokens      pages for the new tokens, block table rows, slot map        (once per step)
+ *     echokv_rotate           rotary positions on the new queries and keys                (per layer)
+ *     echokv_quant_append     new keys and values into the layer's 8-bit cache            (per layer)
+ *     echokv_quant_attention  every new token attends its sequence                        (per layer)
+ *     echokv_release_pages    pages of finished requests back to the free list
+ * The new tokens of a step lie flat, sequence after sequence: token cu_tokens[b] + i is the i-th new token of
+ * sequence b.  They only enqueue work on `stream`, run on cfg->device and leave the calling thread's current device
+ * as it was, allocate nothing and can be captured into a graph.  dev_status (may be NULL) is a device int32 that
+ * receives the first device-side error found; it is not cleared (clear it once, read it whenever).
+ * Common errors: EINVAL (NULL or misaligned pointer, bad number), EUNSUPPORTED (head_dim, page_tokens, n_q_heads /
+ * n_kv_heads as for echokv_create), ECAPACITY (B > max_batch), ECUDA.
+ * ===================================================================================================== */
+
+/* Where echokv_plan_tokens writes; device pointers, all required (those of n_tokens entries may be NULL when n_tokens
+ * is 0).  seq_lens and free_count may be the buffers that the call reads; the others must not overlap its inputs. */
+typedef struct {
+  int32_t* cu_tokens;    /* [B + 1]    first new token of every sequence; the last entry is their number          */
+  int32_t* positions;    /* [n_tokens] index of the token in its sequence                                        */
+  int32_t* token_seqs;   /* [n_tokens] sequence b of the token                                                   */
+  int64_t* slot_map;     /* [n_tokens] pool row of the token: page * page_tokens + position % page_tokens        */
+  int32_t* seq_lens;     /* [B]        tokens of every sequence with the new ones                                */
+  int32_t* free_count;   /* [1]        pages still free                                                          */
+} echokv_step_plan;
+
+/* Block table rows and slot map of a step, from the lengths alone (the paper's paged caches take both as given).
+ * Sequence b (block table row dev_seq_slots[b], NULL = b) holds dev_seq_lens[b] tokens (>= 0) and gets dev_new_lens[b]
+ * (>= 0) more.  It needs ceil((len + new) / P) - ceil(len / P) pages, P = page_tokens.  The free list is a stack:
+ * dev_free_pages[0 .. *dev_free_count - 1] (n_pages entries of room); pages are taken from its top, in the order of
+ * the sequences and of their positions, and written to the block table.
+ * A sequence is served if it needs no page or the pages needed by it and by all sequences before it are there, and if
+ * the new tokens up to its own fit in n_tokens; one that is not served gets no token, its length stays, and the device
+ * status is ECAPACITY.  A bad slot (EBADPAGE) or length (EBADLENGTH) is not served either and needs nothing; a page id
+ * outside the pool goes to the block table as it is, its tokens get slot -1 and the status EBADPAGE.
+ * Entries of positions, token_seqs and slot_map behind the last token are set to -1.
+ * Two sequences with the same slot are a caller's error (their block table row is unspecified).
+ * ECAPACITY also if B > 8192. */
+int echokv_plan_tokens(const echokv_config* cfg, int32_t* dev_block_table, const int32_t* dev_seq_slots,
+                       const int32_t* dev_seq_lens, const int32_t* dev_new_lens, const int32_t* dev_free_pages,
+                       const int32_t* dev_free_count, int B, int n_tokens, const echokv_step_plan* plan,
+                       int32_t* dev_status, void* stream);
+
+/* The pages of B finished sequences (dev_seq_lens[b] tokens in block table row dev_seq_slots[b]) go back to the top of
+ * the free list, in the order of the sequences and of their pages; *dev_free_count is updated.  Bad slots and lengths
+ * are skipped (device status as above); a page id outside the pool, and pages beyond n_pages entries of the list, are
+ * dropped with EBADPAGE / ECAPACITY.  Releasing a sequence twice is a caller's error.  ECAPACITY also if B > 8192. */
+int echokv_release_pages(const echokv_config* cfg, const int32_t* dev_block_table, const int32_t* dev_seq_slots,
+                         const int32_t* dev_seq_lens, int B, int32_t* dev_free_pages, int32_t* dev_free_count,
+                         int32_t* dev_status, void* stream);
+
+/* Rotary position embedding of fresh queries and keys, with up to four position axes (time, height, width of images
+ * and video; one axis for text): echokv_set_rope turns cached keys when they are read and expects q rotated already;
+ * this is the call that rotates q -- and k, for a cache that holds rotated keys, as the 8-bit cache does.
+ * With half = rot_dim / 2, feature j < half pairs with feature j + half (the layout of echokv_set_rope), features from
+ * rot_dim on are copied:
+ *     x'[j] = x[j] cos(a) - x[j + half] sin(a),  x'[j + half] = x[j + half] cos(a) + x[j] sin(a),
+ *     a = dev_positions[axis(j)][token] * theta^(-2 j / rot_dim)
+ * angles reduced in fp64.  inverse != 0 turns by -a: the gradient with respect to x of a rotated x.
+ *  - q, k: [n_tokens] rows of n_q_heads (n_kv_heads) x head_dim elements, `*_stride` elements from row to row, so that
+ *    slices of a fused projection can be given; q_out, k_out likewise, each its input itself (then with the same
+ *    stride) or memory that does not overlap the inputs.  q or k may be NULL with its output: nothing is done for it.
+ *    16-byte aligned rows (EINVAL).
+ *  - dev_positions: int32 [n_axes][n_tokens], any values.
+ *  - sections: host array [n_axes], frequencies of each axis, summing to half (NULL with one axis).  interleaved = 0:
+ *    axis(j) runs through the sections in order.  interleaved = 1: axis(j) = j mod n_axes while j / n_axes <
+ *    sections[axis], otherwise axis 0.
+ *  - rot_dim: 0 = head_dim; otherwise a multiple of 16 (bf16) or 8 (fp32) up to head_dim (EUNSUPPORTED).
+ *  - theta >= 1. */
+int echokv_rotate(const echokv_config* cfg, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                  void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride, const int32_t* dev_positions,
+                  int n_axes, const int32_t* sections, int interleaved, int rot_dim, double theta, int inverse,
+                  int n_tokens, void* stream);
+
+enum { ECHOKV_INT8 = 0, ECHOKV_E4M3 = 1 };          /* echokv_quant_cache.format */
+enum { ECHOKV_QUANT_BLOCK_TOKENS = 16 };            /* tokens that share a scale */
+
+/* The cache of ONE layer in 8 bits: device pointers, 16-byte aligned, borrowed.  A block is 16 consecutive tokens of a
+ * sequence (positions 16 n .. 16 n + 15) and one KV head.  With a its largest magnitude and Q = 127 (int8) or 448 (e4m3),
+ * all in fp32: scale = max(a * (1 / Q), 2^-100), code = round(x * (1 / scale)) to nearest even, value = code * scale.  A block
+ * with an infinity or NaN gets scale NaN and codes 0: whatever attends one of its tokens becomes NaN, nothing else does.
+ * The open block of a sequence (its last len % 16 tokens) waits unquantised in the tail buffers, so that every block
+ * is rounded once and the cache does not depend on how many tokens came per call; an infinity or NaN in it counts for all of
+ * it in the same way. */
+typedef struct {
+  void* k_codes;         /* int8 or e4m3 [n_pages][n_kv_heads][page_tokens][head_dim]      */
+  void* v_codes;
+  float* k_scales;       /* [n_pages][n_kv_heads][page_tokens / 16]                        */
+  float* v_scales;
+  void* k_tail;          /* storage dtype [max_batch][n_kv_heads][16][head_dim], row = position % 16 */
+  void* v_tail;
+  int32_t format;        /* ECHOKV_INT8 or ECHOKV_E4M3                                     */
+  int32_t reserved;
+} echokv_quant_cache;
+
+typedef struct {
+  uint64_t codes_bytes;      /* one of k_codes, v_codes  */
+  uint64_t scales_bytes;     /* one of k_scales, v_scales */
+  uint64_t tail_bytes;       /* one of k_tail, v_tail    */
+  uint64_t workspace_bytes;  /* workspace of echokv_quant_attention */
+} echokv_quant_sizes;
+
+/* Sizes implied by a config.  Pure host arithmetic, no CUDA call. */
+int echokv_query_quant_sizes(const echokv_config* cfg, echokv_quant_sizes* out);
+
+/* Append the step's tokens to the layer's 8-bit cache.  k_new, v_new: [n_tokens] rows of n_kv_heads x head_dim elements of the
+ * storage dtype, k_stride / v_stride elements from row to row (16-byte aligned rows).  slot_map, token_seqs and
+ * cu_tokens are echokv_plan_tokens' (a token with slot -1 is skipped).  A block that the tokens complete is
+ * quantised, from the tail rows of its earlier tokens and the new ones; tokens of a block that stays open go to the tail.
+ * The tokens of a sequence must be appended in order of position, each call beginning where the cache ends (a token
+ * of the open block may be appended again); a sequence may appear once per call.
+ * Bad row, sequence or slot -> device status EBADPAGE, that token is skipped. */
+int echokv_quant_append(const echokv_config* cfg, const echokv_quant_cache* cache, const void* k_new, int64_t k_stride,
+                        const void* v_new, int64_t v_stride, const int64_t* dev_slot_map,
+                        const int32_t* dev_token_seqs, const int32_t* dev_cu_tokens, const int32_t* dev_seq_slots, int B,
+                        int n_tokens, int32_t* dev_status, void* stream);
+
+/* What is done to the scores x = softmax_scale q . k before the softmax; zeros / NULL = nothing.  In this order:
+ *     softcap > 0:   x = softcap * tanh(x / softcap)
+ *     alibi_slopes:  x = x - alibi_slopes[h] * |p - t|      (p, t: positions of the query and the key)
+ *     mask:          key t is seen if t <= p or t < prefix_lens[b]  (a prefix whose tokens see each other)        */
+typedef struct {
+  float softcap;
+  int32_t reserved;
+  const float* alibi_slopes;   /* device fp32 [n_q_heads] or NULL */
+  const int32_t* prefix_lens;  /* device int32 [B] or NULL        */
+} echokv_score_options;
+
+/* Attention over the 8-bit cache (Eq. 7 on the values the cache stands for).  The n new tokens of sequence b are its
+ * last n tokens, already appended: query i sits at position dev_seq_lens[b] - n + i.
+ *  - q: [n_tokens] rows of n_q_heads x head_dim elements, q_stride elements from row to row; out: dense
+ *    [n_tokens][n_q_heads][head_dim] of the storage dtype (both 16-byte aligned).
+ *  - dev_cu_tokens: [B + 1], or NULL for one token per sequence (n_tokens = B).  max_new: an upper bound of the tokens
+ *    any sequence has in this call (1 for a decode step): it selects the kernels.
+ *  - workspace: device buffer of echokv_quant_sizes.workspace_bytes, 256-byte aligned.  Calls that share one must
+ *    not overlap on the device (captured graphs may share it if they run one after the other); nothing is kept in it.
+ *  - rows of out behind the last sequence's are left as they were.  A sequence without new tokens has no output.
+ * A sequence with a bad slot, a length beyond its capacity or shorter than its new tokens, or more than max_new new
+ * tokens: zeros and the device status (EBADPAGE, EBADLENGTH); offsets that decrease or pass n_tokens: EBADLENGTH, nothing is
+ * written for that sequence.  A page id outside the pool: EBADPAGE, the output of its sequence is unspecified.
+ * Scores and sums are fp32; codes enter the products exactly, queries and probabilities as pairs of fp16 (22 bits),
+ * for chunks of bf16 queries (max_new > 8) as single fp16. */
+int echokv_quant_attention(const echokv_config* cfg, const echokv_quant_cache* cache, const echokv_score_options* options,
+                           const void* q, int64_t q_stride, void* out, const int32_t* dev_block_table,
+                           const int32_t* dev_seq_slots, const int32_t* dev_seq_lens, const int32_t* dev_cu_tokens, int B,
+                           int n_tokens, int max_new, void* workspace, uint64_t workspace_bytes, int32_t* dev_status,
+                           void* stream);
+
+/* =====================================================================================================
  * Diagnostics: switches, counters and probes for tests and benchmarks.  No product call depends on them;
  * contexts start on the fastest kernels their shape allows.
  * ===================================================================================================== */

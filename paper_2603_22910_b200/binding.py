@@ -19,6 +19,9 @@ ECHOKV_OK = 0
 ECHOKV_EINVAL, ECHOKV_ENOTANCHOR, ECHOKV_ENOTCOMPRESSED, ECHOKV_ECAPACITY = -1, -2, -3, -4
 ECHOKV_ENOWEIGHTS, ECHOKV_ECUDA, ECHOKV_ETIMEOUT, ECHOKV_EBADPAGE = -5, -6, -7, -8
 ECHOKV_EUNSUPPORTED, ECHOKV_ENOTABLE, ECHOKV_EBADLENGTH, ECHOKV_ESCRATCH = -9, -10, -11, -12
+ECHOKV_INT8, ECHOKV_E4M3 = 0, 1
+ECHOKV_QUANT_BLOCK_TOKENS = 16
+QUANT_FORMATS = {"int8": ECHOKV_INT8, "e4m3": ECHOKV_E4M3}
 
 
 class echokv_config(C.Structure):
@@ -38,6 +41,26 @@ class echokv_sizes(C.Structure):
 class echokv_buffers(C.Structure):
     _fields_ = [("k_pools", C.POINTER(C.c_void_p)), ("v_pools", C.POINTER(C.c_void_p)),
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+class echokv_step_plan(C.Structure):
+    _fields_ = [("cu_tokens", C.c_void_p), ("positions", C.c_void_p), ("token_seqs", C.c_void_p),
+                ("slot_map", C.c_void_p), ("seq_lens", C.c_void_p), ("free_count", C.c_void_p)]
+
+
+class echokv_quant_cache(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
+                ("k_tail", C.c_void_p), ("v_tail", C.c_void_p), ("format", C.c_int32), ("reserved", C.c_int32)]
+
+
+class echokv_quant_sizes(C.Structure):
+    _fields_ = [("codes_bytes", C.c_uint64), ("scales_bytes", C.c_uint64), ("tail_bytes", C.c_uint64),
+                ("workspace_bytes", C.c_uint64)]
+
+
+class echokv_score_options(C.Structure):
+    _fields_ = [("softcap", C.c_float), ("reserved", C.c_int32), ("alibi_slopes", C.c_void_p),
+                ("prefix_lens", C.c_void_p)]
 
 
 EXPORTS = {
@@ -88,6 +111,20 @@ EXPORTS = {
                                                 C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
                                                 C.c_void_p, C.c_void_p]),
     "echokv_noalloc_scratch_bytes": (C.c_uint64, []),
+    "echokv_plan_tokens": (C.c_int, [C.POINTER(echokv_config), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                     C.c_void_p, C.c_int, C.c_int, C.POINTER(echokv_step_plan), C.c_void_p, C.c_void_p]),
+    "echokv_release_pages": (C.c_int, [C.POINTER(echokv_config), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p,
+                                       C.c_void_p, C.c_void_p, C.c_void_p]),
+    "echokv_rotate": (C.c_int, [C.POINTER(echokv_config), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.POINTER(C.c_int32), C.c_int, C.c_int, C.c_double,
+                                C.c_int, C.c_int, C.c_void_p]),
+    "echokv_query_quant_sizes": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_quant_sizes)]),
+    "echokv_quant_append": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_quant_cache), C.c_void_p, C.c_int64, C.c_void_p,
+                                      C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p,
+                                      C.c_void_p]),
+    "echokv_quant_attention": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_quant_cache), C.POINTER(echokv_score_options),
+                                         C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
+                                         C.c_int, C.c_int, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p]),
     "echokv_strerror": (C.c_char_p, [C.c_int]),
 }
 
@@ -377,6 +414,198 @@ def echokv_full_attention_noalloc(cfg: echokv_config, k_pool, v_pool, block_tabl
                                                _ptr(q), _ptr(out), _ptr(seq_slots), _ptr(seq_lens),
                                                q.shape[0], _ptr(status_out), _stream_handle(stream)),
            "echokv_full_attention_noalloc")
+
+
+# ---- a serving step over a cache held in 8 bits ------------------------------------------------------------------
+def _stream_on(device: int, stream) -> int | None:
+    import torch
+    s = torch.cuda.current_stream(device) if stream is None else stream
+    return s.cuda_stream or None
+
+
+def _dense(t, dtype, n, name):
+    """Address of a contiguous device tensor of `dtype` with at least n elements (None stays NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous() or t.numel() < n:
+        raise ValueError("%s: a contiguous %s device tensor of at least %d elements is needed" % (name, dtype, n))
+    return t.data_ptr()
+
+
+def _rows(t, heads, d, dtype, name):
+    """(address, elements from row to row) of a [n][heads][d] device tensor whose rows are dense."""
+    if t.dtype is not dtype or not t.is_cuda or t.dim() != 3 or t.shape[1:] != (heads, d) or (
+            t.shape[0] > 0 and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != d))):
+        raise ValueError("%s: a [tokens][%d][%d] %s device tensor with dense rows is needed" % (name, heads, d, dtype))
+    # (the stride of a single row is anything)
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * d
+
+
+def _dtype(cfg):
+    import torch
+    return torch.bfloat16 if cfg.dtype == ECHOKV_BF16 else torch.float32
+
+
+class StepPlan:
+    """What plan_tokens writes: cu_tokens [B + 1], positions, token_seqs [n_tokens], seq_lens [B], free_count [1] (int32) and
+    slot_map [n_tokens] (int64)."""
+    __slots__ = ("cu_tokens", "positions", "token_seqs", "slot_map", "seq_lens", "free_count")
+
+    def __init__(self, batch: int, n_tokens: int, device, seq_lens=None, free_count=None):
+        import torch
+        buf = torch.empty(2 * batch + 2 * n_tokens + 2, dtype=torch.int32, device=device)
+        self.cu_tokens, self.positions, self.token_seqs, lens, count = buf.split((batch + 1, n_tokens, n_tokens, batch, 1))
+        self.slot_map = torch.empty(n_tokens, dtype=torch.int64, device=device)
+        self.seq_lens = lens if seq_lens is None else seq_lens
+        self.free_count = count if free_count is None else free_count
+
+
+def plan_tokens(cfg: echokv_config, block_table, seq_lens, new_lens, free_pages, free_count, n_tokens: int, seq_slots=None,
+                out: StepPlan | None = None, status=None, stream=None) -> StepPlan:
+    """Pages for new_lens[b] more tokens of sequences that hold seq_lens[b]: fills block_table ([max_batch][max_pages_per_seq]
+    int32) and returns the step's plan for up to n_tokens tokens.  `out` may hold seq_lens and free_count themselves (updated
+    in place) and is reused by captured steps; status: optional int32 device tensor (see echokv.h)."""
+    import torch
+    i32, B = torch.int32, seq_lens.shape[0]
+    if out is None:
+        out = StepPlan(B, n_tokens, seq_lens.device)
+    elif out.cu_tokens.numel() < B + 1 or out.seq_lens.numel() < B or min(out.positions.numel(), out.token_seqs.numel(),
+                                                                          out.slot_map.numel()) < n_tokens:
+        raise ValueError("out: too small for %d sequences and %d tokens" % (B, n_tokens))
+    p = echokv_step_plan(out.cu_tokens.data_ptr(), out.positions.data_ptr(), out.token_seqs.data_ptr(), out.slot_map.data_ptr(),
+                         out.seq_lens.data_ptr(), out.free_count.data_ptr())
+    _check(lib().echokv_plan_tokens(C.byref(cfg), _dense(block_table, i32, cfg.max_batch * cfg.max_pages_per_seq, "block_table"),
+                                    _dense(seq_slots, i32, B, "seq_slots"), _dense(seq_lens, i32, B, "seq_lens"),
+                                    _dense(new_lens, i32, B, "new_lens"), _dense(free_pages, i32, cfg.n_pages, "free_pages"),
+                                    _dense(free_count, i32, 1, "free_count"), B, n_tokens, C.byref(p),
+                                    _dense(status, i32, 1, "status"), _stream_on(cfg.device, stream)), "echokv_plan_tokens")
+    return out
+
+
+def release_pages(cfg: echokv_config, block_table, seq_lens, free_pages, free_count, seq_slots=None, status=None,
+                  stream=None) -> None:
+    """Put the pages of finished sequences back on the free list (free_pages, free_count are updated)."""
+    import torch
+    i32, B = torch.int32, seq_lens.shape[0]
+    _check(lib().echokv_release_pages(C.byref(cfg), _dense(block_table, i32, cfg.max_batch * cfg.max_pages_per_seq, "block_table"),
+                                      _dense(seq_slots, i32, B, "seq_slots"), _dense(seq_lens, i32, B, "seq_lens"), B,
+                                      _dense(free_pages, i32, cfg.n_pages, "free_pages"), _dense(free_count, i32, 1, "free_count"),
+                                      _dense(status, i32, 1, "status"), _stream_on(cfg.device, stream)), "echokv_release_pages")
+
+
+def rotate(cfg: echokv_config, q, k, positions, theta: float, sections=None, rot_dim: int = 0, interleaved: bool = False,
+           inverse: bool = False, q_out=None, k_out=None, stream=None):
+    """Rotary positions on q [T][n_q_heads][d] and k [T][n_kv_heads][d] (either may be None; rows may be slices of a wider
+    tensor); positions int32 [T] or [n_axes][T].  Returns (q_out, k_out), new tensors unless given -- they may be q and k.
+    inverse = True is the gradient's pass."""
+    import torch
+    dt, d = _dtype(cfg), cfg.head_dim
+    some = q if q is not None else k
+    if some is None:
+        raise ValueError("rotate: neither q nor k")
+    T = some.shape[0]
+    axes = 1 if positions.dim() == 1 else positions.shape[0]
+    if positions.shape[-1] != T or (q is not None and k is not None and k.shape[0] != T):
+        raise ValueError("rotate: q, k and positions differ in their number of tokens")
+    args = []
+    outs = []
+    for x, out, heads, name in ((q, q_out, cfg.n_q_heads, "q"), (k, k_out, cfg.n_kv_heads, "k")):
+        if x is None:
+            args.append((None, 0, None, 0))
+            outs.append(None)
+            continue
+        if out is None:
+            out = torch.empty((T, heads, d), dtype=dt, device=x.device)
+        elif out.shape[0] != T:
+            raise ValueError("rotate: an output differs in its number of tokens")
+        args.append(_rows(x, heads, d, dt, name) + _rows(out, heads, d, dt, name + "_out"))
+        outs.append(out)
+    sec = None if sections is None else (C.c_int32 * len(sections))(*sections)
+    if sections is not None and len(sections) != axes:
+        raise ValueError("rotate: one section per position axis")
+    (qp, qs, qo, qos), (kp, ks, ko, kos) = args
+    _check(lib().echokv_rotate(C.byref(cfg), qp, qs, kp, ks, qo, qos, ko, kos, _dense(positions, torch.int32, axes * T, "positions"),
+                               axes, sec, 1 if interleaved else 0, rot_dim, theta, 1 if inverse else 0, T,
+                               _stream_on(cfg.device, stream)), "echokv_rotate")
+    return outs[0], outs[1]
+
+
+def query_quant_sizes(cfg: echokv_config) -> echokv_quant_sizes:
+    out = echokv_quant_sizes()
+    _check(lib().echokv_query_quant_sizes(C.byref(cfg), C.byref(out)), "echokv_query_quant_sizes")
+    return out
+
+
+class QuantCache:
+    """One layer's cache in 8 bits: codes int8 or float8_e4m3fn [n_pages][n_kv_heads][page_tokens][d], a scale for each 16 tokens
+    and head [n_pages][n_kv_heads][page_tokens / 16], and the open blocks' rows in the storage type [max_batch][n_kv_heads][16][d].
+    Allocates them unless they are given; `workspace` may be shared by the layers of a model (calls that share one must not
+    overlap on the device)."""
+
+    def __init__(self, cfg: echokv_config, fmt: str, k_codes=None, v_codes=None, k_scales=None, v_scales=None, k_tail=None,
+                 v_tail=None, workspace=None):
+        import torch
+        if fmt not in QUANT_FORMATS:
+            raise ValueError("format %r is not one of %s" % (fmt, sorted(QUANT_FORMATS)))
+        self.cfg, self.fmt, self.tdtype = cfg, fmt, _dtype(cfg)
+        self.sizes = sizes = query_quant_sizes(cfg)
+        dev = torch.device("cuda", cfg.device)
+        H, P, d, N = cfg.n_kv_heads, cfg.page_tokens, cfg.head_dim, cfg.n_pages
+        code = torch.int8 if fmt == "int8" else torch.float8_e4m3fn
+
+        def held(t, shape, dtype, name):
+            if t is None:
+                return torch.zeros(shape, dtype=dtype, device=dev)
+            if tuple(t.shape) != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+                raise ValueError("%s: a contiguous %s device tensor of shape %s is needed" % (name, dtype, shape))
+            return t
+        self.k_codes = held(k_codes, (N, H, P, d), code, "k_codes")
+        self.v_codes = held(v_codes, (N, H, P, d), code, "v_codes")
+        self.k_scales = held(k_scales, (N, H, P // ECHOKV_QUANT_BLOCK_TOKENS), torch.float32, "k_scales")
+        self.v_scales = held(v_scales, (N, H, P // ECHOKV_QUANT_BLOCK_TOKENS), torch.float32, "v_scales")
+        tail = (cfg.max_batch, H, ECHOKV_QUANT_BLOCK_TOKENS, d)
+        self.k_tail = held(k_tail, tail, self.tdtype, "k_tail")
+        self.v_tail = held(v_tail, tail, self.tdtype, "v_tail")
+        self.workspace = torch.empty(sizes.workspace_bytes, dtype=torch.uint8, device=dev) if workspace is None else workspace
+        self._c = echokv_quant_cache(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scales.data_ptr(),
+                                     self.v_scales.data_ptr(), self.k_tail.data_ptr(), self.v_tail.data_ptr(),
+                                     QUANT_FORMATS[fmt], 0)
+
+    def append(self, k_new, v_new, slot_map, token_seqs, cu_tokens, seq_slots=None, status=None, stream=None) -> None:
+        """k_new, v_new [T][n_kv_heads][d] (rows may be slices of a wider tensor); slot_map, token_seqs, cu_tokens: plan_tokens'."""
+        import torch
+        cfg, T, B = self.cfg, k_new.shape[0], cu_tokens.shape[0] - 1
+        if v_new.shape[0] != T:
+            raise ValueError("k_new and v_new differ in their number of tokens")
+        kp, ks = _rows(k_new, cfg.n_kv_heads, cfg.head_dim, self.tdtype, "k_new")
+        vp, vs = _rows(v_new, cfg.n_kv_heads, cfg.head_dim, self.tdtype, "v_new")
+        _check(lib().echokv_quant_append(C.byref(cfg), C.byref(self._c), kp, ks, vp, vs, _dense(slot_map, torch.int64, T, "slot_map"),
+                                         _dense(token_seqs, torch.int32, T, "token_seqs"),
+                                         _dense(cu_tokens, torch.int32, B + 1, "cu_tokens"), _dense(seq_slots, torch.int32, B, "seq_slots"),
+                                         B, T, _dense(status, torch.int32, 1, "status"), _stream_on(cfg.device, stream)),
+               "echokv_quant_append")
+
+    def attention(self, q, block_table, seq_lens, cu_tokens=None, max_new: int = 1, seq_slots=None, softcap: float = 0.0,
+                  alibi_slopes=None, prefix_lens=None, out=None, status=None, stream=None):
+        """q [T][n_q_heads][d]: the new tokens of every sequence, which are its last ones and already appended (cu_tokens None:
+        one each).  max_new bounds the new tokens of any sequence.  Returns out [T][n_q_heads][d] in the storage type."""
+        import torch
+        cfg, T, B = self.cfg, q.shape[0], seq_lens.shape[0]
+        qp, qs = _rows(q, cfg.n_q_heads, cfg.head_dim, self.tdtype, "q")
+        if out is None:
+            out = torch.empty((T, cfg.n_q_heads, cfg.head_dim), dtype=self.tdtype, device=q.device)
+        opts = None
+        if softcap or alibi_slopes is not None or prefix_lens is not None:
+            opts = C.byref(echokv_score_options(softcap, 0, _dense(alibi_slopes, torch.float32, cfg.n_q_heads, "alibi_slopes"),
+                                                _dense(prefix_lens, torch.int32, B, "prefix_lens")))
+        _check(lib().echokv_quant_attention(C.byref(cfg), C.byref(self._c), opts, qp, qs,
+                                            _dense(out, self.tdtype, T * cfg.n_q_heads * cfg.head_dim, "out"),
+                                            _dense(block_table, torch.int32, cfg.max_batch * cfg.max_pages_per_seq, "block_table"),
+                                            _dense(seq_slots, torch.int32, B, "seq_slots"), _dense(seq_lens, torch.int32, B, "seq_lens"),
+                                            _dense(cu_tokens, torch.int32, B + 1, "cu_tokens"), B, T, max_new, self.workspace.data_ptr(),
+                                            self.workspace.numel(), _dense(status, torch.int32, 1, "status"),
+                                            _stream_on(cfg.device, stream)), "echokv_quant_attention")
+        return out
 
 
 def config_for(w, n_pages: int | None = None, device: int = 0, max_batch: int | None = None) -> echokv_config:

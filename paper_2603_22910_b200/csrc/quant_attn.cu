@@ -1,0 +1,633 @@
+// Attention over a cache held in 8 bits, one or a few queries per sequence (decode steps, drafts to verify).
+//
+//   x_t = scale q . k_t  [capped by softcap tanh(x / softcap)] [- slope |p - t|],   o = sum_t 2^(x_t log2e - m) v_t / sum_t 2^(...)
+//
+// The codes are read once from HBM and that is the bound; everything else has to fit beside the stream (23 bytes per
+// clock and SM).  The design:
+//
+//   work     A unit is one 16-token block (one scale) of one KV head for one tile of 8 query rows (the query heads that share
+//            the KV head, times a sequence's new tokens).  The units of all sequences are laid end to end and cut into
+//            equal shares, one per CTA and within it one per warp, computed on the device from the lengths: ragged
+//            batches, one long request and a thousand short ones all balance.  A share cuts at most two (sequence, head)
+//            items; their partial results (running maximum, sum, output) are combined inside the CTA through shared
+//            memory and between CTAs by a second small kernel.
+//   copies   Each lane copies, by 16-byte cp.async into a ring of its own, exactly the bytes that it will use as matrix operands:
+//            no barrier and no bank conflict, and 16 KB in flight per warp.
+//   products mma.sync m16n8k16 in fp16 with the 8 query rows on the upper half of the M rows; rows 8..15 carry the low-order
+//            halves (q = q_hi + q_lo for fp32 queries, P = P_hi + P_lo), so scores and outputs keep 22 bits at no cost.  Codes
+//            convert to fp16 exactly.  (The tile has few rows: tcgen05's 128 would be padding, and the tensor pipe is a
+//            third busy as it is.)
+//   scales   The K scale multiplies the score, the V scale the probability.  fp16's range is kept by running references, powers of
+//            two: queries per row, V scales per warp; like the running maximum they move only when they must (a factor
+//            of 2^8 of head-room), one vote per block.
+//   tail     The open block is in the storage type: bf16 converts to fp16 exactly around its own power of two, fp32
+//            as a pair of fp16.
+#include "quant_common.cuh"
+
+namespace echokv {
+
+namespace {
+
+constexpr int kQaWarps = 8;
+constexpr int kQaThreads = kQaWarps * 32;
+constexpr int kQaRows = 8;                        // query rows per tile
+constexpr int kQaStages = 4;
+constexpr int kQaMaxCtas = 512;
+constexpr int kQaMinShare = kQaWarps;             // units per CTA at least: one block for every warp
+constexpr float kQaGrow = 8.f;                    // the references move when a score is 2^8 above them
+constexpr float kQaPScale = 32.f;                 // P <= 2^8 times a scale ratio < 2 times 2^5: below 2^15
+
+struct QaDesc {                                   // an item cut at the end of CTA g's share
+  int n_parts;                                    // CTAs that hold parts of it (0: none starts here)
+  int b, tile, h;
+};
+
+__host__ __device__ constexpr int qa_stage_bytes(int D) { return 2 * kQuantBlock * D + 256; }
+
+struct QaSeg {
+  unsigned long long item;                        // first unit of the item
+  unsigned long long item_end;
+  int b, tile, h;
+  int valid, starts, ends;
+};
+
+template <int D>
+struct QaSmem {
+  QaSeg seg[2 * kQaWarps];
+  float m[2 * kQaWarps][kQaRows], l[2 * kQaWarps][kQaRows];
+  float o[2 * kQaWarps][kQaRows][D];
+  unsigned long long pre[kQaThreads + 1];
+  unsigned long long warp_sums[kQaWarps];
+};
+template <int D>
+__host__ __device__ constexpr size_t qa_ring_bytes() { return (size_t)kQaWarps * kQaStages * qa_stage_bytes(D); }
+
+// workspace: [ctas] QaDesc | [ctas][2][8] (m, l) | [ctas][2][8][D] o
+template <int D>
+struct QaWork {
+  QaDesc* desc;
+  float2* ml;
+  float* o;
+  __host__ __device__ explicit QaWork(unsigned char* ws) {
+    desc = reinterpret_cast<QaDesc*>(ws);
+    ml = reinterpret_cast<float2*>(ws + kQaMaxCtas * sizeof(QaDesc));
+    o = reinterpret_cast<float*>(ws + kQaMaxCtas * (sizeof(QaDesc) + 2 * kQaRows * sizeof(float2)));
+  }
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint4 lds16(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds8(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ float lds4(uint32_t a) {
+  float v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
+
+__device__ __forceinline__ int row_tiles(const QuantAttnArgs& a, const QuantSeq& s) {
+  return (s.n * a.group + kQaRows - 1) / kQaRows;
+}
+__device__ __forceinline__ unsigned long long units_of(const QuantAttnArgs& a, const QuantSeq& s) {
+  if (s.error || s.n == 0 || chunk_sequence(a, s)) return 0;
+  return (unsigned long long)row_tiles(a, s) * a.g.n_kv_heads * ((s.len + kQuantBlock - 1) / kQuantBlock);
+}
+
+template <typename T>
+__device__ __forceinline__ float load_elem(const T* p) { return to_f32(*p); }
+
+template <typename T>
+__device__ __forceinline__ T from_f32(float x);
+template <>
+__device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16(x); }
+
+template <typename T, int FMT, int D>
+__global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_constant__ QuantAttnArgs a) {
+  constexpr int KC = D / 64;                      // 16-byte pieces of a key row per lane
+  constexpr int KS = D / 16;                      // k-steps of q . k
+  constexpr int NT = D / 8;                       // output tiles; V bytes per token and lane
+  constexpr bool kF32 = sizeof(T) == 4;
+  extern __shared__ __align__(128) unsigned char qa_raw[];
+  QaSmem<D>& sm = *reinterpret_cast<QaSmem<D>*>(qa_raw + qa_ring_bytes<D>());
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
+  const uint32_t ring = smem_u32(qa_raw) + warp * kQaStages * qa_stage_bytes(D);
+  const QuantGeom& g = a.g;
+  const int H = g.n_kv_heads;
+
+  // ---- the units of the call, and this CTA's and warp's share of them
+  const int per = (a.B + kQaThreads - 1) / kQaThreads;
+  {
+    unsigned long long n = 0;
+    for (int b = tid * per; b < min(a.B, (tid + 1) * per); ++b) {
+      const QuantSeq s = quant_seq(a, b);
+      if (s.error && blockIdx.x == 0) report_opt(a.status, s.error);
+      n += units_of(a, s);
+    }
+    unsigned long long x = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned long long y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) sm.warp_sums[warp] = x;
+    if (tid < 2 * kQaWarps) sm.seg[tid].valid = 0;
+    __syncthreads();
+    unsigned long long before = 0;
+    for (int w = 0; w < warp; ++w) before += sm.warp_sums[w];
+    sm.pre[tid + 1] = before + x;
+    if (tid == 0) sm.pre[0] = 0;
+    __syncthreads();
+  }
+  const unsigned long long total = sm.pre[kQaThreads];
+  unsigned long long share = (total + gridDim.x - 1) / gridDim.x;
+  if (share < kQaMinShare) share = kQaMinShare;
+  const unsigned long long cta0 = min(total, share * blockIdx.x), cta1 = min(total, cta0 + share);
+  const unsigned long long wshare = (cta1 - cta0 + kQaWarps - 1) / kQaWarps;
+  unsigned long long u = min(cta1, cta0 + wshare * warp);
+  const unsigned long long u_end = min(cta1, u + wshare);
+
+  // the sequence of unit u
+  int b = 0;
+  unsigned long long base = 0;                    // first unit of sequence b
+  if (u < u_end) {
+    int lo = 0, hi = kQaThreads;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (sm.pre[mid] <= u) lo = mid; else hi = mid;
+    }
+    b = lo * per;
+    base = sm.pre[lo];
+  }
+
+  while (u < u_end) {
+    QuantSeq s = quant_seq(a, b);
+    unsigned long long n_units = units_of(a, s);
+    while (base + n_units <= u) {
+      base += n_units;
+      ++b;
+      s = quant_seq(a, b);
+      n_units = units_of(a, s);
+    }
+    const int n_blk = (s.len + kQuantBlock - 1) / kQuantBlock, tiles = row_tiles(a, s);
+    const unsigned long long rem = u - base;
+    const int ht = (int)(rem / n_blk), blk0 = (int)(rem - (unsigned long long)ht * n_blk);
+    const int h = ht / tiles, tile = ht - h * tiles;
+    const unsigned long long item = u - blk0, item_end = item + n_blk;
+    const unsigned long long seg_end = min(item_end, u_end);
+    const int nb = (int)(seg_end - u);
+    const int n_full = s.len / kQuantBlock;       // blocks held as codes; block n_full is the open one
+
+    // ---- this lane's query row
+    const int qrow = tile * kQaRows + r;
+    const bool row_ok = qrow < s.n * a.group;
+    const int qi = row_ok ? qrow >> a.group_shift : 0, head = h * a.group + (qrow & (a.group - 1));
+    const int pos = s.len - s.n + qi;
+    const int prefix = a.prefix ? a.prefix[b] : 0;
+    uint32_t qh[KS][2], ql[KS][2];
+    float c_row;
+    {
+      const T* qp = static_cast<const T*>(a.q) + (long long)(s.first + qi) * a.q_stride + (long long)head * D;
+      float top = 0.f;
+      float v[KC * 16];
+#pragma unroll
+      for (int i = 0; i < KC; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; e += Vec16<T>::N)
+          if (row_ok) {
+            Vec16<T>::load(qp + 16 * (c + 4 * i) + e, v + 16 * i + e);
+          } else {
+#pragma unroll
+            for (int f = 0; f < Vec16<T>::N; ++f) v[16 * i + e + f] = 0.f;
+          }
+#pragma unroll
+      for (int e = 0; e < KC * 16; ++e) top = fmaxf(top, fabsf(v[e]));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      float back;
+      const float up = scale_up_to_half(top, &back);
+      c_row = back * a.scale * (a.softcap > 0.f ? 1.f : kLog2e);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          const float x0 = v[4 * ks + 2 * f] * up, x1 = v[4 * ks + 2 * f + 1] * up;
+          qh[ks][f] = h2(x0, x1);
+          if (kF32) {
+            const float2 back2 = h2_float(qh[ks][f]);
+            ql[ks][f] = h2(x0 - back2.x, x1 - back2.y);
+          } else {
+            ql[ks][f] = 0u;
+          }
+        }
+    }
+    const float cap_in = a.softcap > 0.f ? 1.f / a.softcap : 0.f, cap_out = a.softcap * kLog2e;
+    const float slope2 = a.slopes && row_ok ? a.slopes[head] * kLog2e : 0.f;
+
+    float o[NT][4];
+#pragma unroll
+    for (int e = 0; e < NT; ++e)
+#pragma unroll
+      for (int f = 0; f < 4; ++f) o[e][f] = 0.f;
+    float m_ref = -INFINITY, l_run = 0.f, v_ref = 0.f, v_inv = 0.f;
+
+    // scores of the block's 16 tokens (x: tokens 8 t + 2 c + e) -> probabilities as operands, references moved if needed
+    const auto softmax_block = [&](int blk, float (&sc)[2][4], float k_scale, float v_scale, uint32_t (&ph)[2], uint32_t (&pl)[2]) {
+      const float f = c_row * k_scale;
+      float x[4];
+      float mx = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int tok = blk * kQuantBlock + 8 * t + 2 * c + e;
+          float y = (sc[t][e] + sc[t][2 + e]) * f;
+          if (a.softcap > 0.f) y = cap_out * tanh_f32(y * cap_in);
+          if (a.slopes) y -= slope2 * fabsf((float)(pos - tok));
+          const bool seen = tok < s.len && (tok <= pos || tok < prefix);
+          x[2 * t + e] = seen ? y : -INFINITY;
+          mx = fmaxf(mx, x[2 * t + e]);
+        }
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+      const bool grow = mx > m_ref + kQaGrow, v_grow = v_scale > v_ref;
+      if (__any_sync(0xffffffffu, grow) || v_grow) {
+        float alpha = 1.f;
+        if (grow) {
+          alpha = exp2_approx(m_ref - mx);        // 0 the first time
+          m_ref = mx;
+          l_run *= alpha;
+        }
+        if (v_grow) {
+          // the power of two above the scale
+          const uint32_t e = (__float_as_uint(v_scale) >> 23) + 1;
+          const float old = v_ref;
+          v_ref = __uint_as_float(e << 23);
+          v_inv = __uint_as_float((254 - e) << 23);
+          alpha *= old * v_inv;
+        }
+#pragma unroll
+        for (int e = 0; e < NT; ++e)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[e][k] *= alpha;
+      }
+      const float pv = v_scale * v_inv * kQaPScale;
+      float p[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[i] = x[i] == -INFINITY ? 0.f : exp2_approx(x[i] - m_ref);
+        l_run += p[i];
+        p[i] = x[i] == -INFINITY ? 0.f : p[i] * pv;
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        ph[t] = h2(p[2 * t], p[2 * t + 1]);
+        const float2 w = h2_float(ph[t]);
+        pl[t] = h2(p[2 * t] - w.x, p[2 * t + 1] - w.y);
+      }
+    };
+
+    // ---- the blocks held as codes
+    const int n_codes = max(0, min(nb, n_full - blk0));
+    const int32_t* pages = a.table + (long long)s.slot * g.max_pages;
+    int page_base = (blk0 * kQuantBlock) >> g.page_shift;
+    int page_id = 0;
+    const int page_last = (s.len - 1) >> g.page_shift;
+    const auto load_pages = [&]() {
+      const int p = page_base + lane;
+      int id = p <= page_last ? pages[p] : 0;
+      if (id < 0 || id >= g.n_pages) {
+        report_opt(a.status, ECHOKV_EBADPAGE);
+        id = 0;
+      }
+      page_id = id;
+    };
+    load_pages();
+    const auto issue = [&](int j) {
+      if (j < n_codes) {
+        const int t0 = (blk0 + j) * kQuantBlock, pi = t0 >> g.page_shift;
+        if (pi >= page_base + 32) {
+          page_base = pi;
+          load_pages();
+        }
+        const long long page = __shfl_sync(0xffffffffu, page_id, pi - page_base);
+        const int inside = t0 & (g.page_tokens - 1);
+        const long long ph = page * H + h;
+        const long long off = (ph * g.page_tokens + inside) * D;
+        const uint32_t dst = ring + (j % kQaStages) * qa_stage_bytes(D);
+        const unsigned char* kp = g.codes[0] + off + r * D + 16 * c;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < KC; ++i) cp_async16(dst + (t * KC + i) * 512 + lane * 16, kp + t * 8 * D + i * 64);
+        const unsigned char* vp = g.codes[1] + off + 2 * c * D + NT * r;
+        const uint32_t vdst = dst + kQuantBlock * D;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const unsigned char* src = vp + ((t & 1) + (t >> 1) * 8) * D;
+          if (NT == 16) cp_async16(vdst + t * 512 + lane * 16, src);
+          else cp_async8(vdst + t * 256 + lane * 8, src);
+        }
+        const long long so = ph * (g.page_tokens / kQuantBlock) + inside / kQuantBlock;
+        const uint32_t sdst = dst + 2 * kQuantBlock * D + lane * 8;
+        cp_async4(sdst, g.scales[0] + so);
+        cp_async4(sdst + 4, g.scales[1] + so);
+      }
+      cp_commit();
+    };
+#pragma unroll
+    for (int j = 0; j < kQaStages - 1; ++j) issue(j);
+    for (int j = 0; j < n_codes; ++j) {
+      cp_wait<kQaStages - 2>();
+      issue(j + kQaStages - 1);                   // (into the stage read in the iteration before)
+      const uint32_t src = ring + (j % kQaStages) * qa_stage_bytes(D);
+      float sc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      uint4 kw[2][KC];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < KC; ++i) kw[t][i] = lds16(src + (t * KC + i) * 512 + lane * 16);
+      uint32_t vw[4][NT / 4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        if (NT == 16) {
+          const uint4 w = lds16(src + kQuantBlock * D + t * 512 + lane * 16);
+          vw[t][0] = w.x; vw[t][1] = w.y; vw[t][NT / 4 - 2] = w.z; vw[t][NT / 4 - 1] = w.w;
+        } else {
+          const uint2 w = lds8(src + kQuantBlock * D + t * 256 + lane * 8);
+          vw[t][0] = w.x; vw[t][1] = w.y;
+        }
+      }
+      const float k_scale = lds4(src + 2 * kQuantBlock * D + lane * 8), v_scale = lds4(src + 2 * kQuantBlock * D + lane * 8 + 4);
+#pragma unroll
+      for (int i = 0; i < KC; ++i)
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const uint4& k4 = kw[t][i];
+            const uint32_t word = codes_bias<FMT>(w == 0 ? k4.x : w == 1 ? k4.y : w == 2 ? k4.z : k4.w);
+            const int ks = 4 * i + w;
+            mma_m16n8k16_f16(sc[t], qh[ks][0], ql[ks][0], qh[ks][1], ql[ks][1], codes_pair<FMT, 0>(word), codes_pair<FMT, 1>(word));
+          }
+      uint32_t ph[2], pl[2];
+      softmax_block(blk0 + j, sc, k_scale, v_scale, ph, pl);
+#pragma unroll
+      for (int w = 0; w < NT / 4; ++w) {
+        const uint32_t t0 = codes_bias<FMT>(vw[0][w]), t1 = codes_bias<FMT>(vw[1][w]), t2 = codes_bias<FMT>(vw[2][w]),
+                       t3 = codes_bias<FMT>(vw[3][w]);
+        const uint32_t lo01 = __byte_perm(t0, t1, 0x5140), hi01 = __byte_perm(t0, t1, 0x7362);
+        const uint32_t lo23 = __byte_perm(t2, t3, 0x5140), hi23 = __byte_perm(t2, t3, 0x7362);
+        mma_m16n8k16_f16(o[4 * w], ph[0], pl[0], ph[1], pl[1], codes_pair<FMT, 0>(lo01), codes_pair<FMT, 0>(lo23));
+        mma_m16n8k16_f16(o[4 * w + 1], ph[0], pl[0], ph[1], pl[1], codes_pair<FMT, 1>(lo01), codes_pair<FMT, 1>(lo23));
+        mma_m16n8k16_f16(o[4 * w + 2], ph[0], pl[0], ph[1], pl[1], codes_pair<FMT, 0>(hi01), codes_pair<FMT, 0>(hi23));
+        mma_m16n8k16_f16(o[4 * w + 3], ph[0], pl[0], ph[1], pl[1], codes_pair<FMT, 1>(hi01), codes_pair<FMT, 1>(hi23));
+      }
+    }
+    cp_wait<0>();
+
+    // ---- the open block, in the storage type
+    if (n_codes < nb) {
+      const int n_tail = s.len - n_full * kQuantBlock;
+      const T* kt = static_cast<const T*>(g.tail[0]) + ((long long)s.slot * H + h) * kQuantBlock * D;
+      const T* vt = static_cast<const T*>(g.tail[1]) + ((long long)s.slot * H + h) * kQuantBlock * D;
+      // magnitudes compare as integers, infinities and NaN above everything finite; a block with one of those acts as a
+      // block of codes does: scale NaN, values 0 (so that a query that sees none of it is left alone)
+      uint32_t k_top = 0, v_top = 0;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        if (r + 8 * t < n_tail)
+          for (int i = 0; i < KC; ++i)
+            for (int e = 0; e < 16; e += Vec16<T>::N) {
+              float v[Vec16<T>::N];
+              Vec16<T>::load(kt + (r + 8 * t) * D + 16 * (c + 4 * i) + e, v);
+#pragma unroll
+              for (int f = 0; f < Vec16<T>::N; ++f) k_top = max(k_top, __float_as_uint(v[f]) & 0x7fffffffu);
+              Vec16<T>::load(vt + (r + 8 * t) * D + 16 * (c + 4 * i) + e, v);
+#pragma unroll
+              for (int f = 0; f < Vec16<T>::N; ++f) v_top = max(v_top, __float_as_uint(v[f]) & 0x7fffffffu);
+            }
+      k_top = __reduce_max_sync(0xffffffffu, k_top);
+      v_top = __reduce_max_sync(0xffffffffu, v_top);
+      const bool k_ok = k_top < 0x7f800000u, v_ok = v_top < 0x7f800000u;
+      float k_back, v_back;
+      const float k_up = scale_up_to_half(__uint_as_float(k_top), &k_back), v_up = scale_up_to_half(__uint_as_float(v_top), &v_back);
+      if (!k_ok) k_back = __uint_as_float(0x7fc00000u);
+      if (!v_ok) v_back = __uint_as_float(0x7fc00000u);
+      float sc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          float v[4];
+          const T* p = kt + (r + 8 * t) * D + 16 * (c + 4 * (ks >> 2)) + 4 * (ks & 3);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = k_ok && r + 8 * t < n_tail ? load_elem(p + e) * k_up : 0.f;
+          const uint32_t b0 = h2(v[0], v[1]), b1 = h2(v[2], v[3]);
+          mma_m16n8k16_f16(sc[t], qh[ks][0], ql[ks][0], qh[ks][1], ql[ks][1], b0, b1);
+          if (kF32) {
+            const float2 w0 = h2_float(b0), w1 = h2_float(b1);
+            mma_m16n8k16_f16(sc[t], qh[ks][0], ql[ks][0], qh[ks][1], ql[ks][1], h2(v[0] - w0.x, v[1] - w0.y), h2(v[2] - w1.x, v[3] - w1.y));
+          }
+        }
+      uint32_t ph[2], pl[2];
+      softmax_block(n_full, sc, k_back, v_back, ph, pl);
+#pragma unroll
+      for (int e = 0; e < NT; ++e) {
+        float v[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int tok = 2 * c + (t & 1) + (t >> 1) * 8;
+          v[t] = v_ok && tok < n_tail ? load_elem(vt + tok * D + NT * r + e) * v_up : 0.f;
+        }
+        const uint32_t b0 = h2(v[0], v[1]), b1 = h2(v[2], v[3]);
+        mma_m16n8k16_f16(o[e], ph[0], pl[0], ph[1], pl[1], b0, b1);
+        if (kF32) {
+          const float2 w0 = h2_float(b0), w1 = h2_float(b1);
+          mma_m16n8k16_f16(o[e], ph[0], pl[0], ph[1], pl[1], h2(v[0] - w0.x, v[1] - w0.y), h2(v[2] - w1.x, v[3] - w1.y));
+        }
+      }
+    }
+
+    // ---- the segment's result
+    l_run += __shfl_xor_sync(0xffffffffu, l_run, 1);
+    l_run += __shfl_xor_sync(0xffffffffu, l_run, 2);
+    const float o_scale = v_ref * (1.f / kQaPScale);
+    const bool starts = u == item, ends = seg_end == item_end;
+    if (starts && ends) {
+      if (row_ok) {
+        const float inv = l_run == 0.f ? 0.f : o_scale / l_run;
+        T* dst = static_cast<T*>(a.out) + ((long long)(s.first + qi) * a.n_q_heads + head) * D + 2 * c * NT;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int e = 0; e < NT; ++e) dst[k * NT + e] = from_f32<T>((o[e][k] + o[e][2 + k]) * inv);
+      }
+    } else {
+      const int at = 2 * warp + (starts ? 1 : 0);
+      if (lane == 0) {
+        QaSeg& q = sm.seg[at];
+        q.item = item; q.item_end = item_end;
+        q.b = b; q.tile = tile; q.h = h;
+        q.starts = starts; q.ends = ends;
+        q.valid = 1;
+      }
+      if (c == 0) {
+        sm.m[at][r] = m_ref;
+        sm.l[at][r] = l_run;
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < NT; ++e) sm.o[at][r][(2 * c + k) * NT + e] = (o[e][k] + o[e][2 + k]) * o_scale;
+    }
+    u = seg_end;
+  }
+
+  // ---- segments of one item side by side in this CTA: combine them; what is still cut goes to the workspace
+  __syncthreads();
+  const QaWork<D> ws(a.ws);
+  bool desc_written = false;
+  constexpr int E = D / 32;
+  const int row = warp;
+  for (int i = 0; i < 2 * kQaWarps;) {
+    if (!sm.seg[i].valid) { ++i; continue; }
+    int j = i + 1, last = i;
+    while (j < 2 * kQaWarps && (!sm.seg[j].valid || sm.seg[j].item == sm.seg[i].item)) {
+      if (sm.seg[j].valid) last = j;
+      ++j;
+    }
+    const QaSeg first = sm.seg[i];
+    const bool ends = sm.seg[last].ends;
+    float m = -INFINITY;
+    for (int k = i; k <= last; ++k)
+      if (sm.seg[k].valid) m = fmaxf(m, sm.m[k][row]);
+    float l = 0.f, acc[E] = {};
+    for (int k = i; k <= last; ++k)
+      if (sm.seg[k].valid) {
+        const float w = sm.m[k][row] == -INFINITY ? (sm.l[k][row] == 0.f ? 0.f : 1.f) : exp2_approx(sm.m[k][row] - m);
+        l += w * sm.l[k][row];
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] += w * sm.o[k][row][lane * E + e];
+      }
+    if (first.starts && ends) {
+      const QuantSeq s = quant_seq(a, first.b);
+      const int qrow = first.tile * kQaRows + row;
+      if (qrow < s.n * a.group) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        T* dst = static_cast<T*>(a.out) +
+                 ((long long)(s.first + (qrow >> a.group_shift)) * a.n_q_heads + first.h * a.group + (qrow & (a.group - 1))) * D + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) dst[e] = from_f32<T>(acc[e] * inv);
+      }
+    } else {
+      const long long p = ((long long)blockIdx.x * 2 + (first.starts ? 1 : 0)) * kQaRows + row;
+      if (lane == 0) ws.ml[p] = make_float2(m, l);
+#pragma unroll
+      for (int e = 0; e < E; ++e) ws.o[p * D + lane * E + e] = acc[e];
+      if (first.starts) {
+        if (tid == 0) {
+          QaDesc d;
+          d.n_parts = (int)((first.item_end - 1) / share - blockIdx.x) + 1;
+          d.b = first.b; d.tile = first.tile; d.h = first.h;
+          ws.desc[blockIdx.x] = d;
+        }
+        desc_written = true;
+      }
+    }
+    i = j;
+  }
+  if (tid == 0 && !desc_written) ws.desc[blockIdx.x] = QaDesc{0, 0, 0, 0};
+}
+
+// Joins the items that shares cut: block g the one that begins in CTA g and goes on in the next ones.  Also zeroes the rows of unusable sequences.
+template <typename T, int D>
+__global__ void __launch_bounds__(kQaThreads) quant_merge_kernel(const __grid_constant__ QuantAttnArgs a) {
+  constexpr int E = D / 32;
+  const int tid = threadIdx.x, lane = tid & 31, row = tid >> 5;
+  const QaWork<D> ws(a.ws);
+  for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+    const QuantSeq s = quant_seq(a, b);
+    if (s.error && s.n > 0) {
+      T* dst = static_cast<T*>(a.out) + (long long)s.first * a.n_q_heads * D;
+      const long long n = (long long)s.n * a.n_q_heads * D;
+      for (long long i = tid; i < n; i += kQaThreads) dst[i] = from_f32<T>(0.f);
+    }
+  }
+  const QaDesc d = ws.desc[blockIdx.x];
+  if (d.n_parts == 0) return;
+  const auto part = [&](int p) -> long long { return ((long long)(blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * kQaRows + row; };
+  float m = -INFINITY;
+  for (int p = lane; p < d.n_parts; p += 32) m = fmaxf(m, ws.ml[part(p)].x);
+  m = warp_max(m);
+  float l = 0.f, acc[E] = {};
+#pragma unroll 4
+  for (int p = 0; p < d.n_parts; ++p) {
+    const float2 ml = ws.ml[part(p)];
+    const float w = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : exp2_approx(ml.x - m);
+    l += w * ml.y;
+    const float* o = ws.o + part(p) * D + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] += w * o[e];
+  }
+  const QuantSeq s = quant_seq(a, d.b);
+  const int qrow = d.tile * kQaRows + row;
+  if (qrow >= s.n * a.group) return;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* dst = static_cast<T*>(a.out) +
+           ((long long)(s.first + (qrow >> a.group_shift)) * a.n_q_heads + d.h * a.group + (qrow & (a.group - 1))) * D + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) dst[e] = from_f32<T>(acc[e] * inv);
+}
+
+template <typename T, int FMT, int D>
+cudaError_t launch(const QuantAttnArgs& a, int sm_count, cudaStream_t stream) {
+  constexpr size_t smem = qa_ring_bytes<D>() + sizeof(QaSmem<D>);
+  static_assert(smem <= 227 * 1024, "shared memory of one CTA");
+  cudaError_t e = cudaFuncSetAttribute(quant_attn_kernel<T, FMT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  const int grid = sm_count < kQaMaxCtas ? sm_count : kQaMaxCtas;
+  quant_attn_kernel<T, FMT, D><<<grid, kQaThreads, smem, stream>>>(a);
+  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  quant_merge_kernel<T, D><<<grid, kQaThreads, 0, stream>>>(a);
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t launch_t(const QuantAttnArgs& a, int sm_count, cudaStream_t stream) {
+  const bool i8 = a.format == ECHOKV_INT8;
+  if (a.g.head_dim == 128) return i8 ? launch<T, ECHOKV_INT8, 128>(a, sm_count, stream) : launch<T, ECHOKV_E4M3, 128>(a, sm_count, stream);
+  return i8 ? launch<T, ECHOKV_INT8, 64>(a, sm_count, stream) : launch<T, ECHOKV_E4M3, 64>(a, sm_count, stream);
+}
+
+}  // namespace
+
+uint64_t quant_attn_workspace_bytes(int head_dim) {
+  const uint64_t n = (uint64_t)kQaMaxCtas * (sizeof(QaDesc) + 2ull * kQaRows * (sizeof(float2) + (uint64_t)head_dim * sizeof(float)));
+  return (n + 255) / 256 * 256;
+}
+
+cudaError_t launch_quant_attn(const QuantAttnArgs& a, int sm_count, cudaStream_t stream) {
+  return a.dtype == ECHOKV_BF16 ? launch_t<__nv_bfloat16>(a, sm_count, stream) : launch_t<float>(a, sm_count, stream);
+}
+
+}  // namespace echokv

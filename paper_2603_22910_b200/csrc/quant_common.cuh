@@ -1,0 +1,119 @@
+// What the kernels over the 8-bit cache share: the sequences of a call, codes to fp16, the score transforms.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "ptx_sm100.cuh"
+#include "serving.h"
+
+namespace echokv {
+
+// One sequence of a call.  error != 0: nothing is attended; rows [first, first + n) of out are zeroed where n > 0.
+struct QuantSeq {
+  int slot, len, first, n, error;
+};
+
+__device__ __forceinline__ QuantSeq quant_seq(const QuantAttnArgs& a, int b) {
+  QuantSeq s;
+  s.first = b;
+  s.n = 1;
+  s.error = 0;
+  if (a.cu != nullptr) {
+    const int c0 = a.cu[b], c1 = a.cu[b + 1];
+    if (c0 < 0 || c1 < c0 || c1 > a.n_tokens) {
+      s.error = ECHOKV_EBADLENGTH;
+      s.first = 0;
+      s.n = 0;
+    } else {
+      s.first = c0;
+      s.n = c1 - c0;
+    }
+  }
+  s.slot = a.slots ? a.slots[b] : b;
+  s.len = a.lens[b];
+  if (s.n > 0) {
+    if (s.slot < 0 || s.slot >= a.g.max_batch) s.error = ECHOKV_EBADPAGE;
+    else if (s.len < s.n || s.len > a.g.max_pages * a.g.page_tokens || s.n > a.max_new) s.error = ECHOKV_EBADLENGTH;
+  }
+  return s;
+}
+
+__device__ __forceinline__ bool chunk_sequence(const QuantAttnArgs& a, const QuantSeq& s) {
+  return a.chunk_rows > 0 && s.n * a.group >= a.chunk_rows;
+}
+
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// tanh to ~3e-7 of its value: away from 0 by 1 - 2 / (e^{2y} + 1), near 0 (where that form cancels) by the Taylor series
+// y - y^3/3 + 2 y^5/15 - 17 y^7/315 + 62 y^9/2835, whose next term is 1.5e-8 of y at 0.25
+__device__ __forceinline__ float tanh_f32(float y) {
+  const float y2 = y * y;
+  float s = 62.f / 2835.f;
+  s = fmaf(s, y2, -17.f / 315.f);
+  s = fmaf(s, y2, 2.f / 15.f);
+  s = fmaf(s, y2, -1.f / 3.f);
+  s = fmaf(s * y2, y, y);
+  const float e = exp2_approx(fabsf(y) * (2.f * kLog2e));      // +inf for large |y|: the quotient is 0
+  const float t = copysignf(fmaf(-2.f, rcp_approx(e + 1.f), 1.f), y);
+  return y2 < 0.0625f ? s : t;
+}
+
+// fp16 pair
+__device__ __forceinline__ uint32_t h2(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float2 h2_float(uint32_t w) {
+  const __half2 v = *reinterpret_cast<const __half2*>(&w);
+  return __half22float2(v);
+}
+
+// Codes -> fp16, exactly.  int8: 1024 + (c + 128) has the byte c ^ 0x80 as the low bits of its fp16 pattern 0x6400 | u; subtracting
+// 1152 leaves c.  e4m3: the conversion instruction.
+template <int FMT>
+__device__ __forceinline__ uint32_t codes_bias(uint32_t w) { return FMT == ECHOKV_INT8 ? w ^ 0x80808080u : w; }
+// bytes (lo, hi) = (0, 1) or (2, 3) of a word that went through codes_bias
+template <int FMT, int HALF>
+__device__ __forceinline__ uint32_t codes_pair(uint32_t w) {
+  uint32_t r;
+  if (FMT == ECHOKV_INT8) {
+    const uint32_t x = __byte_perm(w, 0x64646464u, HALF ? 0x4342 : 0x4140);
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(0x64806480u));
+  } else {
+    const uint16_t x = (uint16_t)(HALF ? w >> 16 : w & 0xffffu);
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(x));
+  }
+  return r;
+}
+
+__device__ __forceinline__ void mma_m16n8k16_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                                 uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Operands in the storage type are scaled by a power of two that takes their largest magnitude m to [2^14, 2^15): a bf16
+// then is an fp16 exactly down to 2^-31 of the largest.  Returns that power for m in fp32's normal range (else 1: zero, or an
+// infinity or NaN that the products carry on) and its inverse.
+__device__ __forceinline__ float scale_up_to_half(float m, float* inverse) {
+  const int e = (int)(__float_as_uint(m) >> 23) & 0xff;
+  int k = 127 + 14 - e;                        // 2^k * m in [2^14, 2^15)
+  if (e == 0 || e == 255) k = 0;
+  k = k > 126 ? 126 : k < -126 ? -126 : k;
+  *inverse = __uint_as_float((uint32_t)(127 - k) << 23);
+  return __uint_as_float((uint32_t)(127 + k) << 23);
+}
+
+}  // namespace echokv

@@ -1,0 +1,101 @@
+// Host-side launchers of the serving-step kernels (internal to the library): plan, rotation, 8-bit append, 8-bit attention.
+#pragma once
+
+#include "common.cuh"
+
+namespace echokv {
+
+constexpr int kPlanMaxBatch = 8192;                 // sequences of one plan: 20 bytes of shared memory each
+constexpr int kQuantBlock = ECHOKV_QUANT_BLOCK_TOKENS;
+constexpr int kMaxAxes = 4;
+
+__device__ __forceinline__ void report_opt(int32_t* status, int code) {
+  if (status != nullptr) atomicCAS(status, 0, code);
+}
+
+struct PlanArgs {
+  int32_t* table;
+  const int32_t* slots;        // [B] or null
+  const int32_t* lens;
+  const int32_t* new_lens;
+  const int32_t* free_pages;
+  const int32_t* free_count;
+  int B, n_tokens;
+  int page_tokens, page_shift, max_pages, max_batch;
+  long long n_pages;
+  echokv_step_plan out;
+  int32_t* status;
+};
+cudaError_t launch_plan(const PlanArgs& a, cudaStream_t stream);
+
+struct ReleaseArgs {
+  const int32_t* table;
+  const int32_t* slots;
+  const int32_t* lens;
+  int32_t* free_pages;
+  int32_t* free_count;
+  int B, page_tokens, page_shift, max_pages, max_batch;
+  long long n_pages;
+  int32_t* status;
+};
+cudaError_t launch_release(const ReleaseArgs& a, cudaStream_t stream);
+
+struct RotateArgs {
+  const void* in[2];           // q, k (null: nothing to do)
+  void* out[2];
+  long long in_stride[2], out_stride[2];   // elements
+  int heads[2];
+  int head_dim, rot_dim, n_tokens, dtype;
+  bool in_place[2];
+  const int32_t* pos;          // [n_axes][n_tokens]
+  float sign;
+  unsigned char axis[64];      // axis of every frequency index
+  double turns[64];            // theta^(-2 j / rot) / (2 pi)
+};
+cudaError_t launch_rotate(const RotateArgs& a, int sm_count, cudaStream_t stream);
+
+// Geometry of one layer's 8-bit cache, by value into kernels.
+struct QuantGeom {
+  unsigned char* codes[2];     // K, V: [n_pages][H][P][d]
+  float* scales[2];            // [n_pages][H][P / 16]
+  void* tail[2];               // [max_batch][H][16][d]
+  int n_kv_heads, head_dim, page_tokens, page_shift, max_pages, max_batch;
+  long long n_pages;
+};
+
+struct QuantAppendArgs {
+  QuantGeom g;
+  const void* x[2];            // new K, V rows
+  long long stride[2];         // elements
+  const int64_t* slot_map;
+  const int32_t* token_seqs;
+  const int32_t* cu;
+  const int32_t* slots;        // or null
+  int B, n_tokens, dtype, format;
+  int32_t* status;
+};
+cudaError_t launch_quant_append(const QuantAppendArgs& a, int sm_count, cudaStream_t stream);
+
+struct QuantAttnArgs {
+  QuantGeom g;
+  const void* q;
+  long long q_stride;          // elements
+  void* out;
+  const int32_t* table;
+  const int32_t* slots;        // or null
+  const int32_t* lens;
+  const int32_t* cu;           // or null: one token per sequence
+  const float* slopes;         // or null
+  const int32_t* prefix;       // or null
+  int B, n_tokens, max_new;
+  int n_q_heads, group, group_shift, dtype, format;
+  int chunk_rows;              // sequences with at least this many query rows per KV head (new tokens x group) are the
+                               // chunk kernel's; 0: there is none
+  float scale, softcap;
+  unsigned char* ws;
+  int32_t* status;
+};
+uint64_t quant_attn_workspace_bytes(int head_dim);
+cudaError_t launch_quant_attn(const QuantAttnArgs& a, int sm_count, cudaStream_t stream);
+
+}  // namespace echokv
