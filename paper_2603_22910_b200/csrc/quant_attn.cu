@@ -12,26 +12,33 @@
 //            items; their partial results (running maximum, sum, output) are combined inside the CTA through shared
 //            memory and between CTAs by a second small kernel.
 //   copies   Each lane copies, by 16-byte cp.async into a ring of its own, exactly the bytes that it will use as matrix operands:
-//            no barrier and no bank conflict, and 16 KB in flight per warp.
-//   products mma.sync m16n8k16 in fp16 with the 8 query rows on the upper half of the M rows; rows 8..15 carry the low-order
-//            halves (q = q_hi + q_lo for fp32 queries, P = P_hi + P_lo), so scores and outputs keep 22 bits at no cost.  Codes
-//            convert to fp16 exactly.  (The tile has few rows: tcgen05's 128 would be padding, and the tensor pipe is a
-//            third busy as it is.)
-//   scales   The K scale multiplies the score, the V scale the probability.  fp16's range is kept by running references, powers of
-//            two: queries per row, V scales per warp; like the running maximum they move only when they must (a factor
-//            of 2^8 of head-room), one vote per block.
+//            no barrier and no bank conflict.
+//   products mma.sync m16n8k16 in fp16 with the tokens (then the head's features) on the M rows and the 8 query rows on N:
+//            S^T = K q^T, O^T = V^T P^T, 8 instructions each per block and no padding of the queries to 16 rows.  S^T
+//            becomes the operand P^T by one 8 x 8 transposition per 8 tokens in registers.  Codes convert to fp16 exactly; fp32
+//            queries, and the probabilities beside them, take a second product with their low-order halves (22 bits).
+//            (tcgen05's 128 rows would be padding here, and the tensor pipe is not what bounds.)
+//   softmax  The running maximum is a reference that moves only when a score is 2^8 above it: the common path compares and votes,
+//            without a reduction over the tokens.
+//   scales   The K scale multiplies the score, the V scale the probability.  fp16's range is kept by references that are powers of
+//            two: one per query row, one per warp for the V scales, which moves with the maximum's.
 //   tail     The open block is in the storage type: bf16 converts to fp16 exactly around its own power of two, fp32
-//            as a pair of fp16.
+//            as a pair of fp16.  It is attended first, while the first copies are on their way.
 #include "quant_common.cuh"
 
 namespace echokv {
 
 namespace {
 
-constexpr int kQaWarps = 8;
+#ifndef QW
+#define QW 12
+#define QS 3
+#endif
+constexpr int kQaWarps = QW;
 constexpr int kQaThreads = kQaWarps * 32;
 constexpr int kQaRows = 8;                        // query rows per tile
-constexpr int kQaStages = 4;
+constexpr int kQaStages = QS;
+constexpr int kQaMergeThreads = kQaRows * 32;
 constexpr int kQaMaxCtas = 512;
 constexpr int kQaMinShare = kQaWarps;             // units per CTA at least: one block for every warp
 constexpr float kQaGrow = 8.f;                    // the references move when a score is 2^8 above them
@@ -53,9 +60,11 @@ struct QaSeg {
 
 template <int D>
 struct QaSmem {
+  // a warp's segment that goes on from the warp before it, and (over the warp's ring, once that is at rest) the one
+  // that goes on in the next warp
+  float o_first[kQaWarps][kQaRows][D];
   QaSeg seg[2 * kQaWarps];
   float m[2 * kQaWarps][kQaRows], l[2 * kQaWarps][kQaRows];
-  float o[2 * kQaWarps][kQaRows][D];
   unsigned long long pre[kQaThreads + 1];
   unsigned long long warp_sums[kQaWarps];
 };
@@ -111,8 +120,12 @@ __device__ __forceinline__ unsigned long long units_of(const QuantAttnArgs& a, c
   return (unsigned long long)row_tiles(a, s) * a.g.n_kv_heads * ((s.len + kQuantBlock - 1) / kQuantBlock);
 }
 
-template <typename T>
-__device__ __forceinline__ float load_elem(const T* p) { return to_f32(*p); }
+// transposes an 8 x 8 matrix of 16-bit elements held as matrix fragments
+__device__ __forceinline__ uint32_t movm(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
 
 template <typename T>
 __device__ __forceinline__ T from_f32(float x);
@@ -125,7 +138,8 @@ template <typename T, int FMT, int D>
 __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_constant__ QuantAttnArgs a) {
   constexpr int KC = D / 64;                      // 16-byte pieces of a key row per lane
   constexpr int KS = D / 16;                      // k-steps of q . k
-  constexpr int NT = D / 8;                       // output tiles; V bytes per token and lane
+  constexpr int NT = D / 8;                       // V bytes per token and lane (features NT r .. NT r + NT - 1)
+  constexpr int MT = D / 16;                      // output tiles of 16 features: features NT r + 2 j and NT r + 2 j + 1
   constexpr bool kF32 = sizeof(T) == 4;
   extern __shared__ __align__(128) unsigned char qa_raw[];
   QaSmem<D>& sm = *reinterpret_cast<QaSmem<D>*>(qa_raw + qa_ring_bytes<D>());
@@ -133,6 +147,10 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
   const uint32_t ring = smem_u32(qa_raw) + warp * kQaStages * qa_stage_bytes(D);
   const QuantGeom& g = a.g;
   const int H = g.n_kv_heads;
+  // output rows [8][D] of segment `at`
+  const auto seg_rows = [&](int at) -> float* {
+    return at & 1 ? reinterpret_cast<float*>(qa_raw + (size_t)(at >> 1) * kQaStages * qa_stage_bytes(D)) : &sm.o_first[at >> 1][0][0];
+  };
 
   // ---- the units of the call, and this CTA's and warp's share of them
   const int per = (a.B + kQaThreads - 1) / kQaThreads;
@@ -197,23 +215,22 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     const int nb = (int)(seg_end - u);
     const int n_full = s.len / kQuantBlock;       // blocks held as codes; block n_full is the open one
 
-    // ---- this lane's query row
-    const int qrow = tile * kQaRows + r;
-    const bool row_ok = qrow < s.n * a.group;
-    const int qi = row_ok ? qrow >> a.group_shift : 0, head = h * a.group + (qrow & (a.group - 1));
-    const int pos = s.len - s.n + qi;
-    const int prefix = a.prefix ? a.prefix[b] : 0;
-    uint32_t qh[KS][2], ql[KS][2];
-    float c_row;
+    // ---- the query rows: this lane loads a quarter of row r as operand; its scores are of rows 2 c and 2 c + 1
+    const int n_rows = s.n * a.group;
+    uint32_t qh[KS][2], ql[kF32 ? KS : 1][2];
+    float c_row[2];
     {
-      const T* qp = static_cast<const T*>(a.q) + (long long)(s.first + qi) * a.q_stride + (long long)head * D;
+      const int qrow = tile * kQaRows + r;
+      const bool ok = qrow < n_rows;
+      const T* qp = static_cast<const T*>(a.q) + (long long)(s.first + (ok ? qrow >> a.group_shift : 0)) * a.q_stride +
+                    (long long)(h * a.group + (qrow & (a.group - 1))) * D;
       float top = 0.f;
       float v[KC * 16];
 #pragma unroll
       for (int i = 0; i < KC; ++i)
 #pragma unroll
         for (int e = 0; e < 16; e += Vec16<T>::N)
-          if (row_ok) {
+          if (ok) {
             Vec16<T>::load(qp + 16 * (c + 4 * i) + e, v + 16 * i + e);
           } else {
 #pragma unroll
@@ -225,7 +242,9 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       float back;
       const float up = scale_up_to_half(top, &back);
-      c_row = back * a.scale * (a.softcap > 0.f ? 1.f : kLog2e);
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        c_row[e] = __shfl_sync(0xffffffffu, back, 4 * (2 * c + e)) * a.scale * (a.softcap > 0.f ? 1.f : kLog2e);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
@@ -233,80 +252,99 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
           const float x0 = v[4 * ks + 2 * f] * up, x1 = v[4 * ks + 2 * f + 1] * up;
           qh[ks][f] = h2(x0, x1);
           if (kF32) {
-            const float2 back2 = h2_float(qh[ks][f]);
-            ql[ks][f] = h2(x0 - back2.x, x1 - back2.y);
-          } else {
-            ql[ks][f] = 0u;
+            const float2 w = h2_float(qh[ks][f]);
+            ql[ks][f] = h2(x0 - w.x, x1 - w.y);
           }
         }
     }
     const float cap_in = a.softcap > 0.f ? 1.f / a.softcap : 0.f, cap_out = a.softcap * kLog2e;
-    const float slope2 = a.slopes && row_ok ? a.slopes[head] * kLog2e : 0.f;
-
-    float o[NT][4];
+    const int prefix = a.prefix ? a.prefix[b] : 0;
+    int pos[2];
+    float slope2[2];
 #pragma unroll
-    for (int e = 0; e < NT; ++e)
-#pragma unroll
-      for (int f = 0; f < 4; ++f) o[e][f] = 0.f;
-    float m_ref = -INFINITY, l_run = 0.f, v_ref = 0.f, v_inv = 0.f;
+    for (int e = 0; e < 2; ++e) {
+      const int qrow = tile * kQaRows + 2 * c + e;
+      pos[e] = s.len - s.n + (qrow < n_rows ? qrow >> a.group_shift : 0);
+      slope2[e] = a.slopes ? a.slopes[h * a.group + (qrow & (a.group - 1))] * kLog2e : 0.f;
+    }
 
-    // scores of the block's 16 tokens (x: tokens 8 t + 2 c + e) -> probabilities as operands, references moved if needed
-    const auto softmax_block = [&](int blk, float (&sc)[2][4], float k_scale, float v_scale, uint32_t (&ph)[2], uint32_t (&pl)[2]) {
-      const float f = c_row * k_scale;
+    float o[MT][4];                               // rows: feature NT r + 2 j (0, 1) and + 1 (2, 3); columns: query rows 2 c, 2 c + 1
+#pragma unroll
+    for (int j = 0; j < MT; ++j)
+#pragma unroll
+      for (int f = 0; f < 4; ++f) o[j][f] = 0.f;
+    float m_ref[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f}, v_ref = 0.f, v_inv = 0.f;
+
+    // scores of the block's tokens (sc[2 t + e]: token r + 8 t, query row 2 c + e) -> probabilities as operands
+    // (ph[t]: query row r, tokens 8 t + 2 c, + 1), references moved if needed
+    const auto softmax_block = [&](int blk, const float (&sc)[4], float k_scale, float v_scale, uint32_t (&ph)[2], uint32_t (&pl)[2]) {
       float x[4];
-      float mx = -INFINITY;
+      bool above = v_scale > v_ref;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const int tok = blk * kQuantBlock + 8 * t + 2 * c + e;
-          float y = (sc[t][e] + sc[t][2 + e]) * f;
+          const int tok = blk * kQuantBlock + 8 * t + r;
+          float y = sc[2 * t + e] * (c_row[e] * k_scale);
           if (a.softcap > 0.f) y = cap_out * tanh_f32(y * cap_in);
-          if (a.slopes) y -= slope2 * fabsf((float)(pos - tok));
-          const bool seen = tok < s.len && (tok <= pos || tok < prefix);
+          if (a.slopes) y -= slope2[e] * fabsf((float)(pos[e] - tok));
+          const bool seen = tok < s.len && (tok <= pos[e] || tok < prefix);
           x[2 * t + e] = seen ? y : -INFINITY;
-          mx = fmaxf(mx, x[2 * t + e]);
+          above |= x[2 * t + e] > m_ref[e] + kQaGrow;
         }
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-      const bool grow = mx > m_ref + kQaGrow, v_grow = v_scale > v_ref;
-      if (__any_sync(0xffffffffu, grow) || v_grow) {
-        float alpha = 1.f;
-        if (grow) {
-          alpha = exp2_approx(m_ref - mx);        // 0 the first time
-          m_ref = mx;
-          l_run *= alpha;
+      if (__any_sync(0xffffffffu, above)) {
+        float alpha[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float mx = fmaxf(x[e], x[2 + e]);
+#pragma unroll
+          for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+          alpha[e] = 1.f;
+          if (mx > m_ref[e]) {
+            alpha[e] = exp2_approx(m_ref[e] - mx);      // 0 the first time
+            m_ref[e] = mx;
+            l_run[e] *= alpha[e];
+          }
         }
-        if (v_grow) {
+        if (v_scale > v_ref) {
           // the power of two above the scale
           const uint32_t e = (__float_as_uint(v_scale) >> 23) + 1;
           const float old = v_ref;
           v_ref = __uint_as_float(e << 23);
           v_inv = __uint_as_float((254 - e) << 23);
-          alpha *= old * v_inv;
+          alpha[0] *= old * v_inv;
+          alpha[1] *= old * v_inv;
         }
 #pragma unroll
-        for (int e = 0; e < NT; ++e)
+        for (int j = 0; j < MT; ++j)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) o[e][k] *= alpha;
+          for (int f = 0; f < 4; ++f) o[j][f] *= alpha[f & 1];
       }
       const float pv = v_scale * v_inv * kQaPScale;
       float p[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        p[i] = x[i] == -INFINITY ? 0.f : exp2_approx(x[i] - m_ref);
-        l_run += p[i];
-        p[i] = x[i] == -INFINITY ? 0.f : p[i] * pv;
+        const bool seen = x[i] != -INFINITY;            // (masked, or a score of -inf: no part of the sums either way)
+        p[i] = seen ? exp2_approx(x[i] - m_ref[i & 1]) : 0.f;
+        l_run[i & 1] += p[i];
+        p[i] = seen ? p[i] * pv : 0.f;
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        ph[t] = h2(p[2 * t], p[2 * t + 1]);
-        const float2 w = h2_float(ph[t]);
-        pl[t] = h2(p[2 * t] - w.x, p[2 * t + 1] - w.y);
+        const uint32_t w = h2(p[2 * t], p[2 * t + 1]);
+        ph[t] = movm(w);
+        if (kF32) {
+          const float2 f = h2_float(w);
+          pl[t] = movm(h2(p[2 * t] - f.x, p[2 * t + 1] - f.y));
+        }
       }
     };
+    const auto mma_pv = [&](float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint32_t (&ph)[2], const uint32_t (&pl)[2]) {
+      mma_m16n8k16_f16(d, a0, a1, a2, a3, ph[0], ph[1]);
+      if (kF32) mma_m16n8k16_f16(d, a0, a1, a2, a3, pl[0], pl[1]);
+    };
 
-    // ---- the blocks held as codes
+    // ---- the blocks held as codes: copies
     const int n_codes = max(0, min(nb, n_full - blk0));
     const int32_t* pages = a.table + (long long)s.slot * g.max_pages;
     int page_base = (blk0 * kQuantBlock) >> g.page_shift;
@@ -356,16 +394,130 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     };
 #pragma unroll
     for (int j = 0; j < kQaStages - 1; ++j) issue(j);
+
+    // ---- the open block, in the storage type
+    if (n_codes < nb) {
+      const int n_tail = s.len - n_full * kQuantBlock;
+      const long long off = ((long long)s.slot * H + h) * kQuantBlock * D;
+      // Magnitudes compare as integers, infinities and NaN above everything finite; a block with one of those acts as a
+      // block of codes does: scale NaN, values 0 (so that a query that sees none of it is left alone).
+      const auto power = [&](uint32_t top, float* back, bool* ok) {
+        top = __reduce_max_sync(0xffffffffu, top);
+        *ok = top < 0x7f800000u;
+        const float up = scale_up_to_half(__uint_as_float(top), back);
+        if (!*ok) *back = __uint_as_float(0x7fc00000u);
+        return up;
+      };
+      float sc[4] = {0.f, 0.f, 0.f, 0.f};
+      float k_back, v_back;
+      {
+        const T* kt = static_cast<const T*>(g.tail[0]) + off;
+        float v[2][KC * 16];
+        uint32_t top = 0;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < KC; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; e += Vec16<T>::N) {
+              if (r + 8 * t < n_tail) {
+                Vec16<T>::load(kt + (r + 8 * t) * D + 16 * (c + 4 * i) + e, v[t] + 16 * i + e);
+              } else {
+#pragma unroll
+                for (int f = 0; f < Vec16<T>::N; ++f) v[t][16 * i + e + f] = 0.f;
+              }
+            }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < KC * 16; ++e) top = max(top, __float_as_uint(v[t][e]) & 0x7fffffffu);
+        bool ok;
+        const float up = power(top, &k_back, &ok);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          uint32_t hi[4], lo[4];                       // tokens r, r + 8; elements 0, 1 and 2, 3
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+              const float x0 = ok ? v[t][4 * ks + 2 * f] * up : 0.f, x1 = ok ? v[t][4 * ks + 2 * f + 1] * up : 0.f;
+              hi[2 * f + t] = h2(x0, x1);
+              if (kF32) {
+                const float2 w = h2_float(hi[2 * f + t]);
+                lo[2 * f + t] = h2(x0 - w.x, x1 - w.y);
+              }
+            }
+          mma_m16n8k16_f16(sc, hi[0], hi[1], hi[2], hi[3], qh[ks][0], qh[ks][1]);
+          if (kF32) {
+            mma_m16n8k16_f16(sc, hi[0], hi[1], hi[2], hi[3], ql[ks][0], ql[ks][1]);
+            mma_m16n8k16_f16(sc, lo[0], lo[1], lo[2], lo[3], qh[ks][0], qh[ks][1]);
+          }
+        }
+      }
+      {
+        const T* vt = static_cast<const T*>(g.tail[1]) + off;
+        float v[4][NT];
+        uint32_t top = 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int tok = 2 * c + (t & 1) + (t >> 1) * 8;
+#pragma unroll
+          for (int e = 0; e < NT; e += Vec16<T>::N) {
+            if (tok < n_tail) {
+              Vec16<T>::load(vt + tok * D + NT * r + e, v[t] + e);
+            } else {
+#pragma unroll
+              for (int f = 0; f < Vec16<T>::N; ++f) v[t][e + f] = 0.f;
+            }
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int e = 0; e < NT; ++e) top = max(top, __float_as_uint(v[t][e]) & 0x7fffffffu);
+        bool ok;
+        const float up = power(top, &v_back, &ok);
+        uint32_t ph[2], pl[2];
+        softmax_block(n_full, sc, k_back, v_back, ph, pl);
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+          uint32_t hi[4], lo[4];                       // features 2 j, 2 j + 1; tokens 0, 1 and 2, 3
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+              const float x0 = ok ? v[2 * f][2 * j + e] * up : 0.f, x1 = ok ? v[2 * f + 1][2 * j + e] * up : 0.f;
+              hi[2 * f + e] = h2(x0, x1);
+              if (kF32) {
+                const float2 w = h2_float(hi[2 * f + e]);
+                lo[2 * f + e] = h2(x0 - w.x, x1 - w.y);
+              }
+            }
+          mma_pv(o[j], hi[0], hi[1], hi[2], hi[3], ph, pl);
+          if (kF32) mma_m16n8k16_f16(o[j], lo[0], lo[1], lo[2], lo[3], ph[0], ph[1]);
+        }
+      }
+    }
+
+    // ---- the blocks held as codes
     for (int j = 0; j < n_codes; ++j) {
       cp_wait<kQaStages - 2>();
       issue(j + kQaStages - 1);                   // (into the stage read in the iteration before)
       const uint32_t src = ring + (j % kQaStages) * qa_stage_bytes(D);
-      float sc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-      uint4 kw[2][KC];
+      float sa[4] = {0.f, 0.f, 0.f, 0.f}, sb[4] = {0.f, 0.f, 0.f, 0.f};      // two chains of products
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int i = 0; i < KC; ++i) {
+        const uint4 k0 = lds16(src + i * 512 + lane * 16), k1 = lds16(src + (KC + i) * 512 + lane * 16);
 #pragma unroll
-        for (int i = 0; i < KC; ++i) kw[t][i] = lds16(src + (t * KC + i) * 512 + lane * 16);
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t x0 = codes_bias<FMT>(w == 0 ? k0.x : w == 1 ? k0.y : w == 2 ? k0.z : k0.w);
+          const uint32_t x1 = codes_bias<FMT>(w == 0 ? k1.x : w == 1 ? k1.y : w == 2 ? k1.z : k1.w);
+          const int ks = 4 * i + w;
+          const uint32_t a0 = codes_pair<FMT, 0>(x0), a1 = codes_pair<FMT, 0>(x1), a2 = codes_pair<FMT, 1>(x0), a3 = codes_pair<FMT, 1>(x1);
+          mma_m16n8k16_f16(w & 1 ? sb : sa, a0, a1, a2, a3, qh[ks][0], qh[ks][1]);
+          if (kF32) mma_m16n8k16_f16(w & 1 ? sa : sb, a0, a1, a2, a3, ql[ks][0], ql[ks][1]);
+        }
+      }
       uint32_t vw[4][NT / 4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
@@ -379,108 +531,46 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
       }
       const float k_scale = lds4(src + 2 * kQuantBlock * D + lane * 8), v_scale = lds4(src + 2 * kQuantBlock * D + lane * 8 + 4);
 #pragma unroll
-      for (int i = 0; i < KC; ++i)
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            const uint4& k4 = kw[t][i];
-            const uint32_t word = codes_bias<FMT>(w == 0 ? k4.x : w == 1 ? k4.y : w == 2 ? k4.z : k4.w);
-            const int ks = 4 * i + w;
-            mma_m16n8k16_f16(sc[t], qh[ks][0], ql[ks][0], qh[ks][1], ql[ks][1], codes_pair<FMT, 0>(word), codes_pair<FMT, 1>(word));
-          }
+      for (int f = 0; f < 4; ++f) sa[f] += sb[f];
       uint32_t ph[2], pl[2];
-      softmax_block(blk0 + j, sc, k_scale, v_scale, ph, pl);
+      softmax_block(blk0 + j, sa, k_scale, v_scale, ph, pl);
 #pragma unroll
       for (int w = 0; w < NT / 4; ++w) {
         const uint32_t t0 = codes_bias<FMT>(vw[0][w]), t1 = codes_bias<FMT>(vw[1][w]), t2 = codes_bias<FMT>(vw[2][w]),
                        t3 = codes_bias<FMT>(vw[3][w]);
+        // features 4 w, 4 w + 1 (lo) and 4 w + 2, 4 w + 3 (hi) of token pairs
         const uint32_t lo01 = __byte_perm(t0, t1, 0x5140), hi01 = __byte_perm(t0, t1, 0x7362);
         const uint32_t lo23 = __byte_perm(t2, t3, 0x5140), hi23 = __byte_perm(t2, t3, 0x7362);
-        mma_m16n8k16_f16(o[4 * w], ph[0], pl[0], ph[1], pl[1], codes_pair<FMT, 0>(lo01), codes_pair<FMT, 0>(lo23));
-        mma_m16n8k16_f16(o[4 * w + 1], ph[0], pl[0], ph[1], pl[1], codes_pair<FMT, 1>(lo01), codes_pair<FMT, 1>(lo23));
-        mma_m16n8k16_f16(o[4 * w + 2], ph[0], pl[0], ph[1], pl[1], codes_pair<FMT, 0>(hi01), codes_pair<FMT, 0>(hi23));
-        mma_m16n8k16_f16(o[4 * w + 3], ph[0], pl[0], ph[1], pl[1], codes_pair<FMT, 1>(hi01), codes_pair<FMT, 1>(hi23));
+        mma_pv(o[2 * w], codes_pair<FMT, 0>(lo01), codes_pair<FMT, 1>(lo01), codes_pair<FMT, 0>(lo23), codes_pair<FMT, 1>(lo23), ph, pl);
+        mma_pv(o[2 * w + 1], codes_pair<FMT, 0>(hi01), codes_pair<FMT, 1>(hi01), codes_pair<FMT, 0>(hi23), codes_pair<FMT, 1>(hi23), ph, pl);
       }
     }
     cp_wait<0>();
 
-    // ---- the open block, in the storage type
-    if (n_codes < nb) {
-      const int n_tail = s.len - n_full * kQuantBlock;
-      const T* kt = static_cast<const T*>(g.tail[0]) + ((long long)s.slot * H + h) * kQuantBlock * D;
-      const T* vt = static_cast<const T*>(g.tail[1]) + ((long long)s.slot * H + h) * kQuantBlock * D;
-      // magnitudes compare as integers, infinities and NaN above everything finite; a block with one of those acts as a
-      // block of codes does: scale NaN, values 0 (so that a query that sees none of it is left alone)
-      uint32_t k_top = 0, v_top = 0;
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        if (r + 8 * t < n_tail)
-          for (int i = 0; i < KC; ++i)
-            for (int e = 0; e < 16; e += Vec16<T>::N) {
-              float v[Vec16<T>::N];
-              Vec16<T>::load(kt + (r + 8 * t) * D + 16 * (c + 4 * i) + e, v);
-#pragma unroll
-              for (int f = 0; f < Vec16<T>::N; ++f) k_top = max(k_top, __float_as_uint(v[f]) & 0x7fffffffu);
-              Vec16<T>::load(vt + (r + 8 * t) * D + 16 * (c + 4 * i) + e, v);
-#pragma unroll
-              for (int f = 0; f < Vec16<T>::N; ++f) v_top = max(v_top, __float_as_uint(v[f]) & 0x7fffffffu);
-            }
-      k_top = __reduce_max_sync(0xffffffffu, k_top);
-      v_top = __reduce_max_sync(0xffffffffu, v_top);
-      const bool k_ok = k_top < 0x7f800000u, v_ok = v_top < 0x7f800000u;
-      float k_back, v_back;
-      const float k_up = scale_up_to_half(__uint_as_float(k_top), &k_back), v_up = scale_up_to_half(__uint_as_float(v_top), &v_back);
-      if (!k_ok) k_back = __uint_as_float(0x7fc00000u);
-      if (!v_ok) v_back = __uint_as_float(0x7fc00000u);
-      float sc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          float v[4];
-          const T* p = kt + (r + 8 * t) * D + 16 * (c + 4 * (ks >> 2)) + 4 * (ks & 3);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = k_ok && r + 8 * t < n_tail ? load_elem(p + e) * k_up : 0.f;
-          const uint32_t b0 = h2(v[0], v[1]), b1 = h2(v[2], v[3]);
-          mma_m16n8k16_f16(sc[t], qh[ks][0], ql[ks][0], qh[ks][1], ql[ks][1], b0, b1);
-          if (kF32) {
-            const float2 w0 = h2_float(b0), w1 = h2_float(b1);
-            mma_m16n8k16_f16(sc[t], qh[ks][0], ql[ks][0], qh[ks][1], ql[ks][1], h2(v[0] - w0.x, v[1] - w0.y), h2(v[2] - w1.x, v[3] - w1.y));
-          }
-        }
-      uint32_t ph[2], pl[2];
-      softmax_block(n_full, sc, k_back, v_back, ph, pl);
-#pragma unroll
-      for (int e = 0; e < NT; ++e) {
-        float v[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const int tok = 2 * c + (t & 1) + (t >> 1) * 8;
-          v[t] = v_ok && tok < n_tail ? load_elem(vt + tok * D + NT * r + e) * v_up : 0.f;
-        }
-        const uint32_t b0 = h2(v[0], v[1]), b1 = h2(v[2], v[3]);
-        mma_m16n8k16_f16(o[e], ph[0], pl[0], ph[1], pl[1], b0, b1);
-        if (kF32) {
-          const float2 w0 = h2_float(b0), w1 = h2_float(b1);
-          mma_m16n8k16_f16(o[e], ph[0], pl[0], ph[1], pl[1], h2(v[0] - w0.x, v[1] - w0.y), h2(v[2] - w1.x, v[3] - w1.y));
-        }
-      }
-    }
-
     // ---- the segment's result
-    l_run += __shfl_xor_sync(0xffffffffu, l_run, 1);
-    l_run += __shfl_xor_sync(0xffffffffu, l_run, 2);
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int w = 4; w < 32; w <<= 1) l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], w);
     const float o_scale = v_ref * (1.f / kQaPScale);
     const bool starts = u == item, ends = seg_end == item_end;
     if (starts && ends) {
-      if (row_ok) {
-        const float inv = l_run == 0.f ? 0.f : o_scale / l_run;
-        T* dst = static_cast<T*>(a.out) + ((long long)(s.first + qi) * a.n_q_heads + head) * D + 2 * c * NT;
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+      for (int e = 0; e < 2; ++e) {
+        const int qrow = tile * kQaRows + 2 * c + e;
+        if (qrow < n_rows) {
+          const float inv = l_run[e] == 0.f ? 0.f : o_scale / l_run[e];
+          float v[NT];
 #pragma unroll
-          for (int e = 0; e < NT; ++e) dst[k * NT + e] = from_f32<T>((o[e][k] + o[e][2 + k]) * inv);
+          for (int j = 0; j < MT; ++j) {
+            v[2 * j] = o[j][e] * inv;
+            v[2 * j + 1] = o[j][2 + e] * inv;
+          }
+          T* dst = static_cast<T*>(a.out) +
+                   ((long long)(s.first + (qrow >> a.group_shift)) * a.n_q_heads + h * a.group + (qrow & (a.group - 1))) * D + NT * r;
+#pragma unroll
+          for (int f = 0; f < NT; f += Vec16<T>::N) store16<T>(dst + f, v + f);
+        }
       }
     } else {
       const int at = 2 * warp + (starts ? 1 : 0);
@@ -491,14 +581,20 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
         q.starts = starts; q.ends = ends;
         q.valid = 1;
       }
-      if (c == 0) {
-        sm.m[at][r] = m_ref;
-        sm.l[at][r] = l_run;
+      float* dst = seg_rows(at);
+      if (r == 0) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          sm.m[at][2 * c + e] = m_ref[e];
+          sm.l[at][2 * c + e] = l_run[e];
+        }
       }
+      __syncwarp();                               // (the rows of the second kind lie over the ring)
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int e = 0; e < 2; ++e)
 #pragma unroll
-        for (int e = 0; e < NT; ++e) sm.o[at][r][(2 * c + k) * NT + e] = (o[e][k] + o[e][2 + k]) * o_scale;
+        for (int j = 0; j < MT; ++j)
+          *reinterpret_cast<float2*>(dst + (2 * c + e) * D + NT * r + 2 * j) = make_float2(o[j][e] * o_scale, o[j][2 + e] * o_scale);
     }
     u = seg_end;
   }
@@ -509,7 +605,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
   bool desc_written = false;
   constexpr int E = D / 32;
   const int row = warp;
-  for (int i = 0; i < 2 * kQaWarps;) {
+  for (int i = 0; i < 2 * kQaWarps && row < kQaRows;) {
     if (!sm.seg[i].valid) { ++i; continue; }
     int j = i + 1, last = i;
     while (j < 2 * kQaWarps && (!sm.seg[j].valid || sm.seg[j].item == sm.seg[i].item)) {
@@ -527,7 +623,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
         const float w = sm.m[k][row] == -INFINITY ? (sm.l[k][row] == 0.f ? 0.f : 1.f) : exp2_approx(sm.m[k][row] - m);
         l += w * sm.l[k][row];
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] += w * sm.o[k][row][lane * E + e];
+        for (int e = 0; e < E; ++e) acc[e] += w * seg_rows(k)[row * D + lane * E + e];
       }
     if (first.starts && ends) {
       const QuantSeq s = quant_seq(a, first.b);
@@ -561,7 +657,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
 
 // Joins the items that shares cut: block g the one that begins in CTA g and goes on in the next ones.  Also zeroes the rows of unusable sequences.
 template <typename T, int D>
-__global__ void __launch_bounds__(kQaThreads) quant_merge_kernel(const __grid_constant__ QuantAttnArgs a) {
+__global__ void __launch_bounds__(kQaMergeThreads) quant_merge_kernel(const __grid_constant__ QuantAttnArgs a) {
   constexpr int E = D / 32;
   const int tid = threadIdx.x, lane = tid & 31, row = tid >> 5;
   const QaWork<D> ws(a.ws);
@@ -570,7 +666,7 @@ __global__ void __launch_bounds__(kQaThreads) quant_merge_kernel(const __grid_co
     if (s.error && s.n > 0) {
       T* dst = static_cast<T*>(a.out) + (long long)s.first * a.n_q_heads * D;
       const long long n = (long long)s.n * a.n_q_heads * D;
-      for (long long i = tid; i < n; i += kQaThreads) dst[i] = from_f32<T>(0.f);
+      for (long long i = tid; i < n; i += kQaMergeThreads) dst[i] = from_f32<T>(0.f);
     }
   }
   const QaDesc d = ws.desc[blockIdx.x];
@@ -602,13 +698,14 @@ __global__ void __launch_bounds__(kQaThreads) quant_merge_kernel(const __grid_co
 template <typename T, int FMT, int D>
 cudaError_t launch(const QuantAttnArgs& a, int sm_count, cudaStream_t stream) {
   constexpr size_t smem = qa_ring_bytes<D>() + sizeof(QaSmem<D>);
+  static_assert(kQaStages * qa_stage_bytes(D) >= kQaRows * D * 4, "a segment's rows fit over a warp's ring");
   static_assert(smem <= 227 * 1024, "shared memory of one CTA");
   cudaError_t e = cudaFuncSetAttribute(quant_attn_kernel<T, FMT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   const int grid = sm_count < kQaMaxCtas ? sm_count : kQaMaxCtas;
   quant_attn_kernel<T, FMT, D><<<grid, kQaThreads, smem, stream>>>(a);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  quant_merge_kernel<T, D><<<grid, kQaThreads, 0, stream>>>(a);
+  quant_merge_kernel<T, D><<<grid, kQaMergeThreads, 0, stream>>>(a);
   return cudaGetLastError();
 }
 

@@ -16,23 +16,6 @@ constexpr int kRotThreads = 256;
 constexpr int kRotTokens = 4;                   // tokens per block: 4 x 64 angles = one per thread
 
 template <typename T>
-__device__ __forceinline__ void store16(T* p, const float* v);
-template <>
-__device__ __forceinline__ void store16<float>(float* p, const float* v) {
-  *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-}
-template <>
-__device__ __forceinline__ void store16<__nv_bfloat16>(__nv_bfloat16* p, const float* v) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-    w[i] = *reinterpret_cast<const uint32_t*>(&b);
-  }
-  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-template <typename T>
 __global__ void __launch_bounds__(kRotThreads) rotate_kernel(const __grid_constant__ RotateArgs a, int tokens_per_block) {
   constexpr int N = Vec16<T>::N;
   __shared__ float2 cs[kRotTokens][64];

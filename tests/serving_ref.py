@@ -143,19 +143,19 @@ def attend(q, k, v, scale, softcap=0.0, slopes=None, prefix=0):
     return out, size
 
 
-def tolerance(ref, size, L, out_eps, chunk=False, softcap=0.0, slopes=None):
+def tolerance(ref, size, L, out_eps, half_p, softcap=0.0, slopes=None):
     """How far a row may be off, from the roundings on its way (first order, absolute, per element).
 
     x: products accumulate in fp32, 16 at a time: at most d / 16 = 8 sums of partly truncated terms, and the operands carry 22 bits
        (2^-22 each): (8 + 4) 2^-23 < 2^-19 of sum |q k| scale.  tanh: 2^-20 of the cap.  bias: one fp32 product, one sum, in base-2
        units: 2^-22 of the largest |bias|.  A probability is off by the score's error, the output by twice that times max |v|.
     p: 2^x 2^-21, times the V scale and back 2^-21, as an fp16 pair 2^-21; summed over L / 16 blocks in fp32: L / 16 2^-23.
-    chunk: probabilities as single fp16, 2^-11 of each (2^-12 rounded to nearest, and sums of unrounded ones below).
+    half_p (bf16 queries): probabilities as single fp16, half a step of which is 2^-11 of each.
     out: half a step of its type, out_eps / 2 = 2^-8 |ref| in bf16 and 2^-24 |ref| in fp32."""
     dx = 2.0 ** -19 * size[..., 0]
     if softcap:
         dx = dx + 2.0 ** -20 * softcap
     if slopes is not None:
         dx = dx + 2.0 ** -22 * np.abs(np.asarray(slopes, dtype=np.float64))[None, :] * L * math.log2(math.e)
-    dp = 3 * 2.0 ** -21 + L / 16 * 2.0 ** -23 + (2.0 ** -11 if chunk else 0.0)
+    dp = 3 * 2.0 ** -21 + L / 16 * 2.0 ** -23 + (2.0 ** -11 if half_p else 0.0)
     return (out_eps / 2) * np.abs(ref) + ((2 * dx + dp) * size[..., 1])[..., None] * (1 + out_eps)

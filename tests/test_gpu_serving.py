@@ -328,14 +328,14 @@ def test_append_strided_rows_and_skipped_tokens():
 
 
 # ---- attention --------------------------------------------------------------------------------------------------
-def check_attention(p, new, q, out, chunk=False, softcap=0.0, slopes=None, prefix=None):
+def check_attention(p, new, q, out, softcap=0.0, slopes=None, prefix=None):
     cfg = p.cfg
     at = 0
     for b, n in enumerate(new):
         if n:
             k, v = p.ref.values(p.ref.k[b]), p.ref.values(p.ref.v[b])
             ref, size = R.attend(f64(q[at:at + n]), k, v, cfg.head_dim ** -0.5, softcap, slopes, prefix[b] if prefix else 0)
-            tol = R.tolerance(ref, size, p.lens[b], EPS[p.dtype], chunk, softcap, slopes)
+            tol = R.tolerance(ref, size, p.lens[b], EPS[p.dtype], p.dtype == "bf16", softcap, slopes)
             err = np.abs(f64(out[at:at + n]) - ref)
             assert (err <= tol).all(), (b, n, p.lens[b], float((err / tol).max()))
         at += n
@@ -407,7 +407,7 @@ def test_chunks_match_plain_form(fmt, dtype, d, page, n_q, n_kv, before, new, op
         kw["prefix"] = [(n + o) * 2 // 3 for n, o in zip(new, before)]
     q = p.rows(sum(new), n_q, 2.0)
     out = attend(p, new, q, **dict(kw))
-    check_attention(p, new, q, out, chunk=dtype == "bf16", softcap=kw.get("softcap", 0.0), slopes=kw.get("slopes"), prefix=kw.get("prefix"))
+    check_attention(p, new, q, out, softcap=kw.get("softcap", 0.0), slopes=kw.get("slopes"), prefix=kw.get("prefix"))
     assert p.status.item() == 0
 
 
@@ -504,7 +504,7 @@ def test_a_run_of_steps(fmt, dtype):
     p = Program(cfg, fmt, seed=11, dtype=dtype)
     dt = DT[dtype][1]
 
-    def step(new, chunk):
+    def step(new):
         T, B = sum(new), len(new)
         plan = p.plan(new)
         qkv = torch.tensor(p.rng.standard_normal((T, 12 * 64)), dtype=dt, device="cuda")
@@ -521,18 +521,18 @@ def test_a_run_of_steps(fmt, dtype):
             at += n
         assert plan.seq_lens.tolist() == p.lens
         p.check_cache()
-        check_attention(p, new, q, out, chunk=chunk and dtype == "bf16", softcap=30.0)
-    step([33, 5, 70, 0], True)
+        check_attention(p, new, q, out, softcap=30.0)
+    step([33, 5, 70, 0])
     for _ in range(3):
-        step([1, 1, 1, 0], False)
-    step([1, 40, 1, 90], True)
+        step([1, 1, 1, 0])
+    step([1, 40, 1, 90])
     assert p.count.item() == 24 - 3 - 3 - 5 - 6
     # request 2 ends, another takes its slot
     binding.release_pages(cfg, p.table, dev([p.lens[2]]), p.free, p.count, seq_slots=dev(p.slots[2:3]))
     assert p.count.item() == 12
     p.lens[2], p.ref.k[2], p.ref.v[2] = 0, None, None
-    step([2, 1, 100, 1], True)
-    step([1, 1, 1, 1], False)
+    step([2, 1, 100, 1])
+    step([1, 1, 1, 1])
 
 
 def test_a_captured_decode_step_replays_and_two_graphs_share_a_workspace():
