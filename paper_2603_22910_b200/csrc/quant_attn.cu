@@ -11,8 +11,8 @@
 //            batches, one long request and a thousand short ones all balance.  A share cuts at most two (sequence, head)
 //            items; their partial results (running maximum, sum, output) are combined inside the CTA through shared
 //            memory and between CTAs by a second small kernel.
-//   copies   Each lane copies, by 16-byte cp.async into a ring of its own, exactly the bytes that it will use as matrix operands:
-//            no barrier and no bank conflict.
+//   copies   A warp fills a ring of its own by TMA, one box of 16 token rows for K and one for V per block, in the 128-byte
+//            swizzle: every operand read is then free of bank conflicts.  No barrier between warps.
 //   products mma.sync m16n8k16 in fp16 with the tokens (then the head's features) on the M rows and the 8 query rows on N:
 //            S^T = K q^T, O^T = V^T P^T, 8 instructions each per block and no padding of the queries to 16 rows.  S^T
 //            becomes the operand P^T by one 8 x 8 transposition per 8 tokens in registers.  Codes convert to fp16 exactly; fp32
@@ -24,23 +24,24 @@
 //            two: one per query row, one per warp for the V scales, which moves with the maximum's.
 //   tail     The open block is in the storage type: bf16 converts to fp16 exactly around its own power of two, fp32
 //            as a pair of fp16.  It is attended first, while the first copies are on their way.
+#include <type_traits>
+
 #include "quant_common.cuh"
+#include "recon_tc.h"
 
 namespace echokv {
 
 namespace {
 
-#ifndef QW
-#define QW 12
-#define QS 3
-#endif
-constexpr int kQaWarps = QW;
+constexpr int kQaWarps = 12;
 constexpr int kQaThreads = kQaWarps * 32;
 constexpr int kQaRows = 8;                        // query rows per tile
-constexpr int kQaStages = QS;
+constexpr int kQaStages = 3;
 constexpr int kQaMergeThreads = kQaRows * 32;
 constexpr int kQaMaxCtas = 512;
-constexpr int kQaMinShare = kQaWarps;             // units per CTA at least: one block for every warp
+constexpr int kQaItemCost = 6;                     // what an item costs beside its blocks (queries, first copies, result), in
+                                                  // blocks: units are dealt out as if an item began with that many more
+constexpr int kQaMinShare = 2 * kQaWarps;         // units per CTA at least
 constexpr float kQaGrow = 8.f;                    // the references move when a score is 2^8 above them
 constexpr float kQaPScale = 32.f;                 // P <= 2^8 times a scale ratio < 2 times 2^5: below 2^15
 
@@ -49,7 +50,13 @@ struct QaDesc {                                   // an item cut at the end of C
   int b, tile, h;
 };
 
-__host__ __device__ constexpr int qa_stage_bytes(int D) { return 2 * kQuantBlock * D + 256; }
+__host__ __device__ constexpr int qa_stage_bytes(int D) { return 2 * kQuantBlock * D; }      // K codes, V codes
+// byte offset of 16-byte piece x of token row `tok`: rows of 128 bytes (one token of 128 features, two of 64), swizzled
+template <int D>
+__device__ __forceinline__ uint32_t qa_off(int tok, int x) {
+  if (D == 128) return tok * 128 + ((x ^ (tok & 7)) << 4);
+  return (tok >> 1) * 128 + ((((tok & 1) * 4 + x) ^ ((tok >> 1) & 7)) << 4);
+}
 
 struct QaSeg {
   unsigned long long item;                        // first unit of the item
@@ -67,6 +74,7 @@ struct QaSmem {
   float m[2 * kQaWarps][kQaRows], l[2 * kQaWarps][kQaRows];
   unsigned long long pre[kQaThreads + 1];
   unsigned long long warp_sums[kQaWarps];
+  unsigned long long full[kQaWarps][kQaStages];
 };
 template <int D>
 __host__ __device__ constexpr size_t qa_ring_bytes() { return (size_t)kQaWarps * kQaStages * qa_stage_bytes(D); }
@@ -84,18 +92,6 @@ struct QaWork {
   }
 };
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ uint4 lds16(uint32_t a) {
   uint4 v;
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
@@ -106,10 +102,16 @@ __device__ __forceinline__ uint2 lds8(uint32_t a) {
   asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
   return v;
 }
-__device__ __forceinline__ float lds4(uint32_t a) {
-  float v;
-  asm volatile("ld.shared.b32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
-  return v;
+// bounded wait of a whole warp on a copy's barrier
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const long long start = clock64();
+  while (clock64() - start < kWaitLimitCycles) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (mbar_try_wait(bar, parity)) return true;
+  }
+  return false;
 }
 
 __device__ __forceinline__ int row_tiles(const QuantAttnArgs& a, const QuantSeq& s) {
@@ -117,7 +119,8 @@ __device__ __forceinline__ int row_tiles(const QuantAttnArgs& a, const QuantSeq&
 }
 __device__ __forceinline__ unsigned long long units_of(const QuantAttnArgs& a, const QuantSeq& s) {
   if (s.error || s.n == 0 || chunk_sequence(a, s)) return 0;
-  return (unsigned long long)row_tiles(a, s) * a.g.n_kv_heads * ((s.len + kQuantBlock - 1) / kQuantBlock);
+  return (unsigned long long)row_tiles(a, s) * a.g.n_kv_heads *
+         ((s.len + kQuantBlock - 1) / kQuantBlock + kQaItemCost);
 }
 
 // transposes an 8 x 8 matrix of 16-bit elements held as matrix fragments
@@ -135,13 +138,15 @@ template <>
 __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16(x); }
 
 template <typename T, int FMT, int D>
-__global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_constant__ QuantAttnArgs a) {
+__global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k,
+                                                                   const __grid_constant__ CUtensorMap tm_v,
+                                                                   const __grid_constant__ QuantAttnArgs a) {
   constexpr int KC = D / 64;                      // 16-byte pieces of a key row per lane
   constexpr int KS = D / 16;                      // k-steps of q . k
   constexpr int NT = D / 8;                       // V bytes per token and lane (features NT r .. NT r + NT - 1)
   constexpr int MT = D / 16;                      // output tiles of 16 features: features NT r + 2 j and NT r + 2 j + 1
   constexpr bool kF32 = sizeof(T) == 4;
-  extern __shared__ __align__(128) unsigned char qa_raw[];
+  extern __shared__ __align__(1024) unsigned char qa_raw[];
   QaSmem<D>& sm = *reinterpret_cast<QaSmem<D>*>(qa_raw + qa_ring_bytes<D>());
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
   const uint32_t ring = smem_u32(qa_raw) + warp * kQaStages * qa_stage_bytes(D);
@@ -169,6 +174,10 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     }
     if (lane == 31) sm.warp_sums[warp] = x;
     if (tid < 2 * kQaWarps) sm.seg[tid].valid = 0;
+    if (lane == 0) {
+      for (int i = 0; i < kQaStages; ++i) mbar_init(smem_u32(&sm.full[warp][i]), 1);
+      mbar_fence_init();
+    }
     __syncthreads();
     unsigned long long before = 0;
     for (int w = 0; w < warp; ++w) before += sm.warp_sums[w];
@@ -197,7 +206,9 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     base = sm.pre[lo];
   }
 
-  while (u < u_end) {
+  uint32_t filled = 0, used = 0;                  // blocks this warp has asked for and taken from its ring
+  bool dead = false;                              // a copy did not arrive (reported); the warp gives up
+  while (u < u_end && !dead) {
     QuantSeq s = quant_seq(a, b);
     unsigned long long n_units = units_of(a, s);
     while (base + n_units <= u) {
@@ -208,36 +219,84 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     }
     const int n_blk = (s.len + kQuantBlock - 1) / kQuantBlock, tiles = row_tiles(a, s);
     const unsigned long long rem = u - base;
-    const int ht = (int)(rem / n_blk), blk0 = (int)(rem - (unsigned long long)ht * n_blk);
+    const int ht = (int)(rem / (n_blk + kQaItemCost)), at0 = (int)(rem - (unsigned long long)ht * (n_blk + kQaItemCost));
     const int h = ht / tiles, tile = ht - h * tiles;
-    const unsigned long long item = u - blk0, item_end = item + n_blk;
+    const unsigned long long item = u - at0, item_end = item + n_blk + kQaItemCost;
     const unsigned long long seg_end = min(item_end, u_end);
-    const int nb = (int)(seg_end - u);
+    // blocks [blk0, blk0 + nb) of the item
+    const int blk0 = max(0, at0 - kQaItemCost), nb = max(0, (int)(seg_end - item) - kQaItemCost) - blk0;
+    if (nb == 0) {
+      u = seg_end;
+      continue;
+    }
     const int n_full = s.len / kQuantBlock;       // blocks held as codes; block n_full is the open one
 
+    // ---- the blocks held as codes: copies
+    const int n_codes = max(0, min(nb, n_full - blk0));
+    const int32_t* pages = a.table + (long long)s.slot * g.max_pages;
+    // lane l keeps pages and scales of blocks 32 n + l of the segment: of the current 32, and fetched ahead of the next 32
+    int page_cur, page_next;
+    float ks_cur, vs_cur, ks_next = 0.f, vs_next = 0.f;
+    const auto load_pages = [&](int group) {
+      const int j = 32 * group + lane;
+      int id = j < n_codes ? pages[(blk0 + j) * kQuantBlock >> g.page_shift] : 0;
+      if (id < 0 || id >= g.n_pages) {
+        report_opt(a.status, ECHOKV_EBADPAGE);
+        id = 0;
+      }
+      return id;
+    };
+    const auto load_scales = [&](int group, int page, float* ks, float* vs) {
+      const int j = 32 * group + lane;
+      if (j < n_codes) {
+        const int inside = (blk0 + j) * kQuantBlock & (g.page_tokens - 1);
+        const long long at = ((long long)page * H + h) * (g.page_tokens / kQuantBlock) + inside / kQuantBlock;
+        *ks = g.scales[0][at];
+        *vs = g.scales[1][at];
+      }
+    };
+    page_cur = load_pages(0);
     // ---- the query rows: this lane loads a quarter of row r as operand; its scores are of rows 2 c and 2 c + 1
     const int n_rows = s.n * a.group;
     uint32_t qh[KS][2], ql[kF32 ? KS : 1][2];
     float c_row[2];
+    const int qrow_r = tile * kQaRows + r;
+    const bool ok = qrow_r < n_rows;
+    const T* qp = static_cast<const T*>(a.q) + (long long)(s.first + (ok ? qrow_r >> a.group_shift : 0)) * a.q_stride +
+                  (long long)(h * a.group + (qrow_r & (a.group - 1))) * D;
+    float qv[KC * 16];
+#pragma unroll
+    for (int i = 0; i < KC; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; e += Vec16<T>::N)
+        if (ok) {
+          Vec16<T>::load(qp + 16 * (KC * c + i) + e, qv + 16 * i + e);
+        } else {
+#pragma unroll
+          for (int f = 0; f < Vec16<T>::N; ++f) qv[16 * i + e + f] = 0.f;
+        }
+    page_next = load_pages(1);
+    ks_cur = vs_cur = 0.f;
+    load_scales(0, page_cur, &ks_cur, &vs_cur);
+    int group = 0;
+    const auto issue = [&](int j) {
+      const int page = __shfl_sync(0xffffffffu, (j >> 5) == group ? page_cur : page_next, j & 31);
+      const int row = (page * H + h) * (g.page_tokens * D / 128) + ((blk0 + j) * kQuantBlock & (g.page_tokens - 1)) * D / 128;
+      if (lane == 0) {
+        const int st = filled % kQaStages;
+        const uint32_t bar = smem_u32(&sm.full[warp][st]), dst = ring + st * qa_stage_bytes(D);
+        mbar_arrive_expect_tx(bar, qa_stage_bytes(D));
+        tma_load_2d(dst, &tm_k, 0, row, bar);
+        tma_load_2d(dst + kQuantBlock * D, &tm_v, 0, row, bar);
+      }
+      ++filled;
+    };
+    for (int j = 0; j < min(kQaStages, n_codes); ++j) issue(j);
+
     {
-      const int qrow = tile * kQaRows + r;
-      const bool ok = qrow < n_rows;
-      const T* qp = static_cast<const T*>(a.q) + (long long)(s.first + (ok ? qrow >> a.group_shift : 0)) * a.q_stride +
-                    (long long)(h * a.group + (qrow & (a.group - 1))) * D;
       float top = 0.f;
-      float v[KC * 16];
 #pragma unroll
-      for (int i = 0; i < KC; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; e += Vec16<T>::N)
-          if (ok) {
-            Vec16<T>::load(qp + 16 * (c + 4 * i) + e, v + 16 * i + e);
-          } else {
-#pragma unroll
-            for (int f = 0; f < Vec16<T>::N; ++f) v[16 * i + e + f] = 0.f;
-          }
-#pragma unroll
-      for (int e = 0; e < KC * 16; ++e) top = fmaxf(top, fabsf(v[e]));
+      for (int e = 0; e < KC * 16; ++e) top = fmaxf(top, fabsf(qv[e]));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       float back;
@@ -249,7 +308,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
       for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
-          const float x0 = v[4 * ks + 2 * f] * up, x1 = v[4 * ks + 2 * f + 1] * up;
+          const float x0 = qv[4 * ks + 2 * f] * up, x1 = qv[4 * ks + 2 * f + 1] * up;
           qh[ks][f] = h2(x0, x1);
           if (kF32) {
             const float2 w = h2_float(qh[ks][f]);
@@ -273,42 +332,74 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     for (int j = 0; j < MT; ++j)
 #pragma unroll
       for (int f = 0; f < 4; ++f) o[j][f] = 0.f;
-    float m_ref[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f}, v_ref = 0.f, v_inv = 0.f;
+    // Per query row: the reference of its maximum (0 until it has seen a key, which the first one seen moves), and how far
+    // above the reference a score may be before that moves.
+    float m_ref[2] = {0.f, 0.f}, grow[2] = {-3.0e38f, -3.0e38f}, l_run[2] = {0.f, 0.f}, v_ref = 0.f, v_inv = 0.f;
+    const bool plain = !(a.softcap > 0.f) && a.slopes == nullptr;
+    const int pos_first = s.len - s.n + (tile * kQaRows >> a.group_shift);     // the tile's first query: blocks up to it are seen whole
 
-    // scores of the block's tokens (sc[2 t + e]: token r + 8 t, query row 2 c + e) -> probabilities as operands
-    // (ph[t]: query row r, tokens 8 t + 2 c, + 1), references moved if needed
-    const auto softmax_block = [&](int blk, const float (&sc)[4], float k_scale, float v_scale, uint32_t (&ph)[2], uint32_t (&pl)[2]) {
-      float x[4];
-      bool above = v_scale > v_ref;
+    // Scores of NB blocks (sc[n][2 t + e]: token r + 8 t of block blk + n, query row 2 c + e) -> probabilities as operands
+    // (ph[n][t]: query row r, tokens 8 t + 2 c, + 1), references moved if needed.  masked: some token may be unseen.
+    const auto softmax_blocks = [&](auto nb_tag, bool masked, int blk, float (*sc)[4], const float* k_scale, const float* v_scale,
+                                    uint32_t (*ph)[2], uint32_t (*pl)[2]) {
+      constexpr int NB = decltype(nb_tag)::value;
+      bool above = false;
+      // x - m_ref, in base-2 units
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int n = 0; n < NB; ++n) {
+        const float f0 = c_row[0] * k_scale[n], f1 = c_row[1] * k_scale[n];
+        if (plain) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int tok = blk * kQuantBlock + 8 * t + r;
-          float y = sc[2 * t + e] * (c_row[e] * k_scale);
-          if (a.softcap > 0.f) y = cap_out * tanh_f32(y * cap_in);
-          if (a.slopes) y -= slope2[e] * fabsf((float)(pos[e] - tok));
-          const bool seen = tok < s.len && (tok <= pos[e] || tok < prefix);
-          x[2 * t + e] = seen ? y : -INFINITY;
-          above |= x[2 * t + e] > m_ref[e] + kQaGrow;
+          for (int i = 0; i < 4; ++i) sc[n][i] = fmaf(sc[n][i], i & 1 ? f1 : f0, -m_ref[i & 1]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float y = sc[n][i] * (i & 1 ? f1 : f0);
+            if (a.softcap > 0.f) y = cap_out * tanh_f32(y * cap_in);
+            if (a.slopes) y -= slope2[i & 1] * fabsf((float)(pos[i & 1] - ((blk + n) * kQuantBlock + 8 * (i >> 1) + r)));
+            sc[n][i] = y - m_ref[i & 1];
+          }
         }
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int tok = (blk + n) * kQuantBlock + 8 * (i >> 1) + r;
+            if (!(tok < s.len && (tok <= pos[i & 1] || tok < prefix))) sc[n][i] = -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) above |= sc[n][i] > grow[i & 1];
+        above |= v_scale[n] > v_ref;
+      }
       if (__any_sync(0xffffffffu, above)) {
         float alpha[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float mx = fmaxf(x[e], x[2 + e]);
+          float mx = -INFINITY;
+#pragma unroll
+          for (int n = 0; n < NB; ++n) mx = fmaxf(mx, fmaxf(sc[n][e], sc[n][2 + e]));
 #pragma unroll
           for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+          const bool first = grow[e] != kQaGrow;         // nothing seen so far: sum and output are still 0
           alpha[e] = 1.f;
-          if (mx > m_ref[e]) {
-            alpha[e] = exp2_approx(m_ref[e] - mx);      // 0 the first time
-            m_ref[e] = mx;
+          if (mx > (first ? -INFINITY : 0.f)) {
+            if (!first) alpha[e] = exp2_approx(-mx);
+            grow[e] = kQaGrow;
+            m_ref[e] += mx;
             l_run[e] *= alpha[e];
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+              sc[n][e] -= mx;
+              sc[n][2 + e] -= mx;
+            }
           }
         }
-        if (v_scale > v_ref) {
+        float v_top = v_scale[0];
+#pragma unroll
+        for (int n = 1; n < NB; ++n) v_top = fmaxf(v_top, v_scale[n]);
+        if (v_top > v_ref) {
           // the power of two above the scale
-          const uint32_t e = (__float_as_uint(v_scale) >> 23) + 1;
+          const uint32_t e = (__float_as_uint(v_top) >> 23) + 1;
           const float old = v_ref;
           v_ref = __uint_as_float(e << 23);
           v_inv = __uint_as_float((254 - e) << 23);
@@ -320,22 +411,25 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
 #pragma unroll
           for (int f = 0; f < 4; ++f) o[j][f] *= alpha[f & 1];
       }
-      const float pv = v_scale * v_inv * kQaPScale;
-      float p[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool seen = x[i] != -INFINITY;            // (masked, or a score of -inf: no part of the sums either way)
-        p[i] = seen ? exp2_approx(x[i] - m_ref[i & 1]) : 0.f;
-        l_run[i & 1] += p[i];
-        p[i] = seen ? p[i] * pv : 0.f;
-      }
+      for (int n = 0; n < NB; ++n) {
+        const float pv = v_scale[n] * v_inv * kQaPScale;
+        float p[4];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const uint32_t w = h2(p[2 * t], p[2 * t + 1]);
-        ph[t] = movm(w);
-        if (kF32) {
-          const float2 f = h2_float(w);
-          pl[t] = movm(h2(p[2 * t] - f.x, p[2 * t + 1] - f.y));
+        for (int i = 0; i < 4; ++i) {
+          p[i] = exp2_approx(sc[n][i]);
+          l_run[i & 1] += p[i];
+          p[i] *= pv;
+          if (masked && sc[n][i] == -INFINITY) p[i] = 0.f;       // (0 times a scale that is NaN)
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const uint32_t w = h2(p[2 * t], p[2 * t + 1]);
+          ph[n][t] = movm(w);
+          if (kF32) {
+            const float2 f = h2_float(w);
+            pl[n][t] = movm(h2(p[2 * t] - f.x, p[2 * t + 1] - f.y));
+          }
         }
       }
     };
@@ -343,57 +437,6 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
       mma_m16n8k16_f16(d, a0, a1, a2, a3, ph[0], ph[1]);
       if (kF32) mma_m16n8k16_f16(d, a0, a1, a2, a3, pl[0], pl[1]);
     };
-
-    // ---- the blocks held as codes: copies
-    const int n_codes = max(0, min(nb, n_full - blk0));
-    const int32_t* pages = a.table + (long long)s.slot * g.max_pages;
-    int page_base = (blk0 * kQuantBlock) >> g.page_shift;
-    int page_id = 0;
-    const int page_last = (s.len - 1) >> g.page_shift;
-    const auto load_pages = [&]() {
-      const int p = page_base + lane;
-      int id = p <= page_last ? pages[p] : 0;
-      if (id < 0 || id >= g.n_pages) {
-        report_opt(a.status, ECHOKV_EBADPAGE);
-        id = 0;
-      }
-      page_id = id;
-    };
-    load_pages();
-    const auto issue = [&](int j) {
-      if (j < n_codes) {
-        const int t0 = (blk0 + j) * kQuantBlock, pi = t0 >> g.page_shift;
-        if (pi >= page_base + 32) {
-          page_base = pi;
-          load_pages();
-        }
-        const long long page = __shfl_sync(0xffffffffu, page_id, pi - page_base);
-        const int inside = t0 & (g.page_tokens - 1);
-        const long long ph = page * H + h;
-        const long long off = (ph * g.page_tokens + inside) * D;
-        const uint32_t dst = ring + (j % kQaStages) * qa_stage_bytes(D);
-        const unsigned char* kp = g.codes[0] + off + r * D + 16 * c;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int i = 0; i < KC; ++i) cp_async16(dst + (t * KC + i) * 512 + lane * 16, kp + t * 8 * D + i * 64);
-        const unsigned char* vp = g.codes[1] + off + 2 * c * D + NT * r;
-        const uint32_t vdst = dst + kQuantBlock * D;
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const unsigned char* src = vp + ((t & 1) + (t >> 1) * 8) * D;
-          if (NT == 16) cp_async16(vdst + t * 512 + lane * 16, src);
-          else cp_async8(vdst + t * 256 + lane * 8, src);
-        }
-        const long long so = ph * (g.page_tokens / kQuantBlock) + inside / kQuantBlock;
-        const uint32_t sdst = dst + 2 * kQuantBlock * D + lane * 8;
-        cp_async4(sdst, g.scales[0] + so);
-        cp_async4(sdst + 4, g.scales[1] + so);
-      }
-      cp_commit();
-    };
-#pragma unroll
-    for (int j = 0; j < kQaStages - 1; ++j) issue(j);
 
     // ---- the open block, in the storage type
     if (n_codes < nb) {
@@ -421,7 +464,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
 #pragma unroll
             for (int e = 0; e < 16; e += Vec16<T>::N) {
               if (r + 8 * t < n_tail) {
-                Vec16<T>::load(kt + (r + 8 * t) * D + 16 * (c + 4 * i) + e, v[t] + 16 * i + e);
+                Vec16<T>::load(kt + (r + 8 * t) * D + 16 * (KC * c + i) + e, v[t] + 16 * i + e);
               } else {
 #pragma unroll
                 for (int f = 0; f < Vec16<T>::N; ++f) v[t][16 * i + e + f] = 0.f;
@@ -477,8 +520,8 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
           for (int e = 0; e < NT; ++e) top = max(top, __float_as_uint(v[t][e]) & 0x7fffffffu);
         bool ok;
         const float up = power(top, &v_back, &ok);
-        uint32_t ph[2], pl[2];
-        softmax_block(n_full, sc, k_back, v_back, ph, pl);
+        uint32_t ph[1][2], pl[1][2];
+        softmax_blocks(std::integral_constant<int, 1>(), true, n_full, &sc, &k_back, &v_back, ph, pl);
 #pragma unroll
         for (int j = 0; j < MT; ++j) {
           uint32_t hi[4], lo[4];                       // features 2 j, 2 j + 1; tokens 0, 1 and 2, 3
@@ -493,59 +536,111 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
                 lo[2 * f + e] = h2(x0 - w.x, x1 - w.y);
               }
             }
-          mma_pv(o[j], hi[0], hi[1], hi[2], hi[3], ph, pl);
-          if (kF32) mma_m16n8k16_f16(o[j], lo[0], lo[1], lo[2], lo[3], ph[0], ph[1]);
+          mma_pv(o[j], hi[0], hi[1], hi[2], hi[3], ph[0], pl[0]);
+          if (kF32) mma_m16n8k16_f16(o[j], lo[0], lo[1], lo[2], lo[3], ph[0][0], ph[0][1]);
         }
       }
     }
 
-    // ---- the blocks held as codes
-    for (int j = 0; j < n_codes; ++j) {
-      cp_wait<kQaStages - 2>();
-      issue(j + kQaStages - 1);                   // (into the stage read in the iteration before)
-      const uint32_t src = ring + (j % kQaStages) * qa_stage_bytes(D);
-      float sa[4] = {0.f, 0.f, 0.f, 0.f}, sb[4] = {0.f, 0.f, 0.f, 0.f};      // two chains of products
+    // ---- the blocks held as codes, two at a time
+    const auto attend_blocks = [&](auto nb_tag, int j, const uint32_t* src, const float* k_scale, const float* v_scale) {
+      constexpr int NB = decltype(nb_tag)::value;
+      float sc[NB][4];
 #pragma unroll
-      for (int i = 0; i < KC; ++i) {
-        const uint4 k0 = lds16(src + i * 512 + lane * 16), k1 = lds16(src + (KC + i) * 512 + lane * 16);
+      for (int n = 0; n < NB; ++n) {
+        float sb[4] = {0.f, 0.f, 0.f, 0.f};       // two chains of products
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const uint32_t x0 = codes_bias<FMT>(w == 0 ? k0.x : w == 1 ? k0.y : w == 2 ? k0.z : k0.w);
-          const uint32_t x1 = codes_bias<FMT>(w == 0 ? k1.x : w == 1 ? k1.y : w == 2 ? k1.z : k1.w);
-          const int ks = 4 * i + w;
-          const uint32_t a0 = codes_pair<FMT, 0>(x0), a1 = codes_pair<FMT, 0>(x1), a2 = codes_pair<FMT, 1>(x0), a3 = codes_pair<FMT, 1>(x1);
-          mma_m16n8k16_f16(w & 1 ? sb : sa, a0, a1, a2, a3, qh[ks][0], qh[ks][1]);
-          if (kF32) mma_m16n8k16_f16(w & 1 ? sa : sb, a0, a1, a2, a3, ql[ks][0], ql[ks][1]);
+        for (int f = 0; f < 4; ++f) sc[n][f] = 0.f;
+#pragma unroll
+        for (int i = 0; i < KC; ++i) {
+          const uint4 k0 = lds16(src[n] + qa_off<D>(r, KC * c + i)), k1 = lds16(src[n] + qa_off<D>(r + 8, KC * c + i));
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t x0 = codes_bias<FMT>(w == 0 ? k0.x : w == 1 ? k0.y : w == 2 ? k0.z : k0.w);
+            const uint32_t x1 = codes_bias<FMT>(w == 0 ? k1.x : w == 1 ? k1.y : w == 2 ? k1.z : k1.w);
+            const int ks = 4 * i + w;
+            const uint32_t a0 = codes_pair<FMT, 0>(x0), a1 = codes_pair<FMT, 0>(x1), a2 = codes_pair<FMT, 1>(x0), a3 = codes_pair<FMT, 1>(x1);
+            mma_m16n8k16_f16(w & 1 ? sb : sc[n], a0, a1, a2, a3, qh[ks][0], qh[ks][1]);
+            if (kF32) mma_m16n8k16_f16(w & 1 ? sc[n] : sb, a0, a1, a2, a3, ql[ks][0], ql[ks][1]);
+          }
+        }
+#pragma unroll
+        for (int f = 0; f < 4; ++f) sc[n][f] += sb[f];
+      }
+      uint32_t ph[NB][2], pl[NB][2];
+      softmax_blocks(nb_tag, (blk0 + j + NB) * kQuantBlock - 1 > pos_first, blk0 + j, sc, k_scale, v_scale, ph, pl);
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        uint32_t vw[4][NT / 4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const uint32_t at = src[n] + kQuantBlock * D + qa_off<D>(2 * c + (t & 1) + (t >> 1) * 8, r * NT / 16) + (NT == 16 ? 0 : (r & 1) * 8);
+          if (NT == 16) {
+            const uint4 w = lds16(at);
+            vw[t][0] = w.x; vw[t][1] = w.y; vw[t][NT / 4 - 2] = w.z; vw[t][NT / 4 - 1] = w.w;
+          } else {
+            const uint2 w = lds8(at);
+            vw[t][0] = w.x; vw[t][1] = w.y;
+          }
+        }
+#pragma unroll
+        for (int w = 0; w < NT / 4; ++w) {
+          const uint32_t t0 = codes_bias<FMT>(vw[0][w]), t1 = codes_bias<FMT>(vw[1][w]), t2 = codes_bias<FMT>(vw[2][w]),
+                         t3 = codes_bias<FMT>(vw[3][w]);
+          // features 4 w, 4 w + 1 (lo) and 4 w + 2, 4 w + 3 (hi) of token pairs
+          const uint32_t lo01 = __byte_perm(t0, t1, 0x5140), hi01 = __byte_perm(t0, t1, 0x7362);
+          const uint32_t lo23 = __byte_perm(t2, t3, 0x5140), hi23 = __byte_perm(t2, t3, 0x7362);
+          mma_pv(o[2 * w], codes_pair<FMT, 0>(lo01), codes_pair<FMT, 1>(lo01), codes_pair<FMT, 0>(lo23), codes_pair<FMT, 1>(lo23), ph[n], pl[n]);
+          mma_pv(o[2 * w + 1], codes_pair<FMT, 0>(hi01), codes_pair<FMT, 1>(hi01), codes_pair<FMT, 0>(hi23), codes_pair<FMT, 1>(hi23), ph[n], pl[n]);
         }
       }
-      uint32_t vw[4][NT / 4];
+    };
+    for (int j = 0; j < n_codes; j += 2) {
+      if ((j & 31) == 0 && j > 0) {
+        ++group;
+        page_cur = page_next;
+        ks_cur = ks_next;
+        vs_cur = vs_next;
+        page_next = load_pages(group + 1);
+      }
+      if ((j & 31) == 16) load_scales(group + 1, page_next, &ks_next, &vs_next);
+      const bool two = j + 1 < n_codes;
+      uint32_t src[2];
+      float ks[2], vs[2];
+      bool ok = true;
+      const uint32_t used_before = used;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        if (NT == 16) {
-          const uint4 w = lds16(src + kQuantBlock * D + t * 512 + lane * 16);
-          vw[t][0] = w.x; vw[t][1] = w.y; vw[t][NT / 4 - 2] = w.z; vw[t][NT / 4 - 1] = w.w;
-        } else {
-          const uint2 w = lds8(src + kQuantBlock * D + t * 256 + lane * 8);
-          vw[t][0] = w.x; vw[t][1] = w.y;
+      for (int n = 0; n < 2; ++n)
+        if (n == 0 || two) {
+          const int st = used % kQaStages;
+          ok &= warp_wait(smem_u32(&sm.full[warp][st]), (used / kQaStages) & 1);
+          src[n] = ring + st * qa_stage_bytes(D);
+          ++used;
         }
-      }
-      const float k_scale = lds4(src + 2 * kQuantBlock * D + lane * 8), v_scale = lds4(src + 2 * kQuantBlock * D + lane * 8 + 4);
 #pragma unroll
-      for (int f = 0; f < 4; ++f) sa[f] += sb[f];
-      uint32_t ph[2], pl[2];
-      softmax_block(blk0 + j, sa, k_scale, v_scale, ph, pl);
-#pragma unroll
-      for (int w = 0; w < NT / 4; ++w) {
-        const uint32_t t0 = codes_bias<FMT>(vw[0][w]), t1 = codes_bias<FMT>(vw[1][w]), t2 = codes_bias<FMT>(vw[2][w]),
-                       t3 = codes_bias<FMT>(vw[3][w]);
-        // features 4 w, 4 w + 1 (lo) and 4 w + 2, 4 w + 3 (hi) of token pairs
-        const uint32_t lo01 = __byte_perm(t0, t1, 0x5140), hi01 = __byte_perm(t0, t1, 0x7362);
-        const uint32_t lo23 = __byte_perm(t2, t3, 0x5140), hi23 = __byte_perm(t2, t3, 0x7362);
-        mma_pv(o[2 * w], codes_pair<FMT, 0>(lo01), codes_pair<FMT, 1>(lo01), codes_pair<FMT, 0>(lo23), codes_pair<FMT, 1>(lo23), ph, pl);
-        mma_pv(o[2 * w + 1], codes_pair<FMT, 0>(hi01), codes_pair<FMT, 1>(hi01), codes_pair<FMT, 0>(hi23), codes_pair<FMT, 1>(hi23), ph, pl);
+      for (int n = 0; n < 2; ++n) {
+        ks[n] = __shfl_sync(0xffffffffu, ks_cur, (j + n) & 31);
+        vs[n] = __shfl_sync(0xffffffffu, vs_cur, (j + n) & 31);
       }
+      if (!__all_sync(0xffffffffu, ok)) {
+        dead = true;
+        used = used_before;
+        break;
+      }
+      if (two) attend_blocks(std::integral_constant<int, 2>(), j, src, ks, vs);
+      else attend_blocks(std::integral_constant<int, 1>(), j, src, ks, vs);
+      __syncwarp();                               // (all lanes have read the blocks: they may be overwritten)
+      for (int n = 0; n < 2; ++n)
+        if (j + kQaStages + n < n_codes) issue(j + kQaStages + n);
     }
-    cp_wait<0>();
+    if (dead) {
+      // let every copy that was asked for land, as far as it does, before the shared memory is given back
+      if (lane == 0) {
+        report_opt(a.status, ECHOKV_ETIMEOUT);
+        for (; used < filled; ++used) mbar_drain(smem_u32(&sm.full[warp][used % kQaStages]), (used / kQaStages) & 1);
+      }
+      break;
+    }
 
     // ---- the segment's result
 #pragma unroll
@@ -553,7 +648,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
 #pragma unroll
       for (int w = 4; w < 32; w <<= 1) l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], w);
     const float o_scale = v_ref * (1.f / kQaPScale);
-    const bool starts = u == item, ends = seg_end == item_end;
+    const bool starts = blk0 == 0, ends = seg_end == item_end;
     if (starts && ends) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -585,7 +680,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
       if (r == 0) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          sm.m[at][2 * c + e] = m_ref[e];
+          sm.m[at][2 * c + e] = l_run[e] == 0.f ? -INFINITY : m_ref[e];
           sm.l[at][2 * c + e] = l_run[e];
         }
       }
@@ -702,8 +797,15 @@ cudaError_t launch(const QuantAttnArgs& a, int sm_count, cudaStream_t stream) {
   static_assert(smem <= 227 * 1024, "shared memory of one CTA");
   cudaError_t e = cudaFuncSetAttribute(quant_attn_kernel<T, FMT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
+  // the codes as rows of 128 bytes (64 two-byte elements to TMA), boxes of one block
+  CUtensorMap maps[2];
+  for (int i = 0; i < 2; ++i) {
+    const uint64_t dims[2] = {64, (uint64_t)a.g.n_pages * a.g.n_kv_heads * a.g.page_tokens * D / 128}, strides[1] = {128};
+    const uint32_t box[2] = {64, kQuantBlock * D / 128};
+    if ((e = encode_tiled_bf16(&maps[i], a.g.codes[i], 2, dims, strides, box)) != cudaSuccess) return e;
+  }
   const int grid = sm_count < kQaMaxCtas ? sm_count : kQaMaxCtas;
-  quant_attn_kernel<T, FMT, D><<<grid, kQaThreads, smem, stream>>>(a);
+  quant_attn_kernel<T, FMT, D><<<grid, kQaThreads, smem, stream>>>(maps[0], maps[1], a);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   quant_merge_kernel<T, D><<<grid, kQaMergeThreads, 0, stream>>>(a);
   return cudaGetLastError();

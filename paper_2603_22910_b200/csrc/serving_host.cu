@@ -78,6 +78,8 @@ int check_all(const echokv_config* c) {
   if (!c) return ECHOKV_EINVAL;
   int rc = check_heads(c);
   if (rc == ECHOKV_OK) rc = check_pages(c);
+  // (the rows of the 8-bit pools are indexed in 32 bits: 2^31 rows of 64 bytes are 128 GB)
+  if (rc == ECHOKV_OK && (long long)c->n_pages * c->n_kv_heads >= 0x7fffffffll / c->page_tokens) rc = ECHOKV_EINVAL;
   if (rc == ECHOKV_OK && (!(c->softmax_scale >= 0.f) || !std::isfinite(c->softmax_scale))) rc = ECHOKV_EINVAL;
   return rc;
 }
