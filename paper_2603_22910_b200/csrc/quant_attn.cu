@@ -24,8 +24,6 @@
 //            two: one per query row, one per warp for the V scales, which moves with the maximum's.
 //   tail     The open block is in the storage type: bf16 converts to fp16 exactly around its own power of two, fp32
 //            as a pair of fp16.  It is attended first, while the first copies are on their way.
-#include <type_traits>
-
 #include "quant_common.cuh"
 #include "recon_tc.h"
 
@@ -75,6 +73,7 @@ struct QaSmem {
   unsigned long long pre[kQaThreads + 1];
   unsigned long long warp_sums[kQaWarps];
   unsigned long long full[kQaWarps][kQaStages];
+  int4 info[kQaThreads];                          // slot, length, first token, tokens (0: nothing to do) of a small batch
 };
 template <int D>
 __host__ __device__ constexpr size_t qa_ring_bytes() { return (size_t)kQaWarps * kQaStages * qa_stage_bytes(D); }
@@ -114,13 +113,64 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) {
   return false;
 }
 
-__device__ __forceinline__ int row_tiles(const QuantAttnArgs& a, const QuantSeq& s) {
-  return (s.n * a.group + kQaRows - 1) / kQaRows;
+// What the kernel needs of a sequence: w = 0 tokens where nothing is attended here.
+__device__ __forceinline__ int4 seq_info(const QuantAttnArgs& a, int b, bool tell) {
+  const QuantSeq s = quant_seq(a, b);
+  if (s.error && tell) report_opt(a.status, s.error);
+  return make_int4(s.slot, s.len, s.first, s.error || chunk_sequence(a, s) ? 0 : s.n);
 }
-__device__ __forceinline__ unsigned long long units_of(const QuantAttnArgs& a, const QuantSeq& s) {
-  if (s.error || s.n == 0 || chunk_sequence(a, s)) return 0;
-  return (unsigned long long)row_tiles(a, s) * a.g.n_kv_heads *
-         ((s.len + kQuantBlock - 1) / kQuantBlock + kQaItemCost);
+__device__ __forceinline__ int row_tiles(const QuantAttnArgs& a, int n) { return (n * a.group + kQaRows - 1) / kQaRows; }
+__device__ __forceinline__ unsigned long long units_of(const QuantAttnArgs& a, const int4& s) {
+  return (unsigned long long)row_tiles(a, s.w) * a.g.n_kv_heads * ((s.y + kQuantBlock - 1) / kQuantBlock + kQaItemCost);
+}
+// n / d, mostly of numbers that fit 32 bits (a 64-bit division is long)
+__device__ __forceinline__ unsigned long long quotient(unsigned long long n, unsigned long long d) {
+  return ((n | d) >> 32) == 0 ? (unsigned long long)((uint32_t)n / (uint32_t)d) : n / d;
+}
+
+// four consecutive elements of a row in the storage type
+template <typename T>
+struct Quad;
+template <>
+struct Quad<__nv_bfloat16> {
+  uint2 w;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { w = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void zero() { w = make_uint2(0u, 0u); }
+  __device__ __forceinline__ float get(int e) const {
+    const uint32_t x = e < 2 ? w.x : w.y;
+    return __uint_as_float(e & 1 ? x & 0xffff0000u : x << 16);
+  }
+  // magnitudes compare as integers, infinities and NaN above everything finite (a pair of them at once here)
+  __device__ __forceinline__ uint32_t top(uint32_t t) const {
+    return __vmaxu2(t, __vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu));
+  }
+  __device__ __forceinline__ static uint32_t top_bits(uint32_t t) { return max(t & 0xffff0000u, t << 16); }
+};
+template <>
+struct Quad<float> {
+  uint4 w;
+  __device__ __forceinline__ void load(const float* p) { w = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void zero() { w = make_uint4(0u, 0u, 0u, 0u); }
+  __device__ __forceinline__ float get(int e) const { return __uint_as_float(e == 0 ? w.x : e == 1 ? w.y : e == 2 ? w.z : w.w); }
+  __device__ __forceinline__ uint32_t top(uint32_t t) const {
+    return max(max(t, w.x & 0x7fffffffu), max(w.y & 0x7fffffffu, max(w.z & 0x7fffffffu, w.w & 0x7fffffffu)));
+  }
+  __device__ __forceinline__ static uint32_t top_bits(uint32_t t) { return t; }
+};
+// fp16 operands of x * up: the rounded pair and what it leaves
+struct HalfPair {
+  uint32_t hi, lo;
+};
+template <bool LOW>
+__device__ __forceinline__ HalfPair split_pair(float x0, float x1) {
+  HalfPair p;
+  p.hi = h2(x0, x1);
+  p.lo = 0u;
+  if (LOW) {
+    const float2 w = h2_float(p.hi);
+    p.lo = h2(x0 - w.x, x1 - w.y);
+  }
+  return p;
 }
 
 // transposes an 8 x 8 matrix of 16-bit elements held as matrix fragments
@@ -157,13 +207,19 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     return at & 1 ? reinterpret_cast<float*>(qa_raw + (size_t)(at >> 1) * kQaStages * qa_stage_bytes(D)) : &sm.o_first[at >> 1][0][0];
   };
 
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (tid == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_v) : "memory");
+  }
   // ---- the units of the call, and this CTA's and warp's share of them
   const int per = (a.B + kQaThreads - 1) / kQaThreads;
   {
     unsigned long long n = 0;
+#pragma unroll 1
     for (int b = tid * per; b < min(a.B, (tid + 1) * per); ++b) {
-      const QuantSeq s = quant_seq(a, b);
-      if (s.error && blockIdx.x == 0) report_opt(a.status, s.error);
+      const int4 s = seq_info(a, b, blockIdx.x == 0);
+      if (per == 1) sm.info[b] = s;
       n += units_of(a, s);
     }
     unsigned long long x = n;
@@ -186,10 +242,10 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     __syncthreads();
   }
   const unsigned long long total = sm.pre[kQaThreads];
-  unsigned long long share = (total + gridDim.x - 1) / gridDim.x;
+  unsigned long long share = quotient(total + gridDim.x - 1, gridDim.x);
   if (share < kQaMinShare) share = kQaMinShare;
   const unsigned long long cta0 = min(total, share * blockIdx.x), cta1 = min(total, cta0 + share);
-  const unsigned long long wshare = (cta1 - cta0 + kQaWarps - 1) / kQaWarps;
+  const unsigned long long wshare = quotient(cta1 - cta0 + kQaWarps - 1, kQaWarps);
   unsigned long long u = min(cta1, cta0 + wshare * warp);
   const unsigned long long u_end = min(cta1, u + wshare);
 
@@ -197,7 +253,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
   int b = 0;
   unsigned long long base = 0;                    // first unit of sequence b
   if (u < u_end) {
-    int lo = 0, hi = kQaThreads;
+    int lo = 0, hi = min(kQaThreads, a.B);
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (sm.pre[mid] <= u) lo = mid; else hi = mid;
@@ -205,21 +261,24 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     b = lo * per;
     base = sm.pre[lo];
   }
+  const bool plain = !(a.softcap > 0.f) && a.slopes == nullptr;
+  const float cap_in = a.softcap > 0.f ? 1.f / a.softcap : 0.f, cap_out = a.softcap * kLog2e;
 
   uint32_t filled = 0, used = 0;                  // blocks this warp has asked for and taken from its ring
   bool dead = false;                              // a copy did not arrive (reported); the warp gives up
   while (u < u_end && !dead) {
-    QuantSeq s = quant_seq(a, b);
-    unsigned long long n_units = units_of(a, s);
+    int4 info = per == 1 ? sm.info[b] : seq_info(a, b, false);
+    unsigned long long n_units = units_of(a, info);
     while (base + n_units <= u) {
       base += n_units;
       ++b;
-      s = quant_seq(a, b);
-      n_units = units_of(a, s);
+      info = per == 1 ? sm.info[b] : seq_info(a, b, false);
+      n_units = units_of(a, info);
     }
-    const int n_blk = (s.len + kQuantBlock - 1) / kQuantBlock, tiles = row_tiles(a, s);
+    const int slot = info.x, len = info.y, first_token = info.z, n_new = info.w;
+    const int n_blk = (len + kQuantBlock - 1) / kQuantBlock, tiles = row_tiles(a, n_new);
     const unsigned long long rem = u - base;
-    const int ht = (int)(rem / (n_blk + kQaItemCost)), at0 = (int)(rem - (unsigned long long)ht * (n_blk + kQaItemCost));
+    const int ht = (int)quotient(rem, n_blk + kQaItemCost), at0 = (int)(rem - (unsigned long long)ht * (n_blk + kQaItemCost));
     const int h = ht / tiles, tile = ht - h * tiles;
     const unsigned long long item = u - at0, item_end = item + n_blk + kQaItemCost;
     const unsigned long long seg_end = min(item_end, u_end);
@@ -229,11 +288,11 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
       u = seg_end;
       continue;
     }
-    const int n_full = s.len / kQuantBlock;       // blocks held as codes; block n_full is the open one
+    const int n_full = len / kQuantBlock;       // blocks held as codes; block n_full is the open one
 
     // ---- the blocks held as codes: copies
     const int n_codes = max(0, min(nb, n_full - blk0));
-    const int32_t* pages = a.table + (long long)s.slot * g.max_pages;
+    const int32_t* pages = a.table + (long long)slot * g.max_pages;
     // lane l keeps pages and scales of blocks 32 n + l of the segment: of the current 32, and fetched ahead of the next 32
     int page_cur, page_next;
     float ks_cur, vs_cur, ks_next = 0.f, vs_next = 0.f;
@@ -257,12 +316,12 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     };
     page_cur = load_pages(0);
     // ---- the query rows: this lane loads a quarter of row r as operand; its scores are of rows 2 c and 2 c + 1
-    const int n_rows = s.n * a.group;
+    const int n_rows = n_new * a.group;
     uint32_t qh[KS][2], ql[kF32 ? KS : 1][2];
     float c_row[2];
     const int qrow_r = tile * kQaRows + r;
     const bool ok = qrow_r < n_rows;
-    const T* qp = static_cast<const T*>(a.q) + (long long)(s.first + (ok ? qrow_r >> a.group_shift : 0)) * a.q_stride +
+    const T* qp = static_cast<const T*>(a.q) + (long long)(first_token + (ok ? qrow_r >> a.group_shift : 0)) * a.q_stride +
                   (long long)(h * a.group + (qrow_r & (a.group - 1))) * D;
     float qv[KC * 16];
 #pragma unroll
@@ -308,22 +367,18 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
       for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
-          const float x0 = qv[4 * ks + 2 * f] * up, x1 = qv[4 * ks + 2 * f + 1] * up;
-          qh[ks][f] = h2(x0, x1);
-          if (kF32) {
-            const float2 w = h2_float(qh[ks][f]);
-            ql[ks][f] = h2(x0 - w.x, x1 - w.y);
-          }
+          const HalfPair p = split_pair<kF32>(qv[4 * ks + 2 * f] * up, qv[4 * ks + 2 * f + 1] * up);
+          qh[ks][f] = p.hi;
+          if (kF32) ql[ks][f] = p.lo;
         }
     }
-    const float cap_in = a.softcap > 0.f ? 1.f / a.softcap : 0.f, cap_out = a.softcap * kLog2e;
     const int prefix = a.prefix ? a.prefix[b] : 0;
     int pos[2];
     float slope2[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int qrow = tile * kQaRows + 2 * c + e;
-      pos[e] = s.len - s.n + (qrow < n_rows ? qrow >> a.group_shift : 0);
+      pos[e] = len - n_new + (qrow < n_rows ? qrow >> a.group_shift : 0);
       slope2[e] = a.slopes ? a.slopes[h * a.group + (qrow & (a.group - 1))] * kLog2e : 0.f;
     }
 
@@ -335,14 +390,20 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     // Per query row: the reference of its maximum (0 until it has seen a key, which the first one seen moves), and how far
     // above the reference a score may be before that moves.
     float m_ref[2] = {0.f, 0.f}, grow[2] = {-3.0e38f, -3.0e38f}, l_run[2] = {0.f, 0.f}, v_ref = 0.f, v_inv = 0.f;
-    const bool plain = !(a.softcap > 0.f) && a.slopes == nullptr;
-    const int pos_first = s.len - s.n + (tile * kQaRows >> a.group_shift);     // the tile's first query: blocks up to it are seen whole
+    const int pos_first = len - n_new + (tile * kQaRows >> a.group_shift);     // the tile's first query: blocks up to it are seen whole
 
-    // Scores of NB blocks (sc[n][2 t + e]: token r + 8 t of block blk + n, query row 2 c + e) -> probabilities as operands
-    // (ph[n][t]: query row r, tokens 8 t + 2 c, + 1), references moved if needed.  masked: some token may be unseen.
-    const auto softmax_blocks = [&](auto nb_tag, bool masked, int blk, float (*sc)[4], const float* k_scale, const float* v_scale,
-                                    uint32_t (*ph)[2], uint32_t (*pl)[2]) {
-      constexpr int NB = decltype(nb_tag)::value;
+    // a scaled product q . k of token tok and query row 2 c + e -> the score in base-2 units
+    const auto score = [&](float y, int e, int tok) {
+      if (a.softcap > 0.f) y = cap_out * tanh_f32(y * cap_in);
+      if (a.slopes) y -= slope2[e] * fabsf((float)(pos[e] - tok));
+      return y;
+    };
+    // Scores of two blocks (sc[n][2 t + e]: token r + 8 t of block n, query row 2 c + e; the first token is tok0) -> probabilities as
+    // operands (ph[n][t]: query row r, tokens 8 t + 2 c, + 1), references moved if needed.  masked: some token may be unseen,
+    // those from tok_end on all are.
+    constexpr int NB = 2;
+    const auto softmax_blocks = [&](bool masked, int tok0, int tok_end, float (&sc)[NB][4], const float (&k_scale)[NB], const float (&v_scale)[NB],
+                                    uint32_t (&ph)[NB][2], uint32_t (&pl)[NB][2]) {
       bool above = false;
       // x - m_ref, in base-2 units
 #pragma unroll
@@ -353,18 +414,14 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
           for (int i = 0; i < 4; ++i) sc[n][i] = fmaf(sc[n][i], i & 1 ? f1 : f0, -m_ref[i & 1]);
         } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float y = sc[n][i] * (i & 1 ? f1 : f0);
-            if (a.softcap > 0.f) y = cap_out * tanh_f32(y * cap_in);
-            if (a.slopes) y -= slope2[i & 1] * fabsf((float)(pos[i & 1] - ((blk + n) * kQuantBlock + 8 * (i >> 1) + r)));
-            sc[n][i] = y - m_ref[i & 1];
-          }
+          for (int i = 0; i < 4; ++i)
+            sc[n][i] = score(sc[n][i] * (i & 1 ? f1 : f0), i & 1, tok0 + n * kQuantBlock + 8 * (i >> 1) + r) - m_ref[i & 1];
         }
         if (masked) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int tok = (blk + n) * kQuantBlock + 8 * (i >> 1) + r;
-            if (!(tok < s.len && (tok <= pos[i & 1] || tok < prefix))) sc[n][i] = -INFINITY;
+            const int tok = tok0 + n * kQuantBlock + 8 * (i >> 1) + r;
+            if (!(tok < tok_end && (tok <= pos[i & 1] || tok < prefix))) sc[n][i] = -INFINITY;
           }
         }
 #pragma unroll
@@ -424,12 +481,9 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const uint32_t w = h2(p[2 * t], p[2 * t + 1]);
-          ph[n][t] = movm(w);
-          if (kF32) {
-            const float2 f = h2_float(w);
-            pl[n][t] = movm(h2(p[2 * t] - f.x, p[2 * t + 1] - f.y));
-          }
+          const HalfPair w = split_pair<kF32>(p[2 * t], p[2 * t + 1]);
+          ph[n][t] = movm(w.hi);
+          if (kF32) pl[n][t] = movm(w.lo);
         }
       }
     };
@@ -438,119 +492,169 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
       if (kF32) mma_m16n8k16_f16(d, a0, a1, a2, a3, pl[0], pl[1]);
     };
 
-    // ---- the open block, in the storage type
+    // ---- the open block, in the storage type, while the first copies are on their way
     if (n_codes < nb) {
-      const int n_tail = s.len - n_full * kQuantBlock;
-      const long long off = ((long long)s.slot * H + h) * kQuantBlock * D;
-      // Magnitudes compare as integers, infinities and NaN above everything finite; a block with one of those acts as a
-      // block of codes does: scale NaN, values 0 (so that a query that sees none of it is left alone).
-      const auto power = [&](uint32_t top, float* back, bool* ok) {
-        top = __reduce_max_sync(0xffffffffu, top);
-        *ok = top < 0x7f800000u;
-        const float up = scale_up_to_half(__uint_as_float(top), back);
-        if (!*ok) *back = __uint_as_float(0x7fc00000u);
-        return up;
-      };
-      float sc[4] = {0.f, 0.f, 0.f, 0.f};
-      float k_back, v_back;
-      {
-        const T* kt = static_cast<const T*>(g.tail[0]) + off;
-        float v[2][KC * 16];
-        uint32_t top = 0;
+      const int n_open = len - n_full * kQuantBlock;
+      const long long open_at = ((long long)slot * H + h) * kQuantBlock * D;
+      float sc[1][4] = {{0.f, 0.f, 0.f, 0.f}}, ks[1], vs[1];
+      Quad<T> vq[4][NT / 4];                         // value rows 2 c, 2 c + 1, 2 c + 8, 2 c + 9, this lane's features
+      // A block with an infinity or NaN acts as a block of codes does: scale NaN, values 0 (a query that sees none of it is
+      // left alone).
+      const T* kt = static_cast<const T*>(g.tail[0]) + open_at;
+      const T* vt = static_cast<const T*>(g.tail[1]) + open_at;
+      Quad<T> kq[2][KS];
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int i = 0; i < KC; ++i)
-#pragma unroll
-            for (int e = 0; e < 16; e += Vec16<T>::N) {
-              if (r + 8 * t < n_tail) {
-                Vec16<T>::load(kt + (r + 8 * t) * D + 16 * (KC * c + i) + e, v[t] + 16 * i + e);
-              } else {
-#pragma unroll
-                for (int f = 0; f < Vec16<T>::N; ++f) v[t][16 * i + e + f] = 0.f;
-              }
-            }
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int e = 0; e < KC * 16; ++e) top = max(top, __float_as_uint(v[t][e]) & 0x7fffffffu);
-        bool ok;
-        const float up = power(top, &k_back, &ok);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          uint32_t hi[4], lo[4];                       // tokens r, r + 8; elements 0, 1 and 2, 3
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int f = 0; f < 2; ++f) {
-              const float x0 = ok ? v[t][4 * ks + 2 * f] * up : 0.f, x1 = ok ? v[t][4 * ks + 2 * f + 1] * up : 0.f;
-              hi[2 * f + t] = h2(x0, x1);
-              if (kF32) {
-                const float2 w = h2_float(hi[2 * f + t]);
-                lo[2 * f + t] = h2(x0 - w.x, x1 - w.y);
-              }
-            }
-          mma_m16n8k16_f16(sc, hi[0], hi[1], hi[2], hi[3], qh[ks][0], qh[ks][1]);
-          if (kF32) {
-            mma_m16n8k16_f16(sc, hi[0], hi[1], hi[2], hi[3], ql[ks][0], ql[ks][1]);
-            mma_m16n8k16_f16(sc, lo[0], lo[1], lo[2], lo[3], qh[ks][0], qh[ks][1]);
-          }
-        }
-      }
-      {
-        const T* vt = static_cast<const T*>(g.tail[1]) + off;
-        float v[4][NT];
-        uint32_t top = 0;
+        for (int x = 0; x < KS; ++x)
+          if (r + 8 * t < n_open) kq[t][x].load(kt + (r + 8 * t) * D + KC * 16 * c + 4 * x);
+          else kq[t][x].zero();
+      const auto load_values = [&]() {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const int tok = 2 * c + (t & 1) + (t >> 1) * 8;
 #pragma unroll
-          for (int e = 0; e < NT; e += Vec16<T>::N) {
-            if (tok < n_tail) {
-              Vec16<T>::load(vt + tok * D + NT * r + e, v[t] + e);
-            } else {
-#pragma unroll
-              for (int f = 0; f < Vec16<T>::N; ++f) v[t][e + f] = 0.f;
-            }
-          }
+          for (int x = 0; x < NT / 4; ++x)
+            if (tok < n_open) vq[t][x].load(vt + tok * D + NT * r + 4 * x);
+            else vq[t][x].zero();
         }
+      };
+      if (!kF32) load_values();                    // (fp32 rows take twice the registers: the values after the scores)
+      // power of two for a block whose largest magnitude is `top`, over the warp
+      const auto power = [&](uint32_t top, float* back) {
+        top = __reduce_max_sync(0xffffffffu, Quad<T>::top_bits(top));
+        const float up = scale_up_to_half(__uint_as_float(top), back);
+        if (top >= 0x7f800000u) *back = __uint_as_float(0x7fc00000u);
+        return up;
+      };
+      uint32_t top = 0;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int x = 0; x < KS; ++x) top = kq[t][x].top(top);
+      const float k_up = power(top, &ks[0]);
+      const bool k_ok = ks[0] == ks[0];
+#pragma unroll
+      for (int x = 0; x < KS; ++x) {
+        HalfPair p[4];                             // tokens r, r + 8; elements 0, 1 and 2, 3
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (!k_ok) kq[t][x].zero();
+#pragma unroll
+          for (int f = 0; f < 2; ++f) p[2 * f + t] = split_pair<kF32>(kq[t][x].get(2 * f) * k_up, kq[t][x].get(2 * f + 1) * k_up);
+        }
+        mma_m16n8k16_f16(sc[0], p[0].hi, p[1].hi, p[2].hi, p[3].hi, qh[x][0], qh[x][1]);
+        if (kF32) {
+          mma_m16n8k16_f16(sc[0], p[0].hi, p[1].hi, p[2].hi, p[3].hi, ql[x][0], ql[x][1]);
+          mma_m16n8k16_f16(sc[0], p[0].lo, p[1].lo, p[2].lo, p[3].lo, qh[x][0], qh[x][1]);
+        }
+      }
+      if (kF32) load_values();
+      top = 0;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int x = 0; x < NT / 4; ++x) top = vq[t][x].top(top);
+      const float v_up = power(top, &vs[0]);
+      if (vs[0] != vs[0]) {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-          for (int e = 0; e < NT; ++e) top = max(top, __float_as_uint(v[t][e]) & 0x7fffffffu);
-        bool ok;
-        const float up = power(top, &v_back, &ok);
-        uint32_t ph[1][2], pl[1][2];
-        softmax_blocks(std::integral_constant<int, 1>(), true, n_full, &sc, &k_back, &v_back, ph, pl);
+          for (int x = 0; x < NT / 4; ++x) vq[t][x].zero();
+      }
+      // (the first block of the segment: the references are what it says, and there is nothing to scale)
+      float x[4];
 #pragma unroll
-        for (int j = 0; j < MT; ++j) {
-          uint32_t hi[4], lo[4];                       // features 2 j, 2 j + 1; tokens 0, 1 and 2, 3
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int f = 0; f < 2; ++f) {
-              const float x0 = ok ? v[2 * f][2 * j + e] * up : 0.f, x1 = ok ? v[2 * f + 1][2 * j + e] * up : 0.f;
-              hi[2 * f + e] = h2(x0, x1);
-              if (kF32) {
-                const float2 w = h2_float(hi[2 * f + e]);
-                lo[2 * f + e] = h2(x0 - w.x, x1 - w.y);
-              }
-            }
-          mma_pv(o[j], hi[0], hi[1], hi[2], hi[3], ph[0], pl[0]);
-          if (kF32) mma_m16n8k16_f16(o[j], lo[0], lo[1], lo[2], lo[3], ph[0][0], ph[0][1]);
+      for (int i = 0; i < 4; ++i) {
+        const int tok = n_full * kQuantBlock + 8 * (i >> 1) + r;
+        x[i] = tok < len && (tok <= pos[i & 1] || tok < prefix) ? score(sc[0][i] * (c_row[i & 1] * ks[0]), i & 1, tok) : -INFINITY;
+      }
+      {
+        const uint32_t e = (__float_as_uint(vs[0]) >> 23) + 1;        // the power of two above the scale
+        if (vs[0] > 0.f) {
+          v_ref = __uint_as_float(e << 23);
+          v_inv = __uint_as_float((254 - e) << 23);
         }
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float mx = fmaxf(x[e], x[2 + e]);
+#pragma unroll
+        for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+        if (mx > -INFINITY) {
+          m_ref[e] = mx;
+          grow[e] = kQaGrow;
+        }
+      }
+      const float pv = vs[0] * v_inv * kQaPScale;
+      uint32_t ph[1][2], pl[1][2];
+      float p[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[i] = exp2_approx(x[i] - m_ref[i & 1]);
+        l_run[i & 1] += p[i];
+        p[i] = x[i] == -INFINITY ? 0.f : p[i] * pv;
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const HalfPair w = split_pair<kF32>(p[2 * t], p[2 * t + 1]);
+        ph[0][t] = movm(w.hi);
+        if (kF32) pl[0][t] = movm(w.lo);
+      }
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        HalfPair p[4];                             // features 2 m, 2 m + 1; tokens 0, 1 and 2, 3
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int f = 0; f < 2; ++f)
+            p[2 * f + e] = split_pair<kF32>(vq[2 * f][m / 2].get(2 * (m & 1) + e) * v_up, vq[2 * f + 1][m / 2].get(2 * (m & 1) + e) * v_up);
+        mma_pv(o[m], p[0].hi, p[1].hi, p[2].hi, p[3].hi, ph[0], pl[0]);
+        if (kF32) mma_m16n8k16_f16(o[m], p[0].lo, p[1].lo, p[2].lo, p[3].lo, ph[0][0], ph[0][1]);
       }
     }
 
-    // ---- the blocks held as codes, two at a time
-    const auto attend_blocks = [&](auto nb_tag, int j, const uint32_t* src, const float* k_scale, const float* v_scale) {
-      constexpr int NB = decltype(nb_tag)::value;
-      float sc[NB][4];
+    // ---- the blocks held as codes, two per step
+#pragma unroll 1
+    for (int j = 0; j < n_codes; j += 2) {
+      const bool two = j + 1 < n_codes;
+      float sc[2][4], ks[2], vs[2];
+      uint32_t src[2];
 #pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        float sb[4] = {0.f, 0.f, 0.f, 0.f};       // two chains of products
+      for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int f = 0; f < 4; ++f) sc[n][f] = 0.f;
+      if ((j & 31) == 0 && j > 0) {
+        ++group;
+        page_cur = page_next;
+        ks_cur = ks_next;
+        vs_cur = vs_next;
+        page_next = load_pages(group + 1);
+      }
+      if ((j & 31) == 16) load_scales(group + 1, page_next, &ks_next, &vs_next);
+      bool arrived = true;
+      const uint32_t used_before = used;
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        if (n == 0 || two) {
+          const int st = used % kQaStages;
+          arrived &= warp_wait(smem_u32(&sm.full[warp][st]), (used / kQaStages) & 1);
+          src[n] = ring + st * qa_stage_bytes(D);
+          ++used;
+        } else {
+          src[n] = src[0];                         // (an odd last block stands in for its partner, which is masked)
+        }
+        ks[n] = __shfl_sync(0xffffffffu, ks_cur, (j + (two ? n : 0)) & 31);
+        vs[n] = __shfl_sync(0xffffffffu, vs_cur, (j + (two ? n : 0)) & 31);
+      }
+      if (!__all_sync(0xffffffffu, arrived)) {
+        dead = true;
+        used = used_before;
+        break;
+      }
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        float sb[4] = {0.f, 0.f, 0.f, 0.f};        // two chains of products
 #pragma unroll
         for (int i = 0; i < KC; ++i) {
           const uint4 k0 = lds16(src[n] + qa_off<D>(r, KC * c + i)), k1 = lds16(src[n] + qa_off<D>(r + 8, KC * c + i));
@@ -558,19 +662,20 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
           for (int w = 0; w < 4; ++w) {
             const uint32_t x0 = codes_bias<FMT>(w == 0 ? k0.x : w == 1 ? k0.y : w == 2 ? k0.z : k0.w);
             const uint32_t x1 = codes_bias<FMT>(w == 0 ? k1.x : w == 1 ? k1.y : w == 2 ? k1.z : k1.w);
-            const int ks = 4 * i + w;
+            const int x = 4 * i + w;
             const uint32_t a0 = codes_pair<FMT, 0>(x0), a1 = codes_pair<FMT, 0>(x1), a2 = codes_pair<FMT, 1>(x0), a3 = codes_pair<FMT, 1>(x1);
-            mma_m16n8k16_f16(w & 1 ? sb : sc[n], a0, a1, a2, a3, qh[ks][0], qh[ks][1]);
-            if (kF32) mma_m16n8k16_f16(w & 1 ? sc[n] : sb, a0, a1, a2, a3, ql[ks][0], ql[ks][1]);
+            mma_m16n8k16_f16(w & 1 ? sb : sc[n], a0, a1, a2, a3, qh[x][0], qh[x][1]);
+            if (kF32) mma_m16n8k16_f16(w & 1 ? sc[n] : sb, a0, a1, a2, a3, ql[x][0], ql[x][1]);
           }
         }
 #pragma unroll
         for (int f = 0; f < 4; ++f) sc[n][f] += sb[f];
       }
-      uint32_t ph[NB][2], pl[NB][2];
-      softmax_blocks(nb_tag, (blk0 + j + NB) * kQuantBlock - 1 > pos_first, blk0 + j, sc, k_scale, v_scale, ph, pl);
+      const int tok0 = (blk0 + j) * kQuantBlock;
+      uint32_t ph[2][2], pl[2][2];
+      softmax_blocks(!two || tok0 + 2 * kQuantBlock - 1 > pos_first, tok0, two ? 0x7fffffff : tok0 + kQuantBlock, sc, ks, vs, ph, pl);
 #pragma unroll
-      for (int n = 0; n < NB; ++n) {
+      for (int n = 0; n < 2; ++n) {
         uint32_t vw[4][NT / 4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -594,42 +699,8 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
           mma_pv(o[2 * w + 1], codes_pair<FMT, 0>(hi01), codes_pair<FMT, 1>(hi01), codes_pair<FMT, 0>(hi23), codes_pair<FMT, 1>(hi23), ph[n], pl[n]);
         }
       }
-    };
-    for (int j = 0; j < n_codes; j += 2) {
-      if ((j & 31) == 0 && j > 0) {
-        ++group;
-        page_cur = page_next;
-        ks_cur = ks_next;
-        vs_cur = vs_next;
-        page_next = load_pages(group + 1);
-      }
-      if ((j & 31) == 16) load_scales(group + 1, page_next, &ks_next, &vs_next);
-      const bool two = j + 1 < n_codes;
-      uint32_t src[2];
-      float ks[2], vs[2];
-      bool ok = true;
-      const uint32_t used_before = used;
+      __syncwarp();                                // (all lanes have read the blocks: they may be overwritten)
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
-        if (n == 0 || two) {
-          const int st = used % kQaStages;
-          ok &= warp_wait(smem_u32(&sm.full[warp][st]), (used / kQaStages) & 1);
-          src[n] = ring + st * qa_stage_bytes(D);
-          ++used;
-        }
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        ks[n] = __shfl_sync(0xffffffffu, ks_cur, (j + n) & 31);
-        vs[n] = __shfl_sync(0xffffffffu, vs_cur, (j + n) & 31);
-      }
-      if (!__all_sync(0xffffffffu, ok)) {
-        dead = true;
-        used = used_before;
-        break;
-      }
-      if (two) attend_blocks(std::integral_constant<int, 2>(), j, src, ks, vs);
-      else attend_blocks(std::integral_constant<int, 1>(), j, src, ks, vs);
-      __syncwarp();                               // (all lanes have read the blocks: they may be overwritten)
       for (int n = 0; n < 2; ++n)
         if (j + kQaStages + n < n_codes) issue(j + kQaStages + n);
     }
@@ -662,7 +733,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
             v[2 * j + 1] = o[j][2 + e] * inv;
           }
           T* dst = static_cast<T*>(a.out) +
-                   ((long long)(s.first + (qrow >> a.group_shift)) * a.n_q_heads + h * a.group + (qrow & (a.group - 1))) * D + NT * r;
+                   ((long long)(first_token + (qrow >> a.group_shift)) * a.n_q_heads + h * a.group + (qrow & (a.group - 1))) * D + NT * r;
 #pragma unroll
           for (int f = 0; f < NT; f += Vec16<T>::N) store16<T>(dst + f, v + f);
         }
@@ -694,68 +765,67 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     u = seg_end;
   }
 
-  // ---- segments of one item side by side in this CTA: combine them; what is still cut goes to the workspace
+  // ---- segments of one item side by side in this CTA: combine them; what is still cut goes to the workspace.  A warp per query
+  //      row; lane k looks at segment k.
   __syncthreads();
+  if (warp >= kQaRows) return;
   const QaWork<D> ws(a.ws);
-  bool desc_written = false;
   constexpr int E = D / 32;
-  const int row = warp;
-  for (int i = 0; i < 2 * kQaWarps && row < kQaRows;) {
-    if (!sm.seg[i].valid) { ++i; continue; }
-    int j = i + 1, last = i;
-    while (j < 2 * kQaWarps && (!sm.seg[j].valid || sm.seg[j].item == sm.seg[i].item)) {
-      if (sm.seg[j].valid) last = j;
-      ++j;
-    }
-    const QaSeg first = sm.seg[i];
-    const bool ends = sm.seg[last].ends;
-    float m = -INFINITY;
-    for (int k = i; k <= last; ++k)
-      if (sm.seg[k].valid) m = fmaxf(m, sm.m[k][row]);
-    float l = 0.f, acc[E] = {};
-    for (int k = i; k <= last; ++k)
-      if (sm.seg[k].valid) {
-        const float w = sm.m[k][row] == -INFINITY ? (sm.l[k][row] == 0.f ? 0.f : 1.f) : exp2_approx(sm.m[k][row] - m);
-        l += w * sm.l[k][row];
+  static_assert(2 * kQaWarps <= 32, "a lane per segment");
+  const bool is_seg = lane < 2 * kQaWarps && sm.seg[lane < 2 * kQaWarps ? lane : 0].valid;
+  const unsigned long long my_item = is_seg ? sm.seg[lane].item : ~0ull;
+  const float my_m = is_seg ? sm.m[lane][warp] : -INFINITY, my_l = is_seg ? sm.l[lane][warp] : 0.f;
+  uint32_t todo = __ballot_sync(0xffffffffu, is_seg);
+  QaDesc desc = {0, 0, 0, 0};
+  while (todo) {
+    const int i = __ffs(todo) - 1;
+    const uint32_t mine = __ballot_sync(0xffffffffu, my_item == __shfl_sync(0xffffffffu, my_item, i)) & todo;
+    todo &= ~mine;
+    const QaSeg& first = sm.seg[i];
+    const bool starts = first.starts, ends = sm.seg[31 - __clz(mine)].ends;
+    const bool in = (mine >> lane) & 1;
+    const float m = warp_max(in ? my_m : -INFINITY);
+    // (a row that has seen nothing has the sum 0 -- or NaN)
+    const float w = !in || my_l == 0.f ? 0.f : exp2_approx(my_m - m);
+    const float l = warp_sum(in ? w * my_l : 0.f);
+    float acc[E] = {};
+    for (uint32_t left = mine; left; left &= left - 1) {
+      const int k = __ffs(left) - 1;
+      const float wk = __shfl_sync(0xffffffffu, w, k);
+      const float* o = seg_rows(k) + warp * D + lane * E;
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] += w * seg_rows(k)[row * D + lane * E + e];
-      }
-    if (first.starts && ends) {
-      const QuantSeq s = quant_seq(a, first.b);
-      const int qrow = first.tile * kQaRows + row;
-      if (qrow < s.n * a.group) {
+      for (int e = 0; e < E; ++e) acc[e] += wk * o[e];
+    }
+    if (starts && ends) {
+      const int4 s = per == 1 ? sm.info[first.b] : seq_info(a, first.b, false);
+      const int qrow = first.tile * kQaRows + warp;
+      if (qrow < s.w * a.group) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
         T* dst = static_cast<T*>(a.out) +
-                 ((long long)(s.first + (qrow >> a.group_shift)) * a.n_q_heads + first.h * a.group + (qrow & (a.group - 1))) * D + lane * E;
+                 ((long long)(s.z + (qrow >> a.group_shift)) * a.n_q_heads + first.h * a.group + (qrow & (a.group - 1))) * D + lane * E;
 #pragma unroll
         for (int e = 0; e < E; ++e) dst[e] = from_f32<T>(acc[e] * inv);
       }
     } else {
-      const long long p = ((long long)blockIdx.x * 2 + (first.starts ? 1 : 0)) * kQaRows + row;
+      const long long p = ((long long)blockIdx.x * 2 + (starts ? 1 : 0)) * kQaRows + warp;
       if (lane == 0) ws.ml[p] = make_float2(m, l);
 #pragma unroll
       for (int e = 0; e < E; ++e) ws.o[p * D + lane * E + e] = acc[e];
-      if (first.starts) {
-        if (tid == 0) {
-          QaDesc d;
-          d.n_parts = (int)((first.item_end - 1) / share - blockIdx.x) + 1;
-          d.b = first.b; d.tile = first.tile; d.h = first.h;
-          ws.desc[blockIdx.x] = d;
-        }
-        desc_written = true;
-      }
+      if (starts) desc = QaDesc{(int)(quotient(first.item_end - 1, share) - blockIdx.x) + 1, first.b, first.tile, first.h};
     }
-    i = j;
   }
-  if (tid == 0 && !desc_written) ws.desc[blockIdx.x] = QaDesc{0, 0, 0, 0};
+  if (tid == 0) ws.desc[blockIdx.x] = desc;
 }
 
-// Joins the items that shares cut: block g the one that begins in CTA g and goes on in the next ones.  Also zeroes the rows of unusable sequences.
+// Joins the items that shares cut: block g the one that begins in CTA g and goes on in the next ones.  Also zeroes the rows of
+// unusable sequences.  Launched while the first kernel runs, it waits for that one's end.
 template <typename T, int D>
 __global__ void __launch_bounds__(kQaMergeThreads) quant_merge_kernel(const __grid_constant__ QuantAttnArgs a) {
   constexpr int E = D / 32;
   const int tid = threadIdx.x, lane = tid & 31, row = tid >> 5;
   const QaWork<D> ws(a.ws);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+#pragma unroll 1
   for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
     const QuantSeq s = quant_seq(a, b);
     if (s.error && s.n > 0) {
@@ -767,6 +837,7 @@ __global__ void __launch_bounds__(kQaMergeThreads) quant_merge_kernel(const __gr
   const QaDesc d = ws.desc[blockIdx.x];
   if (d.n_parts == 0) return;
   const auto part = [&](int p) -> long long { return ((long long)(blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * kQaRows + row; };
+  const int4 s = seq_info(a, d.b, false);
   float m = -INFINITY;
   for (int p = lane; p < d.n_parts; p += 32) m = fmaxf(m, ws.ml[part(p)].x);
   m = warp_max(m);
@@ -774,18 +845,17 @@ __global__ void __launch_bounds__(kQaMergeThreads) quant_merge_kernel(const __gr
 #pragma unroll 4
   for (int p = 0; p < d.n_parts; ++p) {
     const float2 ml = ws.ml[part(p)];
-    const float w = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : exp2_approx(ml.x - m);
+    const float w = ml.y == 0.f ? 0.f : exp2_approx(ml.x - m);
     l += w * ml.y;
     const float* o = ws.o + part(p) * D + lane * E;
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] += w * o[e];
   }
-  const QuantSeq s = quant_seq(a, d.b);
   const int qrow = d.tile * kQaRows + row;
-  if (qrow >= s.n * a.group) return;
+  if (qrow >= s.w * a.group) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   T* dst = static_cast<T*>(a.out) +
-           ((long long)(s.first + (qrow >> a.group_shift)) * a.n_q_heads + d.h * a.group + (qrow & (a.group - 1))) * D + lane * E;
+           ((long long)(s.z + (qrow >> a.group_shift)) * a.n_q_heads + d.h * a.group + (qrow & (a.group - 1))) * D + lane * E;
 #pragma unroll
   for (int e = 0; e < E; ++e) dst[e] = from_f32<T>(acc[e] * inv);
 }
@@ -807,8 +877,16 @@ cudaError_t launch(const QuantAttnArgs& a, int sm_count, cudaStream_t stream) {
   const int grid = sm_count < kQaMaxCtas ? sm_count : kQaMaxCtas;
   quant_attn_kernel<T, FMT, D><<<grid, kQaThreads, smem, stream>>>(maps[0], maps[1], a);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  quant_merge_kernel<T, D><<<grid, kQaMergeThreads, 0, stream>>>(a);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kQaMergeThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, quant_merge_kernel<T, D>, a);
 }
 
 template <typename T>
