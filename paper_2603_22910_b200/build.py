@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libechokv.so")
 SOURCES = ["echokv_host.cu", "simt_kernels.cu", "stored_mma.cu", "recon_tc.cu", "recon_pair.cu", "recon_quad.cu", "absorbed.cu", "prefill.cu", "noalloc.cu",
-           "serving_host.cu", "plan.cu", "rotate.cu", "quant_append.cu", "quant_attn.cu"]
+           "serving_host.cu", "plan.cu", "rotate.cu", "quant_append.cu", "quant_attn.cu", "quant_chunk.cu"]
 HEADERS = ["common.cuh", "kernels.h", "recon_tc.h", "recon_common.cuh", "stored_mma.h", "absorbed.h", "prefill.h", "ptx_sm100.cuh",
            "serving.h", "quant_common.cuh", os.path.join("..", "..", "include", "echokv.h")]
 

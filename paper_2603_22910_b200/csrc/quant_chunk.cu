@@ -1,0 +1,664 @@
+// Attention over a cache held in 8 bits for chunks of bf16 queries, on the 5th-generation tensor cores.
+//
+//   O = softmax(score(Q K^T)) V over 128 keys at a time, 256 query rows of one KV head per work item (the query heads that
+//   share it, times the new tokens), as two tiles of 128 rows that share every key / value tile, so that one tile's products
+//   run while the other's softmax does.
+//
+// The codes become fp16 operand tiles in shared memory (exactly, for K; rounded to fp16 with their scale, for V) on the way to the
+// products: nothing dequantised is written to memory, and a tile is converted once for 256 query rows.  Roles of a CTA (one per SM):
+//   warps 0-3 / 4-7  softmax of tile 0 / 1, a thread per query row.  Probabilities are taken against a reference per row, 2^(s - ref),
+//                    which moves only when the sum of a tile's probabilities could leave fp16's range: the common tile is done in
+//                    one pass without looking for its maximum; the first, the masked ones and the rare others in two.
+//   warps 8-14       conversion: codes of the next tile are on their way in registers while the present one is turned into fp16 and
+//                    stored in the 128-byte swizzle (key tiles K-major, value tiles as stored, N-major).
+//   warp 15          one thread issues the products: S_x = Q_x K^T from shared memory, O_x += P_x V with P_x in tensor memory
+//                    over the first half of S_x.
+// Tensor memory: S_0 | S_1 | O_0 | O_1.  The K scale multiplies the score beside the row's own factor (one value per 16 columns);
+// V codes times (their scale / the largest scale the row can see) times 64 are below 2^15.
+// Bound: 128 exponentials per row and tile at 16 per clock and SM take twice the products' time.
+// Work items are dealt out by CTA number, those with the most keys first; every wait is bounded.
+#include "quant_common.cuh"
+
+namespace echokv {
+
+namespace {
+
+constexpr int kCkTile = 128;                       // query rows per tile, keys per tile
+constexpr int kCkRows = 2 * kCkTile;
+constexpr int kCkSoftmaxThreads = 256, kCkConvThreads = 224;
+constexpr int kCkThreads = kCkSoftmaxThreads + kCkConvThreads + 32;
+constexpr int kCkLaunchRegs = 128;                 // 16 warps of 128 registers are all there are
+constexpr int kCkSoftmaxRegs = 176, kCkOtherRegs = 80;  // per thread of the first and of the last 8 warps: 256 (176 + 80) = 512 x 128
+constexpr int kCkChunkBytes = kCkTile * 128;       // [128 rows x 64 features] fp16, 128-byte swizzle
+constexpr int kCkRing = 4;                         // scales and V references: see where they are written
+constexpr float kCkGrow = 8.f;
+constexpr float kCkSumLimit = 32768.f;             // a row's probabilities of one tile sum to less: each fits fp16
+constexpr float kCkVScale = 64.f;
+
+struct CkTail {
+  unsigned long long q_full[2], s_full[2], p_ready[2], o_done[2];
+  unsigned long long k_full[2], k_empty[2], v_full[2], v_empty[2], drain;
+  unsigned long long pre[kCkThreads + 1];
+  unsigned long long warp_sums[32];
+  float k_scale[kCkRing][8];                       // [tile][16-key block]
+  float v_ref[kCkRing];                            // [item]
+  float red[3][kCkConvThreads / 32];
+  uint32_t tmem_base;
+  int abort_flag;
+};
+template <int D>
+__host__ __device__ constexpr size_t ck_smem_bytes() { return 1024 + (size_t)(D / 64) * kCkChunkBytes * (2 + 2 + 2) + sizeof(CkTail); }
+
+__device__ __forceinline__ uint64_t ck_desc(uint32_t smem_addr, uint32_t lead_bytes) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((smem_addr & 0x3ffffu) >> 4);
+  d |= static_cast<uint64_t>(lead_bytes >> 4) << 16;
+  d |= static_cast<uint64_t>(1024 >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(2) << 61;
+  return d;
+}
+// fp16 x fp16 -> fp32, M = 128: S with both operands K-major, O with an N-major B operand
+constexpr uint32_t kCkIdescS = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+template <int D>
+__host__ __device__ constexpr uint32_t ck_idesc_pv() { return (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((128u >> 4) << 24); }
+
+// byte offset of 16-byte piece `piece` (8 features) of row `row` in an operand tile of D features
+__device__ __forceinline__ uint32_t ck_off(int row, int piece) {
+  return (piece >> 3) * kCkChunkBytes + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
+}
+__device__ __forceinline__ void sts16(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ bool ck_wait(unsigned long long* bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
+  const uint32_t b = smem_u32(bar);
+  if (mbar_try_wait(b, parity)) return true;
+  const long long start = clock64();
+  for (;;) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (mbar_try_wait(b, parity)) return true;
+    if (*abort_flag) return false;
+    if (clock64() - start > kWaitLimitCycles) {
+      *abort_flag = 1;
+      report_opt(status, ECHOKV_ETIMEOUT);
+      return false;
+    }
+  }
+}
+__device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// tanh(y) / y for z = y^2 <= 1, to 6e-7: the polynomial of degree 5 in z that is nearest in the largest relative error (found by
+// iteratively reweighted least squares on Chebyshev points)
+__device__ __forceinline__ uint64_t tanh_poly_f2(uint64_t z) {
+  uint64_t s = pack_f2(-0.003067061770707369f, -0.003067061770707369f);
+  s = fma_f2(s, z, pack_f2(0.016743119806051254f, 0.016743119806051254f));
+  s = fma_f2(s, z, pack_f2(-0.05160567909479141f, -0.05160567909479141f));
+  s = fma_f2(s, z, pack_f2(0.13281434774398804f, 0.13281434774398804f));
+  s = fma_f2(s, z, pack_f2(-0.3332904279232025f, -0.3332904279232025f));
+  return fma_f2(s, z, pack_f2(0.9999994039535522f, 0.9999994039535522f));
+}
+
+struct CkItem {
+  int b, h, row0;                                  // rows [row0, row0 + 256) of (sequence b, KV head h)
+  int slot, len, first, n, n_rows, act;            // act: tiles that hold a row
+  int prefix, kv_end, n_tiles;
+};
+
+// chunk sequences only; w = 0 otherwise
+__device__ __forceinline__ int4 ck_seq(const QuantAttnArgs& a, int b) {
+  const QuantSeq s = quant_seq(a, b);
+  return make_int4(s.slot, s.len, s.first, s.error || !chunk_sequence(a, s) ? 0 : s.n);
+}
+__device__ __forceinline__ unsigned long long ck_items(const QuantAttnArgs& a, const int4& s) {
+  return (unsigned long long)(((long long)s.w * a.group + kCkRows - 1) / kCkRows) * a.g.n_kv_heads;
+}
+
+template <int FMT, int D>
+__global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid_constant__ QuantAttnArgs a) {
+  constexpr int NC = D / 64;
+  constexpr int kTileBytes = NC * kCkChunkBytes;
+  constexpr int kPieces = D / 16;                  // 16-code pieces of a row
+  constexpr int kRowStep = kCkConvThreads / kPieces;          // rows that the conversion threads take at once,
+  constexpr int NP = (kCkTile + kRowStep - 1) / kRowStep;     // one piece each, in this many goes
+  extern __shared__ unsigned char ck_raw[];
+  const uint32_t smem0 = (smem_u32(ck_raw) + 1023u) & ~1023u;
+  const uint32_t q_addr = smem0, k_addr = q_addr + 2 * kTileBytes, v_addr = k_addr + 2 * kTileBytes;
+  CkTail& t = *reinterpret_cast<CkTail*>(ck_raw + (smem0 - smem_u32(ck_raw)) + 6 * kTileBytes);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const QuantGeom& g = a.g;
+  const int H = g.n_kv_heads;
+  volatile int* abort_flag = &t.abort_flag;
+
+  // ---- barriers, tensor memory, and the items of the call
+  const int per = (a.B + kCkThreads - 1) / kCkThreads;
+  if (tid == 0) {
+    t.abort_flag = 0;
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(smem_u32(&t.q_full[x]), kCkTile);
+      mbar_init(smem_u32(&t.s_full[x]), 1);
+      mbar_init(smem_u32(&t.p_ready[x]), kCkTile);
+      mbar_init(smem_u32(&t.o_done[x]), 1);
+      mbar_init(smem_u32(&t.k_full[x]), kCkConvThreads);
+      mbar_init(smem_u32(&t.k_empty[x]), 1);
+      mbar_init(smem_u32(&t.v_full[x]), kCkConvThreads);
+      mbar_init(smem_u32(&t.v_empty[x]), 1);
+    }
+    mbar_init(smem_u32(&t.drain), 1);
+    mbar_fence_init();
+  }
+  {
+    unsigned long long n = 0;
+#pragma unroll 1
+    for (int b = tid * per; b < min(a.B, (tid + 1) * per); ++b) n += ck_items(a, ck_seq(a, b));
+    unsigned long long x = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned long long y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) t.warp_sums[warp] = x;
+    __syncthreads();
+    unsigned long long before = 0;
+    for (int w = 0; w < warp; ++w) before += t.warp_sums[w];
+    t.pre[tid + 1] = before + x;
+    if (tid == 0) t.pre[0] = 0;
+  }
+  if (warp == kCkThreads / 32 - 1) {
+    tmem_alloc(smem_u32(&t.tmem_base), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = t.tmem_base;
+  const unsigned long long total = t.pre[kCkThreads];
+
+  const auto get_item = [&](unsigned long long index) {
+    int lo = 0, hi = kCkThreads;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (t.pre[mid] <= index) lo = mid; else hi = mid;
+    }
+    CkItem it;
+    it.b = lo * per;
+    unsigned long long base = t.pre[lo];
+    int4 s = ck_seq(a, it.b);
+    while (base + ck_items(a, s) <= index) {
+      base += ck_items(a, s);
+      s = ck_seq(a, ++it.b);
+    }
+    it.slot = s.x; it.len = s.y; it.first = s.z; it.n = s.w;
+    it.n_rows = it.n * a.group;
+    const int rem = (int)(index - base), blocks = (it.n_rows + kCkRows - 1) / kCkRows;
+    it.h = rem % H;
+    it.row0 = (blocks - 1 - rem / H) * kCkRows;                // (the rows that see the most keys first)
+    it.act = it.n_rows - it.row0 > kCkTile ? 2 : 1;
+    it.prefix = a.prefix ? min(a.prefix[it.b], it.len) : 0;
+    const int last_row = min(it.n_rows, it.row0 + kCkRows) - 1;
+    it.kv_end = max(it.len - it.n + (last_row >> a.group_shift) + 1, it.prefix);
+    it.n_tiles = (it.kv_end + kCkTile - 1) / kCkTile;
+    return it;
+  };
+
+  if (warp >= kCkSoftmaxThreads / 32) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCkOtherRegs));
+  else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kCkSoftmaxRegs));
+  if (warp == kCkThreads / 32 - 1) {
+    // =============================== products ===================================================
+    if (lane == 0) {
+      bool alive = true;
+      uint32_t T = 0, n_item = 0, n_p[2] = {0, 0}; // tiles and items so far; tiles of either half
+      for (unsigned long long i = blockIdx.x; i < total && alive; i += gridDim.x, ++n_item) {
+        const CkItem it = get_item(i);
+        const auto issue_s = [&](int x, uint32_t tile) {
+          const uint32_t k = k_addr + (tile & 1) * kTileBytes;
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            tc_mma_bf16(tmem + x * 128, ck_desc(q_addr + x * kTileBytes + (kk >> 2) * kCkChunkBytes, 16) + 2 * (kk & 3),
+                        ck_desc(k + (kk >> 2) * kCkChunkBytes, 16) + 2 * (kk & 3), kCkIdescS, kk > 0 ? 1u : 0u);
+          tc_commit(smem_u32(&t.s_full[x]));
+          if (x == it.act - 1) tc_commit(smem_u32(&t.k_empty[tile & 1]));
+        };
+        // (of both tiles, at work or not: this thread is then never two items ahead of either's softmax warps)
+        for (int x = 0; x < 2 && alive; ++x) alive = ck_wait(&t.q_full[x], n_item & 1, abort_flag, a.status);
+        if (alive) alive = ck_wait(&t.k_full[T & 1], (T >> 1) & 1, abort_flag, a.status);
+        if (!alive) break;
+        tc_fence_after();
+        for (int x = 0; x < it.act; ++x) issue_s(x, T);
+        for (int tile = 0; tile < it.n_tiles && alive; ++tile, ++T) {
+          if (!ck_wait(&t.v_full[T & 1], (T >> 1) & 1, abort_flag, a.status)) { alive = false; break; }
+          const uint64_t vd = ck_desc(v_addr + (T & 1) * kTileBytes, kCkChunkBytes);
+          for (int x = 0; x < it.act && alive; ++x) {
+            if (!ck_wait(&t.p_ready[x], n_p[x] & 1, abort_flag, a.status)) { alive = false; break; }
+            ++n_p[x];
+            tc_fence_after();
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk)         // 16 keys: 8 columns of packed probabilities, 2048 bytes of value rows
+              tc_mma_bf16_tmem_a(tmem + 256 + x * D, tmem + x * 128 + 8 * kk, vd + 128 * kk, ck_idesc_pv<D>(),
+                                 (tile > 0 || kk > 0) ? 1u : 0u);
+            if (tile + 1 == it.n_tiles) tc_commit(smem_u32(&t.o_done[x]));
+            if (x == it.act - 1) tc_commit(smem_u32(&t.v_empty[T & 1]));
+            if (tile + 1 < it.n_tiles) {
+              if (x == 0) {
+                if (!ck_wait(&t.k_full[(T + 1) & 1], ((T + 1) >> 1) & 1, abort_flag, a.status)) { alive = false; break; }
+                tc_fence_after();
+              }
+              issue_s(x, T + 1);
+            }
+          }
+        }
+      }
+      if (!alive) {
+        // every product issued so far retires before the tensor memory is given back
+        tc_commit(smem_u32(&t.drain));
+        mbar_drain(smem_u32(&t.drain), 0);
+      }
+    }
+  } else if (warp >= kCkSoftmaxThreads / 32) {
+    // =============================== conversion =================================================
+    const int ct = tid - kCkSoftmaxThreads;
+    bool alive = true;
+    uint32_t T = 0, n_item = 0;
+    const auto conv_all = [&](bool ok) {           // barrier of the conversion threads, ANDing a flag
+      uint32_t r;
+      asm volatile(
+          "{\n\t.reg .pred p, q;\n\t"
+          "setp.ne.b32 q, %1, 0;\n\t"
+          "bar.red.and.pred p, 1, 224, q;\n\t"
+          "selp.u32 %0, 1, 0, p;\n\t}"
+          : "=r"(r)
+          : "r"(ok ? 1u : 0u)
+          : "memory");
+      return r != 0;
+    };
+    const int my_row = ct / kPieces, my_piece = ct % kPieces;   // this thread's pieces: rows my_row + kRowStep p
+    // the order of a piece's two halves that keeps a row's eight stores on different banks
+    const int half0 = (my_piece >> 2) & 1;
+    const auto store_piece = [&](uint32_t dst, int row, const uint32_t (&w)[8]) {
+      sts16(dst + ck_off(row, 2 * my_piece + half0), half0 ? w[4] : w[0], half0 ? w[5] : w[1], half0 ? w[6] : w[2], half0 ? w[7] : w[3]);
+      sts16(dst + ck_off(row, 2 * my_piece + 1 - half0), half0 ? w[0] : w[4], half0 ? w[1] : w[5], half0 ? w[2] : w[6], half0 ? w[3] : w[7]);
+    };
+    for (unsigned long long i = blockIdx.x; i < total; i += gridDim.x, ++n_item) {
+      if (!conv_all(alive)) break;                 // (a wait that ran out: all leave together)
+      const CkItem it = get_item(i);
+      const int32_t* pages = a.table + (long long)it.slot * g.max_pages;
+      const int n_full = it.len / kQuantBlock, n_codes = min(n_full, (it.kv_end + kQuantBlock - 1) / kQuantBlock);   // blocks of codes seen
+      const bool open = it.kv_end > n_full * kQuantBlock;      // the open block is seen
+      const long long open_at = ((long long)it.slot * H + it.h) * kQuantBlock * D;
+      const auto page_of = [&](int tok) {          // page of a token that exists
+        int id = pages[tok >> g.page_shift];
+        if (id < 0 || id >= g.n_pages) {
+          report_opt(a.status, ECHOKV_EBADPAGE);
+          id = 0;
+        }
+        return id;
+      };
+      const auto scale_at = [&](int blk, int page) {
+        return ((long long)page * H + it.h) * (g.page_tokens / kQuantBlock) + ((blk * kQuantBlock & (g.page_tokens - 1)) / kQuantBlock);
+      };
+      // the largest V scale that the item sees, and the largest magnitudes of its open block
+      float v_top = 0.f;
+      for (int blk = ct; blk < n_codes; blk += kCkConvThreads) v_top = fmaxf(v_top, g.scales[1][scale_at(blk, page_of(blk * kQuantBlock))]);
+      uint32_t open_k = 0, open_v = 0;
+      if (open) {
+        const int n_open = it.len - n_full * kQuantBlock;
+        const uint32_t* kt = reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(g.tail[0]) + open_at);
+        const uint32_t* vt = reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(g.tail[1]) + open_at);
+        for (int w = ct; w < n_open * D / 2; w += kCkConvThreads) {
+          open_k = __vmaxu2(open_k, kt[w] & 0x7fff7fffu);
+          open_v = __vmaxu2(open_v, vt[w] & 0x7fff7fffu);
+        }
+      }
+      open_k = __reduce_max_sync(0xffffffffu, max(open_k & 0xffff0000u, open_k << 16));
+      open_v = __reduce_max_sync(0xffffffffu, max(open_v & 0xffff0000u, open_v << 16));
+      v_top = warp_max(v_top);
+      if (lane == 0) {
+        t.red[0][ct >> 5] = v_top;
+        t.red[1][ct >> 5] = __uint_as_float(open_k);
+        t.red[2][ct >> 5] = __uint_as_float(open_v);
+      }
+      conv_all(true);
+#pragma unroll
+      for (int w = 0; w < kCkConvThreads / 32; ++w) {
+        v_top = fmaxf(v_top, t.red[0][w]);
+        open_k = max(open_k, __float_as_uint(t.red[1][w]));
+        open_v = max(open_v, __float_as_uint(t.red[2][w]));
+      }
+      // A block with an infinity or NaN: its K scale (that of the scores) is NaN, its rows are 0, so that a query that sees
+      // none of it is left alone.
+      float open_back = 1.f;
+      const bool open_bad = open_k >= 0x7f800000u || open_v >= 0x7f800000u;
+      const float open_up = scale_up_to_half(__uint_as_float(open_k), &open_back);
+      if (!open_bad) v_top = fmaxf(v_top, __uint_as_float(open_v) * (1.f / 448.f));
+      // the power of two above it
+      const uint32_t ve = v_top > 0.f ? (__float_as_uint(v_top) >> 23) + 1 : 127u;
+      const float v_ref = __uint_as_float(ve << 23), v_inv = __uint_as_float((254 - ve) << 23);
+      // (the ring: item n + 4's value overwrites item n's when the tiles of items n + 1 to n + 3 have been written, two of
+      // which the products have to have read, the first of them after the softmax warps took item n's result)
+      if (ct == 0) t.v_ref[n_item % kCkRing] = v_ref * (1.f / kCkVScale);
+
+      // codes of this thread's pieces: K's of the next tile and V's of the present one are fetched while the tile before
+      // them is waited for
+      uint4 codes[NP];
+      float vs[NP], ks_own = 0.f;
+      const auto fetch = [&](int which, int tile) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+          const int row = my_row + kRowStep * p, tok = tile * kCkTile + row, blk = tok / kQuantBlock;
+          if (row < kCkTile && blk < n_codes) {
+            const int page = page_of(tok);
+            const long long off = (((long long)page * H + it.h) * g.page_tokens + (tok & (g.page_tokens - 1))) * D + 16 * my_piece;
+            codes[p] = *reinterpret_cast<const uint4*>(g.codes[which] + off);
+            if (which) vs[p] = g.scales[1][scale_at(blk, page)];
+          }
+        }
+        if (which == 0 && ct < 8) {
+          const int blk = tile * 8 + ct;
+          ks_own = 0.f;
+          if (blk < n_codes) {
+            const long long at = scale_at(blk, page_of(blk * kQuantBlock));
+            const float v = g.scales[1][at];
+            ks_own = v == v ? g.scales[0][at] : v;
+          } else if (open && blk == n_full) {
+            ks_own = open_bad ? __uint_as_float(0x7fc00000u) : open_back;
+          }
+        }
+      };
+      // 16 features of a row of the open block as fp16 pairs, or zeros
+      const auto open_row = [&](int which, int row, float up, uint32_t (&w)[8]) {
+        const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(g.tail[which]) + open_at + (long long)row * D + 16 * my_piece;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const uint4 x = *reinterpret_cast<const uint4*>(p + 8 * q);
+          const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[4 * q + e] = h2(__uint_as_float(y[e] << 16) * up, __uint_as_float(y[e] & 0xffff0000u) * up);
+        }
+      };
+      fetch(0, 0);
+      for (int tile = 0; tile < it.n_tiles; ++tile, ++T) {
+        const int st = T & 1;
+        const uint32_t parity = ((T >> 1) & 1) ^ 1;
+        if (alive) alive = ck_wait(&t.k_empty[st], parity, abort_flag, a.status);
+        if (!alive) break;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+          const int row = my_row + kRowStep * p, tok = tile * kCkTile + row, blk = tok / kQuantBlock;
+          if (row >= kCkTile) break;
+          uint32_t w[8];
+          if (blk < n_codes) {
+            const uint32_t c4[4] = {codes[p].x, codes[p].y, codes[p].z, codes[p].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t x = codes_bias<FMT>(c4[e]);
+              w[2 * e] = codes_pair<FMT, 0>(x);
+              w[2 * e + 1] = codes_pair<FMT, 1>(x);
+            }
+          } else if (open && !open_bad && tok < it.len) {
+            open_row(0, tok - n_full * kQuantBlock, open_up, w);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = 0u;
+          }
+          store_piece(k_addr + st * kTileBytes, row, w);
+        }
+        // (the ring: tile T + 4's scales are written when S(T + 2) is complete, so after softmax(T + 1) was)
+        if (ct < 8) t.k_scale[T % kCkRing][ct] = ks_own;
+        fence_proxy_async_smem();
+        mbar_arrive(smem_u32(&t.k_full[st]));
+        fetch(1, tile);
+
+        alive = ck_wait(&t.v_empty[st], parity, abort_flag, a.status);
+        if (!alive) break;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+          const int row = my_row + kRowStep * p, tok = tile * kCkTile + row, blk = tok / kQuantBlock;
+          if (row >= kCkTile) break;
+          uint32_t w[8];
+          if (blk < n_codes && vs[p] == vs[p]) {
+            const float ratio = vs[p] * v_inv * kCkVScale;
+            const uint32_t r2 = h2(ratio, ratio);
+            const uint32_t c4[4] = {codes[p].x, codes[p].y, codes[p].z, codes[p].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t x = codes_bias<FMT>(c4[e]);
+              w[2 * e] = mul_h2(codes_pair<FMT, 0>(x), r2);
+              w[2 * e + 1] = mul_h2(codes_pair<FMT, 1>(x), r2);
+            }
+          } else if (blk >= n_codes && open && !open_bad && tok < it.len) {
+            open_row(1, tok - n_full * kQuantBlock, v_inv * kCkVScale, w);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = 0u;
+          }
+          store_piece(v_addr + st * kTileBytes, row, w);
+        }
+        fence_proxy_async_smem();
+        mbar_arrive(smem_u32(&t.v_full[st]));
+        if (tile + 1 < it.n_tiles) fetch(0, tile + 1);
+      }
+    }
+  } else {
+    // =============================== softmax ====================================================
+    const int x = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lane_base = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    const uint32_t s_addr = lane_base + x * 128, o_addr = lane_base + 256 + x * D;
+    const float cap_in = a.softcap > 0.f ? 1.f / a.softcap : 0.f, cap_out = a.softcap * kLog2e;
+    uint32_t T = 0, n_item = 0, n_mine = 0, n_done = 0;   // (of this half: tiles and results, whose barriers move with them)
+    for (unsigned long long i = blockIdx.x; i < total; i += gridDim.x, ++n_item) {
+      const CkItem it = get_item(i);
+      const int r = it.row0 + x * kCkTile + row;
+      const bool row_ok = r < it.n_rows;
+      const int qi = row_ok ? r >> a.group_shift : 0, head = it.h * a.group + (r & (a.group - 1));
+      const int pos = it.len - it.n + qi;
+      // keys [0, vis) are seen; a row of none of the queries sees everything (its scores are 0) and goes nowhere
+      const int vis = row_ok ? max(pos + 1, it.prefix) : 0x7fffffff;
+      float c_row = 0.f;
+      {
+        const uint4* qp = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (long long)(it.first + qi) * a.q_stride +
+                                                         (long long)head * D);
+        uint32_t w[D / 2];
+#pragma unroll
+        for (int p = 0; p < D / 8; ++p) {
+          uint4 v = make_uint4(0u, 0u, 0u, 0u);
+          if (row_ok) v = qp[p];
+          w[4 * p] = v.x; w[4 * p + 1] = v.y; w[4 * p + 2] = v.z; w[4 * p + 3] = v.w;
+        }
+        float top = 0.f;
+#pragma unroll
+        for (int e = 0; e < D / 2; ++e) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[e] << 16)), fabsf(__uint_as_float(w[e] & 0xffff0000u))));
+        float back;
+        const float up = scale_up_to_half(top, &back);
+        c_row = back * a.scale * (a.softcap > 0.f ? 1.f : kLog2e);
+#pragma unroll
+        for (int e = 0; e < D / 2; ++e) w[e] = h2(__uint_as_float(w[e] << 16) * up, __uint_as_float(w[e] & 0xffff0000u) * up);
+#pragma unroll
+        for (int p = 0; p < D / 8; ++p) sts16(q_addr + x * kTileBytes + ck_off(row, p), w[4 * p], w[4 * p + 1], w[4 * p + 2], w[4 * p + 3]);
+      }
+      fence_proxy_async_smem();
+      mbar_arrive(smem_u32(&t.q_full[x]));
+      if (x >= it.act) {
+        T += it.n_tiles;
+        continue;
+      }
+      const float slope2 = a.slopes && row_ok ? a.slopes[head] * kLog2e : 0.f;
+      float m_ref = -INFINITY, l_run = 0.f;
+      bool alive = true;
+      for (int tile = 0; tile < it.n_tiles; ++tile, ++T, ++n_mine) {
+        alive = __all_sync(0xffffffffu, ck_wait(&t.s_full[x], n_mine & 1, abort_flag, a.status));
+        if (!alive) break;
+        tc_fence_after();
+        const int n_vis = max(0, min(kCkTile, vis - tile * kCkTile));
+        const float* k_scale = t.k_scale[T % kCkRing];
+        uint32_t pk[2][32];                        // the packed probabilities, two keys per column
+        float psum = 0.f;
+        bool careful = true;
+        if (tile > 0 && __all_sync(0xffffffffu, n_vis == kCkTile)) {
+          // every key seen, and the reference where it is
+          uint64_t sum2[2] = {0ull, 0ull};
+          float z_top = 0.f;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t sr[32];
+            tmem_ld32_issue(s_addr + 32 * c, sr);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              const float f = c_row * k_scale[2 * c + (j >> 4)];
+              uint64_t y = pack_u2(sr[j], sr[j + 1]);
+              if (a.softcap > 0.f) {
+                y = mul_f2(y, pack_f2(f * cap_in, f * cap_in));
+                const uint64_t z = mul_f2(y, y);
+                float z0, z1;
+                unpack_f2(z, z0, z1);
+                z_top = fmaxf(z_top, fmaxf(z0, z1));
+                y = mul_f2(y, tanh_poly_f2(z));
+                if (a.slopes) {
+                  const float d0 = slope2 * fabsf((float)(pos - (tile * kCkTile + 32 * c + j))), d1 = slope2 * fabsf((float)(pos - (tile * kCkTile + 32 * c + j + 1)));
+                  y = fma_f2(y, pack_f2(cap_out, cap_out), pack_f2(-m_ref - d0, -m_ref - d1));
+                } else {
+                  y = fma_f2(y, pack_f2(cap_out, cap_out), pack_f2(-m_ref, -m_ref));
+                }
+              } else if (a.slopes) {
+                const float d0 = slope2 * fabsf((float)(pos - (tile * kCkTile + 32 * c + j))), d1 = slope2 * fabsf((float)(pos - (tile * kCkTile + 32 * c + j + 1)));
+                y = fma_f2(y, pack_f2(f, f), pack_f2(-m_ref - d0, -m_ref - d1));
+              } else {
+                y = fma_f2(y, pack_f2(f, f), pack_f2(-m_ref, -m_ref));
+              }
+              float y0, y1;
+              unpack_f2(y, y0, y1);
+              const float p0 = exp2_approx(y0), p1 = exp2_approx(y1);
+              sum2[(j >> 1) & 1] = add_f2(sum2[(j >> 1) & 1], pack_f2(p0, p1));
+              pk[c >> 1][16 * (c & 1) + (j >> 1)] = h2(p0, p1);
+            }
+          }
+          float a0, a1, b0, b1;
+          unpack_f2(sum2[0], a0, a1);
+          unpack_f2(sum2[1], b0, b1);
+          psum = (a0 + a1) + (b0 + b1);
+          // (the polynomial for tanh holds up to 1)
+          careful = !(psum < kCkSumLimit) || z_top > 1.f;
+        }
+        if (__any_sync(0xffffffffu, careful)) {
+          const auto score = [&](uint32_t s, int key, float f) {
+            float y = __uint_as_float(s) * f;
+            if (a.softcap > 0.f) y = cap_out * tanh_f32(y * cap_in);
+            if (a.slopes) y -= slope2 * fabsf((float)(pos - (tile * kCkTile + key)));
+            return y;
+          };
+          float mx = -INFINITY;
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            uint32_t sr[32];
+            tmem_ld32_issue(s_addr + 32 * c, sr);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (32 * c + j < n_vis) mx = fmaxf(mx, score(sr[j], 32 * c + j, c_row * k_scale[2 * c + (j >> 4)]));
+          }
+          const bool grow = mx > m_ref + kCkGrow;
+          float alpha = 1.f;
+          if (grow) {
+            alpha = exp2_approx(m_ref - mx);       // 0 on the first tile
+            m_ref = mx;
+            l_run *= alpha;
+          }
+          if (tile > 0 && __any_sync(0xffffffffu, grow)) {
+            // O_x is at rest (the product that wrote S_x came after every earlier one): rescale this row
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t orow[32];
+              tmem_ld32_issue(o_addr + 32 * c, orow);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 32; ++j) orow[j] = __float_as_uint(__uint_as_float(orow[j]) * alpha);
+              tmem_st32(o_addr + 32 * c, orow);
+            }
+          }
+          psum = 0.f;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t sr[32];
+            tmem_ld32_issue(s_addr + 32 * c, sr);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              const float f = c_row * k_scale[2 * c + (j >> 4)];
+              const float p0 = 32 * c + j < n_vis ? exp2_approx(score(sr[j], 32 * c + j, f) - m_ref) : 0.f;
+              const float p1 = 32 * c + j + 1 < n_vis ? exp2_approx(score(sr[j + 1], 32 * c + j + 1, f) - m_ref) : 0.f;
+              psum += p0 + p1;
+              pk[c >> 1][16 * (c & 1) + (j >> 1)] = h2(p0, p1);
+            }
+          }
+        }
+        l_run += psum;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) tmem_st32(s_addr + 32 * c, pk[c]);
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(smem_u32(&t.p_ready[x]));
+      }
+      if (!alive) break;
+      // ---- the row's result
+      alive = __all_sync(0xffffffffu, ck_wait(&t.o_done[x], n_done & 1, abort_flag, a.status));
+      if (!alive) break;
+      ++n_done;
+      tc_fence_after();
+      const float inv = l_run == 0.f ? 0.f : t.v_ref[n_item % kCkRing] / l_run;
+      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.out) + ((long long)(it.first + qi) * a.n_q_heads + head) * D;
+#pragma unroll 1
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t orow[32];
+        tmem_ld32_issue(o_addr + 32 * c, orow);
+        tmem_ld_wait();
+        if (row_ok) {
+#pragma unroll
+          for (int j = 0; j < 32; j += 8) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(orow[j + e]) * inv;
+            store16<__nv_bfloat16>(dst + 32 * c + j, v);
+          }
+        }
+      }
+      tc_fence_before();
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kCkThreads / 32 - 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int FMT, int D>
+cudaError_t launch(const QuantAttnArgs& a, int sm_count, cudaStream_t stream) {
+  constexpr size_t smem = ck_smem_bytes<D>();
+  static_assert(smem <= 227 * 1024, "shared memory of one CTA");
+  static_assert(kCkThreads == 512 && 256 * (kCkSoftmaxRegs + kCkOtherRegs) <= kCkThreads * kCkLaunchRegs, "registers of the launch");
+  // the warps' shares of the registers must be there at launch, or the ones that ask for more would wait for good
+  static const bool fits = [] {
+    cudaFuncAttributes f;
+    return cudaFuncGetAttributes(&f, quant_chunk_kernel<FMT, D>) == cudaSuccess && f.numRegs == kCkLaunchRegs;
+  }();
+  if (!fits) return cudaErrorInvalidConfiguration;
+  const cudaError_t e = cudaFuncSetAttribute(quant_chunk_kernel<FMT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  quant_chunk_kernel<FMT, D><<<sm_count, kCkThreads, smem, stream>>>(a);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_quant_chunk(const QuantAttnArgs& a, int sm_count, cudaStream_t stream) {
+  const bool i8 = a.format == ECHOKV_INT8;
+  if (a.g.head_dim == 128) return i8 ? launch<ECHOKV_INT8, 128>(a, sm_count, stream) : launch<ECHOKV_E4M3, 128>(a, sm_count, stream);
+  return i8 ? launch<ECHOKV_INT8, 64>(a, sm_count, stream) : launch<ECHOKV_E4M3, 64>(a, sm_count, stream);
+}
+
+}  // namespace echokv

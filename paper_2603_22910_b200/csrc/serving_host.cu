@@ -11,6 +11,8 @@ using namespace echokv;
 namespace {
 
 constexpr int kMaxDevices = 64;
+constexpr int kChunkRows = 64;      // query rows per KV head (new tokens x query heads that share it) from which a bf16 sequence is the chunk
+                                    // kernel's
 
 int sm_count_of(int device, int* out) {
   static std::mutex mutex;
@@ -275,12 +277,14 @@ int echokv_quant_attention(const echokv_config* cfg, const echokv_quant_cache* c
   a.n_q_heads = cfg->n_q_heads; a.group = cfg->n_q_heads / cfg->n_kv_heads; a.group_shift = log2_of(a.group);
   a.dtype = cfg->dtype; a.format = cache->format;
   a.scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.0f / std::sqrt((float)cfg->head_dim);
-  a.chunk_rows = 0;
+  a.chunk_rows = cfg->dtype == ECHOKV_BF16 && (long long)max_new * a.group >= kChunkRows ? kChunkRows : 0;
   a.ws = static_cast<unsigned char*>(workspace);
   a.status = dev_status;
   OnDevice dev(cfg->device);
   if (!dev.ok()) return ECHOKV_ECUDA;
-  return launch_quant_attn(a, dev.sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess ? ECHOKV_OK : ECHOKV_ECUDA;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (a.chunk_rows > 0 && launch_quant_chunk(a, dev.sm_count, s) != cudaSuccess) return ECHOKV_ECUDA;
+  return launch_quant_attn(a, dev.sm_count, s) == cudaSuccess ? ECHOKV_OK : ECHOKV_ECUDA;
 }
 
 }  // extern "C"

@@ -143,7 +143,7 @@ def attend(q, k, v, scale, softcap=0.0, slopes=None, prefix=0):
     return out, size
 
 
-def tolerance(ref, size, L, out_eps, half_p, softcap=0.0, slopes=None):
+def tolerance(ref, size, L, out_eps, half_p, half_v=False, softcap=0.0, slopes=None):
     """How far a row may be off, from the roundings on its way (first order, absolute, per element).
 
     x: products accumulate in fp32, 16 at a time: at most d / 16 = 8 sums of partly truncated terms, and the operands carry 22 bits
@@ -151,11 +151,12 @@ def tolerance(ref, size, L, out_eps, half_p, softcap=0.0, slopes=None):
        units: 2^-22 of the largest |bias|.  A probability is off by the score's error, the output by twice that times max |v|.
     p: 2^x 2^-21, times the V scale and back 2^-21, as an fp16 pair 2^-21; summed over L / 16 blocks in fp32: L / 16 2^-23.
     half_p (bf16 queries): probabilities as single fp16, half a step of which is 2^-11 of each.
+    half_v (chunks): a value is its code times its block's scale over the largest, both rounded to fp16: 2^-11 each.
     out: half a step of its type, out_eps / 2 = 2^-8 |ref| in bf16 and 2^-24 |ref| in fp32."""
     dx = 2.0 ** -19 * size[..., 0]
     if softcap:
         dx = dx + 2.0 ** -20 * softcap
     if slopes is not None:
         dx = dx + 2.0 ** -22 * np.abs(np.asarray(slopes, dtype=np.float64))[None, :] * L * math.log2(math.e)
-    dp = 3 * 2.0 ** -21 + L / 16 * 2.0 ** -23 + (2.0 ** -11 if half_p else 0.0)
+    dp = 3 * 2.0 ** -21 + L / 16 * 2.0 ** -23 + (2.0 ** -11 if half_p else 0.0) + (2.0 ** -10 if half_v else 0.0)
     return (out_eps / 2) * np.abs(ref) + ((2 * dx + dp) * size[..., 1])[..., None] * (1 + out_eps)

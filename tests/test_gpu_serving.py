@@ -11,6 +11,7 @@ pytestmark = pytest.mark.gpu
 DT = {"bf16": (binding.ECHOKV_BF16, torch.bfloat16), "fp32": (binding.ECHOKV_FP32, torch.float32)}
 EPS = {"bf16": 2.0 ** -7, "fp32": 2.0 ** -23}
 BLOCK = 16
+CHUNK_ROWS = 64         # query rows per KV head from which bf16 sequences take the chunk kernel
 
 
 def config(n_q=8, n_kv=2, d=128, page=16, batch=4, pages=16, n_pages=64, dtype="bf16", **kw):
@@ -335,7 +336,8 @@ def check_attention(p, new, q, out, softcap=0.0, slopes=None, prefix=None):
         if n:
             k, v = p.ref.values(p.ref.k[b]), p.ref.values(p.ref.v[b])
             ref, size = R.attend(f64(q[at:at + n]), k, v, cfg.head_dim ** -0.5, softcap, slopes, prefix[b] if prefix else 0)
-            tol = R.tolerance(ref, size, p.lens[b], EPS[p.dtype], p.dtype == "bf16", softcap, slopes)
+            tol = R.tolerance(ref, size, p.lens[b], EPS[p.dtype], p.dtype == "bf16",
+                              p.dtype == "bf16" and n * cfg.n_q_heads // cfg.n_kv_heads >= CHUNK_ROWS, softcap, slopes)
             err = np.abs(f64(out[at:at + n]) - ref)
             assert (err <= tol).all(), (b, n, p.lens[b], float((err / tol).max()))
         at += n
