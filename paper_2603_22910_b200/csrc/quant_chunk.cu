@@ -6,11 +6,13 @@
 //
 // The codes become fp16 operand tiles in shared memory (exactly, for K; rounded to fp16 with their scale, for V) on the way to the
 // products: nothing dequantised is written to memory, and a tile is converted once for 256 query rows.  Roles of a CTA (one per SM):
-//   warps 0-3 / 4-7  softmax of tile 0 / 1, a thread per query row.  Probabilities are taken against a reference per row, 2^(s - ref),
-//                    which moves only when the sum of a tile's probabilities could leave fp16's range: the common tile is done in
-//                    one pass without looking for its maximum; the first, the masked ones and the rare others in two.
+//   warps 0-3 / 4-7  softmax of tile 0 / 1, a thread per query row, 32 keys at a time.  Probabilities are taken against a reference per
+//                    row, 2^(s - ref), a whole number that moves only when 32 probabilities could leave fp16's range: the
+//                    common piece is done in one pass without looking for its maximum.  When it moves, what the row has so far --
+//                    its sum, its output, the probabilities of this tile already stored -- is scaled by a power of two.
 //   warps 8-14       conversion: codes of the next tile are on their way in registers while the present one is turned into fp16 and
-//                    stored in the 128-byte swizzle (key tiles K-major, value tiles as stored, N-major).
+//                    stored in the 128-byte swizzle (key tiles K-major, value tiles as stored, N-major).  Eight lanes of a
+//                    warp keep the pages and scales of the tile's eight blocks.
 //   warp 15          one thread issues the products: S_x = Q_x K^T from shared memory, O_x += P_x V with P_x in tensor memory
 //                    over the first half of S_x.
 // Tensor memory: S_0 | S_1 | O_0 | O_1.  The K scale multiplies the score beside the row's own factor (one value per 16 columns);
@@ -27,12 +29,9 @@ constexpr int kCkTile = 128;                       // query rows per tile, keys 
 constexpr int kCkRows = 2 * kCkTile;
 constexpr int kCkSoftmaxThreads = 256, kCkConvThreads = 224;
 constexpr int kCkThreads = kCkSoftmaxThreads + kCkConvThreads + 32;
-constexpr int kCkLaunchRegs = 128;                 // 16 warps of 128 registers are all there are
-constexpr int kCkSoftmaxRegs = 176, kCkOtherRegs = 80;  // per thread of the first and of the last 8 warps: 256 (176 + 80) = 512 x 128
 constexpr int kCkChunkBytes = kCkTile * 128;       // [128 rows x 64 features] fp16, 128-byte swizzle
 constexpr int kCkRing = 4;                         // scales and V references: see where they are written
-constexpr float kCkGrow = 8.f;
-constexpr float kCkSumLimit = 32768.f;             // a row's probabilities of one tile sum to less: each fits fp16
+constexpr float kCkSumLimit = 32768.f;             // a row's 32 probabilities sum to less: each fits fp16
 constexpr float kCkVScale = 64.f;
 
 struct CkTail {
@@ -90,6 +89,24 @@ __device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
+}
+
+// 16 consecutive columns of this thread's lane, into the first half of r (valid after tmem_ld_wait)
+__device__ __forceinline__ void tmem_ld16_issue(uint32_t addr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st16_regs(uint32_t addr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
 }
 
 // tanh(y) / y for z = y^2 <= 1, to 6e-7: the polynomial of degree 5 in z that is nearest in the largest relative error (found by
@@ -205,8 +222,6 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
     return it;
   };
 
-  if (warp >= kCkSoftmaxThreads / 32) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCkOtherRegs));
-  else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kCkSoftmaxRegs));
   if (warp == kCkThreads / 32 - 1) {
     // =============================== products ===================================================
     if (lane == 0) {
@@ -341,30 +356,37 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       // which the products have to have read, the first of them after the softmax warps took item n's result)
       if (ct == 0) t.v_ref[n_item % kCkRing] = v_ref * (1.f / kCkVScale);
 
-      // codes of this thread's pieces: K's of the next tile and V's of the present one are fetched while the tile before
-      // them is waited for
-      uint4 codes[NP];
-      float vs[NP], ks_own = 0.f;
-      const auto fetch = [&](int which, int tile) {
+      // lane l < 8 keeps page and scales of block l of a tile, fetched two tiles (pages) and one (scales) ahead
+      const auto load_page = [&](int tile) {
+        const int blk = tile * 8 + lane;
+        return lane < 8 && blk < n_codes ? page_of(blk * kQuantBlock) : 0;
+      };
+      float ks_next = 0.f, vs_next = 0.f, vs_cur;
+      const auto load_scales = [&](int tile, int page) {
+        const int blk = tile * 8 + lane;
+        ks_next = vs_next = 0.f;
+        if (lane < 8 && blk < n_codes) {
+          const long long at = scale_at(blk, page);
+          vs_next = g.scales[1][at];
+          ks_next = g.scales[0][at];
+          if (vs_next != vs_next) ks_next = vs_next;
+        } else if (open && blk == n_full) {
+          ks_next = open_bad ? __uint_as_float(0x7fc00000u) : open_back;
+        }
+      };
+      // codes of this thread's pieces, fetched one tile ahead
+      uint4 kc[NP], vc[NP];
+      const unsigned char* k_base = g.codes[0] + 16 * my_piece;
+      const unsigned char* v_base = g.codes[1] + 16 * my_piece;
+      const auto fetch = [&](int tile, int page8) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-          const int row = my_row + kRowStep * p, tok = tile * kCkTile + row, blk = tok / kQuantBlock;
-          if (row < kCkTile && blk < n_codes) {
-            const int page = page_of(tok);
-            const long long off = (((long long)page * H + it.h) * g.page_tokens + (tok & (g.page_tokens - 1))) * D + 16 * my_piece;
-            codes[p] = *reinterpret_cast<const uint4*>(g.codes[which] + off);
-            if (which) vs[p] = g.scales[1][scale_at(blk, page)];
-          }
-        }
-        if (which == 0 && ct < 8) {
-          const int blk = tile * 8 + ct;
-          ks_own = 0.f;
-          if (blk < n_codes) {
-            const long long at = scale_at(blk, page_of(blk * kQuantBlock));
-            const float v = g.scales[1][at];
-            ks_own = v == v ? g.scales[0][at] : v;
-          } else if (open && blk == n_full) {
-            ks_own = open_bad ? __uint_as_float(0x7fc00000u) : open_back;
+          const int row = my_row + kRowStep * p, tok = tile * kCkTile + row;
+          const int page = __shfl_sync(0xffffffffu, page8, (row >> 4) & 7);
+          if (row < kCkTile && tok < n_codes * kQuantBlock) {
+            const long long off = (long long)((page * H + it.h) * g.page_tokens + (tok & (g.page_tokens - 1))) * D;
+            kc[p] = *reinterpret_cast<const uint4*>(k_base + off);
+            vc[p] = *reinterpret_cast<const uint4*>(v_base + off);
           }
         }
       };
@@ -379,11 +401,13 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           for (int e = 0; e < 4; ++e) w[4 * q + e] = h2(__uint_as_float(y[e] << 16) * up, __uint_as_float(y[e] & 0xffff0000u) * up);
         }
       };
-      fetch(0, 0);
+      int page8 = load_page(0), page8_next = load_page(1);
+      load_scales(0, page8);
+      fetch(0, page8);
       for (int tile = 0; tile < it.n_tiles; ++tile, ++T) {
         const int st = T & 1;
         const uint32_t parity = ((T >> 1) & 1) ^ 1;
-        if (alive) alive = ck_wait(&t.k_empty[st], parity, abort_flag, a.status);
+        alive = __all_sync(0xffffffffu, ck_wait(&t.k_empty[st], parity, abort_flag, a.status));
         if (!alive) break;
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
@@ -391,7 +415,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           if (row >= kCkTile) break;
           uint32_t w[8];
           if (blk < n_codes) {
-            const uint32_t c4[4] = {codes[p].x, codes[p].y, codes[p].z, codes[p].w};
+            const uint32_t c4[4] = {kc[p].x, kc[p].y, kc[p].z, kc[p].w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const uint32_t x = codes_bias<FMT>(c4[e]);
@@ -407,22 +431,23 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           store_piece(k_addr + st * kTileBytes, row, w);
         }
         // (the ring: tile T + 4's scales are written when S(T + 2) is complete, so after softmax(T + 1) was)
-        if (ct < 8) t.k_scale[T % kCkRing][ct] = ks_own;
+        if (ct < 8) t.k_scale[T % kCkRing][ct] = ks_next;
+        vs_cur = vs_next;
         fence_proxy_async_smem();
         mbar_arrive(smem_u32(&t.k_full[st]));
-        fetch(1, tile);
 
-        alive = ck_wait(&t.v_empty[st], parity, abort_flag, a.status);
+        alive = __all_sync(0xffffffffu, ck_wait(&t.v_empty[st], parity, abort_flag, a.status));
         if (!alive) break;
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
           const int row = my_row + kRowStep * p, tok = tile * kCkTile + row, blk = tok / kQuantBlock;
+          const float v_scale = __shfl_sync(0xffffffffu, vs_cur, (row >> 4) & 7);
           if (row >= kCkTile) break;
           uint32_t w[8];
-          if (blk < n_codes && vs[p] == vs[p]) {
-            const float ratio = vs[p] * v_inv * kCkVScale;
+          if (blk < n_codes && v_scale == v_scale) {
+            const float ratio = v_scale * v_inv * kCkVScale;
             const uint32_t r2 = h2(ratio, ratio);
-            const uint32_t c4[4] = {codes[p].x, codes[p].y, codes[p].z, codes[p].w};
+            const uint32_t c4[4] = {vc[p].x, vc[p].y, vc[p].z, vc[p].w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const uint32_t x = codes_bias<FMT>(c4[e]);
@@ -439,7 +464,12 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         }
         fence_proxy_async_smem();
         mbar_arrive(smem_u32(&t.v_full[st]));
-        if (tile + 1 < it.n_tiles) fetch(0, tile + 1);
+        if (tile + 1 < it.n_tiles) {
+          page8 = page8_next;
+          fetch(tile + 1, page8);
+          load_scales(tile + 1, page8);
+          page8_next = load_page(tile + 2);
+        }
       }
     }
   } else {
@@ -447,6 +477,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
     const int x = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lane_base = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t s_addr = lane_base + x * 128, o_addr = lane_base + 256 + x * D;
+    const bool plain = !(a.softcap > 0.f) && a.slopes == nullptr;
     const float cap_in = a.softcap > 0.f ? 1.f / a.softcap : 0.f, cap_out = a.softcap * kLog2e;
     uint32_t T = 0, n_item = 0, n_mine = 0, n_done = 0;   // (of this half: tiles and results, whose barriers move with them)
     for (unsigned long long i = blockIdx.x; i < total; i += gridDim.x, ++n_item) {
@@ -486,118 +517,118 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         continue;
       }
       const float slope2 = a.slopes && row_ok ? a.slopes[head] * kLog2e : 0.f;
-      float m_ref = -INFINITY, l_run = 0.f;
-      bool alive = true;
+      float m_ref = 0.f, l_run = 0.f;
+      bool alive = true, started = false;          // started: the row has seen a key, and m_ref is its reference
       for (int tile = 0; tile < it.n_tiles; ++tile, ++T, ++n_mine) {
         alive = __all_sync(0xffffffffu, ck_wait(&t.s_full[x], n_mine & 1, abort_flag, a.status));
         if (!alive) break;
         tc_fence_after();
         const int n_vis = max(0, min(kCkTile, vis - tile * kCkTile));
         const float* k_scale = t.k_scale[T % kCkRing];
-        uint32_t pk[2][32];                        // the packed probabilities, two keys per column
-        float psum = 0.f;
-        bool careful = true;
-        if (tile > 0 && __all_sync(0xffffffffu, n_vis == kCkTile)) {
-          // every key seen, and the reference where it is
-          uint64_t sum2[2] = {0ull, 0ull};
-          float z_top = 0.f;
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+          uint32_t sr[32], pk[16];
+          tmem_ld32_issue(s_addr + 32 * c, sr);
+          float f[2] = {c_row * k_scale[2 * c], c_row * k_scale[2 * c + 1]};     // (16 keys each)
+          const int key0 = tile * kCkTile + 32 * c;
+          const bool masked = __any_sync(0xffffffffu, n_vis < 32 * c + 32);
+          tmem_ld_wait();
+          if (!plain || masked) {
+            // scores in place
+            bool done = false;
+            if (a.softcap > 0.f && !a.slopes && !masked) {
+              uint64_t y[16];
+              float top = 0.f;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t sr[32];
-            tmem_ld32_issue(s_addr + 32 * c, sr);
-            tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-              const float f = c_row * k_scale[2 * c + (j >> 4)];
-              uint64_t y = pack_u2(sr[j], sr[j + 1]);
-              if (a.softcap > 0.f) {
-                y = mul_f2(y, pack_f2(f * cap_in, f * cap_in));
-                const uint64_t z = mul_f2(y, y);
-                float z0, z1;
-                unpack_f2(z, z0, z1);
-                z_top = fmaxf(z_top, fmaxf(z0, z1));
-                y = mul_f2(y, tanh_poly_f2(z));
-                if (a.slopes) {
-                  const float d0 = slope2 * fabsf((float)(pos - (tile * kCkTile + 32 * c + j))), d1 = slope2 * fabsf((float)(pos - (tile * kCkTile + 32 * c + j + 1)));
-                  y = fma_f2(y, pack_f2(cap_out, cap_out), pack_f2(-m_ref - d0, -m_ref - d1));
-                } else {
-                  y = fma_f2(y, pack_f2(cap_out, cap_out), pack_f2(-m_ref, -m_ref));
-                }
-              } else if (a.slopes) {
-                const float d0 = slope2 * fabsf((float)(pos - (tile * kCkTile + 32 * c + j))), d1 = slope2 * fabsf((float)(pos - (tile * kCkTile + 32 * c + j + 1)));
-                y = fma_f2(y, pack_f2(f, f), pack_f2(-m_ref - d0, -m_ref - d1));
-              } else {
-                y = fma_f2(y, pack_f2(f, f), pack_f2(-m_ref, -m_ref));
+              for (int j = 0; j < 16; ++j) {
+                const float g2 = f[j >> 3] * cap_in;
+                y[j] = mul_f2(pack_u2(sr[2 * j], sr[2 * j + 1]), pack_f2(g2, g2));
+                float y0, y1;
+                unpack_f2(y[j], y0, y1);
+                top = fmaxf(top, fmaxf(fabsf(y0), fabsf(y1)));
               }
-              float y0, y1;
-              unpack_f2(y, y0, y1);
-              const float p0 = exp2_approx(y0), p1 = exp2_approx(y1);
-              sum2[(j >> 1) & 1] = add_f2(sum2[(j >> 1) & 1], pack_f2(p0, p1));
-              pk[c >> 1][16 * (c & 1) + (j >> 1)] = h2(p0, p1);
-            }
-          }
-          float a0, a1, b0, b1;
-          unpack_f2(sum2[0], a0, a1);
-          unpack_f2(sum2[1], b0, b1);
-          psum = (a0 + a1) + (b0 + b1);
-          // (the polynomial for tanh holds up to 1)
-          careful = !(psum < kCkSumLimit) || z_top > 1.f;
-        }
-        if (__any_sync(0xffffffffu, careful)) {
-          const auto score = [&](uint32_t s, int key, float f) {
-            float y = __uint_as_float(s) * f;
-            if (a.softcap > 0.f) y = cap_out * tanh_f32(y * cap_in);
-            if (a.slopes) y -= slope2 * fabsf((float)(pos - (tile * kCkTile + key)));
-            return y;
-          };
-          float mx = -INFINITY;
-#pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
-            uint32_t sr[32];
-            tmem_ld32_issue(s_addr + 32 * c, sr);
-            tmem_ld_wait();
+              // (the polynomial holds up to 1; a NaN is smaller than anything here and stays one)
+              if (__all_sync(0xffffffffu, top <= 1.f)) {
+                done = true;
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (32 * c + j < n_vis) mx = fmaxf(mx, score(sr[j], 32 * c + j, c_row * k_scale[2 * c + (j >> 4)]));
+                for (int j = 0; j < 16; ++j) {
+                  const uint64_t z = mul_f2(mul_f2(y[j], tanh_poly_f2(mul_f2(y[j], y[j]))), pack_f2(cap_out, cap_out));
+                  unpack_u2(z, sr[2 * j], sr[2 * j + 1]);
+                }
+              }
+            }
+            if (!done) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) {
+                float y = __uint_as_float(sr[j]) * f[j >> 4];
+                if (a.softcap > 0.f) y = cap_out * tanh_f32(y * cap_in);
+                if (a.slopes) y -= slope2 * fabsf((float)(pos - key0 - j));
+                sr[j] = __float_as_uint(32 * c + j < n_vis ? y : -INFINITY);
+              }
+            }
+            f[0] = f[1] = 1.f;
           }
-          const bool grow = mx > m_ref + kCkGrow;
-          float alpha = 1.f;
-          if (grow) {
-            alpha = exp2_approx(m_ref - mx);       // 0 on the first tile
-            m_ref = mx;
-            l_run *= alpha;
-          }
-          if (tile > 0 && __any_sync(0xffffffffu, grow)) {
-            // O_x is at rest (the product that wrote S_x came after every earlier one): rescale this row
+          float sum = 0.f;
 #pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
-              uint32_t orow[32];
-              tmem_ld32_issue(o_addr + 32 * c, orow);
+          for (int attempt = 0;; ++attempt) {
+            uint64_t sum2[2] = {0ull, 0ull};
+            const uint64_t nm = pack_f2(-m_ref, -m_ref);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              float y0, y1;
+              unpack_f2(fma_f2(pack_u2(sr[2 * j], sr[2 * j + 1]), pack_f2(f[j >> 3], f[j >> 3]), nm), y0, y1);
+              const float p0 = exp2_approx(y0), p1 = exp2_approx(y1);
+              sum2[j & 1] = add_f2(sum2[j & 1], pack_f2(p0, p1));
+              pk[j] = h2(p0, p1);
+            }
+            float a0, a1, b0, b1;
+            unpack_f2(sum2[0], a0, a1);
+            unpack_f2(sum2[1], b0, b1);
+            sum = (a0 + a1) + (b0 + b1);
+            const bool move = !(sum < kCkSumLimit) || !started;
+            if (attempt > 0 || !__any_sync(0xffffffffu, move)) break;
+            // the reference of some row moves
+            float alpha = 1.f;
+            if (move) {
+              float mx = -INFINITY;
+#pragma unroll
+              for (int j = 0; j < 32; ++j) mx = fmaxf(mx, __uint_as_float(sr[j]) * f[j >> 4]);
+              if (!started ? mx > -INFINITY : mx > m_ref) {
+                const float m = ceilf(mx);
+                if (started) alpha = exp2_approx(m_ref - m);
+                m_ref = m;
+                started = true;
+              }
+              l_run *= alpha;
+            }
+            const uint32_t alpha2 = h2(alpha, alpha);
+#pragma unroll 1
+            for (int cc = 0; cc < c; ++cc) {       // probabilities of this tile
+              uint32_t old[32];
+              tmem_ld16_issue(s_addr + 16 * cc, old);
               tmem_ld_wait();
 #pragma unroll
-              for (int j = 0; j < 32; ++j) orow[j] = __float_as_uint(__uint_as_float(orow[j]) * alpha);
-              tmem_st32(o_addr + 32 * c, orow);
+              for (int j = 0; j < 16; ++j) old[j] = mul_h2(old[j], alpha2);
+              tmem_st16(s_addr + 16 * cc, old);
             }
-          }
-          psum = 0.f;
+            if (tile > 0) {
+              // O_x is at rest (the product that wrote S_x came after every earlier one)
+#pragma unroll 1
+              for (int cc = 0; cc < D / 16; ++cc) {
+                uint32_t old[32];
+                tmem_ld16_issue(o_addr + 16 * cc, old);
+                tmem_ld_wait();
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t sr[32];
-            tmem_ld32_issue(s_addr + 32 * c, sr);
-            tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-              const float f = c_row * k_scale[2 * c + (j >> 4)];
-              const float p0 = 32 * c + j < n_vis ? exp2_approx(score(sr[j], 32 * c + j, f) - m_ref) : 0.f;
-              const float p1 = 32 * c + j + 1 < n_vis ? exp2_approx(score(sr[j + 1], 32 * c + j + 1, f) - m_ref) : 0.f;
-              psum += p0 + p1;
-              pk[c >> 1][16 * (c & 1) + (j >> 1)] = h2(p0, p1);
+                for (int j = 0; j < 16; ++j) old[j] = __float_as_uint(__uint_as_float(old[j]) * alpha);
+                tmem_st16(o_addr + 16 * cc, old);
+              }
             }
+            tmem_st_wait();
           }
+          l_run += sum;
+          // over scores that have been read: columns 16 c .. of the tile's 128
+          tmem_st16_regs(s_addr + 16 * c, pk);
         }
-        l_run += psum;
-#pragma unroll
-        for (int c = 0; c < 2; ++c) tmem_st32(s_addr + 32 * c, pk[c]);
         tmem_st_wait();
         tc_fence_before();
         mbar_arrive(smem_u32(&t.p_ready[x]));
@@ -640,13 +671,6 @@ template <int FMT, int D>
 cudaError_t launch(const QuantAttnArgs& a, int sm_count, cudaStream_t stream) {
   constexpr size_t smem = ck_smem_bytes<D>();
   static_assert(smem <= 227 * 1024, "shared memory of one CTA");
-  static_assert(kCkThreads == 512 && 256 * (kCkSoftmaxRegs + kCkOtherRegs) <= kCkThreads * kCkLaunchRegs, "registers of the launch");
-  // the warps' shares of the registers must be there at launch, or the ones that ask for more would wait for good
-  static const bool fits = [] {
-    cudaFuncAttributes f;
-    return cudaFuncGetAttributes(&f, quant_chunk_kernel<FMT, D>) == cudaSuccess && f.numRegs == kCkLaunchRegs;
-  }();
-  if (!fits) return cudaErrorInvalidConfiguration;
   const cudaError_t e = cudaFuncSetAttribute(quant_chunk_kernel<FMT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   quant_chunk_kernel<FMT, D><<<sm_count, kCkThreads, smem, stream>>>(a);
