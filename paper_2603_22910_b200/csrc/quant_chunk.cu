@@ -290,12 +290,13 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           : "memory");
       return r != 0;
     };
-    const int my_row = ct / kPieces, my_piece = ct % kPieces;   // this thread's pieces: rows my_row + kRowStep p
-    // the order of a piece's two halves that keeps a row's eight stores on different banks
-    const int half0 = (my_piece >> 2) & 1;
+    // this thread's pieces: piece my_piece of rows my_row + kRowStep p.  Eight lanes that store together take four pieces of
+    // an even row and of the next one: eight different banks in the swizzle.
+    const int my_row = D == 128 ? (ct >> 5) * 4 + (lane >> 4) * 2 + ((lane >> 2) & 1) : ct / kPieces;
+    const int my_piece = D == 128 ? ((lane >> 3) & 1) * 4 + (lane & 3) : ct % kPieces;
     const auto store_piece = [&](uint32_t dst, int row, const uint32_t (&w)[8]) {
-      sts16(dst + ck_off(row, 2 * my_piece + half0), half0 ? w[4] : w[0], half0 ? w[5] : w[1], half0 ? w[6] : w[2], half0 ? w[7] : w[3]);
-      sts16(dst + ck_off(row, 2 * my_piece + 1 - half0), half0 ? w[0] : w[4], half0 ? w[1] : w[5], half0 ? w[2] : w[6], half0 ? w[3] : w[7]);
+      sts16(dst + ck_off(row, 2 * my_piece), w[0], w[1], w[2], w[3]);
+      sts16(dst + ck_off(row, 2 * my_piece + 1), w[4], w[5], w[6], w[7]);
     };
     for (unsigned long long i = blockIdx.x; i < total; i += gridDim.x, ++n_item) {
       if (!conv_all(alive)) break;                 // (a wait that ran out: all leave together)
@@ -356,10 +357,18 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       // which the products have to have read, the first of them after the softmax warps took item n's result)
       if (ct == 0) t.v_ref[n_item % kCkRing] = v_ref * (1.f / kCkVScale);
 
-      // lane l < 8 keeps page and scales of block l of a tile, fetched two tiles (pages) and one (scales) ahead
-      const auto load_page = [&](int tile) {
+      // lane l < 8 keeps page and scales of block l of a tile, asked for two tiles (pages) and one (scales) ahead and looked at
+      // only when they are needed
+      const auto ask_page = [&](int tile) {
         const int blk = tile * 8 + lane;
-        return lane < 8 && blk < n_codes ? page_of(blk * kQuantBlock) : 0;
+        return lane < 8 && blk < n_codes ? pages[blk * kQuantBlock >> g.page_shift] : 0;
+      };
+      const auto checked = [&](int id) {
+        if (id < 0 || id >= g.n_pages) {
+          report_opt(a.status, ECHOKV_EBADPAGE);
+          id = 0;
+        }
+        return id;
       };
       float ks_next = 0.f, vs_next = 0.f, vs_cur;
       const auto load_scales = [&](int tile, int page) {
@@ -369,7 +378,6 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           const long long at = scale_at(blk, page);
           vs_next = g.scales[1][at];
           ks_next = g.scales[0][at];
-          if (vs_next != vs_next) ks_next = vs_next;
         } else if (open && blk == n_full) {
           ks_next = open_bad ? __uint_as_float(0x7fc00000u) : open_back;
         }
@@ -401,7 +409,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           for (int e = 0; e < 4; ++e) w[4 * q + e] = h2(__uint_as_float(y[e] << 16) * up, __uint_as_float(y[e] & 0xffff0000u) * up);
         }
       };
-      int page8 = load_page(0), page8_next = load_page(1);
+      int page8 = checked(ask_page(0)), page8_next = ask_page(1);
       load_scales(0, page8);
       fetch(0, page8);
       for (int tile = 0; tile < it.n_tiles; ++tile, ++T) {
@@ -431,8 +439,8 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           store_piece(k_addr + st * kTileBytes, row, w);
         }
         // (the ring: tile T + 4's scales are written when S(T + 2) is complete, so after softmax(T + 1) was)
-        if (ct < 8) t.k_scale[T % kCkRing][ct] = ks_next;
         vs_cur = vs_next;
+        if (ct < 8) t.k_scale[T % kCkRing][ct] = vs_cur == vs_cur ? ks_next : vs_cur;
         fence_proxy_async_smem();
         mbar_arrive(smem_u32(&t.k_full[st]));
 
@@ -465,10 +473,10 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         fence_proxy_async_smem();
         mbar_arrive(smem_u32(&t.v_full[st]));
         if (tile + 1 < it.n_tiles) {
-          page8 = page8_next;
-          fetch(tile + 1, page8);
+          page8 = checked(page8_next);
+          page8_next = ask_page(tile + 2);
           load_scales(tile + 1, page8);
-          page8_next = load_page(tile + 2);
+          fetch(tile + 1, page8);
         }
       }
     }
