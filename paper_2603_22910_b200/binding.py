@@ -417,10 +417,13 @@ def echokv_full_attention_noalloc(cfg: echokv_config, k_pool, v_pool, block_tabl
 
 
 # ---- a serving step over a cache held in 8 bits ------------------------------------------------------------------
+# (A decode step's calls are short: what happens here per call is kept short too.)
 def _stream_on(device: int, stream) -> int | None:
+    if stream is not None:
+        return stream.cuda_stream or None
     import torch
-    s = torch.cuda.current_stream(device) if stream is None else stream
-    return s.cuda_stream or None
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)     # the same handle without a Stream object around it
+    return (raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream) or None
 
 
 def _dense(t, dtype, n, name):
@@ -432,13 +435,13 @@ def _dense(t, dtype, n, name):
     return t.data_ptr()
 
 
-def _rows(t, heads, d, dtype, name):
+def _rows(t, n, heads, d, dtype, name):
     """(address, elements from row to row) of a [n][heads][d] device tensor whose rows are dense."""
-    if t.dtype is not dtype or not t.is_cuda or t.dim() != 3 or t.shape[1:] != (heads, d) or (
-            t.shape[0] > 0 and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != d))):
-        raise ValueError("%s: a [tokens][%d][%d] %s device tensor with dense rows is needed" % (name, heads, d, dtype))
+    st = t.stride()
+    if t.dtype is not dtype or t.shape != (n, heads, d) or not t.is_cuda or (n > 0 and (st[2] != 1 or (st[1] != d and heads > 1))):
+        raise ValueError("%s: a [%d tokens][%d][%d] %s device tensor with dense rows is needed" % (name, n, heads, d, dtype))
     # (the stride of a single row is anything)
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * d
+    return t.data_ptr(), st[0] if n > 1 else heads * d
 
 
 def _dtype(cfg):
@@ -449,35 +452,38 @@ def _dtype(cfg):
 class StepPlan:
     """What plan_tokens writes: cu_tokens [B + 1], positions, token_seqs [n_tokens], seq_lens [B], free_count [1] (int32) and
     slot_map [n_tokens] (int64)."""
-    __slots__ = ("cu_tokens", "positions", "token_seqs", "slot_map", "seq_lens", "free_count")
+    __slots__ = ("cu_tokens", "positions", "token_seqs", "slot_map", "seq_lens", "free_count", "_c", "_batch", "_tokens")
 
     def __init__(self, batch: int, n_tokens: int, device, seq_lens=None, free_count=None):
         import torch
         buf = torch.empty(2 * batch + 2 * n_tokens + 2, dtype=torch.int32, device=device)
-        self.cu_tokens, self.positions, self.token_seqs, lens, count = buf.split((batch + 1, n_tokens, n_tokens, batch, 1))
+        self.cu_tokens, self.positions, self.token_seqs, lens, count = buf.split_with_sizes((batch + 1, n_tokens, n_tokens, batch, 1))
         self.slot_map = torch.empty(n_tokens, dtype=torch.int64, device=device)
         self.seq_lens = lens if seq_lens is None else seq_lens
         self.free_count = count if free_count is None else free_count
+        cu = buf.data_ptr()
+        self._c = echokv_step_plan(cu, cu + 4 * (batch + 1), cu + 4 * (batch + 1 + n_tokens), self.slot_map.data_ptr(),
+                                   _dense(self.seq_lens, torch.int32, batch, "seq_lens"),
+                                   _dense(self.free_count, torch.int32, 1, "free_count"))
+        self._batch, self._tokens = batch, n_tokens
 
 
 def plan_tokens(cfg: echokv_config, block_table, seq_lens, new_lens, free_pages, free_count, n_tokens: int, seq_slots=None,
                 out: StepPlan | None = None, status=None, stream=None) -> StepPlan:
     """Pages for new_lens[b] more tokens of sequences that hold seq_lens[b]: fills block_table ([max_batch][max_pages_per_seq]
-    int32) and returns the step's plan for up to n_tokens tokens.  `out` may hold seq_lens and free_count themselves (updated
-    in place) and is reused by captured steps; status: optional int32 device tensor (see echokv.h)."""
+    int32) and returns the step's plan for up to n_tokens tokens.  `out` is used again by later (and captured) steps, and may
+    hold the buffers seq_lens and free_count themselves, which are then updated in place; status: optional int32 device tensor
+    (see echokv.h)."""
     import torch
     i32, B = torch.int32, seq_lens.shape[0]
     if out is None:
         out = StepPlan(B, n_tokens, seq_lens.device)
-    elif out.cu_tokens.numel() < B + 1 or out.seq_lens.numel() < B or min(out.positions.numel(), out.token_seqs.numel(),
-                                                                          out.slot_map.numel()) < n_tokens:
+    elif out._batch < B or out._tokens < n_tokens:
         raise ValueError("out: too small for %d sequences and %d tokens" % (B, n_tokens))
-    p = echokv_step_plan(out.cu_tokens.data_ptr(), out.positions.data_ptr(), out.token_seqs.data_ptr(), out.slot_map.data_ptr(),
-                         out.seq_lens.data_ptr(), out.free_count.data_ptr())
     _check(lib().echokv_plan_tokens(C.byref(cfg), _dense(block_table, i32, cfg.max_batch * cfg.max_pages_per_seq, "block_table"),
                                     _dense(seq_slots, i32, B, "seq_slots"), _dense(seq_lens, i32, B, "seq_lens"),
                                     _dense(new_lens, i32, B, "new_lens"), _dense(free_pages, i32, cfg.n_pages, "free_pages"),
-                                    _dense(free_count, i32, 1, "free_count"), B, n_tokens, C.byref(p),
+                                    _dense(free_count, i32, 1, "free_count"), B, n_tokens, C.byref(out._c),
                                     _dense(status, i32, 1, "status"), _stream_on(cfg.device, stream)), "echokv_plan_tokens")
     return out
 
@@ -499,35 +505,38 @@ def rotate(cfg: echokv_config, q, k, positions, theta: float, sections=None, rot
     tensor); positions int32 [T] or [n_axes][T].  Returns (q_out, k_out), new tensors unless given -- they may be q and k.
     inverse = True is the gradient's pass."""
     import torch
-    dt, d = _dtype(cfg), cfg.head_dim
-    some = q if q is not None else k
-    if some is None:
+    dt, d, n_q, n_kv = _dtype(cfg), cfg.head_dim, cfg.n_q_heads, cfg.n_kv_heads
+    if q is None and k is None:
         raise ValueError("rotate: neither q nor k")
-    T = some.shape[0]
+    T = (k if q is None else q).shape[0]
     axes = 1 if positions.dim() == 1 else positions.shape[0]
-    if positions.shape[-1] != T or (q is not None and k is not None and k.shape[0] != T):
+    if positions.shape[-1] != T:
         raise ValueError("rotate: q, k and positions differ in their number of tokens")
-    args = []
-    outs = []
-    for x, out, heads, name in ((q, q_out, cfg.n_q_heads, "q"), (k, k_out, cfg.n_kv_heads, "k")):
-        if x is None:
-            args.append((None, 0, None, 0))
-            outs.append(None)
-            continue
-        if out is None:
-            out = torch.empty((T, heads, d), dtype=dt, device=x.device)
-        elif out.shape[0] != T:
-            raise ValueError("rotate: an output differs in its number of tokens")
-        args.append(_rows(x, heads, d, dt, name) + _rows(out, heads, d, dt, name + "_out"))
-        outs.append(out)
-    sec = None if sections is None else (C.c_int32 * len(sections))(*sections)
-    if sections is not None and len(sections) != axes:
-        raise ValueError("rotate: one section per position axis")
-    (qp, qs, qo, qos), (kp, ks, ko, kos) = args
+    qp = kp = qo = ko = None
+    qs = ks = qos = kos = 0
+    if q is not None:
+        qp, qs = _rows(q, T, n_q, d, dt, "q")
+        if q_out is None:
+            q_out = torch.empty((T, n_q, d), dtype=dt, device=q.device)
+            qo, qos = q_out.data_ptr(), n_q * d
+        else:
+            qo, qos = _rows(q_out, T, n_q, d, dt, "q_out")
+    if k is not None:
+        kp, ks = _rows(k, T, n_kv, d, dt, "k")
+        if k_out is None:
+            k_out = torch.empty((T, n_kv, d), dtype=dt, device=k.device)
+            ko, kos = k_out.data_ptr(), n_kv * d
+        else:
+            ko, kos = _rows(k_out, T, n_kv, d, dt, "k_out")
+    sec = None
+    if sections is not None:
+        if len(sections) != axes:
+            raise ValueError("rotate: one section per position axis")
+        sec = (C.c_int32 * axes)(*sections)
     _check(lib().echokv_rotate(C.byref(cfg), qp, qs, kp, ks, qo, qos, ko, kos, _dense(positions, torch.int32, axes * T, "positions"),
                                axes, sec, 1 if interleaved else 0, rot_dim, theta, 1 if inverse else 0, T,
                                _stream_on(cfg.device, stream)), "echokv_rotate")
-    return outs[0], outs[1]
+    return (q_out if q is not None else None), (k_out if k is not None else None)
 
 
 def query_quant_sizes(cfg: echokv_config) -> echokv_quant_sizes:
@@ -575,10 +584,8 @@ class QuantCache:
         """k_new, v_new [T][n_kv_heads][d] (rows may be slices of a wider tensor); slot_map, token_seqs, cu_tokens: plan_tokens'."""
         import torch
         cfg, T, B = self.cfg, k_new.shape[0], cu_tokens.shape[0] - 1
-        if v_new.shape[0] != T:
-            raise ValueError("k_new and v_new differ in their number of tokens")
-        kp, ks = _rows(k_new, cfg.n_kv_heads, cfg.head_dim, self.tdtype, "k_new")
-        vp, vs = _rows(v_new, cfg.n_kv_heads, cfg.head_dim, self.tdtype, "v_new")
+        kp, ks = _rows(k_new, T, cfg.n_kv_heads, cfg.head_dim, self.tdtype, "k_new")
+        vp, vs = _rows(v_new, T, cfg.n_kv_heads, cfg.head_dim, self.tdtype, "v_new")
         _check(lib().echokv_quant_append(C.byref(cfg), C.byref(self._c), kp, ks, vp, vs, _dense(slot_map, torch.int64, T, "slot_map"),
                                          _dense(token_seqs, torch.int32, T, "token_seqs"),
                                          _dense(cu_tokens, torch.int32, B + 1, "cu_tokens"), _dense(seq_slots, torch.int32, B, "seq_slots"),
@@ -591,19 +598,22 @@ class QuantCache:
         one each).  max_new bounds the new tokens of any sequence.  Returns out [T][n_q_heads][d] in the storage type."""
         import torch
         cfg, T, B = self.cfg, q.shape[0], seq_lens.shape[0]
-        qp, qs = _rows(q, cfg.n_q_heads, cfg.head_dim, self.tdtype, "q")
+        qp, qs = _rows(q, T, cfg.n_q_heads, cfg.head_dim, self.tdtype, "q")
         if out is None:
             out = torch.empty((T, cfg.n_q_heads, cfg.head_dim), dtype=self.tdtype, device=q.device)
+            op = out.data_ptr()
+        else:
+            op = _dense(out, self.tdtype, T * cfg.n_q_heads * cfg.head_dim, "out")
         opts = None
         if softcap or alibi_slopes is not None or prefix_lens is not None:
             opts = C.byref(echokv_score_options(softcap, 0, _dense(alibi_slopes, torch.float32, cfg.n_q_heads, "alibi_slopes"),
                                                 _dense(prefix_lens, torch.int32, B, "prefix_lens")))
-        _check(lib().echokv_quant_attention(C.byref(cfg), C.byref(self._c), opts, qp, qs,
-                                            _dense(out, self.tdtype, T * cfg.n_q_heads * cfg.head_dim, "out"),
+        _check(lib().echokv_quant_attention(C.byref(cfg), C.byref(self._c), opts, qp, qs, op,
                                             _dense(block_table, torch.int32, cfg.max_batch * cfg.max_pages_per_seq, "block_table"),
                                             _dense(seq_slots, torch.int32, B, "seq_slots"), _dense(seq_lens, torch.int32, B, "seq_lens"),
-                                            _dense(cu_tokens, torch.int32, B + 1, "cu_tokens"), B, T, max_new, self.workspace.data_ptr(),
-                                            self.workspace.numel(), _dense(status, torch.int32, 1, "status"),
+                                            _dense(cu_tokens, torch.int32, B + 1, "cu_tokens"), B, T, max_new,
+                                            _dense(self.workspace, torch.uint8, self.sizes.workspace_bytes, "workspace"),
+                                            self.sizes.workspace_bytes, _dense(status, torch.int32, 1, "status"),
                                             _stream_on(cfg.device, stream)), "echokv_quant_attention")
         return out
 

@@ -243,12 +243,16 @@ __global__ void __launch_bounds__(kPlanThreads) release_kernel(ReleaseArgs a) {
 cudaError_t launch_plan(const PlanArgs& a, cudaStream_t stream) {
   const size_t smem = (size_t)(5 * a.B + 2) * sizeof(int);
   if (smem > 40 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               (5 * kPlanMaxBatch + 2) * (int)sizeof(int));
+    static std::atomic<unsigned long long> done{0};
+    const cudaError_t e = allow_smem(plan_kernel, (5 * kPlanMaxBatch + 2) * sizeof(int), &done);
     if (e != cudaSuccess) return e;
   }
+  if (a.n_tokens <= kPlanSmallTokens) {
+    plan_kernel<<<1, kPlanThreads, smem, stream>>>(a);
+    return cudaGetLastError();
+  }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(a.n_tokens > kPlanSmallTokens ? kPlanCluster : 1);
+  cfg.gridDim = dim3(kPlanCluster);
   cfg.blockDim = dim3(kPlanThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;

@@ -22,8 +22,8 @@
 //            without a reduction over the tokens.
 //   scales   The K scale multiplies the score, the V scale the probability.  fp16's range is kept by references that are powers of
 //            two: one per query row, one per warp for the V scales, which moves with the maximum's.
-//   tail     The open block is in the storage type: bf16 converts to fp16 exactly around its own power of two, fp32
-//            as a pair of fp16.  It is attended first, while the first copies are on their way.
+//   tail     The open block is in the storage type: bf16 rows are operands of the bf16 product as they are, fp32 rows become pairs of
+//            fp16 around their own power of two.  It is attended first, while the first copies are on their way.
 #include "quant_common.cuh"
 #include "recon_tc.h"
 
@@ -157,6 +157,16 @@ struct Quad<float> {
   }
   __device__ __forceinline__ static uint32_t top_bits(uint32_t t) { return t; }
 };
+__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+// c + 0 * a of two bf16 each: a magnitude of 0 as long as every a was finite (and NaN from then on)
+__device__ __forceinline__ uint32_t zero_fma_bf16x2(uint32_t a, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(0u), "r"(c));
+  return d;
+}
 // fp16 operands of x * up: the rounded pair and what it leaves
 struct HalfPair {
   uint32_t hi, lo;
@@ -249,17 +259,15 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
   unsigned long long u = min(cta1, cta0 + wshare * warp);
   const unsigned long long u_end = min(cta1, u + wshare);
 
-  // the sequence of unit u
+  // the sequence of unit u: the last thread whose prefix is not above it, in two votes
   int b = 0;
   unsigned long long base = 0;                    // first unit of sequence b
   if (u < u_end) {
-    int lo = 0, hi = min(kQaThreads, a.B);
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (sm.pre[mid] <= u) lo = mid; else hi = mid;
-    }
-    b = lo * per;
-    base = sm.pre[lo];
+    static_assert(kQaWarps <= 32, "a lane per run of 32 prefixes");
+    const int run = __popc(__ballot_sync(0xffffffffu, lane < kQaWarps && sm.pre[lane * 32] <= u)) - 1;
+    const int at = run * 32 + __popc(__ballot_sync(0xffffffffu, sm.pre[run * 32 + lane] <= u)) - 1;
+    b = at * per;
+    base = sm.pre[at];
   }
   const bool plain = !(a.softcap > 0.f) && a.slopes == nullptr;
   const float cap_in = a.softcap > 0.f ? 1.f / a.softcap : 0.f, cap_out = a.softcap * kLog2e;
@@ -323,17 +331,11 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     const bool ok = qrow_r < n_rows;
     const T* qp = static_cast<const T*>(a.q) + (long long)(first_token + (ok ? qrow_r >> a.group_shift : 0)) * a.q_stride +
                   (long long)(h * a.group + (qrow_r & (a.group - 1))) * D;
-    float qv[KC * 16];
+    Quad<T> qv[KS];
 #pragma unroll
-    for (int i = 0; i < KC; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; e += Vec16<T>::N)
-        if (ok) {
-          Vec16<T>::load(qp + 16 * (KC * c + i) + e, qv + 16 * i + e);
-        } else {
-#pragma unroll
-          for (int f = 0; f < Vec16<T>::N; ++f) qv[16 * i + e + f] = 0.f;
-        }
+    for (int x = 0; x < KS; ++x)
+      if (ok) qv[x].load(qp + KC * 16 * c + 4 * x);
+      else qv[x].zero();
     page_next = load_pages(1);
     ks_cur = vs_cur = 0.f;
     load_scales(0, page_cur, &ks_cur, &vs_cur);
@@ -353,11 +355,14 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     for (int j = 0; j < min(kQaStages, n_codes); ++j) issue(j);
 
     {
-      float top = 0.f;
+      // (magnitudes compare as integers; an infinity or NaN gives the factor 1 and goes on through the products)
+      uint32_t bits = 0;
 #pragma unroll
-      for (int e = 0; e < KC * 16; ++e) top = fmaxf(top, fabsf(qv[e]));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      for (int x = 0; x < KS; ++x) bits = qv[x].top(bits);
+      bits = Quad<T>::top_bits(bits);
+      bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 1));
+      bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 2));
+      const float top = __uint_as_float(bits);
       float back;
       const float up = scale_up_to_half(top, &back);
 #pragma unroll
@@ -367,7 +372,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
       for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
-          const HalfPair p = split_pair<kF32>(qv[4 * ks + 2 * f] * up, qv[4 * ks + 2 * f + 1] * up);
+          const HalfPair p = split_pair<kF32>(qv[ks].get(2 * f) * up, qv[ks].get(2 * f + 1) * up);
           qh[ks][f] = p.hi;
           if (kF32) ql[ks][f] = p.lo;
         }
@@ -389,7 +394,9 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
       for (int f = 0; f < 4; ++f) o[j][f] = 0.f;
     // Per query row: the reference of its maximum (0 until it has seen a key, which the first one seen moves), and how far
     // above the reference a score may be before that moves.
-    float m_ref[2] = {0.f, 0.f}, grow[2] = {-3.0e38f, -3.0e38f}, l_run[2] = {0.f, 0.f}, v_ref = 0.f, v_inv = 0.f;
+    float m_ref[2] = {0.f, 0.f}, grow[2] = {-3.0e38f, -3.0e38f}, l_run[2] = {0.f, 0.f};
+    // the V scales' reference; negative: none yet, and the output in units of 1
+    float v_ref = -kQaPScale, v_inv = 0.f;
     const int pos_first = len - n_new + (tile * kQaRows >> a.group_shift);     // the tile's first query: blocks up to it are seen whole
 
     // a scaled product q . k of token tok and query row 2 c + e -> the score in base-2 units
@@ -457,7 +464,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
         if (v_top > v_ref) {
           // the power of two above the scale
           const uint32_t e = (__float_as_uint(v_top) >> 23) + 1;
-          const float old = v_ref;
+          const float old = fabsf(v_ref);
           v_ref = __uint_as_float(e << 23);
           v_inv = __uint_as_float((254 - e) << 23);
           alpha[0] *= old * v_inv;
@@ -496,13 +503,9 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     if (n_codes < nb) {
       const int n_open = len - n_full * kQuantBlock;
       const long long open_at = ((long long)slot * H + h) * kQuantBlock * D;
-      float sc[1][4] = {{0.f, 0.f, 0.f, 0.f}}, ks[1], vs[1];
-      Quad<T> vq[4][NT / 4];                         // value rows 2 c, 2 c + 1, 2 c + 8, 2 c + 9, this lane's features
-      // A block with an infinity or NaN acts as a block of codes does: scale NaN, values 0 (a query that sees none of it is
-      // left alone).
       const T* kt = static_cast<const T*>(g.tail[0]) + open_at;
       const T* vt = static_cast<const T*>(g.tail[1]) + open_at;
-      Quad<T> kq[2][KS];
+      Quad<T> kq[2][KS], vq[4][NT / 4];              // key rows r, r + 8; value rows 2 c, 2 c + 1, 2 c + 8, 2 c + 9, this lane's features
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -519,44 +522,72 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
             else vq[t][x].zero();
         }
       };
-      if (!kF32) load_values();                    // (fp32 rows take twice the registers: the values after the scores)
-      // power of two for a block whose largest magnitude is `top`, over the warp
-      const auto power = [&](uint32_t top, float* back) {
-        top = __reduce_max_sync(0xffffffffu, Quad<T>::top_bits(top));
-        const float up = scale_up_to_half(__uint_as_float(top), back);
-        if (top >= 0x7f800000u) *back = __uint_as_float(0x7fc00000u);
-        return up;
-      };
-      uint32_t top = 0;
+      if (!kF32) load_values();                      // (fp32 rows take twice the registers: the values after the scores)
+      // A block with an infinity or NaN acts as a block of codes does: its scale is NaN and its values are 0, so that a query
+      // that sees none of it is left alone.
+      float sc[4] = {0.f, 0.f, 0.f, 0.f}, k_mul = a.scale * (a.softcap > 0.f ? 1.f : kLog2e), v_mul = 1.f, v_up = 1.f;
+      float f_row[2] = {k_mul, k_mul};
+      if constexpr (kF32) {
+        // fp16 pairs around a power of two
+        const auto power = [&](uint32_t top, float* back) {
+          top = __reduce_max_sync(0xffffffffu, Quad<T>::top_bits(top));
+          const float up = scale_up_to_half(__uint_as_float(top), back);
+          if (top >= 0x7f800000u) *back = __uint_as_float(0x7fc00000u);
+          return up;
+        };
+        uint32_t top = 0;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int x = 0; x < KS; ++x) top = kq[t][x].top(top);
-      const float k_up = power(top, &ks[0]);
-      const bool k_ok = ks[0] == ks[0];
+          for (int x = 0; x < KS; ++x) top = kq[t][x].top(top);
+        const float k_up = power(top, &k_mul);
+        const bool k_ok = k_mul == k_mul;
 #pragma unroll
-      for (int x = 0; x < KS; ++x) {
-        HalfPair p[4];                             // tokens r, r + 8; elements 0, 1 and 2, 3
+        for (int x = 0; x < KS; ++x) {
+          HalfPair p[4];                             // tokens r, r + 8; elements 0, 1 and 2, 3
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (!k_ok) kq[t][x].zero();
+          for (int t = 0; t < 2; ++t) {
+            if (!k_ok) kq[t][x].zero();
 #pragma unroll
-          for (int f = 0; f < 2; ++f) p[2 * f + t] = split_pair<kF32>(kq[t][x].get(2 * f) * k_up, kq[t][x].get(2 * f + 1) * k_up);
+            for (int f = 0; f < 2; ++f) p[2 * f + t] = split_pair<true>(kq[t][x].get(2 * f) * k_up, kq[t][x].get(2 * f + 1) * k_up);
+          }
+          mma_m16n8k16_f16(sc, p[0].hi, p[1].hi, p[2].hi, p[3].hi, qh[x][0], qh[x][1]);
+          mma_m16n8k16_f16(sc, p[0].hi, p[1].hi, p[2].hi, p[3].hi, ql[x][0], ql[x][1]);
+          mma_m16n8k16_f16(sc, p[0].lo, p[1].lo, p[2].lo, p[3].lo, qh[x][0], qh[x][1]);
         }
-        mma_m16n8k16_f16(sc[0], p[0].hi, p[1].hi, p[2].hi, p[3].hi, qh[x][0], qh[x][1]);
-        if (kF32) {
-          mma_m16n8k16_f16(sc[0], p[0].hi, p[1].hi, p[2].hi, p[3].hi, ql[x][0], ql[x][1]);
-          mma_m16n8k16_f16(sc[0], p[0].lo, p[1].lo, p[2].lo, p[3].lo, qh[x][0], qh[x][1]);
+        f_row[0] = c_row[0] * k_mul;
+        f_row[1] = c_row[1] * k_mul;
+        load_values();
+        top = 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int x = 0; x < NT / 4; ++x) top = vq[t][x].top(top);
+        v_up = power(top, &v_mul);
+        // the power of two above the block's
+        if (v_mul > 0.f) {
+          const uint32_t e = (__float_as_uint(v_mul) >> 23) + 1;
+          v_ref = __uint_as_float(e << 23);
+          v_inv = __uint_as_float((254 - e) << 23);
         }
+        v_mul = v_mul * v_inv * kQaPScale;
+      } else {
+        // bf16 rows are operands as they are.  Zero times an element tells whether it is finite.
+        uint32_t k_bad = 0, v_bad = 0;
+#pragma unroll
+        for (int x = 0; x < KS; ++x) {
+          mma_m16n8k16_bf16(sc, kq[0][x].w.x, kq[1][x].w.x, kq[0][x].w.y, kq[1][x].w.y, qv[x].w.x, qv[x].w.y);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) k_bad = zero_fma_bf16x2(kq[t][x].w.x, zero_fma_bf16x2(kq[t][x].w.y, k_bad));
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int x = 0; x < NT / 4; ++x) v_bad = zero_fma_bf16x2(vq[t][x].w.x, zero_fma_bf16x2(vq[t][x].w.y, v_bad));
+        if (__any_sync(0xffffffffu, (k_bad & 0x7fff7fffu) != 0)) f_row[0] = f_row[1] = __uint_as_float(0x7fc00000u);
+        if (__any_sync(0xffffffffu, (v_bad & 0x7fff7fffu) != 0)) v_mul = __uint_as_float(0x7fc00000u);
       }
-      if (kF32) load_values();
-      top = 0;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int x = 0; x < NT / 4; ++x) top = vq[t][x].top(top);
-      const float v_up = power(top, &vs[0]);
-      if (vs[0] != vs[0]) {
+      if (v_mul != v_mul) {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -567,14 +598,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int tok = n_full * kQuantBlock + 8 * (i >> 1) + r;
-        x[i] = tok < len && (tok <= pos[i & 1] || tok < prefix) ? score(sc[0][i] * (c_row[i & 1] * ks[0]), i & 1, tok) : -INFINITY;
-      }
-      {
-        const uint32_t e = (__float_as_uint(vs[0]) >> 23) + 1;        // the power of two above the scale
-        if (vs[0] > 0.f) {
-          v_ref = __uint_as_float(e << 23);
-          v_inv = __uint_as_float((254 - e) << 23);
-        }
+        x[i] = tok < len && (tok <= pos[i & 1] || tok < prefix) ? score(sc[i] * f_row[i & 1], i & 1, tok) : -INFINITY;
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -586,31 +610,49 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
           grow[e] = kQaGrow;
         }
       }
-      const float pv = vs[0] * v_inv * kQaPScale;
-      uint32_t ph[1][2], pl[1][2];
+      uint32_t ph[2], pl[2];
       float p[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         p[i] = exp2_approx(x[i] - m_ref[i & 1]);
         l_run[i & 1] += p[i];
-        p[i] = x[i] == -INFINITY ? 0.f : p[i] * pv;
+        p[i] = x[i] == -INFINITY ? 0.f : p[i] * v_mul;
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const HalfPair w = split_pair<kF32>(p[2 * t], p[2 * t + 1]);
-        ph[0][t] = movm(w.hi);
-        if (kF32) pl[0][t] = movm(w.lo);
+        if constexpr (kF32) {
+          const HalfPair w = split_pair<true>(p[2 * t], p[2 * t + 1]);
+          ph[t] = movm(w.hi);
+          pl[t] = movm(w.lo);
+        } else {
+          // bf16 has the values' range, a pair of them 16 bits
+          const uint32_t w = pack_bf16x2(p[2 * t], p[2 * t + 1]);
+          ph[t] = movm(w);
+          pl[t] = movm(pack_bf16x2(p[2 * t] - __uint_as_float(w << 16), p[2 * t + 1] - __uint_as_float(w & 0xffff0000u)));
+        }
       }
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        HalfPair p[4];                             // features 2 m, 2 m + 1; tokens 0, 1 and 2, 3
+      for (int m = 0; m < MT; ++m) {                 // features 2 m, 2 m + 1; tokens 0, 1 and 2, 3
+        if constexpr (kF32) {
+          HalfPair w[4];
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+          for (int e = 0; e < 2; ++e)
 #pragma unroll
-          for (int f = 0; f < 2; ++f)
-            p[2 * f + e] = split_pair<kF32>(vq[2 * f][m / 2].get(2 * (m & 1) + e) * v_up, vq[2 * f + 1][m / 2].get(2 * (m & 1) + e) * v_up);
-        mma_pv(o[m], p[0].hi, p[1].hi, p[2].hi, p[3].hi, ph[0], pl[0]);
-        if (kF32) mma_m16n8k16_f16(o[m], p[0].lo, p[1].lo, p[2].lo, p[3].lo, ph[0][0], ph[0][1]);
+            for (int f = 0; f < 2; ++f)
+              w[2 * f + e] = split_pair<true>(vq[2 * f][m / 2].get(2 * (m & 1) + e) * v_up, vq[2 * f + 1][m / 2].get(2 * (m & 1) + e) * v_up);
+          mma_pv(o[m], w[0].hi, w[1].hi, w[2].hi, w[3].hi, ph, pl);
+          mma_m16n8k16_f16(o[m], w[0].lo, w[1].lo, w[2].lo, w[3].lo, ph[0], ph[1]);
+        } else {
+          uint32_t w[4];
+#pragma unroll
+          for (int f = 0; f < 2; ++f) {
+            const uint32_t t0 = m & 1 ? vq[2 * f][m / 2].w.y : vq[2 * f][m / 2].w.x, t1 = m & 1 ? vq[2 * f + 1][m / 2].w.y : vq[2 * f + 1][m / 2].w.x;
+            w[2 * f] = __byte_perm(t0, t1, 0x5410);
+            w[2 * f + 1] = __byte_perm(t0, t1, 0x7632);
+          }
+          mma_m16n8k16_bf16(o[m], w[0], w[1], w[2], w[3], ph[0], ph[1]);
+          mma_m16n8k16_bf16(o[m], w[0], w[1], w[2], w[3], pl[0], pl[1]);
+        }
       }
     }
 
@@ -718,7 +760,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     for (int e = 0; e < 2; ++e)
 #pragma unroll
       for (int w = 4; w < 32; w <<= 1) l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], w);
-    const float o_scale = v_ref * (1.f / kQaPScale);
+    const float o_scale = fabsf(v_ref) * (1.f / kQaPScale);
     const bool starts = blk0 == 0, ends = seg_end == item_end;
     if (starts && ends) {
 #pragma unroll
@@ -865,7 +907,8 @@ cudaError_t launch(const QuantAttnArgs& a, int sm_count, cudaStream_t stream) {
   constexpr size_t smem = qa_ring_bytes<D>() + sizeof(QaSmem<D>);
   static_assert(kQaStages * qa_stage_bytes(D) >= kQaRows * D * 4, "a segment's rows fit over a warp's ring");
   static_assert(smem <= 227 * 1024, "shared memory of one CTA");
-  cudaError_t e = cudaFuncSetAttribute(quant_attn_kernel<T, FMT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  static std::atomic<unsigned long long> done{0};
+  cudaError_t e = allow_smem(quant_attn_kernel<T, FMT, D>, smem, &done);
   if (e != cudaSuccess) return e;
   // the codes as rows of 128 bytes (64 two-byte elements to TMA), boxes of one block
   CUtensorMap maps[2];

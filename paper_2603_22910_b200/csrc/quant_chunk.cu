@@ -679,7 +679,8 @@ template <int FMT, int D>
 cudaError_t launch(const QuantAttnArgs& a, int sm_count, cudaStream_t stream) {
   constexpr size_t smem = ck_smem_bytes<D>();
   static_assert(smem <= 227 * 1024, "shared memory of one CTA");
-  const cudaError_t e = cudaFuncSetAttribute(quant_chunk_kernel<FMT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  static std::atomic<unsigned long long> done{0};
+  const cudaError_t e = allow_smem(quant_chunk_kernel<FMT, D>, smem, &done);
   if (e != cudaSuccess) return e;
   quant_chunk_kernel<FMT, D><<<sm_count, kCkThreads, smem, stream>>>(a);
   return cudaGetLastError();

@@ -1,6 +1,8 @@
 // Host-side launchers of the serving-step kernels (internal to the library): plan, rotation, 8-bit append, 8-bit attention.
 #pragma once
 
+#include <atomic>
+
 #include "common.cuh"
 
 namespace echokv {
@@ -29,6 +31,19 @@ __device__ __forceinline__ void store16<__nv_bfloat16>(__nv_bfloat16* p, const f
     w[i] = *reinterpret_cast<const uint32_t*>(&b);
   }
   *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// The shared memory that `kernel` may ask for at a launch on the current device: set once per device and kernel (one `done` each).
+template <typename K>
+inline cudaError_t allow_smem(K* kernel, size_t bytes, std::atomic<unsigned long long>* done) {
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = 1ull << (device & 63);
+  if (done->load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess) done->fetch_or(bit, std::memory_order_relaxed);
+  return e;
 }
 
 struct PlanArgs {

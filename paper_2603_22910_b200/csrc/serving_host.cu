@@ -198,6 +198,9 @@ int echokv_rotate(const echokv_config* cfg, const void* q, int64_t q_stride, con
   a.pos = dev_positions;
   a.sign = inverse ? -1.f : 1.f;
   int axis = 0, until = sections ? sections[0] : half;
+  // theta^(-2 j / rot) as a running product: 64 factors, 64 roundings of 2^-53
+  const double step = std::pow(theta, -2.0 / rot_dim);
+  double freq = 1.0 / 6.283185307179586476925287;
   for (int j = 0; j < half; ++j) {
     if (interleaved && sections) {
       axis = j % n_axes;
@@ -206,7 +209,8 @@ int echokv_rotate(const echokv_config* cfg, const void* q, int64_t q_stride, con
       while (j >= until) until += sections[++axis];
     }
     a.axis[j] = (unsigned char)axis;
-    a.turns[j] = std::pow(theta, -2.0 * j / rot_dim) / 6.283185307179586476925287;
+    a.turns[j] = freq;
+    freq *= step;
   }
   OnDevice dev(cfg->device);
   if (!dev.ok()) return ECHOKV_ECUDA;

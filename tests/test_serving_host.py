@@ -137,7 +137,7 @@ def test_binding_refuses_wrong_tensors():
         binding.QuantCache(cfg, "int4")
     with pytest.raises(ValueError, match="neither"):
         binding.rotate(cfg, None, None, torch.zeros(1, dtype=torch.int32), 1e4)
-    with pytest.raises(ValueError, match="tokens"):
+    with pytest.raises(ValueError, match="number of tokens"):
         binding.rotate(cfg, torch.zeros(3, 32, 128, dtype=torch.bfloat16), None, torch.zeros(2, dtype=torch.int32), 1e4)
 
 
