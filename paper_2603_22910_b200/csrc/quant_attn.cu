@@ -134,8 +134,18 @@ struct Quad;
 template <>
 struct Quad<__nv_bfloat16> {
   uint2 w;
+  static constexpr int kPerLoad = 2;               // quads of one 16-byte load
   __device__ __forceinline__ void load(const __nv_bfloat16* p) { w = *reinterpret_cast<const uint2*>(p); }
   __device__ __forceinline__ void zero() { w = make_uint2(0u, 0u); }
+  __device__ __forceinline__ static void load16(const __nv_bfloat16* p, Quad* q) {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    q[0].w = make_uint2(v.x, v.y);
+    q[1].w = make_uint2(v.z, v.w);
+  }
+  __device__ __forceinline__ static void zero16(Quad* q) {
+    q[0].zero();
+    q[1].zero();
+  }
   __device__ __forceinline__ float get(int e) const {
     const uint32_t x = e < 2 ? w.x : w.y;
     return __uint_as_float(e & 1 ? x & 0xffff0000u : x << 16);
@@ -149,8 +159,11 @@ struct Quad<__nv_bfloat16> {
 template <>
 struct Quad<float> {
   uint4 w;
+  static constexpr int kPerLoad = 1;
   __device__ __forceinline__ void load(const float* p) { w = *reinterpret_cast<const uint4*>(p); }
   __device__ __forceinline__ void zero() { w = make_uint4(0u, 0u, 0u, 0u); }
+  __device__ __forceinline__ static void load16(const float* p, Quad* q) { q->load(p); }
+  __device__ __forceinline__ static void zero16(Quad* q) { q->zero(); }
   __device__ __forceinline__ float get(int e) const { return __uint_as_float(e == 0 ? w.x : e == 1 ? w.y : e == 2 ? w.z : w.w); }
   __device__ __forceinline__ uint32_t top(uint32_t t) const {
     return max(max(t, w.x & 0x7fffffffu), max(w.y & 0x7fffffffu, max(w.z & 0x7fffffffu, w.w & 0x7fffffffu)));
@@ -333,9 +346,9 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
                   (long long)(h * a.group + (qrow_r & (a.group - 1))) * D;
     Quad<T> qv[KS];
 #pragma unroll
-    for (int x = 0; x < KS; ++x)
-      if (ok) qv[x].load(qp + KC * 16 * c + 4 * x);
-      else qv[x].zero();
+    for (int x = 0; x < KS; x += Quad<T>::kPerLoad)
+      if (ok) Quad<T>::load16(qp + KC * 16 * c + 4 * x, &qv[x]);
+      else Quad<T>::zero16(&qv[x]);
     page_next = load_pages(1);
     ks_cur = vs_cur = 0.f;
     load_scales(0, page_cur, &ks_cur, &vs_cur);
@@ -506,20 +519,21 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
       const T* kt = static_cast<const T*>(g.tail[0]) + open_at;
       const T* vt = static_cast<const T*>(g.tail[1]) + open_at;
       Quad<T> kq[2][KS], vq[4][NT / 4];              // key rows r, r + 8; value rows 2 c, 2 c + 1, 2 c + 8, 2 c + 9, this lane's features
+      // (fp32: the queries' order of features.  bf16: one of their own in which four lanes read 64 bytes side by side.)
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int x = 0; x < KS; ++x)
-          if (r + 8 * t < n_open) kq[t][x].load(kt + (r + 8 * t) * D + KC * 16 * c + 4 * x);
-          else kq[t][x].zero();
+        for (int x = 0; x < KS; x += Quad<T>::kPerLoad)
+          if (r + 8 * t < n_open) Quad<T>::load16(kt + (r + 8 * t) * D + (kF32 ? KC * 16 * c + 4 * x : 16 * x + 8 * c), &kq[t][x]);
+          else Quad<T>::zero16(&kq[t][x]);
       const auto load_values = [&]() {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const int tok = 2 * c + (t & 1) + (t >> 1) * 8;
 #pragma unroll
-          for (int x = 0; x < NT / 4; ++x)
-            if (tok < n_open) vq[t][x].load(vt + tok * D + NT * r + 4 * x);
-            else vq[t][x].zero();
+          for (int x = 0; x < NT / 4; x += Quad<T>::kPerLoad)
+            if (tok < n_open) Quad<T>::load16(vt + tok * D + NT * r + 4 * x, &vq[t][x]);
+            else Quad<T>::zero16(&vq[t][x]);
         }
       };
       if (!kF32) load_values();                      // (fp32 rows take twice the registers: the values after the scores)
@@ -574,9 +588,14 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
       } else {
         // bf16 rows are operands as they are.  Zero times an element tells whether it is finite.
         uint32_t k_bad = 0, v_bad = 0;
+        Quad<T> qt[KS];
+#pragma unroll
+        for (int x = 0; x < KS; x += 2)
+          if (ok) Quad<T>::load16(qp + 16 * x + 8 * c, &qt[x]);
+          else Quad<T>::zero16(&qt[x]);
 #pragma unroll
         for (int x = 0; x < KS; ++x) {
-          mma_m16n8k16_bf16(sc, kq[0][x].w.x, kq[1][x].w.x, kq[0][x].w.y, kq[1][x].w.y, qv[x].w.x, qv[x].w.y);
+          mma_m16n8k16_bf16(sc, kq[0][x].w.x, kq[1][x].w.x, kq[0][x].w.y, kq[1][x].w.y, qt[x].w.x, qt[x].w.y);
 #pragma unroll
           for (int t = 0; t < 2; ++t) k_bad = zero_fma_bf16x2(kq[t][x].w.x, zero_fma_bf16x2(kq[t][x].w.y, k_bad));
         }
