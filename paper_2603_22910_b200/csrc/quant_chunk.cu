@@ -109,15 +109,34 @@ __device__ __forceinline__ void tmem_st16_regs(uint32_t addr, const uint32_t (&r
       : "memory");
 }
 
-// tanh(y) / y for z = y^2 <= 1, to 6e-7: the polynomial of degree 5 in z that is nearest in the largest relative error (found by
-// iteratively reweighted least squares on Chebyshev points)
-__device__ __forceinline__ uint64_t tanh_poly_f2(uint64_t z) {
-  uint64_t s = pack_f2(-0.003067061770707369f, -0.003067061770707369f);
-  s = fma_f2(s, z, pack_f2(0.016743119806051254f, 0.016743119806051254f));
-  s = fma_f2(s, z, pack_f2(-0.05160567909479141f, -0.05160567909479141f));
-  s = fma_f2(s, z, pack_f2(0.13281434774398804f, 0.13281434774398804f));
-  s = fma_f2(s, z, pack_f2(-0.3332904279232025f, -0.3332904279232025f));
-  return fma_f2(s, z, pack_f2(0.9999994039535522f, 0.9999994039535522f));
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
+// y -> tanh(y) for 32 of them, two at a time: y times a polynomial in z = y^2, the nearest one in the largest relative error (found by
+// iteratively reweighted least squares on Chebyshev points) -- of degree 3 for z <= 1/4 (5.5e-7) and of degree 5 for
+// z <= 1 (6e-7).
+template <bool SMALL>
+__device__ __forceinline__ void tanh_pieces(uint32_t (&y)[32]) {
+  constexpr float c0 = SMALL ? 0.999999463558197f : 0.9999994039535522f, c1 = SMALL ? -0.33326318860054016f : -0.3332904279232025f,
+                  c2 = SMALL ? 0.13190296292304993f : 0.13281434774398804f, c3 = SMALL ? -0.04440222680568695f : -0.05160567909479141f;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    const uint64_t y2 = pack_u2(y[2 * j], y[2 * j + 1]), z = mul_f2(y2, y2);
+    uint64_t s;
+    if (SMALL) {
+      s = pack_f2(c3, c3);
+    } else {
+      s = fma_f2(pack_f2(-0.003067061770707369f, -0.003067061770707369f), z, pack_f2(0.016743119806051254f, 0.016743119806051254f));
+      s = fma_f2(s, z, pack_f2(c3, c3));
+    }
+    s = fma_f2(s, z, pack_f2(c2, c2));
+    s = fma_f2(s, z, pack_f2(c1, c1));
+    s = fma_f2(s, z, pack_f2(c0, c0));
+    unpack_u2(mul_f2(y2, s), y[2 * j], y[2 * j + 1]);
+  }
 }
 
 struct CkItem {
@@ -544,37 +563,35 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           if (!plain || masked) {
             // scores in place
             bool done = false;
-            if (a.softcap > 0.f && !a.slopes && !masked) {
-              uint64_t y[16];
-              float top = 0.f;
+            if (a.softcap > 0.f) {
+              const uint64_t g2[2] = {pack_f2(f[0] * cap_in, f[0] * cap_in), pack_f2(f[1] * cap_in, f[1] * cap_in)};
+              float top = 0.f;                     // largest y^2 (a NaN is smaller than anything here and stays one)
 #pragma unroll
               for (int j = 0; j < 16; ++j) {
-                const float g2 = f[j >> 3] * cap_in;
-                y[j] = mul_f2(pack_u2(sr[2 * j], sr[2 * j + 1]), pack_f2(g2, g2));
-                float y0, y1;
-                unpack_f2(y[j], y0, y1);
-                top = fmaxf(top, fmaxf(fabsf(y0), fabsf(y1)));
+                const uint64_t y = mul_f2(pack_u2(sr[2 * j], sr[2 * j + 1]), g2[j >> 3]);
+                unpack_u2(y, sr[2 * j], sr[2 * j + 1]);
+                float z0, z1;
+                unpack_f2(mul_f2(y, y), z0, z1);
+                top = max3(top, z0, z1);
               }
-              // (the polynomial holds up to 1; a NaN is smaller than anything here and stays one)
-              if (__all_sync(0xffffffffu, top <= 1.f)) {
-                done = true;
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                  const uint64_t z = mul_f2(mul_f2(y[j], tanh_poly_f2(mul_f2(y[j], y[j]))), pack_f2(cap_out, cap_out));
-                  unpack_u2(z, sr[2 * j], sr[2 * j + 1]);
-                }
+              if (!a.slopes && !masked) {
+                done = __all_sync(0xffffffffu, top <= 1.f);
+                const bool small = __all_sync(0xffffffffu, top <= 0.25f);
+                if (small) tanh_pieces<true>(sr);
+                else if (done) tanh_pieces<false>(sr);
+                f[0] = f[1] = cap_out;
               }
             }
             if (!done) {
 #pragma unroll
               for (int j = 0; j < 32; ++j) {
-                float y = __uint_as_float(sr[j]) * f[j >> 4];
-                if (a.softcap > 0.f) y = cap_out * tanh_f32(y * cap_in);
+                float y = __uint_as_float(sr[j]);
+                y = a.softcap > 0.f ? cap_out * tanh_f32(y) : y * f[j >> 4];
                 if (a.slopes) y -= slope2 * fabsf((float)(pos - key0 - j));
                 sr[j] = __float_as_uint(32 * c + j < n_vis ? y : -INFINITY);
               }
+              f[0] = f[1] = 1.f;
             }
-            f[0] = f[1] = 1.f;
           }
           float sum = 0.f;
 #pragma unroll 1
