@@ -85,6 +85,11 @@ __device__ __forceinline__ bool ck_wait(unsigned long long* bar, uint32_t parity
     }
   }
 }
+// one arrival for a warp whose lanes are all done
+__device__ __forceinline__ void warp_arrive(unsigned long long* bar) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(bar));
+}
 __device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
@@ -175,13 +180,13 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
   if (tid == 0) {
     t.abort_flag = 0;
     for (int x = 0; x < 2; ++x) {
-      mbar_init(smem_u32(&t.q_full[x]), kCkTile);
+      mbar_init(smem_u32(&t.q_full[x]), kCkTile / 32);
       mbar_init(smem_u32(&t.s_full[x]), 1);
-      mbar_init(smem_u32(&t.p_ready[x]), kCkTile);
+      mbar_init(smem_u32(&t.p_ready[x]), kCkTile / 32);
       mbar_init(smem_u32(&t.o_done[x]), 1);
-      mbar_init(smem_u32(&t.k_full[x]), kCkConvThreads);
+      mbar_init(smem_u32(&t.k_full[x]), kCkConvThreads / 32);
       mbar_init(smem_u32(&t.k_empty[x]), 1);
-      mbar_init(smem_u32(&t.v_full[x]), kCkConvThreads);
+      mbar_init(smem_u32(&t.v_full[x]), kCkConvThreads / 32);
       mbar_init(smem_u32(&t.v_empty[x]), 1);
     }
     mbar_init(smem_u32(&t.drain), 1);
@@ -246,14 +251,21 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
     if (lane == 0) {
       bool alive = true;
       uint32_t T = 0, n_item = 0, n_p[2] = {0, 0}; // tiles and items so far; tiles of either half
+      // operand descriptors: the low words hold the address (in units of 16 bytes, far from a carry), the high words stay
+      uint32_t q_lo0, k_lo0, v_lo0, kmajor_hi, v_hi;
+      unpack_u2(ck_desc(q_addr, 16), q_lo0, kmajor_hi);
+      unpack_u2(ck_desc(k_addr, 16), k_lo0, kmajor_hi);
+      unpack_u2(ck_desc(v_addr, kCkChunkBytes), v_lo0, v_hi);
       for (unsigned long long i = blockIdx.x; i < total && alive; i += gridDim.x, ++n_item) {
         const CkItem it = get_item(i);
         const auto issue_s = [&](int x, uint32_t tile) {
-          const uint32_t k = k_addr + (tile & 1) * kTileBytes;
+          const uint32_t q_lo = q_lo0 + x * (kTileBytes >> 4), k_lo = k_lo0 + (tile & 1) * (kTileBytes >> 4);
 #pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk)
-            tc_mma_bf16(tmem + x * 128, ck_desc(q_addr + x * kTileBytes + (kk >> 2) * kCkChunkBytes, 16) + 2 * (kk & 3),
-                        ck_desc(k + (kk >> 2) * kCkChunkBytes, 16) + 2 * (kk & 3), kCkIdescS, kk > 0 ? 1u : 0u);
+          for (int kk = 0; kk < D / 16; ++kk) {
+            constexpr uint32_t kStep = kCkChunkBytes >> 4;
+            tc_mma_bf16(tmem + x * 128, pack_u2(q_lo + (kk >> 2) * kStep + 2 * (kk & 3), kmajor_hi),
+                        pack_u2(k_lo + (kk >> 2) * kStep + 2 * (kk & 3), kmajor_hi), kCkIdescS, kk > 0 ? 1u : 0u);
+          }
           tc_commit(smem_u32(&t.s_full[x]));
           if (x == it.act - 1) tc_commit(smem_u32(&t.k_empty[tile & 1]));
         };
@@ -265,14 +277,14 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         for (int x = 0; x < it.act; ++x) issue_s(x, T);
         for (int tile = 0; tile < it.n_tiles && alive; ++tile, ++T) {
           if (!ck_wait(&t.v_full[T & 1], (T >> 1) & 1, abort_flag, a.status)) { alive = false; break; }
-          const uint64_t vd = ck_desc(v_addr + (T & 1) * kTileBytes, kCkChunkBytes);
+          const uint32_t v_lo = v_lo0 + (T & 1) * (kTileBytes >> 4);
           for (int x = 0; x < it.act && alive; ++x) {
             if (!ck_wait(&t.p_ready[x], n_p[x] & 1, abort_flag, a.status)) { alive = false; break; }
             ++n_p[x];
             tc_fence_after();
 #pragma unroll
             for (int kk = 0; kk < 8; ++kk)         // 16 keys: 8 columns of packed probabilities, 2048 bytes of value rows
-              tc_mma_bf16_tmem_a(tmem + 256 + x * D, tmem + x * 128 + 8 * kk, vd + 128 * kk, ck_idesc_pv<D>(),
+              tc_mma_bf16_tmem_a(tmem + 256 + x * D, tmem + x * 128 + 8 * kk, pack_u2(v_lo + 128 * kk, v_hi), ck_idesc_pv<D>(),
                                  (tile > 0 || kk > 0) ? 1u : 0u);
             if (tile + 1 == it.n_tiles) tc_commit(smem_u32(&t.o_done[x]));
             if (x == it.act - 1) tc_commit(smem_u32(&t.v_empty[T & 1]));
@@ -461,7 +473,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         vs_cur = vs_next;
         if (ct < 8) t.k_scale[T % kCkRing][ct] = vs_cur == vs_cur ? ks_next : vs_cur;
         fence_proxy_async_smem();
-        mbar_arrive(smem_u32(&t.k_full[st]));
+        warp_arrive(&t.k_full[st]);
 
         alive = __all_sync(0xffffffffu, ck_wait(&t.v_empty[st], parity, abort_flag, a.status));
         if (!alive) break;
@@ -490,7 +502,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           store_piece(v_addr + st * kTileBytes, row, w);
         }
         fence_proxy_async_smem();
-        mbar_arrive(smem_u32(&t.v_full[st]));
+        warp_arrive(&t.v_full[st]);
         if (tile + 1 < it.n_tiles) {
           page8 = checked(page8_next);
           page8_next = ask_page(tile + 2);
@@ -538,7 +550,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         for (int p = 0; p < D / 8; ++p) sts16(q_addr + x * kTileBytes + ck_off(row, p), w[4 * p], w[4 * p + 1], w[4 * p + 2], w[4 * p + 3]);
       }
       fence_proxy_async_smem();
-      mbar_arrive(smem_u32(&t.q_full[x]));
+      warp_arrive(&t.q_full[x]);
       if (x >= it.act) {
         T += it.n_tiles;
         continue;
@@ -656,7 +668,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         }
         tmem_st_wait();
         tc_fence_before();
-        mbar_arrive(smem_u32(&t.p_ready[x]));
+        warp_arrive(&t.p_ready[x]);
       }
       if (!alive) break;
       // ---- the row's result
