@@ -325,9 +325,12 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
     // an even row and of the next one: eight different banks in the swizzle.
     const int my_row = D == 128 ? (ct >> 5) * 4 + (lane >> 4) * 2 + ((lane >> 2) & 1) : ct / kPieces;
     const int my_piece = D == 128 ? ((lane >> 3) & 1) * 4 + (lane & 3) : ct % kPieces;
-    const auto store_piece = [&](uint32_t dst, int row, const uint32_t (&w)[8]) {
-      sts16(dst + ck_off(row, 2 * my_piece), w[0], w[1], w[2], w[3]);
-      sts16(dst + ck_off(row, 2 * my_piece + 1), w[4], w[5], w[6], w[7]);
+    // its two 16-byte halves in an operand tile; kRowStep rows on, the swizzle turns by kRowStep mod 8 (0 or 4)
+    const uint32_t at0 = ck_off(my_row, 2 * my_piece), at1 = ck_off(my_row, 2 * my_piece + 1);
+    const auto store_piece = [&](uint32_t dst, int p, const uint32_t (&w)[8]) {
+      const uint32_t turn = (p & 1) ? (kRowStep & 4) << 4 : 0;
+      sts16(dst + (at0 ^ turn) + p * kRowStep * 128, w[0], w[1], w[2], w[3]);
+      sts16(dst + (at1 ^ turn) + p * kRowStep * 128, w[4], w[5], w[6], w[7]);
     };
     for (unsigned long long i = blockIdx.x; i < total; i += gridDim.x, ++n_item) {
       if (!conv_all(alive)) break;                 // (a wait that ran out: all leave together)
@@ -413,21 +416,22 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           ks_next = open_bad ? __uint_as_float(0x7fc00000u) : open_back;
         }
       };
-      // codes of this thread's pieces, fetched one tile ahead
+      // codes of this thread's pieces, fetched one tile ahead (rows behind the last block of codes: page 0's, not looked at)
       uint4 kc[NP], vc[NP];
       const unsigned char* k_base = g.codes[0] + 16 * my_piece;
       const unsigned char* v_base = g.codes[1] + 16 * my_piece;
       const auto fetch = [&](int tile, int page8) {
+        uint32_t at[NP];
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-          const int row = my_row + kRowStep * p, tok = tile * kCkTile + row;
-          const int page = __shfl_sync(0xffffffffu, page8, (row >> 4) & 7);
-          if (row < kCkTile && tok < n_codes * kQuantBlock) {
-            const long long off = (long long)((page * H + it.h) * g.page_tokens + (tok & (g.page_tokens - 1))) * D;
-            kc[p] = *reinterpret_cast<const uint4*>(k_base + off);
-            vc[p] = *reinterpret_cast<const uint4*>(v_base + off);
-          }
+          const int row = min(my_row + kRowStep * p, kCkTile - 1);
+          const int page = __shfl_sync(0xffffffffu, page8, row >> 4);
+          at[p] = (uint32_t)((page * H + it.h) * g.page_tokens + ((tile * kCkTile + row) & (g.page_tokens - 1)));
         }
+#pragma unroll
+        for (int p = 0; p < NP; ++p) kc[p] = *reinterpret_cast<const uint4*>(k_base + (size_t)at[p] * D);
+#pragma unroll
+        for (int p = 0; p < NP; ++p) vc[p] = *reinterpret_cast<const uint4*>(v_base + (size_t)at[p] * D);
       };
       // 16 features of a row of the open block as fp16 pairs, or zeros
       const auto open_row = [&](int which, int row, float up, uint32_t (&w)[8]) {
@@ -467,7 +471,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[e] = 0u;
           }
-          store_piece(k_addr + st * kTileBytes, row, w);
+          store_piece(k_addr + st * kTileBytes, p, w);
         }
         // (the ring: tile T + 4's scales are written when S(T + 2) is complete, so after softmax(T + 1) was)
         vs_cur = vs_next;
@@ -499,7 +503,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[e] = 0u;
           }
-          store_piece(v_addr + st * kTileBytes, row, w);
+          store_piece(v_addr + st * kTileBytes, p, w);
         }
         fence_proxy_async_smem();
         warp_arrive(&t.v_full[st]);
