@@ -13,7 +13,7 @@
 //   warps 8-14       conversion: codes of the next tile are on their way in registers while the present one is turned into fp16 and
 //                    stored in the 128-byte swizzle (key tiles K-major, value tiles as stored, N-major).  Eight lanes of a
 //                    warp keep the pages and scales of the tile's eight blocks.
-//   warp 15          one thread issues the products: S_x = Q_x K^T from shared memory, O_x += P_x V with P_x in tensor memory
+//   warp 15          issues the products, by one elected thread: S_x = Q_x K^T from shared memory, O_x += P_x V with P_x in tensor memory
 //                    over the first half of S_x.
 // Tensor memory: S_0 | S_1 | O_0 | O_1.  The K scale multiplies the score beside the row's own factor (one value per 16 columns);
 // V codes times (their scale / the largest scale the row can see) times 64 are below 2^15.
@@ -85,6 +85,10 @@ __device__ __forceinline__ bool ck_wait(unsigned long long* bar, uint32_t parity
     }
   }
 }
+// the same for a whole warp, with one answer
+__device__ __forceinline__ bool ck_wait_warp(unsigned long long* bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
+  return __all_sync(0xffffffffu, ck_wait(bar, parity, abort_flag, status)) != 0;
+}
 // one arrival for a warp whose lanes are all done
 __device__ __forceinline__ void warp_arrive(unsigned long long* bar) {
   __syncwarp();
@@ -142,6 +146,35 @@ __device__ __forceinline__ void tanh_pieces(uint32_t (&y)[32]) {
     s = fma_f2(s, z, pack_f2(c0, c0));
     unpack_u2(mul_f2(y2, s), y[2 * j], y[2 * j + 1]);
   }
+}
+
+// Issued by one elected thread of a warp whose lanes are together, so that descriptors stay in uniform registers (from a branch of lane 0
+// alone each operand is moved there anew: 70-90 cycles per product instead of the 32-64 it takes)
+__device__ __forceinline__ void ck_mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void ck_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void ck_commit(unsigned long long* bar) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+      ::"r"(smem_u32(bar))
+      : "memory");
 }
 
 struct CkItem {
@@ -248,7 +281,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
 
   if (warp == kCkThreads / 32 - 1) {
     // =============================== products ===================================================
-    if (lane == 0) {
+    {
       bool alive = true;
       uint32_t T = 0, n_item = 0, n_p[2] = {0, 0}; // tiles and items so far; tiles of either half
       // operand descriptors: the low words hold the address (in units of 16 bytes, far from a carry), the high words stay
@@ -263,34 +296,34 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
             constexpr uint32_t kStep = kCkChunkBytes >> 4;
-            tc_mma_bf16(tmem + x * 128, pack_u2(q_lo + (kk >> 2) * kStep + 2 * (kk & 3), kmajor_hi),
+            ck_mma_ss(tmem + x * 128, pack_u2(q_lo + (kk >> 2) * kStep + 2 * (kk & 3), kmajor_hi),
                         pack_u2(k_lo + (kk >> 2) * kStep + 2 * (kk & 3), kmajor_hi), kCkIdescS, kk > 0 ? 1u : 0u);
           }
-          tc_commit(smem_u32(&t.s_full[x]));
-          if (x == it.act - 1) tc_commit(smem_u32(&t.k_empty[tile & 1]));
+          ck_commit(&t.s_full[x]);
+          if (x == it.act - 1) ck_commit(&t.k_empty[tile & 1]);
         };
         // (of both tiles, at work or not: this thread is then never two items ahead of either's softmax warps)
-        for (int x = 0; x < 2 && alive; ++x) alive = ck_wait(&t.q_full[x], n_item & 1, abort_flag, a.status);
-        if (alive) alive = ck_wait(&t.k_full[T & 1], (T >> 1) & 1, abort_flag, a.status);
+        for (int x = 0; x < 2 && alive; ++x) alive = ck_wait_warp(&t.q_full[x], n_item & 1, abort_flag, a.status);
+        if (alive) alive = ck_wait_warp(&t.k_full[T & 1], (T >> 1) & 1, abort_flag, a.status);
         if (!alive) break;
         tc_fence_after();
         for (int x = 0; x < it.act; ++x) issue_s(x, T);
         for (int tile = 0; tile < it.n_tiles && alive; ++tile, ++T) {
-          if (!ck_wait(&t.v_full[T & 1], (T >> 1) & 1, abort_flag, a.status)) { alive = false; break; }
+          if (!ck_wait_warp(&t.v_full[T & 1], (T >> 1) & 1, abort_flag, a.status)) { alive = false; break; }
           const uint32_t v_lo = v_lo0 + (T & 1) * (kTileBytes >> 4);
           for (int x = 0; x < it.act && alive; ++x) {
-            if (!ck_wait(&t.p_ready[x], n_p[x] & 1, abort_flag, a.status)) { alive = false; break; }
+            if (!ck_wait_warp(&t.p_ready[x], n_p[x] & 1, abort_flag, a.status)) { alive = false; break; }
             ++n_p[x];
             tc_fence_after();
 #pragma unroll
             for (int kk = 0; kk < 8; ++kk)         // 16 keys: 8 columns of packed probabilities, 2048 bytes of value rows
-              tc_mma_bf16_tmem_a(tmem + 256 + x * D, tmem + x * 128 + 8 * kk, pack_u2(v_lo + 128 * kk, v_hi), ck_idesc_pv<D>(),
+              ck_mma_ts(tmem + 256 + x * D, tmem + x * 128 + 8 * kk, pack_u2(v_lo + 128 * kk, v_hi), ck_idesc_pv<D>(),
                                  (tile > 0 || kk > 0) ? 1u : 0u);
-            if (tile + 1 == it.n_tiles) tc_commit(smem_u32(&t.o_done[x]));
-            if (x == it.act - 1) tc_commit(smem_u32(&t.v_empty[T & 1]));
+            if (tile + 1 == it.n_tiles) ck_commit(&t.o_done[x]);
+            if (x == it.act - 1) ck_commit(&t.v_empty[T & 1]);
             if (tile + 1 < it.n_tiles) {
               if (x == 0) {
-                if (!ck_wait(&t.k_full[(T + 1) & 1], ((T + 1) >> 1) & 1, abort_flag, a.status)) { alive = false; break; }
+                if (!ck_wait_warp(&t.k_full[(T + 1) & 1], ((T + 1) >> 1) & 1, abort_flag, a.status)) { alive = false; break; }
                 tc_fence_after();
               }
               issue_s(x, T + 1);
@@ -300,7 +333,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       }
       if (!alive) {
         // every product issued so far retires before the tensor memory is given back
-        tc_commit(smem_u32(&t.drain));
+        ck_commit(&t.drain);
         mbar_drain(smem_u32(&t.drain), 0);
       }
     }
