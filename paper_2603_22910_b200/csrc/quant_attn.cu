@@ -114,10 +114,11 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) {
 }
 
 // What the kernel needs of a sequence: w = 0 tokens where nothing is attended here.
-__device__ __forceinline__ int4 seq_info(const QuantAttnArgs& a, int b, bool tell) {
+// (without: the sequences of many rows are the chunk kernel's)
+__device__ __forceinline__ int4 seq_info(const QuantAttnArgs& a, int b, bool tell, bool without) {
   const QuantSeq s = quant_seq(a, b);
   if (s.error && tell) report_opt(a.status, s.error);
-  return make_int4(s.slot, s.len, s.first, s.error || chunk_sequence(a, s) ? 0 : s.n);
+  return make_int4(s.slot, s.len, s.first, s.error || (without && many_rows(a, s)) ? 0 : s.n);
 }
 __device__ __forceinline__ int row_tiles(const QuantAttnArgs& a, int n) { return (n * a.group + kQaRows - 1) / kQaRows; }
 __device__ __forceinline__ unsigned long long units_of(const QuantAttnArgs& a, const int4& s) {
@@ -236,12 +237,13 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_v) : "memory");
   }
   // ---- the units of the call, and this CTA's and warp's share of them
+  const bool without = take_chunks(a, a.sm_count);
   const int per = (a.B + kQaThreads - 1) / kQaThreads;
   {
     unsigned long long n = 0;
 #pragma unroll 1
     for (int b = tid * per; b < min(a.B, (tid + 1) * per); ++b) {
-      const int4 s = seq_info(a, b, blockIdx.x == 0);
+      const int4 s = seq_info(a, b, blockIdx.x == 0, without);
       if (per == 1) sm.info[b] = s;
       n += units_of(a, s);
     }
@@ -288,12 +290,12 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
   uint32_t filled = 0, used = 0;                  // blocks this warp has asked for and taken from its ring
   bool dead = false;                              // a copy did not arrive (reported); the warp gives up
   while (u < u_end && !dead) {
-    int4 info = per == 1 ? sm.info[b] : seq_info(a, b, false);
+    int4 info = per == 1 ? sm.info[b] : seq_info(a, b, false, without);
     unsigned long long n_units = units_of(a, info);
     while (base + n_units <= u) {
       base += n_units;
       ++b;
-      info = per == 1 ? sm.info[b] : seq_info(a, b, false);
+      info = per == 1 ? sm.info[b] : seq_info(a, b, false, without);
       n_units = units_of(a, info);
     }
     const int slot = info.x, len = info.y, first_token = info.z, n_new = info.w;
@@ -858,7 +860,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
       for (int e = 0; e < E; ++e) acc[e] += wk * o[e];
     }
     if (starts && ends) {
-      const int4 s = per == 1 ? sm.info[first.b] : seq_info(a, first.b, false);
+      const int4 s = per == 1 ? sm.info[first.b] : seq_info(a, first.b, false, without);
       const int qrow = first.tile * kQaRows + warp;
       if (qrow < s.w * a.group) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -898,7 +900,7 @@ __global__ void __launch_bounds__(kQaMergeThreads) quant_merge_kernel(const __gr
   const QaDesc d = ws.desc[blockIdx.x];
   if (d.n_parts == 0) return;
   const auto part = [&](int p) -> long long { return ((long long)(blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * kQaRows + row; };
-  const int4 s = seq_info(a, d.b, false);
+  const int4 s = seq_info(a, d.b, false, false);
   float m = -INFINITY;
   for (int p = lane; p < d.n_parts; p += 32) m = fmaxf(m, ws.ml[part(p)].x);
   m = warp_max(m);

@@ -186,7 +186,7 @@ struct CkItem {
 // chunk sequences only; w = 0 otherwise
 __device__ __forceinline__ int4 ck_seq(const QuantAttnArgs& a, int b) {
   const QuantSeq s = quant_seq(a, b);
-  return make_int4(s.slot, s.len, s.first, s.error || !chunk_sequence(a, s) ? 0 : s.n);
+  return make_int4(s.slot, s.len, s.first, many_rows(a, s) ? s.n : 0);
 }
 __device__ __forceinline__ unsigned long long ck_items(const QuantAttnArgs& a, const int4& s) {
   return (unsigned long long)(((long long)s.w * a.group + kCkRows - 1) / kCkRows) * a.g.n_kv_heads;
@@ -207,6 +207,8 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
   const QuantGeom& g = a.g;
   const int H = g.n_kv_heads;
   volatile int* abort_flag = &t.abort_flag;
+
+  if (!take_chunks(a, a.sm_count)) return;         // (the same answer in every thread)
 
   // ---- barriers, tensor memory, and the items of the call
   const int per = (a.B + kCkThreads - 1) / kCkThreads;
@@ -330,6 +332,8 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
             }
           }
         }
+        // (an idle second half waits for this too: its warps must not run items ahead of the barriers' phases)
+        if (alive && it.act == 1) ck_commit(&t.o_done[1]);
       }
       if (!alive) {
         // every product issued so far retires before the tensor memory is given back
@@ -590,6 +594,8 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       warp_arrive(&t.q_full[x]);
       if (x >= it.act) {
         T += it.n_tiles;
+        if (!__all_sync(0xffffffffu, ck_wait(&t.o_done[x], n_done & 1, abort_flag, a.status))) break;
+        ++n_done;
         continue;
       }
       const float slope2 = a.slopes && row_ok ? a.slopes[head] * kLog2e : 0.f;

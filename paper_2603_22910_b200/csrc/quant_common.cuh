@@ -38,8 +38,33 @@ __device__ __forceinline__ QuantSeq quant_seq(const QuantAttnArgs& a, int b) {
   return s;
 }
 
-__device__ __forceinline__ bool chunk_sequence(const QuantAttnArgs& a, const QuantSeq& s) {
-  return a.chunk_rows > 0 && s.n * a.group >= a.chunk_rows;
+// Which of the two attention kernels takes the sequences of many query rows (chunk_rows of them per KV head and more)?  The row
+// kernel cuts the work of all sequences into equal shares for the whole machine, in units of 16 keys x 8 query rows; the chunk kernel
+// gives 256 query rows and all their keys to one CTA.  Measured (32 / 8 heads of 128, int8): a unit takes the machine 0.63 ns; 128
+// keys of an item take its CTA 2.9 us, as long as the machine takes for 4600 units, so a block of 16 keys for 576.  The chunk
+// kernel's time is that of the longest item, or of all of them over the SMs where they are many.  (One sequence over 8192 keys:
+// 64 tokens 89 us by rows, 185 by chunks, 256 tokens the other way round; 8 sequences: 16 tokens 166 and 165 us, 64 tokens 613
+// and 201.)  Both kernels compute the answer from the lengths, every thread of a block the same one.
+constexpr unsigned long long kChunkUnits = 576;
+__device__ __forceinline__ bool many_rows(const QuantAttnArgs& a, const QuantSeq& s) {
+  return a.chunk_rows > 0 && !s.error && (long long)s.n * a.group >= a.chunk_rows;
+}
+__device__ __forceinline__ bool take_chunks(const QuantAttnArgs& a, int sm_count) {
+  if (a.chunk_rows == 0) return false;
+  __shared__ unsigned long long sums[3];           // units by rows; blocks of all items; blocks of the longest
+  if (threadIdx.x == 0) sums[0] = sums[1] = sums[2] = 0;
+  __syncthreads();
+  for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
+    const QuantSeq s = quant_seq(a, b);
+    if (!many_rows(a, s)) continue;
+    const unsigned long long rows = (unsigned long long)s.n * a.group, blocks = (s.len + kQuantBlock - 1) / kQuantBlock;
+    atomicAdd(&sums[0], (rows + 7) / 8 * blocks * a.g.n_kv_heads);
+    atomicAdd(&sums[1], (rows + 255) / 256 * blocks * a.g.n_kv_heads);
+    atomicMax(&sums[2], blocks);
+  }
+  __syncthreads();
+  const unsigned long long longest = sums[1] / sm_count > sums[2] ? sums[1] / sm_count : sums[2];
+  return sums[0] > kChunkUnits * longest;
 }
 
 __device__ __forceinline__ float exp2_approx(float x) {

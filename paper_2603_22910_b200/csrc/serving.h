@@ -122,8 +122,9 @@ struct QuantAttnArgs {
   const int32_t* prefix;       // or null
   int B, n_tokens, max_new;
   int n_q_heads, group, group_shift, dtype, format;
-  int chunk_rows;              // sequences with at least this many query rows per KV head (new tokens x group) are the
-                               // chunk kernel's; 0: there is none
+  int chunk_rows;              // sequences with at least this many query rows per KV head (new tokens x group) can be the
+                               // chunk kernel's; 0: there is none (see take_chunks)
+  int sm_count;
   float scale, softcap;
   unsigned char* ws;
   int32_t* status;

@@ -11,8 +11,8 @@ using namespace echokv;
 namespace {
 
 constexpr int kMaxDevices = 64;
-constexpr int kChunkRows = 64;      // query rows per KV head (new tokens x query heads that share it) from which a bf16 sequence is the chunk
-                                    // kernel's
+constexpr int kChunkRows = 64;      // query rows per KV head (new tokens x query heads that share it) from which a bf16 sequence can be the
+                                    // chunk kernel's
 
 int sm_count_of(int device, int* out) {
   static std::mutex mutex;
@@ -286,6 +286,7 @@ int echokv_quant_attention(const echokv_config* cfg, const echokv_quant_cache* c
   a.status = dev_status;
   OnDevice dev(cfg->device);
   if (!dev.ok()) return ECHOKV_ECUDA;
+  a.sm_count = dev.sm_count;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (a.chunk_rows > 0 && launch_quant_chunk(a, dev.sm_count, s) != cudaSuccess) return ECHOKV_ECUDA;
   return launch_quant_attn(a, dev.sm_count, s) == cudaSuccess ? ECHOKV_OK : ECHOKV_ECUDA;

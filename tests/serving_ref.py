@@ -119,15 +119,15 @@ class Cache:
         return y
 
 
-def attend(q, k, v, scale, softcap=0.0, slopes=None, prefix=0):
-    """q [n][Hq][d] = the last n tokens, k, v [L][H][d] float64 -> (out [n][Hq][d], bound [n][Hq] of |error| per unit roundoff:
-    the largest sum |q_i k_i| scale of a seen key, and the largest |v| of the head)."""
+def attend(q, k, v, scale, softcap=0.0, slopes=None, prefix=0, only=None):
+    """q [n][Hq][d] = the last n tokens, k, v [L][H][d] float64 -> (out [n][Hq][d], size [n][Hq][2]: the largest sum |q_i k_i| scale
+    of a seen key, and the largest |v| of one); only: the queries that are worked out (the others' rows stay 0)."""
     n, Hq, d = q.shape
     L, H, _ = k.shape
     out = np.zeros((n, Hq, d))
     size = np.zeros((n, Hq, 2))
     t = np.arange(L)
-    for i in range(n):
+    for i in range(n) if only is None else only:
         p = L - n + i
         seen = (t <= p) | (t < prefix)
         for h in range(Hq):

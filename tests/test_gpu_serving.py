@@ -413,6 +413,100 @@ def test_chunks_match_plain_form(fmt, dtype, d, page, n_q, n_kv, before, new, op
     assert p.status.item() == 0
 
 
+def sampled(rng, n):
+    return sorted({0, 1, n // 2, n - 2, n - 1} | set(rng.integers(0, n, 12).tolist()) | set(range(60, min(n, 70))))
+
+
+@pytest.mark.parametrize("opts", [{}, dict(softcap=50.0), dict(softcap=6.0), dict(softcap=0.5), dict(slopes=True), dict(prefix=True),
+                                  dict(softcap=10.0, slopes=True, prefix=True)])
+@pytest.mark.parametrize("fmt,d,page,n_q,n_kv,before,new", [
+    ("int8", 128, 16, 16, 8, [0, 77], [400, 513]), ("e4m3", 64, 64, 8, 8, [300], [700]), ("e4m3", 128, 128, 32, 4, [1003, 0, 0], [150, 299, 1]),
+    ("int8", 64, 32, 4, 4, [0, 9, 130], [640, 640, 641])])
+def test_large_chunks_match_plain_form(opts, fmt, d, page, n_q, n_kv, before, new):
+    """Sizes that go to the tcgen05 kernel: odd lengths, several items, open blocks in the last tile, every score transform."""
+    B = len(new)
+    cfg = config(n_q=n_q, n_kv=n_kv, d=d, page=page, batch=B, pages=1280 // page, n_pages=B * 1280 // page)
+    p = Program(cfg, fmt, seed=n_q + d)
+    p.step(before)
+    p.step(new)
+    kw = dict(opts)
+    if "slopes" in kw:
+        kw["slopes"] = [2.0 ** (-8.0 * (h + 1) / n_q) for h in range(n_q)]
+    if "prefix" in kw:
+        kw["prefix"] = [(n + o) * 2 // 3 for n, o in zip(new, before)]
+    q = p.rows(sum(new), n_q, 2.5)
+    out = attend(p, new, q, **dict(kw))
+    assert p.status.item() == 0 and torch.isfinite(out).all()
+    at = 0
+    for b, n in enumerate(new):
+        only = sampled(p.rng, n) if n > 1 else [0]
+        ref, size = R.attend(f64(q[at:at + n]), p.ref.values(p.ref.k[b]), p.ref.values(p.ref.v[b]), d ** -0.5, kw.get("softcap", 0.0),
+                             kw.get("slopes"), kw["prefix"][b] if "prefix" in kw else 0, only=only)
+        tol = R.tolerance(ref, size, p.lens[b], EPS["bf16"], True, True, kw.get("softcap", 0.0), kw.get("slopes"))
+        err = np.abs(f64(out[at:at + n]) - ref)[only]
+        assert (err <= tol[only]).all(), (b, n, float((err / tol[only]).max()))
+        at += n
+
+
+def test_chunk_whose_scores_grow_and_whose_prefix_is_all():
+    """A reference that has to move in the middle of tiles (keys that grow along the sequence), rows that see the whole sequence, and
+    the same chunk again: the result does not depend on what ran before."""
+    cfg = config(n_q=8, n_kv=8, d=128, page=64, batch=1, pages=12, n_pages=12)
+    p = Program(cfg, "int8", seed=31)
+    k, v = p.rows(700, 8), p.rows(700, 8)
+    k = (k.float() * torch.linspace(0.1, 12, 700, device="cuda")[:, None, None]).bfloat16()
+    p.step([700], k, v)
+    q = p.rows(650, 8, 2.0)
+    for prefix in (0, 700):
+        outs = [attend(p, [650], q, prefix=[prefix]) for _ in range(2)]
+        assert torch.equal(outs[0], outs[1])
+        only = sampled(p.rng, 650)
+        ref, size = R.attend(f64(q), p.ref.values(p.ref.k[0]), p.ref.values(p.ref.v[0]), 128 ** -0.5, prefix=prefix, only=only)
+        tol = R.tolerance(ref, size, 700, EPS["bf16"], True, True)
+        err = np.abs(f64(outs[0]) - ref)[only]
+        assert (err <= tol[only]).all(), float((err / tol[only]).max())
+
+
+@pytest.mark.parametrize("kv", [0, 1])
+def test_infinities_and_nan_in_masked_places_of_chunks(kv):
+    cfg = config(n_q=8, n_kv=8, d=64, page=16, batch=1, pages=48, n_pages=60)
+    nan, inf = float("nan"), float("inf")
+    p = Program(cfg, "e4m3", seed=6)
+    for t in (p.cache.k_tail, p.cache.v_tail, p.cache.k_scales, p.cache.v_scales):
+        t.fill_(nan)
+    x = [p.rows(650, 8), p.rows(650, 8)]
+    x[kv][330, 0, 3], x[kv][648, 1, 9] = nan, inf        # blocks 320.. (codes) of head 0 and 640.. (open) of head 1
+    p.step([650], *x)
+    q = p.rows(650, 8)
+    bad = np.isnan(f64(attend(p, [650], q))).any(-1)
+    first = np.arange(650)
+    assert (bad[:, 0] == (first >= 320)).all() and (bad[:, 1] == (first >= 640)).all() and not bad[:, 2:].any()
+
+
+@pytest.mark.parametrize("n_q,n_kv,d,new", [(8, 2, 64, [16] * 250), (4, 4, 128, [64, 1, 100, 3, 80, 128] * 40), (8, 8, 64, [70, 260, 130] * 35)])
+def test_many_chunks_of_few_rows(n_q, n_kv, d, new):
+    """More items than SMs, several per CTA, most with one tile of query rows (the other one idle) beside sequences that the row
+    kernel takes."""
+    B = len(new)
+    cfg = config(n_q=n_q, n_kv=n_kv, d=d, page=32, batch=B, pages=12, n_pages=12 * B)
+    p = Program(cfg, "e4m3", seed=21)
+    before = [int(x) for x in p.rng.integers(0, 40, B)]
+    p.step(before)
+    p.step(new)
+    q = p.rows(sum(new), n_q, 2.0)
+    out = attend(p, new, q)
+    assert p.status.item() == 0
+    # (the oracle is slow: a sample of the sequences, all of them are finite)
+    assert torch.isfinite(out).all()
+    at = np.concatenate([[0], np.cumsum(new)])
+    for b in sorted({0, 1, 2, B // 3, B // 2, B - 3, B - 2, B - 1}):
+        k, v = p.ref.values(p.ref.k[b]), p.ref.values(p.ref.v[b])
+        ref, size = R.attend(f64(q[at[b]:at[b + 1]]), k, v, d ** -0.5)
+        tol = R.tolerance(ref, size, p.lens[b], EPS["bf16"], True, new[b] * n_q // n_kv >= CHUNK_ROWS)
+        err = np.abs(f64(out[at[b]:at[b + 1]]) - ref)
+        assert (err <= tol).all(), (b, new[b], float((err / tol).max()))
+
+
 def test_one_long_sequence_is_split_over_the_machine():
     cfg = config(n_q=4, n_kv=1, d=128, page=16, batch=1, pages=2000, n_pages=2100)
     p = Program(cfg, "int8", seed=5)
