@@ -461,7 +461,7 @@ int echokv_quant_append(const echokv_config* cfg, const echokv_quant_cache* cach
                         int n_tokens, int32_t* dev_status, void* stream);
 
 /* What is done to the scores x = softmax_scale q . k before the softmax; zeros / NULL = nothing.  In this order:
- *     softcap > 0:   x = softcap * tanh(x / softcap)
+ *     softcap > 0:   x = softcap * tanh(x / softcap)            (at least 1e-30, EINVAL)
  *     alibi_slopes:  x = x - alibi_slopes[h] * |p - t|      (p, t: positions of the query and the key)
  *     mask:          key t is seen if t <= p or t < prefix_lens[b]  (a prefix whose tokens see each other)        */
 typedef struct {
@@ -475,7 +475,8 @@ typedef struct {
  * last n tokens, already appended: query i sits at position dev_seq_lens[b] - n + i.
  *  - q: [n_tokens] rows of n_q_heads x head_dim elements, q_stride elements from row to row; out: dense
  *    [n_tokens][n_q_heads][head_dim] of the storage dtype (both 16-byte aligned).
- *  - dev_cu_tokens: [B + 1], or NULL for one token per sequence (n_tokens = B).  max_new: an upper bound of the tokens
+ *  - n_tokens: at most 2^27 (EINVAL; also echokv_quant_append's).  dev_cu_tokens: [B + 1], or NULL for one token per
+ *    sequence (n_tokens = B).  max_new: an upper bound of the tokens
  *    any sequence has in this call (1 for a decode step): it selects the kernels.
  *  - workspace: device buffer of echokv_quant_sizes.workspace_bytes, 256-byte aligned.  Calls that share one must
  *    not overlap on the device (captured graphs may share it if they run one after the other); nothing is kept in it.

@@ -11,6 +11,7 @@ using namespace echokv;
 namespace {
 
 constexpr int kMaxDevices = 64;
+constexpr int kMaxRows = 1 << 27;   // new tokens of a call: times 8 query heads they still fit 31 bits
 constexpr int kChunkRows = 64;      // query rows per KV head (new tokens x query heads that share it) from which a bf16 sequence can be the
                                     // chunk kernel's
 
@@ -235,7 +236,7 @@ int echokv_quant_append(const echokv_config* cfg, const echokv_quant_cache* cach
                         int n_tokens, int32_t* dev_status, void* stream) {
   int rc = check_all(cfg);
   if (rc != ECHOKV_OK) return rc;
-  if (B < 1 || n_tokens < 0 || n_tokens > (1 << 30)) return ECHOKV_EINVAL;
+  if (B < 1 || n_tokens < 0 || n_tokens > kMaxRows) return ECHOKV_EINVAL;
   QuantAppendArgs a;
   if ((rc = quant_geom(cfg, cache, &a.g)) != ECHOKV_OK) return rc;
   if (B > cfg->max_batch) return ECHOKV_ECAPACITY;
@@ -260,11 +261,12 @@ int echokv_quant_attention(const echokv_config* cfg, const echokv_quant_cache* c
                            void* stream) {
   int rc = check_all(cfg);
   if (rc != ECHOKV_OK) return rc;
-  if (B < 1 || n_tokens < 0 || n_tokens > (1 << 30) || max_new < 1) return ECHOKV_EINVAL;
+  if (B < 1 || n_tokens < 0 || n_tokens > kMaxRows || max_new < 1) return ECHOKV_EINVAL;
   if (!dev_cu_tokens && (n_tokens != B || max_new != 1)) return ECHOKV_EINVAL;
   QuantAttnArgs a;
   if ((rc = quant_geom(cfg, cache, &a.g)) != ECHOKV_OK) return rc;
-  if (options && (!(options->softcap >= 0.f) || !std::isfinite(options->softcap))) return ECHOKV_EINVAL;
+  // (a cap so small that its inverse leaves fp32's range is no cap anybody means)
+  if (options && (!(options->softcap == 0.f || options->softcap >= 1e-30f) || !std::isfinite(options->softcap))) return ECHOKV_EINVAL;
   if (B > cfg->max_batch) return ECHOKV_ECAPACITY;
   if (n_tokens == 0) return ECHOKV_OK;
   const int elem = cfg->dtype == ECHOKV_BF16 ? 2 : 4;

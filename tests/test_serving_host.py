@@ -113,13 +113,14 @@ def test_quant_cache_pointers(lib, field):
 def test_quant_refusals(lib):
     assert append_call(lib, cache=quant_struct(format=2)) == EINVAL
     for kw in (dict(k=None), dict(v=None), dict(ks=1023), dict(vs=1028), dict(k=P1 + 2), dict(rows=None), dict(seqs=None), dict(cu=None),
-               dict(B=0), dict(n=-1)):
+               dict(B=0), dict(n=-1), dict(n=(1 << 27) + 1)):
         assert append_call(lib, **kw) == EINVAL, kw
     assert append_call(lib, B=5) == ECAP
     assert append_call(lib, n=0, k=None) == 0
     for kw in (dict(q=None), dict(out=None), dict(out=P1 + 8), dict(table=None), dict(lens=None), dict(qs=4000), dict(max_new=0), dict(B=0),
                dict(cu=None, n=4, B=2), dict(cu=None, n=2, max_new=2), dict(ws=None), dict(ws=P1 + 128),
-               dict(opts=binding.echokv_score_options(-1.0, 0, None, None)),
+               dict(opts=binding.echokv_score_options(-1.0, 0, None, None)), dict(opts=binding.echokv_score_options(1e-33, 0, None, None)),
+               dict(n=(1 << 27) + 1),
                dict(opts=binding.echokv_score_options(float("nan"), 0, None, None))):
         assert attn_call(lib, **kw) == EINVAL, kw
     need = binding.query_quant_sizes(config()).workspace_bytes
