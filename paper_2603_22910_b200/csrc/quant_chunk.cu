@@ -19,6 +19,8 @@
 // V codes times (their scale / the largest scale the row can see) times 64 are below 2^15.
 // Bound: 128 exponentials per row and tile at 16 per clock and SM take twice the products' time.
 // Work items are dealt out by CTA number, those with the most keys first; every wait is bounded.
+#include <type_traits>
+
 #include "quant_common.cuh"
 
 namespace echokv {
@@ -31,6 +33,8 @@ constexpr int kCkSoftmaxThreads = 256, kCkConvThreads = 224;
 constexpr int kCkThreads = kCkSoftmaxThreads + kCkConvThreads + 32;
 constexpr int kCkChunkBytes = kCkTile * 128;       // [128 rows x 64 features] fp16, 128-byte swizzle
 constexpr int kCkRing = 4;                         // scales and V references: see where they are written
+constexpr float kCkMargin = 8.f;                   // a reference that moves goes 2^8 above the largest score: what comes may be 2^23 larger
+                                                   // before it moves again, and fp16 still holds the largest probability's 2^-17
 constexpr float kCkSumLimit = 32768.f;             // a row's 32 probabilities sum to less: each fits fp16
 constexpr float kCkVScale = 64.f;
 
@@ -124,16 +128,21 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 
-// y -> tanh(y) for 32 of them, two at a time: y times a polynomial in z = y^2, the nearest one in the largest relative error (found by
-// iteratively reweighted least squares on Chebyshev points) -- of degree 3 for z <= 1/4 (5.5e-7) and of degree 5 for
-// z <= 1 (6e-7).
+// x -> tanh(g x) for 32 of them (g[0] for the first 16), two at a time: y times a polynomial in z = y^2, the nearest one in the largest
+// relative error (found by iteratively reweighted least squares on Chebyshev points) -- of degree 3 for z <= 1/4 (5.5e-7) or
+// of degree 5 for z <= 1 (6e-7).  Returns the largest z (a NaN is smaller than anything here and stays one).
 template <bool SMALL>
-__device__ __forceinline__ void tanh_pieces(uint32_t (&y)[32]) {
+__device__ __forceinline__ float tanh_pieces(uint32_t (&x)[32], float g0, float g1) {
   constexpr float c0 = SMALL ? 0.999999463558197f : 0.9999994039535522f, c1 = SMALL ? -0.33326318860054016f : -0.3332904279232025f,
                   c2 = SMALL ? 0.13190296292304993f : 0.13281434774398804f, c3 = SMALL ? -0.04440222680568695f : -0.05160567909479141f;
+  float top = 0.f;
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
-    const uint64_t y2 = pack_u2(y[2 * j], y[2 * j + 1]), z = mul_f2(y2, y2);
+    const float g = j < 8 ? g0 : g1;
+    const uint64_t y = mul_f2(pack_u2(x[2 * j], x[2 * j + 1]), pack_f2(g, g)), z = mul_f2(y, y);
+    float z0, z1;
+    unpack_f2(z, z0, z1);
+    top = max3(top, z0, z1);
     uint64_t s;
     if (SMALL) {
       s = pack_f2(c3, c3);
@@ -144,8 +153,9 @@ __device__ __forceinline__ void tanh_pieces(uint32_t (&y)[32]) {
     s = fma_f2(s, z, pack_f2(c2, c2));
     s = fma_f2(s, z, pack_f2(c1, c1));
     s = fma_f2(s, z, pack_f2(c0, c0));
-    unpack_u2(mul_f2(y2, s), y[2 * j], y[2 * j + 1]);
+    unpack_u2(mul_f2(y, s), x[2 * j], x[2 * j + 1]);
   }
+  return top;
 }
 
 // Issued by one elected thread of a warp whose lanes are together, so that descriptors stay in uniform registers (from a branch of lane 0
@@ -175,6 +185,88 @@ __device__ __forceinline__ void ck_commit(unsigned long long* bar) {
       "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
       ::"r"(smem_u32(bar))
       : "memory");
+}
+
+// What the softmax of a row needs beside its scores.
+struct CkRow {
+  uint32_t s_addr, o_addr;                         // tensor memory: scores (and probabilities) of the tile, output so far
+  float c_row, cap_in, cap_out, slope2;
+  int capped, biased;
+  int pos;
+};
+// 32 keys of a row (columns 32 c .. of the tile, keys key0 ..) the careful way: any score transform, masks (the first n_vis keys of the tile
+// are seen), and the reference moved where the probabilities need it -- then what the row has so far (its sum, the
+// probabilities of this tile already stored, its output if there is one) is scaled by a power of two.  m: the reference, a
+// whole number, -inf until the row has seen a key.  Returns (m, l).  A function of its own, so that the common way's registers
+// and instructions are its own too.
+template <int D>
+__device__ __noinline__ float2 careful_piece(const CkRow w, const int c, const int key0, const int n_vis, const bool has_output, float f0,
+                                             float f1, float m_ref, float l_run) {
+  uint32_t sr[32], pk[16];
+  tmem_st_wait();
+  tmem_ld32_issue(w.s_addr + 32 * c, sr);
+  tmem_ld_wait();
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    float y = __uint_as_float(sr[j]) * (j < 16 ? f0 : f1);
+    if (w.capped) y = w.cap_out * tanh_f32(y * w.cap_in);
+    if (w.biased) y -= w.slope2 * fabsf((float)(w.pos - key0 - j));
+    sr[j] = __float_as_uint(32 * c + j < n_vis ? y : -INFINITY);
+  }
+  float sum = 0.f;
+#pragma unroll 1
+  for (int attempt = 0;; ++attempt) {
+    const float m = m_ref == -INFINITY ? 0.f : m_ref;
+    sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const float p0 = exp2_approx(__uint_as_float(sr[2 * j]) - m), p1 = exp2_approx(__uint_as_float(sr[2 * j + 1]) - m);
+      sum += p0 + p1;
+      pk[j] = h2(p0, p1);
+    }
+    const bool move = !(sum < kCkSumLimit) || m_ref == -INFINITY;
+    if (attempt > 0 || !__any_sync(0xffffffffu, move)) break;
+    float alpha = 1.f;
+    if (move) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) mx = fmaxf(mx, __uint_as_float(sr[j]));
+      if (mx > m_ref - kCkMargin) {
+        const float m_new = ceilf(mx) + kCkMargin;
+        if (m_ref > -INFINITY) alpha = exp2_approx(m_ref - m_new);
+        m_ref = m_new;
+      }
+      l_run *= alpha;
+    }
+    // (through fp32: probabilities near fp16's largest times a power of two below its smallest)
+#pragma unroll 1
+    for (int cc = 0; cc < c; ++cc) {
+      uint32_t old[32];
+      tmem_ld16_issue(w.s_addr + 16 * cc, old);
+      tmem_ld_wait();
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const float2 p = h2_float(old[j]);
+        old[j] = h2(p.x * alpha, p.y * alpha);
+      }
+      tmem_st16(w.s_addr + 16 * cc, old);
+    }
+    if (has_output) {
+      // O is at rest (the product that wrote these scores came after every earlier one)
+#pragma unroll 1
+      for (int cc = 0; cc < D / 16; ++cc) {
+        uint32_t old[32];
+        tmem_ld16_issue(w.o_addr + 16 * cc, old);
+        tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) old[j] = __float_as_uint(__uint_as_float(old[j]) * alpha);
+        tmem_st16(w.o_addr + 16 * cc, old);
+      }
+    }
+    tmem_st_wait();
+  }
+  tmem_st16_regs(w.s_addr + 16 * c, pk);
+  return make_float2(m_ref, l_run + sum);
 }
 
 struct CkItem {
@@ -557,7 +649,6 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
     const int x = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lane_base = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t s_addr = lane_base + x * 128, o_addr = lane_base + 256 + x * D;
-    const bool plain = !(a.softcap > 0.f) && a.slopes == nullptr;
     const float cap_in = a.softcap > 0.f ? 1.f / a.softcap : 0.f, cap_out = a.softcap * kLog2e;
     uint32_t T = 0, n_item = 0, n_mine = 0, n_done = 0;   // (of this half: tiles and results, whose barriers move with them)
     for (unsigned long long i = blockIdx.x; i < total; i += gridDim.x, ++n_item) {
@@ -568,27 +659,33 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       const int pos = it.len - it.n + qi;
       // keys [0, vis) are seen; a row of none of the queries sees everything (its scores are 0) and goes nowhere
       const int vis = row_ok ? max(pos + 1, it.prefix) : 0x7fffffff;
+      // the warp's 32 query rows as fp16 around each row's power of two: 16 (8) lanes to a row, so that they read it side by side
       float c_row = 0.f;
       {
-        const uint4* qp = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (long long)(it.first + qi) * a.q_stride +
-                                                         (long long)head * D);
-        uint32_t w[D / 2];
-#pragma unroll
-        for (int p = 0; p < D / 8; ++p) {
+        constexpr int kLanes = D / 8, kPerGo = 32 / kLanes;
+        const int my = lane / kLanes, p = lane % kLanes;
+        const int r_warp = it.row0 + x * kCkTile + (warp & 3) * 32;
+        const __nv_bfloat16* qb = static_cast<const __nv_bfloat16*>(a.q) + (long long)it.first * a.q_stride + (long long)it.h * a.group * D + 8 * p;
+#pragma unroll 4
+        for (int go = 0; go < kLanes; ++go) {
+          const int rr = go * kPerGo + my, rq = r_warp + rr;           // row of the warp, of the sequence
           uint4 v = make_uint4(0u, 0u, 0u, 0u);
-          if (row_ok) v = qp[p];
-          w[4 * p] = v.x; w[4 * p + 1] = v.y; w[4 * p + 2] = v.z; w[4 * p + 3] = v.w;
+          if (rq < it.n_rows) v = *reinterpret_cast<const uint4*>(qb + (long long)(rq >> a.group_shift) * a.q_stride + (rq & (a.group - 1)) * D);
+          uint32_t top = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+          top = max(top & 0xffff0000u, top << 16);
+#pragma unroll
+          for (int o = kLanes / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+          float back;
+          const float up = scale_up_to_half(__uint_as_float(top), &back);
+          const uint32_t y[4] = {v.x, v.y, v.z, v.w};
+          uint32_t z[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z[e] = h2(__uint_as_float(y[e] << 16) * up, __uint_as_float(y[e] & 0xffff0000u) * up);
+          sts16(q_addr + x * kTileBytes + ck_off((warp & 3) * 32 + rr, p), z[0], z[1], z[2], z[3]);
+          const float mine = __shfl_sync(0xffffffffu, back, (lane % kPerGo) * kLanes);       // of row go * kPerGo + lane % kPerGo
+          if (lane / kPerGo == go) c_row = mine;
         }
-        float top = 0.f;
-#pragma unroll
-        for (int e = 0; e < D / 2; ++e) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[e] << 16)), fabsf(__uint_as_float(w[e] & 0xffff0000u))));
-        float back;
-        const float up = scale_up_to_half(top, &back);
-        c_row = back * a.scale * (a.softcap > 0.f ? 1.f : kLog2e);
-#pragma unroll
-        for (int e = 0; e < D / 2; ++e) w[e] = h2(__uint_as_float(w[e] << 16) * up, __uint_as_float(w[e] & 0xffff0000u) * up);
-#pragma unroll
-        for (int p = 0; p < D / 8; ++p) sts16(q_addr + x * kTileBytes + ck_off(row, p), w[4 * p], w[4 * p + 1], w[4 * p + 2], w[4 * p + 3]);
+        c_row *= a.scale * (a.softcap > 0.f ? 1.f : kLog2e);
       }
       fence_proxy_async_smem();
       warp_arrive(&t.q_full[x]);
@@ -599,115 +696,82 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         continue;
       }
       const float slope2 = a.slopes && row_ok ? a.slopes[head] * kLog2e : 0.f;
-      float m_ref = 0.f, l_run = 0.f;
-      bool alive = true, started = false;          // started: the row has seen a key, and m_ref is its reference
+      CkRow w;
+      w.s_addr = s_addr; w.o_addr = o_addr;
+      w.c_row = c_row; w.cap_in = cap_in; w.cap_out = cap_out; w.slope2 = slope2;
+      w.capped = a.softcap > 0.f; w.biased = a.slopes != nullptr;
+      w.pos = pos;
+      // the reference (-inf until the row has seen a key) and the sum of the row's probabilities
+      float m_ref = -INFINITY, l_run = 0.f;
+      bool alive = true, wide = false;             // wide: the capped scores need the longer polynomial (as the last tile's did)
       for (int tile = 0; tile < it.n_tiles; ++tile, ++T, ++n_mine) {
         alive = __all_sync(0xffffffffu, ck_wait(&t.s_full[x], n_mine & 1, abort_flag, a.status));
         if (!alive) break;
         tc_fence_after();
         const int n_vis = max(0, min(kCkTile, vis - tile * kCkTile));
         const float* k_scale = t.k_scale[T % kCkRing];
-#pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
-          uint32_t sr[32], pk[16];
-          tmem_ld32_issue(s_addr + 32 * c, sr);
-          float f[2] = {c_row * k_scale[2 * c], c_row * k_scale[2 * c + 1]};     // (16 keys each)
-          const int key0 = tile * kCkTile + 32 * c;
-          const bool masked = __any_sync(0xffffffffu, n_vis < 32 * c + 32);
-          tmem_ld_wait();
-          if (!plain || masked) {
-            // scores in place
-            bool done = false;
-            if (a.softcap > 0.f) {
-              const uint64_t g2[2] = {pack_f2(f[0] * cap_in, f[0] * cap_in), pack_f2(f[1] * cap_in, f[1] * cap_in)};
-              float top = 0.f;                     // largest y^2 (a NaN is smaller than anything here and stays one)
-#pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                const uint64_t y = mul_f2(pack_u2(sr[2 * j], sr[2 * j + 1]), g2[j >> 3]);
-                unpack_u2(y, sr[2 * j], sr[2 * j + 1]);
-                float z0, z1;
-                unpack_f2(mul_f2(y, y), z0, z1);
-                top = max3(top, z0, z1);
-              }
-              if (!a.slopes && !masked) {
-                done = __all_sync(0xffffffffu, top <= 1.f);
-                const bool small = __all_sync(0xffffffffu, top <= 0.25f);
-                if (small) tanh_pieces<true>(sr);
-                else if (done) tanh_pieces<false>(sr);
-                f[0] = f[1] = cap_out;
-              }
-            }
-            if (!done) {
-#pragma unroll
-              for (int j = 0; j < 32; ++j) {
-                float y = __uint_as_float(sr[j]);
-                y = a.softcap > 0.f ? cap_out * tanh_f32(y) : y * f[j >> 4];
-                if (a.slopes) y -= slope2 * fabsf((float)(pos - key0 - j));
-                sr[j] = __float_as_uint(32 * c + j < n_vis ? y : -INFINITY);
-              }
-              f[0] = f[1] = 1.f;
-            }
+        // the common way: every key seen, the reference where it is
+        float top = 0.f;
+        const auto piece = [&](auto mode_tag, uint32_t (&sr)[32], int c) {
+          constexpr int kMode = decltype(mode_tag)::value;               // 0: scores as they are, 1 / 2: capped, short / long polynomial
+          float f0 = c_row * k_scale[2 * c], f1 = c_row * k_scale[2 * c + 1];      // (16 keys each)
+          bool bad = false;
+          if (kMode > 0) {
+            const float z = tanh_pieces<kMode == 1>(sr, f0 * cap_in, f1 * cap_in);
+            top = fmaxf(top, z);
+            bad = !(z <= (kMode == 1 ? 0.25f : 1.f));
+            f0 = f1 = cap_out;
           }
-          float sum = 0.f;
-#pragma unroll 1
-          for (int attempt = 0;; ++attempt) {
-            uint64_t sum2[2] = {0ull, 0ull};
-            const uint64_t nm = pack_f2(-m_ref, -m_ref);
+          uint32_t pk[16];
+          uint64_t sum2[2] = {0ull, 0ull};
+          const uint64_t nm = pack_f2(-m_ref, -m_ref);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              float y0, y1;
-              unpack_f2(fma_f2(pack_u2(sr[2 * j], sr[2 * j + 1]), pack_f2(f[j >> 3], f[j >> 3]), nm), y0, y1);
-              const float p0 = exp2_approx(y0), p1 = exp2_approx(y1);
-              sum2[j & 1] = add_f2(sum2[j & 1], pack_f2(p0, p1));
-              pk[j] = h2(p0, p1);
-            }
-            float a0, a1, b0, b1;
-            unpack_f2(sum2[0], a0, a1);
-            unpack_f2(sum2[1], b0, b1);
-            sum = (a0 + a1) + (b0 + b1);
-            const bool move = !(sum < kCkSumLimit) || !started;
-            if (attempt > 0 || !__any_sync(0xffffffffu, move)) break;
-            // the reference of some row moves
-            float alpha = 1.f;
-            if (move) {
-              float mx = -INFINITY;
-#pragma unroll
-              for (int j = 0; j < 32; ++j) mx = fmaxf(mx, __uint_as_float(sr[j]) * f[j >> 4]);
-              if (!started ? mx > -INFINITY : mx > m_ref) {
-                const float m = ceilf(mx);
-                if (started) alpha = exp2_approx(m_ref - m);
-                m_ref = m;
-                started = true;
-              }
-              l_run *= alpha;
-            }
-            const uint32_t alpha2 = h2(alpha, alpha);
-#pragma unroll 1
-            for (int cc = 0; cc < c; ++cc) {       // probabilities of this tile
-              uint32_t old[32];
-              tmem_ld16_issue(s_addr + 16 * cc, old);
-              tmem_ld_wait();
-#pragma unroll
-              for (int j = 0; j < 16; ++j) old[j] = mul_h2(old[j], alpha2);
-              tmem_st16(s_addr + 16 * cc, old);
-            }
-            if (tile > 0) {
-              // O_x is at rest (the product that wrote S_x came after every earlier one)
-#pragma unroll 1
-              for (int cc = 0; cc < D / 16; ++cc) {
-                uint32_t old[32];
-                tmem_ld16_issue(o_addr + 16 * cc, old);
-                tmem_ld_wait();
-#pragma unroll
-                for (int j = 0; j < 16; ++j) old[j] = __float_as_uint(__uint_as_float(old[j]) * alpha);
-                tmem_st16(o_addr + 16 * cc, old);
-              }
-            }
-            tmem_st_wait();
+          for (int j = 0; j < 16; ++j) {
+            const float f = j < 8 ? f0 : f1;
+            float y0, y1;
+            unpack_f2(fma_f2(pack_u2(sr[2 * j], sr[2 * j + 1]), pack_f2(f, f), nm), y0, y1);
+            const float p0 = exp2_approx(y0), p1 = exp2_approx(y1);
+            sum2[j & 1] = add_f2(sum2[j & 1], pack_f2(p0, p1));
+            pk[j] = h2(p0, p1);
           }
+          float a0, a1, b0, b1;
+          unpack_f2(sum2[0], a0, a1);
+          unpack_f2(sum2[1], b0, b1);
+          const float sum = (a0 + a1) + (b0 + b1);
+          bad |= !(sum < kCkSumLimit);
+          if (__any_sync(0xffffffffu, bad)) return false;
           l_run += sum;
           // over scores that have been read: columns 16 c .. of the tile's 128
           tmem_st16_regs(s_addr + 16 * c, pk);
+          return true;
+        };
+        // pieces done the common way; the rest of the tile, from the first one that it does not do for, is done the careful way
+        const auto pieces_of = [&](auto mode_tag) {
+          int c = 0;
+#pragma unroll 1
+          for (; c < 4; ++c) {
+            uint32_t sr[32];
+            tmem_ld32_issue(s_addr + 32 * c, sr);
+            tmem_ld_wait();
+            if (!piece(mode_tag, sr, c)) break;
+          }
+          return c;
+        };
+        int done = 0;
+        if (a.slopes == nullptr && __all_sync(0xffffffffu, n_vis == kCkTile && m_ref > -INFINITY)) {
+          if (!w.capped) {
+            done = pieces_of(std::integral_constant<int, 0>());
+          } else {
+            done = wide ? pieces_of(std::integral_constant<int, 2>()) : pieces_of(std::integral_constant<int, 1>());
+            wide = __any_sync(0xffffffffu, top > 0.25f);
+          }
+        }
+#pragma unroll 1
+        for (int c = done; c < 4; ++c) {
+          const float2 r = careful_piece<D>(w, c, tile * kCkTile + 32 * c, n_vis, tile > 0, c_row * k_scale[2 * c], c_row * k_scale[2 * c + 1],
+                                            m_ref, l_run);
+          m_ref = r.x;
+          l_run = r.y;
         }
         tmem_st_wait();
         tc_fence_before();
