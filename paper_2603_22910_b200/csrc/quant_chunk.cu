@@ -757,8 +757,24 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           }
           return c;
         };
+        const bool full = a.slopes == nullptr && __all_sync(0xffffffffu, n_vis == kCkTile);
+        if (full && tile == 0) {
+          // the first reference: what the first 32 keys ask for (capped scores are at most the uncapped ones, and the cap)
+          uint32_t sr[32];
+          tmem_ld32_issue(s_addr, sr);
+          tmem_ld_wait();
+          float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            mx0 = fmaxf(mx0, __uint_as_float(sr[j]));
+            mx1 = fmaxf(mx1, __uint_as_float(sr[16 + j]));
+          }
+          float mx = fmaxf(mx0 * (c_row * k_scale[0]), mx1 * (c_row * k_scale[1]));
+          if (w.capped) mx = fminf(mx * kLog2e, cap_out);
+          if (mx > -INFINITY) m_ref = ceilf(mx) + kCkMargin;
+        }
         int done = 0;
-        if (a.slopes == nullptr && __all_sync(0xffffffffu, n_vis == kCkTile && m_ref > -INFINITY)) {
+        if (full && __all_sync(0xffffffffu, m_ref > -INFINITY)) {
           if (!w.capped) {
             done = pieces_of(std::integral_constant<int, 0>());
           } else {
