@@ -458,13 +458,13 @@ class StepPlan:
         import torch
         buf = torch.empty(2 * batch + 2 * n_tokens + 2, dtype=torch.int32, device=device)
         self.cu_tokens, self.positions, self.token_seqs, lens, count = buf.split_with_sizes((batch + 1, n_tokens, n_tokens, batch, 1))
-        self.slot_map = torch.empty(n_tokens, dtype=torch.int64, device=device)
+        self.slot_map = buf.new_empty(n_tokens, dtype=torch.int64)
         self.seq_lens = lens if seq_lens is None else seq_lens
         self.free_count = count if free_count is None else free_count
         cu = buf.data_ptr()
         self._c = echokv_step_plan(cu, cu + 4 * (batch + 1), cu + 4 * (batch + 1 + n_tokens), self.slot_map.data_ptr(),
-                                   _dense(self.seq_lens, torch.int32, batch, "seq_lens"),
-                                   _dense(self.free_count, torch.int32, 1, "free_count"))
+                                   lens.data_ptr() if seq_lens is None else _dense(seq_lens, torch.int32, batch, "seq_lens"),
+                                   count.data_ptr() if free_count is None else _dense(free_count, torch.int32, 1, "free_count"))
         self._batch, self._tokens = batch, n_tokens
 
 
@@ -517,14 +517,14 @@ def rotate(cfg: echokv_config, q, k, positions, theta: float, sections=None, rot
     if q is not None:
         qp, qs = _rows(q, T, n_q, d, dt, "q")
         if q_out is None:
-            q_out = torch.empty((T, n_q, d), dtype=dt, device=q.device)
+            q_out = q.new_empty((T, n_q, d))
             qo, qos = q_out.data_ptr(), n_q * d
         else:
             qo, qos = _rows(q_out, T, n_q, d, dt, "q_out")
     if k is not None:
         kp, ks = _rows(k, T, n_kv, d, dt, "k")
         if k_out is None:
-            k_out = torch.empty((T, n_kv, d), dtype=dt, device=k.device)
+            k_out = k.new_empty((T, n_kv, d))
             ko, kos = k_out.data_ptr(), n_kv * d
         else:
             ko, kos = _rows(k_out, T, n_kv, d, dt, "k_out")
@@ -558,6 +558,7 @@ class QuantCache:
             raise ValueError("format %r is not one of %s" % (fmt, sorted(QUANT_FORMATS)))
         self.cfg, self.fmt, self.tdtype = cfg, fmt, _dtype(cfg)
         self.sizes = sizes = query_quant_sizes(cfg)
+        self._ws_bytes = sizes.workspace_bytes
         dev = torch.device("cuda", cfg.device)
         H, P, d, N = cfg.n_kv_heads, cfg.page_tokens, cfg.head_dim, cfg.n_pages
         code = torch.int8 if fmt == "int8" else torch.float8_e4m3fn
@@ -600,7 +601,7 @@ class QuantCache:
         cfg, T, B = self.cfg, q.shape[0], seq_lens.shape[0]
         qp, qs = _rows(q, T, cfg.n_q_heads, cfg.head_dim, self.tdtype, "q")
         if out is None:
-            out = torch.empty((T, cfg.n_q_heads, cfg.head_dim), dtype=self.tdtype, device=q.device)
+            out = q.new_empty((T, cfg.n_q_heads, cfg.head_dim))
             op = out.data_ptr()
         else:
             op = _dense(out, self.tdtype, T * cfg.n_q_heads * cfg.head_dim, "out")
@@ -612,8 +613,8 @@ class QuantCache:
                                             _dense(block_table, torch.int32, cfg.max_batch * cfg.max_pages_per_seq, "block_table"),
                                             _dense(seq_slots, torch.int32, B, "seq_slots"), _dense(seq_lens, torch.int32, B, "seq_lens"),
                                             _dense(cu_tokens, torch.int32, B + 1, "cu_tokens"), B, T, max_new,
-                                            _dense(self.workspace, torch.uint8, self.sizes.workspace_bytes, "workspace"),
-                                            self.sizes.workspace_bytes, _dense(status, torch.int32, 1, "status"),
+                                            _dense(self.workspace, torch.uint8, self._ws_bytes, "workspace"),
+                                            self._ws_bytes, _dense(status, torch.int32, 1, "status"),
                                             _stream_on(cfg.device, stream)), "echokv_quant_attention")
         return out
 

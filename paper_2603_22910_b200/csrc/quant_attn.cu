@@ -302,7 +302,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     const int n_blk = (len + kQuantBlock - 1) / kQuantBlock, tiles = row_tiles(a, n_new);
     const unsigned long long rem = u - base;
     const int ht = (int)quotient(rem, n_blk + kQaItemCost), at0 = (int)(rem - (unsigned long long)ht * (n_blk + kQaItemCost));
-    const int h = ht / tiles, tile = ht - h * tiles;
+    const int h = tiles == 1 ? ht : ht / tiles, tile = ht - h * tiles;
     const unsigned long long item = u - at0, item_end = item + n_blk + kQaItemCost;
     const unsigned long long seg_end = min(item_end, u_end);
     // blocks [blk0, blk0 + nb) of the item

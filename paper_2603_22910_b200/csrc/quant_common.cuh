@@ -14,26 +14,23 @@ struct QuantSeq {
 };
 
 __device__ __forceinline__ QuantSeq quant_seq(const QuantAttnArgs& a, int b) {
+  // (everything that is read is asked for at once)
+  const int c0 = a.cu ? a.cu[b] : b, c1 = a.cu ? a.cu[b + 1] : b + 1, slot = a.slots ? a.slots[b] : b, len = a.lens[b];
   QuantSeq s;
-  s.first = b;
-  s.n = 1;
+  s.slot = slot;
+  s.len = len;
   s.error = 0;
-  if (a.cu != nullptr) {
-    const int c0 = a.cu[b], c1 = a.cu[b + 1];
-    if (c0 < 0 || c1 < c0 || c1 > a.n_tokens) {
-      s.error = ECHOKV_EBADLENGTH;
-      s.first = 0;
-      s.n = 0;
-    } else {
-      s.first = c0;
-      s.n = c1 - c0;
-    }
+  if (c0 < 0 || c1 < c0 || c1 > a.n_tokens) {
+    s.error = ECHOKV_EBADLENGTH;
+    s.first = 0;
+    s.n = 0;
+    return s;
   }
-  s.slot = a.slots ? a.slots[b] : b;
-  s.len = a.lens[b];
+  s.first = c0;
+  s.n = c1 - c0;
   if (s.n > 0) {
-    if (s.slot < 0 || s.slot >= a.g.max_batch) s.error = ECHOKV_EBADPAGE;
-    else if (s.len < s.n || s.len > a.g.max_pages * a.g.page_tokens || s.n > a.max_new) s.error = ECHOKV_EBADLENGTH;
+    if (slot < 0 || slot >= a.g.max_batch) s.error = ECHOKV_EBADPAGE;
+    else if (len < s.n || len > a.g.max_pages * a.g.page_tokens || s.n > a.max_new) s.error = ECHOKV_EBADLENGTH;
   }
   return s;
 }
