@@ -164,22 +164,32 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanArgs a) {
     if (page < 0 || page >= a.n_pages) report_opt(a.status, ECHOKV_EBADPAGE);
     a.table[(long long)slot_s[b] * a.max_pages + old_s[b] + k - page0[b]] = page;
   }
-  // tokens
-  for (int t = first; t < a.n_tokens; t += stride) {
-    int b = -1, pos = -1;
-    long long row = -1;
-    if (t < n_live) {
-      b = find_last(cu, B, t);
-      pos = len_s[b] + t - cu[b];
-      const int pi = pos >> a.page_shift;
-      const int page = pi < old_s[b] ? a.table[(long long)slot_s[b] * a.max_pages + pi]
-                                     : a.free_pages[count - 1 - (page0[b] + pi - old_s[b])];
-      if (page >= 0 && page < a.n_pages) row = (long long)page * a.page_tokens + (pos & (a.page_tokens - 1));
-      else report_opt(a.status, ECHOKV_EBADPAGE);
+  // tokens, four of a thread's at a time so that their page look-ups overlap
+  constexpr int kBatch = 4;
+  for (int t0 = first; t0 < a.n_tokens; t0 += kBatch * stride) {
+    int seq[kBatch], pos[kBatch], page[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int t = t0 + i * stride;
+      seq[i] = pos[i] = page[i] = -1;
+      if (t < n_live) {
+        const int b = find_last(cu, B, t);
+        seq[i] = b;
+        pos[i] = len_s[b] + t - cu[b];
+        const int pi = pos[i] >> a.page_shift;
+        page[i] = pi < old_s[b] ? a.table[(long long)slot_s[b] * a.max_pages + pi] : a.free_pages[count - 1 - (page0[b] + pi - old_s[b])];
+      }
     }
-    a.out.positions[t] = pos;
-    a.out.token_seqs[t] = b;
-    a.out.slot_map[t] = row;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int t = t0 + i * stride;
+      if (t >= a.n_tokens) break;
+      const bool ok = page[i] >= 0 && page[i] < a.n_pages;
+      if (seq[i] >= 0 && !ok) report_opt(a.status, ECHOKV_EBADPAGE);
+      a.out.positions[t] = pos[i];
+      a.out.token_seqs[t] = seq[i];
+      a.out.slot_map[t] = seq[i] >= 0 && ok ? (long long)page[i] * a.page_tokens + (pos[i] & (a.page_tokens - 1)) : -1;
+    }
   }
 }
 
