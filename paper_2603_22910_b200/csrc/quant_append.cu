@@ -60,21 +60,17 @@ __device__ __forceinline__ uint32_t e4m3_pair(float lo, float hi) {
   return r;
 }
 
+// (No clamp: with inv the rounded inverse of a rounded amax / Q, |v| inv <= Q (1 + 2^-21), which rounds to Q.)
 template <int FMT, int N>
 __device__ __forceinline__ uint32_t encode(const float (&v)[N], float inv) {
+  float y[N];
+#pragma unroll
+  for (int e = 0; e < N; e += 2) unpack_f2(mul_f2(pack_f2(v[e], v[e + 1]), pack_f2(inv, inv)), y[e], y[e + 1]);
   uint32_t w = 0;
-  if (FMT == ECHOKV_INT8) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const int c = max(-127, min(127, __float2int_rn(v[e] * inv)));
-      w |= (uint32_t)(c & 0xff) << (8 * e);
-    }
-  } else {
-    float y[N];
-#pragma unroll
-    for (int e = 0; e < N; ++e) y[e] = v[e] * inv;
-#pragma unroll
-    for (int e = 0; e < N; e += 2) w |= e4m3_pair(y[e], y[e + 1]) << (8 * e);
+  for (int e = 0; e < N; e += 2) {
+    if (FMT == ECHOKV_INT8) w |= (__byte_perm((uint32_t)__float2int_rn(y[e]), (uint32_t)__float2int_rn(y[e + 1]), 0x0040) & 0xffffu) << (8 * e);
+    else w |= e4m3_pair(y[e], y[e + 1]) << (8 * e);
   }
   return w;
 }
