@@ -37,6 +37,34 @@ constexpr float kCkMargin = 8.f;                   // a reference that moves goe
                                                    // before it moves again, and fp16 still holds the largest probability's 2^-17
 constexpr float kCkSumLimit = 32768.f;             // a row's 32 probabilities sum to less: each fits fp16
 constexpr float kCkVScale = 64.f;
+constexpr int kCkMaxCtas = 160;                    // (of the workspace's layout)
+#ifndef CKCOST
+#define CKCOST 2
+#endif
+#ifndef CKMIN
+#define CKMIN 6
+#endif
+constexpr int kCkItemCost = CKCOST;                     // what an item costs beside its tiles (queries, first tile, result), in tiles
+constexpr int kCkMinShare = CKMIN;                     // units per CTA at least
+constexpr int kCkMergeCols = 16;                   // features per thread of the merge
+
+struct CkDesc {                                    // an item cut at the end of CTA g's share
+  int n_parts;                                     // CTAs that hold parts of it (0: none starts here)
+  int first, n_rows, h, row0;
+  int pad[3];
+};
+// workspace: [ctas] CkDesc | [ctas][2][256] (m, l) | [ctas][2][D / 4][256] four features of o / l
+template <int D>
+struct CkWork {
+  CkDesc* desc;
+  float2* ml;
+  float4* o;
+  __host__ __device__ explicit CkWork(unsigned char* ws) {
+    desc = reinterpret_cast<CkDesc*>(ws);
+    ml = reinterpret_cast<float2*>(ws + kCkMaxCtas * sizeof(CkDesc));
+    o = reinterpret_cast<float4*>(ws + kCkMaxCtas * (sizeof(CkDesc) + 2 * kCkRows * sizeof(float2)));
+  }
+};
 
 struct CkTail {
   unsigned long long q_full[2], s_full[2], p_ready[2], o_done[2];
@@ -271,17 +299,55 @@ __device__ __noinline__ float2 careful_piece(const CkRow w, const int c, const i
 
 struct CkItem {
   int b, h, row0;                                  // rows [row0, row0 + 256) of (sequence b, KV head h)
-  int slot, len, first, n, n_rows, act;            // act: tiles that hold a row
+  int slot, len, first, n, n_rows, act;            // act: tiles of rows that hold a row
   int prefix, kv_end, n_tiles;
+  int t0, t1;                                      // tiles of keys that are this CTA's (none: t1 <= t0)
+  unsigned long long end;                          // unit behind the item
 };
 
-// chunk sequences only; w = 0 otherwise
-__device__ __forceinline__ int4 ck_seq(const QuantAttnArgs& a, int b) {
+// The row blocks of a sequence: block j holds tokens [j per, (j + 1) per) times the group and sees kv_end(j) keys.  Everything is a
+// power of two but the lengths, so that the tiles of the first j blocks have a closed form.
+struct CkSeq {
+  int slot, len, first, n;                         // (n = 0: not a sequence of this kernel)
+  int prefix, blocks, per_shift;                   // 2^per_shift tokens per block
+  __device__ __forceinline__ int kv_end(int j) const {
+    const long long last = min((long long)n, (long long)(j + 1) << per_shift);
+    return (int)max((long long)(len - n) + last, (long long)prefix);
+  }
+  // sum over i < m of floor(i / 2^shift)
+  __device__ __forceinline__ static unsigned long long floors(unsigned long long m, int shift) {
+    const unsigned long long q = m >> shift, r = m & ((1ull << shift) - 1);
+    return (q == 0 ? 0ull : (q * (q - 1) / 2) << shift) + q * r;
+  }
+  // tiles of blocks [0, j): those that see no more than the prefix, those with all their tokens, the last
+  __device__ __forceinline__ unsigned long long tiles(int j) const {
+    const int full = min(j, blocks - 1), base = len - n;
+    const int flat = prefix > base ? min(full, (prefix - base) >> per_shift) : 0;
+    unsigned long long t = (unsigned long long)flat * ((prefix + kCkTile - 1) / kCkTile);
+    // floor((base + 127 + i per) / 128) for i in (flat, full]
+    if (per_shift <= 7) {
+      const unsigned long long at = (unsigned long long)(base + kCkTile - 1) >> per_shift;
+      t += floors(at + full + 1, 7 - per_shift) - floors(at + flat + 1, 7 - per_shift);
+    } else {
+      t += (unsigned long long)(full - flat) * ((base + kCkTile - 1) / kCkTile) +
+           ((unsigned long long)full * (full + 1) - (unsigned long long)flat * (flat + 1));
+    }
+    return j == blocks ? t + (len + kCkTile - 1) / kCkTile : t;
+  }
+  __device__ __forceinline__ unsigned long long units(int j) const { return tiles(j) + (unsigned long long)j * kCkItemCost; }
+};
+__device__ __forceinline__ CkSeq ck_seq(const QuantAttnArgs& a, int b) {
   const QuantSeq s = quant_seq(a, b);
-  return make_int4(s.slot, s.len, s.first, many_rows(a, s) ? s.n : 0);
+  CkSeq c;
+  c.slot = s.slot; c.len = s.len; c.first = s.first;
+  c.n = many_rows(a, s) ? s.n : 0;
+  c.prefix = a.prefix && c.n > 0 ? min(a.prefix[b], s.len) : 0;
+  c.blocks = (int)(((long long)c.n * a.group + kCkRows - 1) / kCkRows);
+  c.per_shift = 8 - a.group_shift;
+  return c;
 }
-__device__ __forceinline__ unsigned long long ck_items(const QuantAttnArgs& a, const int4& s) {
-  return (unsigned long long)(((long long)s.w * a.group + kCkRows - 1) / kCkRows) * a.g.n_kv_heads;
+__device__ __forceinline__ unsigned long long ck_units(const QuantAttnArgs& a, const CkSeq& s) {
+  return s.n > 0 ? s.units(s.blocks) * a.g.n_kv_heads : 0;
 }
 
 template <int FMT, int D>
@@ -300,7 +366,11 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
   const int H = g.n_kv_heads;
   volatile int* abort_flag = &t.abort_flag;
 
-  if (!take_chunks(a, a.sm_count)) return;         // (the same answer in every thread)
+  const CkWork<D> ws(a.ws);
+  if (!take_chunks(a, a.sm_count)) {               // (the same answer in every thread)
+    if (tid == 0) ws.desc[blockIdx.x].n_parts = 0;
+    return;
+  }
 
   // ---- barriers, tensor memory, and the items of the call
   const int per = (a.B + kCkThreads - 1) / kCkThreads;
@@ -322,7 +392,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
   {
     unsigned long long n = 0;
 #pragma unroll 1
-    for (int b = tid * per; b < min(a.B, (tid + 1) * per); ++b) n += ck_items(a, ck_seq(a, b));
+    for (int b = tid * per; b < min(a.B, (tid + 1) * per); ++b) n += ck_units(a, ck_seq(a, b));
     unsigned long long x = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -346,32 +416,63 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
   const uint32_t tmem = t.tmem_base;
   const unsigned long long total = t.pre[kCkThreads];
 
-  const auto get_item = [&](unsigned long long index) {
+  // this CTA's share of the units
+  const int ctas = (int)min((unsigned long long)gridDim.x, total / kCkMinShare + 1);
+  const unsigned long long u0 = (int)blockIdx.x < ctas ? total * blockIdx.x / ctas : total;
+  const unsigned long long u1 = (int)blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : total;
+
+  // the item that unit u is of, and the tiles of it from there to the share's end
+  const auto get_item = [&](unsigned long long u) {
     int lo = 0, hi = kCkThreads;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (t.pre[mid] <= index) lo = mid; else hi = mid;
+      if (t.pre[mid] <= u) lo = mid; else hi = mid;
     }
     CkItem it;
     it.b = lo * per;
     unsigned long long base = t.pre[lo];
-    int4 s = ck_seq(a, it.b);
-    while (base + ck_items(a, s) <= index) {
-      base += ck_items(a, s);
+    CkSeq s = ck_seq(a, it.b);
+    for (unsigned long long n = ck_units(a, s); base + n <= u; n = ck_units(a, s)) {
+      base += n;
       s = ck_seq(a, ++it.b);
     }
-    it.slot = s.x; it.len = s.y; it.first = s.z; it.n = s.w;
+    it.slot = s.slot; it.len = s.len; it.first = s.first; it.n = s.n;
     it.n_rows = it.n * a.group;
-    const int rem = (int)(index - base), blocks = (it.n_rows + kCkRows - 1) / kCkRows;
-    it.h = rem % H;
-    it.row0 = (blocks - 1 - rem / H) * kCkRows;                // (the rows that see the most keys first)
+    const unsigned long long rem = u - base;
+    int j = 0, j_hi = s.blocks;                    // the row block: the last one whose units begin at or before u
+    while (j_hi - j > 1) {
+      const int mid = (j + j_hi) >> 1;
+      if (s.units(mid) * H <= rem) j = mid; else j_hi = mid;
+    }
+    it.row0 = j * kCkRows;
     it.act = it.n_rows - it.row0 > kCkTile ? 2 : 1;
-    it.prefix = a.prefix ? min(a.prefix[it.b], it.len) : 0;
-    const int last_row = min(it.n_rows, it.row0 + kCkRows) - 1;
-    it.kv_end = max(it.len - it.n + (last_row >> a.group_shift) + 1, it.prefix);
+    it.prefix = s.prefix;
+    it.kv_end = s.kv_end(j);
     it.n_tiles = (it.kv_end + kCkTile - 1) / kCkTile;
+    const unsigned long long in_block = rem - s.units(j) * H, n = it.n_tiles + kCkItemCost;
+    it.h = (int)(in_block / n);
+    const unsigned long long start = u - (in_block - it.h * n);
+    it.end = start + n;
+    it.t0 = max(0, (int)(u - start) - kCkItemCost);
+    it.t1 = (int)(min(u1, it.end) - start) - kCkItemCost;
     return it;
   };
+
+  if (tid == 0) {
+    // an item that begins in this share and goes on behind it
+    CkDesc d = {};
+    if (u1 > u0 && u1 < total) {
+      const CkItem it = get_item(u1 - 1);
+      const unsigned long long start = it.end - it.n_tiles - kCkItemCost;
+      const int done = (int)(u1 - start) - kCkItemCost;        // its tiles up to the share's end
+      const bool begins = start + kCkItemCost >= u0;
+      if (begins && done > 0 && done < it.n_tiles) {
+        d.n_parts = (int)((it.end * ctas - 1) / total) - (int)blockIdx.x + 1;
+        d.first = it.first; d.n_rows = it.n_rows; d.h = it.h; d.row0 = it.row0;
+      }
+    }
+    ws.desc[blockIdx.x] = d;
+  }
 
   if (warp == kCkThreads / 32 - 1) {
     // =============================== products ===================================================
@@ -383,8 +484,10 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       unpack_u2(ck_desc(q_addr, 16), q_lo0, kmajor_hi);
       unpack_u2(ck_desc(k_addr, 16), k_lo0, kmajor_hi);
       unpack_u2(ck_desc(v_addr, kCkChunkBytes), v_lo0, v_hi);
-      for (unsigned long long i = blockIdx.x; i < total && alive; i += gridDim.x, ++n_item) {
-        const CkItem it = get_item(i);
+      for (unsigned long long u = u0; u < u1 && alive;) {
+        const CkItem it = get_item(u);
+        u = it.end;
+        if (it.t1 <= it.t0) continue;
         const auto issue_s = [&](int x, uint32_t tile) {
           const uint32_t q_lo = q_lo0 + x * (kTileBytes >> 4), k_lo = k_lo0 + (tile & 1) * (kTileBytes >> 4);
 #pragma unroll
@@ -402,7 +505,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         if (!alive) break;
         tc_fence_after();
         for (int x = 0; x < it.act; ++x) issue_s(x, T);
-        for (int tile = 0; tile < it.n_tiles && alive; ++tile, ++T) {
+        for (int tile = it.t0; tile < it.t1 && alive; ++tile, ++T) {
           if (!ck_wait_warp(&t.v_full[T & 1], (T >> 1) & 1, abort_flag, a.status)) { alive = false; break; }
           const uint32_t v_lo = v_lo0 + (T & 1) * (kTileBytes >> 4);
           for (int x = 0; x < it.act && alive; ++x) {
@@ -412,10 +515,10 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
 #pragma unroll
             for (int kk = 0; kk < 8; ++kk)         // 16 keys: 8 columns of packed probabilities, 2048 bytes of value rows
               ck_mma_ts(tmem + 256 + x * D, tmem + x * 128 + 8 * kk, pack_u2(v_lo + 128 * kk, v_hi), ck_idesc_pv<D>(),
-                                 (tile > 0 || kk > 0) ? 1u : 0u);
-            if (tile + 1 == it.n_tiles) ck_commit(&t.o_done[x]);
+                                 (tile > it.t0 || kk > 0) ? 1u : 0u);
+            if (tile + 1 == it.t1) ck_commit(&t.o_done[x]);
             if (x == it.act - 1) ck_commit(&t.v_empty[T & 1]);
-            if (tile + 1 < it.n_tiles) {
+            if (tile + 1 < it.t1) {
               if (x == 0) {
                 if (!ck_wait_warp(&t.k_full[(T + 1) & 1], ((T + 1) >> 1) & 1, abort_flag, a.status)) { alive = false; break; }
                 tc_fence_after();
@@ -426,6 +529,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         }
         // (an idle second half waits for this too: its warps must not run items ahead of the barriers' phases)
         if (alive && it.act == 1) ck_commit(&t.o_done[1]);
+        ++n_item;
       }
       if (!alive) {
         // every product issued so far retires before the tensor memory is given back
@@ -461,12 +565,15 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       sts16(dst + (at0 ^ turn) + p * kRowStep * 128, w[0], w[1], w[2], w[3]);
       sts16(dst + (at1 ^ turn) + p * kRowStep * 128, w[4], w[5], w[6], w[7]);
     };
-    for (unsigned long long i = blockIdx.x; i < total; i += gridDim.x, ++n_item) {
+    for (unsigned long long u = u0; u < u1;) {
+      const CkItem it = get_item(u);
+      u = it.end;
+      if (it.t1 <= it.t0) continue;
       if (!conv_all(alive)) break;                 // (a wait that ran out: all leave together)
-      const CkItem it = get_item(i);
       const int32_t* pages = a.table + (long long)it.slot * g.max_pages;
       const int n_full = it.len / kQuantBlock, n_codes = min(n_full, (it.kv_end + kQuantBlock - 1) / kQuantBlock);   // blocks of codes seen
-      const bool open = it.kv_end > n_full * kQuantBlock;      // the open block is seen
+      // the open block is seen, and in one of these tiles
+      const bool open = it.kv_end > n_full * kQuantBlock && n_full / 8 >= it.t0 && n_full / 8 < it.t1;
       const long long open_at = ((long long)it.slot * H + it.h) * kQuantBlock * D;
       const auto page_of = [&](int tok) {          // page of a token that exists
         int id = pages[tok >> g.page_shift];
@@ -479,9 +586,9 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       const auto scale_at = [&](int blk, int page) {
         return ((long long)page * H + it.h) * (g.page_tokens / kQuantBlock) + ((blk * kQuantBlock & (g.page_tokens - 1)) / kQuantBlock);
       };
-      // the largest V scale that the item sees, and the largest magnitudes of its open block
+      // the largest V scale in these tiles, and the largest magnitudes of the open block
       float v_top = 0.f;
-      for (int blk = ct; blk < n_codes; blk += kCkConvThreads) v_top = fmaxf(v_top, g.scales[1][scale_at(blk, page_of(blk * kQuantBlock))]);
+      for (int blk = 8 * it.t0 + ct; blk < min(n_codes, 8 * it.t1); blk += kCkConvThreads) v_top = fmaxf(v_top, g.scales[1][scale_at(blk, page_of(blk * kQuantBlock))]);
       uint32_t open_k = 0, open_v = 0;
       if (open) {
         const int n_open = it.len - n_full * kQuantBlock;
@@ -573,10 +680,10 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           for (int e = 0; e < 4; ++e) w[4 * q + e] = h2(__uint_as_float(y[e] << 16) * up, __uint_as_float(y[e] & 0xffff0000u) * up);
         }
       };
-      int page8 = checked(ask_page(0)), page8_next = ask_page(1);
-      load_scales(0, page8);
-      fetch(0, page8);
-      for (int tile = 0; tile < it.n_tiles; ++tile, ++T) {
+      int page8 = checked(ask_page(it.t0)), page8_next = ask_page(it.t0 + 1);
+      load_scales(it.t0, page8);
+      fetch(it.t0, page8);
+      for (int tile = it.t0; tile < it.t1; ++tile, ++T) {
         const int st = T & 1;
         const uint32_t parity = ((T >> 1) & 1) ^ 1;
         alive = __all_sync(0xffffffffu, ck_wait(&t.k_empty[st], parity, abort_flag, a.status));
@@ -636,13 +743,14 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         }
         fence_proxy_async_smem();
         warp_arrive(&t.v_full[st]);
-        if (tile + 1 < it.n_tiles) {
+        if (tile + 1 < it.t1) {
           page8 = checked(page8_next);
           page8_next = ask_page(tile + 2);
           load_scales(tile + 1, page8);
           fetch(tile + 1, page8);
         }
       }
+      ++n_item;
     }
   } else {
     // =============================== softmax ====================================================
@@ -651,8 +759,10 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
     const uint32_t s_addr = lane_base + x * 128, o_addr = lane_base + 256 + x * D;
     const float cap_in = a.softcap > 0.f ? 1.f / a.softcap : 0.f, cap_out = a.softcap * kLog2e;
     uint32_t T = 0, n_item = 0, n_mine = 0, n_done = 0;   // (of this half: tiles and results, whose barriers move with them)
-    for (unsigned long long i = blockIdx.x; i < total; i += gridDim.x, ++n_item) {
-      const CkItem it = get_item(i);
+    for (unsigned long long u = u0; u < u1;) {
+      const CkItem it = get_item(u);
+      u = it.end;
+      if (it.t1 <= it.t0) continue;
       const int r = it.row0 + x * kCkTile + row;
       const bool row_ok = r < it.n_rows;
       const int qi = row_ok ? r >> a.group_shift : 0, head = it.h * a.group + (r & (a.group - 1));
@@ -690,9 +800,10 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       fence_proxy_async_smem();
       warp_arrive(&t.q_full[x]);
       if (x >= it.act) {
-        T += it.n_tiles;
+        T += it.t1 - it.t0;
         if (!__all_sync(0xffffffffu, ck_wait(&t.o_done[x], n_done & 1, abort_flag, a.status))) break;
         ++n_done;
+        ++n_item;
         continue;
       }
       const float slope2 = a.slopes && row_ok ? a.slopes[head] * kLog2e : 0.f;
@@ -704,7 +815,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       // the reference (-inf until the row has seen a key) and the sum of the row's probabilities
       float m_ref = -INFINITY, l_run = 0.f;
       bool alive = true, wide = false;             // wide: the capped scores need the longer polynomial (as the last tile's did)
-      for (int tile = 0; tile < it.n_tiles; ++tile, ++T, ++n_mine) {
+      for (int tile = it.t0; tile < it.t1; ++tile, ++T, ++n_mine) {
         alive = __all_sync(0xffffffffu, ck_wait(&t.s_full[x], n_mine & 1, abort_flag, a.status));
         if (!alive) break;
         tc_fence_after();
@@ -758,7 +869,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           return c;
         };
         const bool full = a.slopes == nullptr && __all_sync(0xffffffffu, n_vis == kCkTile);
-        if (full && tile == 0) {
+        if (full && tile == it.t0) {
           // the first reference: what the first 32 keys ask for (capped scores are at most the uncapped ones, and the cap)
           uint32_t sr[32];
           tmem_ld32_issue(s_addr, sr);
@@ -784,7 +895,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         }
 #pragma unroll 1
         for (int c = done; c < 4; ++c) {
-          const float2 r = careful_piece<D>(w, c, tile * kCkTile + 32 * c, n_vis, tile > 0, c_row * k_scale[2 * c], c_row * k_scale[2 * c + 1],
+          const float2 r = careful_piece<D>(w, c, tile * kCkTile + 32 * c, n_vis, tile > it.t0, c_row * k_scale[2 * c], c_row * k_scale[2 * c + 1],
                                             m_ref, l_run);
           m_ref = r.x;
           l_run = r.y;
@@ -800,22 +911,31 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       ++n_done;
       tc_fence_after();
       const float inv = l_run == 0.f ? 0.f : t.v_ref[n_item % kCkRing] / l_run;
+      const bool whole = it.t1 - it.t0 == it.n_tiles;
+      // (a part: o / l beside the reference and l, in the slot of an item that goes on from the CTA before or in the next)
+      const long long slot = (long long)blockIdx.x * 2 + (it.t0 == 0);
+      if (!whole) ws.ml[slot * kCkRows + x * kCkTile + row] = make_float2(m_ref, l_run);
+      float4* part = ws.o + slot * (D / 4) * kCkRows + x * kCkTile + row;
       __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.out) + ((long long)(it.first + qi) * a.n_q_heads + head) * D;
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
         uint32_t orow[32];
         tmem_ld32_issue(o_addr + 32 * c, orow);
         tmem_ld_wait();
-        if (row_ok) {
 #pragma unroll
-          for (int j = 0; j < 32; j += 8) {
-            float v[8];
+        for (int j = 0; j < 32; j += 8) {
+          float v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(orow[j + e]) * inv;
+          for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(orow[j + e]) * inv;
+          if (!whole) {
+            part[(8 * c + j / 4) * kCkRows] = make_float4(v[0], v[1], v[2], v[3]);
+            part[(8 * c + j / 4 + 1) * kCkRows] = make_float4(v[4], v[5], v[6], v[7]);
+          } else if (row_ok) {
             store16<__nv_bfloat16>(dst + 32 * c + j, v);
           }
         }
       }
+      ++n_item;
       tc_fence_before();
     }
   }
@@ -827,18 +947,73 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
   }
 }
 
+// The items that were cut: a thread per row and 16 features, parts joined in the order of their keys.
+template <int D>
+__global__ void __launch_bounds__(kCkRows) quant_chunk_merge_kernel(const __grid_constant__ QuantAttnArgs a) {
+  const CkWork<D> ws(a.ws);
+  const int row = threadIdx.x, col = blockIdx.y * kCkMergeCols;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const CkDesc d = ws.desc[blockIdx.x];
+  const int r = d.row0 + row;
+  if (d.n_parts == 0 || r >= d.n_rows) return;
+  const auto slot = [&](int p) -> long long { return (long long)(blockIdx.x + p) * 2 + (p == 0); };
+  float m = -INFINITY;
+  for (int p = 0; p < d.n_parts; ++p) m = fmaxf(m, ws.ml[slot(p) * kCkRows + row].x);
+  float l = 0.f, acc[kCkMergeCols] = {};
+#pragma unroll 2
+  for (int p = 0; p < d.n_parts; ++p) {
+    const float2 ml = ws.ml[slot(p) * kCkRows + row];
+    const float w = ml.y == 0.f ? 0.f : exp2_approx(ml.x - m) * ml.y;
+    l += w;
+    const float4* o = ws.o + (slot(p) * (D / 4) + col / 4) * kCkRows + row;
+#pragma unroll
+    for (int e = 0; e < kCkMergeCols / 4; ++e) {
+      const float4 v = o[e * kCkRows];
+      acc[4 * e] += w * v.x; acc[4 * e + 1] += w * v.y; acc[4 * e + 2] += w * v.z; acc[4 * e + 3] += w * v.w;
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int e = 0; e < kCkMergeCols; ++e) acc[e] *= inv;
+  __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.out) +
+                       ((long long)(d.first + (r >> a.group_shift)) * a.n_q_heads + d.h * a.group + (r & (a.group - 1))) * D + col;
+#pragma unroll
+  for (int e = 0; e < kCkMergeCols; e += 8) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = acc[e + i];
+    store16<__nv_bfloat16>(dst + e, v);
+  }
+}
+
 template <int FMT, int D>
 cudaError_t launch(const QuantAttnArgs& a, int sm_count, cudaStream_t stream) {
   constexpr size_t smem = ck_smem_bytes<D>();
   static_assert(smem <= 227 * 1024, "shared memory of one CTA");
   static std::atomic<unsigned long long> done{0};
-  const cudaError_t e = allow_smem(quant_chunk_kernel<FMT, D>, smem, &done);
+  cudaError_t e = allow_smem(quant_chunk_kernel<FMT, D>, smem, &done);
   if (e != cudaSuccess) return e;
-  quant_chunk_kernel<FMT, D><<<sm_count, kCkThreads, smem, stream>>>(a);
-  return cudaGetLastError();
+  const int grid = sm_count < kCkMaxCtas ? sm_count : kCkMaxCtas;
+  quant_chunk_kernel<FMT, D><<<grid, kCkThreads, smem, stream>>>(a);
+  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid, D / kCkMergeCols);
+  cfg.blockDim = dim3(kCkRows);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, quant_chunk_merge_kernel<D>, a);
 }
 
 }  // namespace
+
+uint64_t quant_chunk_workspace_bytes(int head_dim) {
+  const uint64_t n = (uint64_t)kCkMaxCtas * (sizeof(CkDesc) + 2ull * kCkRows * (sizeof(float2) + (uint64_t)head_dim * sizeof(float)));
+  return (n + 255) / 256 * 256;
+}
 
 cudaError_t launch_quant_chunk(const QuantAttnArgs& a, int sm_count, cudaStream_t stream) {
   const bool i8 = a.format == ECHOKV_INT8;

@@ -42,7 +42,7 @@ __device__ __forceinline__ QuantSeq quant_seq(const QuantAttnArgs& a, int b) {
 // kernel's time is that of the longest item, or of all of them over the SMs where they are many.  (One sequence over 8192 keys:
 // 64 tokens 89 us by rows, 185 by chunks, 256 tokens the other way round; 8 sequences: 16 tokens 166 and 165 us, 64 tokens 613
 // and 201.)  Both kernels compute the answer from the lengths, every thread of a block the same one.
-constexpr unsigned long long kChunkUnits = 576;
+constexpr unsigned long long kChunkUnits = 500;
 __device__ __forceinline__ bool many_rows(const QuantAttnArgs& a, const QuantSeq& s) {
   return a.chunk_rows > 0 && !s.error && (long long)s.n * a.group >= a.chunk_rows;
 }

@@ -132,6 +132,7 @@ struct QuantAttnArgs {
 uint64_t quant_attn_workspace_bytes(int head_dim);
 cudaError_t launch_quant_attn(const QuantAttnArgs& a, int sm_count, cudaStream_t stream);
 // the sequences with chunk_rows query rows and more (bf16)
+uint64_t quant_chunk_workspace_bytes(int head_dim);
 cudaError_t launch_quant_chunk(const QuantAttnArgs& a, int sm_count, cudaStream_t stream);
 
 }  // namespace echokv

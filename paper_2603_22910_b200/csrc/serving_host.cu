@@ -87,6 +87,12 @@ int check_all(const echokv_config* c) {
   return rc;
 }
 
+// (the two attention kernels of a call use it one after the other)
+uint64_t quant_workspace(const echokv_config* c) {
+  const uint64_t rows = quant_attn_workspace_bytes(c->head_dim), chunks = quant_chunk_workspace_bytes(c->head_dim);
+  return c->dtype == ECHOKV_BF16 && chunks > rows ? chunks : rows;
+}
+
 // rows of `width` elements, `stride` elements apart: 16-byte aligned, not overlapping
 bool rows_ok(const void* p, long long stride, int width, int elem) {
   return p != nullptr && aligned(p, 16) && stride >= width && stride * elem % 16 == 0 && stride < (1ll << 40);
@@ -226,7 +232,7 @@ int echokv_query_quant_sizes(const echokv_config* cfg, echokv_quant_sizes* out) 
   out->codes_bytes = rows * cfg->head_dim;
   out->scales_bytes = rows / kQuantBlock * 4;
   out->tail_bytes = (uint64_t)cfg->max_batch * cfg->n_kv_heads * kQuantBlock * cfg->head_dim * (cfg->dtype == ECHOKV_BF16 ? 2 : 4);
-  out->workspace_bytes = quant_attn_workspace_bytes(cfg->head_dim);
+  out->workspace_bytes = quant_workspace(cfg);
   return ECHOKV_OK;
 }
 
@@ -273,7 +279,7 @@ int echokv_quant_attention(const echokv_config* cfg, const echokv_quant_cache* c
   if (!rows_ok(q, q_stride, cfg->n_q_heads * cfg->head_dim, elem)) return ECHOKV_EINVAL;
   if (!out || !aligned(out, 16) || !dev_block_table || !dev_seq_lens) return ECHOKV_EINVAL;
   if (!workspace || !aligned(workspace, 256)) return ECHOKV_EINVAL;
-  if (workspace_bytes < quant_attn_workspace_bytes(cfg->head_dim)) return ECHOKV_ECAPACITY;
+  if (workspace_bytes < quant_workspace(cfg)) return ECHOKV_ECAPACITY;
   a.q = q; a.q_stride = q_stride; a.out = out;
   a.table = dev_block_table; a.slots = dev_seq_slots; a.lens = dev_seq_lens; a.cu = dev_cu_tokens;
   a.softcap = options ? options->softcap : 0.f;
