@@ -66,20 +66,6 @@ struct CkWork {
   }
 };
 
-struct CkTail {
-  unsigned long long q_full[2], s_full[2], p_ready[2], o_done[2];
-  unsigned long long k_full[2], k_empty[2], v_full[2], v_empty[2], drain;
-  unsigned long long pre[kCkThreads + 1];
-  unsigned long long warp_sums[32];
-  float k_scale[kCkRing][8];                       // [tile][16-key block]
-  float v_ref[kCkRing];                            // [item]
-  float red[3][kCkConvThreads / 32];
-  uint32_t tmem_base;
-  int abort_flag;
-};
-template <int D>
-__host__ __device__ constexpr size_t ck_smem_bytes() { return 1024 + (size_t)(D / 64) * kCkChunkBytes * (2 + 2 + 2) + sizeof(CkTail); }
-
 __device__ __forceinline__ uint64_t ck_desc(uint32_t smem_addr, uint32_t lead_bytes) {
   uint64_t d = 0;
   d |= static_cast<uint64_t>((smem_addr & 0x3ffffu) >> 4);
@@ -297,14 +283,6 @@ __device__ __noinline__ float2 careful_piece(const CkRow w, const int c, const i
   return make_float2(m_ref, l_run + sum);
 }
 
-struct CkItem {
-  int b, h, row0;                                  // rows [row0, row0 + 256) of (sequence b, KV head h)
-  int slot, len, first, n, n_rows, act;            // act: tiles of rows that hold a row
-  int prefix, kv_end, n_tiles;
-  int t0, t1;                                      // tiles of keys that are this CTA's (none: t1 <= t0)
-  unsigned long long end;                          // unit behind the item
-};
-
 // The row blocks of a sequence: block j holds tokens [j per, (j + 1) per) times the group and sees kv_end(j) keys.  Everything is a
 // power of two but the lengths, so that the tiles of the first j blocks have a closed form.
 struct CkSeq {
@@ -336,6 +314,14 @@ struct CkSeq {
   }
   __device__ __forceinline__ unsigned long long units(int j) const { return tiles(j) + (unsigned long long)j * kCkItemCost; }
 };
+struct CkItem {
+  CkSeq s;
+  int b, j, h;                                     // row block j of (sequence b, KV head h):
+  int row0, n_rows, act;                           // rows [row0, row0 + 256) of n_rows; act: tiles of rows that hold one
+  int kv_end, n_tiles;
+  int t0, t1;                                      // tiles of keys that are this CTA's (none: t1 <= t0)
+  unsigned long long end;                          // unit behind the item
+};
 __device__ __forceinline__ CkSeq ck_seq(const QuantAttnArgs& a, int b) {
   const QuantSeq s = quant_seq(a, b);
   CkSeq c;
@@ -346,9 +332,28 @@ __device__ __forceinline__ CkSeq ck_seq(const QuantAttnArgs& a, int b) {
   c.per_shift = 8 - a.group_shift;
   return c;
 }
+__device__ __forceinline__ unsigned long long ck_ctas(unsigned long long total) {
+  return min((unsigned long long)gridDim.x, total / kCkMinShare + 1);
+}
 __device__ __forceinline__ unsigned long long ck_units(const QuantAttnArgs& a, const CkSeq& s) {
   return s.n > 0 ? s.units(s.blocks) * a.g.n_kv_heads : 0;
 }
+
+struct CkTail {
+  unsigned long long q_full[2], s_full[2], p_ready[2], o_done[2];
+  unsigned long long k_full[2], k_empty[2], v_full[2], v_empty[2], drain;
+  unsigned long long pre[kCkThreads + 1];
+  unsigned long long warp_sums[32];
+  float k_scale[kCkRing][8];                       // [tile][16-key block]
+  float v_ref[kCkRing];                            // [item]
+  unsigned long long share[2];                     // this CTA's units
+  CkItem item[kCkThreads / 32];                    // every warp's present item (in registers it would spill)
+  float red[3][kCkConvThreads / 32];
+  uint32_t tmem_base;
+  int abort_flag;
+};
+template <int D>
+__host__ __device__ constexpr size_t ck_smem_bytes() { return 1024 + (size_t)(D / 64) * kCkChunkBytes * (2 + 2 + 2) + sizeof(CkTail); }
 
 template <int FMT, int D>
 __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid_constant__ QuantAttnArgs a) {
@@ -405,6 +410,11 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
     for (int w = 0; w < warp; ++w) before += t.warp_sums[w];
     t.pre[tid + 1] = before + x;
     if (tid == 0) t.pre[0] = 0;
+    if (tid == kCkThreads - 1) {
+      const unsigned long long total = before + x, ctas = ck_ctas(total);
+      t.share[0] = blockIdx.x < ctas ? total * blockIdx.x / ctas : total;
+      t.share[1] = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : total;
+    }
   }
   if (warp == kCkThreads / 32 - 1) {
     tmem_alloc(smem_u32(&t.tmem_base), 512);
@@ -414,15 +424,20 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = t.tmem_base;
-  const unsigned long long total = t.pre[kCkThreads];
 
-  // this CTA's share of the units
-  const int ctas = (int)min((unsigned long long)gridDim.x, total / kCkMinShare + 1);
-  const unsigned long long u0 = (int)blockIdx.x < ctas ? total * blockIdx.x / ctas : total;
-  const unsigned long long u1 = (int)blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : total;
-
-  // the item that unit u is of, and the tiles of it from there to the share's end
-  const auto get_item = [&](unsigned long long u) {
+  // (sequence, row block, head) -> the rest; the item begins at unit `start`
+  const auto complete = [&](CkItem& it, unsigned long long start) {
+    it.row0 = it.j * kCkRows;
+    it.n_rows = it.s.n * a.group;
+    it.act = it.n_rows - it.row0 > kCkTile ? 2 : 1;
+    it.kv_end = it.s.kv_end(it.j);
+    it.n_tiles = (it.kv_end + kCkTile - 1) / kCkTile;
+    it.end = start + it.n_tiles + kCkItemCost;
+    it.t0 = start >= t.share[0] ? 0 : max(0, (int)(t.share[0] - start) - kCkItemCost);
+    it.t1 = (int)(min(t.share[1], it.end) - start) - kCkItemCost;
+  };
+  // the item that unit u is of
+  const auto find_item = [&](unsigned long long u) {
     int lo = 0, hi = kCkThreads;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -431,51 +446,75 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
     CkItem it;
     it.b = lo * per;
     unsigned long long base = t.pre[lo];
-    CkSeq s = ck_seq(a, it.b);
-    for (unsigned long long n = ck_units(a, s); base + n <= u; n = ck_units(a, s)) {
+    it.s = ck_seq(a, it.b);
+    for (unsigned long long n = ck_units(a, it.s); base + n <= u; n = ck_units(a, it.s)) {
       base += n;
-      s = ck_seq(a, ++it.b);
+      it.s = ck_seq(a, ++it.b);
     }
-    it.slot = s.slot; it.len = s.len; it.first = s.first; it.n = s.n;
-    it.n_rows = it.n * a.group;
     const unsigned long long rem = u - base;
-    int j = 0, j_hi = s.blocks;                    // the row block: the last one whose units begin at or before u
+    int j = 0, j_hi = it.s.blocks;                 // the row block: the last one whose units begin at or before u
     while (j_hi - j > 1) {
       const int mid = (j + j_hi) >> 1;
-      if (s.units(mid) * H <= rem) j = mid; else j_hi = mid;
+      if (it.s.units(mid) * H <= rem) j = mid; else j_hi = mid;
     }
-    it.row0 = j * kCkRows;
-    it.act = it.n_rows - it.row0 > kCkTile ? 2 : 1;
-    it.prefix = s.prefix;
-    it.kv_end = s.kv_end(j);
-    it.n_tiles = (it.kv_end + kCkTile - 1) / kCkTile;
-    const unsigned long long in_block = rem - s.units(j) * H, n = it.n_tiles + kCkItemCost;
+    it.j = j;
+    const unsigned long long in_block = rem - it.s.units(j) * H;
+    const int n = (it.s.kv_end(j) + kCkTile - 1) / kCkTile + kCkItemCost;
     it.h = (int)(in_block / n);
-    const unsigned long long start = u - (in_block - it.h * n);
-    it.end = start + n;
-    it.t0 = max(0, (int)(u - start) - kCkItemCost);
-    it.t1 = (int)(min(u1, it.end) - start) - kCkItemCost;
+    complete(it, u - (in_block - (unsigned long long)it.h * n));
     return it;
   };
-
-  if (tid == 0) {
-    // an item that begins in this share and goes on behind it
-    CkDesc d = {};
-    if (u1 > u0 && u1 < total) {
-      const CkItem it = get_item(u1 - 1);
-      const unsigned long long start = it.end - it.n_tiles - kCkItemCost;
-      const int done = (int)(u1 - start) - kCkItemCost;        // its tiles up to the share's end
-      const bool begins = start + kCkItemCost >= u0;
-      if (begins && done > 0 && done < it.n_tiles) {
-        d.n_parts = (int)((it.end * ctas - 1) / total) - (int)blockIdx.x + 1;
-        d.first = it.first; d.n_rows = it.n_rows; d.h = it.h; d.row0 = it.row0;
+  // the one after it, as long as that begins before u1
+  const auto next_item = [&](CkItem& it) {
+    if (++it.h == H) {
+      it.h = 0;
+      if (++it.j == it.s.blocks) {
+        it.j = 0;
+        do it.s = ck_seq(a, ++it.b); while (it.s.n == 0);
       }
     }
-    ws.desc[blockIdx.x] = d;
-  }
+    complete(it, it.end);
+  };
+  // the warp's item: the first that has tiles in this share, if any
+  const auto first_item = [&]() {
+    if (t.share[1] <= t.share[0]) return false;
+    CkItem it = find_item(t.share[0]);
+    while (it.t1 <= it.t0) {
+      if (it.end >= t.share[1]) return false;
+      next_item(it);
+    }
+    t.item[warp] = it;                             // (every lane the same)
+    __syncwarp();
+    return true;
+  };
+  // the next one (only the last can be without tiles)
+  const auto another_item = [&]() {
+    CkItem it = t.item[warp];
+    if (it.end >= t.share[1]) return false;
+    next_item(it);
+    __syncwarp();
+    t.item[warp] = it;
+    __syncwarp();
+    return it.t1 > it.t0;
+  };
 
   if (warp == kCkThreads / 32 - 1) {
     // =============================== products ===================================================
+    {
+      // an item that begins in this share and goes on behind it, for the merge
+      CkDesc d = {};
+      const unsigned long long u0 = t.share[0], u1 = t.share[1], total = t.pre[kCkThreads], ctas = ck_ctas(total);
+      if (u1 > u0 && u1 < total) {
+        const CkItem last = find_item(u1 - 1);
+        const unsigned long long start = last.end - last.n_tiles - kCkItemCost;
+        const int done = (int)(u1 - start) - kCkItemCost;      // its tiles up to the share's end
+        if (start + kCkItemCost >= u0 && done > 0 && done < last.n_tiles) {
+          d.n_parts = (int)((last.end * ctas - 1) / total) - (int)blockIdx.x + 1;
+          d.first = last.s.first; d.n_rows = last.n_rows; d.h = last.h; d.row0 = last.row0;
+        }
+      }
+      if (lane == 0) ws.desc[blockIdx.x] = d;
+    }
     {
       bool alive = true;
       uint32_t T = 0, n_item = 0, n_p[2] = {0, 0}; // tiles and items so far; tiles of either half
@@ -484,10 +523,8 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       unpack_u2(ck_desc(q_addr, 16), q_lo0, kmajor_hi);
       unpack_u2(ck_desc(k_addr, 16), k_lo0, kmajor_hi);
       unpack_u2(ck_desc(v_addr, kCkChunkBytes), v_lo0, v_hi);
-      for (unsigned long long u = u0; u < u1 && alive;) {
-        const CkItem it = get_item(u);
-        u = it.end;
-        if (it.t1 <= it.t0) continue;
+      const CkItem& it = t.item[warp];
+      for (bool more = first_item(); more && alive; more = another_item(), ++n_item) {
         const auto issue_s = [&](int x, uint32_t tile) {
           const uint32_t q_lo = q_lo0 + x * (kTileBytes >> 4), k_lo = k_lo0 + (tile & 1) * (kTileBytes >> 4);
 #pragma unroll
@@ -529,7 +566,6 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         }
         // (an idle second half waits for this too: its warps must not run items ahead of the barriers' phases)
         if (alive && it.act == 1) ck_commit(&t.o_done[1]);
-        ++n_item;
       }
       if (!alive) {
         // every product issued so far retires before the tensor memory is given back
@@ -565,16 +601,14 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       sts16(dst + (at0 ^ turn) + p * kRowStep * 128, w[0], w[1], w[2], w[3]);
       sts16(dst + (at1 ^ turn) + p * kRowStep * 128, w[4], w[5], w[6], w[7]);
     };
-    for (unsigned long long u = u0; u < u1;) {
-      const CkItem it = get_item(u);
-      u = it.end;
-      if (it.t1 <= it.t0) continue;
+    const CkItem& it = t.item[warp];
+    for (bool more = first_item(); more; more = another_item(), ++n_item) {
       if (!conv_all(alive)) break;                 // (a wait that ran out: all leave together)
-      const int32_t* pages = a.table + (long long)it.slot * g.max_pages;
-      const int n_full = it.len / kQuantBlock, n_codes = min(n_full, (it.kv_end + kQuantBlock - 1) / kQuantBlock);   // blocks of codes seen
+      const int32_t* pages = a.table + (long long)it.s.slot * g.max_pages;
+      const int n_full = it.s.len / kQuantBlock, n_codes = min(n_full, (it.kv_end + kQuantBlock - 1) / kQuantBlock);   // blocks of codes seen
       // the open block is seen, and in one of these tiles
       const bool open = it.kv_end > n_full * kQuantBlock && n_full / 8 >= it.t0 && n_full / 8 < it.t1;
-      const long long open_at = ((long long)it.slot * H + it.h) * kQuantBlock * D;
+      const long long open_at = ((long long)it.s.slot * H + it.h) * kQuantBlock * D;
       const auto page_of = [&](int tok) {          // page of a token that exists
         int id = pages[tok >> g.page_shift];
         if (id < 0 || id >= g.n_pages) {
@@ -586,12 +620,66 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       const auto scale_at = [&](int blk, int page) {
         return ((long long)page * H + it.h) * (g.page_tokens / kQuantBlock) + ((blk * kQuantBlock & (g.page_tokens - 1)) / kQuantBlock);
       };
+      // lane l < 8 keeps page and scales of block l of a tile, asked for two tiles (pages) and one (scales) ahead and looked at
+      // only when they are needed
+      const auto ask_page = [&](int tile) {
+        const int blk = tile * 8 + lane;
+        return lane < 8 && blk < n_codes ? pages[blk * kQuantBlock >> g.page_shift] : 0;
+      };
+      const auto checked = [&](int id) {
+        if (id < 0 || id >= g.n_pages) {
+          report_opt(a.status, ECHOKV_EBADPAGE);
+          id = 0;
+        }
+        return id;
+      };
+      float ks_next = 0.f, vs_next = 0.f, vs_cur;
+      const auto load_scales = [&](int tile, int page) {
+        const int blk = tile * 8 + lane;
+        ks_next = vs_next = 0.f;
+        if (lane < 8 && blk < n_codes) {
+          const long long at = scale_at(blk, page);
+          vs_next = g.scales[1][at];
+          ks_next = g.scales[0][at];
+        }
+      };
+      // codes of this thread's pieces, fetched one tile ahead (rows behind the last block of codes: page 0's, not looked at)
+      uint4 kc[NP], vc[NP];
+      const unsigned char* k_base = g.codes[0] + 16 * my_piece;
+      const unsigned char* v_base = g.codes[1] + 16 * my_piece;
+      const auto fetch = [&](int tile, int page8) {
+        uint32_t at[NP];
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+          const int row = min(my_row + kRowStep * p, kCkTile - 1);
+          const int page = __shfl_sync(0xffffffffu, page8, row >> 4);
+          at[p] = (uint32_t)((page * H + it.h) * g.page_tokens + ((tile * kCkTile + row) & (g.page_tokens - 1)));
+        }
+#pragma unroll
+        for (int p = 0; p < NP; ++p) kc[p] = *reinterpret_cast<const uint4*>(k_base + (size_t)at[p] * D);
+#pragma unroll
+        for (int p = 0; p < NP; ++p) vc[p] = *reinterpret_cast<const uint4*>(v_base + (size_t)at[p] * D);
+      };
+      // 16 features of a row of the open block as fp16 pairs, or zeros
+      const auto open_row = [&](int which, int row, float up, uint32_t (&w)[8]) {
+        const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(g.tail[which]) + open_at + (long long)row * D + 16 * my_piece;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const uint4 x = *reinterpret_cast<const uint4*>(p + 8 * q);
+          const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[4 * q + e] = h2(__uint_as_float(y[e] << 16) * up, __uint_as_float(y[e] & 0xffff0000u) * up);
+        }
+      };
+      int page8 = checked(ask_page(it.t0)), page8_next = ask_page(it.t0 + 1);
+      load_scales(it.t0, page8);
+      fetch(it.t0, page8);
       // the largest V scale in these tiles, and the largest magnitudes of the open block
       float v_top = 0.f;
       for (int blk = 8 * it.t0 + ct; blk < min(n_codes, 8 * it.t1); blk += kCkConvThreads) v_top = fmaxf(v_top, g.scales[1][scale_at(blk, page_of(blk * kQuantBlock))]);
       uint32_t open_k = 0, open_v = 0;
       if (open) {
-        const int n_open = it.len - n_full * kQuantBlock;
+        const int n_open = it.s.len - n_full * kQuantBlock;
         const uint32_t* kt = reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(g.tail[0]) + open_at);
         const uint32_t* vt = reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(g.tail[1]) + open_at);
         for (int w = ct; w < n_open * D / 2; w += kCkConvThreads) {
@@ -627,62 +715,6 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       // which the products have to have read, the first of them after the softmax warps took item n's result)
       if (ct == 0) t.v_ref[n_item % kCkRing] = v_ref * (1.f / kCkVScale);
 
-      // lane l < 8 keeps page and scales of block l of a tile, asked for two tiles (pages) and one (scales) ahead and looked at
-      // only when they are needed
-      const auto ask_page = [&](int tile) {
-        const int blk = tile * 8 + lane;
-        return lane < 8 && blk < n_codes ? pages[blk * kQuantBlock >> g.page_shift] : 0;
-      };
-      const auto checked = [&](int id) {
-        if (id < 0 || id >= g.n_pages) {
-          report_opt(a.status, ECHOKV_EBADPAGE);
-          id = 0;
-        }
-        return id;
-      };
-      float ks_next = 0.f, vs_next = 0.f, vs_cur;
-      const auto load_scales = [&](int tile, int page) {
-        const int blk = tile * 8 + lane;
-        ks_next = vs_next = 0.f;
-        if (lane < 8 && blk < n_codes) {
-          const long long at = scale_at(blk, page);
-          vs_next = g.scales[1][at];
-          ks_next = g.scales[0][at];
-        } else if (open && blk == n_full) {
-          ks_next = open_bad ? __uint_as_float(0x7fc00000u) : open_back;
-        }
-      };
-      // codes of this thread's pieces, fetched one tile ahead (rows behind the last block of codes: page 0's, not looked at)
-      uint4 kc[NP], vc[NP];
-      const unsigned char* k_base = g.codes[0] + 16 * my_piece;
-      const unsigned char* v_base = g.codes[1] + 16 * my_piece;
-      const auto fetch = [&](int tile, int page8) {
-        uint32_t at[NP];
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
-          const int row = min(my_row + kRowStep * p, kCkTile - 1);
-          const int page = __shfl_sync(0xffffffffu, page8, row >> 4);
-          at[p] = (uint32_t)((page * H + it.h) * g.page_tokens + ((tile * kCkTile + row) & (g.page_tokens - 1)));
-        }
-#pragma unroll
-        for (int p = 0; p < NP; ++p) kc[p] = *reinterpret_cast<const uint4*>(k_base + (size_t)at[p] * D);
-#pragma unroll
-        for (int p = 0; p < NP; ++p) vc[p] = *reinterpret_cast<const uint4*>(v_base + (size_t)at[p] * D);
-      };
-      // 16 features of a row of the open block as fp16 pairs, or zeros
-      const auto open_row = [&](int which, int row, float up, uint32_t (&w)[8]) {
-        const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(g.tail[which]) + open_at + (long long)row * D + 16 * my_piece;
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const uint4 x = *reinterpret_cast<const uint4*>(p + 8 * q);
-          const uint32_t y[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[4 * q + e] = h2(__uint_as_float(y[e] << 16) * up, __uint_as_float(y[e] & 0xffff0000u) * up);
-        }
-      };
-      int page8 = checked(ask_page(it.t0)), page8_next = ask_page(it.t0 + 1);
-      load_scales(it.t0, page8);
-      fetch(it.t0, page8);
       for (int tile = it.t0; tile < it.t1; ++tile, ++T) {
         const int st = T & 1;
         const uint32_t parity = ((T >> 1) & 1) ^ 1;
@@ -701,7 +733,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
               w[2 * e] = codes_pair<FMT, 0>(x);
               w[2 * e + 1] = codes_pair<FMT, 1>(x);
             }
-          } else if (open && !open_bad && tok < it.len) {
+          } else if (open && !open_bad && tok < it.s.len) {
             open_row(0, tok - n_full * kQuantBlock, open_up, w);
           } else {
 #pragma unroll
@@ -711,7 +743,10 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         }
         // (the ring: tile T + 4's scales are written when S(T + 2) is complete, so after softmax(T + 1) was)
         vs_cur = vs_next;
-        if (ct < 8) t.k_scale[T % kCkRing][ct] = vs_cur == vs_cur ? ks_next : vs_cur;
+        if (ct < 8) {
+          if (open && tile * 8 + ct == n_full) ks_next = open_bad ? __uint_as_float(0x7fc00000u) : open_back;
+          t.k_scale[T % kCkRing][ct] = vs_cur == vs_cur ? ks_next : vs_cur;
+        }
         fence_proxy_async_smem();
         warp_arrive(&t.k_full[st]);
 
@@ -733,7 +768,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
               w[2 * e] = mul_h2(codes_pair<FMT, 0>(x), r2);
               w[2 * e + 1] = mul_h2(codes_pair<FMT, 1>(x), r2);
             }
-          } else if (blk >= n_codes && open && !open_bad && tok < it.len) {
+          } else if (blk >= n_codes && open && !open_bad && tok < it.s.len) {
             open_row(1, tok - n_full * kQuantBlock, v_inv * kCkVScale, w);
           } else {
 #pragma unroll
@@ -750,7 +785,6 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           fetch(tile + 1, page8);
         }
       }
-      ++n_item;
     }
   } else {
     // =============================== softmax ====================================================
@@ -759,24 +793,15 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
     const uint32_t s_addr = lane_base + x * 128, o_addr = lane_base + 256 + x * D;
     const float cap_in = a.softcap > 0.f ? 1.f / a.softcap : 0.f, cap_out = a.softcap * kLog2e;
     uint32_t T = 0, n_item = 0, n_mine = 0, n_done = 0;   // (of this half: tiles and results, whose barriers move with them)
-    for (unsigned long long u = u0; u < u1;) {
-      const CkItem it = get_item(u);
-      u = it.end;
-      if (it.t1 <= it.t0) continue;
-      const int r = it.row0 + x * kCkTile + row;
-      const bool row_ok = r < it.n_rows;
-      const int qi = row_ok ? r >> a.group_shift : 0, head = it.h * a.group + (r & (a.group - 1));
-      const int pos = it.len - it.n + qi;
-      // keys [0, vis) are seen; a row of none of the queries sees everything (its scores are 0) and goes nowhere
-      const int vis = row_ok ? max(pos + 1, it.prefix) : 0x7fffffff;
+    const auto load_q = [&](const CkItem& it) {
       // the warp's 32 query rows as fp16 around each row's power of two: 16 (8) lanes to a row, so that they read it side by side
       float c_row = 0.f;
       {
         constexpr int kLanes = D / 8, kPerGo = 32 / kLanes;
         const int my = lane / kLanes, p = lane % kLanes;
         const int r_warp = it.row0 + x * kCkTile + (warp & 3) * 32;
-        const __nv_bfloat16* qb = static_cast<const __nv_bfloat16*>(a.q) + (long long)it.first * a.q_stride + (long long)it.h * a.group * D + 8 * p;
-#pragma unroll 4
+        const __nv_bfloat16* qb = static_cast<const __nv_bfloat16*>(a.q) + (long long)it.s.first * a.q_stride + (long long)it.h * a.group * D + 8 * p;
+#pragma unroll 8
         for (int go = 0; go < kLanes; ++go) {
           const int rr = go * kPerGo + my, rq = r_warp + rr;           // row of the warp, of the sequence
           uint4 v = make_uint4(0u, 0u, 0u, 0u);
@@ -799,13 +824,27 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       }
       fence_proxy_async_smem();
       warp_arrive(&t.q_full[x]);
+      return c_row;
+    };
+    const CkItem& it = t.item[warp];
+    bool more = first_item();
+    float c_row = more ? load_q(it) : 0.f;
+    while (more) {
       if (x >= it.act) {
         T += it.t1 - it.t0;
         if (!__all_sync(0xffffffffu, ck_wait(&t.o_done[x], n_done & 1, abort_flag, a.status))) break;
         ++n_done;
         ++n_item;
+        more = another_item();
+        if (more) c_row = load_q(it);
         continue;
       }
+      const int r = it.row0 + x * kCkTile + row;
+      const bool row_ok = r < it.n_rows;
+      const int qi = row_ok ? r >> a.group_shift : 0, head = it.h * a.group + (r & (a.group - 1));
+      const int pos = it.s.len - it.s.n + qi;
+      // keys [0, vis) are seen; a row of none of the queries sees everything (its scores are 0) and goes nowhere
+      const int vis = row_ok ? max(pos + 1, it.s.prefix) : 0x7fffffff;
       const float slope2 = a.slopes && row_ok ? a.slopes[head] * kLog2e : 0.f;
       CkRow w;
       w.s_addr = s_addr; w.o_addr = o_addr;
@@ -821,16 +860,19 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         tc_fence_after();
         const int n_vis = max(0, min(kCkTile, vis - tile * kCkTile));
         const float* k_scale = t.k_scale[T % kCkRing];
-        // the common way: every key seen, the reference where it is
+        // the common way: the reference where it is
         float top = 0.f;
-        const auto piece = [&](auto mode_tag, uint32_t (&sr)[32], int c) {
+        const auto piece = [&](auto mode_tag, auto masked_tag, uint32_t (&sr)[32], int c) {
           constexpr int kMode = decltype(mode_tag)::value;               // 0: scores as they are, 1 / 2: capped, short / long polynomial
+          constexpr bool kMasked = decltype(masked_tag)::value;          // some key of the tile is not seen
+          const int vis_c = max(0, min(32, n_vis - 32 * c));
+          const uint32_t seen = kMasked ? (uint32_t)((1ull << vis_c) - 1) : 0xffffffffu;
           float f0 = c_row * k_scale[2 * c], f1 = c_row * k_scale[2 * c + 1];      // (16 keys each)
           bool bad = false;
           if (kMode > 0) {
             const float z = tanh_pieces<kMode == 1>(sr, f0 * cap_in, f1 * cap_in);
             top = fmaxf(top, z);
-            bad = !(z <= (kMode == 1 ? 0.25f : 1.f));
+            bad = !(z <= (kMode == 1 ? 0.25f : 1.f)) && (!kMasked || vis_c > 0);
             f0 = f1 = cap_out;
           }
           uint32_t pk[16];
@@ -841,6 +883,8 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
             const float f = j < 8 ? f0 : f1;
             float y0, y1;
             unpack_f2(fma_f2(pack_u2(sr[2 * j], sr[2 * j + 1]), pack_f2(f, f), nm), y0, y1);
+            if (kMasked && !(seen >> (2 * j) & 1)) y0 = -INFINITY;
+            if (kMasked && !(seen >> (2 * j + 1) & 1)) y1 = -INFINITY;
             const float p0 = exp2_approx(y0), p1 = exp2_approx(y1);
             sum2[j & 1] = add_f2(sum2[j & 1], pack_f2(p0, p1));
             pk[j] = h2(p0, p1);
@@ -856,20 +900,25 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           tmem_st16_regs(s_addr + 16 * c, pk);
           return true;
         };
-        // pieces done the common way; the rest of the tile, from the first one that it does not do for, is done the careful way
-        const auto pieces_of = [&](auto mode_tag) {
-          int c = 0;
+        // pieces from c on done the common way; the rest of the tile, from the first one that it does not do for, the careful way
+        const auto pieces_of = [&](auto mode_tag, auto masked_tag, int c) {
 #pragma unroll 1
           for (; c < 4; ++c) {
             uint32_t sr[32];
             tmem_ld32_issue(s_addr + 32 * c, sr);
             tmem_ld_wait();
-            if (!piece(mode_tag, sr, c)) break;
+            if (!piece(mode_tag, masked_tag, sr, c)) break;
           }
           return c;
         };
-        const bool full = a.slopes == nullptr && __all_sync(0xffffffffu, n_vis == kCkTile);
-        if (full && tile == it.t0) {
+        const auto careful = [&](int c) {
+          const float2 r = careful_piece<D>(w, c, tile * kCkTile + 32 * c, n_vis, tile > it.t0, c_row * k_scale[2 * c], c_row * k_scale[2 * c + 1],
+                                            m_ref, l_run);
+          m_ref = r.x;
+          l_run = r.y;
+        };
+        const bool full = __all_sync(0xffffffffu, n_vis == kCkTile);
+        if (!w.biased && full && tile == it.t0) {
           // the first reference: what the first 32 keys ask for (capped scores are at most the uncapped ones, and the cap)
           uint32_t sr[32];
           tmem_ld32_issue(s_addr, sr);
@@ -885,38 +934,44 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           if (mx > -INFINITY) m_ref = ceilf(mx) + kCkMargin;
         }
         int done = 0;
-        if (full && __all_sync(0xffffffffu, m_ref > -INFINITY)) {
-          if (!w.capped) {
-            done = pieces_of(std::integral_constant<int, 0>());
-          } else {
-            done = wide ? pieces_of(std::integral_constant<int, 2>()) : pieces_of(std::integral_constant<int, 1>());
-            wide = __any_sync(0xffffffffu, top > 0.25f);
+        if (!w.biased) {
+          // (a row that sees none of these keys needs no reference)
+          if (!__all_sync(0xffffffffu, m_ref > -INFINITY || n_vis == 0)) careful(done++);
+          if (__all_sync(0xffffffffu, m_ref > -INFINITY || n_vis == 0)) {
+            const auto go = [&](auto mode_tag) {
+              done = full ? pieces_of(mode_tag, std::false_type(), done) : pieces_of(mode_tag, std::true_type(), done);
+            };
+            if (!w.capped) {
+              go(std::integral_constant<int, 0>());
+            } else {
+              if (wide) go(std::integral_constant<int, 2>()); else go(std::integral_constant<int, 1>());
+              wide = __any_sync(0xffffffffu, top > 0.25f);
+            }
           }
         }
 #pragma unroll 1
-        for (int c = done; c < 4; ++c) {
-          const float2 r = careful_piece<D>(w, c, tile * kCkTile + 32 * c, n_vis, tile > it.t0, c_row * k_scale[2 * c], c_row * k_scale[2 * c + 1],
-                                            m_ref, l_run);
-          m_ref = r.x;
-          l_run = r.y;
-        }
+        for (; done < 4; ++done) careful(done);
         tmem_st_wait();
         tc_fence_before();
         warp_arrive(&t.p_ready[x]);
       }
       if (!alive) break;
-      // ---- the row's result
-      alive = __all_sync(0xffffffffu, ck_wait(&t.o_done[x], n_done & 1, abort_flag, a.status));
-      if (!alive) break;
-      ++n_done;
-      tc_fence_after();
+      // ---- the row's result.  The next item's queries come first: its scores are then under way meanwhile.  (This
+      // item's scores are complete; its V reference stays in the ring until the products have seen the next queries.)
       const float inv = l_run == 0.f ? 0.f : t.v_ref[n_item % kCkRing] / l_run;
       const bool whole = it.t1 - it.t0 == it.n_tiles;
       // (a part: o / l beside the reference and l, in the slot of an item that goes on from the CTA before or in the next)
       const long long slot = (long long)blockIdx.x * 2 + (it.t0 == 0);
       if (!whole) ws.ml[slot * kCkRows + x * kCkTile + row] = make_float2(m_ref, l_run);
       float4* part = ws.o + slot * (D / 4) * kCkRows + x * kCkTile + row;
-      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.out) + ((long long)(it.first + qi) * a.n_q_heads + head) * D;
+      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.out) + ((long long)(it.s.first + qi) * a.n_q_heads + head) * D;
+      ++n_item;
+      more = another_item();
+      if (more) c_row = load_q(it);
+      alive = __all_sync(0xffffffffu, ck_wait(&t.o_done[x], n_done & 1, abort_flag, a.status));
+      if (!alive) break;
+      ++n_done;
+      tc_fence_after();
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
         uint32_t orow[32];
@@ -935,7 +990,6 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           }
         }
       }
-      ++n_item;
       tc_fence_before();
     }
   }
