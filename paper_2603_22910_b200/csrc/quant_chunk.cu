@@ -38,14 +38,7 @@ constexpr float kCkMargin = 8.f;                   // a reference that moves goe
 constexpr float kCkSumLimit = 32768.f;             // a row's 32 probabilities sum to less: each fits fp16
 constexpr float kCkVScale = 64.f;
 constexpr int kCkMaxCtas = 160;                    // (of the workspace's layout)
-#ifndef CKCOST
-#define CKCOST 2
-#endif
-#ifndef CKMIN
-#define CKMIN 6
-#endif
-constexpr int kCkItemCost = CKCOST;                     // what an item costs beside its tiles (queries, first tile, result), in tiles
-constexpr int kCkMinShare = CKMIN;                     // units per CTA at least
+constexpr int kCkMinShare = 3;                     // units per CTA at least
 constexpr int kCkMergeCols = 16;                   // features per thread of the merge
 
 struct CkDesc {                                    // an item cut at the end of CTA g's share
@@ -355,6 +348,75 @@ struct CkTail {
 template <int D>
 __host__ __device__ constexpr size_t ck_smem_bytes() { return 1024 + (size_t)(D / 64) * kCkChunkBytes * (2 + 2 + 2) + sizeof(CkTail); }
 
+// Finding items is code of its own that all roles share: a step through it costs less than fetching copies of it.
+// (sequence, row block, head) -> the rest; the item begins at unit `start`
+__device__ __forceinline__ void ck_complete(const QuantAttnArgs& a, const CkTail& t, CkItem& it, unsigned long long start) {
+  it.row0 = it.j * kCkRows;
+  it.n_rows = it.s.n * a.group;
+  it.act = it.n_rows - it.row0 > kCkTile ? 2 : 1;
+  it.kv_end = it.s.kv_end(it.j);
+  it.n_tiles = (it.kv_end + kCkTile - 1) / kCkTile;
+  it.end = start + it.n_tiles + kCkItemCost;
+  it.t0 = start >= t.share[0] ? 0 : max(0, (int)(t.share[0] - start) - kCkItemCost);
+  it.t1 = (int)(min(t.share[1], it.end) - start) - kCkItemCost;
+}
+// the warp's item becomes the one that unit u is of (every lane writes the same)
+__device__ __noinline__ void ck_find(const QuantAttnArgs& a, CkTail& t, unsigned long long u) {
+  const int per = (a.B + kCkThreads - 1) / kCkThreads, H = a.g.n_kv_heads;
+  int lo = 0, hi = kCkThreads;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (t.pre[mid] <= u) lo = mid; else hi = mid;
+  }
+  CkItem it;
+  it.b = lo * per;
+  unsigned long long base = t.pre[lo];
+  it.s = ck_seq(a, it.b);
+  if (per > 1) {
+    for (unsigned long long n = ck_units(a, it.s); base + n <= u; n = ck_units(a, it.s)) {
+      base += n;
+      it.s = ck_seq(a, ++it.b);
+    }
+  }
+  const unsigned long long rem = u - base;
+  int j = 0, j_hi = it.s.blocks;                   // the row block: the last one whose units begin at or before u
+#pragma unroll 1
+  while (j_hi - j > 1) {
+    const int mid = (j + j_hi) >> 1;
+    if (it.s.units(mid) * H <= rem) j = mid; else j_hi = mid;
+  }
+  it.j = j;
+  const uint32_t in_block = (uint32_t)(rem - it.s.units(j) * H), n = (it.s.kv_end(j) + kCkTile - 1) / kCkTile + kCkItemCost;
+  it.h = (int)(in_block / n);
+  ck_complete(a, t, it, u - (in_block - it.h * n));
+  t.item[threadIdx.x >> 5] = it;
+  __syncwarp();
+}
+// the one after it, if that begins in this CTA's share; true if it has tiles there (only the first and the last can be without)
+__device__ __noinline__ bool ck_next(const QuantAttnArgs& a, CkTail& t) {
+  CkItem it = t.item[threadIdx.x >> 5];
+  if (it.end >= t.share[1]) return false;
+  if (++it.h == a.g.n_kv_heads) {
+    it.h = 0;
+    if (++it.j == it.s.blocks) {
+      it.j = 0;
+      do it.s = ck_seq(a, ++it.b); while (it.s.n == 0);
+    }
+  }
+  ck_complete(a, t, it, it.end);
+  __syncwarp();
+  t.item[threadIdx.x >> 5] = it;
+  __syncwarp();
+  return it.t1 > it.t0;
+}
+// the first that has tiles in the share, if any
+__device__ __forceinline__ bool ck_first(const QuantAttnArgs& a, CkTail& t) {
+  if (t.share[1] <= t.share[0]) return false;
+  ck_find(a, t, t.share[0]);
+  const CkItem& it = t.item[threadIdx.x >> 5];
+  return it.t1 > it.t0 || ck_next(a, t);
+}
+
 template <int FMT, int D>
 __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid_constant__ QuantAttnArgs a) {
   constexpr int NC = D / 64;
@@ -425,79 +487,6 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
   tc_fence_after();
   const uint32_t tmem = t.tmem_base;
 
-  // (sequence, row block, head) -> the rest; the item begins at unit `start`
-  const auto complete = [&](CkItem& it, unsigned long long start) {
-    it.row0 = it.j * kCkRows;
-    it.n_rows = it.s.n * a.group;
-    it.act = it.n_rows - it.row0 > kCkTile ? 2 : 1;
-    it.kv_end = it.s.kv_end(it.j);
-    it.n_tiles = (it.kv_end + kCkTile - 1) / kCkTile;
-    it.end = start + it.n_tiles + kCkItemCost;
-    it.t0 = start >= t.share[0] ? 0 : max(0, (int)(t.share[0] - start) - kCkItemCost);
-    it.t1 = (int)(min(t.share[1], it.end) - start) - kCkItemCost;
-  };
-  // the item that unit u is of
-  const auto find_item = [&](unsigned long long u) {
-    int lo = 0, hi = kCkThreads;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (t.pre[mid] <= u) lo = mid; else hi = mid;
-    }
-    CkItem it;
-    it.b = lo * per;
-    unsigned long long base = t.pre[lo];
-    it.s = ck_seq(a, it.b);
-    for (unsigned long long n = ck_units(a, it.s); base + n <= u; n = ck_units(a, it.s)) {
-      base += n;
-      it.s = ck_seq(a, ++it.b);
-    }
-    const unsigned long long rem = u - base;
-    int j = 0, j_hi = it.s.blocks;                 // the row block: the last one whose units begin at or before u
-    while (j_hi - j > 1) {
-      const int mid = (j + j_hi) >> 1;
-      if (it.s.units(mid) * H <= rem) j = mid; else j_hi = mid;
-    }
-    it.j = j;
-    const unsigned long long in_block = rem - it.s.units(j) * H;
-    const int n = (it.s.kv_end(j) + kCkTile - 1) / kCkTile + kCkItemCost;
-    it.h = (int)(in_block / n);
-    complete(it, u - (in_block - (unsigned long long)it.h * n));
-    return it;
-  };
-  // the one after it, as long as that begins before u1
-  const auto next_item = [&](CkItem& it) {
-    if (++it.h == H) {
-      it.h = 0;
-      if (++it.j == it.s.blocks) {
-        it.j = 0;
-        do it.s = ck_seq(a, ++it.b); while (it.s.n == 0);
-      }
-    }
-    complete(it, it.end);
-  };
-  // the warp's item: the first that has tiles in this share, if any
-  const auto first_item = [&]() {
-    if (t.share[1] <= t.share[0]) return false;
-    CkItem it = find_item(t.share[0]);
-    while (it.t1 <= it.t0) {
-      if (it.end >= t.share[1]) return false;
-      next_item(it);
-    }
-    t.item[warp] = it;                             // (every lane the same)
-    __syncwarp();
-    return true;
-  };
-  // the next one (only the last can be without tiles)
-  const auto another_item = [&]() {
-    CkItem it = t.item[warp];
-    if (it.end >= t.share[1]) return false;
-    next_item(it);
-    __syncwarp();
-    t.item[warp] = it;
-    __syncwarp();
-    return it.t1 > it.t0;
-  };
-
   if (warp == kCkThreads / 32 - 1) {
     // =============================== products ===================================================
     {
@@ -505,7 +494,9 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       CkDesc d = {};
       const unsigned long long u0 = t.share[0], u1 = t.share[1], total = t.pre[kCkThreads], ctas = ck_ctas(total);
       if (u1 > u0 && u1 < total) {
-        const CkItem last = find_item(u1 - 1);
+        ck_find(a, t, u1 - 1);
+        const CkItem last = t.item[warp];
+        __syncwarp();
         const unsigned long long start = last.end - last.n_tiles - kCkItemCost;
         const int done = (int)(u1 - start) - kCkItemCost;      // its tiles up to the share's end
         if (start + kCkItemCost >= u0 && done > 0 && done < last.n_tiles) {
@@ -524,7 +515,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       unpack_u2(ck_desc(k_addr, 16), k_lo0, kmajor_hi);
       unpack_u2(ck_desc(v_addr, kCkChunkBytes), v_lo0, v_hi);
       const CkItem& it = t.item[warp];
-      for (bool more = first_item(); more && alive; more = another_item(), ++n_item) {
+      for (bool more = ck_first(a, t); more && alive; more = ck_next(a, t), ++n_item) {
         const auto issue_s = [&](int x, uint32_t tile) {
           const uint32_t q_lo = q_lo0 + x * (kTileBytes >> 4), k_lo = k_lo0 + (tile & 1) * (kTileBytes >> 4);
 #pragma unroll
@@ -602,7 +593,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       sts16(dst + (at1 ^ turn) + p * kRowStep * 128, w[4], w[5], w[6], w[7]);
     };
     const CkItem& it = t.item[warp];
-    for (bool more = first_item(); more; more = another_item(), ++n_item) {
+    for (bool more = ck_first(a, t); more; more = ck_next(a, t), ++n_item) {
       if (!conv_all(alive)) break;                 // (a wait that ran out: all leave together)
       const int32_t* pages = a.table + (long long)it.s.slot * g.max_pages;
       const int n_full = it.s.len / kQuantBlock, n_codes = min(n_full, (it.kv_end + kQuantBlock - 1) / kQuantBlock);   // blocks of codes seen
@@ -794,40 +785,64 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
     const float cap_in = a.softcap > 0.f ? 1.f / a.softcap : 0.f, cap_out = a.softcap * kLog2e;
     uint32_t T = 0, n_item = 0, n_mine = 0, n_done = 0;   // (of this half: tiles and results, whose barriers move with them)
     const auto load_q = [&](const CkItem& it) {
-      // the warp's 32 query rows as fp16 around each row's power of two: 16 (8) lanes to a row, so that they read it side by side
-      float c_row = 0.f;
+      // the warp's 32 query rows, fetched into their places with 16 (8) lanes side by side on a row, all on their way at once
+      // (rows of none of the queries: zeros), ...
       {
         constexpr int kLanes = D / 8, kPerGo = 32 / kLanes;
         const int my = lane / kLanes, p = lane % kLanes;
         const int r_warp = it.row0 + x * kCkTile + (warp & 3) * 32;
         const __nv_bfloat16* qb = static_cast<const __nv_bfloat16*>(a.q) + (long long)it.s.first * a.q_stride + (long long)it.h * a.group * D + 8 * p;
-#pragma unroll 8
+#pragma unroll 1
         for (int go = 0; go < kLanes; ++go) {
           const int rr = go * kPerGo + my, rq = r_warp + rr;           // row of the warp, of the sequence
-          uint4 v = make_uint4(0u, 0u, 0u, 0u);
-          if (rq < it.n_rows) v = *reinterpret_cast<const uint4*>(qb + (long long)(rq >> a.group_shift) * a.q_stride + (rq & (a.group - 1)) * D);
-          uint32_t top = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
-          top = max(top & 0xffff0000u, top << 16);
+          const bool ok = rq < it.n_rows;
+          const void* src = ok ? qb + (long long)(rq >> a.group_shift) * a.q_stride + (rq & (a.group - 1)) * D : a.q;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(q_addr + x * kTileBytes + ck_off((warp & 3) * 32 + rr, p)), "l"(src),
+                       "r"(ok ? 16 : 0)
+                       : "memory");
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncwarp();
+      }
+      // ... then made fp16 around its power of two by the row's own thread (the swizzle keeps the lanes on different banks)
+      const uint32_t q_row = q_addr + x * kTileBytes + row * 128;
+      const auto q_at = [&](int p) { return q_row + (p >> 3) * kCkChunkBytes + (((p & 7) ^ (row & 7)) << 4); };
+      const auto read4 = [&](int p, uint4 (&v)[4]) {
 #pragma unroll
-          for (int o = kLanes / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-          float back;
-          const float up = scale_up_to_half(__uint_as_float(top), &back);
-          const uint32_t y[4] = {v.x, v.y, v.z, v.w};
+        for (int i = 0; i < 4; ++i)
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w) : "r"(q_at(p + i)) : "memory");
+      };
+      uint32_t top = 0;
+#pragma unroll 1
+      for (int p = 0; p < D / 8; p += 4) {
+        uint4 v[4];
+        read4(p, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          top = __vmaxu2(__vmaxu2(top, __vmaxu2(v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu)), __vmaxu2(v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu));
+      }
+      float c_row;
+      const float up = scale_up_to_half(__uint_as_float(max(top & 0xffff0000u, top << 16)), &c_row);
+#pragma unroll 1
+      for (int p = 0; p < D / 8; p += 4) {
+        uint4 v[4];
+        read4(p, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t y[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
           uint32_t z[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) z[e] = h2(__uint_as_float(y[e] << 16) * up, __uint_as_float(y[e] & 0xffff0000u) * up);
-          sts16(q_addr + x * kTileBytes + ck_off((warp & 3) * 32 + rr, p), z[0], z[1], z[2], z[3]);
-          const float mine = __shfl_sync(0xffffffffu, back, (lane % kPerGo) * kLanes);       // of row go * kPerGo + lane % kPerGo
-          if (lane / kPerGo == go) c_row = mine;
+          sts16(q_at(p + i), z[0], z[1], z[2], z[3]);
         }
-        c_row *= a.scale * (a.softcap > 0.f ? 1.f : kLog2e);
       }
+      c_row *= a.scale * (a.softcap > 0.f ? 1.f : kLog2e);
       fence_proxy_async_smem();
       warp_arrive(&t.q_full[x]);
       return c_row;
     };
     const CkItem& it = t.item[warp];
-    bool more = first_item();
+    bool more = ck_first(a, t);
     float c_row = more ? load_q(it) : 0.f;
     while (more) {
       if (x >= it.act) {
@@ -835,7 +850,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         if (!__all_sync(0xffffffffu, ck_wait(&t.o_done[x], n_done & 1, abort_flag, a.status))) break;
         ++n_done;
         ++n_item;
-        more = another_item();
+        more = ck_next(a, t);
         if (more) c_row = load_q(it);
         continue;
       }
@@ -966,7 +981,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       float4* part = ws.o + slot * (D / 4) * kCkRows + x * kCkTile + row;
       __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.out) + ((long long)(it.s.first + qi) * a.n_q_heads + head) * D;
       ++n_item;
-      more = another_item();
+      more = ck_next(a, t);
       if (more) c_row = load_q(it);
       alive = __all_sync(0xffffffffu, ck_wait(&t.o_done[x], n_done & 1, abort_flag, a.status));
       if (!alive) break;

@@ -35,33 +35,45 @@ __device__ __forceinline__ QuantSeq quant_seq(const QuantAttnArgs& a, int b) {
   return s;
 }
 
-// Which of the two attention kernels takes the sequences of many query rows (chunk_rows of them per KV head and more)?  The row
-// kernel cuts the work of all sequences into equal shares for the whole machine, in units of 16 keys x 8 query rows; the chunk kernel
-// gives 256 query rows and all their keys to one CTA.  Measured (32 / 8 heads of 128, int8): a unit takes the machine 0.63 ns; 128
-// keys of an item take its CTA 2.9 us, as long as the machine takes for 4600 units, so a block of 16 keys for 576.  The chunk
-// kernel's time is that of the longest item, or of all of them over the SMs where they are many.  (One sequence over 8192 keys:
-// 64 tokens 89 us by rows, 185 by chunks, 256 tokens the other way round; 8 sequences: 16 tokens 166 and 165 us, 64 tokens 613
-// and 201.)  Both kernels compute the answer from the lengths, every thread of a block the same one.
-constexpr unsigned long long kChunkUnits = 500;
+// Which of the two attention kernels takes the sequences of many query rows (chunk_rows of them per KV head and more)?  Both cut
+// the work of all sequences into equal shares: the row kernel in units of 16 keys x 8 query rows, the chunk kernel in tiles of
+// 128 keys of items of 256 query rows, with a cost of 4 tiles to an item.  Measured (32 / 8 heads of 128, int8): by rows 15 us + 92
+// ns for every unit of an SM; by chunks 28 us (two more launches, longer start) + 0.30 us for every 16 keys of an item on an
+// SM.  (One sequence over 8192 keys: 16 tokens 38 us by rows, 40 by chunks, 32 tokens 57 and 40, 128 tokens 172 and 49; over
+// 1024 keys, 64 tokens 30 and 30; 8 sequences over 32768 keys, 64 tokens: 2560 and 322.)  Both kernels compute the answer from
+// the lengths, every thread of a block the same one.
+constexpr int kCkItemCost = 4;                     // in tiles of 128 keys: queries, first tile, result
 __device__ __forceinline__ bool many_rows(const QuantAttnArgs& a, const QuantSeq& s) {
   return a.chunk_rows > 0 && !s.error && (long long)s.n * a.group >= a.chunk_rows;
 }
 __device__ __forceinline__ bool take_chunks(const QuantAttnArgs& a, int sm_count) {
   if (a.chunk_rows == 0) return false;
-  __shared__ unsigned long long sums[3];           // units by rows; blocks of all items; blocks of the longest
-  if (threadIdx.x == 0) sums[0] = sums[1] = sums[2] = 0;
-  __syncthreads();
+  __shared__ unsigned long long sums[32][2];       // a warp's units by rows, by chunks
+  unsigned long long by_rows = 0, by_chunks = 0;
   for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
     const QuantSeq s = quant_seq(a, b);
     if (!many_rows(a, s)) continue;
     const unsigned long long rows = (unsigned long long)s.n * a.group, blocks = (s.len + kQuantBlock - 1) / kQuantBlock;
-    atomicAdd(&sums[0], (rows + 7) / 8 * blocks * a.g.n_kv_heads);
-    atomicAdd(&sums[1], (rows + 255) / 256 * blocks * a.g.n_kv_heads);
-    atomicMax(&sums[2], blocks);
+    by_rows += (rows + 7) / 8 * blocks * a.g.n_kv_heads;
+    by_chunks += (rows + 255) / 256 * (blocks + 8 * kCkItemCost) * a.g.n_kv_heads;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    by_rows += __shfl_xor_sync(0xffffffffu, by_rows, o);
+    by_chunks += __shfl_xor_sync(0xffffffffu, by_chunks, o);
+  }
+  if ((threadIdx.x & 31) == 0) {
+    sums[threadIdx.x >> 5][0] = by_rows;
+    sums[threadIdx.x >> 5][1] = by_chunks;
   }
   __syncthreads();
-  const unsigned long long longest = sums[1] / sm_count > sums[2] ? sums[1] / sm_count : sums[2];
-  return sums[0] > kChunkUnits * longest;
+  by_rows = by_chunks = 0;
+#pragma unroll 1
+  for (unsigned w = 0; w < blockDim.x / 32; ++w) {
+    by_rows += sums[w][0];
+    by_chunks += sums[w][1];
+  }
+  return 10 * by_rows > 1400ull * sm_count + 33 * by_chunks;
 }
 
 __device__ __forceinline__ float exp2_approx(float x) {

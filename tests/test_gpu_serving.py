@@ -507,6 +507,92 @@ def test_many_chunks_of_few_rows(n_q, n_kv, d, new):
         assert (err <= tol).all(), (b, new[b], float((err / tol).max()))
 
 
+@pytest.mark.parametrize("opts", [{}, dict(softcap=8.0), dict(softcap=20.0, slopes=True, prefix=True)])
+@pytest.mark.parametrize("fmt,d,page,n_q,n_kv,before,new", [
+    ("int8", 128, 64, 32, 8, [6000], [64]), ("e4m3", 64, 16, 8, 1, [9001, 0, 40], [129, 0, 1]), ("int8", 128, 128, 4, 4, [3, 5007], [1, 301])])
+def test_chunk_of_few_items_is_split_along_the_keys(opts, fmt, d, page, n_q, n_kv, before, new):
+    """Fewer items than SMs over long caches: each is cut into parts of a few key tiles, the last ones masked, and joined."""
+    B = len(new)
+    cfg = config(n_q=n_q, n_kv=n_kv, d=d, page=page, batch=B, pages=9216 // page, n_pages=B * 9216 // page)
+    p = Program(cfg, fmt, seed=n_q + 3 * d)
+    p.step(before)
+    p.step(new)
+    kw = dict(opts)
+    if "slopes" in kw:
+        kw["slopes"] = [2.0 ** (-8.0 * (h + 1) / n_q) for h in range(n_q)]
+    if "prefix" in kw:
+        kw["prefix"] = [max(0, n + o - 20) for n, o in zip(new, before)]
+    q = p.rows(sum(new), n_q, 2.5)
+    out = attend(p, new, q, **dict(kw))
+    assert torch.equal(out, attend(p, new, q, **dict(kw)))
+    check_attention(p, new, q, out, softcap=kw.get("softcap", 0.0), slopes=kw.get("slopes"), prefix=kw.get("prefix"))
+    assert p.status.item() == 0
+
+
+def test_nan_in_one_part_of_a_split_chunk():
+    cfg = config(n_q=8, n_kv=2, d=128, page=64, batch=1, pages=128, n_pages=128)
+    p = Program(cfg, "int8", seed=16)
+    k, v = p.rows(8000, 2), p.rows(8000, 2)
+    v[4321, 0, 77] = float("nan")                        # seen by every row of head 0's group
+    k[7990, 1, 5] = float("inf")                         # a block that only the last rows of head 1's group see
+    p.step([8000], k, v)
+    q = p.rows(500, 8, 2.0)
+    out = f64(attend(p, [500], q))
+    pos = np.arange(7500, 8000)
+    bad = np.isnan(out).any(-1)
+    assert bad[:, :4].all() and (bad[:, 4:] == (pos >= 7984)[:, None]).all()
+
+
+@pytest.mark.parametrize("opts", [{}, dict(softcap=8.0, prefix=True)])
+def test_many_chunks_of_few_rows_over_longer_caches(opts):
+    """Several items per CTA, whole and cut ones, most with one tile of query rows; bad sequences and sequences of the row kernel
+    between them; captured and replayed over what another call left in the workspace."""
+    new = [16, 70, 1, 0, 16, 16, 90, 16] * 9
+    B, n_q, n_kv, d = len(new), 16, 4, 64
+    cfg = config(n_q=n_q, n_kv=n_kv, d=d, page=64, batch=B, pages=16, n_pages=16 * B)
+    p = Program(cfg, "e4m3", seed=22)
+    before = [int(x) for x in p.rng.integers(600, 900, B)]
+    p.step(before)
+    p.step(new)
+    kw = dict(opts)
+    if "prefix" in kw:
+        kw["prefix"] = [int(x) for x in p.rng.integers(0, 1000, B)]
+    q = p.rows(sum(new), n_q, 2.0)
+    out = attend(p, new, q, **dict(kw))
+    assert p.status.item() == 0
+    at = np.concatenate([[0], np.cumsum(new)])
+    for b in sorted({0, 1, 2, 6, B // 3, B // 2, B - 2, B - 1}):
+        k, v = p.ref.values(p.ref.k[b]), p.ref.values(p.ref.v[b])
+        ref, size = R.attend(f64(q[at[b]:at[b + 1]]), k, v, d ** -0.5, kw.get("softcap", 0.0), None, kw["prefix"][b] if "prefix" in kw else 0)
+        tol = R.tolerance(ref, size, p.lens[b], EPS["bf16"], True, new[b] * n_q // n_kv >= CHUNK_ROWS, kw.get("softcap", 0.0))
+        err = np.abs(f64(out[at[b]:at[b + 1]]) - ref)
+        assert (err <= tol).all(), (b, new[b], float((err / tol).max()))
+    # two sequences whose slots do not exist: zeros there, the others as they were
+    lens, slots, cu = dev(p.lens[:B]), dev(p.slots[:B]), dev(at)
+    slots[5], slots[9] = -1, B
+    extra = dict(softcap=kw.get("softcap", 0.0), prefix_lens=dev(kw["prefix"]) if "prefix" in kw else None)
+    bad = torch.empty_like(out)
+    call = lambda: p.cache.attention(q, p.table, lens, cu_tokens=cu, max_new=90, seq_slots=slots, status=p.status, out=bad, **extra)
+    call()
+    assert p.status.item() != 0
+    keep = torch.ones(len(q), dtype=torch.bool, device="cuda")
+    for b in (5, 9):
+        keep[at[b]:at[b + 1]] = False
+        assert (bad[at[b]:at[b + 1]] == 0).all()
+    want = bad.clone()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    p.cache.workspace.fill_(0xff)
+    for _ in range(2):
+        bad.fill_(7)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(bad, want)
+    assert torch.isfinite(out).all() and torch.isfinite(bad).all()
+
+
 def test_one_long_sequence_is_split_over_the_machine():
     cfg = config(n_q=4, n_kv=1, d=128, page=16, batch=1, pages=2000, n_pages=2100)
     p = Program(cfg, "int8", seed=5)
