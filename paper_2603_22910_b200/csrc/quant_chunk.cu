@@ -214,23 +214,34 @@ __device__ __noinline__ float2 careful_piece(const CkRow w, const int c, const i
   tmem_ld32_issue(w.s_addr + 32 * c, sr);
   tmem_ld_wait();
 #pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    float y = __uint_as_float(sr[j]) * (j < 16 ? f0 : f1);
-    if (w.capped) y = w.cap_out * tanh_f32(y * w.cap_in);
-    if (w.biased) y -= w.slope2 * fabsf((float)(w.pos - key0 - j));
-    sr[j] = __float_as_uint(32 * c + j < n_vis ? y : -INFINITY);
+  for (int j = 0; j < 32; ++j) sr[j] = __float_as_uint(__uint_as_float(sr[j]) * (j < 16 ? f0 : f1));
+  // (a loop for each transform: branches inside one loop cost 2 us a piece)
+  if (w.capped) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) sr[j] = __float_as_uint(w.cap_out * tanh_f32(__uint_as_float(sr[j]) * w.cap_in));
+  }
+  if (w.biased) {
+    const float d = (float)(w.pos - key0);         // (exact up to 2^24 keys, as the distances themselves)
+#pragma unroll
+    for (int j = 0; j < 32; ++j) sr[j] = __float_as_uint(__uint_as_float(sr[j]) - w.slope2 * fabsf(d - j));
+  }
+  const int vis_c = n_vis - 32 * c;
+  if (__any_sync(0xffffffffu, vis_c < 32)) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) sr[j] = j < vis_c ? sr[j] : 0xff800000u;
   }
   float sum = 0.f;
 #pragma unroll 1
   for (int attempt = 0;; ++attempt) {
     const float m = m_ref == -INFINITY ? 0.f : m_ref;
-    sum = 0.f;
+    float sums[2] = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
       const float p0 = exp2_approx(__uint_as_float(sr[2 * j]) - m), p1 = exp2_approx(__uint_as_float(sr[2 * j + 1]) - m);
-      sum += p0 + p1;
+      sums[j & 1] += p0 + p1;
       pk[j] = h2(p0, p1);
     }
+    sum = sums[0] + sums[1];
     const bool move = !(sum < kCkSumLimit) || m_ref == -INFINITY;
     if (attempt > 0 || !__any_sync(0xffffffffu, move)) break;
     float alpha = 1.f;
