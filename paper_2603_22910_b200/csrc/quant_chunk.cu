@@ -10,6 +10,8 @@
 //                    row, 2^(s - ref), a whole number that moves only when 32 probabilities could leave fp16's range: the
 //                    common piece is done in one pass without looking for its maximum.  When it moves, what the row has so far --
 //                    its sum, its output, the probabilities of this tile already stored -- is scaled by a power of two.
+//                    (Two threads per row: 436 against 383 us when the whole took that; asking for the next 32 scores before
+//                    the present ones are done: 481 against 435.)
 //   warps 8-14       conversion: codes of the next tile are on their way in registers while the present one is turned into fp16 and
 //                    stored in the 128-byte swizzle (key tiles K-major, value tiles as stored, N-major).  Eight lanes of a
 //                    warp keep the pages and scales of the tile's eight blocks.
@@ -17,8 +19,14 @@
 //                    over the first half of S_x.
 // Tensor memory: S_0 | S_1 | O_0 | O_1.  The K scale multiplies the score beside the row's own factor (one value per 16 columns);
 // V codes times (their scale / the largest scale the row can see) times 64 are below 2^15.
-// Bound: 128 exponentials per row and tile at 16 per clock and SM take twice the products' time.
-// Work items are dealt out by CTA number, those with the most keys first; every wait is bounded.
+// Work: the key tiles of all items, with a cost of 4 tiles to each item, are laid end to end and cut into equal shares, one per CTA.
+// A share cuts at most two items; the parts of an item -- o / l, reference, l -- go to the workspace and a second kernel
+// joins them in the order of their keys.  (2 x 1024 tokens over 8192 keys, 256 items for 148 SMs: 433 -> 393 us; one sequence of 64
+// tokens over 32768 keys, 8 items: 630 -> 87 us.)  Every wait is bounded.
+// Bound: 128 exponentials per row and tile at 16 per clock and SM take twice the products' time.  Measured (2 x 1024 tokens over
+// 8192 keys, 32 / 8 heads, e4m3): 297 us = 868 TFLOP/s without a cap, 380 us = 680 with one; a tile of 128 keys takes both halves 2.4 us
+// where its products take 0.55 and its exponentials 1.1: each half's scores -> probabilities -> products chain is longer
+// than what the other half covers.  Tensor pipe 38 / 30 %, exponentials' pipe 39 / 31 %, issue slots 43 / 49 % busy.
 #include <type_traits>
 
 #include "quant_common.cuh"
