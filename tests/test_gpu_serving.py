@@ -593,6 +593,30 @@ def test_many_chunks_of_few_rows_over_longer_caches(opts):
     assert torch.isfinite(out).all() and torch.isfinite(bad).all()
 
 
+def test_more_sequences_than_threads_with_chunks_among_them():
+    """640 sequences, every tenth a chunk over a longer cache, the others one token; query rows inside a wider tensor."""
+    B, n_q, n_kv, d = 640, 16, 8, 64
+    new = [16 + b % 7 if b % 10 == 3 else b % 3 % 2 for b in range(B)]
+    cfg = config(n_q=n_q, n_kv=n_kv, d=d, page=64, batch=B, pages=20, n_pages=64 * 20 + 640)
+    p = Program(cfg, "int8", seed=29)
+    before = [int(p.rng.integers(900, 1200)) if b % 10 == 3 else b % 40 for b in range(B)]
+    p.step(before)
+    new = [40 + n if n >= 16 else n for n in new]
+    p.step(new)
+    q = p.rows(sum(new), n_q + 2 * n_kv, 2.0)[:, :n_q]
+    out = attend(p, new, q)
+    assert p.status.item() == 0 and torch.isfinite(out).all()
+    at = np.concatenate([[0], np.cumsum(new)])
+    for b in (3, 4, 13, 313, 316, 633, 637):
+        if new[b] == 0:
+            continue
+        k, v = p.ref.values(p.ref.k[b]), p.ref.values(p.ref.v[b])
+        ref, size = R.attend(f64(q[at[b]:at[b + 1]]), k, v, d ** -0.5)
+        tol = R.tolerance(ref, size, p.lens[b], EPS["bf16"], True, new[b] * n_q // n_kv >= CHUNK_ROWS)
+        err = np.abs(f64(out[at[b]:at[b + 1]]) - ref)
+        assert (err <= tol).all(), (b, new[b], float((err / tol).max()))
+
+
 def test_one_long_sequence_is_split_over_the_machine():
     cfg = config(n_q=4, n_kv=1, d=128, page=16, batch=1, pages=2000, n_pages=2100)
     p = Program(cfg, "int8", seed=5)
