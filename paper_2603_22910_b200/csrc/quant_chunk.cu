@@ -653,12 +653,13 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           ks_next = g.scales[0][at];
         }
       };
-      // codes of this thread's pieces, fetched one tile ahead (rows behind the last block of codes: page 0's, not looked at)
+      // codes of this thread's pieces, fetched one tile ahead: K's when the present tile's K has been converted, so that they are on
+      // their way while V is, and the other way round (rows behind the last block of codes: page 0's, not looked at)
       uint4 kc[NP], vc[NP];
+      uint32_t at[NP];
       const unsigned char* k_base = g.codes[0] + 16 * my_piece;
       const unsigned char* v_base = g.codes[1] + 16 * my_piece;
-      const auto fetch = [&](int tile, int page8) {
-        uint32_t at[NP];
+      const auto fetch_k = [&](int tile, int page8) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
           const int row = min(my_row + kRowStep * p, kCkTile - 1);
@@ -667,6 +668,8 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         }
 #pragma unroll
         for (int p = 0; p < NP; ++p) kc[p] = *reinterpret_cast<const uint4*>(k_base + (size_t)at[p] * D);
+      };
+      const auto fetch_v = [&] {
 #pragma unroll
         for (int p = 0; p < NP; ++p) vc[p] = *reinterpret_cast<const uint4*>(v_base + (size_t)at[p] * D);
       };
@@ -683,7 +686,8 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       };
       int page8 = checked(ask_page(it.t0)), page8_next = ask_page(it.t0 + 1);
       load_scales(it.t0, page8);
-      fetch(it.t0, page8);
+      fetch_k(it.t0, page8);
+      fetch_v();
       // the largest V scale in these tiles, and the largest magnitudes of the open block
       float v_top = 0.f;
       for (int blk = 8 * it.t0 + ct; blk < min(n_codes, 8 * it.t1); blk += kCkConvThreads) v_top = fmaxf(v_top, g.scales[1][scale_at(blk, page_of(blk * kQuantBlock))]);
@@ -759,6 +763,12 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         }
         fence_proxy_async_smem();
         warp_arrive(&t.k_full[st]);
+        if (tile + 1 < it.t1) {
+          page8 = checked(page8_next);
+          page8_next = ask_page(tile + 2);
+          load_scales(tile + 1, page8);
+          fetch_k(tile + 1, page8);
+        }
 
         alive = __all_sync(0xffffffffu, ck_wait(&t.v_empty[st], parity, abort_flag, a.status));
         if (!alive) break;
@@ -788,12 +798,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         }
         fence_proxy_async_smem();
         warp_arrive(&t.v_full[st]);
-        if (tile + 1 < it.t1) {
-          page8 = checked(page8_next);
-          page8_next = ask_page(tile + 2);
-          load_scales(tile + 1, page8);
-          fetch(tile + 1, page8);
-        }
+        if (tile + 1 < it.t1) fetch_v();
       }
     }
   } else {
