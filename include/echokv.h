@@ -478,7 +478,7 @@ typedef struct {
  *  - n_tokens: at most 2^27 (EINVAL; also echokv_quant_append's).  dev_cu_tokens: [B + 1], or NULL for one token per
  *    sequence (n_tokens = B).  max_new: an upper bound of the tokens
  *    any sequence has in this call (1 for a decode step): it selects the kernels.
- *  - workspace: device buffer of echokv_quant_sizes.workspace_bytes, 256-byte aligned.  Calls that share one must
+ *  - workspace: device buffer of echokv_quant_sizes.workspace_bytes (bf16, head_dim 128: 42 MB), 256-byte aligned.  Calls that share one must
  *    not overlap on the device (captured graphs may share it if they run one after the other); nothing is kept in it.
  *  - rows of out behind the last sequence's are left as they were.  A sequence without new tokens has no output.
  * A sequence with a bad slot, a length beyond its capacity or shorter than its new tokens, or more than max_new new
@@ -487,8 +487,8 @@ typedef struct {
  * Scores and sums are fp32; codes enter the products exactly; bf16 queries as fp16 (exact around each row's power of two) with
  * probabilities rounded to fp16, fp32 queries and their probabilities as pairs of fp16 (22 bits).  For a bf16 sequence
  * with 64 query rows per KV head or more (its new tokens times n_q_heads / n_kv_heads) the values may be rounded to fp16 as
- * well, in units of the largest value scale that 256 neighbouring rows see (large batches of such sequences run on the
- * tcgen05 kernel). */
+ * well, in units of the largest value scale that 256 neighbouring rows see (such sequences run on the
+ * tcgen05 kernel where that is the faster one, by their lengths). */
 int echokv_quant_attention(const echokv_config* cfg, const echokv_quant_cache* cache, const echokv_score_options* options,
                            const void* q, int64_t q_stride, void* out, const int32_t* dev_block_table,
                            const int32_t* dev_seq_slots, const int32_t* dev_seq_lens, const int32_t* dev_cu_tokens, int B,
