@@ -548,8 +548,8 @@ def query_quant_sizes(cfg: echokv_config) -> echokv_quant_sizes:
 class QuantCache:
     """One layer's cache in 8 bits: codes int8 or float8_e4m3fn [n_pages][n_kv_heads][page_tokens][d], a scale for each 16 tokens
     and head [n_pages][n_kv_heads][page_tokens / 16], and the open blocks' rows in the storage type [max_batch][n_kv_heads][16][d].
-    Allocates them unless they are given; `workspace` may be shared by the layers of a model (calls that share one must not
-    overlap on the device)."""
+    Allocates them unless they are given; `workspace` (42 MB in bf16 with heads of 128) is best shared by the layers of a model
+    (calls that share one must not overlap on the device)."""
 
     def __init__(self, cfg: echokv_config, fmt: str, k_codes=None, v_codes=None, k_scales=None, v_scales=None, k_tail=None,
                  v_tail=None, workspace=None):

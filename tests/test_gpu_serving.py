@@ -593,6 +593,47 @@ def test_many_chunks_of_few_rows_over_longer_caches(opts):
     assert torch.isfinite(out).all() and torch.isfinite(bad).all()
 
 
+def test_chunk_calls_with_bad_lengths_spare_rows_and_two_streams():
+    """Sequences over max_new or shorter than their new tokens are zeros, rows behind the last sequence stay, the others as they should
+    be; two calls on two streams, each with a workspace of its own, do not disturb each other."""
+    cfg = config(n_q=16, n_kv=8, d=128, page=64, batch=6, pages=40, n_pages=240)
+    p = Program(cfg, "int8", seed=41)
+    p.step([2000, 1800, 900, 1500, 30, 2200])
+    new = [150, 90, 260, 129, 64, 1]
+    p.step(new)
+    q = p.rows(sum(new) + 9, 16, 2.0)
+    good = attend(p, new, q[:sum(new)])
+    check_attention(p, new, q, good)
+    at = np.concatenate([[0], np.cumsum(new)])
+    lens = dev(p.lens[:6])
+    lens[4] = 63
+    call = dict(cu_tokens=dev(at), max_new=200, seq_slots=dev(p.slots[:6]))
+    out = torch.full_like(q, 7.0)
+    p.cache.attention(q, p.table, lens, out=out, status=p.status, **call)
+    assert p.status.item() != 0
+    for b in (2, 4):
+        assert (out[at[b]:at[b + 1]] == 0).all()
+        out[at[b]:at[b + 1]] = good[at[b]:at[b + 1]]
+    check_attention(p, new, q, out[:sum(new)])
+    assert (out[at[-1]:] == 7).all()
+    p.status.zero_()
+    other = binding.QuantCache(cfg, "int8", k_codes=p.cache.k_codes, v_codes=p.cache.v_codes, k_scales=p.cache.k_scales,
+                               v_scales=p.cache.v_scales, k_tail=p.cache.k_tail, v_tail=p.cache.v_tail)
+    q = q[:sum(new)]
+    call = dict(cu_tokens=dev(at), max_new=260, seq_slots=dev(p.slots[:6]))
+    lens = dev(p.lens[:6])
+    want = p.cache.attention(q, p.table, lens, status=p.status, **call)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    outs = []
+    for _ in range(8):
+        for st, c in zip(streams, (p.cache, other)):
+            with torch.cuda.stream(st):
+                outs.append(c.attention(q, p.table, lens, status=p.status, **call))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs) and p.status.item() == 0
+
+
 def test_more_sequences_than_threads_with_chunks_among_them():
     """640 sequences, every tenth a chunk over a longer cache, the others one token; query rows inside a wider tensor."""
     B, n_q, n_kv, d = 640, 16, 8, 64
