@@ -485,7 +485,8 @@ typedef struct {
  * tokens: zeros and the device status (EBADPAGE, EBADLENGTH); offsets that decrease or pass n_tokens: EBADLENGTH, nothing is
  * written for that sequence.  A page id outside the pool: EBADPAGE, the output of its sequence is unspecified.
  * Scores and sums are fp32; codes enter the products exactly; bf16 queries as fp16 (exact around each row's power of two) with
- * probabilities rounded to fp16, fp32 queries and their probabilities as pairs of fp16 (22 bits).  For a bf16 sequence
+ * probabilities rounded to fp16 (one below 2^-24 of its row's largest may count as 0 beside it), fp32 queries and their
+ * probabilities as pairs of fp16 (22 bits).  For a bf16 sequence
  * with 64 query rows per KV head or more (its new tokens times n_q_heads / n_kv_heads) the values may be rounded to fp16 as
  * well, in units of the largest value scale that 256 neighbouring rows see (such sequences run on the
  * tcgen05 kernel where that is the faster one, by their lengths). */

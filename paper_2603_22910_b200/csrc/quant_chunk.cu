@@ -43,9 +43,14 @@ constexpr int kCkSoftmaxThreads = 256, kCkConvThreads = 224;
 constexpr int kCkThreads = kCkSoftmaxThreads + kCkConvThreads + 32;
 constexpr int kCkChunkBytes = kCkTile * 128;       // [128 rows x 64 features] fp16, 128-byte swizzle
 constexpr int kCkRing = 4;                         // scales and V references: see where they are written
-constexpr float kCkMargin = 8.f;                   // a reference that moves goes 2^8 above the largest score: what comes may be 2^23 larger
-                                                   // before it moves again, and fp16 still holds the largest probability's 2^-17
-constexpr float kCkSumLimit = 32768.f;             // a row's 32 probabilities sum to less: each fits fp16
+// A reference that moves goes 2^r below the largest score the row has seen, so that its largest probability is above 2^(r - 1).  What
+// is less than 2^-25 is 0 as fp16, while the sum (fp32) keeps it: over n keys up to n 2^-(24 + r) of the largest one's mass.  r =
+// log2 n - 13 holds that to 2^-11, what rounding a probability to fp16 does (up to r = 8, 2 million keys); r is 0 at least, which leaves
+// room for a sum 2^11 to 2^16 as large before the reference moves again.  Measured (2 x 1024 tokens over 8192 keys, scores of spread
+// 2.5): 299 us, 416 with r = 6, 343 if the first reference comes from 32 keys instead of 128.  (References 2^8 ABOVE the scores never move
+// here, 293 us, but with 0.9 of the mass on the first of 8192 keys the output is 6 % off, of 32768 keys half.)
+__device__ __forceinline__ float ck_below(int n_keys) { return (float)min(8, max(0, 32 - __clz(n_keys - 1) - 13)); }
+constexpr float kCkSumLimit = 65504.f;             // a row's 32 probabilities sum to less: each fits fp16
 constexpr float kCkVScale = 64.f;
 constexpr int kCkMaxCtas = 160;                    // (of the workspace's layout)
 constexpr int kCkMinShare = 3;                     // units per CTA at least
@@ -207,7 +212,7 @@ __device__ __forceinline__ void ck_commit(unsigned long long* bar) {
 // What the softmax of a row needs beside its scores.
 struct CkRow {
   uint32_t s_addr, o_addr;                         // tensor memory: scores (and probabilities) of the tile, output so far
-  float c_row, cap_in, cap_out, slope2;
+  float c_row, cap_in, cap_out, slope2, below;
   int capped, biased;
   int pos;
 };
@@ -259,8 +264,8 @@ __device__ __noinline__ float2 careful_piece(const CkRow w, const int c, const i
       float mx = -INFINITY;
 #pragma unroll
       for (int j = 0; j < 32; ++j) mx = fmaxf(mx, __uint_as_float(sr[j]));
-      if (mx > m_ref - kCkMargin) {
-        const float m_new = ceilf(mx) + kCkMargin;
+      if (mx > m_ref + w.below) {
+        const float m_new = ceilf(mx) - w.below;
         if (m_ref > -INFINITY) alpha = exp2_approx(m_ref - m_new);
         m_ref = m_new;
       }
@@ -890,6 +895,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       CkRow w;
       w.s_addr = s_addr; w.o_addr = o_addr;
       w.c_row = c_row; w.cap_in = cap_in; w.cap_out = cap_out; w.slope2 = slope2;
+      w.below = ck_below(it.kv_end);
       w.capped = a.softcap > 0.f; w.biased = a.slopes != nullptr;
       w.pos = pos;
       // the reference (-inf until the row has seen a key) and the sum of the row's probabilities
@@ -960,19 +966,23 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         };
         const bool full = __all_sync(0xffffffffu, n_vis == kCkTile);
         if (!w.biased && full && tile == it.t0) {
-          // the first reference: what the first 32 keys ask for (capped scores are at most the uncapped ones, and the cap)
-          uint32_t sr[32];
-          tmem_ld32_issue(s_addr, sr);
-          tmem_ld_wait();
-          float mx0 = -INFINITY, mx1 = -INFINITY;
+          // the first reference: what the tile's 128 keys ask for (capped scores are at most the uncapped ones, and the cap)
+          float mx = -INFINITY;
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            uint32_t sr[32];
+            tmem_ld32_issue(s_addr + 32 * c, sr);
+            tmem_ld_wait();
+            float mx0 = -INFINITY, mx1 = -INFINITY;
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            mx0 = fmaxf(mx0, __uint_as_float(sr[j]));
-            mx1 = fmaxf(mx1, __uint_as_float(sr[16 + j]));
+            for (int j = 0; j < 16; ++j) {
+              mx0 = fmaxf(mx0, __uint_as_float(sr[j]));
+              mx1 = fmaxf(mx1, __uint_as_float(sr[16 + j]));
+            }
+            mx = fmaxf(mx, fmaxf(mx0 * (c_row * k_scale[2 * c]), mx1 * (c_row * k_scale[2 * c + 1])));
           }
-          float mx = fmaxf(mx0 * (c_row * k_scale[0]), mx1 * (c_row * k_scale[1]));
           if (w.capped) mx = fminf(mx * kLog2e, cap_out);
-          if (mx > -INFINITY) m_ref = ceilf(mx) + kCkMargin;
+          if (mx > -INFINITY) m_ref = ceilf(mx) - w.below;
         }
         int done = 0;
         if (!w.biased) {

@@ -1,0 +1,59 @@
+"""Chunks over the 8-bit cache where the softmax's range matters: a key that holds most of a row's mass, scores near the cap.  All values
+are positive, so that what a sum of probabilities loses cannot hide behind terms that cancel: bounds are relative to the output."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests import serving_ref as R
+from tests.test_gpu_serving import Program, attend, config, dev, f64, sampled
+
+pytestmark = pytest.mark.gpu
+BASE = 0                # the feature that carries the scores' common part
+
+
+def program(rng, L, n, n_q, n_kv, d, fmt, page=64, sigma=0.5, base_k=None):
+    """A sequence of L tokens, the last n of them queries: scores of spread sigma from the features but BASE, where key t holds
+    base_k[t] and every query 16."""
+    cfg = config(n_q=n_q, n_kv=n_kv, d=d, page=page, batch=1, pages=-(-L // page), n_pages=-(-L // page))
+    p = Program(cfg, fmt, seed=L + n)
+    k = rng.standard_normal((L, n_kv, d)).astype(np.float32)
+    v = (1.0 + 0.25 * rng.uniform(-1, 1, (L, n_kv, d))).astype(np.float32)
+    k[..., BASE] = base_k[:, None]
+    q = rng.standard_normal((n, n_q, d)).astype(np.float32) * sigma
+    q[..., BASE] = 16.0
+    v[0] = 2.0 ** -9
+    as_dev = lambda x: torch.tensor(x, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    p.step([L], as_dev(k), as_dev(v))
+    return p, as_dev(q)
+
+
+def check(p, q, out, only, softcap=0.0):
+    """All values are positive, so every relative error of a term is at most that of the output.  2^-8: the output's rounding; 3 2^-11: the
+    probability, its value and the value's scale as fp16; 2^-11: probabilities below fp16's normal numbers (2^-14) are off by up to 2^-25
+    each, the largest is above 2^(r - 1) with 2^r >= L / 2^13, so L of them by less than 2^-11 of it; scores: 2^-19 of sum |q k| scale and 2^-20 of the cap, in numerator and denominator;
+    the sums: 2^-23 for each 16 keys."""
+    n, L, d = q.shape[0], p.lens[0], p.cfg.head_dim
+    ref, size = R.attend(f64(q), p.ref.values(p.ref.k[0]), p.ref.values(p.ref.v[0]), d ** -0.5, softcap, only=only)
+    rel = 2.0 ** -8 + 4 * 2.0 ** -11 + L / 16 * 2.0 ** -23 + 2 * (2.0 ** -19 * size[only, :, :1] + 2.0 ** -20 * softcap)
+    err = np.abs(f64(out)[only] - ref[only]) / ref[only]
+    assert n and np.isfinite(err).all() and (err <= rel * (1 + 2.0 ** -6)).all(), (float((err / rel).max()), float(err.max()))
+
+
+@pytest.mark.parametrize("mass", [0.5, 0.9, 0.99])
+@pytest.mark.parametrize("L,n,n_q,n_kv,d,fmt", [
+    (2048, 200, 8, 4, 64, "int8"), (8192, 96, 4, 1, 128, "e4m3"), (32768, 70, 2, 2, 128, "int8"), (4096, 1900, 32, 32, 64, "int8")])
+@pytest.mark.parametrize("softcap", [0.0, 100.0])
+def test_chunk_whose_first_key_holds_most_of_the_mass(mass, L, n, n_q, n_kv, d, fmt, softcap):
+    """Items cut along the keys, and (last sizes: more items than SMs) whole ones."""
+    rng = np.random.default_rng(L + n)
+    s = math.log(mass / (1 - mass)) + math.log(L) + 0.5 * 0.5 ** 2
+    if softcap:
+        s = softcap * math.atanh(s / softcap)
+    base = np.zeros(L, dtype=np.float32)
+    base[0] = s * math.sqrt(d) / 16.0
+    p, q = program(rng, L, n, n_q, n_kv, d, fmt, base_k=base)
+    out = attend(p, [n], q, **(dict(softcap=softcap) if softcap else {}))
+    assert p.status.item() == 0
+    check(p, q, out, sampled(rng, n)[:12], softcap)
