@@ -966,7 +966,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         };
         const bool full = __all_sync(0xffffffffu, n_vis == kCkTile);
         if (!w.biased && full && tile == it.t0) {
-          // the first reference: what the tile's 128 keys ask for (capped scores are at most the uncapped ones, and the cap)
+          // the first reference: what the tile's 128 keys ask for (the capped scores' largest is the largest score's)
           float mx = -INFINITY;
 #pragma unroll 1
           for (int c = 0; c < 4; ++c) {
@@ -981,7 +981,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
             }
             mx = fmaxf(mx, fmaxf(mx0 * (c_row * k_scale[2 * c]), mx1 * (c_row * k_scale[2 * c + 1])));
           }
-          if (w.capped) mx = fminf(mx * kLog2e, cap_out);
+          if (w.capped) mx = cap_out * tanh_f32(mx * cap_in);
           if (mx > -INFINITY) m_ref = ceilf(mx) - w.below;
         }
         int done = 0;

@@ -57,3 +57,15 @@ def test_chunk_whose_first_key_holds_most_of_the_mass(mass, L, n, n_q, n_kv, d, 
     out = attend(p, [n], q, **(dict(softcap=softcap) if softcap else {}))
     assert p.status.item() == 0
     check(p, q, out, sampled(rng, n)[:12], softcap)
+
+
+@pytest.mark.parametrize("softcap,ratio", [(30.0, 0.7), (50.0, 0.9), (50.0, 1.2), (100.0, 1.0), (50.0, -1.1), (5.0, 4.0)])
+@pytest.mark.parametrize("L,n,n_q,n_kv,d,fmt", [(8192, 96, 4, 1, 128, "int8"), (2048, 1200, 32, 32, 64, "e4m3"), (2048, 300, 8, 2, 128, "int8")])
+def test_chunk_whose_scores_are_near_the_cap(softcap, ratio, L, n, n_q, n_kv, d, fmt):
+    """Every score is about ratio times the cap, so the capped one is far below both."""
+    rng = np.random.default_rng(n)
+    base = np.full(L, softcap * ratio * math.sqrt(d) / 16.0, dtype=np.float32)
+    p, q = program(rng, L, n, n_q, n_kv, d, fmt, base_k=base, sigma=2.0)
+    out = attend(p, [n], q, softcap=softcap)
+    assert p.status.item() == 0
+    check(p, q, out, sampled(rng, n)[:12], softcap)
