@@ -454,7 +454,8 @@ int echokv_query_quant_sizes(const echokv_config* cfg, echokv_quant_sizes* out);
  * quantised, from the tail rows of its earlier tokens and the new ones; tokens of a block that stays open go to the tail.
  * The tokens of a sequence must be appended in order of position, each call beginning where the cache ends (a token
  * of the open block may be appended again); a sequence may appear once per call.
- * Bad row, sequence or slot -> device status EBADPAGE, that token is skipped. */
+ * Bad row, sequence or slot -> device status EBADPAGE, that token is skipped.  Skipped tokens may lie anywhere among a sequence's:
+ * the others, whose rows follow one another, are held as if they had come alone. */
 int echokv_quant_append(const echokv_config* cfg, const echokv_quant_cache* cache, const void* k_new, int64_t k_stride,
                         const void* v_new, int64_t v_stride, const int64_t* dev_slot_map,
                         const int32_t* dev_token_seqs, const int32_t* dev_cu_tokens, const int32_t* dev_seq_slots, int B,
