@@ -21,9 +21,9 @@
 //   softmax  The running maximum is a reference that moves only when a score is 2^8 above it: the common path compares and votes,
 //            without a reduction over the tokens.
 //   scales   The K scale multiplies the score, the V scale the probability.  fp16's range is kept by references that are powers of
-//            two: one per query row, one per warp for the V scales, which moves with the maximum's.
+//            two: two per query row, one of them for the V scales that the row sees, which moves with the maximum's.
 //   tail     The open block is in the storage type: bf16 rows are operands of the bf16 product as they are, fp32 rows become pairs of
-//            fp16 around their own power of two.  It is attended first, while the first copies are on their way.
+//            fp16, each token's around its own power of two.  It is attended first, while the first copies are on their way.
 // Measured: 16 sequences over 32768 keys (1.07 GB of codes) 177 us, 6.1 TB/s; 32 ragged ones with capped scores, e4m3, 168 us,
 // 6.0 TB/s; one token over 777 keys 12.5 us, all latency (this kernel 7.5, the second one 3, launches).
 // (Rings filled by cp.async: 4.4 TB/s.  Warps x stages, first case: 12 x 3 177 us, 10 x 4 193, 8 x 4 192, 16 x 2 225.)
@@ -44,7 +44,8 @@ constexpr int kQaItemCost = 6;                     // what an item costs beside 
                                                   // blocks: units are dealt out as if an item began with that many more
 constexpr int kQaMinShare = 2 * kQaWarps;         // units per CTA at least
 constexpr float kQaGrow = 8.f;                    // the references move when a score is 2^8 above them
-constexpr float kQaPScale = 32.f;                 // P <= 2^8 times a scale ratio < 2 times 2^5: below 2^15
+constexpr float kQaPScale = 32.f;                 // P <= 2^8 times a scale ratio <= 1 times 2^5: 2^13 at most
+constexpr int kQaLeastExp = 27;                   // references of V scales are 2^-100 or more, as the scales are
 
 struct QaDesc {                                   // an item cut at the end of CTA g's share
   int n_parts;                                    // CTAs that hold parts of it (0: none starts here)
@@ -413,8 +414,9 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     // Per query row: the reference of its maximum (0 until it has seen a key, which the first one seen moves), and how far
     // above the reference a score may be before that moves.
     float m_ref[2] = {0.f, 0.f}, grow[2] = {-3.0e38f, -3.0e38f}, l_run[2] = {0.f, 0.f};
-    // the V scales' reference; negative: none yet, and the output in units of 1
-    float v_ref = -kQaPScale, v_inv = 0.f;
+    // the reference of the V scales that the row sees (negative: none yet, and the output in units of 1), kQaPScale / it; the smaller
+    // one of the two rows
+    float v_ref[2] = {-kQaPScale, -kQaPScale}, v_inv[2] = {0.f, 0.f}, v_low = -kQaPScale;
     const int pos_first = len - n_new + (tile * kQaRows >> a.group_shift);     // the tile's first query: blocks up to it are seen whole
 
     // a scaled product q . k of token tok and query row 2 c + e -> the score in base-2 units
@@ -430,6 +432,11 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     const auto softmax_blocks = [&](bool masked, int tok0, int tok_end, float (&sc)[NB][4], const float (&k_scale)[NB], const float (&v_scale)[NB],
                                     uint32_t (&ph)[NB][2], uint32_t (&pl)[NB][2]) {
       bool above = false;
+      // the V scale where the row sees some of the block
+      const auto seen_scale = [&](int n, int e) {
+        const int tok = tok0 + n * kQuantBlock;
+        return !masked || (tok < tok_end && (tok <= pos[e] || tok < prefix)) ? v_scale[n] : -INFINITY;
+      };
       // x - m_ref, in base-2 units
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
@@ -451,7 +458,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) above |= sc[n][i] > grow[i & 1];
-        above |= v_scale[n] > v_ref;
+        above |= v_scale[n] > v_low;
       }
       if (__any_sync(0xffffffffu, above)) {
         float alpha[2];
@@ -476,18 +483,19 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
             }
           }
         }
-        float v_top = v_scale[0];
 #pragma unroll
-        for (int n = 1; n < NB; ++n) v_top = fmaxf(v_top, v_scale[n]);
-        if (v_top > v_ref) {
-          // the power of two above the scale
-          const uint32_t e = (__float_as_uint(v_top) >> 23) + 1;
-          const float old = fabsf(v_ref);
-          v_ref = __uint_as_float(e << 23);
-          v_inv = __uint_as_float((254 - e) << 23);
-          alpha[0] *= old * v_inv;
-          alpha[1] *= old * v_inv;
+        for (int e = 0; e < 2; ++e) {
+          const float v_top = fmaxf(seen_scale(0, e), seen_scale(1, e));
+          if (v_top > v_ref[e]) {
+            // the power of two above the scale
+            const int ex = max((int)(__float_as_uint(v_top) >> 23) + 1, kQaLeastExp);
+            const float old = fabsf(v_ref[e]) * (1.f / kQaPScale);
+            v_ref[e] = __uint_as_float(ex << 23);
+            v_inv[e] = kQaPScale * __uint_as_float((254 - ex) << 23);
+            alpha[e] *= old * v_inv[e];
+          }
         }
+        v_low = fminf(v_ref[0], v_ref[1]);
 #pragma unroll
         for (int j = 0; j < MT; ++j)
 #pragma unroll
@@ -495,13 +503,13 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
       }
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
-        const float pv = v_scale[n] * v_inv * kQaPScale;
+        const float pv[2] = {v_scale[n] * v_inv[0], v_scale[n] * v_inv[1]};
         float p[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           p[i] = exp2_approx(sc[n][i]);
           l_run[i & 1] += p[i];
-          p[i] *= pv;
+          p[i] *= pv[i & 1];
           if (masked && sc[n][i] == -INFINITY) p[i] = 0.f;       // (0 times a scale that is NaN)
         }
 #pragma unroll
@@ -544,23 +552,24 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
       if (!kF32) load_values();                      // (fp32 rows take twice the registers: the values after the scores)
       // A block with an infinity or NaN acts as a block of codes does: its scale is NaN and its values are 0, so that a query
       // that sees none of it is left alone.
-      float sc[4] = {0.f, 0.f, 0.f, 0.f}, k_mul = a.scale * (a.softcap > 0.f ? 1.f : kLog2e), v_mul = 1.f, v_up = 1.f;
-      float f_row[2] = {k_mul, k_mul};
+      float sc[4] = {0.f, 0.f, 0.f, 0.f}, v_mul = 1.f;
+      float f_row[2], f_tok[2] = {1.f, 1.f};         // what the products of query row 2 c + e and token r + 8 t are multiplied by
+      float v_up[4], v_tok[2];                       // fp32: the powers of two of this lane's value rows; 1 / that of tokens r, r + 8
       if constexpr (kF32) {
-        // fp16 pairs around a power of two
-        const auto power = [&](uint32_t top, float* back) {
-          top = __reduce_max_sync(0xffffffffu, Quad<T>::top_bits(top));
-          const float up = scale_up_to_half(__uint_as_float(top), back);
-          if (top >= 0x7f800000u) *back = __uint_as_float(0x7fc00000u);
-          return up;
-        };
-        uint32_t top = 0;
+        // fp16 pairs, each token's around its own power of two: what a query does not see has no part in what it does
+        uint32_t bad = 0;
+        float k_up[2];
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t) {
+          uint32_t top = 0;
 #pragma unroll
           for (int x = 0; x < KS; ++x) top = kq[t][x].top(top);
-        const float k_up = power(top, &k_mul);
-        const bool k_ok = k_mul == k_mul;
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          k_up[t] = scale_up_to_half(__uint_as_float(top), &f_tok[t]);
+          bad |= top >= 0x7f800000u;
+        }
+        const bool k_ok = !__any_sync(0xffffffffu, bad);
 #pragma unroll
         for (int x = 0; x < KS; ++x) {
           HalfPair p[4];                             // tokens r, r + 8; elements 0, 1 and 2, 3
@@ -568,28 +577,35 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
           for (int t = 0; t < 2; ++t) {
             if (!k_ok) kq[t][x].zero();
 #pragma unroll
-            for (int f = 0; f < 2; ++f) p[2 * f + t] = split_pair<true>(kq[t][x].get(2 * f) * k_up, kq[t][x].get(2 * f + 1) * k_up);
+            for (int f = 0; f < 2; ++f) p[2 * f + t] = split_pair<true>(kq[t][x].get(2 * f) * k_up[t], kq[t][x].get(2 * f + 1) * k_up[t]);
           }
           mma_m16n8k16_f16(sc, p[0].hi, p[1].hi, p[2].hi, p[3].hi, qh[x][0], qh[x][1]);
           mma_m16n8k16_f16(sc, p[0].hi, p[1].hi, p[2].hi, p[3].hi, ql[x][0], ql[x][1]);
           mma_m16n8k16_f16(sc, p[0].lo, p[1].lo, p[2].lo, p[3].lo, qh[x][0], qh[x][1]);
         }
-        f_row[0] = c_row[0] * k_mul;
-        f_row[1] = c_row[1] * k_mul;
+        f_row[0] = k_ok ? c_row[0] : __uint_as_float(0x7fc00000u);
+        f_row[1] = k_ok ? c_row[1] : __uint_as_float(0x7fc00000u);
         load_values();
-        top = 0;
+        bad = 0;
+        float back[4];                               // (0 for a row of zeros)
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 4; ++t) {
+          uint32_t top = 0;
 #pragma unroll
           for (int x = 0; x < NT / 4; ++x) top = vq[t][x].top(top);
-        v_up = power(top, &v_mul);
-        // the power of two above the block's
-        if (v_mul > 0.f) {
-          const uint32_t e = (__float_as_uint(v_mul) >> 23) + 1;
-          v_ref = __uint_as_float(e << 23);
-          v_inv = __uint_as_float((254 - e) << 23);
+#pragma unroll
+          for (int w = 4; w < 32; w <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, w));
+          v_up[t] = scale_up_to_half(__uint_as_float(top), &back[t]);
+          if (top < 0x00800000u) back[t] = 0.f;
+          bad |= top >= 0x7f800000u;
         }
-        v_mul = v_mul * v_inv * kQaPScale;
+        if (__any_sync(0xffffffffu, bad)) v_mul = __uint_as_float(0x7fc00000u);
+        // token r is value row r & 1 of lanes r / 2, r + 8 the row two on
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const float even = __shfl_sync(0xffffffffu, back[2 * t], r >> 1), odd = __shfl_sync(0xffffffffu, back[2 * t + 1], r >> 1);
+          v_tok[t] = r & 1 ? odd : even;
+        }
       } else {
         // bf16 rows are operands as they are.  Zero times an element tells whether it is finite.
         uint32_t k_bad = 0, v_bad = 0;
@@ -608,7 +624,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
         for (int t = 0; t < 4; ++t)
 #pragma unroll
           for (int x = 0; x < NT / 4; ++x) v_bad = zero_fma_bf16x2(vq[t][x].w.x, zero_fma_bf16x2(vq[t][x].w.y, v_bad));
-        if (__any_sync(0xffffffffu, (k_bad & 0x7fff7fffu) != 0)) f_row[0] = f_row[1] = __uint_as_float(0x7fc00000u);
+        f_row[0] = f_row[1] = __any_sync(0xffffffffu, (k_bad & 0x7fff7fffu) != 0) ? __uint_as_float(0x7fc00000u) : a.scale * (a.softcap > 0.f ? 1.f : kLog2e);
         if (__any_sync(0xffffffffu, (v_bad & 0x7fff7fffu) != 0)) v_mul = __uint_as_float(0x7fc00000u);
       }
       if (v_mul != v_mul) {
@@ -622,7 +638,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int tok = n_full * kQuantBlock + 8 * (i >> 1) + r;
-        x[i] = tok < len && (tok <= pos[i & 1] || tok < prefix) ? score(sc[i] * f_row[i & 1], i & 1, tok) : -INFINITY;
+        x[i] = tok < len && (tok <= pos[i & 1] || tok < prefix) ? score(sc[i] * (f_row[i & 1] * f_tok[i >> 1]), i & 1, tok) : -INFINITY;
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -636,11 +652,27 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
       }
       uint32_t ph[2], pl[2];
       float p[4];
+      if constexpr (kF32) {
+        // a row's reference: the largest 1 / power of two of the values that it sees
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float top = fmaxf(x[e] == -INFINITY ? 0.f : v_tok[0], x[2 + e] == -INFINITY ? 0.f : v_tok[1]);
+#pragma unroll
+          for (int w = 4; w < 32; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+          if (top > 0.f) {
+            v_ref[e] = fmaxf(top, __uint_as_float(kQaLeastExp << 23));
+            v_inv[e] = kQaPScale * __uint_as_float((254u << 23) - __float_as_uint(v_ref[e]));
+          }
+        }
+        v_low = fminf(v_ref[0], v_ref[1]);
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         p[i] = exp2_approx(x[i] - m_ref[i & 1]);
         l_run[i & 1] += p[i];
-        p[i] = x[i] == -INFINITY ? 0.f : p[i] * v_mul;
+        float m = v_mul;
+        if (kF32) m *= v_tok[i >> 1] * v_inv[i & 1];
+        p[i] = x[i] == -INFINITY ? 0.f : p[i] * m;
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -663,7 +695,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
           for (int e = 0; e < 2; ++e)
 #pragma unroll
             for (int f = 0; f < 2; ++f)
-              w[2 * f + e] = split_pair<true>(vq[2 * f][m / 2].get(2 * (m & 1) + e) * v_up, vq[2 * f + 1][m / 2].get(2 * (m & 1) + e) * v_up);
+              w[2 * f + e] = split_pair<true>(vq[2 * f][m / 2].get(2 * (m & 1) + e) * v_up[2 * f], vq[2 * f + 1][m / 2].get(2 * (m & 1) + e) * v_up[2 * f + 1]);
           mma_pv(o[m], w[0].hi, w[1].hi, w[2].hi, w[3].hi, ph, pl);
           mma_m16n8k16_f16(o[m], w[0].lo, w[1].lo, w[2].lo, w[3].lo, ph[0], ph[1]);
         } else {
@@ -784,14 +816,14 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     for (int e = 0; e < 2; ++e)
 #pragma unroll
       for (int w = 4; w < 32; w <<= 1) l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], w);
-    const float o_scale = fabsf(v_ref) * (1.f / kQaPScale);
+    const float o_scale[2] = {fabsf(v_ref[0]) * (1.f / kQaPScale), fabsf(v_ref[1]) * (1.f / kQaPScale)};
     const bool starts = blk0 == 0, ends = seg_end == item_end;
     if (starts && ends) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int qrow = tile * kQaRows + 2 * c + e;
         if (qrow < n_rows) {
-          const float inv = l_run[e] == 0.f ? 0.f : o_scale / l_run[e];
+          const float inv = l_run[e] == 0.f ? 0.f : o_scale[e] / l_run[e];
           float v[NT];
 #pragma unroll
           for (int j = 0; j < MT; ++j) {
@@ -826,7 +858,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
       for (int e = 0; e < 2; ++e)
 #pragma unroll
         for (int j = 0; j < MT; ++j)
-          *reinterpret_cast<float2*>(dst + (2 * c + e) * D + NT * r + 2 * j) = make_float2(o[j][e] * o_scale, o[j][2 + e] * o_scale);
+          *reinterpret_cast<float2*>(dst + (2 * c + e) * D + NT * r + 2 * j) = make_float2(o[j][e] * o_scale[e], o[j][2 + e] * o_scale[e]);
     }
     u = seg_end;
   }

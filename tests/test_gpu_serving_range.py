@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from tests import serving_ref as R
-from tests.test_gpu_serving import Program, attend, config, dev, f64, sampled
+from tests.test_gpu_serving import Program, attend, check_attention, config, f64, sampled
 
 pytestmark = pytest.mark.gpu
 BASE = 0                # the feature that carries the scores' common part
@@ -69,3 +69,57 @@ def test_chunk_whose_scores_are_near_the_cap(softcap, ratio, L, n, n_q, n_kv, d,
     out = attend(p, [n], q, softcap=softcap)
     assert p.status.item() == 0
     check(p, q, out, sampled(rng, n)[:12], softcap)
+
+
+# ---- decode steps and drafts: values of very different sizes -------------------------------------------------------------
+def values(p, L, H, blocks):
+    """K and V rows of L tokens; V rows from token t on, for (t, size) in blocks, are standard normal times size."""
+    k, v = p.rows(L, H), p.rows(L, H).float()
+    size = torch.zeros(L, device="cuda")
+    for t, s in blocks:
+        size[t:] = s
+    return k, (v * size[:, None, None]).to(k.dtype)
+
+
+@pytest.mark.parametrize("size", [1e-6, 1e-12, 1e-20])
+@pytest.mark.parametrize("d,L", [(128, 53), (64, 700)])
+def test_open_block_of_zero_values_beside_small_ones(d, L, size):
+    cfg = config(n_q=2, n_kv=2, d=d, batch=1, pages=48, n_pages=48, dtype="fp32")
+    p = Program(cfg, "int8", seed=L, dtype="fp32")
+    p.step([L], *values(p, L, 2, [(0, size), (L // 16 * 16, 0.0)]))
+    q = p.rows(1, 2, 2.0)
+    check_attention(p, [1], q, attend(p, [1], q))
+
+
+@pytest.mark.parametrize("d,before,new", [(128, 16, 9), (64, 300, 11), (64, 0, 14)])
+def test_a_large_value_of_the_open_block_that_the_first_drafts_do_not_see(d, before, new):
+    cfg = config(n_q=2, n_kv=2, d=d, batch=1, pages=48, n_pages=48, dtype="fp32")
+    p = Program(cfg, "e4m3", seed=new, dtype="fp32")
+    L = before + new
+    p.step([L], *values(p, L, 2, [(0, 1.0), (L - 2, 1e12), (L - 1, 1e30)]))
+    q = p.rows(new, 2, 2.0)
+    check_attention(p, [new], q, attend(p, [new], q))
+
+
+@pytest.mark.parametrize("dtype,d,n_q,before,new", [("fp32", 128, 2, 8, 40), ("bf16", 128, 2, 8, 40), ("bf16", 64, 8, 294, 10),
+                                                    ("fp32", 64, 4, 24, 24)])
+def test_a_large_value_of_a_block_that_the_first_drafts_do_not_see(dtype, d, n_q, before, new):
+    """The last block of codes holds large values; the queries before it are attended beside it, eight rows at a time."""
+    cfg = config(n_q=n_q, n_kv=2, d=d, batch=1, pages=48, n_pages=48, dtype=dtype)
+    p = Program(cfg, "int8", seed=new, dtype=dtype)
+    L = before + new
+    p.step([L], *values(p, L, 2, [(0, 1.0), (L // 16 * 16 - 16, 1e12), (L // 16 * 16, 1e-12)]))
+    q = p.rows(new, n_q, 2.0)
+    check_attention(p, [new], q, attend(p, [new], q))
+
+
+@pytest.mark.parametrize("kv", [0, 1])
+def test_a_large_key_or_value_of_the_open_block_and_a_prefix(kv):
+    cfg = config(n_q=2, n_kv=2, d=64, batch=1, pages=48, n_pages=48, dtype="fp32")
+    p = Program(cfg, "int8", seed=kv, dtype="fp32")
+    x = [p.rows(78, 2), p.rows(78, 2)]
+    x[kv][77] *= 1e25
+    p.step([78], *x)
+    q = p.rows(12, 2, 2.0)
+    out = attend(p, [12], q, prefix=[70])
+    check_attention(p, [12], q, out, prefix=[70])
