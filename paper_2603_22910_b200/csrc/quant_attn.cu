@@ -483,12 +483,25 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
             }
           }
         }
+        // (the open block's output is in units of 1: a first reference far below it would take it out of fp32's range)
+        int least[2] = {kQaLeastExp, kQaLeastExp};
+        if (!kF32 && n_codes < nb && __any_sync(0xffffffffu, v_low < 0.f)) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < MT; ++j) top = max(top, max(__float_as_uint(o[j][e]) & 0x7fffffffu, __float_as_uint(o[j][2 + e]) & 0x7fffffffu));
+#pragma unroll
+            for (int w = 4; w < 32; w <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, w));
+            if (v_ref[e] < 0.f) least[e] = max(kQaLeastExp, (int)(top >> 23) - 95);      // 2^100 of the reference's units at most
+          }
+        }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const float v_top = fmaxf(seen_scale(0, e), seen_scale(1, e));
           if (v_top > v_ref[e]) {
             // the power of two above the scale
-            const int ex = max((int)(__float_as_uint(v_top) >> 23) + 1, kQaLeastExp);
+            const int ex = max((int)(__float_as_uint(v_top) >> 23) + 1, least[e]);
             const float old = fabsf(v_ref[e]) * (1.f / kQaPScale);
             v_ref[e] = __uint_as_float(ex << 23);
             v_inv[e] = kQaPScale * __uint_as_float((254 - ex) << 23);

@@ -123,3 +123,17 @@ def test_a_large_key_or_value_of_the_open_block_and_a_prefix(kv):
     q = p.rows(12, 2, 2.0)
     out = attend(p, [12], q, prefix=[70])
     check_attention(p, [12], q, out, prefix=[70])
+
+
+@pytest.mark.parametrize("scale", ["as appended", 0.0])
+@pytest.mark.parametrize("dtype,size", [("bf16", 3e7), ("bf16", 1e30), ("bf16", 1.0), ("fp32", 1e30)])
+def test_blocks_of_zero_values_beside_large_ones(dtype, size, scale):
+    """A block of zeros has the scale 2^-100, or 0 if the caller filled the cache so; then ordinary blocks, and the large open block."""
+    cfg = config(n_q=4, n_kv=2, d=128, batch=2, pages=48, n_pages=96, dtype=dtype)
+    p = Program(cfg, "int8", seed=5, dtype=dtype)
+    kv = [values(p, 101, 2, [(96, size)]), values(p, 149, 2, [(32, 1e-3), (64, 0.0), (80, 1.0), (144, size)])]
+    p.step([101, 149], torch.cat([kv[0][0], kv[1][0]]), torch.cat([kv[0][1], kv[1][1]]))
+    if scale == 0.0:
+        p.cache.v_scales[p.cache.v_scales < 1e-29] = 0.0
+    q = p.rows(2, 4, 2.0)
+    check_attention(p, [1, 1], q, attend(p, [1, 1], q))
