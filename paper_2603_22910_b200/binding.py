@@ -7,6 +7,7 @@ loading fails loudly otherwise -- there is no fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import math
 import os
@@ -172,6 +173,18 @@ def _stream_handle(stream) -> int | None:
     return s.cuda_stream or None
 
 
+_CURRENT = contextlib.nullcontext()
+
+
+def _memory_of(stream):
+    """Where new tensors of a call on `stream` (None: the current one) are allocated: in that stream's memory, since the current
+    stream's may still be in use by what is queued there."""
+    if stream is None:
+        return _CURRENT
+    import torch
+    return torch.cuda.stream(stream)
+
+
 def make_config(*, n_layers, n_q_heads, n_kv_heads, head_dim, group_size, n_retained_heads,
                 page_tokens, max_batch, max_pages_per_seq, n_pages, dtype, softmax_scale=0.0,
                 device=0, n_retained_dims=0, save_k=0) -> echokv_config:
@@ -264,7 +277,7 @@ class Context:
                                            _stream_handle(stream)), "echokv_compress_layer")
 
     def decode_attention(self, layer: int, q, seq_lens, out=None, seq_slots=None, stream=None):
-        out = self._out(q) if out is None else out
+        out = self._out(q, stream) if out is None else out
         _check(lib().echokv_decode_attention(self.handle, layer, _ptr(q), _ptr(out), _ptr(seq_slots),
                                              _ptr(seq_lens), q.shape[0], _stream_handle(stream)),
                "echokv_decode_attention")
@@ -278,8 +291,9 @@ class Context:
         if getattr(self, "prefill_scratch", None) is None:
             n = C.c_uint64(0)
             _check(lib().echokv_prefill_scratch_bytes(C.byref(self.cfg), C.byref(n)), "echokv_prefill_scratch_bytes")
-            self.prefill_scratch = self.torch.empty(n.value, dtype=self.torch.uint8, device=self.device)
-        out = self._out(q) if out is None else out
+            with _memory_of(stream):
+                self.prefill_scratch = self.torch.empty(n.value, dtype=self.torch.uint8, device=self.device)
+        out = self._out(q, stream) if out is None else out
         _check(lib().echokv_prefill_attention(self.handle, layer, _ptr(q), _ptr(out), q.shape[1], _ptr(seq_slots),
                                               _ptr(seq_lens), q.shape[0], _ptr(k_recent), _ptr(v_recent),
                                               self.prefill_scratch.data_ptr(),
@@ -288,7 +302,7 @@ class Context:
         return out
 
     def full_attention(self, layer: int, q, seq_lens, out=None, seq_slots=None, stream=None):
-        out = self._out(q) if out is None else out
+        out = self._out(q, stream) if out is None else out
         _check(lib().echokv_full_attention(self.handle, layer, _ptr(q), _ptr(out), _ptr(seq_slots),
                                            _ptr(seq_lens), q.shape[0], _stream_handle(stream)),
                "echokv_full_attention")
@@ -351,7 +365,8 @@ class Context:
             return
         n = C.c_uint64(0)
         _check(lib().echokv_rope_table_bytes(C.byref(self.cfg), C.byref(n)), "echokv_rope_table_bytes")
-        self.rope_table = self.torch.empty(n.value, dtype=self.torch.uint8, device=self.device)
+        with _memory_of(stream):
+            self.rope_table = self.torch.empty(n.value, dtype=self.torch.uint8, device=self.device)
         _check(lib().echokv_set_rope(self.handle, float(theta), self.rope_table.data_ptr(), n.value,
                                      _stream_handle(stream)), "echokv_set_rope")
 
@@ -395,13 +410,15 @@ class Context:
 
     def diag_bounded_wait(self, limit_cycles: int, stream=None):
         """Run the bounded-wait probe; returns the device tensor int32[2] saying how its two warps left."""
-        left = self.torch.zeros(2, dtype=self.torch.int32, device=self.device)
+        with _memory_of(stream):
+            left = self.torch.zeros(2, dtype=self.torch.int32, device=self.device)
         _check(lib().echokv_diag_bounded_wait(self.handle, int(limit_cycles), left.data_ptr(), _stream_handle(stream)),
                "echokv_diag_bounded_wait")
         return left
 
-    def _out(self, q):
-        return self.torch.empty(q.shape, dtype=self.torch.float32, device=self.device)
+    def _out(self, q, stream):
+        with _memory_of(stream):
+            return self.torch.empty(q.shape, dtype=self.torch.float32, device=self.device)
 
 
 def echokv_full_attention_noalloc(cfg: echokv_config, k_pool, v_pool, block_table, q, out, seq_lens,
@@ -418,6 +435,8 @@ def echokv_full_attention_noalloc(cfg: echokv_config, k_pool, v_pool, block_tabl
 
 # ---- a serving step over a cache held in 8 bits ------------------------------------------------------------------
 # (A decode step's calls are short: what happens here per call is kept short too.)
+# stream: the torch stream that a call runs on, the current one if None.  New tensors are allocated for it.  As with torch's own
+# operators the caller orders streams: inputs have to be ready on it, and who uses the outputs elsewhere waits for it.
 def _stream_on(device: int, stream) -> int | None:
     if stream is not None:
         return stream.cuda_stream or None
@@ -477,7 +496,8 @@ def plan_tokens(cfg: echokv_config, block_table, seq_lens, new_lens, free_pages,
     import torch
     i32, B = torch.int32, seq_lens.shape[0]
     if out is None:
-        out = StepPlan(B, n_tokens, seq_lens.device)
+        with _memory_of(stream):
+            out = StepPlan(B, n_tokens, seq_lens.device)
     elif out._batch < B or out._tokens < n_tokens:
         raise ValueError("out: too small for %d sequences and %d tokens" % (B, n_tokens))
     _check(lib().echokv_plan_tokens(C.byref(cfg), _dense(block_table, i32, cfg.max_batch * cfg.max_pages_per_seq, "block_table"),
@@ -517,14 +537,16 @@ def rotate(cfg: echokv_config, q, k, positions, theta: float, sections=None, rot
     if q is not None:
         qp, qs = _rows(q, T, n_q, d, dt, "q")
         if q_out is None:
-            q_out = q.new_empty((T, n_q, d))
+            with _memory_of(stream):
+                q_out = q.new_empty((T, n_q, d))
             qo, qos = q_out.data_ptr(), n_q * d
         else:
             qo, qos = _rows(q_out, T, n_q, d, dt, "q_out")
     if k is not None:
         kp, ks = _rows(k, T, n_kv, d, dt, "k")
         if k_out is None:
-            k_out = k.new_empty((T, n_kv, d))
+            with _memory_of(stream):
+                k_out = k.new_empty((T, n_kv, d))
             ko, kos = k_out.data_ptr(), n_kv * d
         else:
             ko, kos = _rows(k_out, T, n_kv, d, dt, "k_out")
@@ -601,7 +623,8 @@ class QuantCache:
         cfg, T, B = self.cfg, q.shape[0], seq_lens.shape[0]
         qp, qs = _rows(q, T, cfg.n_q_heads, cfg.head_dim, self.tdtype, "q")
         if out is None:
-            out = q.new_empty((T, cfg.n_q_heads, cfg.head_dim))
+            with _memory_of(stream):
+                out = q.new_empty((T, cfg.n_q_heads, cfg.head_dim))
             op = out.data_ptr()
         else:
             op = _dense(out, self.tdtype, T * cfg.n_q_heads * cfg.head_dim, "out")
