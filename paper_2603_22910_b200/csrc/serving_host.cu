@@ -53,6 +53,12 @@ class OnDevice {
 
 inline bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
+// arrays of int32 or fp32 (NULL where one is optional)
+template <typename... P>
+inline bool words(const P*... p) {
+  return (aligned(p, 4) && ...);
+}
+
 int log2_of(int v) {
   int s = 0;
   while ((1 << s) < v) ++s;
@@ -126,6 +132,9 @@ int echokv_plan_tokens(const echokv_config* cfg, int32_t* dev_block_table, const
   if (B < 1 || n_tokens < 0 || n_tokens > (1 << 30)) return ECHOKV_EINVAL;
   if (!plan->cu_tokens || !plan->seq_lens || !plan->free_count) return ECHOKV_EINVAL;
   if (n_tokens > 0 && (!plan->positions || !plan->token_seqs || !plan->slot_map)) return ECHOKV_EINVAL;
+  if (!words(dev_block_table, dev_seq_slots, dev_seq_lens, dev_new_lens, dev_free_pages, dev_free_count, dev_status, plan->cu_tokens,
+             plan->positions, plan->token_seqs, plan->seq_lens, plan->free_count) || !aligned(plan->slot_map, 8))
+    return ECHOKV_EINVAL;
   const int rc = check_pages(cfg);
   if (rc != ECHOKV_OK) return rc;
   if (B > cfg->max_batch || B > kPlanMaxBatch) return ECHOKV_ECAPACITY;
@@ -146,6 +155,7 @@ int echokv_release_pages(const echokv_config* cfg, const int32_t* dev_block_tabl
                          const int32_t* dev_seq_lens, int B, int32_t* dev_free_pages, int32_t* dev_free_count,
                          int32_t* dev_status, void* stream) {
   if (!cfg || !dev_block_table || !dev_seq_lens || !dev_free_pages || !dev_free_count || B < 1) return ECHOKV_EINVAL;
+  if (!words(dev_block_table, dev_seq_slots, dev_seq_lens, dev_free_pages, dev_free_count, dev_status)) return ECHOKV_EINVAL;
   const int rc = check_pages(cfg);
   if (rc != ECHOKV_OK) return rc;
   if (B > cfg->max_batch || B > kPlanMaxBatch) return ECHOKV_ECAPACITY;
@@ -250,6 +260,7 @@ int echokv_quant_append(const echokv_config* cfg, const echokv_quant_cache* cach
   const int elem = cfg->dtype == ECHOKV_BF16 ? 2 : 4, width = cfg->n_kv_heads * cfg->head_dim;
   if (!rows_ok(k_new, k_stride, width, elem) || !rows_ok(v_new, v_stride, width, elem)) return ECHOKV_EINVAL;
   if (!dev_slot_map || !dev_token_seqs || !dev_cu_tokens) return ECHOKV_EINVAL;
+  if (!aligned(dev_slot_map, 8) || !words(dev_token_seqs, dev_cu_tokens, dev_seq_slots, dev_status)) return ECHOKV_EINVAL;
   a.x[0] = k_new; a.x[1] = v_new;
   a.stride[0] = k_stride; a.stride[1] = v_stride;
   a.slot_map = dev_slot_map; a.token_seqs = dev_token_seqs; a.cu = dev_cu_tokens; a.slots = dev_seq_slots;
@@ -278,6 +289,8 @@ int echokv_quant_attention(const echokv_config* cfg, const echokv_quant_cache* c
   const int elem = cfg->dtype == ECHOKV_BF16 ? 2 : 4;
   if (!rows_ok(q, q_stride, cfg->n_q_heads * cfg->head_dim, elem)) return ECHOKV_EINVAL;
   if (!out || !aligned(out, 16) || !dev_block_table || !dev_seq_lens) return ECHOKV_EINVAL;
+  if (!words(dev_block_table, dev_seq_slots, dev_seq_lens, dev_cu_tokens, dev_status)) return ECHOKV_EINVAL;
+  if (options && !words(options->alibi_slopes, options->prefix_lens)) return ECHOKV_EINVAL;
   if (!workspace || !aligned(workspace, 256)) return ECHOKV_EINVAL;
   if (workspace_bytes < quant_workspace(cfg)) return ECHOKV_ECAPACITY;
   a.q = q; a.q_stride = q_stride; a.out = out;

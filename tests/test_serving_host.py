@@ -187,3 +187,34 @@ def test_attend_ref_is_plain_softmax():
     full, _ = R.attend(q, k, v, 0.125, prefix=7)
     last, _ = R.attend(q[:1], k, v, 0.125)
     assert np.allclose(full[:1], last)
+
+
+# ---- pointers and buffers that a kernel could not use ------------------------------------------------------------
+def test_misaligned_small_arrays_are_refused(lib):
+    """Every int32, fp32 and int64 array: an address off its type's would end the kernel with a misaligned access."""
+    bad = P1 + 2
+    for kw in (dict(table=bad), dict(slots=bad), dict(lens=bad), dict(new=bad), dict(pages=bad), dict(count=bad)):
+        assert plan_call(lib, **kw) == EINVAL, kw
+    for i in range(6):
+        p = [P1] * 6
+        p[i] = P1 + (4 if i == 3 else 2)                                # (slot_map is int64)
+        assert plan_call(lib, plan=binding.echokv_step_plan(*p)) == EINVAL, i
+    cfg, s = config(), binding.echokv_step_plan(*([P1] * 6))
+    assert lib.echokv_plan_tokens(C.byref(cfg), P1, None, P1, P1, P1, P1, 2, 4, C.byref(s), bad, None) == EINVAL
+    for i in range(6):
+        p = [P1] * 6
+        p[i] = bad
+        table, slots, lens, pages, count, status = p
+        assert lib.echokv_release_pages(C.byref(cfg), table, slots, lens, 1, pages, count, status, None) == EINVAL, i
+    assert rotate_call(lib, pos=bad) == EINVAL
+    for kw in (dict(rows=P1 + 4), dict(seqs=bad), dict(cu=bad)):
+        assert append_call(lib, **kw) == EINVAL, kw
+    cache = quant_struct()
+    for slots, status in ((bad, None), (None, bad)):
+        assert lib.echokv_quant_append(C.byref(cfg), C.byref(cache), P1, 1024, P1, 1024, P1, P1, P1, slots, 2, 4, status, None) == EINVAL
+        need = binding.query_quant_sizes(cfg).workspace_bytes
+        assert lib.echokv_quant_attention(C.byref(cfg), C.byref(cache), None, P1, 4096, P1, P1, slots, P1, P1, 2, 4, 3, P1, need, status,
+                                          None) == EINVAL
+    for kw in (dict(table=bad), dict(lens=bad), dict(cu=bad), dict(opts=binding.echokv_score_options(0.0, 0, bad, None)),
+               dict(opts=binding.echokv_score_options(0.0, 0, None, bad))):
+        assert attn_call(lib, **kw) == EINVAL, kw
