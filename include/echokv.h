@@ -475,7 +475,8 @@ typedef struct {
 /* Attention over the 8-bit cache (Eq. 7 on the values the cache stands for).  The n new tokens of sequence b are its
  * last n tokens, already appended: query i sits at position dev_seq_lens[b] - n + i.
  *  - q: [n_tokens] rows of n_q_heads x head_dim elements, q_stride elements from row to row; out: dense
- *    [n_tokens][n_q_heads][head_dim] of the storage dtype (both 16-byte aligned).
+ *    [n_tokens][n_q_heads][head_dim] of the storage dtype (both 16-byte aligned).  out may be q itself if that is dense,
+ *    and otherwise must not overlap it (EINVAL).
  *  - n_tokens: at most 2^27 (EINVAL; also echokv_quant_append's).  dev_cu_tokens: [B + 1], or NULL for one token per
  *    sequence (n_tokens = B).  max_new: an upper bound of the tokens
  *    any sequence has in this call (1 for a decode step): it selects the kernels.

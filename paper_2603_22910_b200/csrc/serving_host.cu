@@ -104,6 +104,13 @@ bool rows_ok(const void* p, long long stride, int width, int elem) {
   return p != nullptr && aligned(p, 16) && stride >= width && stride * elem % 16 == 0 && stride < (1ll << 40);
 }
 
+// does one of `n` rows (`width` bytes, `stride` bytes apart) have a byte of [other, other + size)?
+bool rows_meet(const void* rows, long long stride, long long width, long long n, const void* other, long long size) {
+  const long long from = (long long)(reinterpret_cast<uintptr_t>(other) - reinterpret_cast<uintptr_t>(rows));
+  const long long i = from < width ? 0 : (from - width) / stride + 1;      // the first row that ends behind `other`
+  return i < n && i * stride < from + size;
+}
+
 int quant_geom(const echokv_config* c, const echokv_quant_cache* q, QuantGeom* g) {
   if (!q || !q->k_codes || !q->v_codes || !q->k_scales || !q->v_scales || !q->k_tail || !q->v_tail) return ECHOKV_EINVAL;
   if (!aligned(q->k_codes, 16) || !aligned(q->v_codes, 16) || !aligned(q->k_scales, 16) || !aligned(q->v_scales, 16) ||
@@ -289,6 +296,11 @@ int echokv_quant_attention(const echokv_config* cfg, const echokv_quant_cache* c
   const int elem = cfg->dtype == ECHOKV_BF16 ? 2 : 4;
   if (!rows_ok(q, q_stride, cfg->n_q_heads * cfg->head_dim, elem)) return ECHOKV_EINVAL;
   if (!out || !aligned(out, 16) || !dev_block_table || !dev_seq_lens) return ECHOKV_EINVAL;
+  // (the kernels read an item's queries before they write its rows, so in place is as good as apart)
+  const long long row_bytes = (long long)cfg->n_q_heads * cfg->head_dim * elem;
+  if (!(q == out && (n_tokens == 1 || q_stride * elem == row_bytes)) &&
+      rows_meet(q, q_stride * elem, row_bytes, n_tokens, out, n_tokens * row_bytes))
+    return ECHOKV_EINVAL;
   if (!words(dev_block_table, dev_seq_slots, dev_seq_lens, dev_cu_tokens, dev_status)) return ECHOKV_EINVAL;
   if (options && !words(options->alibi_slopes, options->prefix_lens)) return ECHOKV_EINVAL;
   if (!workspace || !aligned(workspace, 256)) return ECHOKV_EINVAL;

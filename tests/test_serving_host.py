@@ -218,3 +218,16 @@ def test_misaligned_small_arrays_are_refused(lib):
     for kw in (dict(table=bad), dict(lens=bad), dict(cu=bad), dict(opts=binding.echokv_score_options(0.0, 0, bad, None)),
                dict(opts=binding.echokv_score_options(0.0, 0, None, bad))):
         assert attn_call(lib, **kw) == EINVAL, kw
+
+
+def test_outputs_that_partly_overlap_the_queries_are_refused(lib):
+    """out may be q itself where that is dense; 4 rows of 8192 bytes each otherwise lie beside it, between its rows or behind it."""
+    row = 32 * 128 * 2
+    need = binding.query_quant_sizes(config()).workspace_bytes
+    q = P1 + 16 * row
+    call = lambda out, qs=4096, n=4: attn_call(lib, q=q, qs=qs, out=out, n=n, ws_bytes=need - 1)  # noqa: E731  (ECAP: nothing else is wrong)
+    for out, qs in ((q, 4096), (q - 4 * row, 4096), (q + 4 * row, 4096), (q + row, 6 * 4096), (q + 2 * row, 6 * 4096), (q - 4 * row, 5 * 4096)):
+        assert call(out, qs) == ECAP, (out - q, qs)
+    for out, qs in ((q + 16, 4096), (q - 16, 4096), (q + row, 4096), (q - row, 4096), (q + 4 * row - 16, 4096), (q, 2 * 4096), (q + 3 * row, 6 * 4096),
+                    (q - 3 * row, 6 * 4096), (q + row, 3 * 4096), (q + 18 * row, 6 * 4096)):
+        assert call(out, qs) == EINVAL, (out - q, qs)
