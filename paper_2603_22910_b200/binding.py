@@ -486,12 +486,23 @@ class StepPlan:
                                    count.data_ptr() if free_count is None else _dense(free_count, torch.int32, 1, "free_count"))
         self._batch, self._tokens = batch, n_tokens
 
+    def _beginning(self, batch: int, n_tokens: int) -> StepPlan:
+        """The plan of a smaller step in the same buffers."""
+        if batch == self._batch and n_tokens == self._tokens:
+            return self
+        part = object.__new__(StepPlan)
+        part.cu_tokens, part.seq_lens, part.free_count = self.cu_tokens[:batch + 1], self.seq_lens[:batch], self.free_count
+        part.positions, part.token_seqs, part.slot_map = self.positions[:n_tokens], self.token_seqs[:n_tokens], self.slot_map[:n_tokens]
+        part._c, part._batch, part._tokens = self._c, batch, n_tokens
+        return part
+
 
 def plan_tokens(cfg: echokv_config, block_table, seq_lens, new_lens, free_pages, free_count, n_tokens: int, seq_slots=None,
                 out: StepPlan | None = None, status=None, stream=None) -> StepPlan:
     """Pages for new_lens[b] more tokens of sequences that hold seq_lens[b]: fills block_table ([max_batch][max_pages_per_seq]
     int32) and returns the step's plan for up to n_tokens tokens.  `out` is used again by later (and captured) steps, and may
-    hold the buffers seq_lens and free_count themselves, which are then updated in place; status: optional int32 device tensor
+    hold the buffers seq_lens and free_count themselves, which are then updated in place; for a step smaller than it the returned
+    plan holds the beginnings of its tensors (behind them an earlier step's entries remain).  status: optional int32 device tensor
     (see echokv.h)."""
     import torch
     i32, B = torch.int32, seq_lens.shape[0]
@@ -505,7 +516,7 @@ def plan_tokens(cfg: echokv_config, block_table, seq_lens, new_lens, free_pages,
                                     _dense(new_lens, i32, B, "new_lens"), _dense(free_pages, i32, cfg.n_pages, "free_pages"),
                                     _dense(free_count, i32, 1, "free_count"), B, n_tokens, C.byref(out._c),
                                     _dense(status, i32, 1, "status"), _stream_on(cfg.device, stream)), "echokv_plan_tokens")
-    return out
+    return out._beginning(B, n_tokens)
 
 
 def release_pages(cfg: echokv_config, block_table, seq_lens, free_pages, free_count, seq_slots=None, status=None,
