@@ -445,20 +445,20 @@ def _stream_on(device: int, stream) -> int | None:
     return (raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream) or None
 
 
-def _dense(t, dtype, n, name):
-    """Address of a contiguous device tensor of `dtype` with at least n elements (None stays NULL)."""
+def _dense(t, dtype, n, name, device):
+    """Address of a contiguous tensor of `dtype` with at least n elements on CUDA device `device` (None stays NULL)."""
     if t is None:
         return None
-    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous() or t.numel() < n:
-        raise ValueError("%s: a contiguous %s device tensor of at least %d elements is needed" % (name, dtype, n))
+    if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or t.numel() < n:
+        raise ValueError("%s: a contiguous %s device tensor of at least %d elements is needed, on cuda:%d" % (name, dtype, n, device))
     return t.data_ptr()
 
 
-def _rows(t, n, heads, d, dtype, name):
-    """(address, elements from row to row) of a [n][heads][d] device tensor whose rows are dense."""
+def _rows(t, n, heads, d, dtype, name, device):
+    """(address, elements from row to row) of a [n][heads][d] tensor on CUDA device `device` whose rows are dense."""
     st = t.stride()
-    if t.dtype is not dtype or t.shape != (n, heads, d) or not t.is_cuda or (n > 0 and (st[2] != 1 or (st[1] != d and heads > 1))):
-        raise ValueError("%s: a [%d tokens][%d][%d] %s device tensor with dense rows is needed" % (name, n, heads, d, dtype))
+    if t.dtype is not dtype or t.shape != (n, heads, d) or t.get_device() != device or (n > 0 and (st[2] != 1 or (st[1] != d and heads > 1))):
+        raise ValueError("%s: a [%d tokens][%d][%d] %s device tensor with dense rows is needed, on cuda:%d" % (name, n, heads, d, dtype, device))
     # (the stride of a single row is anything)
     return t.data_ptr(), st[0] if n > 1 else heads * d
 
@@ -471,7 +471,7 @@ def _dtype(cfg):
 class StepPlan:
     """What plan_tokens writes: cu_tokens [B + 1], positions, token_seqs [n_tokens], seq_lens [B], free_count [1] (int32) and
     slot_map [n_tokens] (int64)."""
-    __slots__ = ("cu_tokens", "positions", "token_seqs", "slot_map", "seq_lens", "free_count", "_c", "_batch", "_tokens")
+    __slots__ = ("cu_tokens", "positions", "token_seqs", "slot_map", "seq_lens", "free_count", "_c", "_batch", "_tokens", "_device")
 
     def __init__(self, batch: int, n_tokens: int, device, seq_lens=None, free_count=None):
         import torch
@@ -482,9 +482,9 @@ class StepPlan:
         self.free_count = count if free_count is None else free_count
         cu = buf.data_ptr()
         self._c = echokv_step_plan(cu, cu + 4 * (batch + 1), cu + 4 * (batch + 1 + n_tokens), self.slot_map.data_ptr(),
-                                   lens.data_ptr() if seq_lens is None else _dense(seq_lens, torch.int32, batch, "seq_lens"),
-                                   count.data_ptr() if free_count is None else _dense(free_count, torch.int32, 1, "free_count"))
-        self._batch, self._tokens = batch, n_tokens
+                                   lens.data_ptr() if seq_lens is None else _dense(seq_lens, torch.int32, batch, "seq_lens", buf.get_device()),
+                                   count.data_ptr() if free_count is None else _dense(free_count, torch.int32, 1, "free_count", buf.get_device()))
+        self._batch, self._tokens, self._device = batch, n_tokens, buf.get_device()
 
     def _beginning(self, batch: int, n_tokens: int) -> StepPlan:
         """The plan of a smaller step in the same buffers."""
@@ -493,7 +493,7 @@ class StepPlan:
         part = object.__new__(StepPlan)
         part.cu_tokens, part.seq_lens, part.free_count = self.cu_tokens[:batch + 1], self.seq_lens[:batch], self.free_count
         part.positions, part.token_seqs, part.slot_map = self.positions[:n_tokens], self.token_seqs[:n_tokens], self.slot_map[:n_tokens]
-        part._c, part._batch, part._tokens = self._c, batch, n_tokens
+        part._c, part._batch, part._tokens, part._device = self._c, batch, n_tokens, self._device
         return part
 
 
@@ -511,11 +511,13 @@ def plan_tokens(cfg: echokv_config, block_table, seq_lens, new_lens, free_pages,
             out = StepPlan(B, n_tokens, seq_lens.device)
     elif out._batch < B or out._tokens < n_tokens:
         raise ValueError("out: too small for %d sequences and %d tokens" % (B, n_tokens))
-    _check(lib().echokv_plan_tokens(C.byref(cfg), _dense(block_table, i32, cfg.max_batch * cfg.max_pages_per_seq, "block_table"),
-                                    _dense(seq_slots, i32, B, "seq_slots"), _dense(seq_lens, i32, B, "seq_lens"),
-                                    _dense(new_lens, i32, B, "new_lens"), _dense(free_pages, i32, cfg.n_pages, "free_pages"),
-                                    _dense(free_count, i32, 1, "free_count"), B, n_tokens, C.byref(out._c),
-                                    _dense(status, i32, 1, "status"), _stream_on(cfg.device, stream)), "echokv_plan_tokens")
+    elif out._device != cfg.device:
+        raise ValueError("out: a plan on cuda:%d is needed" % cfg.device)
+    _check(lib().echokv_plan_tokens(C.byref(cfg), _dense(block_table, i32, cfg.max_batch * cfg.max_pages_per_seq, "block_table", cfg.device),
+                                    _dense(seq_slots, i32, B, "seq_slots", cfg.device), _dense(seq_lens, i32, B, "seq_lens", cfg.device),
+                                    _dense(new_lens, i32, B, "new_lens", cfg.device), _dense(free_pages, i32, cfg.n_pages, "free_pages", cfg.device),
+                                    _dense(free_count, i32, 1, "free_count", cfg.device), B, n_tokens, C.byref(out._c),
+                                    _dense(status, i32, 1, "status", cfg.device), _stream_on(cfg.device, stream)), "echokv_plan_tokens")
     return out._beginning(B, n_tokens)
 
 
@@ -524,10 +526,10 @@ def release_pages(cfg: echokv_config, block_table, seq_lens, free_pages, free_co
     """Put the pages of finished sequences back on the free list (free_pages, free_count are updated)."""
     import torch
     i32, B = torch.int32, seq_lens.shape[0]
-    _check(lib().echokv_release_pages(C.byref(cfg), _dense(block_table, i32, cfg.max_batch * cfg.max_pages_per_seq, "block_table"),
-                                      _dense(seq_slots, i32, B, "seq_slots"), _dense(seq_lens, i32, B, "seq_lens"), B,
-                                      _dense(free_pages, i32, cfg.n_pages, "free_pages"), _dense(free_count, i32, 1, "free_count"),
-                                      _dense(status, i32, 1, "status"), _stream_on(cfg.device, stream)), "echokv_release_pages")
+    _check(lib().echokv_release_pages(C.byref(cfg), _dense(block_table, i32, cfg.max_batch * cfg.max_pages_per_seq, "block_table", cfg.device),
+                                      _dense(seq_slots, i32, B, "seq_slots", cfg.device), _dense(seq_lens, i32, B, "seq_lens", cfg.device), B,
+                                      _dense(free_pages, i32, cfg.n_pages, "free_pages", cfg.device), _dense(free_count, i32, 1, "free_count", cfg.device),
+                                      _dense(status, i32, 1, "status", cfg.device), _stream_on(cfg.device, stream)), "echokv_release_pages")
 
 
 def rotate(cfg: echokv_config, q, k, positions, theta: float, sections=None, rot_dim: int = 0, interleaved: bool = False,
@@ -546,27 +548,27 @@ def rotate(cfg: echokv_config, q, k, positions, theta: float, sections=None, rot
     qp = kp = qo = ko = None
     qs = ks = qos = kos = 0
     if q is not None:
-        qp, qs = _rows(q, T, n_q, d, dt, "q")
+        qp, qs = _rows(q, T, n_q, d, dt, "q", cfg.device)
         if q_out is None:
             with _memory_of(stream):
                 q_out = q.new_empty((T, n_q, d))
             qo, qos = q_out.data_ptr(), n_q * d
         else:
-            qo, qos = _rows(q_out, T, n_q, d, dt, "q_out")
+            qo, qos = _rows(q_out, T, n_q, d, dt, "q_out", cfg.device)
     if k is not None:
-        kp, ks = _rows(k, T, n_kv, d, dt, "k")
+        kp, ks = _rows(k, T, n_kv, d, dt, "k", cfg.device)
         if k_out is None:
             with _memory_of(stream):
                 k_out = k.new_empty((T, n_kv, d))
             ko, kos = k_out.data_ptr(), n_kv * d
         else:
-            ko, kos = _rows(k_out, T, n_kv, d, dt, "k_out")
+            ko, kos = _rows(k_out, T, n_kv, d, dt, "k_out", cfg.device)
     sec = None
     if sections is not None:
         if len(sections) != axes:
             raise ValueError("rotate: one section per position axis")
         sec = (C.c_int32 * axes)(*sections)
-    _check(lib().echokv_rotate(C.byref(cfg), qp, qs, kp, ks, qo, qos, ko, kos, _dense(positions, torch.int32, axes * T, "positions"),
+    _check(lib().echokv_rotate(C.byref(cfg), qp, qs, kp, ks, qo, qos, ko, kos, _dense(positions, torch.int32, axes * T, "positions", cfg.device),
                                axes, sec, 1 if interleaved else 0, rot_dim, theta, 1 if inverse else 0, T,
                                _stream_on(cfg.device, stream)), "echokv_rotate")
     return (q_out if q is not None else None), (k_out if k is not None else None)
@@ -599,8 +601,8 @@ class QuantCache:
         def held(t, shape, dtype, name):
             if t is None:
                 return torch.zeros(shape, dtype=dtype, device=dev)
-            if tuple(t.shape) != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
-                raise ValueError("%s: a contiguous %s device tensor of shape %s is needed" % (name, dtype, shape))
+            if tuple(t.shape) != shape or t.dtype is not dtype or t.get_device() != cfg.device or not t.is_contiguous():
+                raise ValueError("%s: a contiguous %s device tensor of shape %s is needed, on cuda:%d" % (name, dtype, shape, cfg.device))
             return t
         self.k_codes = held(k_codes, (N, H, P, d), code, "k_codes")
         self.v_codes = held(v_codes, (N, H, P, d), code, "v_codes")
@@ -610,6 +612,7 @@ class QuantCache:
         self.k_tail = held(k_tail, tail, self.tdtype, "k_tail")
         self.v_tail = held(v_tail, tail, self.tdtype, "v_tail")
         self.workspace = torch.empty(sizes.workspace_bytes, dtype=torch.uint8, device=dev) if workspace is None else workspace
+        _dense(self.workspace, torch.uint8, self._ws_bytes, "workspace", cfg.device)
         self._c = echokv_quant_cache(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scales.data_ptr(),
                                      self.v_scales.data_ptr(), self.k_tail.data_ptr(), self.v_tail.data_ptr(),
                                      QUANT_FORMATS[fmt], 0)
@@ -618,12 +621,12 @@ class QuantCache:
         """k_new, v_new [T][n_kv_heads][d] (rows may be slices of a wider tensor); slot_map, token_seqs, cu_tokens: plan_tokens'."""
         import torch
         cfg, T, B = self.cfg, k_new.shape[0], cu_tokens.shape[0] - 1
-        kp, ks = _rows(k_new, T, cfg.n_kv_heads, cfg.head_dim, self.tdtype, "k_new")
-        vp, vs = _rows(v_new, T, cfg.n_kv_heads, cfg.head_dim, self.tdtype, "v_new")
-        _check(lib().echokv_quant_append(C.byref(cfg), C.byref(self._c), kp, ks, vp, vs, _dense(slot_map, torch.int64, T, "slot_map"),
-                                         _dense(token_seqs, torch.int32, T, "token_seqs"),
-                                         _dense(cu_tokens, torch.int32, B + 1, "cu_tokens"), _dense(seq_slots, torch.int32, B, "seq_slots"),
-                                         B, T, _dense(status, torch.int32, 1, "status"), _stream_on(cfg.device, stream)),
+        kp, ks = _rows(k_new, T, cfg.n_kv_heads, cfg.head_dim, self.tdtype, "k_new", cfg.device)
+        vp, vs = _rows(v_new, T, cfg.n_kv_heads, cfg.head_dim, self.tdtype, "v_new", cfg.device)
+        _check(lib().echokv_quant_append(C.byref(cfg), C.byref(self._c), kp, ks, vp, vs, _dense(slot_map, torch.int64, T, "slot_map", cfg.device),
+                                         _dense(token_seqs, torch.int32, T, "token_seqs", cfg.device),
+                                         _dense(cu_tokens, torch.int32, B + 1, "cu_tokens", cfg.device), _dense(seq_slots, torch.int32, B, "seq_slots", cfg.device),
+                                         B, T, _dense(status, torch.int32, 1, "status", cfg.device), _stream_on(cfg.device, stream)),
                "echokv_quant_append")
 
     def attention(self, q, block_table, seq_lens, cu_tokens=None, max_new: int = 1, seq_slots=None, softcap: float = 0.0,
@@ -632,23 +635,23 @@ class QuantCache:
         one each).  max_new bounds the new tokens of any sequence.  Returns out [T][n_q_heads][d] in the storage type."""
         import torch
         cfg, T, B = self.cfg, q.shape[0], seq_lens.shape[0]
-        qp, qs = _rows(q, T, cfg.n_q_heads, cfg.head_dim, self.tdtype, "q")
+        qp, qs = _rows(q, T, cfg.n_q_heads, cfg.head_dim, self.tdtype, "q", cfg.device)
         if out is None:
             with _memory_of(stream):
                 out = q.new_empty((T, cfg.n_q_heads, cfg.head_dim))
             op = out.data_ptr()
         else:
-            op = _dense(out, self.tdtype, T * cfg.n_q_heads * cfg.head_dim, "out")
+            op = _dense(out, self.tdtype, T * cfg.n_q_heads * cfg.head_dim, "out", cfg.device)
         opts = None
         if softcap or alibi_slopes is not None or prefix_lens is not None:
-            opts = C.byref(echokv_score_options(softcap, 0, _dense(alibi_slopes, torch.float32, cfg.n_q_heads, "alibi_slopes"),
-                                                _dense(prefix_lens, torch.int32, B, "prefix_lens")))
+            opts = C.byref(echokv_score_options(softcap, 0, _dense(alibi_slopes, torch.float32, cfg.n_q_heads, "alibi_slopes", cfg.device),
+                                                _dense(prefix_lens, torch.int32, B, "prefix_lens", cfg.device)))
         _check(lib().echokv_quant_attention(C.byref(cfg), C.byref(self._c), opts, qp, qs, op,
-                                            _dense(block_table, torch.int32, cfg.max_batch * cfg.max_pages_per_seq, "block_table"),
-                                            _dense(seq_slots, torch.int32, B, "seq_slots"), _dense(seq_lens, torch.int32, B, "seq_lens"),
-                                            _dense(cu_tokens, torch.int32, B + 1, "cu_tokens"), B, T, max_new,
-                                            _dense(self.workspace, torch.uint8, self._ws_bytes, "workspace"),
-                                            self._ws_bytes, _dense(status, torch.int32, 1, "status"),
+                                            _dense(block_table, torch.int32, cfg.max_batch * cfg.max_pages_per_seq, "block_table", cfg.device),
+                                            _dense(seq_slots, torch.int32, B, "seq_slots", cfg.device), _dense(seq_lens, torch.int32, B, "seq_lens", cfg.device),
+                                            _dense(cu_tokens, torch.int32, B + 1, "cu_tokens", cfg.device), B, T, max_new,
+                                            _dense(self.workspace, torch.uint8, self._ws_bytes, "workspace", cfg.device),
+                                            self._ws_bytes, _dense(status, torch.int32, 1, "status", cfg.device),
                                             _stream_on(cfg.device, stream)), "echokv_quant_attention")
         return out
 

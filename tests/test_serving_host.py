@@ -231,3 +231,74 @@ def test_outputs_that_partly_overlap_the_queries_are_refused(lib):
     for out, qs in ((q + 16, 4096), (q - 16, 4096), (q + row, 4096), (q - row, 4096), (q + 4 * row - 16, 4096), (q, 2 * 4096), (q + 3 * row, 6 * 4096),
                     (q - 3 * row, 6 * 4096), (q + row, 3 * 4096), (q + 18 * row, 6 * 4096)):
         assert call(out, qs) == EINVAL, (out - q, qs)
+
+
+class OnGpu:
+    """What the binding asks of a tensor, without a GPU: `shape` elements on device `index`."""
+    is_cuda = True
+
+    def __init__(self, dtype, *shape, index=1):
+        self.dtype, self.shape, self.index = dtype, torch.Size(shape), index
+        self.device = torch.device("cuda", index)
+
+    def get_device(self):
+        return self.index
+
+    def numel(self):
+        return self.shape.numel()
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self):
+        return torch.empty(self.shape, device="meta").stride()
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return P1
+
+
+class NoStream:
+    cuda_stream = 0
+
+
+def test_tensors_of_another_device_are_refused():
+    """The kernels run on cfg.device: an address of another GPU's memory would fault there."""
+    cfg, i32, bf16 = config(), torch.int32, torch.bfloat16
+    small = dict(block_table=(i32, 4, 8), seq_lens=(i32, 2), new_lens=(i32, 2), free_pages=(i32, 32), free_count=(i32, 1), seq_slots=(i32, 2),
+                 status=(i32, 1))
+    plan = object.__new__(binding.StepPlan)
+    plan._batch, plan._tokens, plan._device, plan._c = 2, 4, 0, binding.echokv_step_plan(*([P1] * 6))
+
+    def refused(fn, tensors, wrong, **kw):
+        args = {n: OnGpu(*t, index=1 if n == wrong else 0) for n, t in tensors.items()}
+        with pytest.raises(ValueError, match=wrong):
+            fn(**args, stream=NoStream(), **kw)
+    for name in small:
+        refused(lambda **kw: binding.plan_tokens(cfg, n_tokens=4, out=plan, **kw), small, name)
+    plan._device = 1
+    with pytest.raises(ValueError, match="out"):
+        binding.plan_tokens(cfg, n_tokens=4, out=plan, stream=NoStream(), **{n: OnGpu(*t, index=0) for n, t in small.items()})
+    free = {n: t for n, t in small.items() if n != "new_lens"}
+    for name in free:
+        refused(lambda **kw: binding.release_pages(cfg, **kw), free, name)
+    turn = dict(q=(bf16, 4, 32, 128), k=(bf16, 4, 8, 128), positions=(i32, 4), q_out=(bf16, 4, 32, 128), k_out=(bf16, 4, 8, 128))
+    for name in turn:
+        refused(lambda **kw: binding.rotate(cfg, theta=1e4, **kw), turn, name)
+    held = dict(k_codes=(torch.int8, 32, 8, 16, 128), v_codes=(torch.int8, 32, 8, 16, 128), k_scales=(torch.float32, 32, 8, 1),
+                v_scales=(torch.float32, 32, 8, 1), k_tail=(bf16, 4, 8, 16, 128), v_tail=(bf16, 4, 8, 16, 128),
+                workspace=(torch.uint8, 1 << 30))
+    for name in held:
+        with pytest.raises(ValueError, match=name):
+            binding.QuantCache(cfg, "int8", **{n: OnGpu(*t, index=1 if n == name else 0) for n, t in held.items()})
+    cache = binding.QuantCache(cfg, "int8", **{n: OnGpu(*t, index=0) for n, t in held.items()})
+    new = dict(k_new=(bf16, 4, 8, 128), v_new=(bf16, 4, 8, 128), slot_map=(torch.int64, 4), token_seqs=(i32, 4), cu_tokens=(i32, 3),
+               seq_slots=(i32, 2), status=(i32, 1))
+    for name in new:
+        refused(cache.append, new, name)
+    attend = dict(q=(bf16, 4, 32, 128), block_table=(i32, 4, 8), seq_lens=(i32, 2), cu_tokens=(i32, 3), seq_slots=(i32, 2),
+                  alibi_slopes=(torch.float32, 32), prefix_lens=(i32, 2), out=(bf16, 4, 32, 128), status=(i32, 1))
+    for name in attend:
+        refused(cache.attention, attend, name, max_new=3)
