@@ -471,7 +471,7 @@ def _dtype(cfg):
 class StepPlan:
     """What plan_tokens writes: cu_tokens [B + 1], positions, token_seqs [n_tokens], seq_lens [B], free_count [1] (int32) and
     slot_map [n_tokens] (int64)."""
-    __slots__ = ("cu_tokens", "positions", "token_seqs", "slot_map", "seq_lens", "free_count", "_c", "_batch", "_tokens", "_device")
+    __slots__ = ("cu_tokens", "positions", "token_seqs", "slot_map", "seq_lens", "free_count", "_c", "_held", "_batch", "_tokens", "_device")
 
     def __init__(self, batch: int, n_tokens: int, device, seq_lens=None, free_count=None):
         import torch
@@ -484,6 +484,7 @@ class StepPlan:
         self._c = echokv_step_plan(cu, cu + 4 * (batch + 1), cu + 4 * (batch + 1 + n_tokens), self.slot_map.data_ptr(),
                                    lens.data_ptr() if seq_lens is None else _dense(seq_lens, torch.int32, batch, "seq_lens", buf.get_device()),
                                    count.data_ptr() if free_count is None else _dense(free_count, torch.int32, 1, "free_count", buf.get_device()))
+        self._held = buf, self.slot_map, self.seq_lens, self.free_count       # (what _c's addresses are of, whatever becomes of the attributes)
         self._batch, self._tokens, self._device = batch, n_tokens, buf.get_device()
 
     def _beginning(self, batch: int, n_tokens: int) -> StepPlan:
@@ -493,7 +494,7 @@ class StepPlan:
         part = object.__new__(StepPlan)
         part.cu_tokens, part.seq_lens, part.free_count = self.cu_tokens[:batch + 1], self.seq_lens[:batch], self.free_count
         part.positions, part.token_seqs, part.slot_map = self.positions[:n_tokens], self.token_seqs[:n_tokens], self.slot_map[:n_tokens]
-        part._c, part._batch, part._tokens, part._device = self._c, batch, n_tokens, self._device
+        part._c, part._held, part._batch, part._tokens, part._device = self._c, self._held, batch, n_tokens, self._device
         return part
 
 
@@ -584,7 +585,13 @@ class QuantCache:
     """One layer's cache in 8 bits: codes int8 or float8_e4m3fn [n_pages][n_kv_heads][page_tokens][d], a scale for each 16 tokens
     and head [n_pages][n_kv_heads][page_tokens / 16], and the open blocks' rows in the storage type [max_batch][n_kv_heads][16][d].
     Allocates them unless they are given; `workspace` (42 MB in bf16 with heads of 128) is best shared by the layers of a model
-    (calls that share one must not overlap on the device)."""
+    (calls that share one must not overlap on the device).  The other tensors are the cache's for its life."""
+    _FIXED = frozenset(("cfg", "k_codes", "v_codes", "k_scales", "v_scales", "k_tail", "v_tail"))
+
+    def __setattr__(self, name, value):
+        if name in self._FIXED and name in self.__dict__:
+            raise AttributeError("%s: the library holds its address; make a new QuantCache" % name)
+        self.__dict__[name] = value
 
     def __init__(self, cfg: echokv_config, fmt: str, k_codes=None, v_codes=None, k_scales=None, v_scales=None, k_tail=None,
                  v_tail=None, workspace=None):

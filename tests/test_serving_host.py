@@ -302,3 +302,26 @@ def test_tensors_of_another_device_are_refused():
                   alibi_slopes=(torch.float32, 32), prefix_lens=(i32, 2), out=(bf16, 4, 32, 128), status=(i32, 1))
     for name in attend:
         refused(cache.attention, attend, name, max_new=3)
+
+
+def test_the_tensors_whose_addresses_a_cache_and_a_plan_hold_stay():
+    """An attribute that is set anew would leave the library with the address of freed memory."""
+    cfg, bf16 = config(), torch.bfloat16
+    held = dict(k_codes=(torch.int8, 32, 8, 16, 128), v_codes=(torch.int8, 32, 8, 16, 128), k_scales=(torch.float32, 32, 8, 1),
+                v_scales=(torch.float32, 32, 8, 1), k_tail=(bf16, 4, 8, 16, 128), v_tail=(bf16, 4, 8, 16, 128),
+                workspace=(torch.uint8, 1 << 30))
+    cache = binding.QuantCache(cfg, "int8", **{n: OnGpu(*t, index=0) for n, t in held.items()})
+    for name in list(held)[:6] + ["cfg"]:
+        before = getattr(cache, name)
+        with pytest.raises(AttributeError, match=name):
+            setattr(cache, name, None)
+        assert getattr(cache, name) is before
+    cache.workspace = OnGpu(torch.uint8, 1 << 30, index=0)                # (checked at every call)
+    lens, count = torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    p = binding.StepPlan(2, 4, "cpu", seq_lens=lens, free_count=count)
+    q = p._beginning(1, 2)
+    addresses = [t.data_ptr() for t in (p.slot_map, lens, count)]
+    p.slot_map = p.seq_lens = p.free_count = None
+    q.slot_map = q.seq_lens = q.free_count = None
+    for plan in (p, q):
+        assert [t.data_ptr() for t in plan._held[1:]] == addresses
