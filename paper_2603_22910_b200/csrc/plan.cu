@@ -17,7 +17,9 @@ namespace {
 
 constexpr int kPlanThreads = 512;
 constexpr int kPlanCluster = 8;
-constexpr int kPlanSmallTokens = 4096;             // up to here one CTA is as fast as eight
+// Up to so many tokens one CTA, above it a cluster of eight (64 sequences; 256 tokens 5.0 us with one, 5.7 with eight; 1024 5.3 and
+// 5.6; 2048 6.4 and 5.7; 4096 8.6 and 5.8)
+constexpr int kPlanSmallTokens = 1024;
 
 // exclusive prefix sum over the block's threads; *total = sum over all
 __device__ __forceinline__ long long block_scan(long long v, long long* warp_sums, long long* total) {
