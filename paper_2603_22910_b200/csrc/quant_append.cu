@@ -4,7 +4,7 @@
 // takes one (block, head, K or V): a lane holds head_dim / 32 elements of each of the 16 rows, all 16 loads in flight at once,
 // the largest magnitude by one warp reduction, the codes go back 128 contiguous bytes a row.  (K and V by one warp, 32 loads in
 // flight at half the warps: 46 against 44 us for 33 thousand tokens, 5.6 against 4.3 us for a decode step.)
-// Measured: 33 thousand tokens of 8 bf16 heads of 128 in 43 us (198 MB, 4.6 TB/s), a decode step of 128 tokens in 4.1 us.  What
+// Measured: 33 thousand tokens of 8 bf16 heads of 128 in 42 us (198 MB, 4.7 TB/s), a decode step of 128 tokens in 4.3 us.  What
 // keeps it from the memory's rate: a warp's 16 loads are all it has in flight until its block is reduced and written.
 // (2, 4 and 16 warps per CTA: 79, 54 and 43.4 us; 3 CTAs per SM instead of 4: 46.6.)
 // A CTA looks at 16 consecutive new tokens of the step; the tokens in it that end a block (the last row of a block, or the last

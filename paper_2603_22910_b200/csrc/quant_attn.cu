@@ -25,7 +25,7 @@
 //   tail     The open block is in the storage type: bf16 rows are operands of the bf16 product as they are, fp32 rows become pairs of
 //            fp16, each token's around its own power of two.  It is attended first, while the first copies are on their way.
 // Measured: 16 sequences over 32768 keys (1.07 GB of codes) 177 us, 6.1 TB/s; 32 ragged ones with capped scores, e4m3, 168 us,
-// 6.0 TB/s; one token over 777 keys 12.5 us, all latency (this kernel 7.5, the second one 3, launches).
+// 6.0 TB/s; one token over 777 keys 12.6 us, all latency (this kernel 7.5, the second one 3, launches).
 // (Rings filled by cp.async: 4.4 TB/s.  Warps x stages, first case: 12 x 3 177 us, 10 x 4 193, 8 x 4 192, 16 x 2 225.)
 #include "quant_common.cuh"
 #include "recon_tc.h"

@@ -24,11 +24,11 @@
 // joins them in the order of their keys.  (2 x 1024 tokens over 8192 keys, 256 items for 148 SMs: 433 -> 393 us; one sequence of 64
 // tokens over 32768 keys, 8 items: 630 -> 87 us.)  Every wait is bounded.
 // Bound: 128 exponentials per row and tile at 16 per clock and SM take twice the products' time.  Measured (2 x 1024 tokens over
-// 8192 keys, 32 / 8 heads, e4m3): 293 us = 880 TFLOP/s without a cap, 379 us = 680 with one; a tile of 128 keys takes both halves 2.4 us
+// 8192 keys, 32 / 8 heads, e4m3): 300 us = 860 TFLOP/s without a cap, 396 us = 650 with one; a tile of 128 keys takes both halves 2.4 us
 // where its products take 1.1 and its exponentials 1.1: each half's scores -> probabilities (1.45 us) -> products (1.0 us) chain is
-// longer than what the other half covers.  Tensor pipe 38 / 30 %, exponentials' pipe 39 / 31 %, issue slots 43 / 49 % busy.
+// longer than what the other half covers.  Tensor pipe 38 / 29 %, exponentials' pipe 38 / 30 %, issue slots 45 / 48 % busy.
 // (Scores in pieces of 64 keys, so that the next 64's products run while the softmax works on these: half as wide and
-// half again as many products, 400 us against 293.)
+// half again as many products, 400 us against 293 then.)
 #include <type_traits>
 
 #include "quant_common.cuh"
