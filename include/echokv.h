@@ -351,9 +351,10 @@ uint64_t echokv_noalloc_scratch_bytes(void);
  *     echokv_quant_attention  every new token attends its sequence                        (per layer)
  *     echokv_release_pages    pages of finished requests back to the free list
  * The new tokens of a step lie flat, sequence after sequence: token cu_tokens[b] + i is the i-th new token of
- * sequence b.  They only enqueue work on `stream`, run on cfg->device and leave the calling thread's current device
- * as it was, allocate nothing and can be captured into a graph.  dev_status (may be NULL) is a device int32 that
- * receives the first device-side error found; it is not cleared (clear it once, read it whenever).
+ * sequence b.  They only enqueue work on `stream` (what they read has to be ready there: the caller orders streams),
+ * run on cfg->device and leave the calling thread's current device as it was, allocate nothing and can be captured
+ * into a graph.  dev_status (may be NULL) is a device int32 that receives the first device-side error found; it is
+ * not cleared (clear it once, read it whenever).
  * Common errors: EINVAL (NULL or misaligned pointer, bad number), EUNSUPPORTED (head_dim, page_tokens, n_q_heads /
  * n_kv_heads as for echokv_create), ECAPACITY (B > max_batch), ECUDA.
  * ===================================================================================================== */
@@ -491,7 +492,8 @@ typedef struct {
  * probabilities as pairs of fp16 (22 bits).  For a bf16 sequence
  * with 64 query rows per KV head or more (its new tokens times n_q_heads / n_kv_heads) the values and the ratio of their scale to
  * the largest one that 256 neighbouring rows see may be rounded to fp16 as well: a block whose scale is less than 2^-20 of
- * that loses bits (such sequences run on the tcgen05 kernel where that is the faster one, by their lengths). */
+ * that loses bits, and so does a key of the open block 2^31 smaller than that block's largest (such sequences run on the
+ * tcgen05 kernel where that is the faster one, by their lengths). */
 int echokv_quant_attention(const echokv_config* cfg, const echokv_quant_cache* cache, const echokv_score_options* options,
                            const void* q, int64_t q_stride, void* out, const int32_t* dev_block_table,
                            const int32_t* dev_seq_slots, const int32_t* dev_seq_lens, const int32_t* dev_cu_tokens, int B,

@@ -639,7 +639,9 @@ class QuantCache:
     def attention(self, q, block_table, seq_lens, cu_tokens=None, max_new: int = 1, seq_slots=None, softcap: float = 0.0,
                   alibi_slopes=None, prefix_lens=None, out=None, status=None, stream=None):
         """q [T][n_q_heads][d]: the new tokens of every sequence, which are its last ones and already appended (cu_tokens None:
-        one each).  max_new bounds the new tokens of any sequence.  Returns out [T][n_q_heads][d] in the storage type."""
+        one each).  max_new bounds the new tokens of any sequence; one with more gets zeros and a status.  Returns out
+        [T][n_q_heads][d] in the storage type, which may be q itself; rows behind the last sequence's stay as they are (in a new
+        tensor: anything)."""
         import torch
         cfg, T, B = self.cfg, q.shape[0], seq_lens.shape[0]
         qp, qs = _rows(q, T, cfg.n_q_heads, cfg.head_dim, self.tdtype, "q", cfg.device)
