@@ -490,10 +490,9 @@ typedef struct {
  * Scores and sums are fp32; codes enter the products exactly; bf16 queries as fp16 (exact around each row's power of two) with
  * probabilities rounded to fp16 (one below 2^-24 of its row's largest may count as 0 beside it), fp32 queries and their
  * probabilities as pairs of fp16 (22 bits).  For a bf16 sequence
- * with 64 query rows per KV head or more (its new tokens times n_q_heads / n_kv_heads) the values and the ratio of their scale to
- * the largest one that 256 neighbouring rows see may be rounded to fp16 as well: a block whose scale is less than 2^-20 of
- * that loses bits, and so does a key of the open block 2^31 smaller than that block's largest (such sequences run on the
- * tcgen05 kernel where that is the faster one, by their lengths). */
+ * with 64 query rows per KV head or more (its new tokens times n_q_heads / n_kv_heads) the values and their scales may be
+ * rounded to fp16 as well, and a key or value of the open block that is 2^-28 of that block's largest loses bits (such
+ * sequences run on the tcgen05 kernel where that is the faster one, by their lengths). */
 int echokv_quant_attention(const echokv_config* cfg, const echokv_quant_cache* cache, const echokv_score_options* options,
                            const void* q, int64_t q_stride, void* out, const int32_t* dev_block_table,
                            const int32_t* dev_seq_slots, const int32_t* dev_seq_lens, const int32_t* dev_cu_tokens, int B,

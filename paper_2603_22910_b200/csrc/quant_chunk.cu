@@ -17,14 +17,17 @@
 //                    warp keep the pages and scales of the tile's eight blocks.
 //   warp 15          issues the products, by one elected thread: S_x = Q_x K^T from shared memory, O_x += P_x V with P_x in tensor memory
 //                    over the first half of S_x.
-// Tensor memory: S_0 | S_1 | O_0 | O_1.  The K scale multiplies the score beside the row's own factor (one value per 16 columns);
-// V codes times (their scale / the largest scale the row can see) times 64 are below 2^15.
+// Tensor memory: S_0 | S_1 | O_0 | O_1.  The K scale multiplies the score beside the row's own factor (one value per 16 columns).
+// A V scale is split at the power of two above it: the rest of it times 64 multiplies the codes on their way to fp16 (below 2^15), the
+// power, in units of the item's largest, the probabilities, whose reference is per row: values that a row does not see have no
+// part in its range.  (With the whole scale on the codes, in units of the largest: 300 against 305 us plain, 397 both capped, but a
+// value 2^40 times the others took the rows before it to a hundred times their tolerance.)
 // Work: the key tiles of all items, with a cost of 4 tiles to each item, are laid end to end and cut into equal shares, one per CTA.
 // A share cuts at most two items; the parts of an item -- o / l, reference, l -- go to the workspace and a second kernel
 // joins them in the order of their keys.  (2 x 1024 tokens over 8192 keys, 256 items for 148 SMs: 433 -> 393 us; one sequence of 64
 // tokens over 32768 keys, 8 items: 630 -> 87 us.)  Every wait is bounded.
 // Bound: 128 exponentials per row and tile at 16 per clock and SM take twice the products' time.  Measured (2 x 1024 tokens over
-// 8192 keys, 32 / 8 heads, e4m3): 300 us = 860 TFLOP/s without a cap, 396 us = 650 with one; a tile of 128 keys takes both halves 2.4 us
+// 8192 keys, 32 / 8 heads, e4m3): 305 us = 845 TFLOP/s without a cap, 397 us = 649 with one; a tile of 128 keys takes both halves 2.4 us
 // where its products take 1.1 and its exponentials 1.1: each half's scores -> probabilities (1.45 us) -> products (1.0 us) chain is
 // longer than what the other half covers.  Tensor pipe 38 / 29 %, exponentials' pipe 38 / 30 %, issue slots 45 / 48 % busy.
 // (Scores in pieces of 64 keys, so that the next 64's products run while the softmax works on these: half as wide and
@@ -47,11 +50,12 @@ constexpr int kCkRing = 4;                         // scales and V references: s
 // is less than 2^-25 is 0 as fp16, while the sum (fp32) keeps it: over n keys up to n 2^-(24 + r) of the largest one's mass.  r =
 // log2 n - 13 holds that to 2^-11, what rounding a probability to fp16 does (up to r = 8, 2 million keys); r is 0 at least, which leaves
 // room for a sum 2^11 to 2^16 as large before the reference moves again.  Measured (2 x 1024 tokens over 8192 keys, scores of spread
-// 2.5): 299 us, 416 with r = 6, 343 if the first reference comes from 32 keys instead of 128.  (References 2^8 ABOVE the scores never move
-// here, 293 us, but with 0.9 of the mass on the first of 8192 keys the output is 6 % off, of 32768 keys half.)
+// 2.5): 299 us, 416 with r = 6, 343 if the first reference comes from 32 keys instead of 128 (V scales whole on the codes, as they were
+// then).  (References 2^8 ABOVE the scores never move here, 293 us, but with 0.9 of the mass on the first of 8192 keys the output is 6 % off, of 32768 keys half.)
 __device__ __forceinline__ float ck_below(int n_keys) { return (float)min(8, max(0, 32 - __clz(n_keys - 1) - 13)); }
 constexpr float kCkSumLimit = 65504.f;             // a row's 32 probabilities sum to less: each fits fp16
 constexpr float kCkVScale = 64.f;
+constexpr int kCkVSpan = 90;                      // V scales below 2^-90 of the item's largest share its unit (a sum of 2^-e times 2^11 pieces fits fp32)
 constexpr int kCkMaxCtas = 160;                    // (of the workspace's layout)
 constexpr int kCkMinShare = 3;                     // units per CTA at least
 constexpr int kCkMergeCols = 16;                   // features per thread of the merge
@@ -223,7 +227,7 @@ struct CkRow {
 // and instructions are its own too.
 template <int D>
 __device__ __noinline__ float2 careful_piece(const CkRow w, const int c, const int key0, const int n_vis, const bool has_output, float f0,
-                                             float f1, float m_ref, float l_run) {
+                                             float f1, const float4 v_exp, float m_ref, float l_run) {
   uint32_t sr[32], pk[16];
   tmem_st_wait();
   tmem_ld32_issue(w.s_addr + 32 * c, sr);
@@ -245,6 +249,9 @@ __device__ __noinline__ float2 careful_piece(const CkRow w, const int c, const i
 #pragma unroll
     for (int j = 0; j < 32; ++j) sr[j] = j < vis_c ? sr[j] : 0xff800000u;
   }
+  // (with the V scale's part, as the common way has it)
+#pragma unroll
+  for (int j = 0; j < 32; ++j) sr[j] = __float_as_uint(__uint_as_float(sr[j]) + (j < 16 ? v_exp.x : v_exp.z));
   float sum = 0.f;
 #pragma unroll 1
   for (int attempt = 0;; ++attempt) {
@@ -253,11 +260,11 @@ __device__ __noinline__ float2 careful_piece(const CkRow w, const int c, const i
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
       const float p0 = exp2_approx(__uint_as_float(sr[2 * j]) - m), p1 = exp2_approx(__uint_as_float(sr[2 * j + 1]) - m);
-      sums[j & 1] += p0 + p1;
+      sums[j >> 3] += p0 + p1;
       pk[j] = h2(p0, p1);
     }
-    sum = sums[0] + sums[1];
-    const bool move = !(sum < kCkSumLimit) || m_ref == -INFINITY;
+    sum = fmaf(sums[0], v_exp.y, sums[1] * v_exp.w);
+    const bool move = !(sums[0] + sums[1] < kCkSumLimit) || m_ref == -INFINITY;
     if (attempt > 0 || !__any_sync(0xffffffffu, move)) break;
     float alpha = 1.f;
     if (move) {
@@ -364,6 +371,7 @@ struct CkTail {
   unsigned long long pre[kCkThreads + 1];
   unsigned long long warp_sums[32];
   float k_scale[kCkRing][8];                       // [tile][16-key block]
+  alignas(16) float2 v_exp[kCkRing][8];                        // [tile][16-key block] how far the block's V scale is below the item's, (e, 2^-e), e <= 0
   float v_ref[kCkRing];                            // [item]
   unsigned long long share[2];                     // this CTA's units
   CkItem item[kCkThreads / 32];                    // every warp's present item (in registers it would spill)
@@ -728,10 +736,14 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       float open_back = 1.f;
       const bool open_bad = open_k >= 0x7f800000u || open_v >= 0x7f800000u;
       const float open_up = scale_up_to_half(__uint_as_float(open_k), &open_back);
-      if (!open_bad) v_top = fmaxf(v_top, __uint_as_float(open_v) * (1.f / 448.f));
+      const float open_scale = open_bad ? 0.f : __uint_as_float(open_v) * (1.f / 448.f);
+      v_top = fmaxf(v_top, open_scale);
       // the power of two above it
       const uint32_t ve = v_top > 0.f ? (__float_as_uint(v_top) >> 23) + 1 : 127u;
-      const float v_ref = __uint_as_float(ve << 23), v_inv = __uint_as_float((254 - ve) << 23);
+      const float v_ref = __uint_as_float(ve << 23);
+      // a block's values are held in units of the power of two above its own scale, the rest is its probabilities'
+      const auto v_exponent = [&](float scale) { return min(max((__float_as_uint(scale) >> 23) + 1, (uint32_t)max(1, (int)ve - kCkVSpan)), ve); };
+      const auto v_unit = [&](float scale) { return kCkVScale * __uint_as_float((254 - v_exponent(scale)) << 23); };
       // (the ring: item n + 4's value overwrites item n's when the tiles of items n + 1 to n + 3 have been written, two of
       // which the products have to have read, the first of them after the softmax warps took item n's result)
       if (ct == 0) t.v_ref[n_item % kCkRing] = v_ref * (1.f / kCkVScale);
@@ -767,6 +779,8 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         if (ct < 8) {
           if (open && tile * 8 + ct == n_full) ks_next = open_bad ? __uint_as_float(0x7fc00000u) : open_back;
           t.k_scale[T % kCkRing][ct] = vs_cur == vs_cur ? ks_next : vs_cur;
+          const uint32_t below = ve - v_exponent(open && tile * 8 + ct == n_full ? open_scale : vs_cur);
+          t.v_exp[T % kCkRing][ct] = make_float2(-(float)below, __uint_as_float((127u + below) << 23));
         }
         fence_proxy_async_smem();
         warp_arrive(&t.k_full[st]);
@@ -777,17 +791,18 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           fetch_k(tile + 1, page8);
         }
 
+        // what the values of this lane's block are multiplied by
+        const float ratio = vs_cur * v_unit(vs_cur);
+        const uint32_t r2_mine = h2(ratio, ratio);
         alive = __all_sync(0xffffffffu, ck_wait(&t.v_empty[st], parity, abort_flag, a.status));
         if (!alive) break;
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
           const int row = my_row + kRowStep * p, tok = tile * kCkTile + row, blk = tok / kQuantBlock;
-          const float v_scale = __shfl_sync(0xffffffffu, vs_cur, (row >> 4) & 7);
+          const uint32_t r2 = __shfl_sync(0xffffffffu, r2_mine, (row >> 4) & 7);
           if (row >= kCkTile) break;
           uint32_t w[8];
-          if (blk < n_codes && v_scale == v_scale) {
-            const float ratio = v_scale * v_inv * kCkVScale;
-            const uint32_t r2 = h2(ratio, ratio);
+          if (blk < n_codes && (r2 & 0x7fffu) <= 0x7c00u) {          // (not NaN)
             const uint32_t c4[4] = {vc[p].x, vc[p].y, vc[p].z, vc[p].w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -796,7 +811,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
               w[2 * e + 1] = mul_h2(codes_pair<FMT, 1>(x), r2);
             }
           } else if (blk >= n_codes && open && !open_bad && tok < it.s.len) {
-            open_row(1, tok - n_full * kQuantBlock, v_inv * kCkVScale, w);
+            open_row(1, tok - n_full * kQuantBlock, v_unit(open_scale), w);
           } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[e] = 0u;
@@ -922,27 +937,30 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
             bad = !(z <= (kMode == 1 ? 0.25f : 1.f)) && (!kMasked || vis_c > 0);
             f0 = f1 = cap_out;
           }
+          // p times 2^e of its block's V scale: what a row does not see has no part in its products' range
+          const float4 ve = *reinterpret_cast<const float4*>(&t.v_exp[T % kCkRing][2 * c]);
           uint32_t pk[16];
-          uint64_t sum2[2] = {0ull, 0ull};
-          const uint64_t nm = pack_f2(-m_ref, -m_ref);
+          uint64_t sum2[2] = {0ull, 0ull};           // of the first 16 keys, of the others
+          const uint64_t nm0 = pack_f2(ve.x - m_ref, ve.x - m_ref), nm1 = pack_f2(ve.z - m_ref, ve.z - m_ref);
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
             const float f = j < 8 ? f0 : f1;
             float y0, y1;
-            unpack_f2(fma_f2(pack_u2(sr[2 * j], sr[2 * j + 1]), pack_f2(f, f), nm), y0, y1);
+            unpack_f2(fma_f2(pack_u2(sr[2 * j], sr[2 * j + 1]), pack_f2(f, f), j < 8 ? nm0 : nm1), y0, y1);
             if (kMasked && !(seen >> (2 * j) & 1)) y0 = -INFINITY;
             if (kMasked && !(seen >> (2 * j + 1) & 1)) y1 = -INFINITY;
             const float p0 = exp2_approx(y0), p1 = exp2_approx(y1);
-            sum2[j & 1] = add_f2(sum2[j & 1], pack_f2(p0, p1));
+            sum2[j >> 3] = add_f2(sum2[j >> 3], pack_f2(p0, p1));
             pk[j] = h2(p0, p1);
           }
           float a0, a1, b0, b1;
           unpack_f2(sum2[0], a0, a1);
           unpack_f2(sum2[1], b0, b1);
-          const float sum = (a0 + a1) + (b0 + b1);
-          bad |= !(sum < kCkSumLimit);
+          a0 += a1;
+          b0 += b1;
+          bad |= !(a0 + b0 < kCkSumLimit);
           if (__any_sync(0xffffffffu, bad)) return false;
-          l_run += sum;
+          l_run += fmaf(a0, ve.y, b0 * ve.w);
           // over scores that have been read: columns 16 c .. of the tile's 128
           tmem_st16_regs(s_addr + 16 * c, pk);
           return true;
@@ -960,7 +978,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         };
         const auto careful = [&](int c) {
           const float2 r = careful_piece<D>(w, c, tile * kCkTile + 32 * c, n_vis, tile > it.t0, c_row * k_scale[2 * c], c_row * k_scale[2 * c + 1],
-                                            m_ref, l_run);
+                                            *reinterpret_cast<const float4*>(&t.v_exp[T % kCkRing][2 * c]), m_ref, l_run);
           m_ref = r.x;
           l_run = r.y;
         };
@@ -979,9 +997,14 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
               mx0 = fmaxf(mx0, __uint_as_float(sr[j]));
               mx1 = fmaxf(mx1, __uint_as_float(sr[16 + j]));
             }
-            mx = fmaxf(mx, fmaxf(mx0 * (c_row * k_scale[2 * c]), mx1 * (c_row * k_scale[2 * c + 1])));
+            mx0 *= c_row * k_scale[2 * c];
+            mx1 *= c_row * k_scale[2 * c + 1];
+            if (w.capped) {
+              mx0 = cap_out * tanh_f32(mx0 * cap_in);
+              mx1 = cap_out * tanh_f32(mx1 * cap_in);
+            }
+            mx = fmaxf(mx, fmaxf(mx0 + t.v_exp[T % kCkRing][2 * c].x, mx1 + t.v_exp[T % kCkRing][2 * c + 1].x));
           }
-          if (w.capped) mx = cap_out * tanh_f32(mx * cap_in);
           if (mx > -INFINITY) m_ref = ceilf(mx) - w.below;
         }
         int done = 0;

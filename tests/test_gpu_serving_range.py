@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from tests import serving_ref as R
-from tests.test_gpu_serving import Program, attend, check_attention, config, f64, sampled
+from tests.test_gpu_serving import EPS, Program, attend, check_attention, config, f64, sampled
 
 pytestmark = pytest.mark.gpu
 BASE = 0                # the feature that carries the scores' common part
@@ -137,3 +137,20 @@ def test_blocks_of_zero_values_beside_large_ones(dtype, size, scale):
         p.cache.v_scales[p.cache.v_scales < 1e-29] = 0.0
     q = p.rows(2, 4, 2.0)
     check_attention(p, [1, 1], q, attend(p, [1, 1], q))
+
+
+@pytest.mark.parametrize("size", [1e-12, 1e7, 1e12, 1e30])
+@pytest.mark.parametrize("d,n_q,n_kv,L,new,softcap", [(128, 8, 2, 900, 300, 0.0), (64, 32, 32, 1500, 700, 0.0), (128, 4, 1, 6007, 100, 20.0)])
+def test_a_large_value_that_the_first_rows_of_a_chunk_do_not_see(d, n_q, n_kv, L, new, softcap, size):
+    """Values change by `size` inside the chunk, at the end of a block and inside the open one: rows before that see ordinary ones."""
+    cfg = config(n_q=n_q, n_kv=n_kv, d=d, page=64, batch=1, pages=-(-L // 64), n_pages=-(-L // 64))
+    p = Program(cfg, "int8", seed=L)
+    p.step([L], *values(p, L, n_kv, [(0, 1.0), ((L - new // 2) // 16 * 16, size), ((L - new // 4) // 16 * 16, 1.0), (L - 2, size)]))
+    q = p.rows(new, n_q, 2.0)
+    out = attend(p, [new], q, softcap=softcap)
+    only = sorted(set(sampled(p.rng, new)) | {new - new // 2 - 17, new - new // 4 - 17, new - 3})
+    ref, seen = R.attend(f64(q), p.ref.values(p.ref.k[0]), p.ref.values(p.ref.v[0]), d ** -0.5, softcap, only=only)
+    # (2^-11: probabilities below fp16's normal numbers, see above)
+    tol = R.tolerance(ref, seen, L, EPS["bf16"], True, True, softcap) + 2.0 ** -11 * seen[..., 1:]
+    err = np.abs(f64(out) - ref)[only]
+    assert (err <= tol[only]).all(), float((err / tol[only]).max())
