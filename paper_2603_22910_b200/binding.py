@@ -22,6 +22,7 @@ ECHOKV_ENOWEIGHTS, ECHOKV_ECUDA, ECHOKV_ETIMEOUT, ECHOKV_EBADPAGE = -5, -6, -7, 
 ECHOKV_EUNSUPPORTED, ECHOKV_ENOTABLE, ECHOKV_EBADLENGTH, ECHOKV_ESCRATCH = -9, -10, -11, -12
 ECHOKV_INT8, ECHOKV_E4M3 = 0, 1
 ECHOKV_QUANT_BLOCK_TOKENS = 16
+ECHOKV_FP4_GROUP, ECHOKV_FP4_MAX_SELECT = 16, 1024
 QUANT_FORMATS = {"int8": ECHOKV_INT8, "e4m3": ECHOKV_E4M3}
 
 
@@ -62,6 +63,21 @@ class echokv_quant_sizes(C.Structure):
 class echokv_score_options(C.Structure):
     _fields_ = [("softcap", C.c_float), ("reserved", C.c_int32), ("alibi_slopes", C.c_void_p),
                 ("prefix_lens", C.c_void_p)]
+
+
+class echokv_fp4_cache(C.Structure):
+    _fields_ = [("blocks", C.c_void_p), ("bounds", C.c_void_p), ("bound_scales", C.c_void_p), ("k_unit", C.c_float),
+                ("v_unit", C.c_float)]
+
+
+class echokv_fp4_sizes(C.Structure):
+    _fields_ = [("blocks_bytes", C.c_uint64), ("bounds_bytes", C.c_uint64), ("bound_scales_bytes", C.c_uint64),
+                ("workspace_bytes", C.c_uint64)]
+
+
+class echokv_rotation(C.Structure):
+    _fields_ = [("theta", C.c_double), ("sections", C.POINTER(C.c_int32)), ("n_axes", C.c_int32), ("interleaved", C.c_int32),
+                ("rot_dim", C.c_int32), ("reserved", C.c_int32)]
 
 
 EXPORTS = {
@@ -126,6 +142,21 @@ EXPORTS = {
     "echokv_quant_attention": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_quant_cache), C.POINTER(echokv_score_options),
                                          C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
                                          C.c_int, C.c_int, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p]),
+    "echokv_query_fp4_sizes": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fp4_sizes)]),
+    "echokv_fp4_append": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fp4_cache), C.POINTER(echokv_rotation), C.c_void_p,
+                                    C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                    C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]),
+    "echokv_fp4_read": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fp4_cache), C.c_void_p, C.c_int, C.c_void_p, C.c_int64,
+                                  C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "echokv_fp4_attention": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fp4_cache), C.POINTER(echokv_score_options),
+                                       C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
+                                       C.c_int, C.c_int, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p]),
+    "echokv_fp4_select": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fp4_cache), C.c_void_p, C.c_int64, C.c_void_p,
+                                    C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p,
+                                    C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p]),
+    "echokv_fp4_sparse_attention": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fp4_cache), C.POINTER(echokv_score_options),
+                                              C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                              C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p]),
     "echokv_strerror": (C.c_char_p, [C.c_int]),
 }
 
@@ -662,6 +693,192 @@ class QuantCache:
                                             _dense(self.workspace, torch.uint8, self._ws_bytes, "workspace", cfg.device),
                                             self._ws_bytes, _dense(status, torch.int32, 1, "status", cfg.device),
                                             _stream_on(cfg.device, stream)), "echokv_quant_attention")
+        return out
+
+
+# ---- the same step over a cache held in 4 bits ---------------------------------------------------------------------
+class Rotation:
+    """Rotary positions for Fp4Cache.append: theta, and as in rotate() the sections of several position axes and rot_dim (a multiple of
+    16; 0: the whole head)."""
+    __slots__ = ("_c", "_sections", "n_axes")
+
+    def __init__(self, cfg: echokv_config, theta: float, n_axes: int = 1, sections=None, rot_dim: int = 0, interleaved: bool = False):
+        if sections is not None and len(sections) != n_axes:
+            raise ValueError("Rotation: one section per position axis")
+        half = (rot_dim or cfg.head_dim) // 2
+        if not 0 <= rot_dim <= cfg.head_dim or rot_dim % 16 or n_axes < 1 or (n_axes > 1 if sections is None else sum(sections) != half):
+            raise ValueError("Rotation: rot_dim is a multiple of 16 up to the head's, the sections sum to half of it")
+        self.n_axes = n_axes
+        self._sections = None if sections is None else (C.c_int32 * n_axes)(*sections)
+        self._c = echokv_rotation(theta, self._sections, n_axes, 1 if interleaved else 0, rot_dim, 0)
+
+
+def query_fp4_sizes(cfg: echokv_config) -> echokv_fp4_sizes:
+    out = echokv_fp4_sizes()
+    _check(lib().echokv_query_fp4_sizes(C.byref(cfg), C.byref(out)), "echokv_query_fp4_sizes")
+    return out
+
+
+class Fp4Cache:
+    """One layer's cache in 4 bits: blocks uint8 [n_pages][n_kv_heads][page_tokens / 16][18 d] and, for select_pages, the bounds of
+    every page's keys, int8 [n_pages][n_kv_heads][2][d] around fp32 scales [n_pages][n_kv_heads] (`selection` False: none are kept).
+    Allocates them unless they are given; `workspace` is best shared by the layers of a model (calls that share one must not overlap
+    on the device).  k_unit, v_unit: the magnitudes of keys and values are held around them (see echokv.h).  The other tensors
+    are the cache's for its life."""
+    _FIXED = frozenset(("cfg", "blocks", "bounds", "bound_scales", "k_unit", "v_unit"))
+
+    def __setattr__(self, name, value):
+        if name in self._FIXED and name in self.__dict__:
+            raise AttributeError("%s: the library holds it; make a new Fp4Cache" % name)
+        self.__dict__[name] = value
+
+    def __init__(self, cfg: echokv_config, k_unit: float = 1.0, v_unit: float = 1.0, blocks=None, bounds=None, bound_scales=None,
+                 selection: bool = True, workspace=None):
+        import torch
+        self.cfg, self.tdtype, self.k_unit, self.v_unit = cfg, _dtype(cfg), k_unit, v_unit
+        self.sizes = sizes = query_fp4_sizes(cfg)
+        if not all(2.0 ** -60 <= u <= 2.0 ** 60 for u in (k_unit, v_unit)):
+            raise ValueError("k_unit, v_unit: between 2^-60 and 2^60")
+        if (bounds is None) != (bound_scales is None) or (bounds is not None and not selection):
+            raise ValueError("bounds and bound_scales go together, and with selection")
+        self._ws_bytes = sizes.workspace_bytes
+        dev = torch.device("cuda", cfg.device)
+        H, P, d, N = cfg.n_kv_heads, cfg.page_tokens, cfg.head_dim, cfg.n_pages
+
+        def held(t, shape, dtype, name):
+            if t is None:
+                return torch.zeros(shape, dtype=dtype, device=dev)
+            if tuple(t.shape) != shape or t.dtype is not dtype or t.get_device() != cfg.device or not t.is_contiguous():
+                raise ValueError("%s: a contiguous %s device tensor of shape %s is needed, on cuda:%d" % (name, dtype, shape, cfg.device))
+            return t
+        self.blocks = held(blocks, (N, H, P // 16, 18 * d), torch.uint8, "blocks")
+        self.bounds = held(bounds, (N, H, 2, d), torch.int8, "bounds") if selection else None
+        self.bound_scales = held(bound_scales, (N, H), torch.float32, "bound_scales") if selection else None
+        self.workspace = torch.empty(sizes.workspace_bytes, dtype=torch.uint8, device=dev) if workspace is None else workspace
+        _dense(self.workspace, torch.uint8, self._ws_bytes, "workspace", cfg.device)
+        self._c = echokv_fp4_cache(self.blocks.data_ptr(), _ptr(self.bounds), _ptr(self.bound_scales), k_unit, v_unit)
+
+    def append(self, k_new, v_new, slot_map, q=None, rotation: Rotation | None = None, positions=None, q_out=None, status=None,
+               stream=None):
+        """k_new, v_new [T][n_kv_heads][d] (rows may be slices of a wider tensor) into the pool rows slot_map (plan_tokens').  With a
+        rotation, keys are turned to positions (int32 [T] or [n_axes][T]) on their way, and q [T][n_q_heads][d], if given, into the
+        returned q_out (which may be q)."""
+        import torch
+        cfg, T, d = self.cfg, k_new.shape[0], self.cfg.head_dim
+        if q is not None and rotation is None:
+            raise ValueError("append: queries are turned, so a rotation is needed")
+        if (rotation is None) != (positions is None):
+            raise ValueError("append: rotation and positions go together")
+        kp, ks = _rows(k_new, T, cfg.n_kv_heads, d, self.tdtype, "k_new", cfg.device)
+        vp, vs = _rows(v_new, T, cfg.n_kv_heads, d, self.tdtype, "v_new", cfg.device)
+        qp = qo = rot = pos = None
+        qs = qos = 0
+        if rotation is not None:
+            if (1 if positions.dim() == 1 else positions.shape[0]) != rotation.n_axes or positions.shape[-1] != T:
+                raise ValueError("append: positions are [n_axes][n_tokens]")
+            rot, pos = C.byref(rotation._c), _dense(positions, torch.int32, rotation.n_axes * T, "positions", cfg.device)
+        if q is not None:
+            qp, qs = _rows(q, T, cfg.n_q_heads, d, self.tdtype, "q", cfg.device)
+            if q_out is None:
+                with _memory_of(stream):
+                    q_out = q.new_empty((T, cfg.n_q_heads, d))
+                qo, qos = q_out.data_ptr(), cfg.n_q_heads * d
+            else:
+                qo, qos = _rows(q_out, T, cfg.n_q_heads, d, self.tdtype, "q_out", cfg.device)
+        _check(lib().echokv_fp4_append(C.byref(cfg), C.byref(self._c), rot, qp, qs, qo, qos, kp, ks, vp, vs, pos,
+                                       _dense(slot_map, torch.int64, T, "slot_map", cfg.device), T,
+                                       _dense(status, torch.int32, 1, "status", cfg.device), _stream_on(cfg.device, stream)), "echokv_fp4_append")
+        return q_out if q is not None else None
+
+    def read(self, slot_map, k_out=None, v_out=None, status=None, stream=None):
+        """The rows that the cache holds in the pool rows slot_map: (k, v) [T][n_kv_heads][d] in the storage type, new tensors unless
+        given."""
+        import torch
+        cfg, T, H, d = self.cfg, slot_map.shape[0], self.cfg.n_kv_heads, self.cfg.head_dim
+        with _memory_of(stream):
+            k_out = torch.empty((T, H, d), dtype=self.tdtype, device=slot_map.device) if k_out is None else k_out
+            v_out = torch.empty((T, H, d), dtype=self.tdtype, device=slot_map.device) if v_out is None else v_out
+        at = _rows(k_out, T, H, d, self.tdtype, "k_out", cfg.device) + _rows(v_out, T, H, d, self.tdtype, "v_out", cfg.device)
+        _check(lib().echokv_fp4_read(C.byref(cfg), C.byref(self._c), _dense(slot_map, torch.int64, T, "slot_map", cfg.device), T, *at,
+                                     _dense(status, torch.int32, 1, "status", cfg.device), _stream_on(cfg.device, stream)), "echokv_fp4_read")
+        return k_out, v_out
+
+    def _queries(self, q, out, stream):
+        cfg, T = self.cfg, q.shape[0]
+        qp, qs = _rows(q, T, cfg.n_q_heads, cfg.head_dim, self.tdtype, "q", cfg.device)
+        if out is None:
+            with _memory_of(stream):
+                out = q.new_empty((T, cfg.n_q_heads, cfg.head_dim))
+            return qp, qs, out, out.data_ptr()
+        return qp, qs, out, _dense(out, self.tdtype, T * cfg.n_q_heads * cfg.head_dim, "out", cfg.device)
+
+    def attention(self, q, block_table, seq_lens, cu_tokens=None, max_new: int = 1, seq_slots=None, softcap: float = 0.0,
+                  alibi_slopes=None, prefix_lens=None, out=None, status=None, stream=None):
+        """As QuantCache.attention: q [T][n_q_heads][d], the new tokens of every sequence, attend the whole of it."""
+        import torch
+        cfg, T, B = self.cfg, q.shape[0], seq_lens.shape[0]
+        qp, qs, out, op = self._queries(q, out, stream)
+        opts = None
+        if softcap or alibi_slopes is not None or prefix_lens is not None:
+            opts = C.byref(echokv_score_options(softcap, 0, _dense(alibi_slopes, torch.float32, cfg.n_q_heads, "alibi_slopes", cfg.device),
+                                                _dense(prefix_lens, torch.int32, B, "prefix_lens", cfg.device)))
+        _check(lib().echokv_fp4_attention(C.byref(cfg), C.byref(self._c), opts, qp, qs, op,
+                                          _dense(block_table, torch.int32, cfg.max_batch * cfg.max_pages_per_seq, "block_table", cfg.device),
+                                          _dense(seq_slots, torch.int32, B, "seq_slots", cfg.device), _dense(seq_lens, torch.int32, B, "seq_lens", cfg.device),
+                                          _dense(cu_tokens, torch.int32, B + 1, "cu_tokens", cfg.device), B, T, max_new,
+                                          _dense(self.workspace, torch.uint8, self._ws_bytes, "workspace", cfg.device), self._ws_bytes,
+                                          _dense(status, torch.int32, 1, "status", cfg.device), _stream_on(cfg.device, stream)),
+               "echokv_fp4_attention")
+        return out
+
+    def _batch(self, seq_slots):
+        return self.cfg.max_batch if seq_slots is None else seq_slots.shape[0]
+
+    def select_pages(self, q, block_table, token_seqs, positions, n_select: int, n_first: int = 1, n_recent: int = 1, seq_slots=None,
+                     out=None, status=None, stream=None):
+        """The n_select pages of its sequence that each token reads, per KV head: int32 [T][n_kv_heads][n_select], ascending, -1 behind
+        the last one -- the first n_first, the last n_recent, and those with the largest scores (see echokv.h).  token_seqs, positions:
+        plan_tokens'."""
+        import torch
+        cfg, T, B = self.cfg, q.shape[0], self._batch(seq_slots)
+        if self.bounds is None:
+            raise ValueError("select_pages: a cache made without selection has no bounds")
+        qp, qs = _rows(q, T, cfg.n_q_heads, cfg.head_dim, self.tdtype, "q", cfg.device)
+        if out is None:
+            with _memory_of(stream):
+                out = torch.empty((T, cfg.n_kv_heads, n_select), dtype=torch.int32, device=q.device)
+        _check(lib().echokv_fp4_select(C.byref(cfg), C.byref(self._c), qp, qs,
+                                       _dense(block_table, torch.int32, cfg.max_batch * cfg.max_pages_per_seq, "block_table", cfg.device),
+                                       _dense(seq_slots, torch.int32, B, "seq_slots", cfg.device),
+                                       _dense(token_seqs, torch.int32, T, "token_seqs", cfg.device),
+                                       _dense(positions, torch.int32, T, "positions", cfg.device), B, T, n_select, n_first, n_recent,
+                                       _dense(out, torch.int32, T * cfg.n_kv_heads * n_select, "out", cfg.device),
+                                       _dense(self.workspace, torch.uint8, self._ws_bytes, "workspace", cfg.device), self._ws_bytes,
+                                       _dense(status, torch.int32, 1, "status", cfg.device), _stream_on(cfg.device, stream)),
+               "echokv_fp4_select")
+        return out
+
+    def sparse_attention(self, q, block_table, token_seqs, positions, pages, seq_slots=None, softcap: float = 0.0, alibi_slopes=None,
+                         out=None, status=None, stream=None):
+        """q [T][n_q_heads][d]: every token attends the pages that pages [T][n_kv_heads][n_select] lists of its sequence (select_pages', or
+        any others), keys up to its own position.  Rows of tokens with sequence -1 stay as they are (in a new tensor: anything)."""
+        import torch
+        cfg, T, B = self.cfg, q.shape[0], self._batch(seq_slots)
+        if pages.dim() != 3 or pages.shape[0] != T or pages.shape[1] != cfg.n_kv_heads:
+            raise ValueError("pages: [%d tokens][%d][n_select] is needed" % (T, cfg.n_kv_heads))
+        qp, qs, out, op = self._queries(q, out, stream)
+        opts = None
+        if softcap or alibi_slopes is not None:
+            opts = C.byref(echokv_score_options(softcap, 0, _dense(alibi_slopes, torch.float32, cfg.n_q_heads, "alibi_slopes", cfg.device), None))
+        _check(lib().echokv_fp4_sparse_attention(C.byref(cfg), C.byref(self._c), opts, qp, qs, op,
+                                                 _dense(block_table, torch.int32, cfg.max_batch * cfg.max_pages_per_seq, "block_table", cfg.device),
+                                                 _dense(seq_slots, torch.int32, B, "seq_slots", cfg.device),
+                                                 _dense(token_seqs, torch.int32, T, "token_seqs", cfg.device),
+                                                 _dense(positions, torch.int32, T, "positions", cfg.device),
+                                                 _dense(pages, torch.int32, pages.numel(), "pages", cfg.device), pages.shape[2], B, T,
+                                                 _dense(self.workspace, torch.uint8, self._ws_bytes, "workspace", cfg.device), self._ws_bytes,
+                                                 _dense(status, torch.int32, 1, "status", cfg.device), _stream_on(cfg.device, stream)),
+               "echokv_fp4_sparse_attention")
         return out
 
 

@@ -1,0 +1,401 @@
+// Append to a cache held in 4 bits with the rotation on the way, the bounds of the pages that it touches, and rows read back.
+//
+//   y = R(position) x,   s = e4m3(max |y| / (6 unit)),   code = e2m1(y / (s unit))        for every 16 features of a token
+//
+// Bytes bound it: every row is read once, queries written once, keys and values in 9/32 of their bytes.  A block takes a few tokens.  Its
+// threads first form the (cos, sin) of the tokens' rot / 2 angles in shared memory, once for all heads of q and k: in fp64, rounded to
+// fp32 once, so that the codes are those of the exact angle but for the last bit of a cosine.  A unit of q is 8 features of the first
+// half of a rotation and their partners of the second.  A unit of k and v is a group of 16 features of both: the thread reads its
+// key group and that group's partners (which another thread of the warp has as its own, so they come from the first level cache), turns
+// it, and has all it needs for the scale without asking other threads.  A token that is not finite is told by a vote.
+// The format has no rows that wait: a token is written where it belongs and no other token matters.
+#include "fp4_common.cuh"
+
+namespace echokv {
+
+namespace {
+
+constexpr int kFaThreads = 256;
+constexpr int kFaTokens = 4;                       // tokens per block: 4 x 64 angles = one per thread
+
+// 8 elements in the storage type as they are in memory
+template <typename T>
+struct Eight {
+  static constexpr int W = sizeof(T) * 8 / 16;
+  uint4 w[W];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
+  }
+  __device__ __forceinline__ void store(T* p) const {
+#pragma unroll
+    for (int i = 0; i < W; ++i) reinterpret_cast<uint4*>(p)[i] = w[i];
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+#pragma unroll
+    for (int i = 0; i < W; ++i) Vec16<T>::load(reinterpret_cast<const T*>(&w[i]), v + i * (8 / W));
+  }
+};
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; i += Vec16<T>::N) store16<T>(p + i, v + i);
+}
+
+// (cos, sin) of frequency index j of token t: two neighbours of a piece of 8 side by side, pieces next, so that what lanes of
+// neighbouring pieces read together is contiguous
+__device__ __forceinline__ int turn_at(int j, int pieces) { return (((j & 7) >> 1) * pieces + (j >> 3)) * 2 + (j & 1); }
+// 8 features of one half of a rotation (sign -1: the first, +1: the second) and their partners -> turned, every step rounded
+__device__ __forceinline__ void turn8(float (&x)[8], const float (&partner)[8], const float2* cs, int piece, int pieces, float sign) {
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const float4 w = *reinterpret_cast<const float4*>(&cs[((e >> 1) * pieces + piece) * 2]);
+    x[e] = __fadd_rn(__fmul_rn(x[e], w.x), sign * __fmul_rn(partner[e], w.y));
+    x[e + 1] = __fadd_rn(__fmul_rn(x[e + 1], w.z), sign * __fmul_rn(partner[e + 1], w.w));
+  }
+}
+
+// 16 values -> their scale's code and 8 bytes of codes
+struct Group {
+  uint32_t scale;
+  uint2 codes;
+};
+__device__ __forceinline__ float largest(const float (&x)[2][8]) {
+  uint32_t top = 0;                                // (magnitudes compare as integers, infinities and NaN above everything finite)
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(x[i >> 3][i & 7]) & 0x7fffffffu);
+  return __uint_as_float(top);
+}
+__device__ __forceinline__ Group encode(const float (&x)[2][8], float a, float unit6, float inv_unit) {
+  Group r;
+  r.scale = e4m3_code(__fmul_rn(a, unit6));
+  const float s = h2_float(e4m3_scales(r.scale)).x;
+  const float m = s > 0.f ? __fdiv_rn(inv_unit, s) : 0.f;
+  uint32_t w[2] = {0u, 0u};
+#pragma unroll
+  for (int i = 0; i < 16; i += 2) w[i >> 3] |= e2m1_byte(__fmul_rn(x[i >> 3][i & 7], m), __fmul_rn(x[i >> 3][(i & 7) + 1], m)) << (4 * (i & 7));
+  r.codes = make_uint2(w[0], w[1]);
+  return r;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kFaThreads, 4) fp4_append_kernel(const __grid_constant__ Fp4AppendArgs a, int tokens_per_block) {
+  constexpr int G = D / kFp4Group;                 // groups of a head (4 or 8 lanes side by side)
+  __shared__ __align__(16) float2 cs[kFaTokens][64];
+  const int half = a.rot_dim >> 1, pieces = half >> 3, tid = threadIdx.x, lane = tid & 31;
+  const int t0 = blockIdx.x * tokens_per_block, nt = min(tokens_per_block, a.n_tokens - t0);
+  const Fp4Geom& g = a.g;
+  const int H = g.n_kv_heads;
+  for (int i = tid; i < nt * half; i += kFaThreads) {
+    const int t = i / half, j = i - t * half;
+    const double turns = (double)a.pos[(long long)a.axis[j] * a.n_tokens + t0 + t] * a.turns[j];
+    double s, c;
+    sincospi(2.0 * (turns - rint(turns)), &s, &c);
+    cs[t][turn_at(j, pieces)] = make_float2((float)c, (float)s);
+  }
+  __syncthreads();
+
+  // ---- keys and values
+  const int items = nt * H * G, steps = (items + kFaThreads - 1) / kFaThreads;
+#pragma unroll 1
+  for (int step = 0; step < steps; ++step) {
+    const int i = step * kFaThreads + tid;
+    const bool live = i < items;                   // (a head's G lanes are all live or none is)
+    const int u = live ? i / G : 0, grp = i % G, t = u / H, h = u - t * H;
+    const long long row = live ? a.slot_map[t0 + t] : -1;
+    const bool in_pool = row >= 0 && (row >> g.page_shift) < g.n_pages;
+    if (live && row != -1 && !in_pool) report_opt(a.status, ECHOKV_EBADPAGE);
+    Eight<T> k[2], p[2], v[2];
+    float x[2][8], y[2][8];
+    bool second[2], turn[2];
+    if (in_pool) {
+      const T* kp = static_cast<const T*>(a.x[0]) + (long long)(t0 + t) * a.stride[0] + h * D;
+      const T* vp = static_cast<const T*>(a.x[1]) + (long long)(t0 + t) * a.stride[1] + h * D + grp * kFp4Group;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int f = grp * kFp4Group + 8 * e;
+        second[e] = f >= half;
+        turn[e] = f < a.rot_dim;
+        k[e].load(kp + f);
+        p[e].load(kp + (turn[e] ? second[e] ? f - half : f + half : f));
+        v[e].load(vp + 8 * e);
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int f = grp * kFp4Group + 8 * e;
+        k[e].get(x[e]);
+        if (turn[e]) {
+          float w[8];
+          p[e].get(w);
+          turn8(x[e], w, cs[t], (second[e] ? f - half : f) >> 3, pieces, second[e] ? 1.f : -1.f);
+        }
+        v[e].get(y[e]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e >> 3][e & 7] = y[e >> 3][e & 7] = 0.f;
+    }
+    const float ka = largest(x), va = largest(y);
+    const uint32_t vote = __ballot_sync(0xffffffffu, max(__float_as_uint(ka), __float_as_uint(va)) >= 0x7f800000u);
+    if (!in_pool) continue;
+    Group kg = encode(x, ka, a.unit6[0], a.inv_unit[0]), vg = encode(y, va, a.unit6[1], a.inv_unit[1]);
+    if (vote >> (lane & ~(G - 1)) & ((1u << G) - 1)) {
+      kg.scale = kE4m3Nan;
+      vg.scale = 0u;
+      kg.codes = vg.codes = make_uint2(0u, 0u);
+    }
+    const int inside = (int)(row & (g.page_tokens - 1)), r = inside & 15, f = grp * kFp4Group;
+    unsigned char* blk = g.blocks + (((row >> g.page_shift) * H + h) * (g.page_tokens / 16) + (inside >> 4)) * fp4_block_bytes(D);
+    *reinterpret_cast<uint2*>(blk + fp4_k_at(D, r, f)) = kg.codes;
+    if (D == 128) {
+      *reinterpret_cast<uint2*>(blk + fp4_v_at(D, r, f)) = vg.codes;
+    } else {
+      *reinterpret_cast<uint32_t*>(blk + fp4_v_at(D, r, f)) = vg.codes.x;
+      *reinterpret_cast<uint32_t*>(blk + fp4_v_at(D, r, f + 8)) = vg.codes.y;
+    }
+    blk[fp4_ks_at(D, r, f)] = (unsigned char)kg.scale;
+    blk[fp4_vs_at(D, r, f)] = (unsigned char)vg.scale;
+  }
+
+  // ---- queries: 8 features and their partners, or two pieces of what is only copied
+  if (a.q == nullptr) return;
+  constexpr int U = D / 16, kStep = kFaThreads / U, kBatch = sizeof(T) == 2 ? 2 : 1;
+  const int c = tid % U;
+  const bool turn = c < pieces;
+  const int e0 = turn ? c * 8 : a.rot_dim + 2 * (c - pieces) * 8, e1 = turn ? half + c * 8 : e0 + 8;
+  if (!turn && a.q == a.q_out) return;
+  const int n = nt * a.n_q_heads;
+#pragma unroll 1
+  for (int u = tid / U; u < n; u += kBatch * kStep) {
+    Eight<T> x[kBatch][2];
+    T* dst[kBatch];
+    int tok[kBatch];
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      const int at = u + b * kStep;
+      tok[b] = at / a.n_q_heads;
+      dst[b] = nullptr;
+      if (at < n) {
+        const int head = at - tok[b] * a.n_q_heads;
+        const T* src = static_cast<const T*>(a.q) + (long long)(t0 + tok[b]) * a.q_stride + head * D;
+        dst[b] = static_cast<T*>(a.q_out) + (long long)(t0 + tok[b]) * a.q_out_stride + head * D;
+        x[b][0].load(src + e0);
+        x[b][1].load(src + e1);
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      if (dst[b] == nullptr) continue;
+      if (turn) {
+        float y0[8], y1[8], z0[8], z1[8];
+        x[b][0].get(y0);
+        x[b][1].get(y1);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          z0[e] = y0[e];
+          z1[e] = y1[e];
+        }
+        turn8(z0, y1, cs[tok[b]], c, pieces, -1.f);
+        turn8(z1, y0, cs[tok[b]], c, pieces, 1.f);
+        store8<T>(dst[b] + e0, z0);
+        store8<T>(dst[b] + e1, z1);
+      } else {
+        x[b][0].store(dst[b] + e0);
+        x[b][1].store(dst[b] + e1);
+      }
+    }
+  }
+}
+
+// Bounds of the pages that the call touched: a block looks at 32 tokens for the last ones of their pages; a warp takes such a page for
+// one head, eight tokens at a time (a lane: a quarter of a token's features), and joins its lanes at the end.  Reads what the
+// first kernel wrote, from the second level cache.
+constexpr int kFbWarps = 8;
+
+template <int D>
+__global__ void __launch_bounds__(kFbWarps * 32) fp4_bounds_kernel(const __grid_constant__ Fp4AppendArgs a) {
+  constexpr int N = D / 8;                         // feature pairs of a lane
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
+  const Fp4Geom& g = a.g;
+  const int H = g.n_kv_heads;
+  const int worker = blockIdx.y * kFbWarps + warp, workers = gridDim.y * kFbWarps;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const auto row_of = [&](long long i) {
+    const long long row = i < a.n_tokens ? a.slot_map[i] : -1;
+    return row >= 0 && (row >> g.page_shift) < g.n_pages ? row : -1;
+  };
+  const long long i = (long long)blockIdx.x * 32 + lane, mine = row_of(i);
+  bool last = mine >= 0;
+  if (last) {
+    // the next token that has a row, if one of this page can come
+    long long next = -1;
+    const int left = g.page_tokens - 1 - (int)(mine & (g.page_tokens - 1));
+    for (int j = 1; j <= left && next < 0 && i + j < a.n_tokens; ++j) next = row_of(i + j);
+    last = next < 0 || (next >> g.page_shift) != (mine >> g.page_shift);
+  }
+  uint32_t pages = __ballot_sync(0xffffffffu, last);
+  for (int at = 0; pages; pages &= pages - 1, ++at) {
+    const long long row = __shfl_sync(0xffffffffu, mine, __ffs(pages) - 1);
+    const long long page = row >> g.page_shift;
+    const int n = (int)(row & (g.page_tokens - 1)) + 1;
+    for (int h = (worker + workers - at * H % workers) % workers; h < H; h += workers) {
+      const unsigned char* blk = g.blocks + (page * H + h) * (g.page_tokens / 16) * fp4_block_bytes(D);
+      __half2 top[N], low[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        top[e] = __half2half2(__ushort_as_half(0xfc00));        // -inf
+        low[e] = __half2half2(__ushort_as_half(0x7c00));
+      }
+      bool nan = false;
+#pragma unroll 2
+      for (int tok = r; tok < n; tok += 8) {
+        const unsigned char* b = blk + (tok >> 4) * fp4_block_bytes(D);
+        uint32_t w[D / 32];
+        if constexpr (D == 128) {
+          const uint4 v = *reinterpret_cast<const uint4*>(b + fp4_k_at(D, tok & 15, c * (D / 4)));
+          w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        } else {
+          const uint2 v = *reinterpret_cast<const uint2*>(b + fp4_k_at(D, tok & 15, c * (D / 4)));
+          w[0] = v.x; w[1] = v.y;
+        }
+#pragma unroll
+        for (int q = 0; q < D / 64; ++q) {         // groups of the lane
+          const uint32_t code = b[fp4_ks_at(D, tok & 15, c * (D / 4) + 16 * q)];
+          nan |= (code & 0x7fu) == kE4m3Nan;
+          const uint32_t s = e4m3_scales(code | code << 8);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const uint32_t x = w[2 * q + (e >> 2)] >> (8 * (e & 3)), y = fp4_mul(e2m1_pair<0>(x), s);
+            const __half2 z = *reinterpret_cast<const __half2*>(&y);
+            top[8 * q + e] = __hmax2(top[8 * q + e], z);
+            low[8 * q + e] = __hmin2(low[8 * q + e], z);
+          }
+        }
+      }
+      float most = 0.f;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+          top[e] = __hmax2(top[e], __shfl_xor_sync(0xffffffffu, top[e], o));
+          low[e] = __hmin2(low[e], __shfl_xor_sync(0xffffffffu, low[e], o));
+        }
+        const float2 x = __half22float2(top[e]), y = __half22float2(low[e]);
+        most = fmaxf(most, fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(y.x), fabsf(y.y))));
+      }
+      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+      nan = __any_sync(0xffffffffu, nan);
+      const float scale = fmaxf(__fmul_rn(most, 1.f / 127.f), 0x1p-60f), inv = nan ? 0.f : __frcp_rn(scale);
+      // (a lane writes N / 4 of the features that its quarter has: pairs r N / 8 and on)
+      const auto code = [&](float x) { return (uint32_t)min(127, max(-127, nan ? 0 : __float2int_rn(__fmul_rn(x, inv)))) & 0xffu; };
+      int8_t* out = g.bounds + (page * H + h) * 2 * D + c * (D / 4) + r * (N / 4);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {                // (registers have no index: the lane's own r picks one of eight)
+        if (k != r) continue;
+        uint32_t wt = 0, wl = 0;
+#pragma unroll
+        for (int e = 0; e < N / 8; ++e) {
+          const float2 x = __half22float2(top[k * (N / 8) + e]), y = __half22float2(low[k * (N / 8) + e]);
+          wt |= (code(x.x) | code(x.y) << 8) << (16 * e);
+          wl |= (code(y.x) | code(y.y) << 8) << (16 * e);
+        }
+        if constexpr (D == 128) {
+          *reinterpret_cast<uint32_t*>(out) = wt;
+          *reinterpret_cast<uint32_t*>(out + D) = wl;
+        } else {
+          *reinterpret_cast<uint16_t*>(out) = (uint16_t)wt;
+          *reinterpret_cast<uint16_t*>(out + D) = (uint16_t)wl;
+        }
+      }
+      if (lane == 0) g.bound_scales[page * H + h] = nan ? __uint_as_float(0x7fc00000u) : scale;
+    }
+  }
+}
+
+// Rows back: a thread per group of 16 features of a token and head, key and value.
+template <typename T, int D>
+__global__ void __launch_bounds__(kFaThreads) fp4_read_kernel(const __grid_constant__ Fp4ReadArgs a) {
+  constexpr int G = D / kFp4Group;
+  const Fp4Geom& g = a.g;
+  const int H = g.n_kv_heads;
+  const long long i = (long long)blockIdx.x * kFaThreads + threadIdx.x;
+  if (i >= (long long)a.n_tokens * H * G) return;
+  const int grp = (int)(i % G), f = grp * kFp4Group;
+  const int t = (int)(i / (G * H)), h = (int)(i / G) - t * H;
+  const long long row = a.slot_map[t];
+  const bool in_pool = row >= 0 && (row >> g.page_shift) < g.n_pages;
+  if (row != -1 && !in_pool) report_opt(a.status, ECHOKV_EBADPAGE);
+  uint32_t w[2][2] = {}, s[2] = {};
+  if (in_pool) {
+    const int inside = (int)(row & (g.page_tokens - 1)), r = inside & 15;
+    const unsigned char* blk = g.blocks + (((row >> g.page_shift) * H + h) * (g.page_tokens / 16) + (inside >> 4)) * fp4_block_bytes(D);
+    const uint2 k = *reinterpret_cast<const uint2*>(blk + fp4_k_at(D, r, f));
+    w[0][0] = k.x; w[0][1] = k.y;
+    w[1][0] = *reinterpret_cast<const uint32_t*>(blk + fp4_v_at(D, r, f));
+    w[1][1] = *reinterpret_cast<const uint32_t*>(blk + fp4_v_at(D, r, f + 8));
+    s[0] = blk[fp4_ks_at(D, r, f)];
+    s[1] = blk[fp4_vs_at(D, r, f)];
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    if (a.out[k] == nullptr) continue;
+    const uint32_t s2 = e4m3_scales(s[k] | s[k] << 8);
+    T* dst = static_cast<T*>(a.out[k]) + (long long)t * a.stride[k] + h * D + f;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 x = h2_float(fp4_mul(e2m1_pair<0>(w[k][p] >> (8 * e)), s2));
+        v[2 * e] = __fmul_rn(x.x, a.unit[k]);
+        v[2 * e + 1] = __fmul_rn(x.y, a.unit[k]);
+      }
+      store8<T>(dst + 8 * p, v);
+    }
+  }
+}
+
+template <typename T, int D>
+cudaError_t launch_append(const Fp4AppendArgs& a, int sm_count, cudaStream_t stream) {
+  // few tokens: one per block, so that a decode step's rows spread over the SMs
+  const int per_block = a.n_tokens <= 4 * sm_count ? 1 : kFaTokens;
+  fp4_append_kernel<T, D><<<(unsigned)((a.n_tokens + per_block - 1) / per_block), kFaThreads, 0, stream>>>(a, per_block);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess || a.g.bounds == nullptr) return e;
+  cudaLaunchConfig_t cfg = {};
+  // (few tokens, each the last one of its page: the heads of a page over several blocks)
+  const int blocks = (a.n_tokens + 31) / 32;
+  cfg.gridDim = dim3(blocks, blocks >= sm_count ? 1 : min((32 * a.g.n_kv_heads + kFbWarps - 1) / kFbWarps, (2 * sm_count + blocks - 1) / blocks));
+  cfg.blockDim = dim3(kFbWarps * 32);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, fp4_bounds_kernel<D>, a);
+}
+
+}  // namespace
+
+cudaError_t launch_fp4_append(const Fp4AppendArgs& a, int sm_count, cudaStream_t stream) {
+  if (a.dtype == ECHOKV_BF16) return a.g.head_dim == 128 ? launch_append<__nv_bfloat16, 128>(a, sm_count, stream) : launch_append<__nv_bfloat16, 64>(a, sm_count, stream);
+  return a.g.head_dim == 128 ? launch_append<float, 128>(a, sm_count, stream) : launch_append<float, 64>(a, sm_count, stream);
+}
+
+cudaError_t launch_fp4_read(const Fp4ReadArgs& a, cudaStream_t stream) {
+  const long long n = (long long)a.n_tokens * a.g.n_kv_heads * (a.g.head_dim / kFp4Group);
+  const unsigned grid = (unsigned)((n + kFaThreads - 1) / kFaThreads);
+  const bool wide = a.g.head_dim == 128;
+  if (a.dtype == ECHOKV_BF16) {
+    if (wide) fp4_read_kernel<__nv_bfloat16, 128><<<grid, kFaThreads, 0, stream>>>(a);
+    else fp4_read_kernel<__nv_bfloat16, 64><<<grid, kFaThreads, 0, stream>>>(a);
+  } else {
+    if (wide) fp4_read_kernel<float, 128><<<grid, kFaThreads, 0, stream>>>(a);
+    else fp4_read_kernel<float, 64><<<grid, kFaThreads, 0, stream>>>(a);
+  }
+  return cudaGetLastError();
+}
+
+}  // namespace echokv

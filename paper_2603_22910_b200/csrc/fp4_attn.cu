@@ -1,0 +1,705 @@
+// Attention over a cache held in 4 bits, one or a few queries per sequence (decode steps, drafts to verify), over the whole cache or over
+// pages that each token lists.
+//
+//   x_t = scale q . k_t  [capped by softcap tanh(x / softcap)] [- slope |p - t|],   o = sum_t 2^(x_t log2e - m) v_t / sum_t 2^(...)
+//
+// The blocks are read once from HBM and that is the bound; beside the stream every value has to be turned into fp16, 41 of them per
+// clock and SM.  The design:
+//
+//   work     A unit is one 16-token block of one KV head for one tile of 8 query rows (the query heads that share the KV head, times a
+//            sequence's new tokens).  The units of all sequences are laid end to end and cut into equal shares, one per CTA and
+//            within it one per warp, computed on the device from the lengths.  A share cuts at most two (sequence, head) items;
+//            their partial results (running maximum, sum, output) are combined inside the CTA through shared memory and between CTAs by a
+//            second small kernel.  With lists an item is one token and head, its blocks those of its listed pages.
+//   copies   A block is 18 d contiguous bytes (K and V codes and scales): one bulk copy into a ring of the warp's own, two blocks to a
+//            stage.  The block's layout is the operands': what a lane reads lies side by side with what its neighbours read.
+//   products mma.sync m16n8k16 in fp16 with the tokens (then the head's features) on the M rows and the 8 query rows on N.  A value
+//            e2m1 x e4m3 has 6 bits and lies between 2^-10 and 2688: it is an fp16 exactly.  fp32 queries, and the
+//            probabilities beside them, take a second product with their low-order halves (22 bits).
+//   softmax  The running maximum is a reference that moves only when a score is 2^8 above it; probabilities are 2^5 times themselves, so
+//            that fp16 holds them down to 2^-29 of the reference.
+#include "fp4_common.cuh"
+#include "quant_rows.cuh"
+
+namespace echokv {
+
+namespace {
+
+constexpr int kFqWarps = 12;
+constexpr int kFqThreads = kFqWarps * 32;
+constexpr int kFqRows = 8;                        // query rows per tile
+constexpr int kFqStages = 3;                      // of two blocks each
+constexpr int kFqMergeThreads = kFqRows * 32;
+constexpr int kFqMaxCtas = 512;
+constexpr int kFqItemCost = 6;                    // what an item costs beside its blocks (queries, first copies, result), in blocks
+constexpr int kFqMinShare = 2 * kFqWarps;         // units per CTA at least
+constexpr float kFqBelow = 5.f;                   // the reference stands 2^5 below the largest score it was taken from,
+constexpr float kFqGrow = 8.f + kFqBelow;         // and moves when a score is 2^13 above it (probabilities up to there fit fp16)
+constexpr int kFqNowhere = 0x40000000;            // the first token of a block that nobody sees
+
+__host__ __device__ constexpr int fq_stage_bytes(int D) { return 2 * fp4_block_bytes(D); }
+
+template <int D>
+struct FqSmem {
+  // a warp's segment that goes on from the warp before it, and (over the warp's ring, once that is at rest) the one
+  // that goes on in the next warp
+  float o_first[kFqWarps][kFqRows][D];
+  QaSeg seg[2 * kFqWarps];
+  float m[2 * kFqWarps][kFqRows], l[2 * kFqWarps][kFqRows];
+  unsigned long long pre[kFqThreads + 1];
+  unsigned long long warp_sums[kFqWarps];
+  unsigned long long full[kFqWarps][kFqStages];
+  int4 info[kFqThreads];                          // slot, length, first token, tokens (0: nothing to do) of a small batch
+};
+template <int D>
+__host__ __device__ constexpr size_t fq_ring_bytes() { return (size_t)kFqWarps * kFqStages * fq_stage_bytes(D); }
+
+// workspace: [ctas] QaDesc | [ctas][2][8] (m, l) | [ctas][2][8][D] o
+template <int D>
+struct FqWork {
+  QaDesc* desc;
+  float2* ml;
+  float* o;
+  __host__ __device__ explicit FqWork(unsigned char* ws) {
+    desc = reinterpret_cast<QaDesc*>(ws);
+    ml = reinterpret_cast<float2*>(ws + kFqMaxCtas * sizeof(QaDesc));
+    o = reinterpret_cast<float*>(ws + kFqMaxCtas * (sizeof(QaDesc) + 2 * kFqRows * sizeof(float2)));
+  }
+};
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+
+// Item owners: the sequences of the call, or with lists its tokens.
+template <bool LIST>
+__device__ __forceinline__ int owners(const Fp4AttnArgs& a) { return LIST ? a.n_tokens : a.B; }
+template <bool LIST>
+__device__ __forceinline__ QuantSeq owner(const Fp4AttnArgs& a, int b) {
+  if (!LIST) return quant_seq(a, b);
+  QuantSeq s;
+  const int seq = a.t.seqs[b], pos = a.t.positions[b];
+  s.first = b;
+  s.n = seq < 0 ? 0 : 1;
+  s.slot = 0;
+  s.error = 0;
+  s.len = pos + 1;
+  if (seq < 0) return s;
+  if (seq < a.B) s.slot = a.slots ? a.slots[seq] : seq;
+  if (seq >= a.B || s.slot < 0 || s.slot >= a.g.max_batch) s.error = ECHOKV_EBADPAGE;
+  else if (pos < 0 || pos >= a.g.max_pages * a.g.page_tokens) s.error = ECHOKV_EBADLENGTH;
+  return s;
+}
+// What the kernel needs of an owner: w = 0 tokens where nothing is attended here.
+// (without: the sequences of many rows are the chunk kernel's)
+template <bool LIST>
+__device__ __forceinline__ int4 owner_info(const Fp4AttnArgs& a, int b, bool tell, bool without) {
+  const QuantSeq s = owner<LIST>(a, b);
+  if (s.error && tell) report_opt(a.status, s.error);
+  return make_int4(s.slot, s.len, s.first, s.error || (without && many_rows(a, s)) ? 0 : s.n);
+}
+__device__ __forceinline__ int row_tiles(const QuantAttnArgs& a, int n) { return (n * a.group + kFqRows - 1) / kFqRows; }
+template <bool LIST>
+__device__ __forceinline__ int blocks_of(const Fp4AttnArgs& a, int len) {
+  if (LIST) return min(a.t.n_select, ((len - 1) >> a.g.page_shift) + 1) << (a.g.page_shift - 4);
+  return (len + kQuantBlock - 1) / kQuantBlock;
+}
+template <bool LIST>
+__device__ __forceinline__ unsigned long long units_of(const Fp4AttnArgs& a, const int4& s) {
+  return s.w == 0 ? 0 : (unsigned long long)row_tiles(a, s.w) * a.g.n_kv_heads * (blocks_of<LIST>(a, s.y) + kFqItemCost);
+}
+
+template <typename T, int D, bool LIST>
+__global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_constant__ Fp4AttnArgs a) {
+  constexpr int KC = D / 64;                      // groups of a key row per lane
+  constexpr int KS = D / 16;                      // k-steps of q . k
+  constexpr int NT = D / 8;                       // features of the output per lane (NT r .. NT r + NT - 1)
+  constexpr int MT = D / 16;                      // output tiles of 16 features: features NT r + 2 j and NT r + 2 j + 1
+  constexpr int BB = fp4_block_bytes(D);
+  constexpr int NB = 2;                           // blocks of a step
+  constexpr bool kF32 = sizeof(T) == 4;
+  extern __shared__ __align__(1024) unsigned char fq_raw[];
+  FqSmem<D>& sm = *reinterpret_cast<FqSmem<D>*>(fq_raw + fq_ring_bytes<D>());
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
+  const uint32_t ring = smem_u32(fq_raw) + warp * kFqStages * fq_stage_bytes(D);
+  const QuantGeom& g = a.g;
+  const int H = g.n_kv_heads;
+  // output rows [8][D] of segment `at`
+  const auto seg_rows = [&](int at) -> float* {
+    return at & 1 ? reinterpret_cast<float*>(fq_raw + (size_t)(at >> 1) * kFqStages * fq_stage_bytes(D)) : &sm.o_first[at >> 1][0][0];
+  };
+
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // ---- the units of the call, and this CTA's and warp's share of them
+  const bool without = !LIST && take_chunks(a, a.sm_count);
+  const int n_own = owners<LIST>(a), per = (n_own + kFqThreads - 1) / kFqThreads;
+  {
+    unsigned long long n = 0;
+#pragma unroll 1
+    for (int b = tid * per; b < min(n_own, (tid + 1) * per); ++b) {
+      const int4 s = owner_info<LIST>(a, b, blockIdx.x == 0, without);
+      if (per == 1) sm.info[b] = s;
+      n += units_of<LIST>(a, s);
+    }
+    unsigned long long x = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned long long y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) sm.warp_sums[warp] = x;
+    if (tid < 2 * kFqWarps) sm.seg[tid].valid = 0;
+    if (lane == 0) {
+      for (int i = 0; i < kFqStages; ++i) mbar_init(smem_u32(&sm.full[warp][i]), 1);
+      mbar_fence_init();
+    }
+    __syncthreads();
+    unsigned long long before = 0;
+    for (int w = 0; w < warp; ++w) before += sm.warp_sums[w];
+    sm.pre[tid + 1] = before + x;
+    if (tid == 0) sm.pre[0] = 0;
+    __syncthreads();
+  }
+  const unsigned long long total = sm.pre[kFqThreads];
+  unsigned long long share = quotient(total + gridDim.x - 1, gridDim.x);
+  if (share < kFqMinShare) share = kFqMinShare;
+  const unsigned long long cta0 = min(total, share * blockIdx.x), cta1 = min(total, cta0 + share);
+  const unsigned long long wshare = quotient(cta1 - cta0 + kFqWarps - 1, kFqWarps);
+  unsigned long long u = min(cta1, cta0 + wshare * warp);
+  const unsigned long long u_end = min(cta1, u + wshare);
+
+  // the owner of unit u: the last thread whose prefix is not above it, in two votes
+  int b = 0;
+  unsigned long long base = 0;                    // first unit of owner b
+  if (u < u_end) {
+    static_assert(kFqWarps <= 32, "a lane per run of 32 prefixes");
+    const int run = __popc(__ballot_sync(0xffffffffu, lane < kFqWarps && sm.pre[lane * 32] <= u)) - 1;
+    const int at = run * 32 + __popc(__ballot_sync(0xffffffffu, sm.pre[run * 32 + lane] <= u)) - 1;
+    b = at * per;
+    base = sm.pre[at];
+  }
+  const bool plain = !(a.softcap > 0.f) && a.slopes == nullptr;
+  const float cap_in = a.softcap > 0.f ? 1.f / a.softcap : 0.f, cap_out = a.softcap * kLog2e;
+
+  uint32_t filled = 0, used = 0;                  // stages this warp has asked for and taken from its ring
+  bool dead = false;                              // a copy did not arrive (reported); the warp gives up
+  while (u < u_end && !dead) {
+    int4 info = per == 1 ? sm.info[b] : owner_info<LIST>(a, b, false, without);
+    unsigned long long n_units = units_of<LIST>(a, info);
+    while (base + n_units <= u) {
+      base += n_units;
+      ++b;
+      info = per == 1 ? sm.info[b] : owner_info<LIST>(a, b, false, without);
+      n_units = units_of<LIST>(a, info);
+    }
+    const int slot = info.x, len = info.y, first_token = info.z, n_new = info.w;
+    const int n_blk = blocks_of<LIST>(a, len), tiles = row_tiles(a, n_new);
+    const unsigned long long rem = u - base;
+    const int ht = (int)quotient(rem, n_blk + kFqItemCost), at0 = (int)(rem - (unsigned long long)ht * (n_blk + kFqItemCost));
+    const int h = tiles == 1 ? ht : ht / tiles, tile = ht - h * tiles;
+    const unsigned long long item = u - at0, item_end = item + n_blk + kFqItemCost;
+    const unsigned long long seg_end = min(item_end, u_end);
+    // blocks [blk0, blk0 + nb) of the item
+    const int blk0 = max(0, at0 - kFqItemCost), nb = max(0, (int)(seg_end - item) - kFqItemCost) - blk0;
+    if (nb == 0) {
+      u = seg_end;
+      continue;
+    }
+
+    // ---- copies
+    const int32_t* pages = a.table + (long long)slot * g.max_pages;
+    const int32_t* list = LIST ? a.t.pages + ((long long)first_token * H + h) * a.t.n_select : nullptr;
+    // lane l keeps the place of block 32 n + l of the segment (block of the pool, and with lists its first token): of the current
+    // 32, and asked for ahead of the next 32
+    struct Place {
+      int page, tok;
+    };
+    const auto look_up = [&](int group) {
+      Place p = {0, kFqNowhere};
+      const int j = 32 * group + lane;
+      if (j < nb) {
+        int logical = (blk0 + j) * kQuantBlock >> g.page_shift;
+        if (LIST) {
+          const int own = (len - 1) >> g.page_shift;
+          const int e = list[logical];
+          if (e > own) report_opt(a.status, ECHOKV_EBADPAGE);
+          logical = e < 0 || e > own ? -1 : e;
+        }
+        if (logical >= 0) {
+          p.page = pages[logical];
+          p.tok = (logical << g.page_shift) + ((blk0 + j) * kQuantBlock & (g.page_tokens - 1));
+          if (p.page < 0 || p.page >= g.n_pages) {
+            report_opt(a.status, ECHOKV_EBADPAGE);
+            p.page = 0;
+          }
+        }
+      }
+      return p;
+    };
+    Place cur = look_up(0);
+    // ---- the query rows: this lane loads a quarter of row r as operand; its scores are of rows 2 c and 2 c + 1
+    const int n_rows = n_new * a.group;
+    uint32_t qh[KS][2], ql[kF32 ? KS : 1][2];
+    float c_row[2];
+    const int qrow_r = tile * kFqRows + r;
+    const bool ok = qrow_r < n_rows;
+    const T* qp = static_cast<const T*>(a.q) + (long long)(first_token + (ok ? qrow_r >> a.group_shift : 0)) * a.q_stride +
+                  (long long)(h * a.group + (qrow_r & (a.group - 1))) * D;
+    Quad<T> qv[KS];
+#pragma unroll
+    for (int x = 0; x < KS; x += Quad<T>::kPerLoad)
+      if (ok) Quad<T>::load16(qp + KC * 16 * c + 4 * x, &qv[x]);
+      else Quad<T>::zero16(&qv[x]);
+    Place next = look_up(1);
+    int group = 0;
+    const int n_steps = (nb + NB - 1) / NB;
+    const auto issue = [&](int step) {
+      const int st = filled % kFqStages;
+      const uint32_t bar = smem_u32(&sm.full[warp][st]), dst = ring + st * fq_stage_bytes(D);
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        const int j = step * NB + n;
+        const int page = __shfl_sync(0xffffffffu, (j >> 5) == group ? cur.page : next.page, j & 31);
+        if (lane == 0 && j < nb) {
+          if (n == 0) mbar_arrive_expect_tx(bar, j + 1 < nb ? 2 * BB : BB);
+          const int inside = (blk0 + j) & ((g.page_tokens >> 4) - 1);
+          bulk_load(dst + n * BB, g.blocks + (((long long)page * H + h) * (g.page_tokens >> 4) + inside) * BB, BB, bar);
+        }
+      }
+      ++filled;
+    };
+    for (int s = 0; s < min(kFqStages, n_steps); ++s) issue(s);
+
+    {
+      // (magnitudes compare as integers; an infinity or NaN gives the factor 1 and goes on through the products)
+      uint32_t bits = 0;
+#pragma unroll
+      for (int x = 0; x < KS; ++x) bits = qv[x].top(bits);
+      bits = Quad<T>::top_bits(bits);
+      bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 1));
+      bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 2));
+      const float top = __uint_as_float(bits);
+      float back;
+      const float up = scale_up_to_half(top, &back);
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        c_row[e] = __shfl_sync(0xffffffffu, back, 4 * (2 * c + e)) * a.scale * (a.softcap > 0.f ? 1.f : kLog2e);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          const HalfPair p = split_pair<kF32>(qv[ks].get(2 * f) * up, qv[ks].get(2 * f + 1) * up);
+          qh[ks][f] = p.hi;
+          if (kF32) ql[ks][f] = p.lo;
+        }
+    }
+    const int prefix = !LIST && a.prefix ? a.prefix[b] : 0;
+    int pos[2];
+    float slope2[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int qrow = tile * kFqRows + 2 * c + e;
+      pos[e] = len - n_new + (qrow < n_rows ? qrow >> a.group_shift : 0);
+      slope2[e] = a.slopes ? a.slopes[h * a.group + (qrow & (a.group - 1))] * kLog2e : 0.f;
+    }
+
+    float o[MT][4];                               // rows: feature NT r + 2 j (0, 1) and + 1 (2, 3); columns: query rows 2 c, 2 c + 1
+#pragma unroll
+    for (int j = 0; j < MT; ++j)
+#pragma unroll
+      for (int f = 0; f < 4; ++f) o[j][f] = 0.f;
+    // Per query row: the reference of its maximum (0 until it has seen a key, which the first one seen moves), and how far
+    // above the reference a score may be before that moves.
+    float m_ref[2] = {0.f, 0.f}, grow[2] = {-3.0e38f, -3.0e38f}, l_run[2] = {0.f, 0.f};
+    const int pos_first = len - n_new + (tile * kFqRows >> a.group_shift);     // the tile's first query: blocks up to it are seen whole
+
+    // a scaled product q . k of token tok and query row 2 c + e -> the score in base-2 units
+    const auto score = [&](float y, int e, int tok) {
+      if (a.softcap > 0.f) y = cap_out * tanh_f32(y * cap_in);
+      if (a.slopes) y -= slope2[e] * fabsf((float)(pos[e] - tok));
+      return y;
+    };
+
+#pragma unroll 1
+    for (int step = 0; step < n_steps; ++step) {
+      const int j = step * NB;
+      if ((j & 31) == 0 && j > 0) {
+        ++group;
+        cur = next;
+        next = look_up(group + 1);
+      }
+      const int st = used % kFqStages;
+      if (!__all_sync(0xffffffffu, warp_wait(smem_u32(&sm.full[warp][st]), (used / kFqStages) & 1))) {
+        dead = true;
+        break;
+      }
+      ++used;
+      // an odd last block stands in for its partner, which is masked
+      const bool two = j + 1 < nb;
+      uint32_t src[NB];
+      int tok0[NB];
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        src[n] = ring + st * fq_stage_bytes(D) + (two ? n : 0) * BB;
+        tok0[n] = LIST ? __shfl_sync(0xffffffffu, cur.tok, (j + n) & 31) : (blk0 + j + n) * kQuantBlock;
+        if (n > 0 && !two) tok0[n] = kFqNowhere;
+      }
+      const bool masked = max(tok0[0], tok0[1]) + kQuantBlock - 1 > pos_first;
+      const auto seen = [&](int tok, int e) { return tok <= pos[e] || (!LIST && tok < prefix); };
+
+      // ---- scores
+      float sc[NB][4];                            // [n][2 t + e]: token r + 8 t of block n, query row 2 c + e
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        float sb[4] = {0.f, 0.f, 0.f, 0.f};        // two chains of products
+#pragma unroll
+        for (int f = 0; f < 4; ++f) sc[n][f] = 0.f;
+        uint32_t kw[2][2 * KC], ks[2][KC];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const uint32_t at = src[n] + t * 4 * D + lane * 8 * KC;
+          if constexpr (D == 128) {
+            const uint4 v = lds16(at);
+            kw[t][0] = v.x; kw[t][1] = v.y; kw[t][2 * KC - 2] = v.z; kw[t][2 * KC - 1] = v.w;
+            uint16_t w;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(src[n] + 16 * D + (r + 8 * t) * 8 + 2 * c) : "memory");
+            const uint32_t s = e4m3_scales(w);
+            ks[t][0] = __byte_perm(s, 0u, 0x1010);
+            ks[t][KC - 1] = __byte_perm(s, 0u, 0x3232);
+          } else {
+            const uint2 v = lds8(at);
+            kw[t][0] = v.x; kw[t][1] = v.y;
+            uint16_t w;
+            asm volatile("{\n\t.reg .u8 b;\n\tld.shared.u8 b, [%1];\n\tcvt.u16.u8 %0, b;\n\t}" : "=h"(w) : "r"(src[n] + 16 * D + (r + 8 * t) * 4 + c) : "memory");
+            const uint32_t s = e4m3_scales(w);
+            ks[t][0] = __byte_perm(s, 0u, 0x1010);
+          }
+        }
+#pragma unroll
+        for (int w = 0; w < 2 * KC; ++w) {
+          uint32_t x[2][4];
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            x[t][0] = fp4_mul(e2m1_pair<0>(kw[t][w]), ks[t][w / 2]);
+            x[t][1] = fp4_mul(e2m1_pair<1>(kw[t][w]), ks[t][w / 2]);
+            x[t][2] = fp4_mul(e2m1_pair<2>(kw[t][w]), ks[t][w / 2]);
+            x[t][3] = fp4_mul(e2m1_pair<3>(kw[t][w]), ks[t][w / 2]);
+          }
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            mma_m16n8k16_f16(s ? sb : sc[n], x[0][2 * s], x[1][2 * s], x[0][2 * s + 1], x[1][2 * s + 1], qh[2 * w + s][0], qh[2 * w + s][1]);
+            if (kF32) mma_m16n8k16_f16(s ? sc[n] : sb, x[0][2 * s], x[1][2 * s], x[0][2 * s + 1], x[1][2 * s + 1], ql[2 * w + s][0], ql[2 * w + s][1]);
+          }
+        }
+#pragma unroll
+        for (int f = 0; f < 4; ++f) sc[n][f] += sb[f];
+      }
+
+      // ---- probabilities as operands (ph[n][t]: query row r, tokens 8 t + 2 c, + 1), the reference moved if needed
+      uint32_t ph[NB][2], pl[NB][2];
+      bool above = false;
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        if (plain) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sc[n][i] = fmaf(sc[n][i], c_row[i & 1], -m_ref[i & 1]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sc[n][i] = score(sc[n][i] * c_row[i & 1], i & 1, tok0[n] + 8 * (i >> 1) + r) - m_ref[i & 1];
+        }
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!seen(tok0[n] + 8 * (i >> 1) + r, i & 1)) sc[n][i] = -INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) above |= sc[n][i] > grow[i & 1];
+      }
+      if (__any_sync(0xffffffffu, above)) {
+        float alpha[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float mx = fmaxf(fmaxf(sc[0][e], sc[0][2 + e]), fmaxf(sc[1][e], sc[1][2 + e]));
+#pragma unroll
+          for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+          mx -= kFqBelow;
+          const bool first = grow[e] != kFqGrow;         // nothing seen so far: sum and output are still 0
+          alpha[e] = 1.f;
+          if (mx > (first ? -INFINITY : 0.f)) {
+            if (!first) alpha[e] = exp2_approx(-mx);
+            grow[e] = kFqGrow;
+            m_ref[e] += mx;
+            l_run[e] *= alpha[e];
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+              sc[n][e] -= mx;
+              sc[n][2 + e] -= mx;
+            }
+          }
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int f = 0; f < 4; ++f) o[m][f] *= alpha[f & 1];
+      }
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[i] = exp2_approx(sc[n][i]);
+          l_run[i & 1] += p[i];
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const HalfPair w = split_pair<kF32>(p[2 * t], p[2 * t + 1]);
+          ph[n][t] = movm(w.hi);
+          if (kF32) pl[n][t] = movm(w.lo);
+        }
+      }
+
+      // ---- output
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        uint32_t even[2][D / 64], odd[2][D / 64], vs[2];      // [tokens 2 c, + 1 | 8 on]: features 2 i and 2 i + 1, a byte for both tokens
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const uint32_t at = src[n] + 8 * D + t * 4 * D + lane * 8 * KC;
+          uint32_t t0[D / 64], t1[D / 64];
+          if constexpr (D == 128) {
+            const uint4 v = lds16(at);
+            t0[0] = v.x; t0[D / 64 - 1] = v.y; t1[0] = v.z; t1[D / 64 - 1] = v.w;
+          } else {
+            const uint2 v = lds8(at);
+            t0[0] = v.x; t1[0] = v.y;
+          }
+#pragma unroll
+          for (int w = 0; w < D / 64; ++w) {
+            even[t][w] = (t0[w] & 0x0f0f0f0fu) | ((t1[w] << 4) & 0xf0f0f0f0u);
+            odd[t][w] = ((t0[w] >> 4) & 0x0f0f0f0fu) | (t1[w] & 0xf0f0f0f0u);
+          }
+          uint16_t w;
+          asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(src[n] + 17 * D + (r * NT / 16) * 16 + 8 * t + 2 * c) : "memory");
+          vs[t] = e4m3_scales(w);
+          // (behind the sequence's end there may be anything: a NaN times a probability of 0)
+          if (masked) {
+            const int tok = tok0[n] + 8 * t + 2 * c;
+            if (tok >= len) vs[t] = 0u;
+            else if (tok + 1 >= len) vs[t] &= 0xffffu;
+          }
+        }
+#pragma unroll
+        for (int w = 0; w < D / 64; ++w) {
+          const auto tile_of = [&](auto byte_tag) {
+            constexpr int B = decltype(byte_tag)::value;
+            const uint32_t a0 = fp4_mul(e2m1_pair<B>(even[0][w]), vs[0]), a1 = fp4_mul(e2m1_pair<B>(odd[0][w]), vs[0]);
+            const uint32_t a2 = fp4_mul(e2m1_pair<B>(even[1][w]), vs[1]), a3 = fp4_mul(e2m1_pair<B>(odd[1][w]), vs[1]);
+            mma_m16n8k16_f16(o[4 * w + B], a0, a1, a2, a3, ph[n][0], ph[n][1]);
+            if (kF32) mma_m16n8k16_f16(o[4 * w + B], a0, a1, a2, a3, pl[n][0], pl[n][1]);
+          };
+          tile_of(std::integral_constant<int, 0>());
+          tile_of(std::integral_constant<int, 1>());
+          tile_of(std::integral_constant<int, 2>());
+          tile_of(std::integral_constant<int, 3>());
+        }
+      }
+      __syncwarp();                                // (all lanes have read the stage: it may be overwritten)
+      if (step + kFqStages < n_steps) issue(step + kFqStages);
+    }
+    if (dead) {
+      // let every copy that was asked for land, as far as it does, before the shared memory is given back
+      if (lane == 0) {
+        report_opt(a.status, ECHOKV_ETIMEOUT);
+        for (; used < filled; ++used) mbar_drain(smem_u32(&sm.full[warp][used % kFqStages]), (used / kFqStages) & 1);
+      }
+      break;
+    }
+
+    // ---- the segment's result
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int w = 4; w < 32; w <<= 1) l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], w);
+    const bool starts = blk0 == 0, ends = seg_end == item_end;
+    if (starts && ends) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int qrow = tile * kFqRows + 2 * c + e;
+        if (qrow < n_rows) {
+          const float inv = l_run[e] == 0.f ? 0.f : a.out_scale / l_run[e];
+          float v[NT];
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            v[2 * m] = o[m][e] * inv;
+            v[2 * m + 1] = o[m][2 + e] * inv;
+          }
+          T* dst = static_cast<T*>(a.out) +
+                   ((long long)(first_token + (qrow >> a.group_shift)) * a.n_q_heads + h * a.group + (qrow & (a.group - 1))) * D + NT * r;
+#pragma unroll
+          for (int f = 0; f < NT; f += Vec16<T>::N) store16<T>(dst + f, v + f);
+        }
+      }
+    } else {
+      const int at = 2 * warp + (starts ? 1 : 0);
+      if (lane == 0) {
+        QaSeg& q = sm.seg[at];
+        q.item = item; q.item_end = item_end;
+        q.b = b; q.tile = tile; q.h = h;
+        q.starts = starts; q.ends = ends;
+        q.valid = 1;
+      }
+      float* dst = seg_rows(at);
+      if (r == 0) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          sm.m[at][2 * c + e] = l_run[e] == 0.f ? -INFINITY : m_ref[e];
+          sm.l[at][2 * c + e] = l_run[e];
+        }
+      }
+      __syncwarp();                               // (the rows of the second kind lie over the ring)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+          *reinterpret_cast<float2*>(dst + (2 * c + e) * D + NT * r + 2 * m) = make_float2(o[m][e], o[m][2 + e]);
+    }
+    u = seg_end;
+  }
+
+  // ---- segments of one item side by side in this CTA: combine them; what is still cut goes to the workspace.  A warp per query
+  //      row; lane k looks at segment k.
+  __syncthreads();
+  if (warp >= kFqRows) return;
+  const FqWork<D> ws(a.ws);
+  constexpr int E = D / 32;
+  static_assert(2 * kFqWarps <= 32, "a lane per segment");
+  const bool is_seg = lane < 2 * kFqWarps && sm.seg[lane < 2 * kFqWarps ? lane : 0].valid;
+  const unsigned long long my_item = is_seg ? sm.seg[lane].item : ~0ull;
+  const float my_m = is_seg ? sm.m[lane][warp] : -INFINITY, my_l = is_seg ? sm.l[lane][warp] : 0.f;
+  uint32_t todo = __ballot_sync(0xffffffffu, is_seg);
+  QaDesc desc = {0, 0, 0, 0};
+  while (todo) {
+    const int i = __ffs(todo) - 1;
+    const uint32_t mine = __ballot_sync(0xffffffffu, my_item == __shfl_sync(0xffffffffu, my_item, i)) & todo;
+    todo &= ~mine;
+    const QaSeg& first = sm.seg[i];
+    const bool starts = first.starts, ends = sm.seg[31 - __clz(mine)].ends;
+    const bool in = (mine >> lane) & 1;
+    const float m = warp_max(in ? my_m : -INFINITY);
+    // (a row that has seen nothing has the sum 0 -- or NaN)
+    const float w = !in || my_l == 0.f ? 0.f : exp2_approx(my_m - m);
+    const float l = warp_sum(in ? w * my_l : 0.f);
+    float acc[E] = {};
+    for (uint32_t left = mine; left; left &= left - 1) {
+      const int k = __ffs(left) - 1;
+      const float wk = __shfl_sync(0xffffffffu, w, k);
+      const float* o = seg_rows(k) + warp * D + lane * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += wk * o[e];
+    }
+    if (starts && ends) {
+      const int4 s = per == 1 ? sm.info[first.b] : owner_info<LIST>(a, first.b, false, without);
+      const int qrow = first.tile * kFqRows + warp;
+      if (qrow < s.w * a.group) {
+        const float inv = l == 0.f ? 0.f : a.out_scale / l;
+        T* dst = static_cast<T*>(a.out) +
+                 ((long long)(s.z + (qrow >> a.group_shift)) * a.n_q_heads + first.h * a.group + (qrow & (a.group - 1))) * D + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) dst[e] = from_f32<T>(acc[e] * inv);
+      }
+    } else {
+      const long long p = ((long long)blockIdx.x * 2 + (starts ? 1 : 0)) * kFqRows + warp;
+      if (lane == 0) ws.ml[p] = make_float2(m, l);
+#pragma unroll
+      for (int e = 0; e < E; ++e) ws.o[p * D + lane * E + e] = acc[e];
+      if (starts) desc = QaDesc{(int)(quotient(first.item_end - 1, share) - blockIdx.x) + 1, first.b, first.tile, first.h};
+    }
+  }
+  if (tid == 0) ws.desc[blockIdx.x] = desc;
+}
+
+// Joins the items that shares cut: block g the one that begins in CTA g and goes on in the next ones.  Also zeroes the rows of
+// unusable sequences (tokens).  Launched while the first kernel runs, it waits for that one's end.
+template <typename T, int D, bool LIST>
+__global__ void __launch_bounds__(kFqMergeThreads) fp4_merge_kernel(const __grid_constant__ Fp4AttnArgs a) {
+  constexpr int E = D / 32;
+  const int tid = threadIdx.x, lane = tid & 31, row = tid >> 5;
+  const FqWork<D> ws(a.ws);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+#pragma unroll 1
+  for (int b = blockIdx.x; b < owners<LIST>(a); b += gridDim.x) {
+    const QuantSeq s = owner<LIST>(a, b);
+    if (s.error && s.n > 0) {
+      T* dst = static_cast<T*>(a.out) + (long long)s.first * a.n_q_heads * D;
+      const long long n = (long long)s.n * a.n_q_heads * D;
+      for (long long i = tid; i < n; i += kFqMergeThreads) dst[i] = from_f32<T>(0.f);
+    }
+  }
+  const QaDesc d = ws.desc[blockIdx.x];
+  if (d.n_parts == 0) return;
+  const auto part = [&](int p) -> long long { return ((long long)(blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * kFqRows + row; };
+  const int4 s = owner_info<LIST>(a, d.b, false, false);
+  float m = -INFINITY;
+  for (int p = lane; p < d.n_parts; p += 32) m = fmaxf(m, ws.ml[part(p)].x);
+  m = warp_max(m);
+  float l = 0.f, acc[E] = {};
+#pragma unroll 4
+  for (int p = 0; p < d.n_parts; ++p) {
+    const float2 ml = ws.ml[part(p)];
+    const float w = ml.y == 0.f ? 0.f : exp2_approx(ml.x - m);
+    l += w * ml.y;
+    const float* o = ws.o + part(p) * D + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] += w * o[e];
+  }
+  const int qrow = d.tile * kFqRows + row;
+  if (qrow >= s.w * a.group) return;
+  const float inv = l == 0.f ? 0.f : a.out_scale / l;
+  T* dst = static_cast<T*>(a.out) +
+           ((long long)(s.z + (qrow >> a.group_shift)) * a.n_q_heads + d.h * a.group + (qrow & (a.group - 1))) * D + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) dst[e] = from_f32<T>(acc[e] * inv);
+}
+
+template <typename T, int D, bool LIST>
+cudaError_t launch(const Fp4AttnArgs& a, int sm_count, cudaStream_t stream) {
+  constexpr size_t smem = fq_ring_bytes<D>() + sizeof(FqSmem<D>);
+  static_assert(kFqStages * fq_stage_bytes(D) >= kFqRows * D * 4, "a segment's rows fit over a warp's ring");
+  static_assert(smem <= 227 * 1024, "shared memory of one CTA");
+  static std::atomic<unsigned long long> done{0};
+  cudaError_t e = allow_smem(fp4_attn_kernel<T, D, LIST>, smem, &done);
+  if (e != cudaSuccess) return e;
+  const int grid = sm_count < kFqMaxCtas ? sm_count : kFqMaxCtas;
+  fp4_attn_kernel<T, D, LIST><<<grid, kFqThreads, smem, stream>>>(a);
+  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kFqMergeThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, fp4_merge_kernel<T, D, LIST>, a);
+}
+
+template <typename T, int D>
+cudaError_t launch_l(const Fp4AttnArgs& a, int sm_count, cudaStream_t stream) {
+  return a.t.seqs ? launch<T, D, true>(a, sm_count, stream) : launch<T, D, false>(a, sm_count, stream);
+}
+
+}  // namespace
+
+uint64_t fp4_attn_workspace_bytes(int head_dim) {
+  const uint64_t n = (uint64_t)kFqMaxCtas * (sizeof(QaDesc) + 2ull * kFqRows * (sizeof(float2) + (uint64_t)head_dim * sizeof(float)));
+  return (n + 255) / 256 * 256;
+}
+
+cudaError_t launch_fp4_attn(const Fp4AttnArgs& a, int sm_count, cudaStream_t stream) {
+  if (a.dtype == ECHOKV_BF16) return a.g.head_dim == 128 ? launch_l<__nv_bfloat16, 128>(a, sm_count, stream) : launch_l<__nv_bfloat16, 64>(a, sm_count, stream);
+  return a.g.head_dim == 128 ? launch_l<float, 128>(a, sm_count, stream) : launch_l<float, 64>(a, sm_count, stream);
+}
+
+}  // namespace echokv

@@ -1,0 +1,40 @@
+// What the kernels over the 4-bit cache share: codes and scales to fp16 and back.
+#pragma once
+
+#include "quant_common.cuh"
+
+namespace echokv {
+
+// byte I of w (two e2m1 codes) -> fp16 pair, low half first; exact
+template <int I>
+__device__ __forceinline__ uint32_t e2m1_pair(uint32_t w) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 b;\n\tcvt.u8.u32 b, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, b;\n\t}" : "=r"(r) : "r"(w >> (8 * I)));
+  return r;
+}
+// two e4m3 scales (low 16 bits) -> fp16 pair; exact
+__device__ __forceinline__ uint32_t e4m3_scales(uint32_t w) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)w));
+  return r;
+}
+__device__ __forceinline__ uint32_t fp4_mul(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// two fp32 -> a byte of two e2m1 codes (to nearest even, at most 6), lo in its low half
+__device__ __forceinline__ uint32_t e2m1_byte(float lo, float hi) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 b;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %1, %2;\n\tcvt.u32.u8 %0, b;\n\t}" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// fp32 >= 0 -> e4m3 (to nearest even, at most 448)
+__device__ __forceinline__ uint32_t e4m3_code(float x) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.f), "f"(x));
+  return r & 0xffu;
+}
+constexpr uint32_t kE4m3Nan = 0x7fu;
+
+}  // namespace echokv

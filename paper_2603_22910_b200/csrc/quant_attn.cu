@@ -27,7 +27,7 @@
 // Measured: 16 sequences over 32768 keys (1.07 GB of codes) 177 us, 6.1 TB/s; 32 ragged ones with capped scores, e4m3, 168 us,
 // 6.0 TB/s; one token over 777 keys 12.6 us, all latency (this kernel 7.5, the second one 3, launches).
 // (Rings filled by cp.async: 4.4 TB/s.  Warps x stages, first case: 12 x 3 177 us, 10 x 4 193, 8 x 4 192, 16 x 2 225.)
-#include "quant_common.cuh"
+#include "quant_rows.cuh"
 #include "recon_tc.h"
 
 namespace echokv {
@@ -47,11 +47,6 @@ constexpr float kQaGrow = 8.f;                    // the references move when a 
 constexpr float kQaPScale = 32.f;                 // P <= 2^8 times a scale ratio <= 1 times 2^5: 2^13 at most
 constexpr int kQaLeastExp = 27;                   // references of V scales are 2^-100 or more, as the scales are
 
-struct QaDesc {                                   // an item cut at the end of CTA g's share
-  int n_parts;                                    // CTAs that hold parts of it (0: none starts here)
-  int b, tile, h;
-};
-
 __host__ __device__ constexpr int qa_stage_bytes(int D) { return 2 * kQuantBlock * D; }      // K codes, V codes
 // byte offset of 16-byte piece x of token row `tok`: rows of 128 bytes (one token of 128 features, two of 64), swizzled
 template <int D>
@@ -59,13 +54,6 @@ __device__ __forceinline__ uint32_t qa_off(int tok, int x) {
   if (D == 128) return tok * 128 + ((x ^ (tok & 7)) << 4);
   return (tok >> 1) * 128 + ((((tok & 1) * 4 + x) ^ ((tok >> 1) & 7)) << 4);
 }
-
-struct QaSeg {
-  unsigned long long item;                        // first unit of the item
-  unsigned long long item_end;
-  int b, tile, h;
-  int valid, starts, ends;
-};
 
 template <int D>
 struct QaSmem {
@@ -95,28 +83,6 @@ struct QaWork {
   }
 };
 
-__device__ __forceinline__ uint4 lds16(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
-  return v;
-}
-__device__ __forceinline__ uint2 lds8(uint32_t a) {
-  uint2 v;
-  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
-  return v;
-}
-// bounded wait of a whole warp on a copy's barrier
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const long long start = clock64();
-  while (clock64() - start < kWaitLimitCycles) {
-#pragma unroll 1
-    for (int i = 0; i < 64; ++i)
-      if (mbar_try_wait(bar, parity)) return true;
-  }
-  return false;
-}
-
 // What the kernel needs of a sequence: w = 0 tokens where nothing is attended here.
 // (without: the sequences of many rows are the chunk kernel's)
 __device__ __forceinline__ int4 seq_info(const QuantAttnArgs& a, int b, bool tell, bool without) {
@@ -128,53 +94,6 @@ __device__ __forceinline__ int row_tiles(const QuantAttnArgs& a, int n) { return
 __device__ __forceinline__ unsigned long long units_of(const QuantAttnArgs& a, const int4& s) {
   return (unsigned long long)row_tiles(a, s.w) * a.g.n_kv_heads * ((s.y + kQuantBlock - 1) / kQuantBlock + kQaItemCost);
 }
-// n / d, mostly of numbers that fit 32 bits (a 64-bit division is long)
-__device__ __forceinline__ unsigned long long quotient(unsigned long long n, unsigned long long d) {
-  return ((n | d) >> 32) == 0 ? (unsigned long long)((uint32_t)n / (uint32_t)d) : n / d;
-}
-
-// four consecutive elements of a row in the storage type
-template <typename T>
-struct Quad;
-template <>
-struct Quad<__nv_bfloat16> {
-  uint2 w;
-  static constexpr int kPerLoad = 2;               // quads of one 16-byte load
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { w = *reinterpret_cast<const uint2*>(p); }
-  __device__ __forceinline__ void zero() { w = make_uint2(0u, 0u); }
-  __device__ __forceinline__ static void load16(const __nv_bfloat16* p, Quad* q) {
-    const uint4 v = *reinterpret_cast<const uint4*>(p);
-    q[0].w = make_uint2(v.x, v.y);
-    q[1].w = make_uint2(v.z, v.w);
-  }
-  __device__ __forceinline__ static void zero16(Quad* q) {
-    q[0].zero();
-    q[1].zero();
-  }
-  __device__ __forceinline__ float get(int e) const {
-    const uint32_t x = e < 2 ? w.x : w.y;
-    return __uint_as_float(e & 1 ? x & 0xffff0000u : x << 16);
-  }
-  // magnitudes compare as integers, infinities and NaN above everything finite (a pair of them at once here)
-  __device__ __forceinline__ uint32_t top(uint32_t t) const {
-    return __vmaxu2(t, __vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu));
-  }
-  __device__ __forceinline__ static uint32_t top_bits(uint32_t t) { return max(t & 0xffff0000u, t << 16); }
-};
-template <>
-struct Quad<float> {
-  uint4 w;
-  static constexpr int kPerLoad = 1;
-  __device__ __forceinline__ void load(const float* p) { w = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void zero() { w = make_uint4(0u, 0u, 0u, 0u); }
-  __device__ __forceinline__ static void load16(const float* p, Quad* q) { q->load(p); }
-  __device__ __forceinline__ static void zero16(Quad* q) { q->zero(); }
-  __device__ __forceinline__ float get(int e) const { return __uint_as_float(e == 0 ? w.x : e == 1 ? w.y : e == 2 ? w.z : w.w); }
-  __device__ __forceinline__ uint32_t top(uint32_t t) const {
-    return max(max(t, w.x & 0x7fffffffu), max(w.y & 0x7fffffffu, max(w.z & 0x7fffffffu, w.w & 0x7fffffffu)));
-  }
-  __device__ __forceinline__ static uint32_t top_bits(uint32_t t) { return t; }
-};
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
@@ -185,36 +104,6 @@ __device__ __forceinline__ uint32_t zero_fma_bf16x2(uint32_t a, uint32_t c) {
   asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(0u), "r"(c));
   return d;
 }
-// fp16 operands of x * up: the rounded pair and what it leaves
-struct HalfPair {
-  uint32_t hi, lo;
-};
-template <bool LOW>
-__device__ __forceinline__ HalfPair split_pair(float x0, float x1) {
-  HalfPair p;
-  p.hi = h2(x0, x1);
-  p.lo = 0u;
-  if (LOW) {
-    const float2 w = h2_float(p.hi);
-    p.lo = h2(x0 - w.x, x1 - w.y);
-  }
-  return p;
-}
-
-// transposes an 8 x 8 matrix of 16-bit elements held as matrix fragments
-__device__ __forceinline__ uint32_t movm(uint32_t x) {
-  uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-  return y;
-}
-
-template <typename T>
-__device__ __forceinline__ T from_f32(float x);
-template <>
-__device__ __forceinline__ float from_f32<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16(x); }
-
 template <typename T, int FMT, int D>
 __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k,
                                                                    const __grid_constant__ CUtensorMap tm_v,

@@ -34,7 +34,7 @@
 // half again as many products, 400 us against 293 then.)
 #include <type_traits>
 
-#include "quant_common.cuh"
+#include "fp4_common.cuh"
 
 namespace echokv {
 
@@ -123,11 +123,6 @@ __device__ __forceinline__ bool ck_wait_warp(unsigned long long* bar, uint32_t p
 __device__ __forceinline__ void warp_arrive(unsigned long long* bar) {
   __syncwarp();
   if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(bar));
-}
-__device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
 }
 
 // 16 consecutive columns of this thread's lane, into the first half of r (valid after tmem_ld_wait)
@@ -627,6 +622,104 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       sts16(dst + (at1 ^ turn) + p * kRowStep * 128, w[4], w[5], w[6], w[7]);
     };
     const CkItem& it = t.item[warp];
+    if constexpr (FMT == kFp4) {
+      // a piece is a group of 16 features of a token: 8 bytes of codes and their scale, exact in fp16
+      constexpr int BB = fp4_block_bytes(D);
+      struct Piece4 {
+        uint2 codes;
+        uint32_t scale;
+      };
+      const auto convert = [&](const Piece4& x, bool there, uint32_t (&w)[8]) {
+        const uint32_t s2 = e4m3_scales(x.scale | x.scale << 8);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          w[e] = there ? fp4_mul(e2m1_pair<0>(x.codes.x >> (8 * e)), s2) : 0u;
+          w[4 + e] = there ? fp4_mul(e2m1_pair<0>(x.codes.y >> (8 * e)), s2) : 0u;
+        }
+      };
+      for (bool more = ck_first(a, t); more && alive; more = ck_next(a, t)) {
+        const int32_t* pages = a.table + (long long)it.s.slot * g.max_pages;
+        // lane l < 8 looks up block l of a tile, one tile ahead (blocks behind the end: block 0 of the pool, not looked at)
+        const auto ask_page = [&](int tile) {
+          const int tok = (tile * 8 + lane) * kQuantBlock;
+          return lane < 8 && tok < it.s.len ? pages[tok >> g.page_shift] : 0;
+        };
+        const auto checked = [&](int id) {
+          if (id < 0 || id >= g.n_pages) {
+            report_opt(a.status, ECHOKV_EBADPAGE);
+            id = 0;
+          }
+          return id;
+        };
+        const unsigned char* blk[NP];
+        Piece4 kc[NP], vc[NP];
+        const auto fetch_k = [&](int tile, int page8) {
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            const int row = min(my_row + kRowStep * p, kCkTile - 1);
+            const int page = __shfl_sync(0xffffffffu, page8, row >> 4);
+            const int inside = (tile * 8 + (row >> 4)) & ((g.page_tokens >> 4) - 1);
+            blk[p] = g.blocks + (((long long)page * H + it.h) * (g.page_tokens >> 4) + inside) * BB;
+          }
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            const int r = min(my_row + kRowStep * p, kCkTile - 1) & 15, f = 16 * my_piece;
+            kc[p].codes = *reinterpret_cast<const uint2*>(blk[p] + fp4_k_at(D, r, f));
+            kc[p].scale = blk[p][fp4_ks_at(D, r, f)];
+          }
+        };
+        const auto fetch_v = [&] {
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            const int r = min(my_row + kRowStep * p, kCkTile - 1) & 15, f = 16 * my_piece;
+            if constexpr (D == 128) {
+              vc[p].codes = *reinterpret_cast<const uint2*>(blk[p] + fp4_v_at(D, r, f));
+            } else {
+              vc[p].codes.x = *reinterpret_cast<const uint32_t*>(blk[p] + fp4_v_at(D, r, f));
+              vc[p].codes.y = *reinterpret_cast<const uint32_t*>(blk[p] + fp4_v_at(D, r, f + 8));
+            }
+            vc[p].scale = blk[p][fp4_vs_at(D, r, f)];
+          }
+        };
+        int page_next = ask_page(it.t0 + 1);
+        fetch_k(it.t0, checked(ask_page(it.t0)));
+        fetch_v();
+        for (int tile = it.t0; tile < it.t1; ++tile, ++T) {
+          const int st = T & 1;
+          const uint32_t parity = ((T >> 1) & 1) ^ 1;
+          alive = __all_sync(0xffffffffu, ck_wait(&t.k_empty[st], parity, abort_flag, a.status));
+          if (!alive) break;
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            const int row = my_row + kRowStep * p;
+            if (row >= kCkTile) break;
+            uint32_t w[8];
+            convert(kc[p], tile * kCkTile + row < it.s.len, w);
+            store_piece(k_addr + st * kTileBytes, p, w);
+          }
+          fence_proxy_async_smem();
+          warp_arrive(&t.k_full[st]);
+          if (tile + 1 < it.t1) {
+            // (the values of this tile are in registers: their places are not needed any more)
+            fetch_k(tile + 1, checked(page_next));
+            page_next = ask_page(tile + 2);
+          }
+          alive = __all_sync(0xffffffffu, ck_wait(&t.v_empty[st], parity, abort_flag, a.status));
+          if (!alive) break;
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            const int row = my_row + kRowStep * p;
+            if (row >= kCkTile) break;
+            uint32_t w[8];
+            convert(vc[p], tile * kCkTile + row < it.s.len, w);
+            store_piece(v_addr + st * kTileBytes, p, w);
+          }
+          fence_proxy_async_smem();
+          warp_arrive(&t.v_full[st]);
+          if (tile + 1 < it.t1) fetch_v();
+        }
+      }
+    } else
     for (bool more = ck_first(a, t); more; more = ck_next(a, t), ++n_item) {
       if (!conv_all(alive)) break;                 // (a wait that ran out: all leave together)
       const int32_t* pages = a.table + (long long)it.s.slot * g.max_pages;
@@ -807,8 +900,8 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const uint32_t x = codes_bias<FMT>(c4[e]);
-              w[2 * e] = mul_h2(codes_pair<FMT, 0>(x), r2);
-              w[2 * e + 1] = mul_h2(codes_pair<FMT, 1>(x), r2);
+              w[2 * e] = fp4_mul(codes_pair<FMT, 0>(x), r2);
+              w[2 * e + 1] = fp4_mul(codes_pair<FMT, 1>(x), r2);
             }
           } else if (blk >= n_codes && open && !open_bad && tok < it.s.len) {
             open_row(1, tok - n_full * kQuantBlock, v_unit(open_scale), w);
@@ -921,7 +1014,11 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         if (!alive) break;
         tc_fence_after();
         const int n_vis = max(0, min(kCkTile, vis - tile * kCkTile));
-        const float* k_scale = t.k_scale[T % kCkRing];
+        // (the values of the 4-bit cache are whole in their operands)
+        const auto k_scale = [&](int i) { return FMT == kFp4 ? 1.f : t.k_scale[T % kCkRing][i]; };
+        const auto v_exp2 = [&](int c) {
+          return FMT == kFp4 ? make_float4(0.f, 1.f, 0.f, 1.f) : *reinterpret_cast<const float4*>(&t.v_exp[T % kCkRing][2 * c]);
+        };
         // the common way: the reference where it is
         float top = 0.f;
         const auto piece = [&](auto mode_tag, auto masked_tag, uint32_t (&sr)[32], int c) {
@@ -929,7 +1026,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           constexpr bool kMasked = decltype(masked_tag)::value;          // some key of the tile is not seen
           const int vis_c = max(0, min(32, n_vis - 32 * c));
           const uint32_t seen = kMasked ? (uint32_t)((1ull << vis_c) - 1) : 0xffffffffu;
-          float f0 = c_row * k_scale[2 * c], f1 = c_row * k_scale[2 * c + 1];      // (16 keys each)
+          float f0 = c_row * k_scale(2 * c), f1 = c_row * k_scale(2 * c + 1);      // (16 keys each)
           bool bad = false;
           if (kMode > 0) {
             const float z = tanh_pieces<kMode == 1>(sr, f0 * cap_in, f1 * cap_in);
@@ -938,7 +1035,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
             f0 = f1 = cap_out;
           }
           // p times 2^e of its block's V scale: what a row does not see has no part in its products' range
-          const float4 ve = *reinterpret_cast<const float4*>(&t.v_exp[T % kCkRing][2 * c]);
+          const float4 ve = v_exp2(c);
           uint32_t pk[16];
           uint64_t sum2[2] = {0ull, 0ull};           // of the first 16 keys, of the others
           const uint64_t nm0 = pack_f2(ve.x - m_ref, ve.x - m_ref), nm1 = pack_f2(ve.z - m_ref, ve.z - m_ref);
@@ -977,8 +1074,8 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           return c;
         };
         const auto careful = [&](int c) {
-          const float2 r = careful_piece<D>(w, c, tile * kCkTile + 32 * c, n_vis, tile > it.t0, c_row * k_scale[2 * c], c_row * k_scale[2 * c + 1],
-                                            *reinterpret_cast<const float4*>(&t.v_exp[T % kCkRing][2 * c]), m_ref, l_run);
+          const float2 r = careful_piece<D>(w, c, tile * kCkTile + 32 * c, n_vis, tile > it.t0, c_row * k_scale(2 * c), c_row * k_scale(2 * c + 1),
+                                            v_exp2(c), m_ref, l_run);
           m_ref = r.x;
           l_run = r.y;
         };
@@ -997,13 +1094,13 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
               mx0 = fmaxf(mx0, __uint_as_float(sr[j]));
               mx1 = fmaxf(mx1, __uint_as_float(sr[16 + j]));
             }
-            mx0 *= c_row * k_scale[2 * c];
-            mx1 *= c_row * k_scale[2 * c + 1];
+            mx0 *= c_row * k_scale(2 * c);
+            mx1 *= c_row * k_scale(2 * c + 1);
             if (w.capped) {
               mx0 = cap_out * tanh_f32(mx0 * cap_in);
               mx1 = cap_out * tanh_f32(mx1 * cap_in);
             }
-            mx = fmaxf(mx, fmaxf(mx0 + t.v_exp[T % kCkRing][2 * c].x, mx1 + t.v_exp[T % kCkRing][2 * c + 1].x));
+            mx = fmaxf(mx, fmaxf(mx0 + v_exp2(c).x, mx1 + v_exp2(c).z));
           }
           if (mx > -INFINITY) m_ref = ceilf(mx) - w.below;
         }
@@ -1032,7 +1129,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
       if (!alive) break;
       // ---- the row's result.  The next item's queries come first: its scores are then under way meanwhile.  (This
       // item's scores are complete; its V reference stays in the ring until the products have seen the next queries.)
-      const float inv = l_run == 0.f ? 0.f : t.v_ref[n_item % kCkRing] / l_run;
+      const float inv = l_run == 0.f ? 0.f : (FMT == kFp4 ? a.out_scale : t.v_ref[n_item % kCkRing]) / l_run;
       const bool whole = it.t1 - it.t0 == it.n_tiles;
       // (a part: o / l beside the reference and l, in the slot of an item that goes on from the CTA before or in the next)
       const long long slot = (long long)blockIdx.x * 2 + (it.t0 == 0);
@@ -1144,6 +1241,7 @@ uint64_t quant_chunk_workspace_bytes(int head_dim) {
 }
 
 cudaError_t launch_quant_chunk(const QuantAttnArgs& a, int sm_count, cudaStream_t stream) {
+  if (a.format == kFp4) return a.g.head_dim == 128 ? launch<kFp4, 128>(a, sm_count, stream) : launch<kFp4, 64>(a, sm_count, stream);
   const bool i8 = a.format == ECHOKV_INT8;
   if (a.g.head_dim == 128) return i8 ? launch<ECHOKV_INT8, 128>(a, sm_count, stream) : launch<ECHOKV_E4M3, 128>(a, sm_count, stream);
   return i8 ? launch<ECHOKV_INT8, 64>(a, sm_count, stream) : launch<ECHOKV_E4M3, 64>(a, sm_count, stream);

@@ -87,8 +87,9 @@ struct RotateArgs {
 };
 cudaError_t launch_rotate(const RotateArgs& a, int sm_count, cudaStream_t stream);
 
-// Geometry of one layer's 8-bit cache, by value into kernels.
+// Geometry of one layer's 8-bit (or 4-bit) cache, by value into kernels.
 struct QuantGeom {
+  unsigned char* blocks;       // 4 bits: [n_pages][H][P / 16] blocks of 18 d bytes (the next three are not used then)
   unsigned char* codes[2];     // K, V: [n_pages][H][P][d]
   float* scales[2];            // [n_pages][H][P / 16]
   void* tail[2];               // [max_batch][H][16][d]
@@ -126,6 +127,7 @@ struct QuantAttnArgs {
                                // chunk kernel's; 0: there is none (see take_chunks)
   int sm_count;
   float scale, softcap;
+  float out_scale;             // 4 bits: what the output is multiplied by
   unsigned char* ws;
   int32_t* status;
 };
@@ -134,5 +136,81 @@ cudaError_t launch_quant_attn(const QuantAttnArgs& a, int sm_count, cudaStream_t
 // the sequences with chunk_rows query rows and more (bf16)
 uint64_t quant_chunk_workspace_bytes(int head_dim);
 cudaError_t launch_quant_chunk(const QuantAttnArgs& a, int sm_count, cudaStream_t stream);
+
+// ---- the cache held in 4 bits -------------------------------------------------------------------------------------
+constexpr int kFp4 = 2;                             // QuantAttnArgs.format of it (beside ECHOKV_INT8, ECHOKV_E4M3)
+constexpr int kFp4Group = ECHOKV_FP4_GROUP;
+__host__ __device__ constexpr int fp4_block_bytes(int d) { return 18 * d; }
+// byte offsets in a block: K codes, V codes, K scales, V scales
+__host__ __device__ constexpr int fp4_k_at(int d, int tok, int f) { return tok * (d / 2) + f / 2; }
+__host__ __device__ constexpr int fp4_v_at(int d, int tok, int f) {
+  return 8 * d + (((tok / 8 * 8 + f / (d / 8)) * 4 + tok / 2 % 4) * 2 + tok % 2) * (d / 16) + f % (d / 8) / 2;
+}
+__host__ __device__ constexpr int fp4_ks_at(int d, int tok, int f) { return 16 * d + tok * (d / 16) + f / 16; }
+__host__ __device__ constexpr int fp4_vs_at(int d, int tok, int f) { return 17 * d + f / 16 * 16 + tok; }
+
+struct Fp4Geom {
+  unsigned char* blocks;
+  int8_t* bounds;              // or null
+  float* bound_scales;
+  int n_kv_heads, head_dim, page_tokens, page_shift, max_pages, max_batch;
+  long long n_pages;
+};
+
+struct Fp4AppendArgs {
+  Fp4Geom g;
+  const void* q;               // or null
+  void* q_out;
+  const void* x[2];            // new K, V rows
+  long long q_stride, q_out_stride, stride[2];   // elements
+  const int32_t* pos;          // [n_axes][n_tokens], or null: no rotation
+  const int64_t* slot_map;
+  int n_q_heads, n_tokens, dtype, rot_dim;
+  float unit6[2], inv_unit[2]; // 1 / (6 unit), 1 / unit
+  int32_t* status;
+  unsigned char axis[64];      // axis of every frequency index
+  double turns[64];            // theta^(-2 j / rot) / (2 pi)
+};
+cudaError_t launch_fp4_append(const Fp4AppendArgs& a, int sm_count, cudaStream_t stream);
+
+struct Fp4ReadArgs {
+  Fp4Geom g;
+  const int64_t* slot_map;
+  void* out[2];                // or null
+  long long stride[2];         // elements
+  float unit[2];
+  int n_tokens, dtype;
+  int32_t* status;
+};
+cudaError_t launch_fp4_read(const Fp4ReadArgs& a, cudaStream_t stream);
+
+// Tokens as queries of their own: sequence and position of each.
+struct Fp4Tokens {
+  const int32_t* seqs;         // [n_tokens]
+  const int32_t* positions;
+  const int32_t* pages;        // [n_tokens][H][n_select]
+  int n_select;
+};
+
+struct Fp4SelectArgs {
+  Fp4Geom g;
+  const void* q;
+  long long q_stride;
+  const int32_t* table;
+  const int32_t* slots;        // or null
+  Fp4Tokens t;
+  int32_t* out;
+  int B, n_tokens, n_first, n_recent, n_q_heads, group, group_shift, dtype;
+  unsigned char* ws;
+  int32_t* status;
+};
+uint64_t fp4_select_workspace_bytes();
+cudaError_t launch_fp4_select(const Fp4SelectArgs& a, int sm_count, cudaStream_t stream);
+
+struct Fp4AttnArgs : QuantAttnArgs {
+  Fp4Tokens t;                 // t.seqs null: the whole cache, by sequences
+};
+uint64_t fp4_attn_workspace_bytes(int head_dim);
+cudaError_t launch_fp4_attn(const Fp4AttnArgs& a, int sm_count, cudaStream_t stream);
 
 }  // namespace echokv

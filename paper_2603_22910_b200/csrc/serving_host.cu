@@ -1,4 +1,4 @@
-// C-ABI of the serving step over an 8-bit cache: argument checking and kernel arguments.  No call allocates; the calling
+// C-ABI of the serving step over an 8-bit or 4-bit cache: argument checking and kernel arguments.  No call allocates; the calling
 // thread's current device is put back.
 #include <cmath>
 #include <cstring>
@@ -111,12 +111,37 @@ bool rows_meet(const void* rows, long long stride, long long width, long long n,
   return i < n && i * stride < from + size;
 }
 
+// frequencies of each position axis (none given: one axis has them all)
+bool sections_ok(int half, int n_axes, const int32_t* sections) {
+  if (!sections) return n_axes == 1;
+  int sum = 0;
+  for (int i = 0; i < n_axes; ++i) {
+    if (sections[i] < 0 || sections[i] > half) return false;
+    sum += sections[i];
+  }
+  return sum == half;
+}
+// the axis of every frequency index
+void set_axes(int half, int n_axes, const int32_t* sections, int interleaved, unsigned char* out) {
+  int axis = 0, until = sections ? sections[0] : half;
+  for (int j = 0; j < half; ++j) {
+    if (interleaved && sections) {
+      axis = j % n_axes;
+      if (j / n_axes >= sections[axis]) axis = 0;
+    } else {
+      while (j >= until) until += sections[++axis];
+    }
+    out[j] = (unsigned char)axis;
+  }
+}
+
 int quant_geom(const echokv_config* c, const echokv_quant_cache* q, QuantGeom* g) {
   if (!q || !q->k_codes || !q->v_codes || !q->k_scales || !q->v_scales || !q->k_tail || !q->v_tail) return ECHOKV_EINVAL;
   if (!aligned(q->k_codes, 16) || !aligned(q->v_codes, 16) || !aligned(q->k_scales, 16) || !aligned(q->v_scales, 16) ||
       !aligned(q->k_tail, 16) || !aligned(q->v_tail, 16))
     return ECHOKV_EINVAL;
   if (q->format != ECHOKV_INT8 && q->format != ECHOKV_E4M3) return ECHOKV_EINVAL;
+  g->blocks = nullptr;
   g->codes[0] = static_cast<unsigned char*>(q->k_codes); g->codes[1] = static_cast<unsigned char*>(q->v_codes);
   g->scales[0] = q->k_scales; g->scales[1] = q->v_scales;
   g->tail[0] = q->k_tail; g->tail[1] = q->v_tail;
@@ -124,6 +149,68 @@ int quant_geom(const echokv_config* c, const echokv_quant_cache* q, QuantGeom* g
   g->page_tokens = c->page_tokens; g->page_shift = log2_of(c->page_tokens);
   g->max_pages = c->max_pages_per_seq; g->max_batch = c->max_batch;
   g->n_pages = c->n_pages;
+  return ECHOKV_OK;
+}
+
+uint64_t fp4_workspace(const echokv_config* c) {
+  uint64_t n = fp4_attn_workspace_bytes(c->head_dim);
+  if (c->dtype == ECHOKV_BF16 && quant_chunk_workspace_bytes(c->head_dim) > n) n = quant_chunk_workspace_bytes(c->head_dim);
+  return fp4_select_workspace_bytes() > n ? fp4_select_workspace_bytes() : n;
+}
+
+bool unit_ok(float u) { return u >= 0x1p-60f && u <= 0x1p60f; }
+
+int fp4_geom(const echokv_config* c, const echokv_fp4_cache* q, Fp4Geom* g) {
+  if (!q || !q->blocks || !aligned(q->blocks, 16) || !unit_ok(q->k_unit) || !unit_ok(q->v_unit)) return ECHOKV_EINVAL;
+  if ((q->bounds == nullptr) != (q->bound_scales == nullptr) || !aligned(q->bounds, 16) || !aligned(q->bound_scales, 16)) return ECHOKV_EINVAL;
+  g->blocks = static_cast<unsigned char*>(q->blocks);
+  g->bounds = static_cast<int8_t*>(q->bounds);
+  g->bound_scales = q->bound_scales;
+  g->n_kv_heads = c->n_kv_heads; g->head_dim = c->head_dim;
+  g->page_tokens = c->page_tokens; g->page_shift = log2_of(c->page_tokens);
+  g->max_pages = c->max_pages_per_seq; g->max_batch = c->max_batch;
+  g->n_pages = c->n_pages;
+  return ECHOKV_OK;
+}
+
+// what the two attentions over the 4-bit cache have in common: everything but how queries belong to sequences
+int fp4_attention_args(const echokv_config* cfg, const echokv_fp4_cache* cache, const echokv_score_options* options, const void* q,
+                       int64_t q_stride, void* out, const int32_t* table, const int32_t* slots, int B, int n_tokens, void* workspace,
+                       uint64_t workspace_bytes, int32_t* status, Fp4AttnArgs* a) {
+  Fp4Geom g;
+  const int rc = fp4_geom(cfg, cache, &g);
+  if (rc != ECHOKV_OK) return rc;
+  if (options && (!(options->softcap == 0.f || options->softcap >= 1e-30f) || !std::isfinite(options->softcap))) return ECHOKV_EINVAL;
+  if (B > cfg->max_batch) return ECHOKV_ECAPACITY;
+  if (n_tokens == 0) return ECHOKV_OK;
+  const int elem = cfg->dtype == ECHOKV_BF16 ? 2 : 4;
+  if (!rows_ok(q, q_stride, cfg->n_q_heads * cfg->head_dim, elem)) return ECHOKV_EINVAL;
+  if (!out || !aligned(out, 16) || !table) return ECHOKV_EINVAL;
+  const long long row_bytes = (long long)cfg->n_q_heads * cfg->head_dim * elem;
+  if (!(q == out && (n_tokens == 1 || q_stride * elem == row_bytes)) &&
+      rows_meet(q, q_stride * elem, row_bytes, n_tokens, out, n_tokens * row_bytes))
+    return ECHOKV_EINVAL;
+  if (!words(table, slots, status)) return ECHOKV_EINVAL;
+  if (options && !words(options->alibi_slopes, options->prefix_lens)) return ECHOKV_EINVAL;
+  if (!workspace || !aligned(workspace, 256)) return ECHOKV_EINVAL;
+  if (workspace_bytes < fp4_workspace(cfg)) return ECHOKV_ECAPACITY;
+  std::memset(static_cast<void*>(a), 0, sizeof(*a));
+  a->g.blocks = g.blocks;
+  a->g.n_kv_heads = g.n_kv_heads; a->g.head_dim = g.head_dim;
+  a->g.page_tokens = g.page_tokens; a->g.page_shift = g.page_shift;
+  a->g.max_pages = g.max_pages; a->g.max_batch = g.max_batch; a->g.n_pages = g.n_pages;
+  a->q = q; a->q_stride = q_stride; a->out = out;
+  a->table = table; a->slots = slots;
+  a->softcap = options ? options->softcap : 0.f;
+  a->slopes = options ? options->alibi_slopes : nullptr;
+  a->prefix = options ? options->prefix_lens : nullptr;
+  a->B = B; a->n_tokens = n_tokens;
+  a->n_q_heads = cfg->n_q_heads; a->group = cfg->n_q_heads / cfg->n_kv_heads; a->group_shift = log2_of(a->group);
+  a->dtype = cfg->dtype; a->format = kFp4;
+  a->scale = (cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.0f / std::sqrt((float)cfg->head_dim)) * cache->k_unit;
+  a->out_scale = cache->v_unit;
+  a->ws = static_cast<unsigned char*>(workspace);
+  a->status = status;
   return ECHOKV_OK;
 }
 
@@ -191,16 +278,7 @@ int echokv_rotate(const echokv_config* cfg, const void* q, int64_t q_stride, con
   if (rot_dim < 0 || rot_dim > d || rot_dim % (32 / elem) != 0) return ECHOKV_EUNSUPPORTED;
   const int half = rot_dim / 2;
   RotateArgs a;
-  if (sections) {
-    int sum = 0;
-    for (int i = 0; i < n_axes; ++i) {
-      if (sections[i] < 0 || sections[i] > half) return ECHOKV_EINVAL;
-      sum += sections[i];
-    }
-    if (sum != half) return ECHOKV_EINVAL;
-  } else if (n_axes != 1) {
-    return ECHOKV_EINVAL;
-  }
+  if (!sections_ok(half, n_axes, sections)) return ECHOKV_EINVAL;
   if (n_tokens == 0) return ECHOKV_OK;
   if (!dev_positions || !aligned(dev_positions, 4)) return ECHOKV_EINVAL;
   const void* in[2] = {q, k};
@@ -221,18 +299,11 @@ int echokv_rotate(const echokv_config* cfg, const void* q, int64_t q_stride, con
   a.head_dim = d; a.rot_dim = rot_dim; a.n_tokens = n_tokens; a.dtype = cfg->dtype;
   a.pos = dev_positions;
   a.sign = inverse ? -1.f : 1.f;
-  int axis = 0, until = sections ? sections[0] : half;
+  set_axes(half, n_axes, sections, interleaved, a.axis);
   // theta^(-2 j / rot) as a running product: 64 factors, 64 roundings of 2^-53
   const double step = std::pow(theta, -2.0 / rot_dim);
   double freq = 1.0 / 6.283185307179586476925287;
   for (int j = 0; j < half; ++j) {
-    if (interleaved && sections) {
-      axis = j % n_axes;
-      if (j / n_axes >= sections[axis]) axis = 0;
-    } else {
-      while (j >= until) until += sections[++axis];
-    }
-    a.axis[j] = (unsigned char)axis;
     a.turns[j] = freq;
     freq *= step;
   }
@@ -315,6 +386,7 @@ int echokv_quant_attention(const echokv_config* cfg, const echokv_quant_cache* c
   a.dtype = cfg->dtype; a.format = cache->format;
   a.scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.0f / std::sqrt((float)cfg->head_dim);
   a.chunk_rows = cfg->dtype == ECHOKV_BF16 && (long long)max_new * a.group >= kChunkRows ? kChunkRows : 0;
+  a.out_scale = 1.f;
   a.ws = static_cast<unsigned char*>(workspace);
   a.status = dev_status;
   OnDevice dev(cfg->device);
@@ -323,6 +395,164 @@ int echokv_quant_attention(const echokv_config* cfg, const echokv_quant_cache* c
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (a.chunk_rows > 0 && launch_quant_chunk(a, dev.sm_count, s) != cudaSuccess) return ECHOKV_ECUDA;
   return launch_quant_attn(a, dev.sm_count, s) == cudaSuccess ? ECHOKV_OK : ECHOKV_ECUDA;
+}
+
+int echokv_query_fp4_sizes(const echokv_config* cfg, echokv_fp4_sizes* out) {
+  if (!out) return ECHOKV_EINVAL;
+  const int rc = check_all(cfg);
+  if (rc != ECHOKV_OK) return rc;
+  const uint64_t heads = (uint64_t)cfg->n_pages * cfg->n_kv_heads;
+  out->blocks_bytes = heads * (cfg->page_tokens / 16) * fp4_block_bytes(cfg->head_dim);
+  out->bounds_bytes = heads * 2 * cfg->head_dim;
+  out->bound_scales_bytes = heads * 4;
+  out->workspace_bytes = fp4_workspace(cfg);
+  return ECHOKV_OK;
+}
+
+int echokv_fp4_append(const echokv_config* cfg, const echokv_fp4_cache* cache, const echokv_rotation* rotation, const void* q,
+                      int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k_new, int64_t k_stride, const void* v_new,
+                      int64_t v_stride, const int32_t* dev_positions, const int64_t* dev_slot_map, int n_tokens,
+                      int32_t* dev_status, void* stream) {
+  int rc = check_all(cfg);
+  if (rc != ECHOKV_OK) return rc;
+  if (n_tokens < 0 || n_tokens > kMaxRows) return ECHOKV_EINVAL;
+  Fp4AppendArgs a;
+  std::memset(&a, 0, sizeof(a));
+  if ((rc = fp4_geom(cfg, cache, &a.g)) != ECHOKV_OK) return rc;
+  if ((q == nullptr) != (q_out == nullptr) || (q && !rotation)) return ECHOKV_EINVAL;
+  const int elem = cfg->dtype == ECHOKV_BF16 ? 2 : 4, d = cfg->head_dim, width = cfg->n_kv_heads * d;
+  if (rotation) {
+    const echokv_rotation& r = *rotation;
+    if (!(r.theta >= 1.0) || !std::isfinite(r.theta) || r.n_axes < 1 || r.n_axes > kMaxAxes) return ECHOKV_EINVAL;
+    a.rot_dim = r.rot_dim == 0 ? d : r.rot_dim;
+    if (a.rot_dim < 0 || a.rot_dim > d || a.rot_dim % 16 != 0) return ECHOKV_EUNSUPPORTED;
+    if (!sections_ok(a.rot_dim / 2, r.n_axes, r.sections)) return ECHOKV_EINVAL;
+    set_axes(a.rot_dim / 2, r.n_axes, r.sections, r.interleaved, a.axis);
+    for (int j = 0; j < a.rot_dim / 2; ++j) a.turns[j] = std::pow(r.theta, -2.0 * j / a.rot_dim) / 6.283185307179586476925287;
+  }
+  if (n_tokens == 0) return ECHOKV_OK;
+  if (rotation && (!dev_positions || !aligned(dev_positions, 4))) return ECHOKV_EINVAL;
+  if (!rows_ok(k_new, k_stride, width, elem) || !rows_ok(v_new, v_stride, width, elem)) return ECHOKV_EINVAL;
+  if (!dev_slot_map || !aligned(dev_slot_map, 8) || !words(dev_status)) return ECHOKV_EINVAL;
+  if (q) {
+    const int q_width = cfg->n_q_heads * d;
+    if (!rows_ok(q, q_stride, q_width, elem) || !rows_ok(q_out, q_out_stride, q_width, elem)) return ECHOKV_EINVAL;
+    if (q == q_out && q_stride != q_out_stride) return ECHOKV_EINVAL;
+  }
+  a.q = q; a.q_out = q_out; a.q_stride = q_stride; a.q_out_stride = q_out_stride;
+  a.x[0] = k_new; a.x[1] = v_new;
+  a.stride[0] = k_stride; a.stride[1] = v_stride;
+  a.pos = rotation ? dev_positions : nullptr;
+  a.slot_map = dev_slot_map;
+  a.n_q_heads = cfg->n_q_heads; a.n_tokens = n_tokens; a.dtype = cfg->dtype;
+  const float units[2] = {cache->k_unit, cache->v_unit};
+  for (int i = 0; i < 2; ++i) {
+    a.unit6[i] = (float)(1.0 / (6.0 * units[i]));
+    a.inv_unit[i] = (float)(1.0 / units[i]);
+  }
+  a.status = dev_status;
+  OnDevice dev(cfg->device);
+  if (!dev.ok()) return ECHOKV_ECUDA;
+  return launch_fp4_append(a, dev.sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess ? ECHOKV_OK : ECHOKV_ECUDA;
+}
+
+int echokv_fp4_read(const echokv_config* cfg, const echokv_fp4_cache* cache, const int64_t* dev_slot_map, int n_tokens, void* k_out,
+                    int64_t k_stride, void* v_out, int64_t v_stride, int32_t* dev_status, void* stream) {
+  int rc = check_all(cfg);
+  if (rc != ECHOKV_OK) return rc;
+  if (n_tokens < 0 || n_tokens > kMaxRows || (!k_out && !v_out)) return ECHOKV_EINVAL;
+  Fp4ReadArgs a;
+  if ((rc = fp4_geom(cfg, cache, &a.g)) != ECHOKV_OK) return rc;
+  if (n_tokens == 0) return ECHOKV_OK;
+  const int elem = cfg->dtype == ECHOKV_BF16 ? 2 : 4, width = cfg->n_kv_heads * cfg->head_dim;
+  if ((k_out && !rows_ok(k_out, k_stride, width, elem)) || (v_out && !rows_ok(v_out, v_stride, width, elem))) return ECHOKV_EINVAL;
+  if (!dev_slot_map || !aligned(dev_slot_map, 8) || !words(dev_status)) return ECHOKV_EINVAL;
+  a.slot_map = dev_slot_map;
+  a.out[0] = k_out; a.out[1] = v_out;
+  a.stride[0] = k_stride; a.stride[1] = v_stride;
+  a.unit[0] = cache->k_unit; a.unit[1] = cache->v_unit;
+  a.n_tokens = n_tokens; a.dtype = cfg->dtype;
+  a.status = dev_status;
+  OnDevice dev(cfg->device);
+  if (!dev.ok()) return ECHOKV_ECUDA;
+  return launch_fp4_read(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? ECHOKV_OK : ECHOKV_ECUDA;
+}
+
+int echokv_fp4_attention(const echokv_config* cfg, const echokv_fp4_cache* cache, const echokv_score_options* options, const void* q,
+                         int64_t q_stride, void* out, const int32_t* dev_block_table, const int32_t* dev_seq_slots,
+                         const int32_t* dev_seq_lens, const int32_t* dev_cu_tokens, int B, int n_tokens, int max_new, void* workspace,
+                         uint64_t workspace_bytes, int32_t* dev_status, void* stream) {
+  int rc = check_all(cfg);
+  if (rc != ECHOKV_OK) return rc;
+  if (B < 1 || n_tokens < 0 || n_tokens > kMaxRows || max_new < 1) return ECHOKV_EINVAL;
+  if (!dev_cu_tokens && (n_tokens != B || max_new != 1)) return ECHOKV_EINVAL;
+  Fp4AttnArgs a;
+  rc = fp4_attention_args(cfg, cache, options, q, q_stride, out, dev_block_table, dev_seq_slots, B, n_tokens, workspace, workspace_bytes,
+                          dev_status, &a);
+  if (rc != ECHOKV_OK || n_tokens == 0) return rc;
+  if (!dev_seq_lens || !words(dev_seq_lens, dev_cu_tokens)) return ECHOKV_EINVAL;
+  a.lens = dev_seq_lens; a.cu = dev_cu_tokens; a.max_new = max_new;
+  a.chunk_rows = cfg->dtype == ECHOKV_BF16 && (long long)max_new * a.group >= kChunkRows ? kChunkRows : 0;
+  OnDevice dev(cfg->device);
+  if (!dev.ok()) return ECHOKV_ECUDA;
+  a.sm_count = dev.sm_count;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (a.chunk_rows > 0 && launch_quant_chunk(a, dev.sm_count, s) != cudaSuccess) return ECHOKV_ECUDA;
+  return launch_fp4_attn(a, dev.sm_count, s) == cudaSuccess ? ECHOKV_OK : ECHOKV_ECUDA;
+}
+
+int echokv_fp4_select(const echokv_config* cfg, const echokv_fp4_cache* cache, const void* q, int64_t q_stride,
+                      const int32_t* dev_block_table, const int32_t* dev_seq_slots, const int32_t* dev_token_seqs,
+                      const int32_t* dev_positions, int B, int n_tokens, int n_select, int n_first, int n_recent, int32_t* dev_pages,
+                      void* workspace, uint64_t workspace_bytes, int32_t* dev_status, void* stream) {
+  int rc = check_all(cfg);
+  if (rc != ECHOKV_OK) return rc;
+  if (B < 1 || n_tokens < 0 || n_tokens > kMaxRows || n_select < 1 || n_select > ECHOKV_FP4_MAX_SELECT) return ECHOKV_EINVAL;
+  if (n_first < 0 || n_recent < 1 || n_first > n_select - n_recent) return ECHOKV_EINVAL;
+  if ((long long)n_tokens * cfg->n_kv_heads > 0x7fffffffll) return ECHOKV_EINVAL;      // (a block each at most)
+  Fp4SelectArgs a;
+  if ((rc = fp4_geom(cfg, cache, &a.g)) != ECHOKV_OK) return rc;
+  if (!a.g.bounds) return ECHOKV_EINVAL;
+  if (B > cfg->max_batch) return ECHOKV_ECAPACITY;
+  if (n_tokens == 0) return ECHOKV_OK;
+  if (!rows_ok(q, q_stride, cfg->n_q_heads * cfg->head_dim, cfg->dtype == ECHOKV_BF16 ? 2 : 4)) return ECHOKV_EINVAL;
+  if (!dev_block_table || !dev_token_seqs || !dev_positions || !dev_pages) return ECHOKV_EINVAL;
+  if (!words(dev_block_table, dev_seq_slots, dev_token_seqs, dev_positions, dev_pages, dev_status)) return ECHOKV_EINVAL;
+  if (!workspace || !aligned(workspace, 256)) return ECHOKV_EINVAL;
+  if (workspace_bytes < fp4_workspace(cfg)) return ECHOKV_ECAPACITY;
+  a.q = q; a.q_stride = q_stride; a.table = dev_block_table; a.slots = dev_seq_slots;
+  a.t.seqs = dev_token_seqs; a.t.positions = dev_positions; a.t.pages = nullptr; a.t.n_select = n_select;
+  a.out = dev_pages;
+  a.B = B; a.n_tokens = n_tokens; a.n_first = n_first; a.n_recent = n_recent;
+  a.n_q_heads = cfg->n_q_heads; a.group = cfg->n_q_heads / cfg->n_kv_heads; a.group_shift = log2_of(a.group);
+  a.dtype = cfg->dtype;
+  a.ws = static_cast<unsigned char*>(workspace);
+  a.status = dev_status;
+  OnDevice dev(cfg->device);
+  if (!dev.ok()) return ECHOKV_ECUDA;
+  return launch_fp4_select(a, dev.sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess ? ECHOKV_OK : ECHOKV_ECUDA;
+}
+
+int echokv_fp4_sparse_attention(const echokv_config* cfg, const echokv_fp4_cache* cache, const echokv_score_options* options,
+                                const void* q, int64_t q_stride, void* out, const int32_t* dev_block_table,
+                                const int32_t* dev_seq_slots, const int32_t* dev_token_seqs, const int32_t* dev_positions,
+                                const int32_t* dev_pages, int n_select, int B, int n_tokens, void* workspace,
+                                uint64_t workspace_bytes, int32_t* dev_status, void* stream) {
+  int rc = check_all(cfg);
+  if (rc != ECHOKV_OK) return rc;
+  if (B < 1 || n_tokens < 0 || n_tokens > kMaxRows || n_select < 1 || n_select > ECHOKV_FP4_MAX_SELECT) return ECHOKV_EINVAL;
+  if (options && options->prefix_lens) return ECHOKV_EINVAL;
+  Fp4AttnArgs a;
+  rc = fp4_attention_args(cfg, cache, options, q, q_stride, out, dev_block_table, dev_seq_slots, B, n_tokens, workspace, workspace_bytes,
+                          dev_status, &a);
+  if (rc != ECHOKV_OK || n_tokens == 0) return rc;
+  if (!dev_token_seqs || !dev_positions || !dev_pages || !words(dev_token_seqs, dev_positions, dev_pages)) return ECHOKV_EINVAL;
+  a.max_new = 1;
+  a.t.seqs = dev_token_seqs; a.t.positions = dev_positions; a.t.pages = dev_pages; a.t.n_select = n_select;
+  OnDevice dev(cfg->device);
+  if (!dev.ok()) return ECHOKV_ECUDA;
+  a.sm_count = dev.sm_count;
+  return launch_fp4_attn(a, dev.sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess ? ECHOKV_OK : ECHOKV_ECUDA;
 }
 
 }  // extern "C"
