@@ -208,14 +208,14 @@ __global__ void __launch_bounds__(kFaThreads, 4) fp4_append_kernel(const __grid_
 }
 
 // Bounds of the pages that the call touched: a block looks at 32 tokens for the last ones of their pages; a warp takes such a page for
-// one head, eight tokens at a time (a lane: a quarter of a token's features), and joins its lanes at the end.  Reads what the
-// first kernel wrote, from the second level cache.
+// one head.  A lane has 8 features of every second (fourth) token, so that little is left to join at the end.  Reads what the first
+// kernel wrote, from the second level cache.
 constexpr int kFbWarps = 8;
 
 template <int D>
 __global__ void __launch_bounds__(kFbWarps * 32) fp4_bounds_kernel(const __grid_constant__ Fp4AppendArgs a) {
-  constexpr int N = D / 8;                         // feature pairs of a lane
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
+  constexpr int L = D / 8, R = 32 / L;             // lanes of a token, tokens of a load
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane / L, f = lane % L * 8;
   const Fp4Geom& g = a.g;
   const int H = g.n_kv_heads;
   const int worker = blockIdx.y * kFbWarps + warp, workers = gridDim.y * kFbWarps;
@@ -240,73 +240,64 @@ __global__ void __launch_bounds__(kFbWarps * 32) fp4_bounds_kernel(const __grid_
     const int n = (int)(row & (g.page_tokens - 1)) + 1;
     for (int h = (worker + workers - at * H % workers) % workers; h < H; h += workers) {
       const unsigned char* blk = g.blocks + (page * H + h) * (g.page_tokens / 16) * fp4_block_bytes(D);
-      __half2 top[N], low[N];
+      __half2 top[4], low[4];
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
+      for (int e = 0; e < 4; ++e) {
         top[e] = __half2half2(__ushort_as_half(0xfc00));        // -inf
         low[e] = __half2half2(__ushort_as_half(0x7c00));
       }
       bool nan = false;
-#pragma unroll 2
-      for (int tok = r; tok < n; tok += 8) {
-        const unsigned char* b = blk + (tok >> 4) * fp4_block_bytes(D);
-        uint32_t w[D / 32];
-        if constexpr (D == 128) {
-          const uint4 v = *reinterpret_cast<const uint4*>(b + fp4_k_at(D, tok & 15, c * (D / 4)));
-          w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-        } else {
-          const uint2 v = *reinterpret_cast<const uint2*>(b + fp4_k_at(D, tok & 15, c * (D / 4)));
-          w[0] = v.x; w[1] = v.y;
+#pragma unroll 1
+      for (int tok = r; tok < n; tok += 8 * R) {
+        uint32_t w[8], code[8];                    // eight tokens in flight
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int t = min(tok + k * R, n - 1);   // (the last one again: it changes nothing)
+          const unsigned char* b = blk + (t >> 4) * fp4_block_bytes(D);
+          w[k] = *reinterpret_cast<const uint32_t*>(b + fp4_k_at(D, t & 15, f));
+          code[k] = b[fp4_ks_at(D, t & 15, f)];
         }
 #pragma unroll
-        for (int q = 0; q < D / 64; ++q) {         // groups of the lane
-          const uint32_t code = b[fp4_ks_at(D, tok & 15, c * (D / 4) + 16 * q)];
-          nan |= (code & 0x7fu) == kE4m3Nan;
-          const uint32_t s = e4m3_scales(code | code << 8);
+        for (int k = 0; k < 8; ++k) {
+          nan |= (code[k] & 0x7fu) == kE4m3Nan;
+          const uint32_t s = e4m3_scales(code[k] | code[k] << 8);
+          uint32_t x[4];
+          e2m1_bytes(w[k], x);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const uint32_t x = w[2 * q + (e >> 2)] >> (8 * (e & 3)), y = fp4_mul(e2m1_pair<0>(x), s);
-            const __half2 z = *reinterpret_cast<const __half2*>(&y);
-            top[8 * q + e] = __hmax2(top[8 * q + e], z);
-            low[8 * q + e] = __hmin2(low[8 * q + e], z);
+          for (int e = 0; e < 4; ++e) {
+            x[e] = fp4_mul(x[e], s);
+            const __half2 z = *reinterpret_cast<const __half2*>(&x[e]);
+            top[e] = __hmax2(top[e], z);
+            low[e] = __hmin2(low[e], z);
           }
         }
       }
       float most = 0.f;
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
+      for (int e = 0; e < 4; ++e) {
 #pragma unroll
-        for (int o = 4; o < 32; o <<= 1) {
+        for (int o = L; o < 32; o <<= 1) {
           top[e] = __hmax2(top[e], __shfl_xor_sync(0xffffffffu, top[e], o));
           low[e] = __hmin2(low[e], __shfl_xor_sync(0xffffffffu, low[e], o));
         }
         const float2 x = __half22float2(top[e]), y = __half22float2(low[e]);
         most = fmaxf(most, fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(y.x), fabsf(y.y))));
       }
-      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+      most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));      // (magnitudes: their bits are in their order)
       nan = __any_sync(0xffffffffu, nan);
-      const float scale = fmaxf(__fmul_rn(most, 1.f / 127.f), 0x1p-60f), inv = nan ? 0.f : __frcp_rn(scale);
-      // (a lane writes N / 4 of the features that its quarter has: pairs r N / 8 and on)
-      const auto code = [&](float x) { return (uint32_t)min(127, max(-127, nan ? 0 : __float2int_rn(__fmul_rn(x, inv)))) & 0xffu; };
-      int8_t* out = g.bounds + (page * H + h) * 2 * D + c * (D / 4) + r * (N / 4);
+      const float scale = fmaxf(__fmul_rn(most, 1.f / 127.f), 0x1p-60f), inv = __frcp_rn(scale);
+      if (r == 0) {
+        uint32_t out[2][2] = {};
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {                // (registers have no index: the lane's own r picks one of eight)
-        if (k != r) continue;
-        uint32_t wt = 0, wl = 0;
-#pragma unroll
-        for (int e = 0; e < N / 8; ++e) {
-          const float2 x = __half22float2(top[k * (N / 8) + e]), y = __half22float2(low[k * (N / 8) + e]);
-          wt |= (code(x.x) | code(x.y) << 8) << (16 * e);
-          wl |= (code(y.x) | code(y.y) << 8) << (16 * e);
+        for (int e = 0; e < 8; ++e) {
+          const float2 x = __half22float2(top[e >> 1]), y = __half22float2(low[e >> 1]);
+          const auto code = [&](float v) { return (uint32_t)(nan ? 0 : min(127, max(-127, __float2int_rn(__fmul_rn(v, inv))))) & 0xffu; };
+          out[0][e >> 2] |= code(e & 1 ? x.y : x.x) << (8 * (e & 3));
+          out[1][e >> 2] |= code(e & 1 ? y.y : y.x) << (8 * (e & 3));
         }
-        if constexpr (D == 128) {
-          *reinterpret_cast<uint32_t*>(out) = wt;
-          *reinterpret_cast<uint32_t*>(out + D) = wl;
-        } else {
-          *reinterpret_cast<uint16_t*>(out) = (uint16_t)wt;
-          *reinterpret_cast<uint16_t*>(out + D) = (uint16_t)wl;
-        }
+        int8_t* dst = g.bounds + (page * H + h) * 2 * D + f;
+        *reinterpret_cast<uint2*>(dst) = make_uint2(out[0][0], out[0][1]);
+        *reinterpret_cast<uint2*>(dst + D) = make_uint2(out[1][0], out[1][1]);
       }
       if (lane == 0) g.bound_scales[page * H + h] = nan ? __uint_as_float(0x7fc00000u) : scale;
     }
@@ -347,7 +338,7 @@ __global__ void __launch_bounds__(kFaThreads) fp4_read_kernel(const __grid_const
       float v[8];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float2 x = h2_float(fp4_mul(e2m1_pair<0>(w[k][p] >> (8 * e)), s2));
+        const float2 x = h2_float(fp4_mul(e2m1_pair(w[k][p] >> (8 * e)), s2));
         v[2 * e] = __fmul_rn(x.x, a.unit[k]);
         v[2 * e + 1] = __fmul_rn(x.y, a.unit[k]);
       }

@@ -19,6 +19,8 @@
 //   softmax  The running maximum is a reference that moves only when a score is 2^8 above it; probabilities are 2^5 times themselves, so
 //            that fp16 holds them down to 2^-29 of the reference.
 #include "fp4_common.cuh"
+#include <type_traits>
+
 #include "quant_rows.cuh"
 
 namespace echokv {
@@ -49,6 +51,7 @@ struct FqSmem {
   unsigned long long pre[kFqThreads + 1];
   unsigned long long warp_sums[kFqWarps];
   unsigned long long full[kFqWarps][kFqStages];
+  int2 tok[kFqWarps][kFqStages];                  // with lists: first tokens of a stage's blocks
   int4 info[kFqThreads];                          // slot, length, first token, tokens (0: nothing to do) of a small batch
 };
 template <int D>
@@ -182,7 +185,9 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
   const bool plain = !(a.softcap > 0.f) && a.slopes == nullptr;
   const float cap_in = a.softcap > 0.f ? 1.f / a.softcap : 0.f, cap_out = a.softcap * kLog2e;
 
-  uint32_t filled = 0, used = 0;                  // stages this warp has asked for and taken from its ring
+  const float out_scale = a.out_scale;
+  int fill = 0, take = 0;                         // the stages of this warp's ring that are filled and taken next,
+  uint32_t phase = 0;                             // and the parity of the latter's barrier
   bool dead = false;                              // a copy did not arrive (reported); the warp gives up
   while (u < u_end && !dead) {
     int4 info = per == 1 ? sm.info[b] : owner_info<LIST>(a, b, false, without);
@@ -210,16 +215,17 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
     // ---- copies
     const int32_t* pages = a.table + (long long)slot * g.max_pages;
     const int32_t* list = LIST ? a.t.pages + ((long long)first_token * H + h) * a.t.n_select : nullptr;
-    // lane l keeps the place of block 32 n + l of the segment (block of the pool, and with lists its first token): of the current
-    // 32, and asked for ahead of the next 32
+    // lane l keeps the place of block 32 n + l of the segment (block of the pool, and with lists its first token): of the 32 that are
+    // being asked for, and looked up ahead of the next 32
     struct Place {
-      int page, tok;
+      int blk, tok;
     };
+    const int in_page = g.page_shift - 4;          // log2 of a page's blocks
     const auto look_up = [&](int group) {
       Place p = {0, kFqNowhere};
       const int j = 32 * group + lane;
       if (j < nb) {
-        int logical = (blk0 + j) * kQuantBlock >> g.page_shift;
+        int logical = (blk0 + j) >> in_page;
         if (LIST) {
           const int own = (len - 1) >> g.page_shift;
           const int e = list[logical];
@@ -227,12 +233,14 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
           logical = e < 0 || e > own ? -1 : e;
         }
         if (logical >= 0) {
-          p.page = pages[logical];
-          p.tok = (logical << g.page_shift) + ((blk0 + j) * kQuantBlock & (g.page_tokens - 1));
-          if (p.page < 0 || p.page >= g.n_pages) {
+          int page = pages[logical];
+          if (page < 0 || page >= g.n_pages) {
             report_opt(a.status, ECHOKV_EBADPAGE);
-            p.page = 0;
+            page = 0;
           }
+          const int inside = (blk0 + j) & ((1 << in_page) - 1);
+          p.blk = ((page * H + h) << in_page) + inside;
+          p.tok = (logical << g.page_shift) + inside * kQuantBlock;
         }
       }
       return p;
@@ -252,24 +260,33 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
       if (ok) Quad<T>::load16(qp + KC * 16 * c + 4 * x, &qv[x]);
       else Quad<T>::zero16(&qv[x]);
     Place next = look_up(1);
-    int group = 0;
     const int n_steps = (nb + NB - 1) / NB;
-    const auto issue = [&](int step) {
-      const int st = filled % kFqStages;
-      const uint32_t bar = smem_u32(&sm.full[warp][st]), dst = ring + st * fq_stage_bytes(D);
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        const int j = step * NB + n;
-        const int page = __shfl_sync(0xffffffffu, (j >> 5) == group ? cur.page : next.page, j & 31);
-        if (lane == 0 && j < nb) {
-          if (n == 0) mbar_arrive_expect_tx(bar, j + 1 < nb ? 2 * BB : BB);
-          const int inside = (blk0 + j) & ((g.page_tokens >> 4) - 1);
-          bulk_load(dst + n * BB, g.blocks + (((long long)page * H + h) * (g.page_tokens >> 4) + inside) * BB, BB, bar);
-        }
+    int left = 0;                                  // stages asked for and not yet taken
+    int asked = 0;                                 // steps whose copies are under way or done
+    const auto issue = [&]() {
+      if ((asked & 15) == 0 && asked > 0) {
+        cur = next;
+        next = look_up((asked >> 4) + 1);
       }
-      ++filled;
+      const int j = asked * NB;
+      const int b0 = __shfl_sync(0xffffffffu, cur.blk, j & 31), b1 = __shfl_sync(0xffffffffu, cur.blk, (j + 1) & 31);
+      int2 tok;
+      if (LIST) {
+        tok.x = __shfl_sync(0xffffffffu, cur.tok, j & 31);
+        tok.y = __shfl_sync(0xffffffffu, cur.tok, (j + 1) & 31);
+      }
+      if (lane == 0) {
+        const uint32_t bar = smem_u32(&sm.full[warp][fill]), dst = ring + fill * fq_stage_bytes(D);
+        if (LIST) sm.tok[warp][fill] = tok;
+        mbar_arrive_expect_tx(bar, j + 1 < nb ? 2 * BB : BB);
+        bulk_load(dst, g.blocks + (long long)b0 * BB, BB, bar);
+        if (j + 1 < nb) bulk_load(dst + BB, g.blocks + (long long)b1 * BB, BB, bar);
+      }
+      ++asked;
+      ++left;
+      fill = fill == kFqStages - 1 ? 0 : fill + 1;
     };
-    for (int s = 0; s < min(kFqStages, n_steps); ++s) issue(s);
+    while (asked < min(kFqStages, n_steps)) issue();
 
     {
       // (magnitudes compare as integers; an infinity or NaN gives the factor 1 and goes on through the products)
@@ -321,49 +338,55 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
       return y;
     };
 
-#pragma unroll 1
-    for (int step = 0; step < n_steps; ++step) {
-      const int j = step * NB;
-      if ((j & 31) == 0 && j > 0) {
-        ++group;
-        cur = next;
-        next = look_up(group + 1);
-      }
-      const int st = used % kFqStages;
-      if (!__all_sync(0xffffffffu, warp_wait(smem_u32(&sm.full[warp][st]), (used / kFqStages) & 1))) {
-        dead = true;
-        break;
-      }
-      ++used;
-      // an odd last block stands in for its partner, which is masked
-      const bool two = j + 1 < nb;
-      uint32_t src[NB];
+    // One step: two blocks of the stage that has arrived.  MASKED: some of their tokens may be unseen, or the second block is not there.
+    const auto attend = [&](auto masked_tag, int step, uint32_t src) {
+      constexpr bool MASKED = decltype(masked_tag)::value;
       int tok0[NB];
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        src[n] = ring + st * fq_stage_bytes(D) + (two ? n : 0) * BB;
-        tok0[n] = LIST ? __shfl_sync(0xffffffffu, cur.tok, (j + n) & 31) : (blk0 + j + n) * kQuantBlock;
-        if (n > 0 && !two) tok0[n] = kFqNowhere;
+      if (LIST) {
+        const int2 t = sm.tok[warp][take];
+        tok0[0] = t.x;
+        tok0[1] = t.y;
+      } else {
+        tok0[0] = (blk0 + step * NB) * kQuantBlock;
+        tok0[1] = tok0[0] + kQuantBlock;
       }
-      const bool masked = max(tok0[0], tok0[1]) + kQuantBlock - 1 > pos_first;
+      const bool two = !MASKED || step * NB + 1 < nb;
+      if (!two) tok0[1] = kFqNowhere;              // (the first block stands in for it)
       const auto seen = [&](int tok, int e) { return tok <= pos[e] || (!LIST && tok < prefix); };
+      const uint32_t part[NB] = {src, two ? src + BB : src};
+
+      // ---- the values' codes and scales (used last: on their way while the scores are worked out)
+      uint32_t vt[NB][2][2][D / 64], vs[NB][2];    // [tokens 2 c, + 1 | 8 on][which of the two]
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const uint32_t at = part[n] + 8 * D + t * 4 * D + lane * 8 * KC;
+          if constexpr (D == 128) {
+            const uint4 v = lds16(at);
+            vt[n][t][0][0] = v.x; vt[n][t][0][D / 64 - 1] = v.y; vt[n][t][1][0] = v.z; vt[n][t][1][D / 64 - 1] = v.w;
+          } else {
+            const uint2 v = lds8(at);
+            vt[n][t][0][0] = v.x; vt[n][t][1][0] = v.y;
+          }
+          uint16_t w;
+          asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(part[n] + 17 * D + (r * NT / 16) * 16 + 8 * t + 2 * c) : "memory");
+          vs[n][t] = e4m3_scales(w);
+        }
 
       // ---- scores
       float sc[NB][4];                            // [n][2 t + e]: token r + 8 t of block n, query row 2 c + e
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
-        float sb[4] = {0.f, 0.f, 0.f, 0.f};        // two chains of products
-#pragma unroll
-        for (int f = 0; f < 4; ++f) sc[n][f] = 0.f;
         uint32_t kw[2][2 * KC], ks[2][KC];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const uint32_t at = src[n] + t * 4 * D + lane * 8 * KC;
+          const uint32_t at = part[n] + t * 4 * D + lane * 8 * KC;
           if constexpr (D == 128) {
             const uint4 v = lds16(at);
             kw[t][0] = v.x; kw[t][1] = v.y; kw[t][2 * KC - 2] = v.z; kw[t][2 * KC - 1] = v.w;
             uint16_t w;
-            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(src[n] + 16 * D + (r + 8 * t) * 8 + 2 * c) : "memory");
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(part[n] + 16 * D + (r + 8 * t) * 8 + 2 * c) : "memory");
             const uint32_t s = e4m3_scales(w);
             ks[t][0] = __byte_perm(s, 0u, 0x1010);
             ks[t][KC - 1] = __byte_perm(s, 0u, 0x3232);
@@ -371,25 +394,37 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
             const uint2 v = lds8(at);
             kw[t][0] = v.x; kw[t][1] = v.y;
             uint16_t w;
-            asm volatile("{\n\t.reg .u8 b;\n\tld.shared.u8 b, [%1];\n\tcvt.u16.u8 %0, b;\n\t}" : "=h"(w) : "r"(src[n] + 16 * D + (r + 8 * t) * 4 + c) : "memory");
+            asm volatile("{\n\t.reg .u8 b;\n\tld.shared.u8 b, [%1];\n\tcvt.u16.u8 %0, b;\n\t}" : "=h"(w) : "r"(part[n] + 16 * D + (r + 8 * t) * 4 + c) : "memory");
             const uint32_t s = e4m3_scales(w);
             ks[t][0] = __byte_perm(s, 0u, 0x1010);
           }
         }
+        // two chains of products.  (fp32: the tensor core cuts its sums off where it adds to them, 2^-23 of the sum each time and always
+        // towards 0, so a word's products are summed by themselves and the low-order halves' apart.)
+        float sb[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int f = 0; f < 4; ++f) sc[n][f] = 0.f;
 #pragma unroll
         for (int w = 0; w < 2 * KC; ++w) {
           uint32_t x[2][4];
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
-            x[t][0] = fp4_mul(e2m1_pair<0>(kw[t][w]), ks[t][w / 2]);
-            x[t][1] = fp4_mul(e2m1_pair<1>(kw[t][w]), ks[t][w / 2]);
-            x[t][2] = fp4_mul(e2m1_pair<2>(kw[t][w]), ks[t][w / 2]);
-            x[t][3] = fp4_mul(e2m1_pair<3>(kw[t][w]), ks[t][w / 2]);
-          }
+            e2m1_bytes(kw[t][w], x[t]);
 #pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            mma_m16n8k16_f16(s ? sb : sc[n], x[0][2 * s], x[1][2 * s], x[0][2 * s + 1], x[1][2 * s + 1], qh[2 * w + s][0], qh[2 * w + s][1]);
-            if (kF32) mma_m16n8k16_f16(s ? sc[n] : sb, x[0][2 * s], x[1][2 * s], x[0][2 * s + 1], x[1][2 * s + 1], ql[2 * w + s][0], ql[2 * w + s][1]);
+            for (int i = 0; i < 4; ++i) x[t][i] = fp4_mul(x[t][i], ks[t][w / 2]);
+          }
+          if constexpr (kF32) {
+            float hi[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              mma_m16n8k16_f16(hi, x[0][2 * s], x[1][2 * s], x[0][2 * s + 1], x[1][2 * s + 1], qh[2 * w + s][0], qh[2 * w + s][1]);
+              mma_m16n8k16_f16(sb, x[0][2 * s], x[1][2 * s], x[0][2 * s + 1], x[1][2 * s + 1], ql[2 * w + s][0], ql[2 * w + s][1]);
+            }
+#pragma unroll
+            for (int f = 0; f < 4; ++f) sc[n][f] += hi[f];
+          } else {
+            mma_m16n8k16_f16(sc[n], x[0][0], x[1][0], x[0][1], x[1][1], qh[2 * w][0], qh[2 * w][1]);
+            mma_m16n8k16_f16(sb, x[0][2], x[1][2], x[0][3], x[1][3], qh[2 * w + 1][0], qh[2 * w + 1][1]);
           }
         }
 #pragma unroll
@@ -397,8 +432,7 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
       }
 
       // ---- probabilities as operands (ph[n][t]: query row r, tokens 8 t + 2 c, + 1), the reference moved if needed
-      uint32_t ph[NB][2], pl[NB][2];
-      bool above = false;
+      float most[2] = {-INFINITY, -INFINITY};
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         if (plain) {
@@ -408,19 +442,19 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
 #pragma unroll
           for (int i = 0; i < 4; ++i) sc[n][i] = score(sc[n][i] * c_row[i & 1], i & 1, tok0[n] + 8 * (i >> 1) + r) - m_ref[i & 1];
         }
-        if (masked) {
+        if (MASKED) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             if (!seen(tok0[n] + 8 * (i >> 1) + r, i & 1)) sc[n][i] = -INFINITY;
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) above |= sc[n][i] > grow[i & 1];
+        for (int e = 0; e < 2; ++e) most[e] = fmaxf(most[e], fmaxf(sc[n][e], sc[n][2 + e]));
       }
-      if (__any_sync(0xffffffffu, above)) {
+      if (__any_sync(0xffffffffu, most[0] > grow[0] || most[1] > grow[1])) {
         float alpha[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float mx = fmaxf(fmaxf(sc[0][e], sc[0][2 + e]), fmaxf(sc[1][e], sc[1][2 + e]));
+          float mx = most[e];
 #pragma unroll
           for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
           mx -= kFqBelow;
@@ -443,6 +477,7 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
 #pragma unroll
           for (int f = 0; f < 4; ++f) o[m][f] *= alpha[f & 1];
       }
+      uint32_t ph[NB][2], pl[NB][2];
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         float p[4];
@@ -459,59 +494,88 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
         }
       }
 
-      // ---- output
+      // ---- output (fp32: the step's products are summed by themselves, as above)
+      float step_o[kF32 ? MT : 1][4];
+      if (kF32) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int f = 0; f < 4; ++f) step_o[kF32 ? m : 0][f] = 0.f;
+      }
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
-        uint32_t even[2][D / 64], odd[2][D / 64], vs[2];      // [tokens 2 c, + 1 | 8 on]: features 2 i and 2 i + 1, a byte for both tokens
+        // (behind the sequence's end there may be anything: a NaN times a probability of 0)
+        if (MASKED) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const uint32_t at = src[n] + 8 * D + t * 4 * D + lane * 8 * KC;
-          uint32_t t0[D / 64], t1[D / 64];
-          if constexpr (D == 128) {
-            const uint4 v = lds16(at);
-            t0[0] = v.x; t0[D / 64 - 1] = v.y; t1[0] = v.z; t1[D / 64 - 1] = v.w;
-          } else {
-            const uint2 v = lds8(at);
-            t0[0] = v.x; t1[0] = v.y;
-          }
-#pragma unroll
-          for (int w = 0; w < D / 64; ++w) {
-            even[t][w] = (t0[w] & 0x0f0f0f0fu) | ((t1[w] << 4) & 0xf0f0f0f0u);
-            odd[t][w] = ((t0[w] >> 4) & 0x0f0f0f0fu) | (t1[w] & 0xf0f0f0f0u);
-          }
-          uint16_t w;
-          asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(src[n] + 17 * D + (r * NT / 16) * 16 + 8 * t + 2 * c) : "memory");
-          vs[t] = e4m3_scales(w);
-          // (behind the sequence's end there may be anything: a NaN times a probability of 0)
-          if (masked) {
+          for (int t = 0; t < 2; ++t) {
             const int tok = tok0[n] + 8 * t + 2 * c;
-            if (tok >= len) vs[t] = 0u;
-            else if (tok + 1 >= len) vs[t] &= 0xffffu;
+            if (tok >= len) vs[n][t] = 0u;
+            else if (tok + 1 >= len) vs[n][t] &= 0xffffu;
           }
         }
 #pragma unroll
         for (int w = 0; w < D / 64; ++w) {
-          const auto tile_of = [&](auto byte_tag) {
-            constexpr int B = decltype(byte_tag)::value;
-            const uint32_t a0 = fp4_mul(e2m1_pair<B>(even[0][w]), vs[0]), a1 = fp4_mul(e2m1_pair<B>(odd[0][w]), vs[0]);
-            const uint32_t a2 = fp4_mul(e2m1_pair<B>(even[1][w]), vs[1]), a3 = fp4_mul(e2m1_pair<B>(odd[1][w]), vs[1]);
-            mma_m16n8k16_f16(o[4 * w + B], a0, a1, a2, a3, ph[n][0], ph[n][1]);
-            if (kF32) mma_m16n8k16_f16(o[4 * w + B], a0, a1, a2, a3, pl[n][0], pl[n][1]);
-          };
-          tile_of(std::integral_constant<int, 0>());
-          tile_of(std::integral_constant<int, 1>());
-          tile_of(std::integral_constant<int, 2>());
-          tile_of(std::integral_constant<int, 3>());
+          uint32_t x[2][4], y[2][4];
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            // features 2 i and 2 i + 1, a byte for both tokens
+            e2m1_bytes(fp4_zip(vt[n][t][0][w], vt[n][t][1][w] << 4), x[t]);
+            e2m1_bytes(fp4_zip(vt[n][t][0][w] >> 4, vt[n][t][1][w]), y[t]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              x[t][i] = fp4_mul(x[t][i], vs[n][t]);
+              y[t][i] = fp4_mul(y[t][i], vs[n][t]);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float (&acc)[4] = kF32 ? step_o[kF32 ? 4 * w + i : 0] : o[4 * w + i];
+            mma_m16n8k16_f16(acc, x[0][i], y[0][i], x[1][i], y[1][i], ph[n][0], ph[n][1]);
+            if (kF32) mma_m16n8k16_f16(acc, x[0][i], y[0][i], x[1][i], y[1][i], pl[n][0], pl[n][1]);
+          }
         }
       }
+      if (kF32) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int f = 0; f < 4; ++f) o[m][f] += step_o[kF32 ? m : 0][f];
+      }
+    };
+#pragma unroll 1
+    for (int step = 0; step < n_steps; ++step) {
+      if (!__all_sync(0xffffffffu, warp_wait(smem_u32(&sm.full[warp][take]), phase))) {
+        dead = true;
+        break;
+      }
+      bool masked;
+      if (LIST) {
+        const int2 t = sm.tok[warp][take];
+        masked = max(t.x, t.y) + kQuantBlock - 1 > pos_first || step * NB + 1 >= nb;
+      } else {
+        masked = (blk0 + (step + 1) * NB) * kQuantBlock - 1 > pos_first || step * NB + 1 >= nb;
+      }
+      const uint32_t src = ring + take * fq_stage_bytes(D);
+      if (masked) attend(std::true_type(), step, src); else attend(std::false_type(), step, src);
       __syncwarp();                                // (all lanes have read the stage: it may be overwritten)
-      if (step + kFqStages < n_steps) issue(step + kFqStages);
+      if (++take == kFqStages) {
+        take = 0;
+        phase ^= 1;
+      }
+      --left;
+      if (asked < n_steps) issue();
     }
     if (dead) {
       // let every copy that was asked for land, as far as it does, before the shared memory is given back
       if (lane == 0) {
         report_opt(a.status, ECHOKV_ETIMEOUT);
-        for (; used < filled; ++used) mbar_drain(smem_u32(&sm.full[warp][used % kFqStages]), (used / kFqStages) & 1);
+        for (; left > 0; --left) {
+          mbar_drain(smem_u32(&sm.full[warp][take]), phase);
+          if (++take == kFqStages) {
+            take = 0;
+            phase ^= 1;
+          }
+        }
       }
       break;
     }
@@ -527,7 +591,7 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
       for (int e = 0; e < 2; ++e) {
         const int qrow = tile * kFqRows + 2 * c + e;
         if (qrow < n_rows) {
-          const float inv = l_run[e] == 0.f ? 0.f : a.out_scale / l_run[e];
+          const float inv = l_run[e] == 0.f ? 0.f : out_scale / l_run[e];
           float v[NT];
 #pragma unroll
           for (int m = 0; m < MT; ++m) {
@@ -602,7 +666,7 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
       const int4 s = per == 1 ? sm.info[first.b] : owner_info<LIST>(a, first.b, false, without);
       const int qrow = first.tile * kFqRows + warp;
       if (qrow < s.w * a.group) {
-        const float inv = l == 0.f ? 0.f : a.out_scale / l;
+        const float inv = l == 0.f ? 0.f : out_scale / l;
         T* dst = static_cast<T*>(a.out) +
                  ((long long)(s.z + (qrow >> a.group_shift)) * a.n_q_heads + first.h * a.group + (qrow & (a.group - 1))) * D + lane * E;
 #pragma unroll
@@ -637,6 +701,7 @@ __global__ void __launch_bounds__(kFqMergeThreads) fp4_merge_kernel(const __grid
     }
   }
   const QaDesc d = ws.desc[blockIdx.x];
+  const float out_scale = a.out_scale;
   if (d.n_parts == 0) return;
   const auto part = [&](int p) -> long long { return ((long long)(blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * kFqRows + row; };
   const int4 s = owner_info<LIST>(a, d.b, false, false);
@@ -655,7 +720,7 @@ __global__ void __launch_bounds__(kFqMergeThreads) fp4_merge_kernel(const __grid
   }
   const int qrow = d.tile * kFqRows + row;
   if (qrow >= s.w * a.group) return;
-  const float inv = l == 0.f ? 0.f : a.out_scale / l;
+  const float inv = l == 0.f ? 0.f : out_scale / l;
   T* dst = static_cast<T*>(a.out) +
            ((long long)(s.z + (qrow >> a.group_shift)) * a.n_q_heads + d.h * a.group + (qrow & (a.group - 1))) * D + lane * E;
 #pragma unroll

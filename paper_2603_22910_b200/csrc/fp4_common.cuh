@@ -5,17 +5,28 @@
 
 namespace echokv {
 
-// byte I of w (two e2m1 codes) -> fp16 pair, low half first; exact
-template <int I>
+// byte 0 of w (two e2m1 codes) -> fp16 pair, low half first; exact
 __device__ __forceinline__ uint32_t e2m1_pair(uint32_t w) {
   uint32_t r;
-  asm("{\n\t.reg .b8 b;\n\tcvt.u8.u32 b, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, b;\n\t}" : "=r"(r) : "r"(w >> (8 * I)));
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, b0;\n\t}" : "=r"(r) : "r"(w));
   return r;
+}
+// all four bytes
+__device__ __forceinline__ void e2m1_bytes(uint32_t w, uint32_t (&h)[4]) {
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\tcvt.rn.f16x2.e2m1x2 %2, b2;\n\tcvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
 }
 // two e4m3 scales (low 16 bits) -> fp16 pair; exact
 __device__ __forceinline__ uint32_t e4m3_scales(uint32_t w) {
   uint32_t r;
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)w));
+  return r;
+}
+// the low halves of a's bytes and of b's << 4 (b given shifted), or the high halves of a's (given shifted) and of b's
+__device__ __forceinline__ uint32_t fp4_zip(uint32_t low, uint32_t high) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xe4;" : "=r"(r) : "r"(low), "r"(high), "r"(0x0f0f0f0fu));      // low & m | high & ~m
   return r;
 }
 __device__ __forceinline__ uint32_t fp4_mul(uint32_t a, uint32_t b) {

@@ -633,8 +633,8 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
         const uint32_t s2 = e4m3_scales(x.scale | x.scale << 8);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          w[e] = there ? fp4_mul(e2m1_pair<0>(x.codes.x >> (8 * e)), s2) : 0u;
-          w[4 + e] = there ? fp4_mul(e2m1_pair<0>(x.codes.y >> (8 * e)), s2) : 0u;
+          w[e] = there ? fp4_mul(e2m1_pair(x.codes.x >> (8 * e)), s2) : 0u;
+          w[4 + e] = there ? fp4_mul(e2m1_pair(x.codes.y >> (8 * e)), s2) : 0u;
         }
       };
       for (bool more = ck_first(a, t); more && alive; more = ck_next(a, t)) {
