@@ -796,10 +796,17 @@ class Fp4Cache:
         import torch
         cfg, T, H, d = self.cfg, slot_map.shape[0], self.cfg.n_kv_heads, self.cfg.head_dim
         with _memory_of(stream):
-            k_out = torch.empty((T, H, d), dtype=self.tdtype, device=slot_map.device) if k_out is None else k_out
-            v_out = torch.empty((T, H, d), dtype=self.tdtype, device=slot_map.device) if v_out is None else v_out
-        at = _rows(k_out, T, H, d, self.tdtype, "k_out", cfg.device) + _rows(v_out, T, H, d, self.tdtype, "v_out", cfg.device)
-        _check(lib().echokv_fp4_read(C.byref(cfg), C.byref(self._c), _dense(slot_map, torch.int64, T, "slot_map", cfg.device), T, *at,
+            if k_out is None:
+                k_out = slot_map.new_empty((T, H, d), dtype=self.tdtype)
+                kp, ks = k_out.data_ptr(), H * d
+            else:
+                kp, ks = _rows(k_out, T, H, d, self.tdtype, "k_out", cfg.device)
+            if v_out is None:
+                v_out = slot_map.new_empty((T, H, d), dtype=self.tdtype)
+                vp, vs = v_out.data_ptr(), H * d
+            else:
+                vp, vs = _rows(v_out, T, H, d, self.tdtype, "v_out", cfg.device)
+        _check(lib().echokv_fp4_read(C.byref(cfg), C.byref(self._c), _dense(slot_map, torch.int64, T, "slot_map", cfg.device), T, kp, ks, vp, vs,
                                      _dense(status, torch.int32, 1, "status", cfg.device), _stream_on(cfg.device, stream)), "echokv_fp4_read")
         return k_out, v_out
 

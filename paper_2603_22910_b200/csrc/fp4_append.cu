@@ -83,6 +83,7 @@ __global__ void __launch_bounds__(kFaThreads, 4) fp4_append_kernel(const __grid_
   constexpr int G = D / kFp4Group;                 // groups of a head (4 or 8 lanes side by side)
   __shared__ __align__(16) float2 cs[kFaTokens][64];
   const int half = a.rot_dim >> 1, pieces = half >> 3, tid = threadIdx.x, lane = tid & 31;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int t0 = blockIdx.x * tokens_per_block, nt = min(tokens_per_block, a.n_tokens - t0);
   const Fp4Geom& g = a.g;
   const int H = g.n_kv_heads;

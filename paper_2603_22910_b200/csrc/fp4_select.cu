@@ -17,9 +17,14 @@ namespace echokv {
 
 namespace {
 
-constexpr int kFsWarps = 16;
-constexpr int kFsThreads = kFsWarps * 32;
-constexpr int kFsStep = kFsWarps * 16;             // pages that a block takes at once
+// Few (token, head) pairs: blocks of 16 warps that fetch a step ahead; many: of 8, and four blocks to an SM.
+template <int NW>
+struct FsShape {
+  static constexpr int kThreads = NW * 32;
+  static constexpr int kStep = NW * 16;            // pages that a block takes at once
+  static constexpr bool kAhead = NW == 16;
+};
+constexpr int kFsMergeWarps = 8;
 constexpr int kFsEntries = 16384;                  // keys of a block, of all its tokens
 constexpr int kFsMaxTokens = 8;                    // tokens of a block: each has room for 2048 keys, ECHOKV_FP4_MAX_SELECT and a step
 constexpr int kFsMaxParts = 320;                   // (token, head, part of the pages) with a place in the workspace
@@ -37,10 +42,10 @@ struct FsPart {
   }
 };
 
-struct FsSmem {
-  uint32_t key[ECHOKV_FP4_MAX_SELECT], page[ECHOKV_FP4_MAX_SELECT];
+// of the warps that choose for one token
+struct FsGroup {
   uint32_t hist[256];
-  uint32_t red[kFsWarps][4];
+  uint32_t red[16][4];
   uint32_t bin, want, whole;
 };
 
@@ -57,13 +62,29 @@ __device__ __forceinline__ uint32_t ordered(float x) {
   return b >> 31 ? ~b : b | 0x80000000u;
 }
 
-// The k largest of n keys (of equal ones the first; all that are not 0 if there are no more) and their pages, in their order, to
-// sm.key / sm.page; returns how many.  For the whole block, after a barrier; ends with one.
-__device__ __noinline__ int choose(const uint32_t* key, const uint32_t* page, int n, int k, FsSmem& sm) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+// Which of n keys are the k largest (of equal ones the first; all that are not 0 if there are no more).  For a group of `warps` warps (warp:
+// this one's number among them, bar: their barrier), after a barrier of theirs.
+struct FsChoice {
+  uint32_t lo, bin, want;                          // keys whose (key - lo) << up >> shift is above bin, and the first `want` of those that are bin
+  int up, shift;
+  bool all, none;
+  // +1: taken in any case, 0: one of the last bin, -1: not taken
+  __device__ __forceinline__ int side(uint32_t x) const {
+    if (x == 0) return -1;
+    if (x == kFsAlways || all) return 1;
+    if (none) return -1;
+    const uint32_t p = (x - lo) << up >> shift;
+    return p > bin ? 1 : p == bin ? 0 : -1;
+  }
+};
+__device__ __forceinline__ void group_sync(int bar, int warps) { asm volatile("bar.sync %0, %1;" ::"r"(bar), "r"(32 * warps) : "memory"); }
+
+__device__ __noinline__ FsChoice choose(const uint32_t* key, int n, int k, FsGroup& sm, int warp, int warps, int bar) {
+  const int lane = threadIdx.x & 31, tid = warp * 32 + lane, threads = 32 * warps;
   // what lies between 0 and always: how much, from where to where
   uint32_t always = 0, some = 0, lo = 0xffffffffu, hi = 0;
-  for (int i = tid; i < n; i += kFsThreads) {
+#pragma unroll 4
+  for (int i = tid; i < n; i += threads) {
     const uint32_t x = key[i];
     const bool normal = x != 0 && x != kFsAlways;
     always += x == kFsAlways;
@@ -81,32 +102,34 @@ __device__ __noinline__ int choose(const uint32_t* key, const uint32_t* page, in
     sm.red[warp][2] = lo;
     sm.red[warp][3] = hi;
   }
-  if (tid < 256) sm.hist[tid] = 0;
-  __syncthreads();
+  for (int i = tid; i < 256; i += threads) sm.hist[i] = 0;
+  group_sync(bar, warps);
   always = some = hi = 0;
   lo = 0xffffffffu;
-#pragma unroll
-  for (int w = 0; w < kFsWarps; ++w) {
+  for (int w = 0; w < warps; ++w) {
     always += sm.red[w][0];
     some += sm.red[w][1];
     lo = min(lo, sm.red[w][2]);
     hi = max(hi, sm.red[w][3]);
   }
-  // the normal keys' place between lo and hi, from bit 31 down
-  const int up = hi > lo ? __clz(hi - lo) : 0;
-  const auto place = [&](uint32_t x) { return (x - lo) << up; };
-  uint32_t want = (uint32_t)k - min((uint32_t)k, always), bin = 0;      // normal keys to be taken; the top bits of the least one's place
-  int shift = 32;
-  const bool all = some <= want, none = !all && want == 0;
-  while (!all && !none && shift > 0) {
-    shift -= 8;
-    for (int i = tid; i < n; i += kFsThreads) {
+  FsChoice f;
+  f.lo = lo;
+  f.up = hi > lo ? __clz(hi - lo) : 0;             // the normal keys' place between lo and hi, from bit 31 down
+  f.want = (uint32_t)k - min((uint32_t)k, always);
+  f.bin = 0;
+  f.shift = 32;
+  f.all = some <= f.want;
+  f.none = !f.all && f.want == 0;
+  while (!f.all && !f.none && f.shift > 0) {
+    f.shift -= 8;
+#pragma unroll 4
+    for (int i = tid; i < n; i += threads) {
       const uint32_t x = key[i];
       if (x == 0 || x == kFsAlways) continue;
-      const uint32_t p = place(x);
-      if (shift == 24 || p >> (shift + 8) == bin) atomicAdd(&sm.hist[p >> shift & 255], 1u);
+      const uint32_t p = (x - lo) << f.up;
+      if (f.shift == 24 || p >> (f.shift + 8) == f.bin) atomicAdd(&sm.hist[p >> f.shift & 255], 1u);
     }
-    __syncthreads();
+    group_sync(bar, warps);
     if (warp == 0) {
       // eight bins to a lane, from the top
       uint32_t c[8], sum = 0;
@@ -123,50 +146,48 @@ __device__ __noinline__ int choose(const uint32_t* key, const uint32_t* page, in
         if (lane >= o) before += y;
       }
       before -= sum;
-      if (before < want && want <= before + sum) {
+      if (before < f.want && f.want <= before + sum) {
 #pragma unroll
         for (int b = 0; b < 8; ++b) {
-          if (before < want && want <= before + c[b]) {
-            sm.bin = bin << 8 | (uint32_t)(255 - 8 * lane - b);
-            sm.want = want - before;
-            sm.whole = want - before == c[b];
+          if (before < f.want && f.want <= before + c[b]) {
+            sm.bin = f.bin << 8 | (uint32_t)(255 - 8 * lane - b);
+            sm.want = f.want - before;
+            sm.whole = f.want - before == c[b];
           }
           before += c[b];
         }
       }
     }
-    __syncthreads();
-    bin = sm.bin;
-    want = sm.want;
+    group_sync(bar, warps);
+    f.bin = sm.bin;
+    f.want = sm.want;
     if (sm.whole) break;                           // (the bin is taken as a whole: nothing below it matters)
   }
-  // +1: taken in any case, 0: in the last bin, where the first `want` are taken, -1: not taken
-  const auto side = [&](uint32_t x) {
-    if (x == 0) return -1;
-    if (x == kFsAlways || all) return 1;
-    if (none) return -1;
-    const uint32_t p = place(x) >> shift;
-    return p > bin ? 1 : p == bin ? 0 : -1;
-  };
+  return f;
+}
+
+// The chosen ones of n keys in their order: take(place, index) for each, by all warps of a group.  Returns how many (k at most).
+template <typename F>
+__device__ __forceinline__ int chosen(const FsChoice& f, const uint32_t* key, int n, int k, FsGroup& sm, int warp, int warps, int bar, const F& take) {
+  const int lane = threadIdx.x & 31;
   // every warp has a run of the keys
-  const int run = ((n + kFsWarps - 1) / kFsWarps + 31) & ~31, from = warp * run, until = min(n, from + run);
+  const int run = ((n + warps - 1) / warps + 31) & ~31, from = min(n, warp * run), until = min(n, from + run);
   uint32_t above = 0, equal = 0;
   for (int i = from + lane; i < until; i += 32) {
-    const int s = side(key[i]);
+    const int s = f.side(key[i]);
     above += s > 0;
     equal += s == 0;
   }
   above = __reduce_add_sync(0xffffffffu, above);
   equal = __reduce_add_sync(0xffffffffu, equal);
-  __syncthreads();                                 // (sm.red has been read)
+  group_sync(bar, warps);                          // (sm.red has been read)
   if (lane == 0) {
     sm.red[warp][0] = above;
     sm.red[warp][1] = equal;
   }
-  __syncthreads();
+  group_sync(bar, warps);
   uint32_t before_above = 0, before_equal = 0, all_above = 0, all_equal = 0;
-#pragma unroll
-  for (int w = 0; w < kFsWarps; ++w) {
+  for (int w = 0; w < warps; ++w) {
     if (w < warp) {
       before_above += sm.red[w][0];
       before_equal += sm.red[w][1];
@@ -177,21 +198,50 @@ __device__ __noinline__ int choose(const uint32_t* key, const uint32_t* page, in
   const uint32_t lower = (1u << lane) - 1;
 #pragma unroll 1
   for (int i0 = from; i0 < until; i0 += 32) {
-    const int i = i0 + lane;
-    const uint32_t x = i < until ? key[i] : 0;
-    const int s = side(x);
+    const int i = i0 + lane, s = f.side(i < until ? key[i] : 0u);
     const uint32_t b_above = __ballot_sync(0xffffffffu, s > 0), b_equal = __ballot_sync(0xffffffffu, s == 0);
     const uint32_t rank_equal = before_equal + __popc(b_equal & lower), rank_above = before_above + __popc(b_above & lower);
-    const uint32_t at = rank_above + min(rank_equal, want);
-    if ((s > 0 || (s == 0 && rank_equal < want)) && at < (uint32_t)k) {      // (k at most, whatever the keys)
-      sm.key[at] = x;
-      sm.page[at] = page[i];
-    }
+    const uint32_t at = rank_above + min(rank_equal, f.want);
+    if ((s > 0 || (s == 0 && rank_equal < f.want)) && at < (uint32_t)k) take((int)at, i);      // (k at most, whatever the keys)
     before_above += __popc(b_above);
     before_equal += __popc(b_equal);
   }
-  __syncthreads();
-  return (int)min((uint32_t)k, all_above + min(all_equal, want));
+  return (int)min((uint32_t)k, all_above + min(all_equal, f.want));
+}
+// The pages of a buffer's keys: those of the first `kept` ones are listed, the others follow one another.
+struct FsPages {
+  uint32_t* list;
+  int kept;
+  uint32_t start;
+  __device__ __forceinline__ uint32_t operator()(int i) const { return i < kept ? list[i] : start + (uint32_t)(i - kept); }
+};
+// The buffer cut down to the k chosen ones, listed, by the group's first warp alone (what it writes lies before what it still
+// reads); where there are fewer, keys of 0 behind them.
+__device__ __forceinline__ void cut_down(uint32_t* key, const FsPages& page, int n, int k, FsGroup& sm, int warp, int warps, int bar) {
+  const FsChoice f = choose(key, n, k, sm, warp, warps, bar);
+  if (warp == 0) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t lower = (1u << lane) - 1;
+    uint32_t above = 0, equal = 0;
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += 32) {
+      const uint32_t x = i0 + lane < n ? key[i0 + lane] : 0u, y = i0 + lane < n ? page(i0 + lane) : 0u;
+      const int s = f.side(x);
+      const uint32_t b_above = __ballot_sync(0xffffffffu, s > 0), b_equal = __ballot_sync(0xffffffffu, s == 0);
+      const uint32_t rank_equal = equal + __popc(b_equal & lower);
+      const uint32_t at = above + __popc(b_above & lower) + min(rank_equal, f.want);
+      __syncwarp();
+      if ((s > 0 || (s == 0 && rank_equal < f.want)) && at < (uint32_t)k) {
+        key[at] = x;
+        page.list[at] = y;
+      }
+      above += __popc(b_above);
+      equal += __popc(b_equal);
+      __syncwarp();
+    }
+    for (uint32_t i = above + min(equal, f.want) + lane; i < (uint32_t)k; i += 32) key[i] = 0u;
+  }
+  group_sync(bar, warps);
 }
 
 // One token: its sequence's row of the block table and its own page (-1 with an error).
@@ -213,16 +263,17 @@ __device__ __forceinline__ FsToken token_of(const Fp4SelectArgs& a, int i) {
   return t;
 }
 // all pages up to the own one and -1 behind them (none: own = -1)
-__device__ __forceinline__ void write_all(const Fp4SelectArgs& a, int token, int h, int own) {
+__device__ __forceinline__ void write_all(const Fp4SelectArgs& a, int token, int h, int own, int tid, int threads) {
   int32_t* out = a.out + ((long long)token * a.g.n_kv_heads + h) * a.t.n_select;
-  for (int j = threadIdx.x; j < a.t.n_select; j += kFsThreads) out[j] = j <= own ? j : -1;
+  for (int j = tid; j < a.t.n_select; j += threads) out[j] = j <= own ? j : -1;
 }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kFsThreads, 2) fp4_select_kernel(const __grid_constant__ Fp4SelectArgs a, int tile_tokens, int capacity) {
+template <typename T, int D, int NW>
+__global__ void __launch_bounds__(FsShape<NW>::kThreads, NW == 16 ? 1 : 4) fp4_select_kernel(const __grid_constant__ Fp4SelectArgs a, int tile_tokens, int capacity) {
   constexpr int W = D / 64;                        // 16-byte pieces of a lane: features 64 i + 16 c and on
+  constexpr int kThreads = FsShape<NW>::kThreads, kStep = FsShape<NW>::kStep;
   extern __shared__ __align__(16) uint32_t fs_raw[];
-  __shared__ FsSmem sm;
+  __shared__ FsGroup sm[kFsMaxTokens];
   __shared__ __align__(16) uint32_t q_code[kFsMaxTokens * 8][2][D / 4];      // query rows: q+ and q-
   __shared__ float q_scale[kFsMaxTokens * 8];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
@@ -231,7 +282,7 @@ __global__ void __launch_bounds__(kFsThreads, 2) fp4_select_kernel(const __grid_
   const int h = blockIdx.x % H, i0 = (int)(blockIdx.x / H) * tile_tokens, n_tok = min(tile_tokens, a.n_tokens - i0);
   const int part = blockIdx.y, parts = gridDim.y;
   uint32_t* key_of = fs_raw;                       // [tile_tokens][capacity]
-  uint32_t* page_of = fs_raw + tile_tokens * capacity;
+  uint32_t* list_of = fs_raw + tile_tokens * capacity;                // [tile_tokens][K]
 
   // the tokens one sequence after the other
   for (int k0 = 0, k1; k0 < n_tok; k0 = k1) {
@@ -246,11 +297,11 @@ __global__ void __launch_bounds__(kFsThreads, 2) fp4_select_kernel(const __grid_
     }
     if (most < K) {
       if (parts == 1)
-        for (int k = k0; k < k1; ++k) write_all(a, i0 + k, h, token_of(a, i0 + k).own);
+        for (int k = k0; k < k1; ++k) write_all(a, i0 + k, h, token_of(a, i0 + k).own, tid, kThreads);
       else if (tid == 0) FsPart(a.ws).counts[blockIdx.x * parts + part] = 0;
       continue;
     }
-    const int share = ((most + parts) / parts + kFsStep - 1) / kFsStep * kFsStep;
+    const int share = ((most + parts) / parts + kStep - 1) / kStep * kStep;
     const int p0 = min(most + 1, part * share), p1 = min(most + 1, p0 + share);
     const int32_t* table = a.table + (long long)first.slot * g.max_pages;
     // this lane's two pages of the next step, looked up ahead
@@ -266,7 +317,7 @@ __global__ void __launch_bounds__(kFsThreads, 2) fp4_select_kernel(const __grid_
 
     // ---- query rows as codes, a warp per row (a lane: D / 32 features)
     const int rows = (k1 - k0) << a.group_shift, groups = (rows + 7) >> 3;
-    for (int row = warp; row < 8 * groups; row += kFsWarps) {
+    for (int row = warp; row < 8 * groups; row += NW) {
       constexpr int N = D / 32;
       float x[N] = {};
       if (row < rows) {
@@ -292,40 +343,34 @@ __global__ void __launch_bounds__(kFsThreads, 2) fp4_select_kernel(const __grid_
     }
     __syncthreads();
 
+    // ---- the warps that choose for one token
+    int warps = NW;
+    while (warps * (k1 - k0) > NW) warps >>= 1;
+    const int my_k = warp / warps, my_warp = warp - my_k * warps, bar = 1 + my_k;      // (my_k of the run)
+    uint32_t* my_key = key_of + my_k * capacity;
+    FsPages my_page = {list_of + my_k * K, 0, (uint32_t)p0};
+
     // ---- pages [p0, p1), 16 to a warp
-    int n = 0;                                     // keys in the buffer, the same for all tokens
-    for (int base = p0; base < p1; base += kFsStep) {
-      if (n + kFsStep > capacity) {
-        __syncthreads();
-        int left = 0;
-        for (int k = 0; k < k1 - k0; ++k) {
-          uint32_t *key = key_of + k * capacity, *page = page_of + k * capacity;
-          const int m = choose(key, page, n, K, sm);
-          for (int j = tid; j < K; j += kFsThreads) {
-            key[j] = j < m ? sm.key[j] : 0u;
-            page[j] = j < m ? sm.page[j] : 0u;
-          }
-          left = K;
-          __syncthreads();
-        }
-        n = left;
-      }
-      const int at = base + warp * 16 + r;
+    struct Bounds {
       uint4 hi[2][W], lo[2][W];
-      float s_page[2];
+      float scale[2];
+    };
+    const auto fetch = [&](Bounds& b) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const long long line = (long long)ids[t] * H + h;
         const uint4* p = reinterpret_cast<const uint4*>(g.bounds + line * 2 * D) + c;
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-          hi[t][i] = p[4 * i];
-          lo[t][i] = p[D / 16 + 4 * i];
+          b.hi[t][i] = p[4 * i];
+          b.lo[t][i] = p[D / 16 + 4 * i];
         }
-        s_page[t] = g.bound_scales[line];
+        b.scale[t] = g.bound_scales[line];
       }
-      ids[0] = look_up(at + kFsStep);
-      ids[1] = look_up(at + kFsStep + 8);
+    };
+    int n = 0;                                     // keys in the buffer, the same for all tokens
+    const auto score = [&](const Bounds& b, int base) {
+      const int at = base + warp * 16 + r;
 #pragma unroll 1
       for (int grp = 0; grp < groups; ++grp) {
         int acc[4] = {0, 0, 0, 0};
@@ -333,10 +378,10 @@ __global__ void __launch_bounds__(kFsThreads, 2) fp4_select_kernel(const __grid_
         for (int i = 0; i < W; ++i) {
           const uint4 qp = *reinterpret_cast<const uint4*>(&q_code[8 * grp + r][0][16 * i + 4 * c]);
           const uint4 qn = *reinterpret_cast<const uint4*>(&q_code[8 * grp + r][1][16 * i + 4 * c]);
-          mma_s8(acc, hi[0][i].x, hi[1][i].x, hi[0][i].y, hi[1][i].y, qp.x, qp.y);
-          mma_s8(acc, hi[0][i].z, hi[1][i].z, hi[0][i].w, hi[1][i].w, qp.z, qp.w);
-          mma_s8(acc, lo[0][i].x, lo[1][i].x, lo[0][i].y, lo[1][i].y, qn.x, qn.y);
-          mma_s8(acc, lo[0][i].z, lo[1][i].z, lo[0][i].w, lo[1][i].w, qn.z, qn.w);
+          mma_s8(acc, b.hi[0][i].x, b.hi[1][i].x, b.hi[0][i].y, b.hi[1][i].y, qp.x, qp.y);
+          mma_s8(acc, b.hi[0][i].z, b.hi[1][i].z, b.hi[0][i].w, b.hi[1][i].w, qp.z, qp.w);
+          mma_s8(acc, b.lo[0][i].x, b.lo[1][i].x, b.lo[0][i].y, b.lo[1][i].y, qn.x, qn.y);
+          mma_s8(acc, b.lo[0][i].z, b.lo[1][i].z, b.lo[0][i].w, b.lo[1][i].w, qn.z, qn.w);
         }
         const float2 s_col = *reinterpret_cast<const float2*>(&q_scale[8 * grp + 2 * c]);
 #pragma unroll
@@ -344,7 +389,7 @@ __global__ void __launch_bounds__(kFsThreads, 2) fp4_select_kernel(const __grid_
           uint32_t k[2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float x = __fmul_rn(__fmul_rn(e ? s_col.y : s_col.x, s_page[t]), (float)acc[2 * t + e]);
+            const float x = __fmul_rn(__fmul_rn(e ? s_col.y : s_col.x, b.scale[t]), (float)acc[2 * t + e]);
             k[e] = ordered(x != x ? 3.402823466e38f : x);
           }
           if (a.group > 1) k[0] = max(k[0], k[1]);
@@ -359,50 +404,77 @@ __global__ void __launch_bounds__(kFsThreads, 2) fp4_select_kernel(const __grid_
             const int own = a.t.positions[i0 + k0 + tok] >> g.page_shift;
             const bool always = page < a.n_first || page > own - a.n_recent;
             key_of[tok * capacity + to] = page > own ? 0u : always ? kFsAlways : k[e];
-            page_of[tok * capacity + to] = (uint32_t)page;
           }
         }
       }
-      n += min(kFsStep, p1 - base);
+    };
+    Bounds now;
+    if (FsShape<NW>::kAhead && p0 < p1) fetch(now);
+#pragma unroll 1
+    for (int base = p0; base < p1; base += kStep) {
+      if (n + kStep > capacity) {
+        __syncthreads();
+        if (my_k < k1 - k0) cut_down(my_key, my_page, n, K, sm[my_k], my_warp, warps, bar);
+        n = K;
+        my_page.kept = K;
+        my_page.start = (uint32_t)base;
+        __syncthreads();
+      }
+      if (!FsShape<NW>::kAhead) fetch(now);
+      // (a step past the end fetches page 0 of the pool)
+      ids[0] = look_up(base + kStep + warp * 16 + r);
+      ids[1] = look_up(base + kStep + warp * 16 + r + 8);
+      if (FsShape<NW>::kAhead) {
+        Bounds next;
+        fetch(next);
+        score(now, base);
+        now = next;
+      } else {
+        score(now, base);
+      }
+      n += min(kStep, p1 - base);
     }
     __syncthreads();
 
     // ---- the choice
-    for (int k = 0; k < k1 - k0; ++k) {
-      const int own = token_of(a, i0 + k0 + k).own;
+    if (my_k < k1 - k0) {
+      const int token = i0 + k0 + my_k, own = token_of(a, token).own;
       if (parts == 1 && own < K) {
-        write_all(a, i0 + k0 + k, h, own);
-        continue;
-      }
-      const int m = choose(key_of + k * capacity, page_of + k * capacity, n, K, sm);
-      if (parts == 1) {
-        int32_t* out = a.out + ((long long)(i0 + k0 + k) * H + h) * K;
-        for (int j = tid; j < K; j += kFsThreads) out[j] = j < m ? (int32_t)sm.page[j] : -1;
+        write_all(a, token, h, own, my_warp * 32 + lane, 32 * warps);
       } else {
-        const FsPart ws(a.ws);
-        const int slot = blockIdx.x * parts + part;
-        for (int j = tid; j < m; j += kFsThreads) {
-          ws.keys[slot * ECHOKV_FP4_MAX_SELECT + j] = sm.key[j];
-          ws.pages[slot * ECHOKV_FP4_MAX_SELECT + j] = sm.page[j];
+        const FsChoice f = choose(my_key, n, K, sm[my_k], my_warp, warps, bar);
+        if (parts == 1) {
+          int32_t* out = a.out + ((long long)token * H + h) * K;
+          const int m = chosen(f, my_key, n, K, sm[my_k], my_warp, warps, bar, [&](int at, int i) { out[at] = (int32_t)my_page(i); });
+          for (int j = m + my_warp * 32 + lane; j < K; j += 32 * warps) out[j] = -1;
+        } else {
+          const FsPart ws(a.ws);
+          const int slot = blockIdx.x * parts + part;
+          const int m = chosen(f, my_key, n, K, sm[my_k], my_warp, warps, bar, [&](int at, int i) {
+            ws.keys[slot * ECHOKV_FP4_MAX_SELECT + at] = my_key[i];
+            ws.pages[slot * ECHOKV_FP4_MAX_SELECT + at] = my_page(i);
+          });
+          if (tid == 0) ws.counts[slot] = m;
         }
-        if (tid == 0) ws.counts[slot] = m;
       }
-      __syncthreads();                             // (sm and the buffer are used again)
     }
+    __syncthreads();                               // (the buffers are used again)
   }
 }
 
 // Chooses among what the parts of one token and head chose (each of them ascending, and so all of them one after the other).
-__global__ void __launch_bounds__(kFsThreads) fp4_select_merge_kernel(const __grid_constant__ Fp4SelectArgs a, int parts, int capacity) {
+__global__ void __launch_bounds__(kFsMergeWarps * 32) fp4_select_merge_kernel(const __grid_constant__ Fp4SelectArgs a, int parts, int capacity) {
+  constexpr int kThreads = kFsMergeWarps * 32;
   extern __shared__ __align__(16) uint32_t fs_raw[];
-  __shared__ FsSmem sm;
-  const int tid = threadIdx.x, H = a.g.n_kv_heads, K = a.t.n_select, token = blockIdx.x / H, h = blockIdx.x % H;
+  __shared__ FsGroup sm;
+  const int tid = threadIdx.x, warp = tid >> 5, H = a.g.n_kv_heads, K = a.t.n_select, token = blockIdx.x / H, h = blockIdx.x % H;
   uint32_t *key = fs_raw, *page = fs_raw + capacity;
+  const FsPages pages = {page, capacity, 0u};
   const FsPart ws(a.ws);
   const int own = token_of(a, token).own;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (own < K) {
-    write_all(a, token, h, own);
+    write_all(a, token, h, own, tid, kThreads);
     return;
   }
   int n = 0;
@@ -410,33 +482,48 @@ __global__ void __launch_bounds__(kFsThreads) fp4_select_merge_kernel(const __gr
     const int slot = blockIdx.x * parts + p, m = ws.counts[slot];
     if (n + m > capacity) {
       __syncthreads();
-      n = choose(key, page, n, K, sm);
-      for (int j = tid; j < n; j += kFsThreads) {
-        key[j] = sm.key[j];
-        page[j] = sm.page[j];
-      }
-      __syncthreads();
+      cut_down(key, pages, n, K, sm, warp, kFsMergeWarps, 1);
+      n = K;
     }
-    for (int j = tid; j < m; j += kFsThreads) {
+    for (int j = tid; j < m; j += kThreads) {
       key[n + j] = ws.keys[slot * ECHOKV_FP4_MAX_SELECT + j];
       page[n + j] = ws.pages[slot * ECHOKV_FP4_MAX_SELECT + j];
     }
     n += m;
   }
   __syncthreads();
-  n = choose(key, page, n, K, sm);
+  const FsChoice f = choose(key, n, K, sm, warp, kFsMergeWarps, 1);
   int32_t* out = a.out + ((long long)token * H + h) * K;
-  for (int j = tid; j < K; j += kFsThreads) out[j] = j < n ? (int32_t)sm.page[j] : -1;
+  const int m = chosen(f, key, n, K, sm, warp, kFsMergeWarps, 1, [&](int at, int i) { out[at] = (int32_t)page[i]; });
+  for (int j = m + tid; j < K; j += kThreads) out[j] = -1;
+}
+
+int capacity_of(int tokens, int K, int step, long long wanted) {
+  long long c = wanted < kFsEntries / tokens ? wanted : kFsEntries / tokens;
+  const long long least = K + step;                // (1280 at most: 8 tokens have 2048 entries each)
+  return (int)((c > least ? c : least) + 31) / 32 * 32;
+}
+
+template <typename T, int D, int NW>
+cudaError_t launch_main(const Fp4SelectArgs& a, int tile_tokens, int parts, cudaStream_t stream) {
+  constexpr int kStep = FsShape<NW>::kStep;
+  const long long tiles = (a.n_tokens + tile_tokens - 1) / tile_tokens;
+  const int capacity = capacity_of(tile_tokens, a.t.n_select, kStep, (a.g.max_pages + parts - 1) / parts + 2 * kStep);
+  static std::atomic<unsigned long long> done{0};
+  const cudaError_t e = allow_smem(fp4_select_kernel<T, D, NW>, kFsEntries * 4 + kFsMaxTokens * (32 + ECHOKV_FP4_MAX_SELECT) * 4, &done);
+  if (e != cudaSuccess) return e;
+  fp4_select_kernel<T, D, NW><<<dim3((unsigned)(tiles * a.g.n_kv_heads), parts), FsShape<NW>::kThreads, (size_t)tile_tokens * (capacity + a.t.n_select) * 4, stream>>>(
+      a, tile_tokens, capacity);
+  return cudaGetLastError();
 }
 
 template <typename T, int D>
 cudaError_t launch(const Fp4SelectArgs& a, int sm_count, cudaStream_t stream) {
-  const int H = a.g.n_kv_heads, K = a.t.n_select;
-  const long long heads = (long long)a.n_tokens * H;
-  // tokens of a block: as many as leave a block for every SM; with one, its pages may be in parts
+  const int K = a.t.n_select;
+  const long long heads = (long long)a.n_tokens * a.g.n_kv_heads;
+  // tokens of a block: as many as leave blocks enough for every SM; with few tokens the pages of one may be in parts
   int tile_tokens = 1;
-  while (tile_tokens < kFsMaxTokens && heads >= 2ll * tile_tokens * sm_count) tile_tokens *= 2;
-  const long long tiles = (a.n_tokens + tile_tokens - 1) / tile_tokens;
+  while (tile_tokens < kFsMaxTokens && heads >= 4ll * tile_tokens * sm_count) tile_tokens *= 2;
   int parts = 1;
   if (tile_tokens == 1) {
     const long long room = sm_count < kFsMaxParts ? sm_count : kFsMaxParts;
@@ -444,32 +531,22 @@ cudaError_t launch(const Fp4SelectArgs& a, int sm_count, cudaStream_t stream) {
     parts = (int)(room / heads < most ? room / heads : most);
     if (parts < 1) parts = 1;
   }
-  const auto capacity_of = [&](int tokens, long long wanted) {
-    long long c = wanted < kFsEntries / tokens ? wanted : kFsEntries / tokens;
-    const long long least = K + kFsStep;           // (1280 at most: 8 tokens have 2048 entries each)
-    return (int)((c > least ? c : least) + 31) / 32 * 32;
-  };
-  const int capacity = capacity_of(tile_tokens, ((a.g.max_pages + parts - 1) / parts + 2 * kFsStep));
-  const size_t smem = (size_t)tile_tokens * capacity * 8;
+  cudaError_t e = heads * parts <= sm_count ? launch_main<T, D, 16>(a, tile_tokens, parts, stream) : launch_main<T, D, 8>(a, tile_tokens, parts, stream);
+  if (e != cudaSuccess || parts == 1) return e;
+  const int capacity = capacity_of(1, K, K, (long long)parts * K);
   static std::atomic<unsigned long long> done{0};
-  cudaError_t e = allow_smem(fp4_select_kernel<T, D>, kFsEntries * 8 + 8 * 32 * 8, &done);
-  if (e != cudaSuccess) return e;
-  fp4_select_kernel<T, D><<<dim3((unsigned)(tiles * H), parts), kFsThreads, smem, stream>>>(a, tile_tokens, capacity);
-  if ((e = cudaGetLastError()) != cudaSuccess || parts == 1) return e;
-  const int merge_capacity = capacity_of(1, (long long)parts * K > 2 * K ? (long long)parts * K : 2 * K);
-  static std::atomic<unsigned long long> done_merge{0};
-  if ((e = allow_smem(fp4_select_merge_kernel, kFsEntries * 8 + 8 * 32 * 8, &done_merge)) != cudaSuccess) return e;
+  if ((e = allow_smem(fp4_select_merge_kernel, kFsEntries * 8 + 32 * 8, &done)) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)heads);
-  cfg.blockDim = dim3(kFsThreads);
-  cfg.dynamicSmemBytes = (size_t)merge_capacity * 8;
+  cfg.blockDim = dim3(kFsMergeWarps * 32);
+  cfg.dynamicSmemBytes = (size_t)capacity * 8;
   cfg.stream = stream;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, fp4_select_merge_kernel, a, parts, merge_capacity);
+  return cudaLaunchKernelEx(&cfg, fp4_select_merge_kernel, a, parts, capacity);
 }
 
 }  // namespace
