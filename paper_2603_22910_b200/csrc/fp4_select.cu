@@ -4,9 +4,10 @@
 //
 // The sum is one product of whole numbers, [q+ | q-] . [top | low], of 2 d terms: mma.sync m16n8k32 on 8-bit integers with the
 // pages on the M rows and the query rows on N, exact in 32 bits, so that equal pages are equal and the choice does not depend on
-// the order of anything.  A block takes one KV head of one token, or of up to 8 where there are tokens enough for all SMs (a page's
-// bounds are then read once for those of one sequence).  A warp takes 16 pages at a time and writes their scores, as whole numbers in the order
-// of the floats, in the pages' order to shared memory.  The n_select largest are then found by counting eight bits at a time from the
+// the order of anything.  A block takes one KV head of one token, or of up to 8 neighbours of one sequence where there are tokens enough
+// for all SMs (a page's bounds are then read once for them).  A warp takes 16 pages at a time, whose bounds its lanes have asked for
+// four steps before (two, where the keys of many tokens leave no room), each the pieces that it will use itself, and writes their scores, as whole numbers in the order of the
+// floats, in the pages' order to shared memory.  The n_select largest are then found by counting eight bits at a time from the
 // top of what the keys differ in, and copied in order: what comes out is ascending, and of equal scores the first pages stay.
 // When the buffer is full it is cut down to n_select in the same way, so that a sequence may have any number of pages.  Few tokens over
 // long caches are split along the pages; a second kernel then chooses among what the parts chose.
@@ -17,14 +18,9 @@ namespace echokv {
 
 namespace {
 
-// Few (token, head) pairs: blocks of 16 warps that fetch a step ahead; many: of 8, and four blocks to an SM.
-template <int NW>
-struct FsShape {
-  static constexpr int kThreads = NW * 32;
-  static constexpr int kStep = NW * 16;            // pages that a block takes at once
-  static constexpr bool kAhead = NW == 16;
-};
-constexpr int kFsMergeWarps = 8;
+constexpr int kFsWarps = 8;
+constexpr int kFsThreads = kFsWarps * 32;
+constexpr int kFsStep = kFsWarps * 16;             // pages that a block takes at once
 constexpr int kFsEntries = 16384;                  // keys of a block, of all its tokens
 constexpr int kFsMaxTokens = 8;                    // tokens of a block: each has room for 2048 keys, ECHOKV_FP4_MAX_SELECT and a step
 constexpr int kFsMaxParts = 320;                   // (token, head, part of the pages) with a place in the workspace
@@ -45,7 +41,7 @@ struct FsPart {
 // of the warps that choose for one token
 struct FsGroup {
   uint32_t hist[256];
-  uint32_t red[16][4];
+  uint32_t red[kFsWarps][4], side[kFsWarps][2];
   uint32_t bin, want, whole;
 };
 
@@ -180,20 +176,19 @@ __device__ __forceinline__ int chosen(const FsChoice& f, const uint32_t* key, in
   }
   above = __reduce_add_sync(0xffffffffu, above);
   equal = __reduce_add_sync(0xffffffffu, equal);
-  group_sync(bar, warps);                          // (sm.red has been read)
   if (lane == 0) {
-    sm.red[warp][0] = above;
-    sm.red[warp][1] = equal;
+    sm.side[warp][0] = above;
+    sm.side[warp][1] = equal;
   }
   group_sync(bar, warps);
   uint32_t before_above = 0, before_equal = 0, all_above = 0, all_equal = 0;
   for (int w = 0; w < warps; ++w) {
     if (w < warp) {
-      before_above += sm.red[w][0];
-      before_equal += sm.red[w][1];
+      before_above += sm.side[w][0];
+      before_equal += sm.side[w][1];
     }
-    all_above += sm.red[w][0];
-    all_equal += sm.red[w][1];
+    all_above += sm.side[w][0];
+    all_equal += sm.side[w][1];
   }
   const uint32_t lower = (1u << lane) - 1;
 #pragma unroll 1
@@ -268,60 +263,102 @@ __device__ __forceinline__ void write_all(const Fp4SelectArgs& a, int token, int
   for (int j = tid; j < a.t.n_select; j += threads) out[j] = j <= own ? j : -1;
 }
 
-template <typename T, int D, int NW>
-__global__ void __launch_bounds__(FsShape<NW>::kThreads, NW == 16 ? 1 : 4) fp4_select_kernel(const __grid_constant__ Fp4SelectArgs a, int tile_tokens, int capacity) {
+// bytes of a step's bounds for one warp: 16 pages, a lane's pieces [piece][lane] and scales [2][lane]
+__host__ __device__ constexpr int fs_stage_bytes(int d) { return 16 * 2 * d + 2 * 32 * 4; }
+
+template <typename T, int D, int kFsDepth>
+__global__ void __launch_bounds__(kFsThreads, 2) fp4_select_kernel(const __grid_constant__ Fp4SelectArgs a, int tile_tokens, int capacity) {
   constexpr int W = D / 64;                        // 16-byte pieces of a lane: features 64 i + 16 c and on
-  constexpr int kThreads = FsShape<NW>::kThreads, kStep = FsShape<NW>::kStep;
-  extern __shared__ __align__(16) uint32_t fs_raw[];
-  __shared__ FsGroup sm[kFsMaxTokens];
-  __shared__ __align__(16) uint32_t q_code[kFsMaxTokens * 8][2][D / 4];      // query rows: q+ and q-
-  __shared__ float q_scale[kFsMaxTokens * 8];
+  extern __shared__ __align__(16) unsigned char fs_raw[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
   const Fp4Geom& g = a.g;
   const int H = g.n_kv_heads, K = a.t.n_select;
-  const int h = blockIdx.x % H, i0 = (int)(blockIdx.x / H) * tile_tokens, n_tok = min(tile_tokens, a.n_tokens - i0);
+  const int h = blockIdx.x % H, i0 = (int)(blockIdx.x / H);
   const int part = blockIdx.y, parts = gridDim.y;
-  uint32_t* key_of = fs_raw;                       // [tile_tokens][capacity]
-  uint32_t* list_of = fs_raw + tile_tokens * capacity;                // [tile_tokens][K]
+  const uint32_t ring = smem_u32(fs_raw) + warp * kFsDepth * fs_stage_bytes(D);
+  // [warps][depth] stages | [rows][2] query codes, q+ and q- | [rows] their scales | [tokens] groups | [tokens][capacity] keys | [tokens][K] lists
+  const int rows8 = (tile_tokens * a.group + 7) & ~7;
+  uint32_t (*q_code)[2][D / 4] = reinterpret_cast<uint32_t (*)[2][D / 4]>(fs_raw + kFsWarps * kFsDepth * fs_stage_bytes(D));
+  float* q_scale = reinterpret_cast<float*>(q_code + rows8);
+  FsGroup* sm = reinterpret_cast<FsGroup*>(q_scale + rows8);
+  uint32_t* key_of = reinterpret_cast<uint32_t*>(sm + tile_tokens);
+  uint32_t* list_of = key_of + tile_tokens * capacity;
 
-  // the tokens one sequence after the other
-  for (int k0 = 0, k1; k0 < n_tok; k0 = k1) {
-    const FsToken first = token_of(a, i0 + k0);
-    k1 = k0 + 1;
-    while (k1 < n_tok && first.error == 0 && a.t.seqs[i0 + k1] == a.t.seqs[i0 + k0]) ++k1;
-    int most = -1;                                 // the last page that one of them sees
-    for (int k = k0; k < k1; ++k) {
-      const FsToken t = token_of(a, i0 + k);
-      if (t.error != 0 && t.error != kFsNotAsked && tid == 0 && part == 0) report_opt(a.status, t.error);
-      most = max(most, t.own);
+  // the block's tokens: i0 and those behind it at the following positions of its sequence, up to the next multiple of
+  // tile_tokens; a token that belongs to one before it has nothing to do
+  const FsToken first = token_of(a, i0);
+  const int pos0 = a.t.positions[i0];
+  int n_tok = 1;
+  {
+    const int seq = a.t.seqs[i0];
+    const auto follows = [&](int i) { return a.t.seqs[i] == seq && a.t.positions[i] - pos0 == i - i0; };
+    if (first.error == 0) {
+      if (i0 > 0 && pos0 % tile_tokens != 0 && follows(i0 - 1)) return;
+      while (n_tok < tile_tokens && i0 + n_tok < a.n_tokens && (pos0 + n_tok) % tile_tokens != 0 && token_of(a, i0 + n_tok).error == 0 && follows(i0 + n_tok))
+        ++n_tok;
     }
-    if (most < K) {
-      if (parts == 1)
-        for (int k = k0; k < k1; ++k) write_all(a, i0 + k, h, token_of(a, i0 + k).own, tid, kThreads);
-      else if (tid == 0) FsPart(a.ws).counts[blockIdx.x * parts + part] = 0;
-      continue;
-    }
-    const int share = ((most + parts) / parts + kStep - 1) / kStep * kStep;
-    const int p0 = min(most + 1, part * share), p1 = min(most + 1, p0 + share);
-    const int32_t* table = a.table + (long long)first.slot * g.max_pages;
-    // this lane's two pages of the next step, looked up ahead
-    const auto look_up = [&](int page) {
-      int id = page < p1 ? table[page] : 0;
-      if (id < 0 || id >= g.n_pages) {
+  }
+  if (first.error != 0 && first.error != kFsNotAsked && tid == 0 && part == 0 && h == 0) report_opt(a.status, first.error);
+  const int most = first.error == 0 ? (pos0 + n_tok - 1) >> g.page_shift : -1;      // the last page that one of them sees
+  if (most < K) {
+    if (parts == 1)
+      for (int k = 0; k < n_tok; ++k) write_all(a, i0 + k, h, most < 0 ? -1 : (pos0 + k) >> g.page_shift, tid, kFsThreads);
+    else if (tid == 0) FsPart(a.ws).counts[blockIdx.x * parts + part] = 0;
+    return;
+  }
+  const int share = ((most + parts) / parts + kFsStep - 1) / kFsStep * kFsStep;
+  const int p0 = min(most + 1, part * share), p1 = min(most + 1, p0 + share), n_steps = (p1 - p0 + kFsStep - 1) / kFsStep;
+  const int32_t* table = a.table + (long long)first.slot * g.max_pages;
+  // this lane's pages of a step (rows r and r + 8 of the warp's 16)
+  struct Ids {
+    int id[2];
+  };
+  const auto look_up = [&](int step) {
+    Ids x;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int page = p0 + step * kFsStep + warp * 16 + r + 8 * t;
+      x.id[t] = page < p1 ? table[page] : 0;
+      if (x.id[t] < 0 || x.id[t] >= g.n_pages) {
         report_opt(a.status, ECHOKV_EBADPAGE);
-        id = 0;
+        x.id[t] = 0;
       }
-      return id;
-    };
-    int ids[2] = {look_up(p0 + warp * 16 + r), look_up(p0 + warp * 16 + r + 8)};
+    }
+    return x;
+  };
+  const auto ask = [&](int step, const Ids& x) {
+    if (step < n_steps) {
+      const uint32_t dst = ring + step % kFsDepth * fs_stage_bytes(D);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const long long line = (long long)x.id[t] * H + h;
+        const int8_t* p = g.bounds + line * 2 * D + 16 * c;
+#pragma unroll
+        for (int i = 0; i < 2 * W; ++i)            // (the largest values' pieces, then the smallest ones')
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + ((t * 2 * W + i) * 32 + lane) * 16), "l"(p + 64 * i) : "memory");
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + 16 * 2 * D + (t * 32 + lane) * 4), "l"(g.bound_scales + line) : "memory");
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  Ids ids;
+  {
+    Ids x[kFsDepth];
+#pragma unroll
+    for (int i = 0; i < kFsDepth; ++i) x[i] = look_up(i);
+#pragma unroll
+    for (int i = 0; i < kFsDepth; ++i) ask(i, x[i]);
+    ids = look_up(kFsDepth);
+  }
 
+  {
     // ---- query rows as codes, a warp per row (a lane: D / 32 features)
-    const int rows = (k1 - k0) << a.group_shift, groups = (rows + 7) >> 3;
-    for (int row = warp; row < 8 * groups; row += NW) {
+    const int rows = n_tok << a.group_shift, groups = (rows + 7) >> 3;
+    for (int row = warp; row < 8 * groups; row += kFsWarps) {
       constexpr int N = D / 32;
       float x[N] = {};
       if (row < rows) {
-        const T* p = static_cast<const T*>(a.q) + (long long)(i0 + k0 + (row >> a.group_shift)) * a.q_stride +
+        const T* p = static_cast<const T*>(a.q) + (long long)(i0 + (row >> a.group_shift)) * a.q_stride +
                      (long long)(h * a.group + (row & (a.group - 1))) * D + N * lane;
 #pragma unroll
         for (int e = 0; e < N; ++e) x[e] = to_f32(p[e]);
@@ -344,101 +381,81 @@ __global__ void __launch_bounds__(FsShape<NW>::kThreads, NW == 16 ? 1 : 4) fp4_s
     __syncthreads();
 
     // ---- the warps that choose for one token
-    int warps = NW;
-    while (warps * (k1 - k0) > NW) warps >>= 1;
-    const int my_k = warp / warps, my_warp = warp - my_k * warps, bar = 1 + my_k;      // (my_k of the run)
+    int warps = kFsWarps;
+    while (warps * n_tok > kFsWarps) warps >>= 1;
+    const int my_k = warp / warps, my_warp = warp - my_k * warps, bar = 1 + my_k;
     uint32_t* my_key = key_of + my_k * capacity;
     FsPages my_page = {list_of + my_k * K, 0, (uint32_t)p0};
 
     // ---- pages [p0, p1), 16 to a warp
-    struct Bounds {
-      uint4 hi[2][W], lo[2][W];
-      float scale[2];
-    };
-    const auto fetch = [&](Bounds& b) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const long long line = (long long)ids[t] * H + h;
-        const uint4* p = reinterpret_cast<const uint4*>(g.bounds + line * 2 * D) + c;
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-          b.hi[t][i] = p[4 * i];
-          b.lo[t][i] = p[D / 16 + 4 * i];
-        }
-        b.scale[t] = g.bound_scales[line];
-      }
-    };
     int n = 0;                                     // keys in the buffer, the same for all tokens
-    const auto score = [&](const Bounds& b, int base) {
-      const int at = base + warp * 16 + r;
 #pragma unroll 1
-      for (int grp = 0; grp < groups; ++grp) {
-        int acc[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-          const uint4 qp = *reinterpret_cast<const uint4*>(&q_code[8 * grp + r][0][16 * i + 4 * c]);
-          const uint4 qn = *reinterpret_cast<const uint4*>(&q_code[8 * grp + r][1][16 * i + 4 * c]);
-          mma_s8(acc, b.hi[0][i].x, b.hi[1][i].x, b.hi[0][i].y, b.hi[1][i].y, qp.x, qp.y);
-          mma_s8(acc, b.hi[0][i].z, b.hi[1][i].z, b.hi[0][i].w, b.hi[1][i].w, qp.z, qp.w);
-          mma_s8(acc, b.lo[0][i].x, b.lo[1][i].x, b.lo[0][i].y, b.lo[1][i].y, qn.x, qn.y);
-          mma_s8(acc, b.lo[0][i].z, b.lo[1][i].z, b.lo[0][i].w, b.lo[1][i].w, qn.z, qn.w);
-        }
-        const float2 s_col = *reinterpret_cast<const float2*>(&q_scale[8 * grp + 2 * c]);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          uint32_t k[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float x = __fmul_rn(__fmul_rn(e ? s_col.y : s_col.x, b.scale[t]), (float)acc[2 * t + e]);
-            k[e] = ordered(x != x ? 3.402823466e38f : x);
-          }
-          if (a.group > 1) k[0] = max(k[0], k[1]);
-          if (a.group > 2) k[0] = max(k[0], __shfl_xor_sync(0xffffffffu, k[0], 1));
-          if (a.group > 4) k[0] = max(k[0], __shfl_xor_sync(0xffffffffu, k[0], 2));
-          const int page = at + 8 * t, to = n + page - base;
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            // (the column that writes for its token: the first of the token's)
-            const int row = 8 * grp + 2 * c + e, tok = row >> a.group_shift;
-            if (row >= rows || (row & (a.group - 1)) != 0 || page >= p1) continue;
-            const int own = a.t.positions[i0 + k0 + tok] >> g.page_shift;
-            const bool always = page < a.n_first || page > own - a.n_recent;
-            key_of[tok * capacity + to] = page > own ? 0u : always ? kFsAlways : k[e];
-          }
-        }
-      }
-    };
-    Bounds now;
-    if (FsShape<NW>::kAhead && p0 < p1) fetch(now);
-#pragma unroll 1
-    for (int base = p0; base < p1; base += kStep) {
-      if (n + kStep > capacity) {
+    for (int step = 0; step < n_steps; ++step) {
+      const int base = p0 + step * kFsStep, at = base + warp * 16 + r;
+      if (n + kFsStep > capacity) {
         __syncthreads();
-        if (my_k < k1 - k0) cut_down(my_key, my_page, n, K, sm[my_k], my_warp, warps, bar);
+        if (my_k < n_tok) cut_down(my_key, my_page, n, K, sm[my_k], my_warp, warps, bar);
         n = K;
         my_page.kept = K;
         my_page.start = (uint32_t)base;
         __syncthreads();
       }
-      if (!FsShape<NW>::kAhead) fetch(now);
-      // (a step past the end fetches page 0 of the pool)
-      ids[0] = look_up(base + kStep + warp * 16 + r);
-      ids[1] = look_up(base + kStep + warp * 16 + r + 8);
-      if (FsShape<NW>::kAhead) {
-        Bounds next;
-        fetch(next);
-        score(now, base);
-        now = next;
-      } else {
-        score(now, base);
+      const Ids coming = ids;
+      ids = look_up(step + kFsDepth + 1);
+      asm volatile("cp.async.wait_group %0;" ::"n"(kFsDepth - 1) : "memory");
+      const uint32_t src = ring + step % kFsDepth * fs_stage_bytes(D);
+      uint4 b[2][2 * W];                           // [page r, r + 8][the largest values' pieces, the smallest ones']
+      float s_page[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int i = 0; i < 2 * W; ++i)
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(b[t][i].x), "=r"(b[t][i].y), "=r"(b[t][i].z), "=r"(b[t][i].w)
+                       : "r"(src + ((t * 2 * W + i) * 32 + lane) * 16) : "memory");
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(s_page[t]) : "r"(src + 16 * 2 * D + (t * 32 + lane) * 4) : "memory");
       }
-      n += min(kStep, p1 - base);
+#pragma unroll 1
+      for (int grp = 0; grp < groups; ++grp) {
+        int acc[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 2 * W; ++i) {
+          const uint4 q = *reinterpret_cast<const uint4*>(&q_code[8 * grp + r][i / W][16 * (i % W) + 4 * c]);
+          mma_s8(acc, b[0][i].x, b[1][i].x, b[0][i].y, b[1][i].y, q.x, q.y);
+          mma_s8(acc, b[0][i].z, b[1][i].z, b[0][i].w, b[1][i].w, q.z, q.w);
+        }
+        const float2 s_col = *reinterpret_cast<const float2*>(&q_scale[8 * grp + 2 * c]);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          // (a page whose scale is NaN: the largest finite score; then the largest over the columns of a token, in all of its lanes)
+          float x[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            x[e] = __fmul_rn(__fmul_rn(e ? s_col.y : s_col.x, s_page[t]), (float)acc[2 * t + e]);
+            if (x[e] != x[e]) x[e] = 3.402823466e38f;
+          }
+          if (a.group > 1) x[0] = fmaxf(x[0], x[1]);
+          if (a.group > 2) x[0] = fmaxf(x[0], __shfl_xor_sync(0xffffffffu, x[0], 1));
+          if (a.group > 4) x[0] = fmaxf(x[0], __shfl_xor_sync(0xffffffffu, x[0], 2));
+          const int page = at + 8 * t;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            // (the column that writes for its token: the first of the token's)
+            const int row = 8 * grp + 2 * c + e, tok = row >> a.group_shift;
+            if (row >= rows || (row & (a.group - 1)) != 0 || page >= p1) continue;
+            const int own = (pos0 + tok) >> g.page_shift;
+            const bool always = page < a.n_first || page > own - a.n_recent;
+            key_of[tok * capacity + n + page - base] = page > own ? 0u : always ? kFsAlways : ordered(x[e]);
+          }
+        }
+      }
+      ask(step + kFsDepth, coming);                // (over what this lane has read)
+      n += min(kFsStep, p1 - base);
     }
     __syncthreads();
 
     // ---- the choice
-    if (my_k < k1 - k0) {
-      const int token = i0 + k0 + my_k, own = token_of(a, token).own;
+    if (my_k < n_tok) {
+      const int token = i0 + my_k, own = (pos0 + my_k) >> g.page_shift;
       if (parts == 1 && own < K) {
         write_all(a, token, h, own, my_warp * 32 + lane, 32 * warps);
       } else {
@@ -458,17 +475,16 @@ __global__ void __launch_bounds__(FsShape<NW>::kThreads, NW == 16 ? 1 : 4) fp4_s
         }
       }
     }
-    __syncthreads();                               // (the buffers are used again)
   }
 }
 
 // Chooses among what the parts of one token and head chose (each of them ascending, and so all of them one after the other).
-__global__ void __launch_bounds__(kFsMergeWarps * 32) fp4_select_merge_kernel(const __grid_constant__ Fp4SelectArgs a, int parts, int capacity) {
-  constexpr int kThreads = kFsMergeWarps * 32;
-  extern __shared__ __align__(16) uint32_t fs_raw[];
+__global__ void __launch_bounds__(kFsWarps * 32) fp4_select_merge_kernel(const __grid_constant__ Fp4SelectArgs a, int parts, int capacity) {
+  constexpr int kThreads = kFsWarps * 32;
+  extern __shared__ __align__(16) unsigned char fs_raw[];
   __shared__ FsGroup sm;
   const int tid = threadIdx.x, warp = tid >> 5, H = a.g.n_kv_heads, K = a.t.n_select, token = blockIdx.x / H, h = blockIdx.x % H;
-  uint32_t *key = fs_raw, *page = fs_raw + capacity;
+  uint32_t *key = reinterpret_cast<uint32_t*>(fs_raw), *page = key + capacity;
   const FsPages pages = {page, capacity, 0u};
   const FsPart ws(a.ws);
   const int own = token_of(a, token).own;
@@ -482,7 +498,7 @@ __global__ void __launch_bounds__(kFsMergeWarps * 32) fp4_select_merge_kernel(co
     const int slot = blockIdx.x * parts + p, m = ws.counts[slot];
     if (n + m > capacity) {
       __syncthreads();
-      cut_down(key, pages, n, K, sm, warp, kFsMergeWarps, 1);
+      cut_down(key, pages, n, K, sm, warp, kFsWarps, 1);
       n = K;
     }
     for (int j = tid; j < m; j += kThreads) {
@@ -492,38 +508,25 @@ __global__ void __launch_bounds__(kFsMergeWarps * 32) fp4_select_merge_kernel(co
     n += m;
   }
   __syncthreads();
-  const FsChoice f = choose(key, n, K, sm, warp, kFsMergeWarps, 1);
+  const FsChoice f = choose(key, n, K, sm, warp, kFsWarps, 1);
   int32_t* out = a.out + ((long long)token * H + h) * K;
-  const int m = chosen(f, key, n, K, sm, warp, kFsMergeWarps, 1, [&](int at, int i) { out[at] = (int32_t)page[i]; });
+  const int m = chosen(f, key, n, K, sm, warp, kFsWarps, 1, [&](int at, int i) { out[at] = (int32_t)page[i]; });
   for (int j = m + tid; j < K; j += kThreads) out[j] = -1;
 }
 
 int capacity_of(int tokens, int K, int step, long long wanted) {
   long long c = wanted < kFsEntries / tokens ? wanted : kFsEntries / tokens;
-  const long long least = K + step;                // (1280 at most: 8 tokens have 2048 entries each)
+  const long long least = K + step;                // (1152 at most: 8 tokens have 2048 entries each)
   return (int)((c > least ? c : least) + 31) / 32 * 32;
-}
-
-template <typename T, int D, int NW>
-cudaError_t launch_main(const Fp4SelectArgs& a, int tile_tokens, int parts, cudaStream_t stream) {
-  constexpr int kStep = FsShape<NW>::kStep;
-  const long long tiles = (a.n_tokens + tile_tokens - 1) / tile_tokens;
-  const int capacity = capacity_of(tile_tokens, a.t.n_select, kStep, (a.g.max_pages + parts - 1) / parts + 2 * kStep);
-  static std::atomic<unsigned long long> done{0};
-  const cudaError_t e = allow_smem(fp4_select_kernel<T, D, NW>, kFsEntries * 4 + kFsMaxTokens * (32 + ECHOKV_FP4_MAX_SELECT) * 4, &done);
-  if (e != cudaSuccess) return e;
-  fp4_select_kernel<T, D, NW><<<dim3((unsigned)(tiles * a.g.n_kv_heads), parts), FsShape<NW>::kThreads, (size_t)tile_tokens * (capacity + a.t.n_select) * 4, stream>>>(
-      a, tile_tokens, capacity);
-  return cudaGetLastError();
 }
 
 template <typename T, int D>
 cudaError_t launch(const Fp4SelectArgs& a, int sm_count, cudaStream_t stream) {
   const int K = a.t.n_select;
   const long long heads = (long long)a.n_tokens * a.g.n_kv_heads;
-  // tokens of a block: as many as leave blocks enough for every SM; with few tokens the pages of one may be in parts
+  // tokens of a block: as many as leave a block for every SM; with few tokens the pages of one may be in parts
   int tile_tokens = 1;
-  while (tile_tokens < kFsMaxTokens && heads >= 4ll * tile_tokens * sm_count) tile_tokens *= 2;
+  while (tile_tokens < kFsMaxTokens && heads >= 2ll * tile_tokens * sm_count) tile_tokens *= 2;
   int parts = 1;
   if (tile_tokens == 1) {
     const long long room = sm_count < kFsMaxParts ? sm_count : kFsMaxParts;
@@ -531,22 +534,40 @@ cudaError_t launch(const Fp4SelectArgs& a, int sm_count, cudaStream_t stream) {
     parts = (int)(room / heads < most ? room / heads : most);
     if (parts < 1) parts = 1;
   }
-  cudaError_t e = heads * parts <= sm_count ? launch_main<T, D, 16>(a, tile_tokens, parts, stream) : launch_main<T, D, 8>(a, tile_tokens, parts, stream);
-  if (e != cudaSuccess || parts == 1) return e;
-  const int capacity = capacity_of(1, K, K, (long long)parts * K);
-  static std::atomic<unsigned long long> done{0};
-  if ((e = allow_smem(fp4_select_merge_kernel, kFsEntries * 8 + 32 * 8, &done)) != cudaSuccess) return e;
+  const int capacity = capacity_of(tile_tokens, K, kFsStep, (a.g.max_pages + parts - 1) / parts + 2 * kFsStep);
+  const auto smem_of = [&](int depth) {
+    const int rows = (tile_tokens * a.group + 7) & ~7;
+    return (size_t)kFsWarps * depth * fs_stage_bytes(D) + (size_t)rows * (2 * D + 4) + tile_tokens * (sizeof(FsGroup) + 4ull * (capacity + K));
+  };
+  constexpr size_t kRoom = 227 * 1024;
+  static_assert(kFsWarps * 2 * fs_stage_bytes(128) + kFsMaxTokens * 8 * 260 + kFsMaxTokens * sizeof(FsGroup) + kFsEntries * 4 +
+                kFsMaxTokens * (32 + ECHOKV_FP4_MAX_SELECT) * 4 <= kRoom, "shared memory of one CTA, however many tokens and pages");
+  const dim3 grid((unsigned)heads, parts);
+  cudaError_t e;
+  if (smem_of(4) <= kRoom) {
+    static std::atomic<unsigned long long> done{0};
+    if ((e = allow_smem(fp4_select_kernel<T, D, 4>, kRoom, &done)) != cudaSuccess) return e;
+    fp4_select_kernel<T, D, 4><<<grid, kFsThreads, smem_of(4), stream>>>(a, tile_tokens, capacity);
+  } else {
+    static std::atomic<unsigned long long> done{0};
+    if ((e = allow_smem(fp4_select_kernel<T, D, 2>, kRoom, &done)) != cudaSuccess) return e;
+    fp4_select_kernel<T, D, 2><<<grid, kFsThreads, smem_of(2), stream>>>(a, tile_tokens, capacity);
+  }
+  if ((e = cudaGetLastError()) != cudaSuccess || parts == 1) return e;
+  const int merge_capacity = capacity_of(1, K, K, (long long)parts * K);
+  static std::atomic<unsigned long long> done_merge{0};
+  if ((e = allow_smem(fp4_select_merge_kernel, kFsEntries * 8 + 32 * 8, &done_merge)) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)heads);
-  cfg.blockDim = dim3(kFsMergeWarps * 32);
-  cfg.dynamicSmemBytes = (size_t)capacity * 8;
+  cfg.blockDim = dim3(kFsThreads);
+  cfg.dynamicSmemBytes = (size_t)merge_capacity * 8;
   cfg.stream = stream;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, fp4_select_merge_kernel, a, parts, capacity);
+  return cudaLaunchKernelEx(&cfg, fp4_select_merge_kernel, a, parts, merge_capacity);
 }
 
 }  // namespace
