@@ -27,14 +27,16 @@ namespace echokv {
 
 namespace {
 
-constexpr int kFqWarps = 12;
-constexpr int kFqThreads = kFqWarps * 32;
+// (heads of 128: 12 warps 119.5 us for 16 x 32768 keys, 14 134, 16 121; of 64, 16 x 8192 keys of 32 heads: 12 89, 16 79)
+template <int D>
+struct FqShape {
+  static constexpr int kWarps = D == 128 ? 12 : 16, kThreads = kWarps * 32;
+};
 constexpr int kFqRows = 8;                        // query rows per tile
 constexpr int kFqStages = 3;                      // of two blocks each
 constexpr int kFqMergeThreads = kFqRows * 32;
 constexpr int kFqMaxCtas = 512;
 constexpr int kFqItemCost = 6;                    // what an item costs beside its blocks (queries, first copies, result), in blocks
-constexpr int kFqMinShare = 2 * kFqWarps;         // units per CTA at least
 constexpr float kFqBelow = 5.f;                   // the reference stands 2^5 below the largest score it was taken from,
 constexpr float kFqGrow = 8.f + kFqBelow;         // and moves when a score is 2^13 above it (probabilities up to there fit fp16)
 constexpr int kFqNowhere = 0x40000000;            // the first token of a block that nobody sees
@@ -45,17 +47,18 @@ template <int D>
 struct FqSmem {
   // a warp's segment that goes on from the warp before it, and (over the warp's ring, once that is at rest) the one
   // that goes on in the next warp
-  float o_first[kFqWarps][kFqRows][D];
-  QaSeg seg[2 * kFqWarps];
-  float m[2 * kFqWarps][kFqRows], l[2 * kFqWarps][kFqRows];
-  unsigned long long pre[kFqThreads + 1];
-  unsigned long long warp_sums[kFqWarps];
-  unsigned long long full[kFqWarps][kFqStages];
-  int2 tok[kFqWarps][kFqStages];                  // with lists: first tokens of a stage's blocks
-  int4 info[kFqThreads];                          // slot, length, first token, tokens (0: nothing to do) of a small batch
+  static constexpr int kWarps = FqShape<D>::kWarps;
+  float o_first[kWarps][kFqRows][D];
+  QaSeg seg[2 * kWarps];
+  float m[2 * kWarps][kFqRows], l[2 * kWarps][kFqRows];
+  unsigned long long pre[FqShape<D>::kThreads + 1];
+  unsigned long long warp_sums[kWarps];
+  unsigned long long full[kWarps][kFqStages];
+  int2 tok[kWarps][kFqStages];                  // with lists: first tokens of a stage's blocks
+  int4 info[FqShape<D>::kThreads];                          // slot, length, first token, tokens (0: nothing to do) of a small batch
 };
 template <int D>
-__host__ __device__ constexpr size_t fq_ring_bytes() { return (size_t)kFqWarps * kFqStages * fq_stage_bytes(D); }
+__host__ __device__ constexpr size_t fq_ring_bytes() { return (size_t)FqShape<D>::kWarps * kFqStages * fq_stage_bytes(D); }
 
 // workspace: [ctas] QaDesc | [ctas][2][8] (m, l) | [ctas][2][8][D] o
 template <int D>
@@ -114,7 +117,8 @@ __device__ __forceinline__ unsigned long long units_of(const Fp4AttnArgs& a, con
 }
 
 template <typename T, int D, bool LIST>
-__global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_constant__ Fp4AttnArgs a) {
+__global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const __grid_constant__ Fp4AttnArgs a) {
+  constexpr int kFqWarps = FqShape<D>::kWarps, kFqThreads = FqShape<D>::kThreads, kFqMinShare = 2 * kFqWarps;      // (units of a CTA at least)
   constexpr int KC = D / 64;                      // groups of a key row per lane
   constexpr int KS = D / 16;                      // k-steps of q . k
   constexpr int NT = D / 8;                       // features of the output per lane (NT r .. NT r + NT - 1)
@@ -248,10 +252,12 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
     Place cur = look_up(0);
     // ---- the query rows: this lane loads a quarter of row r as operand; its scores are of rows 2 c and 2 c + 1
     const int n_rows = n_new * a.group;
+    // up to four rows stand in the even columns, so that a lane's second column is nobody's and costs nothing
+    const bool spread = n_rows - tile * kFqRows <= 4;
     uint32_t qh[KS][2], ql[kF32 ? KS : 1][2];
     float c_row[2];
-    const int qrow_r = tile * kFqRows + r;
-    const bool ok = qrow_r < n_rows;
+    const int qrow_r = tile * kFqRows + (spread ? r >> 1 : r);
+    const bool ok = qrow_r < n_rows && !(spread && (r & 1));
     const T* qp = static_cast<const T*>(a.q) + (long long)(first_token + (ok ? qrow_r >> a.group_shift : 0)) * a.q_stride +
                   (long long)(h * a.group + (qrow_r & (a.group - 1))) * D;
     Quad<T> qv[KS];
@@ -312,11 +318,12 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
         }
     }
     const int prefix = !LIST && a.prefix ? a.prefix[b] : 0;
-    int pos[2];
+    int pos[2], row_of[2];                        // (row_of: 8 where the column is nobody's)
     float slope2[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const int qrow = tile * kFqRows + 2 * c + e;
+      row_of[e] = spread ? (e == 0 ? c : kFqRows) : 2 * c + e;
+      const int qrow = tile * kFqRows + (row_of[e] & (kFqRows - 1));
       pos[e] = len - n_new + (qrow < n_rows ? qrow >> a.group_shift : 0);
       slope2[e] = a.slopes ? a.slopes[h * a.group + (qrow & (a.group - 1))] * kLog2e : 0.f;
     }
@@ -339,8 +346,9 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
     };
 
     // One step: two blocks of the stage that has arrived.  MASKED: some of their tokens may be unseen, or the second block is not there.
-    const auto attend = [&](auto masked_tag, int step, uint32_t src) {
+    const auto attend = [&](auto masked_tag, auto spread_tag, int step, uint32_t src) {
       constexpr bool MASKED = decltype(masked_tag)::value;
+      constexpr int E = decltype(spread_tag)::value ? 1 : 2;      // columns of a lane that are anybody's
       int tok0[NB];
       if (LIST) {
         const int2 t = sm.tok[warp][take];
@@ -437,29 +445,28 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
       for (int n = 0; n < NB; ++n) {
         if (plain) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) sc[n][i] = fmaf(sc[n][i], c_row[i & 1], -m_ref[i & 1]);
+          for (int i = 0; i < 4; i += 3 - E) sc[n][i] = fmaf(sc[n][i], c_row[i & 1], -m_ref[i & 1]);
         } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) sc[n][i] = score(sc[n][i] * c_row[i & 1], i & 1, tok0[n] + 8 * (i >> 1) + r) - m_ref[i & 1];
+          for (int i = 0; i < 4; i += 3 - E) sc[n][i] = score(sc[n][i] * c_row[i & 1], i & 1, tok0[n] + 8 * (i >> 1) + r) - m_ref[i & 1];
         }
         if (MASKED) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < 4; i += 3 - E)
             if (!seen(tok0[n] + 8 * (i >> 1) + r, i & 1)) sc[n][i] = -INFINITY;
         }
 #pragma unroll
-        for (int e = 0; e < 2; ++e) most[e] = fmaxf(most[e], fmaxf(sc[n][e], sc[n][2 + e]));
+        for (int e = 0; e < E; ++e) most[e] = fmaxf(most[e], fmaxf(sc[n][e], sc[n][2 + e]));
       }
-      if (__any_sync(0xffffffffu, most[0] > grow[0] || most[1] > grow[1])) {
-        float alpha[2];
+      if (__any_sync(0xffffffffu, most[0] > grow[0] || (E == 2 && most[1] > grow[1]))) {
+        float alpha[2] = {1.f, 1.f};
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < E; ++e) {
           float mx = most[e];
 #pragma unroll
           for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
           mx -= kFqBelow;
           const bool first = grow[e] != kFqGrow;         // nothing seen so far: sum and output are still 0
-          alpha[e] = 1.f;
           if (mx > (first ? -INFINITY : 0.f)) {
             if (!first) alpha[e] = exp2_approx(-mx);
             grow[e] = kFqGrow;
@@ -475,14 +482,14 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-          for (int f = 0; f < 4; ++f) o[m][f] *= alpha[f & 1];
+          for (int f = 0; f < 4; f += 3 - E) o[m][f] *= alpha[f & 1];
       }
       uint32_t ph[NB][2], pl[NB][2];
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
-        float p[4];
+        float p[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 4; i += 3 - E) {
           p[i] = exp2_approx(sc[n][i]);
           l_run[i & 1] += p[i];
         }
@@ -556,7 +563,11 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
         masked = (blk0 + (step + 1) * NB) * kQuantBlock - 1 > pos_first || step * NB + 1 >= nb;
       }
       const uint32_t src = ring + take * fq_stage_bytes(D);
-      if (masked) attend(std::true_type(), step, src); else attend(std::false_type(), step, src);
+      if (spread) {
+        if (masked) attend(std::true_type(), std::true_type(), step, src); else attend(std::false_type(), std::true_type(), step, src);
+      } else {
+        if (masked) attend(std::true_type(), std::false_type(), step, src); else attend(std::false_type(), std::false_type(), step, src);
+      }
       __syncwarp();                                // (all lanes have read the stage: it may be overwritten)
       if (++take == kFqStages) {
         take = 0;
@@ -589,8 +600,8 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
     if (starts && ends) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int qrow = tile * kFqRows + 2 * c + e;
-        if (qrow < n_rows) {
+        const int qrow = tile * kFqRows + row_of[e];
+        if (row_of[e] < kFqRows && qrow < n_rows) {
           const float inv = l_run[e] == 0.f ? 0.f : out_scale / l_run[e];
           float v[NT];
 #pragma unroll
@@ -617,16 +628,18 @@ __global__ void __launch_bounds__(kFqThreads, 1) fp4_attn_kernel(const __grid_co
       if (r == 0) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          sm.m[at][2 * c + e] = l_run[e] == 0.f ? -INFINITY : m_ref[e];
-          sm.l[at][2 * c + e] = l_run[e];
+          if (row_of[e] == kFqRows) continue;
+          sm.m[at][row_of[e]] = l_run[e] == 0.f ? -INFINITY : m_ref[e];
+          sm.l[at][row_of[e]] = l_run[e];
         }
       }
       __syncwarp();                               // (the rows of the second kind lie over the ring)
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+      for (int e = 0; e < 2; ++e) {
+        if (row_of[e] == kFqRows) continue;
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-          *reinterpret_cast<float2*>(dst + (2 * c + e) * D + NT * r + 2 * m) = make_float2(o[m][e], o[m][2 + e]);
+        for (int m = 0; m < MT; ++m) *reinterpret_cast<float2*>(dst + row_of[e] * D + NT * r + 2 * m) = make_float2(o[m][e], o[m][2 + e]);
+      }
     }
     u = seg_end;
   }
@@ -736,7 +749,7 @@ cudaError_t launch(const Fp4AttnArgs& a, int sm_count, cudaStream_t stream) {
   cudaError_t e = allow_smem(fp4_attn_kernel<T, D, LIST>, smem, &done);
   if (e != cudaSuccess) return e;
   const int grid = sm_count < kFqMaxCtas ? sm_count : kFqMaxCtas;
-  fp4_attn_kernel<T, D, LIST><<<grid, kFqThreads, smem, stream>>>(a);
+  fp4_attn_kernel<T, D, LIST><<<grid, FqShape<D>::kThreads, smem, stream>>>(a);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
