@@ -43,6 +43,13 @@ constexpr int kFqNowhere = 0x40000000;            // the first token of a block 
 
 __host__ __device__ constexpr int fq_stage_bytes(int D) { return 2 * fp4_block_bytes(D); }
 
+template <int THREADS>
+struct FqPlanShared {
+  unsigned long long pre[THREADS + 1];
+  unsigned long long warp_sums[THREADS / 32];
+  int4 info[THREADS];                             // slot, length, first token, tokens (0: nothing to do) of the owners
+};
+
 template <int D>
 struct FqSmem {
   // a warp's segment that goes on from the warp before it, and (over the warp's ring, once that is at rest) the one
@@ -51,25 +58,21 @@ struct FqSmem {
   float o_first[kWarps][kFqRows][D];
   QaSeg seg[2 * kWarps];
   float m[2 * kWarps][kFqRows], l[2 * kWarps][kFqRows];
-  unsigned long long pre[FqShape<D>::kThreads + 1];
-  unsigned long long warp_sums[kWarps];
   unsigned long long full[kWarps][kFqStages];
+  FqPlanShared<FqShape<D>::kThreads> plan;
   int2 tok[kWarps][kFqStages];                  // with lists: first tokens of a stage's blocks
-  int4 info[FqShape<D>::kThreads];                          // slot, length, first token, tokens (0: nothing to do) of a small batch
 };
 template <int D>
 __host__ __device__ constexpr size_t fq_ring_bytes() { return (size_t)FqShape<D>::kWarps * kFqStages * fq_stage_bytes(D); }
 
-// workspace: [ctas] QaDesc | [ctas][2][8] (m, l) | [ctas][2][8][D] o
+// workspace: [ctas][2][8] (m, l) | [ctas][2][8][D] o
 template <int D>
 struct FqWork {
-  QaDesc* desc;
   float2* ml;
   float* o;
   __host__ __device__ explicit FqWork(unsigned char* ws) {
-    desc = reinterpret_cast<QaDesc*>(ws);
-    ml = reinterpret_cast<float2*>(ws + kFqMaxCtas * sizeof(QaDesc));
-    o = reinterpret_cast<float*>(ws + kFqMaxCtas * (sizeof(QaDesc) + 2 * kFqRows * sizeof(float2)));
+    ml = reinterpret_cast<float2*>(ws);
+    o = reinterpret_cast<float*>(ws + kFqMaxCtas * 2 * kFqRows * sizeof(float2));
   }
 };
 
@@ -116,6 +119,106 @@ __device__ __forceinline__ unsigned long long units_of(const Fp4AttnArgs& a, con
   return s.w == 0 ? 0 : (unsigned long long)row_tiles(a, s.w) * a.g.n_kv_heads * (blocks_of<LIST>(a, s.y) + kFqItemCost);
 }
 
+// How the work of a call is cut: every block of either kernel works it out from the lengths.  Up to 32 owners: a lane of every warp has
+// one, and no thread waits for another; more: a thread has a run of them.
+template <bool LIST, int THREADS>
+struct FqPlan {
+  const Fp4AttnArgs& a;
+  FqPlanShared<THREADS>& sm;
+  int n_own, per;
+  bool few, without;
+  int4 mine;                                      // (few) of this lane's owner
+  unsigned long long mine_pre, total, share;
+  // found: the owner of a unit, the first unit of it
+  int b;
+  unsigned long long base;
+  int4 info;
+
+  __device__ __forceinline__ FqPlan(const Fp4AttnArgs& args, FqPlanShared<THREADS>& shared, int ctas, int min_share, bool tell) : a(args), sm(shared) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    without = !LIST && take_chunks(a, a.sm_count);
+    n_own = owners<LIST>(a);
+    few = n_own <= 32;
+    per = (n_own + THREADS - 1) / THREADS;
+    unsigned long long n = 0;
+    if (few) {
+      mine = make_int4(0, 0, 0, 0);
+      if (lane < n_own) mine = owner_info<LIST>(a, lane, tell && warp == 0, without);
+      n = units_of<LIST>(a, mine);
+    } else {
+#pragma unroll 1
+      for (int k = tid * per; k < min(n_own, (tid + 1) * per); ++k) {
+        const int4 s = owner_info<LIST>(a, k, tell, without);
+        if (per == 1) sm.info[k] = s;
+        n += units_of<LIST>(a, s);
+      }
+    }
+    unsigned long long x = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned long long y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (few) {
+      mine_pre = x - n;
+      total = __shfl_sync(0xffffffffu, x, 31);
+    } else {
+      if (lane == 31) sm.warp_sums[warp] = x;
+      __syncthreads();
+      unsigned long long before = 0;
+      for (int w = 0; w < warp; ++w) before += sm.warp_sums[w];
+      sm.pre[tid + 1] = before + x;
+      if (tid == 0) sm.pre[0] = 0;
+      __syncthreads();
+      total = sm.pre[THREADS];
+    }
+    share = quotient(total + ctas - 1, ctas);
+    if (share < (unsigned long long)min_share) share = min_share;
+  }
+  __device__ __forceinline__ int4 info_of(int k) const {
+    if (few) return make_int4(__shfl_sync(0xffffffffu, mine.x, k), __shfl_sync(0xffffffffu, mine.y, k), __shfl_sync(0xffffffffu, mine.z, k), __shfl_sync(0xffffffffu, mine.w, k));
+    return per == 1 ? sm.info[k] : owner_info<LIST>(a, k, false, without);
+  }
+  // the owner of unit u < total, by a whole warp: the last one whose units begin at or before it
+  __device__ __forceinline__ void locate(unsigned long long u) {
+    const int lane = threadIdx.x & 31;
+    if (few) {
+      b = __popc(__ballot_sync(0xffffffffu, lane < n_own && mine_pre <= u)) - 1;
+      base = __shfl_sync(0xffffffffu, mine_pre, b);
+      info = info_of(b);
+      return;
+    }
+    static_assert(THREADS <= 1024, "a lane per run of 32 prefixes");
+    const int run = __popc(__ballot_sync(0xffffffffu, lane < THREADS / 32 && sm.pre[lane * 32 < THREADS ? lane * 32 : 0] <= u)) - 1;
+    const int at = run * 32 + __popc(__ballot_sync(0xffffffffu, sm.pre[run * 32 + lane] <= u)) - 1;
+    b = at * per;
+    base = sm.pre[at];
+    info = info_of(b);
+    for (unsigned long long n = units_of<LIST>(a, info); base + n <= u; n = units_of<LIST>(a, info)) {
+      base += n;
+      info = info_of(++b);
+    }
+  }
+};
+// The item of a unit of the owner that the plan has found.
+struct FqItem {
+  int n_blk, h, tile;
+  unsigned long long first, end;                  // its units: kFqItemCost, then one per block
+};
+template <bool LIST, int THREADS>
+__device__ __forceinline__ FqItem item_of(const FqPlan<LIST, THREADS>& p, unsigned long long u) {
+  FqItem it;
+  it.n_blk = blocks_of<LIST>(p.a, p.info.y);
+  const int tiles = row_tiles(p.a, p.info.w), n = it.n_blk + kFqItemCost;
+  const unsigned long long rem = u - p.base;
+  const int ht = (int)quotient(rem, n);
+  it.h = tiles == 1 ? ht : ht / tiles;
+  it.tile = ht - it.h * tiles;
+  it.first = p.base + (unsigned long long)ht * n;
+  it.end = it.first + n;
+  return it;
+}
+
 template <typename T, int D, bool LIST>
 __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const __grid_constant__ Fp4AttnArgs a) {
   constexpr int kFqWarps = FqShape<D>::kWarps, kFqThreads = FqShape<D>::kThreads, kFqMinShare = 2 * kFqWarps;      // (units of a CTA at least)
@@ -138,54 +241,19 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
   };
 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  // ---- the units of the call, and this CTA's and warp's share of them
-  const bool without = !LIST && take_chunks(a, a.sm_count);
-  const int n_own = owners<LIST>(a), per = (n_own + kFqThreads - 1) / kFqThreads;
-  {
-    unsigned long long n = 0;
-#pragma unroll 1
-    for (int b = tid * per; b < min(n_own, (tid + 1) * per); ++b) {
-      const int4 s = owner_info<LIST>(a, b, blockIdx.x == 0, without);
-      if (per == 1) sm.info[b] = s;
-      n += units_of<LIST>(a, s);
-    }
-    unsigned long long x = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const unsigned long long y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
-    }
-    if (lane == 31) sm.warp_sums[warp] = x;
-    if (tid < 2 * kFqWarps) sm.seg[tid].valid = 0;
-    if (lane == 0) {
-      for (int i = 0; i < kFqStages; ++i) mbar_init(smem_u32(&sm.full[warp][i]), 1);
-      mbar_fence_init();
-    }
-    __syncthreads();
-    unsigned long long before = 0;
-    for (int w = 0; w < warp; ++w) before += sm.warp_sums[w];
-    sm.pre[tid + 1] = before + x;
-    if (tid == 0) sm.pre[0] = 0;
-    __syncthreads();
+  if (lane == 0) {
+    for (int i = 0; i < kFqStages; ++i) mbar_init(smem_u32(&sm.full[warp][i]), 1);
+    mbar_fence_init();
   }
-  const unsigned long long total = sm.pre[kFqThreads];
-  unsigned long long share = quotient(total + gridDim.x - 1, gridDim.x);
-  if (share < kFqMinShare) share = kFqMinShare;
+  if (lane < 2) sm.seg[2 * warp + lane].valid = 0;
+  __syncwarp();
+  // ---- this CTA's and warp's share of the call's units
+  FqPlan<LIST, kFqThreads> plan(a, sm.plan, gridDim.x, kFqMinShare, blockIdx.x == 0);
+  const unsigned long long total = plan.total, share = plan.share;
   const unsigned long long cta0 = min(total, share * blockIdx.x), cta1 = min(total, cta0 + share);
   const unsigned long long wshare = quotient(cta1 - cta0 + kFqWarps - 1, kFqWarps);
   unsigned long long u = min(cta1, cta0 + wshare * warp);
   const unsigned long long u_end = min(cta1, u + wshare);
-
-  // the owner of unit u: the last thread whose prefix is not above it, in two votes
-  int b = 0;
-  unsigned long long base = 0;                    // first unit of owner b
-  if (u < u_end) {
-    static_assert(kFqWarps <= 32, "a lane per run of 32 prefixes");
-    const int run = __popc(__ballot_sync(0xffffffffu, lane < kFqWarps && sm.pre[lane * 32] <= u)) - 1;
-    const int at = run * 32 + __popc(__ballot_sync(0xffffffffu, sm.pre[run * 32 + lane] <= u)) - 1;
-    b = at * per;
-    base = sm.pre[at];
-  }
   const bool plain = !(a.softcap > 0.f) && a.slopes == nullptr;
   const float cap_in = a.softcap > 0.f ? 1.f / a.softcap : 0.f, cap_out = a.softcap * kLog2e;
 
@@ -194,20 +262,11 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
   uint32_t phase = 0;                             // and the parity of the latter's barrier
   bool dead = false;                              // a copy did not arrive (reported); the warp gives up
   while (u < u_end && !dead) {
-    int4 info = per == 1 ? sm.info[b] : owner_info<LIST>(a, b, false, without);
-    unsigned long long n_units = units_of<LIST>(a, info);
-    while (base + n_units <= u) {
-      base += n_units;
-      ++b;
-      info = per == 1 ? sm.info[b] : owner_info<LIST>(a, b, false, without);
-      n_units = units_of<LIST>(a, info);
-    }
-    const int slot = info.x, len = info.y, first_token = info.z, n_new = info.w;
-    const int n_blk = blocks_of<LIST>(a, len), tiles = row_tiles(a, n_new);
-    const unsigned long long rem = u - base;
-    const int ht = (int)quotient(rem, n_blk + kFqItemCost), at0 = (int)(rem - (unsigned long long)ht * (n_blk + kFqItemCost));
-    const int h = tiles == 1 ? ht : ht / tiles, tile = ht - h * tiles;
-    const unsigned long long item = u - at0, item_end = item + n_blk + kFqItemCost;
+    plan.locate(u);
+    const FqItem it = item_of(plan, u);
+    const int slot = plan.info.x, len = plan.info.y, first_token = plan.info.z, n_new = plan.info.w, b = plan.b;
+    const int h = it.h, tile = it.tile, at0 = (int)(u - it.first);
+    const unsigned long long item = it.first, item_end = it.end;
     const unsigned long long seg_end = min(item_end, u_end);
     // blocks [blk0, blk0 + nb) of the item
     const int blk0 = max(0, at0 - kFqItemCost), nb = max(0, (int)(seg_end - item) - kFqItemCost) - blk0;
@@ -265,7 +324,7 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
     for (int x = 0; x < KS; x += Quad<T>::kPerLoad)
       if (ok) Quad<T>::load16(qp + KC * 16 * c + 4 * x, &qv[x]);
       else Quad<T>::zero16(&qv[x]);
-    Place next = look_up(1);
+    Place next = {0, kFqNowhere};
     const int n_steps = (nb + NB - 1) / NB;
     int left = 0;                                  // stages asked for and not yet taken
     int asked = 0;                                 // steps whose copies are under way or done
@@ -293,6 +352,7 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
       fill = fill == kFqStages - 1 ? 0 : fill + 1;
     };
     while (asked < min(kFqStages, n_steps)) issue();
+    next = look_up(1);                             // (not needed before the sixteenth step)
 
     {
       // (magnitudes compare as integers; an infinity or NaN gives the factor 1 and goes on through the products)
@@ -655,7 +715,6 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
   const unsigned long long my_item = is_seg ? sm.seg[lane].item : ~0ull;
   const float my_m = is_seg ? sm.m[lane][warp] : -INFINITY, my_l = is_seg ? sm.l[lane][warp] : 0.f;
   uint32_t todo = __ballot_sync(0xffffffffu, is_seg);
-  QaDesc desc = {0, 0, 0, 0};
   while (todo) {
     const int i = __ffs(todo) - 1;
     const uint32_t mine = __ballot_sync(0xffffffffu, my_item == __shfl_sync(0xffffffffu, my_item, i)) & todo;
@@ -676,7 +735,7 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
       for (int e = 0; e < E; ++e) acc[e] += wk * o[e];
     }
     if (starts && ends) {
-      const int4 s = per == 1 ? sm.info[first.b] : owner_info<LIST>(a, first.b, false, without);
+      const int4 s = plan.info_of(first.b);
       const int qrow = first.tile * kFqRows + warp;
       if (qrow < s.w * a.group) {
         const float inv = l == 0.f ? 0.f : out_scale / l;
@@ -690,22 +749,32 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
       if (lane == 0) ws.ml[p] = make_float2(m, l);
 #pragma unroll
       for (int e = 0; e < E; ++e) ws.o[p * D + lane * E + e] = acc[e];
-      if (starts) desc = QaDesc{(int)(quotient(first.item_end - 1, share) - blockIdx.x) + 1, first.b, first.tile, first.h};
     }
   }
-  if (tid == 0) ws.desc[blockIdx.x] = desc;
 }
 
-// Joins the items that shares cut: block g the one that begins in CTA g and goes on in the next ones.  Also zeroes the rows of
-// unusable sequences (tokens).  Launched while the first kernel runs, it waits for that one's end.
+// Joins the items that shares cut: block g the one whose first block of keys is in CTA g and that goes on in the next ones.  Also zeroes
+// the rows of unusable sequences (tokens).  Launched while the first kernel runs, it works out what it has to join and waits for that
+// one's end.
 template <typename T, int D, bool LIST>
 __global__ void __launch_bounds__(kFqMergeThreads) fp4_merge_kernel(const __grid_constant__ Fp4AttnArgs a) {
   constexpr int E = D / 32;
+  __shared__ FqPlanShared<kFqMergeThreads> shared;
   const int tid = threadIdx.x, lane = tid & 31, row = tid >> 5;
   const FqWork<D> ws(a.ws);
+  FqPlan<LIST, kFqMergeThreads> plan(a, shared, gridDim.x, 2 * FqShape<D>::kWarps, false);
+  const unsigned long long from = plan.share * blockIdx.x, behind = from + plan.share;      // the units of CTA g
+  int n_parts = 0;
+  FqItem it = {};
+  if (behind < plan.total) {
+    plan.locate(behind);
+    it = item_of(plan, behind);
+    const unsigned long long first_block = it.first + kFqItemCost;
+    if (first_block < behind && first_block >= from) n_parts = (int)quotient(it.end - 1, plan.share) - (int)blockIdx.x + 1;
+  }
   asm volatile("griddepcontrol.wait;" ::: "memory");
 #pragma unroll 1
-  for (int b = blockIdx.x; b < owners<LIST>(a); b += gridDim.x) {
+  for (int b = blockIdx.x; b < plan.n_own; b += gridDim.x) {
     const QuantSeq s = owner<LIST>(a, b);
     if (s.error && s.n > 0) {
       T* dst = static_cast<T*>(a.out) + (long long)s.first * a.n_q_heads * D;
@@ -713,17 +782,16 @@ __global__ void __launch_bounds__(kFqMergeThreads) fp4_merge_kernel(const __grid
       for (long long i = tid; i < n; i += kFqMergeThreads) dst[i] = from_f32<T>(0.f);
     }
   }
-  const QaDesc d = ws.desc[blockIdx.x];
   const float out_scale = a.out_scale;
-  if (d.n_parts == 0) return;
+  if (n_parts == 0) return;
   const auto part = [&](int p) -> long long { return ((long long)(blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * kFqRows + row; };
-  const int4 s = owner_info<LIST>(a, d.b, false, false);
+  const int4 s = plan.info;
   float m = -INFINITY;
-  for (int p = lane; p < d.n_parts; p += 32) m = fmaxf(m, ws.ml[part(p)].x);
+  for (int p = lane; p < n_parts; p += 32) m = fmaxf(m, ws.ml[part(p)].x);
   m = warp_max(m);
   float l = 0.f, acc[E] = {};
 #pragma unroll 4
-  for (int p = 0; p < d.n_parts; ++p) {
+  for (int p = 0; p < n_parts; ++p) {
     const float2 ml = ws.ml[part(p)];
     const float w = ml.y == 0.f ? 0.f : exp2_approx(ml.x - m);
     l += w * ml.y;
@@ -731,11 +799,11 @@ __global__ void __launch_bounds__(kFqMergeThreads) fp4_merge_kernel(const __grid
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] += w * o[e];
   }
-  const int qrow = d.tile * kFqRows + row;
+  const int qrow = it.tile * kFqRows + row;
   if (qrow >= s.w * a.group) return;
   const float inv = l == 0.f ? 0.f : out_scale / l;
   T* dst = static_cast<T*>(a.out) +
-           ((long long)(s.z + (qrow >> a.group_shift)) * a.n_q_heads + d.h * a.group + (qrow & (a.group - 1))) * D + lane * E;
+           ((long long)(s.z + (qrow >> a.group_shift)) * a.n_q_heads + it.h * a.group + (qrow & (a.group - 1))) * D + lane * E;
 #pragma unroll
   for (int e = 0; e < E; ++e) dst[e] = from_f32<T>(acc[e] * inv);
 }
@@ -771,7 +839,7 @@ cudaError_t launch_l(const Fp4AttnArgs& a, int sm_count, cudaStream_t stream) {
 }  // namespace
 
 uint64_t fp4_attn_workspace_bytes(int head_dim) {
-  const uint64_t n = (uint64_t)kFqMaxCtas * (sizeof(QaDesc) + 2ull * kFqRows * (sizeof(float2) + (uint64_t)head_dim * sizeof(float)));
+  const uint64_t n = (uint64_t)kFqMaxCtas * 2 * kFqRows * (sizeof(float2) + (uint64_t)head_dim * sizeof(float));
   return (n + 255) / 256 * 256;
 }
 
