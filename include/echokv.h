@@ -503,16 +503,16 @@ int echokv_quant_attention(const echokv_config* cfg, const echokv_quant_cache* c
  * The same step over a cache held in 4 bits: rotate and append in one call, attend the whole cache or chosen pages.
  *
  *     echokv_plan_tokens            as above                                                       (once per step)
- *     echokv_fp4_append             rotary positions on the new queries and keys, keys and values into the cache
- *     echokv_fp4_attention          every new token attends its sequence                           (per layer), or
- *     echokv_fp4_select             which pages of its sequence each new token reads, by bounds on their scores
- *     echokv_fp4_sparse_attention   every new token attends those pages                            (per layer)
- *     echokv_fp4_read               rows back in the storage type (to move a sequence to another cache, or to look at it)
+ *     echokv_fourbit_append             rotary positions on the new queries and keys, keys and values into the cache
+ *     echokv_fourbit_attention          every new token attends its sequence                           (per layer), or
+ *     echokv_fourbit_select             which pages of its sequence each new token reads, by bounds on their scores
+ *     echokv_fourbit_sparse_attention   every new token attends those pages                            (per layer)
+ *     echokv_fourbit_read               rows back in the storage type (to move a sequence to another cache, or to look at it)
  * Everything said above about the serving calls holds: no context, no allocation, any stream, capturable, cfg->device.
  * ===================================================================================================== */
 
-enum { ECHOKV_FP4_GROUP = 16 };              /* features that share a scale; also the tokens of a block */
-enum { ECHOKV_FP4_MAX_SELECT = 1024 };       /* pages that a query may choose */
+enum { ECHOKV_FOURBIT_GROUP = 16 };              /* features that share a scale; also the tokens of a block */
+enum { ECHOKV_FOURBIT_MAX_SELECT = 1024 };       /* pages that a query may choose */
 
 /* The cache of ONE layer in 4 bits (4.5 with the scales): device pointers, 16-byte aligned, borrowed.  A group is 16 consecutive
  * features of one token and KV head.  With a its largest magnitude and unit = k_unit or v_unit, all in fp32:
@@ -520,13 +520,13 @@ enum { ECHOKV_FP4_MAX_SELECT = 1024 };       /* pages that a query may choose */
  *     most 6; 0 where s is 0),  value = code * s * unit.
  * A token is held by itself: what is in the cache does not depend on how many came per call, or in which order.
  * A token whose key or value has an infinity or NaN (in this KV head) gets K scales NaN and values 0: whatever attends it becomes
- * NaN, nothing else does.  V scales are never NaN in a cache that echokv_fp4_append wrote; tokens behind a sequence's end may be anything.
+ * NaN, nothing else does.  V scales are never NaN in a cache that echokv_fourbit_append wrote; tokens behind a sequence's end may be anything.
  *   blocks: [n_pages][n_kv_heads][page_tokens / 16] blocks of 18 head_dim bytes (16 tokens):
  *     K codes  [16 tokens][head_dim / 2]   feature 2 i in the low half of byte i
  *     V codes  [token / 8][feature / (head_dim / 8)][token / 2 % 4][token % 2][head_dim / 16]   (token pairs side by side)
  *     K scales [16 tokens][head_dim / 16]  e4m3
  *     V scales [head_dim / 16][16 tokens]  e4m3
- *   bounds, bound_scales (both or neither NULL; echokv_fp4_select needs them): for every page and KV head the largest and the
+ *   bounds, bound_scales (both or neither NULL; echokv_fourbit_select needs them): for every page and KV head the largest and the
  *     smallest value that each feature of its keys has, in 8 bits around one scale (units of k_unit):
  *     int8 [n_pages][n_kv_heads][2][head_dim] and fp32 [n_pages][n_kv_heads];  with a the largest magnitude of all,
  *     scale = max(a * (1 / 127), 2^-60), code = round(x * (1 / scale)).  A page with a NaN key: scale NaN, codes 0. */
@@ -535,17 +535,17 @@ typedef struct {
   void* bounds;                /* or NULL */
   float* bound_scales;         /* or NULL */
   float k_unit, v_unit;        /* 2^-60 .. 2^60: a group's largest magnitude should lie between about unit / 10 and 2688 unit */
-} echokv_fp4_cache;
+} echokv_fourbit_cache;
 
 typedef struct {
   uint64_t blocks_bytes;
   uint64_t bounds_bytes;
   uint64_t bound_scales_bytes;
-  uint64_t workspace_bytes;    /* of echokv_fp4_attention, echokv_fp4_select and echokv_fp4_sparse_attention */
-} echokv_fp4_sizes;
+  uint64_t workspace_bytes;    /* of echokv_fourbit_attention, echokv_fourbit_select and echokv_fourbit_sparse_attention */
+} echokv_fourbit_sizes;
 
 /* Sizes implied by a config.  Pure host arithmetic, no CUDA call. */
-int echokv_query_fp4_sizes(const echokv_config* cfg, echokv_fp4_sizes* out);
+int echokv_query_fourbit_sizes(const echokv_config* cfg, echokv_fourbit_sizes* out);
 
 /* A rotation as echokv_rotate's arguments describe it (rot_dim: 0 = head_dim, otherwise a multiple of 16). */
 typedef struct {
@@ -563,7 +563,7 @@ typedef struct {
  *    that this call writes (a sequence's tokens come in order of position, each call beginning where the cache ends or before).
  *  - a pool row may appear once per call.
  * Rows are 16-byte aligned (EINVAL); n_tokens at most 2^27. */
-int echokv_fp4_append(const echokv_config* cfg, const echokv_fp4_cache* cache, const echokv_rotation* rotation, const void* q,
+int echokv_fourbit_append(const echokv_config* cfg, const echokv_fourbit_cache* cache, const echokv_rotation* rotation, const void* q,
                       int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k_new, int64_t k_stride, const void* v_new,
                       int64_t v_stride, const int32_t* dev_positions, const int64_t* dev_slot_map, int n_tokens,
                       int32_t* dev_status, void* stream);
@@ -571,14 +571,14 @@ int echokv_fp4_append(const echokv_config* cfg, const echokv_fp4_cache* cache, c
 /* Rows back: k_out, v_out ([n_tokens] rows of n_kv_heads x head_dim elements of the storage dtype; either may be NULL) receive the
  * values of pool rows dev_slot_map[i], rounded to the storage type (exact in fp32 and bf16 where unit is a power of two).
  * Slot -1: zeros; a bad slot: zeros and EBADPAGE.  A token that was not finite reads as keys NaN, values 0. */
-int echokv_fp4_read(const echokv_config* cfg, const echokv_fp4_cache* cache, const int64_t* dev_slot_map, int n_tokens, void* k_out,
+int echokv_fourbit_read(const echokv_config* cfg, const echokv_fourbit_cache* cache, const int64_t* dev_slot_map, int n_tokens, void* k_out,
                     int64_t k_stride, void* v_out, int64_t v_stride, int32_t* dev_status, void* stream);
 
 /* echokv_quant_attention over this cache: the same arguments, options, masks, statuses and rules for out and workspace
- * (echokv_fp4_sizes.workspace_bytes).  The cache's values enter the products exactly; bf16 queries as fp16 (exact around each row's
+ * (echokv_fourbit_sizes.workspace_bytes).  The cache's values enter the products exactly; bf16 queries as fp16 (exact around each row's
  * power of two) with probabilities rounded to fp16 (one below 2^-29 of its row's largest may count as 0; in chunks 2^-24), fp32 queries
  * and their probabilities as pairs of fp16 (22 bits). */
-int echokv_fp4_attention(const echokv_config* cfg, const echokv_fp4_cache* cache, const echokv_score_options* options, const void* q,
+int echokv_fourbit_attention(const echokv_config* cfg, const echokv_fourbit_cache* cache, const echokv_score_options* options, const void* q,
                          int64_t q_stride, void* out, const int32_t* dev_block_table, const int32_t* dev_seq_slots,
                          const int32_t* dev_seq_lens, const int32_t* dev_cu_tokens, int B, int n_tokens, int max_new, void* workspace,
                          uint64_t workspace_bytes, int32_t* dev_status, void* stream);
@@ -592,20 +592,20 @@ int echokv_fp4_attention(const echokv_config* cfg, const echokv_fp4_cache* cache
  * with top and low the page's bounds, s_q = a * (1 / 127) limited to 2^-60 .. 2^100, a the largest magnitude of the query
  * row, code = round(q * (1 / s_q)); the sum is exact, the products are fp32.  A page whose scale is NaN counts as the largest finite
  * score; a query row with an infinity or NaN as a row of zeros.
- * n_first >= 0, n_recent >= 1, n_first + n_recent <= n_select <= ECHOKV_FP4_MAX_SELECT (EINVAL).  Tokens with sequence -1: -1 entries.
+ * n_first >= 0, n_recent >= 1, n_first + n_recent <= n_select <= ECHOKV_FOURBIT_MAX_SELECT (EINVAL).  Tokens with sequence -1: -1 entries.
  * A bad sequence, slot or page -> EBADPAGE, position -> EBADLENGTH: -1 entries (a bad page id: unspecified pages, all of them < p + 1). */
-int echokv_fp4_select(const echokv_config* cfg, const echokv_fp4_cache* cache, const void* q, int64_t q_stride,
+int echokv_fourbit_select(const echokv_config* cfg, const echokv_fourbit_cache* cache, const void* q, int64_t q_stride,
                       const int32_t* dev_block_table, const int32_t* dev_seq_slots, const int32_t* dev_token_seqs,
                       const int32_t* dev_positions, int B, int n_tokens, int n_select, int n_first, int n_recent, int32_t* dev_pages,
                       void* workspace, uint64_t workspace_bytes, int32_t* dev_status, void* stream);
 
 /* Every token attends the listed pages of its sequence, keys up to its own position: token i, KV head h the pages dev_pages[i][h]
- * [0 .. n_select - 1] (echokv_fp4_select's, or the caller's own: in any order, -1 anywhere is skipped; of the list, the first
+ * [0 .. n_select - 1] (echokv_fourbit_select's, or the caller's own: in any order, -1 anywhere is skipped; of the list, the first
  * position / page_tokens + 1 entries are looked at; a page listed twice counts twice; one behind the token's own: EBADPAGE,
- * skipped).  options as for echokv_fp4_attention, without prefixes (EINVAL).  A token that has no key: zeros.
- * out, q: as for echokv_fp4_attention.  Rows of tokens with sequence -1 stay as they are.  A bad sequence or slot -> EBADPAGE,
- * position -> EBADLENGTH: zeros.  n_select 1 .. ECHOKV_FP4_MAX_SELECT. */
-int echokv_fp4_sparse_attention(const echokv_config* cfg, const echokv_fp4_cache* cache, const echokv_score_options* options,
+ * skipped).  options as for echokv_fourbit_attention, without prefixes (EINVAL).  A token that has no key: zeros.
+ * out, q: as for echokv_fourbit_attention.  Rows of tokens with sequence -1 stay as they are.  A bad sequence or slot -> EBADPAGE,
+ * position -> EBADLENGTH: zeros.  n_select 1 .. ECHOKV_FOURBIT_MAX_SELECT. */
+int echokv_fourbit_sparse_attention(const echokv_config* cfg, const echokv_fourbit_cache* cache, const echokv_score_options* options,
                                 const void* q, int64_t q_stride, void* out, const int32_t* dev_block_table,
                                 const int32_t* dev_seq_slots, const int32_t* dev_token_seqs, const int32_t* dev_positions,
                                 const int32_t* dev_pages, int n_select, int B, int n_tokens, void* workspace,

@@ -22,7 +22,7 @@ ECHOKV_ENOWEIGHTS, ECHOKV_ECUDA, ECHOKV_ETIMEOUT, ECHOKV_EBADPAGE = -5, -6, -7, 
 ECHOKV_EUNSUPPORTED, ECHOKV_ENOTABLE, ECHOKV_EBADLENGTH, ECHOKV_ESCRATCH = -9, -10, -11, -12
 ECHOKV_INT8, ECHOKV_E4M3 = 0, 1
 ECHOKV_QUANT_BLOCK_TOKENS = 16
-ECHOKV_FP4_GROUP, ECHOKV_FP4_MAX_SELECT = 16, 1024
+ECHOKV_FOURBIT_GROUP, ECHOKV_FOURBIT_MAX_SELECT = 16, 1024
 QUANT_FORMATS = {"int8": ECHOKV_INT8, "e4m3": ECHOKV_E4M3}
 
 
@@ -65,12 +65,12 @@ class echokv_score_options(C.Structure):
                 ("prefix_lens", C.c_void_p)]
 
 
-class echokv_fp4_cache(C.Structure):
+class echokv_fourbit_cache(C.Structure):
     _fields_ = [("blocks", C.c_void_p), ("bounds", C.c_void_p), ("bound_scales", C.c_void_p), ("k_unit", C.c_float),
                 ("v_unit", C.c_float)]
 
 
-class echokv_fp4_sizes(C.Structure):
+class echokv_fourbit_sizes(C.Structure):
     _fields_ = [("blocks_bytes", C.c_uint64), ("bounds_bytes", C.c_uint64), ("bound_scales_bytes", C.c_uint64),
                 ("workspace_bytes", C.c_uint64)]
 
@@ -142,19 +142,19 @@ EXPORTS = {
     "echokv_quant_attention": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_quant_cache), C.POINTER(echokv_score_options),
                                          C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
                                          C.c_int, C.c_int, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p]),
-    "echokv_query_fp4_sizes": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fp4_sizes)]),
-    "echokv_fp4_append": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fp4_cache), C.POINTER(echokv_rotation), C.c_void_p,
+    "echokv_query_fourbit_sizes": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fourbit_sizes)]),
+    "echokv_fourbit_append": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fourbit_cache), C.POINTER(echokv_rotation), C.c_void_p,
                                     C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
                                     C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]),
-    "echokv_fp4_read": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fp4_cache), C.c_void_p, C.c_int, C.c_void_p, C.c_int64,
+    "echokv_fourbit_read": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fourbit_cache), C.c_void_p, C.c_int, C.c_void_p, C.c_int64,
                                   C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
-    "echokv_fp4_attention": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fp4_cache), C.POINTER(echokv_score_options),
+    "echokv_fourbit_attention": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fourbit_cache), C.POINTER(echokv_score_options),
                                        C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
                                        C.c_int, C.c_int, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p]),
-    "echokv_fp4_select": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fp4_cache), C.c_void_p, C.c_int64, C.c_void_p,
+    "echokv_fourbit_select": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fourbit_cache), C.c_void_p, C.c_int64, C.c_void_p,
                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p,
                                     C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p]),
-    "echokv_fp4_sparse_attention": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fp4_cache), C.POINTER(echokv_score_options),
+    "echokv_fourbit_sparse_attention": (C.c_int, [C.POINTER(echokv_config), C.POINTER(echokv_fourbit_cache), C.POINTER(echokv_score_options),
                                               C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                               C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p]),
     "echokv_strerror": (C.c_char_p, [C.c_int]),
@@ -713,9 +713,9 @@ class Rotation:
         self._c = echokv_rotation(theta, self._sections, n_axes, 1 if interleaved else 0, rot_dim, 0)
 
 
-def query_fp4_sizes(cfg: echokv_config) -> echokv_fp4_sizes:
-    out = echokv_fp4_sizes()
-    _check(lib().echokv_query_fp4_sizes(C.byref(cfg), C.byref(out)), "echokv_query_fp4_sizes")
+def query_fourbit_sizes(cfg: echokv_config) -> echokv_fourbit_sizes:
+    out = echokv_fourbit_sizes()
+    _check(lib().echokv_query_fourbit_sizes(C.byref(cfg), C.byref(out)), "echokv_query_fourbit_sizes")
     return out
 
 
@@ -736,7 +736,7 @@ class Fp4Cache:
                  selection: bool = True, workspace=None):
         import torch
         self.cfg, self.tdtype, self.k_unit, self.v_unit = cfg, _dtype(cfg), k_unit, v_unit
-        self.sizes = sizes = query_fp4_sizes(cfg)
+        self.sizes = sizes = query_fourbit_sizes(cfg)
         if not all(2.0 ** -60 <= u <= 2.0 ** 60 for u in (k_unit, v_unit)):
             raise ValueError("k_unit, v_unit: between 2^-60 and 2^60")
         if (bounds is None) != (bound_scales is None) or (bounds is not None and not selection):
@@ -756,7 +756,7 @@ class Fp4Cache:
         self.bound_scales = held(bound_scales, (N, H), torch.float32, "bound_scales") if selection else None
         self.workspace = torch.empty(sizes.workspace_bytes, dtype=torch.uint8, device=dev) if workspace is None else workspace
         _dense(self.workspace, torch.uint8, self._ws_bytes, "workspace", cfg.device)
-        self._c = echokv_fp4_cache(self.blocks.data_ptr(), _ptr(self.bounds), _ptr(self.bound_scales), k_unit, v_unit)
+        self._c = echokv_fourbit_cache(self.blocks.data_ptr(), _ptr(self.bounds), _ptr(self.bound_scales), k_unit, v_unit)
 
     def append(self, k_new, v_new, slot_map, q=None, rotation: Rotation | None = None, positions=None, q_out=None, status=None,
                stream=None):
@@ -785,9 +785,9 @@ class Fp4Cache:
                 qo, qos = q_out.data_ptr(), cfg.n_q_heads * d
             else:
                 qo, qos = _rows(q_out, T, cfg.n_q_heads, d, self.tdtype, "q_out", cfg.device)
-        _check(lib().echokv_fp4_append(C.byref(cfg), C.byref(self._c), rot, qp, qs, qo, qos, kp, ks, vp, vs, pos,
+        _check(lib().echokv_fourbit_append(C.byref(cfg), C.byref(self._c), rot, qp, qs, qo, qos, kp, ks, vp, vs, pos,
                                        _dense(slot_map, torch.int64, T, "slot_map", cfg.device), T,
-                                       _dense(status, torch.int32, 1, "status", cfg.device), _stream_on(cfg.device, stream)), "echokv_fp4_append")
+                                       _dense(status, torch.int32, 1, "status", cfg.device), _stream_on(cfg.device, stream)), "echokv_fourbit_append")
         return q_out if q is not None else None
 
     def read(self, slot_map, k_out=None, v_out=None, status=None, stream=None):
@@ -806,8 +806,8 @@ class Fp4Cache:
                 vp, vs = v_out.data_ptr(), H * d
             else:
                 vp, vs = _rows(v_out, T, H, d, self.tdtype, "v_out", cfg.device)
-        _check(lib().echokv_fp4_read(C.byref(cfg), C.byref(self._c), _dense(slot_map, torch.int64, T, "slot_map", cfg.device), T, kp, ks, vp, vs,
-                                     _dense(status, torch.int32, 1, "status", cfg.device), _stream_on(cfg.device, stream)), "echokv_fp4_read")
+        _check(lib().echokv_fourbit_read(C.byref(cfg), C.byref(self._c), _dense(slot_map, torch.int64, T, "slot_map", cfg.device), T, kp, ks, vp, vs,
+                                     _dense(status, torch.int32, 1, "status", cfg.device), _stream_on(cfg.device, stream)), "echokv_fourbit_read")
         return k_out, v_out
 
     def _queries(self, q, out, stream):
@@ -829,13 +829,13 @@ class Fp4Cache:
         if softcap or alibi_slopes is not None or prefix_lens is not None:
             opts = C.byref(echokv_score_options(softcap, 0, _dense(alibi_slopes, torch.float32, cfg.n_q_heads, "alibi_slopes", cfg.device),
                                                 _dense(prefix_lens, torch.int32, B, "prefix_lens", cfg.device)))
-        _check(lib().echokv_fp4_attention(C.byref(cfg), C.byref(self._c), opts, qp, qs, op,
+        _check(lib().echokv_fourbit_attention(C.byref(cfg), C.byref(self._c), opts, qp, qs, op,
                                           _dense(block_table, torch.int32, cfg.max_batch * cfg.max_pages_per_seq, "block_table", cfg.device),
                                           _dense(seq_slots, torch.int32, B, "seq_slots", cfg.device), _dense(seq_lens, torch.int32, B, "seq_lens", cfg.device),
                                           _dense(cu_tokens, torch.int32, B + 1, "cu_tokens", cfg.device), B, T, max_new,
                                           _dense(self.workspace, torch.uint8, self._ws_bytes, "workspace", cfg.device), self._ws_bytes,
                                           _dense(status, torch.int32, 1, "status", cfg.device), _stream_on(cfg.device, stream)),
-               "echokv_fp4_attention")
+               "echokv_fourbit_attention")
         return out
 
     def _batch(self, seq_slots):
@@ -854,7 +854,7 @@ class Fp4Cache:
         if out is None:
             with _memory_of(stream):
                 out = torch.empty((T, cfg.n_kv_heads, n_select), dtype=torch.int32, device=q.device)
-        _check(lib().echokv_fp4_select(C.byref(cfg), C.byref(self._c), qp, qs,
+        _check(lib().echokv_fourbit_select(C.byref(cfg), C.byref(self._c), qp, qs,
                                        _dense(block_table, torch.int32, cfg.max_batch * cfg.max_pages_per_seq, "block_table", cfg.device),
                                        _dense(seq_slots, torch.int32, B, "seq_slots", cfg.device),
                                        _dense(token_seqs, torch.int32, T, "token_seqs", cfg.device),
@@ -862,7 +862,7 @@ class Fp4Cache:
                                        _dense(out, torch.int32, T * cfg.n_kv_heads * n_select, "out", cfg.device),
                                        _dense(self.workspace, torch.uint8, self._ws_bytes, "workspace", cfg.device), self._ws_bytes,
                                        _dense(status, torch.int32, 1, "status", cfg.device), _stream_on(cfg.device, stream)),
-               "echokv_fp4_select")
+               "echokv_fourbit_select")
         return out
 
     def sparse_attention(self, q, block_table, token_seqs, positions, pages, seq_slots=None, softcap: float = 0.0, alibi_slopes=None,
@@ -877,7 +877,7 @@ class Fp4Cache:
         opts = None
         if softcap or alibi_slopes is not None:
             opts = C.byref(echokv_score_options(softcap, 0, _dense(alibi_slopes, torch.float32, cfg.n_q_heads, "alibi_slopes", cfg.device), None))
-        _check(lib().echokv_fp4_sparse_attention(C.byref(cfg), C.byref(self._c), opts, qp, qs, op,
+        _check(lib().echokv_fourbit_sparse_attention(C.byref(cfg), C.byref(self._c), opts, qp, qs, op,
                                                  _dense(block_table, torch.int32, cfg.max_batch * cfg.max_pages_per_seq, "block_table", cfg.device),
                                                  _dense(seq_slots, torch.int32, B, "seq_slots", cfg.device),
                                                  _dense(token_seqs, torch.int32, T, "token_seqs", cfg.device),
@@ -885,7 +885,7 @@ class Fp4Cache:
                                                  _dense(pages, torch.int32, pages.numel(), "pages", cfg.device), pages.shape[2], B, T,
                                                  _dense(self.workspace, torch.uint8, self._ws_bytes, "workspace", cfg.device), self._ws_bytes,
                                                  _dense(status, torch.int32, 1, "status", cfg.device), _stream_on(cfg.device, stream)),
-               "echokv_fp4_sparse_attention")
+               "echokv_fourbit_sparse_attention")
         return out
 
 

@@ -22,19 +22,19 @@ constexpr int kFsWarps = 8;
 constexpr int kFsThreads = kFsWarps * 32;
 constexpr int kFsStep = kFsWarps * 16;             // pages that a block takes at once
 constexpr int kFsEntries = 16384;                  // keys of a block, of all its tokens
-constexpr int kFsMaxTokens = 8;                    // tokens of a block: each has room for 2048 keys, ECHOKV_FP4_MAX_SELECT and a step
+constexpr int kFsMaxTokens = 8;                    // tokens of a block: each has room for 2048 keys, ECHOKV_FOURBIT_MAX_SELECT and a step
 constexpr int kFsMaxParts = 320;                   // (token, head, part of the pages) with a place in the workspace
 constexpr int kFsMinPages = 512;                   // pages of a part at least
 constexpr uint32_t kFsAlways = 0xffffffffu;        // key of a page that is taken in any case (0: of one behind the token's own)
 
 struct FsPart {
-  uint32_t* keys;                                  // [kFsMaxParts][ECHOKV_FP4_MAX_SELECT]
+  uint32_t* keys;                                  // [kFsMaxParts][ECHOKV_FOURBIT_MAX_SELECT]
   uint32_t* pages;
   int* counts;                                     // [kFsMaxParts]
   __host__ __device__ explicit FsPart(unsigned char* ws) {
     keys = reinterpret_cast<uint32_t*>(ws);
-    pages = keys + kFsMaxParts * ECHOKV_FP4_MAX_SELECT;
-    counts = reinterpret_cast<int*>(pages + kFsMaxParts * ECHOKV_FP4_MAX_SELECT);
+    pages = keys + kFsMaxParts * ECHOKV_FOURBIT_MAX_SELECT;
+    counts = reinterpret_cast<int*>(pages + kFsMaxParts * ECHOKV_FOURBIT_MAX_SELECT);
   }
 };
 
@@ -468,8 +468,8 @@ __global__ void __launch_bounds__(kFsThreads, 2) fp4_select_kernel(const __grid_
           const FsPart ws(a.ws);
           const int slot = blockIdx.x * parts + part;
           const int m = chosen(f, my_key, n, K, sm[my_k], my_warp, warps, bar, [&](int at, int i) {
-            ws.keys[slot * ECHOKV_FP4_MAX_SELECT + at] = my_key[i];
-            ws.pages[slot * ECHOKV_FP4_MAX_SELECT + at] = my_page(i);
+            ws.keys[slot * ECHOKV_FOURBIT_MAX_SELECT + at] = my_key[i];
+            ws.pages[slot * ECHOKV_FOURBIT_MAX_SELECT + at] = my_page(i);
           });
           if (tid == 0) ws.counts[slot] = m;
         }
@@ -502,8 +502,8 @@ __global__ void __launch_bounds__(kFsWarps * 32) fp4_select_merge_kernel(const _
       n = K;
     }
     for (int j = tid; j < m; j += kThreads) {
-      key[n + j] = ws.keys[slot * ECHOKV_FP4_MAX_SELECT + j];
-      page[n + j] = ws.pages[slot * ECHOKV_FP4_MAX_SELECT + j];
+      key[n + j] = ws.keys[slot * ECHOKV_FOURBIT_MAX_SELECT + j];
+      page[n + j] = ws.pages[slot * ECHOKV_FOURBIT_MAX_SELECT + j];
     }
     n += m;
   }
@@ -541,7 +541,7 @@ cudaError_t launch(const Fp4SelectArgs& a, int sm_count, cudaStream_t stream) {
   };
   constexpr size_t kRoom = 227 * 1024;
   static_assert(kFsWarps * 2 * fs_stage_bytes(128) + kFsMaxTokens * 8 * 260 + kFsMaxTokens * sizeof(FsGroup) + kFsEntries * 4 +
-                kFsMaxTokens * (32 + ECHOKV_FP4_MAX_SELECT) * 4 <= kRoom, "shared memory of one CTA, however many tokens and pages");
+                kFsMaxTokens * (32 + ECHOKV_FOURBIT_MAX_SELECT) * 4 <= kRoom, "shared memory of one CTA, however many tokens and pages");
   const dim3 grid((unsigned)heads, parts);
   cudaError_t e;
   if (smem_of(4) <= kRoom) {
@@ -573,7 +573,7 @@ cudaError_t launch(const Fp4SelectArgs& a, int sm_count, cudaStream_t stream) {
 }  // namespace
 
 uint64_t fp4_select_workspace_bytes() {
-  const uint64_t n = (uint64_t)kFsMaxParts * (2 * ECHOKV_FP4_MAX_SELECT + 1) * 4;
+  const uint64_t n = (uint64_t)kFsMaxParts * (2 * ECHOKV_FOURBIT_MAX_SELECT + 1) * 4;
   return (n + 255) / 256 * 256;
 }
 

@@ -139,7 +139,7 @@ cudaError_t launch_quant_chunk(const QuantAttnArgs& a, int sm_count, cudaStream_
 
 // ---- the cache held in 4 bits -------------------------------------------------------------------------------------
 constexpr int kFp4 = 2;                             // QuantAttnArgs.format of it (beside ECHOKV_INT8, ECHOKV_E4M3)
-constexpr int kFp4Group = ECHOKV_FP4_GROUP;
+constexpr int kFp4Group = ECHOKV_FOURBIT_GROUP;
 __host__ __device__ constexpr int fp4_block_bytes(int d) { return 18 * d; }
 // byte offsets in a block: K codes, V codes, K scales, V scales
 __host__ __device__ constexpr int fp4_k_at(int d, int tok, int f) { return tok * (d / 2) + f / 2; }

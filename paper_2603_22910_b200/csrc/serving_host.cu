@@ -160,7 +160,7 @@ uint64_t fp4_workspace(const echokv_config* c) {
 
 bool unit_ok(float u) { return u >= 0x1p-60f && u <= 0x1p60f; }
 
-int fp4_geom(const echokv_config* c, const echokv_fp4_cache* q, Fp4Geom* g) {
+int fp4_geom(const echokv_config* c, const echokv_fourbit_cache* q, Fp4Geom* g) {
   if (!q || !q->blocks || !aligned(q->blocks, 16) || !unit_ok(q->k_unit) || !unit_ok(q->v_unit)) return ECHOKV_EINVAL;
   if ((q->bounds == nullptr) != (q->bound_scales == nullptr) || !aligned(q->bounds, 16) || !aligned(q->bound_scales, 16)) return ECHOKV_EINVAL;
   g->blocks = static_cast<unsigned char*>(q->blocks);
@@ -174,7 +174,7 @@ int fp4_geom(const echokv_config* c, const echokv_fp4_cache* q, Fp4Geom* g) {
 }
 
 // what the two attentions over the 4-bit cache have in common: everything but how queries belong to sequences
-int fp4_attention_args(const echokv_config* cfg, const echokv_fp4_cache* cache, const echokv_score_options* options, const void* q,
+int fp4_attention_args(const echokv_config* cfg, const echokv_fourbit_cache* cache, const echokv_score_options* options, const void* q,
                        int64_t q_stride, void* out, const int32_t* table, const int32_t* slots, int B, int n_tokens, void* workspace,
                        uint64_t workspace_bytes, int32_t* status, Fp4AttnArgs* a) {
   Fp4Geom g;
@@ -397,7 +397,7 @@ int echokv_quant_attention(const echokv_config* cfg, const echokv_quant_cache* c
   return launch_quant_attn(a, dev.sm_count, s) == cudaSuccess ? ECHOKV_OK : ECHOKV_ECUDA;
 }
 
-int echokv_query_fp4_sizes(const echokv_config* cfg, echokv_fp4_sizes* out) {
+int echokv_query_fourbit_sizes(const echokv_config* cfg, echokv_fourbit_sizes* out) {
   if (!out) return ECHOKV_EINVAL;
   const int rc = check_all(cfg);
   if (rc != ECHOKV_OK) return rc;
@@ -409,7 +409,7 @@ int echokv_query_fp4_sizes(const echokv_config* cfg, echokv_fp4_sizes* out) {
   return ECHOKV_OK;
 }
 
-int echokv_fp4_append(const echokv_config* cfg, const echokv_fp4_cache* cache, const echokv_rotation* rotation, const void* q,
+int echokv_fourbit_append(const echokv_config* cfg, const echokv_fourbit_cache* cache, const echokv_rotation* rotation, const void* q,
                       int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k_new, int64_t k_stride, const void* v_new,
                       int64_t v_stride, const int32_t* dev_positions, const int64_t* dev_slot_map, int n_tokens,
                       int32_t* dev_status, void* stream) {
@@ -456,14 +456,15 @@ int echokv_fp4_append(const echokv_config* cfg, const echokv_fp4_cache* cache, c
   return launch_fp4_append(a, dev.sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess ? ECHOKV_OK : ECHOKV_ECUDA;
 }
 
-int echokv_fp4_read(const echokv_config* cfg, const echokv_fp4_cache* cache, const int64_t* dev_slot_map, int n_tokens, void* k_out,
+int echokv_fourbit_read(const echokv_config* cfg, const echokv_fourbit_cache* cache, const int64_t* dev_slot_map, int n_tokens, void* k_out,
                     int64_t k_stride, void* v_out, int64_t v_stride, int32_t* dev_status, void* stream) {
   int rc = check_all(cfg);
   if (rc != ECHOKV_OK) return rc;
-  if (n_tokens < 0 || n_tokens > kMaxRows || (!k_out && !v_out)) return ECHOKV_EINVAL;
+  if (n_tokens < 0 || n_tokens > kMaxRows) return ECHOKV_EINVAL;
   Fp4ReadArgs a;
   if ((rc = fp4_geom(cfg, cache, &a.g)) != ECHOKV_OK) return rc;
   if (n_tokens == 0) return ECHOKV_OK;
+  if (!k_out && !v_out) return ECHOKV_EINVAL;
   const int elem = cfg->dtype == ECHOKV_BF16 ? 2 : 4, width = cfg->n_kv_heads * cfg->head_dim;
   if ((k_out && !rows_ok(k_out, k_stride, width, elem)) || (v_out && !rows_ok(v_out, v_stride, width, elem))) return ECHOKV_EINVAL;
   if (!dev_slot_map || !aligned(dev_slot_map, 8) || !words(dev_status)) return ECHOKV_EINVAL;
@@ -478,7 +479,7 @@ int echokv_fp4_read(const echokv_config* cfg, const echokv_fp4_cache* cache, con
   return launch_fp4_read(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? ECHOKV_OK : ECHOKV_ECUDA;
 }
 
-int echokv_fp4_attention(const echokv_config* cfg, const echokv_fp4_cache* cache, const echokv_score_options* options, const void* q,
+int echokv_fourbit_attention(const echokv_config* cfg, const echokv_fourbit_cache* cache, const echokv_score_options* options, const void* q,
                          int64_t q_stride, void* out, const int32_t* dev_block_table, const int32_t* dev_seq_slots,
                          const int32_t* dev_seq_lens, const int32_t* dev_cu_tokens, int B, int n_tokens, int max_new, void* workspace,
                          uint64_t workspace_bytes, int32_t* dev_status, void* stream) {
@@ -501,13 +502,13 @@ int echokv_fp4_attention(const echokv_config* cfg, const echokv_fp4_cache* cache
   return launch_fp4_attn(a, dev.sm_count, s) == cudaSuccess ? ECHOKV_OK : ECHOKV_ECUDA;
 }
 
-int echokv_fp4_select(const echokv_config* cfg, const echokv_fp4_cache* cache, const void* q, int64_t q_stride,
+int echokv_fourbit_select(const echokv_config* cfg, const echokv_fourbit_cache* cache, const void* q, int64_t q_stride,
                       const int32_t* dev_block_table, const int32_t* dev_seq_slots, const int32_t* dev_token_seqs,
                       const int32_t* dev_positions, int B, int n_tokens, int n_select, int n_first, int n_recent, int32_t* dev_pages,
                       void* workspace, uint64_t workspace_bytes, int32_t* dev_status, void* stream) {
   int rc = check_all(cfg);
   if (rc != ECHOKV_OK) return rc;
-  if (B < 1 || n_tokens < 0 || n_tokens > kMaxRows || n_select < 1 || n_select > ECHOKV_FP4_MAX_SELECT) return ECHOKV_EINVAL;
+  if (B < 1 || n_tokens < 0 || n_tokens > kMaxRows || n_select < 1 || n_select > ECHOKV_FOURBIT_MAX_SELECT) return ECHOKV_EINVAL;
   if (n_first < 0 || n_recent < 1 || n_first > n_select - n_recent) return ECHOKV_EINVAL;
   if ((long long)n_tokens * cfg->n_kv_heads > 0x7fffffffll) return ECHOKV_EINVAL;      // (a block each at most)
   Fp4SelectArgs a;
@@ -533,14 +534,14 @@ int echokv_fp4_select(const echokv_config* cfg, const echokv_fp4_cache* cache, c
   return launch_fp4_select(a, dev.sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess ? ECHOKV_OK : ECHOKV_ECUDA;
 }
 
-int echokv_fp4_sparse_attention(const echokv_config* cfg, const echokv_fp4_cache* cache, const echokv_score_options* options,
+int echokv_fourbit_sparse_attention(const echokv_config* cfg, const echokv_fourbit_cache* cache, const echokv_score_options* options,
                                 const void* q, int64_t q_stride, void* out, const int32_t* dev_block_table,
                                 const int32_t* dev_seq_slots, const int32_t* dev_token_seqs, const int32_t* dev_positions,
                                 const int32_t* dev_pages, int n_select, int B, int n_tokens, void* workspace,
                                 uint64_t workspace_bytes, int32_t* dev_status, void* stream) {
   int rc = check_all(cfg);
   if (rc != ECHOKV_OK) return rc;
-  if (B < 1 || n_tokens < 0 || n_tokens > kMaxRows || n_select < 1 || n_select > ECHOKV_FP4_MAX_SELECT) return ECHOKV_EINVAL;
+  if (B < 1 || n_tokens < 0 || n_tokens > kMaxRows || n_select < 1 || n_select > ECHOKV_FOURBIT_MAX_SELECT) return ECHOKV_EINVAL;
   if (options && options->prefix_lens) return ECHOKV_EINVAL;
   Fp4AttnArgs a;
   rc = fp4_attention_args(cfg, cache, options, q, q_stride, out, dev_block_table, dev_seq_slots, B, n_tokens, workspace, workspace_bytes,
