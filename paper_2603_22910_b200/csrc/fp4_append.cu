@@ -102,7 +102,8 @@ __global__ void __launch_bounds__(kFaThreads, 4) fp4_append_kernel(const __grid_
   for (int step = 0; step < steps; ++step) {
     const int i = step * kFaThreads + tid;
     const bool live = i < items;                   // (a head's G lanes are all live or none is)
-    const int u = live ? i / G : 0, grp = i % G, t = u / H, h = u - t * H;
+    // (a block's tokens side by side: what they write of a block's rows, four tokens a sector, is then written together)
+    const int u = live ? i / G : 0, grp = i % G, h = u / nt, t = u - h * nt;
     const long long row = live ? a.slot_map[t0 + t] : -1;
     const bool in_pool = row >= 0 && (row >> g.page_shift) < g.n_pages;
     if (live && row != -1 && !in_pool) report_opt(a.status, ECHOKV_EBADPAGE);
@@ -215,7 +216,7 @@ constexpr int kFbWarps = 8;
 
 template <int D>
 __global__ void __launch_bounds__(kFbWarps * 32) fp4_bounds_kernel(const __grid_constant__ Fp4AppendArgs a) {
-  constexpr int L = D / 8, R = 32 / L;             // lanes of a token, tokens of a load
+  constexpr int L = D / 8, R = 32 / L, kLoads = 8;                    // lanes of a token, tokens of a load, loads in flight
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane / L, f = lane % L * 8;
   const Fp4Geom& g = a.g;
   const int H = g.n_kv_heads;
@@ -234,12 +235,14 @@ __global__ void __launch_bounds__(kFbWarps * 32) fp4_bounds_kernel(const __grid_
     for (int j = 1; j <= left && next < 0 && i + j < a.n_tokens; ++j) next = row_of(i + j);
     last = next < 0 || (next >> g.page_shift) != (mine >> g.page_shift);
   }
-  uint32_t pages = __ballot_sync(0xffffffffu, last);
-  for (int at = 0; pages; pages &= pages - 1, ++at) {
+  // (page, head) pairs in turn: `off` is this warp's next one, from the present page's first head on
+  int off = worker;
+  for (uint32_t pages = __ballot_sync(0xffffffffu, last); pages; pages &= pages - 1, off -= H) {
     const long long row = __shfl_sync(0xffffffffu, mine, __ffs(pages) - 1);
     const long long page = row >> g.page_shift;
     const int n = (int)(row & (g.page_tokens - 1)) + 1;
-    for (int h = (worker + workers - at * H % workers) % workers; h < H; h += workers) {
+    for (; off < H; off += workers) {
+      const int h = off;
       const unsigned char* blk = g.blocks + (page * H + h) * (g.page_tokens / 16) * fp4_block_bytes(D);
       __half2 top[4], low[4];
 #pragma unroll
@@ -249,17 +252,17 @@ __global__ void __launch_bounds__(kFbWarps * 32) fp4_bounds_kernel(const __grid_
       }
       bool nan = false;
 #pragma unroll 1
-      for (int tok = r; tok < n; tok += 8 * R) {
-        uint32_t w[8], code[8];                    // eight tokens in flight
+      for (int tok = r; tok < n; tok += kLoads * R) {
+        uint32_t w[kLoads], code[kLoads];          // (that many tokens in flight)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < kLoads; ++k) {
           const int t = min(tok + k * R, n - 1);   // (the last one again: it changes nothing)
           const unsigned char* b = blk + (t >> 4) * fp4_block_bytes(D);
           w[k] = *reinterpret_cast<const uint32_t*>(b + fp4_k_at(D, t & 15, f));
           code[k] = b[fp4_ks_at(D, t & 15, f)];
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < kLoads; ++k) {
           nan |= (code[k] & 0x7fu) == kE4m3Nan;
           const uint32_t s = e4m3_scales(code[k] | code[k] << 8);
           uint32_t x[4];
@@ -312,9 +315,11 @@ __global__ void __launch_bounds__(kFaThreads) fp4_read_kernel(const __grid_const
   const Fp4Geom& g = a.g;
   const int H = g.n_kv_heads;
   const long long i = (long long)blockIdx.x * kFaThreads + threadIdx.x;
-  if (i >= (long long)a.n_tokens * H * G) return;
+  // (four tokens of a head side by side: their values share the cache's sectors)
   const int grp = (int)(i % G), f = grp * kFp4Group;
-  const int t = (int)(i / (G * H)), h = (int)(i / G) - t * H;
+  const long long u = i / (4 * G);
+  const int t = (int)(u / H) * 4 + (int)(i / G) % 4, h = (int)(u % H);
+  if (t >= a.n_tokens) return;
   const long long row = a.slot_map[t];
   const bool in_pool = row >= 0 && (row >> g.page_shift) < g.n_pages;
   if (row != -1 && !in_pool) report_opt(a.status, ECHOKV_EBADPAGE);
@@ -377,7 +382,7 @@ cudaError_t launch_fp4_append(const Fp4AppendArgs& a, int sm_count, cudaStream_t
 }
 
 cudaError_t launch_fp4_read(const Fp4ReadArgs& a, cudaStream_t stream) {
-  const long long n = (long long)a.n_tokens * a.g.n_kv_heads * (a.g.head_dim / kFp4Group);
+  const long long n = (a.n_tokens + 3ll) / 4 * 4 * a.g.n_kv_heads * (a.g.head_dim / kFp4Group);
   const unsigned grid = (unsigned)((n + kFaThreads - 1) / kFaThreads);
   const bool wide = a.g.head_dim == 128;
   if (a.dtype == ECHOKV_BF16) {
