@@ -112,7 +112,8 @@ __global__ void __launch_bounds__(kFaThreads, 4) fp4_append_kernel(const __grid_
   constexpr int G = D / kFp4Group;                 // groups of a head (4 or 8 lanes side by side)
   __shared__ __align__(16) float cs[kFaTokens][128];
   const int half = a.rot_dim >> 1, pieces = half >> 3, tid = threadIdx.x, lane = tid & 31;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  after_the_one_before();
+  let_the_next_one_come();
   const int t0 = blockIdx.x * tokens_per_block, nt = min(tokens_per_block, a.n_tokens - t0);
   const Fp4Geom& g = a.g;
   const int H = g.n_kv_heads;
@@ -246,7 +247,7 @@ __global__ void __launch_bounds__(kFbWarps * 32) fp4_bounds_kernel(const __grid_
   const Fp4Geom& g = a.g;
   const int H = g.n_kv_heads;
   const int worker = blockIdx.y * kFbWarps + warp, workers = gridDim.y * kFbWarps;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  after_the_one_before();
   const auto row_of = [&](long long i) {
     const long long row = i < a.n_tokens ? a.slot_map[i] : -1;
     return row >= 0 && (row >> g.page_shift) < g.n_pages ? row : -1;
@@ -337,6 +338,7 @@ __global__ void __launch_bounds__(kFbWarps * 32) fp4_bounds_kernel(const __grid_
 template <typename T, int D>
 __global__ void __launch_bounds__(kFaThreads) fp4_read_kernel(const __grid_constant__ Fp4ReadArgs a) {
   constexpr int G = D / kFp4Group;
+  after_the_one_before();
   const Fp4Geom& g = a.g;
   const int H = g.n_kv_heads;
   const long long i = (long long)blockIdx.x * kFaThreads + threadIdx.x;
@@ -383,21 +385,12 @@ template <typename T, int D>
 cudaError_t launch_append(const Fp4AppendArgs& a, int sm_count, cudaStream_t stream) {
   // few tokens: one per block, so that a decode step's rows spread over the SMs
   const int per_block = a.n_tokens <= 4 * sm_count ? 1 : kFaTokens;
-  fp4_append_kernel<T, D><<<(unsigned)((a.n_tokens + per_block - 1) / per_block), kFaThreads, 0, stream>>>(a, per_block);
-  cudaError_t e = cudaGetLastError();
+  cudaError_t e = launch_early(fp4_append_kernel<T, D>, dim3((unsigned)((a.n_tokens + per_block - 1) / per_block)), kFaThreads, 0, stream, a, per_block);
   if (e != cudaSuccess || a.g.bounds == nullptr) return e;
-  cudaLaunchConfig_t cfg = {};
   // (few tokens, each the last one of its page: the heads of a page over several blocks)
   const int blocks = (a.n_tokens + 31) / 32;
-  cfg.gridDim = dim3(blocks, blocks >= sm_count ? 1 : min((32 * a.g.n_kv_heads + kFbWarps - 1) / kFbWarps, (2 * sm_count + blocks - 1) / blocks));
-  cfg.blockDim = dim3(kFbWarps * 32);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, fp4_bounds_kernel<D>, a);
+  const int y = blocks >= sm_count ? 1 : min((32 * a.g.n_kv_heads + kFbWarps - 1) / kFbWarps, (2 * sm_count + blocks - 1) / blocks);
+  return launch_early(fp4_bounds_kernel<D>, dim3(blocks, y), kFbWarps * 32, 0, stream, a);
 }
 
 }  // namespace
@@ -411,14 +404,11 @@ cudaError_t launch_fp4_read(const Fp4ReadArgs& a, cudaStream_t stream) {
   const long long n = (a.n_tokens + 3ll) / 4 * 4 * a.g.n_kv_heads * (a.g.head_dim / kFp4Group);
   const unsigned grid = (unsigned)((n + kFaThreads - 1) / kFaThreads);
   const bool wide = a.g.head_dim == 128;
-  if (a.dtype == ECHOKV_BF16) {
-    if (wide) fp4_read_kernel<__nv_bfloat16, 128><<<grid, kFaThreads, 0, stream>>>(a);
-    else fp4_read_kernel<__nv_bfloat16, 64><<<grid, kFaThreads, 0, stream>>>(a);
-  } else {
-    if (wide) fp4_read_kernel<float, 128><<<grid, kFaThreads, 0, stream>>>(a);
-    else fp4_read_kernel<float, 64><<<grid, kFaThreads, 0, stream>>>(a);
-  }
-  return cudaGetLastError();
+  if (a.dtype == ECHOKV_BF16)
+    return wide ? launch_early(fp4_read_kernel<__nv_bfloat16, 128>, dim3(grid), kFaThreads, 0, stream, a)
+                : launch_early(fp4_read_kernel<__nv_bfloat16, 64>, dim3(grid), kFaThreads, 0, stream, a);
+  return wide ? launch_early(fp4_read_kernel<float, 128>, dim3(grid), kFaThreads, 0, stream, a)
+              : launch_early(fp4_read_kernel<float, 64>, dim3(grid), kFaThreads, 0, stream, a);
 }
 
 }  // namespace echokv

@@ -240,13 +240,14 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
     return at & 1 ? reinterpret_cast<float*>(fq_raw + (size_t)(at >> 1) * kFqStages * fq_stage_bytes(D)) : &sm.o_first[at >> 1][0][0];
   };
 
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (lane == 0) {
     for (int i = 0; i < kFqStages; ++i) mbar_init(smem_u32(&sm.full[warp][i]), 1);
     mbar_fence_init();
   }
   if (lane < 2) sm.seg[2 * warp + lane].valid = 0;
   __syncwarp();
+  after_the_one_before();
+  let_the_next_one_come();                        // (the second kernel reads what this one does, and waits for its end)
   // ---- this CTA's and warp's share of the call's units
   FqPlan<LIST, kFqThreads> plan(a, sm.plan, gridDim.x, kFqMinShare, blockIdx.x == 0);
   const unsigned long long total = plan.total, share = plan.share;
@@ -772,7 +773,7 @@ __global__ void __launch_bounds__(kFqMergeThreads) fp4_merge_kernel(const __grid
     const unsigned long long first_block = it.first + kFqItemCost;
     if (first_block < behind && first_block >= from) n_parts = (int)quotient(it.end - 1, plan.share) - (int)blockIdx.x + 1;
   }
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  after_the_one_before();
 #pragma unroll 1
   for (int b = blockIdx.x; b < plan.n_own; b += gridDim.x) {
     const QuantSeq s = owner<LIST>(a, b);
@@ -817,18 +818,8 @@ cudaError_t launch(const Fp4AttnArgs& a, int sm_count, cudaStream_t stream) {
   cudaError_t e = allow_smem(fp4_attn_kernel<T, D, LIST>, smem, &done);
   if (e != cudaSuccess) return e;
   const int grid = sm_count < kFqMaxCtas ? sm_count : kFqMaxCtas;
-  fp4_attn_kernel<T, D, LIST><<<grid, FqShape<D>::kThreads, smem, stream>>>(a);
-  if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(kFqMergeThreads);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, fp4_merge_kernel<T, D, LIST>, a);
+  if ((e = launch_early(fp4_attn_kernel<T, D, LIST>, dim3(grid), FqShape<D>::kThreads, smem, stream, a)) != cudaSuccess) return e;
+  return launch_early(fp4_merge_kernel<T, D, LIST>, dim3(grid), kFqMergeThreads, 0, stream, a);
 }
 
 template <typename T, int D>

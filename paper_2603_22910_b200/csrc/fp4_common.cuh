@@ -48,4 +48,23 @@ __device__ __forceinline__ uint32_t e4m3_code(float x) {
 }
 constexpr uint32_t kE4m3Nan = 0x7fu;
 
+// A kernel whose blocks may be there before the one before it on the stream has ended.  It begins with after_the_one_before(), behind which
+// everything that was written before is seen; where it lets its own successor come early, it does so after that.
+template <typename... P, typename... A>
+inline cudaError_t launch_early(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+__device__ __forceinline__ void after_the_one_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_the_next_one_come() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 }  // namespace echokv

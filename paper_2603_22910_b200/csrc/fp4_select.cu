@@ -284,6 +284,7 @@ __global__ void __launch_bounds__(kFsThreads, 2) fp4_select_kernel(const __grid_
   uint32_t* key_of = reinterpret_cast<uint32_t*>(sm + tile_tokens);
   uint32_t* list_of = key_of + tile_tokens * capacity;
 
+  after_the_one_before();
   // the block's tokens: i0 and those behind it at the following positions of its sequence, up to the next multiple of
   // tile_tokens; a token that belongs to one before it has nothing to do
   const FsToken first = token_of(a, i0);
@@ -488,7 +489,7 @@ __global__ void __launch_bounds__(kFsWarps * 32) fp4_select_merge_kernel(const _
   const FsPages pages = {page, capacity, 0u};
   const FsPart ws(a.ws);
   const int own = token_of(a, token).own;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  after_the_one_before();
   if (own < K) {
     write_all(a, token, h, own, tid, kThreads);
     return;
@@ -547,27 +548,17 @@ cudaError_t launch(const Fp4SelectArgs& a, int sm_count, cudaStream_t stream) {
   if (smem_of(4) <= kRoom) {
     static std::atomic<unsigned long long> done{0};
     if ((e = allow_smem(fp4_select_kernel<T, D, 4>, kRoom, &done)) != cudaSuccess) return e;
-    fp4_select_kernel<T, D, 4><<<grid, kFsThreads, smem_of(4), stream>>>(a, tile_tokens, capacity);
+    e = launch_early(fp4_select_kernel<T, D, 4>, grid, kFsThreads, smem_of(4), stream, a, tile_tokens, capacity);
   } else {
     static std::atomic<unsigned long long> done{0};
     if ((e = allow_smem(fp4_select_kernel<T, D, 2>, kRoom, &done)) != cudaSuccess) return e;
-    fp4_select_kernel<T, D, 2><<<grid, kFsThreads, smem_of(2), stream>>>(a, tile_tokens, capacity);
+    e = launch_early(fp4_select_kernel<T, D, 2>, grid, kFsThreads, smem_of(2), stream, a, tile_tokens, capacity);
   }
-  if ((e = cudaGetLastError()) != cudaSuccess || parts == 1) return e;
+  if (e != cudaSuccess || parts == 1) return e;
   const int merge_capacity = capacity_of(1, K, K, (long long)parts * K);
   static std::atomic<unsigned long long> done_merge{0};
   if ((e = allow_smem(fp4_select_merge_kernel, kFsEntries * 8 + 32 * 8, &done_merge)) != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)heads);
-  cfg.blockDim = dim3(kFsThreads);
-  cfg.dynamicSmemBytes = (size_t)merge_capacity * 8;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, fp4_select_merge_kernel, a, parts, merge_capacity);
+  return launch_early(fp4_select_merge_kernel, dim3((unsigned)heads), kFsThreads, (size_t)merge_capacity * 8, stream, a, parts, merge_capacity);
 }
 
 }  // namespace
