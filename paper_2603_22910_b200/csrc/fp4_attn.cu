@@ -6,7 +6,7 @@
 // The blocks are read once from HBM and that is the bound; beside the stream every value has to be turned into fp16, 41 of them per
 // clock and SM.  The design:
 //
-//   work     A unit is one 16-token block of one KV head for one tile of 8 query rows (the query heads that share the KV head, times a
+//   work     A unit is one 16-token block of one KV head for 8 or 16 query rows (the query heads that share the KV head, times a
 //            sequence's new tokens).  The units of all sequences are laid end to end and cut into equal shares, one per CTA and
 //            within it one per warp, computed on the device from the lengths.  A share cuts at most two (sequence, head) items;
 //            their partial results (running maximum, sum, output) are combined inside the CTA through shared memory and between CTAs by a
@@ -27,14 +27,15 @@ namespace echokv {
 
 namespace {
 
-// (heads of 128: 12 warps 119.5 us for 16 x 32768 keys, 14 134, 16 121; of 64, 16 x 8192 keys of 32 heads: 12 89, 16 79)
-template <int D>
+// Q tiles of 8 query rows make up an item: 1, or 2 where a call may have more rows than one tile has (their values are then converted once).
+// (Heads of 128, one tile: 12 warps 119.5 us for 16 x 32768 keys, 14 134, 16 121; of 64, 16 x 8192 keys of 32 heads: 12 89, 16 79.)
+template <int D, int Q>
 struct FqShape {
-  static constexpr int kWarps = D == 128 ? 12 : 16, kThreads = kWarps * 32;
+  static constexpr int kWarps = Q == 2 ? (D == 128 ? 8 : 12) : D == 128 ? 12 : 16, kThreads = kWarps * 32;
+  static constexpr int kRows = 8 * Q;
 };
-constexpr int kFqRows = 8;                        // query rows per tile
+constexpr int kFqTile = 8;                        // query rows per tile
 constexpr int kFqStages = 3;                      // of two blocks each
-constexpr int kFqMergeThreads = kFqRows * 32;
 constexpr int kFqMaxCtas = 512;
 constexpr int kFqItemCost = 6;                    // what an item costs beside its blocks (queries, first copies, result), in blocks
 constexpr float kFqBelow = 5.f;                   // the reference stands 2^5 below the largest score it was taken from,
@@ -50,29 +51,29 @@ struct FqPlanShared {
   int4 info[THREADS];                             // slot, length, first token, tokens (0: nothing to do) of the owners
 };
 
-template <int D>
+template <int D, int Q>
 struct FqSmem {
   // a warp's segment that goes on from the warp before it, and (over the warp's ring, once that is at rest) the one
   // that goes on in the next warp
-  static constexpr int kWarps = FqShape<D>::kWarps;
-  float o_first[kWarps][kFqRows][D];
+  static constexpr int kWarps = FqShape<D, Q>::kWarps, kRows = FqShape<D, Q>::kRows;
+  float o_first[kWarps][kRows][D];
   QaSeg seg[2 * kWarps];
-  float m[2 * kWarps][kFqRows], l[2 * kWarps][kFqRows];
+  float m[2 * kWarps][kRows], l[2 * kWarps][kRows];
   unsigned long long full[kWarps][kFqStages];
-  FqPlanShared<FqShape<D>::kThreads> plan;
+  FqPlanShared<FqShape<D, Q>::kThreads> plan;
   int2 tok[kWarps][kFqStages];                  // with lists: first tokens of a stage's blocks
 };
-template <int D>
-__host__ __device__ constexpr size_t fq_ring_bytes() { return (size_t)FqShape<D>::kWarps * kFqStages * fq_stage_bytes(D); }
+template <int D, int Q>
+__host__ __device__ constexpr size_t fq_ring_bytes() { return (size_t)FqShape<D, Q>::kWarps * kFqStages * fq_stage_bytes(D); }
 
-// workspace: [ctas][2][8] (m, l) | [ctas][2][8][D] o
-template <int D>
+// workspace: [ctas][2][rows] (m, l) | [ctas][2][rows][D] o
+template <int ROWS>
 struct FqWork {
   float2* ml;
   float* o;
   __host__ __device__ explicit FqWork(unsigned char* ws) {
     ml = reinterpret_cast<float2*>(ws);
-    o = reinterpret_cast<float*>(ws + kFqMaxCtas * 2 * kFqRows * sizeof(float2));
+    o = reinterpret_cast<float*>(ws + kFqMaxCtas * 2 * ROWS * sizeof(float2));
   }
 };
 
@@ -108,20 +109,21 @@ __device__ __forceinline__ int4 owner_info(const Fp4AttnArgs& a, int b, bool tel
   if (s.error && tell) report_opt(a.status, s.error);
   return make_int4(s.slot, s.len, s.first, s.error || (without && many_rows(a, s)) ? 0 : s.n);
 }
-__device__ __forceinline__ int row_tiles(const QuantAttnArgs& a, int n) { return (n * a.group + kFqRows - 1) / kFqRows; }
+template <int ROWS>
+__device__ __forceinline__ int row_items(const QuantAttnArgs& a, int n) { return (n * a.group + ROWS - 1) / ROWS; }
 template <bool LIST>
 __device__ __forceinline__ int blocks_of(const Fp4AttnArgs& a, int len) {
   if (LIST) return min(a.t.n_select, ((len - 1) >> a.g.page_shift) + 1) << (a.g.page_shift - 4);
   return (len + kQuantBlock - 1) / kQuantBlock;
 }
-template <bool LIST>
+template <bool LIST, int ROWS>
 __device__ __forceinline__ unsigned long long units_of(const Fp4AttnArgs& a, const int4& s) {
-  return s.w == 0 ? 0 : (unsigned long long)row_tiles(a, s.w) * a.g.n_kv_heads * (blocks_of<LIST>(a, s.y) + kFqItemCost);
+  return s.w == 0 ? 0 : (unsigned long long)row_items<ROWS>(a, s.w) * a.g.n_kv_heads * (blocks_of<LIST>(a, s.y) + kFqItemCost);
 }
 
 // How the work of a call is cut: every block of either kernel works it out from the lengths.  Up to 32 owners: a lane of every warp has
 // one, and no thread waits for another; more: a thread has a run of them.
-template <bool LIST, int THREADS>
+template <bool LIST, int THREADS, int ROWS>
 struct FqPlan {
   const Fp4AttnArgs& a;
   FqPlanShared<THREADS>& sm;
@@ -144,13 +146,13 @@ struct FqPlan {
     if (few) {
       mine = make_int4(0, 0, 0, 0);
       if (lane < n_own) mine = owner_info<LIST>(a, lane, tell && warp == 0, without);
-      n = units_of<LIST>(a, mine);
+      n = units_of<LIST, ROWS>(a, mine);
     } else {
 #pragma unroll 1
       for (int k = tid * per; k < min(n_own, (tid + 1) * per); ++k) {
         const int4 s = owner_info<LIST>(a, k, tell, without);
         if (per == 1) sm.info[k] = s;
-        n += units_of<LIST>(a, s);
+        n += units_of<LIST, ROWS>(a, s);
       }
     }
     unsigned long long x = n;
@@ -194,7 +196,7 @@ struct FqPlan {
     b = at * per;
     base = sm.pre[at];
     info = info_of(b);
-    for (unsigned long long n = units_of<LIST>(a, info); base + n <= u; n = units_of<LIST>(a, info)) {
+    for (unsigned long long n = units_of<LIST, ROWS>(a, info); base + n <= u; n = units_of<LIST, ROWS>(a, info)) {
       base += n;
       info = info_of(++b);
     }
@@ -205,11 +207,11 @@ struct FqItem {
   int n_blk, h, tile;
   unsigned long long first, end;                  // its units: kFqItemCost, then one per block
 };
-template <bool LIST, int THREADS>
-__device__ __forceinline__ FqItem item_of(const FqPlan<LIST, THREADS>& p, unsigned long long u) {
+template <bool LIST, int THREADS, int ROWS>
+__device__ __forceinline__ FqItem item_of(const FqPlan<LIST, THREADS, ROWS>& p, unsigned long long u) {
   FqItem it;
   it.n_blk = blocks_of<LIST>(p.a, p.info.y);
-  const int tiles = row_tiles(p.a, p.info.w), n = it.n_blk + kFqItemCost;
+  const int tiles = row_items<ROWS>(p.a, p.info.w), n = it.n_blk + kFqItemCost;
   const unsigned long long rem = u - p.base;
   const int ht = (int)quotient(rem, n);
   it.h = tiles == 1 ? ht : ht / tiles;
@@ -219,9 +221,10 @@ __device__ __forceinline__ FqItem item_of(const FqPlan<LIST, THREADS>& p, unsign
   return it;
 }
 
-template <typename T, int D, bool LIST>
-__global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const __grid_constant__ Fp4AttnArgs a) {
-  constexpr int kFqWarps = FqShape<D>::kWarps, kFqThreads = FqShape<D>::kThreads, kFqMinShare = 2 * kFqWarps;      // (units of a CTA at least)
+template <typename T, int D, bool LIST, int Q>
+__global__ void __launch_bounds__(FqShape<D, Q>::kThreads, 1) fp4_attn_kernel(const __grid_constant__ Fp4AttnArgs a) {
+  constexpr int kFqWarps = FqShape<D, Q>::kWarps, kFqThreads = FqShape<D, Q>::kThreads, kRows = FqShape<D, Q>::kRows;
+  constexpr int kFqMinShare = 2 * kFqWarps;       // units of a CTA at least
   constexpr int KC = D / 64;                      // groups of a key row per lane
   constexpr int KS = D / 16;                      // k-steps of q . k
   constexpr int NT = D / 8;                       // features of the output per lane (NT r .. NT r + NT - 1)
@@ -230,12 +233,12 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
   constexpr int NB = 2;                           // blocks of a step
   constexpr bool kF32 = sizeof(T) == 4;
   extern __shared__ __align__(1024) unsigned char fq_raw[];
-  FqSmem<D>& sm = *reinterpret_cast<FqSmem<D>*>(fq_raw + fq_ring_bytes<D>());
+  FqSmem<D, Q>& sm = *reinterpret_cast<FqSmem<D, Q>*>(fq_raw + fq_ring_bytes<D, Q>());
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
   const uint32_t ring = smem_u32(fq_raw) + warp * kFqStages * fq_stage_bytes(D);
   const QuantGeom& g = a.g;
   const int H = g.n_kv_heads;
-  // output rows [8][D] of segment `at`
+  // output rows [rows][D] of segment `at`
   const auto seg_rows = [&](int at) -> float* {
     return at & 1 ? reinterpret_cast<float*>(fq_raw + (size_t)(at >> 1) * kFqStages * fq_stage_bytes(D)) : &sm.o_first[at >> 1][0][0];
   };
@@ -249,7 +252,7 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
   after_the_one_before();
   let_the_next_one_come();                        // (the second kernel reads what this one does, and waits for its end)
   // ---- this CTA's and warp's share of the call's units
-  FqPlan<LIST, kFqThreads> plan(a, sm.plan, gridDim.x, kFqMinShare, blockIdx.x == 0);
+  FqPlan<LIST, kFqThreads, kRows> plan(a, sm.plan, gridDim.x, kFqMinShare, blockIdx.x == 0);
   const unsigned long long total = plan.total, share = plan.share;
   const unsigned long long cta0 = min(total, share * blockIdx.x), cta1 = min(total, cta0 + share);
   const unsigned long long wshare = quotient(cta1 - cta0 + kFqWarps - 1, kFqWarps);
@@ -310,21 +313,24 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
       return p;
     };
     Place cur = look_up(0);
-    // ---- the query rows: this lane loads a quarter of row r as operand; its scores are of rows 2 c and 2 c + 1
-    const int n_rows = n_new * a.group;
+    // ---- the query rows: this lane loads a quarter of row r of every tile as operand; its scores are of rows 2 c and 2 c + 1
+    const int n_rows = n_new * a.group, row0 = tile * kRows;
     // up to four rows stand in the even columns, so that a lane's second column is nobody's and costs nothing
-    const bool spread = n_rows - tile * kFqRows <= 4;
-    uint32_t qh[KS][2], ql[kF32 ? KS : 1][2];
-    float c_row[2];
-    const int qrow_r = tile * kFqRows + (spread ? r >> 1 : r);
-    const bool ok = qrow_r < n_rows && !(spread && (r & 1));
-    const T* qp = static_cast<const T*>(a.q) + (long long)(first_token + (ok ? qrow_r >> a.group_shift : 0)) * a.q_stride +
-                  (long long)(h * a.group + (qrow_r & (a.group - 1))) * D;
-    Quad<T> qv[KS];
+    const bool spread = n_rows - row0 <= 4, two_tiles = Q == 2 && n_rows - row0 > kFqTile;
+    uint32_t qh[Q][KS][2], ql[kF32 ? KS : 1][2];
+    float c_row[Q][2];
+    Quad<T> qv[Q][KS];
 #pragma unroll
-    for (int x = 0; x < KS; x += Quad<T>::kPerLoad)
-      if (ok) Quad<T>::load16(qp + KC * 16 * c + 4 * x, &qv[x]);
-      else Quad<T>::zero16(&qv[x]);
+    for (int q = 0; q < Q; ++q) {
+      const int qrow_r = row0 + q * kFqTile + (spread ? r >> 1 : r);
+      const bool ok = qrow_r < n_rows && !(spread && (r & 1));
+      const T* qp = static_cast<const T*>(a.q) + (long long)(first_token + (ok ? qrow_r >> a.group_shift : 0)) * a.q_stride +
+                    (long long)(h * a.group + (qrow_r & (a.group - 1))) * D;
+#pragma unroll
+      for (int x = 0; x < KS; x += Quad<T>::kPerLoad)
+        if (ok) Quad<T>::load16(qp + KC * 16 * c + 4 * x, &qv[q][x]);
+        else Quad<T>::zero16(&qv[q][x]);
+    }
     Place next = {0, kFqNowhere};
     const int n_steps = (nb + NB - 1) / NB;
     int left = 0;                                  // stages asked for and not yet taken
@@ -355,11 +361,12 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
     while (asked < min(kFqStages, n_steps)) issue();
     next = look_up(1);                             // (not needed before the sixteenth step)
 
-    {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
       // (magnitudes compare as integers; an infinity or NaN gives the factor 1 and goes on through the products)
       uint32_t bits = 0;
 #pragma unroll
-      for (int x = 0; x < KS; ++x) bits = qv[x].top(bits);
+      for (int x = 0; x < KS; ++x) bits = qv[q][x].top(bits);
       bits = Quad<T>::top_bits(bits);
       bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 1));
       bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 2));
@@ -368,48 +375,60 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
       const float up = scale_up_to_half(top, &back);
 #pragma unroll
       for (int e = 0; e < 2; ++e)
-        c_row[e] = __shfl_sync(0xffffffffu, back, 4 * (2 * c + e)) * a.scale * (a.softcap > 0.f ? 1.f : kLog2e);
+        c_row[q][e] = __shfl_sync(0xffffffffu, back, 4 * (2 * c + e)) * a.scale * (a.softcap > 0.f ? 1.f : kLog2e);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
-          const HalfPair p = split_pair<kF32>(qv[ks].get(2 * f) * up, qv[ks].get(2 * f + 1) * up);
-          qh[ks][f] = p.hi;
+          const HalfPair p = split_pair<kF32>(qv[q][ks].get(2 * f) * up, qv[q][ks].get(2 * f + 1) * up);
+          qh[q][ks][f] = p.hi;
           if (kF32) ql[ks][f] = p.lo;
         }
     }
     const int prefix = !LIST && a.prefix ? a.prefix[b] : 0;
-    int pos[2], row_of[2];                        // (row_of: 8 where the column is nobody's)
-    float slope2[2];
+    int pos[Q][2], row_of[Q][2];                  // (row_of: -1 where the column is nobody's)
+    float slope2[Q][2];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      row_of[e] = spread ? (e == 0 ? c : kFqRows) : 2 * c + e;
-      const int qrow = tile * kFqRows + (row_of[e] & (kFqRows - 1));
-      pos[e] = len - n_new + (qrow < n_rows ? qrow >> a.group_shift : 0);
-      slope2[e] = a.slopes ? a.slopes[h * a.group + (qrow & (a.group - 1))] * kLog2e : 0.f;
-    }
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        row_of[q][e] = spread ? (q == 0 && e == 0 ? c : -1) : q * kFqTile + 2 * c + e;
+        const int qrow = row0 + max(row_of[q][e], 0);
+        pos[q][e] = len - n_new + (qrow < n_rows ? qrow >> a.group_shift : 0);
+        slope2[q][e] = a.slopes ? a.slopes[h * a.group + (qrow & (a.group - 1))] * kLog2e : 0.f;
+      }
 
-    float o[MT][4];                               // rows: feature NT r + 2 j (0, 1) and + 1 (2, 3); columns: query rows 2 c, 2 c + 1
+    float o[Q][MT][4];                            // rows: feature NT r + 2 j (0, 1) and + 1 (2, 3); columns: query rows 2 c, 2 c + 1
 #pragma unroll
-    for (int j = 0; j < MT; ++j)
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
-      for (int f = 0; f < 4; ++f) o[j][f] = 0.f;
+      for (int j = 0; j < MT; ++j)
+#pragma unroll
+        for (int f = 0; f < 4; ++f) o[q][j][f] = 0.f;
     // Per query row: the reference of its maximum (0 until it has seen a key, which the first one seen moves), and how far
     // above the reference a score may be before that moves.
-    float m_ref[2] = {0.f, 0.f}, grow[2] = {-3.0e38f, -3.0e38f}, l_run[2] = {0.f, 0.f};
-    const int pos_first = len - n_new + (tile * kFqRows >> a.group_shift);     // the tile's first query: blocks up to it are seen whole
+    float m_ref[Q][2], grow[Q][2], l_run[Q][2];
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        m_ref[q][e] = l_run[q][e] = 0.f;
+        grow[q][e] = -3.0e38f;
+      }
+    const int pos_first = len - n_new + (row0 >> a.group_shift);               // the item's first query: blocks up to it are seen whole
 
-    // a scaled product q . k of token tok and query row 2 c + e -> the score in base-2 units
-    const auto score = [&](float y, int e, int tok) {
+    // a scaled product q . k of token tok and a query row -> the score in base-2 units
+    const auto score = [&](float y, int at, float slope, int tok) {
       if (a.softcap > 0.f) y = cap_out * tanh_f32(y * cap_in);
-      if (a.slopes) y -= slope2[e] * fabsf((float)(pos[e] - tok));
+      if (a.slopes) y -= slope * fabsf((float)(at - tok));
       return y;
     };
 
     // One step: two blocks of the stage that has arrived.  MASKED: some of their tokens may be unseen, or the second block is not there.
-    const auto attend = [&](auto masked_tag, auto spread_tag, int step, uint32_t src) {
+    const auto attend = [&](auto masked_tag, auto spread_tag, auto tiles_tag, int step, uint32_t src) {
       constexpr bool MASKED = decltype(masked_tag)::value;
       constexpr int E = decltype(spread_tag)::value ? 1 : 2;      // columns of a lane that are anybody's
+      constexpr int L = decltype(tiles_tag)::value;               // tiles that have a row
       int tok0[NB];
       if (LIST) {
         const int2 t = sm.tok[warp][take];
@@ -421,7 +440,7 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
       }
       const bool two = !MASKED || step * NB + 1 < nb;
       if (!two) tok0[1] = kFqNowhere;              // (the first block stands in for it)
-      const auto seen = [&](int tok, int e) { return tok <= pos[e] || (!LIST && tok < prefix); };
+      const auto seen = [&](int tok, int at) { return tok <= at || (!LIST && tok < prefix); };
       const uint32_t part[NB] = {src, two ? src + BB : src};
 
       // ---- the values' codes and scales (used last: on their way while the scores are worked out)
@@ -444,7 +463,7 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
         }
 
       // ---- scores
-      float sc[NB][4];                            // [n][2 t + e]: token r + 8 t of block n, query row 2 c + e
+      float sc[L][NB][4];                         // [tile][n][2 t + e]: token r + 8 t of block n, query row 2 c + e
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         uint32_t kw[2][2 * KC], ks[2][KC];
@@ -470,9 +489,11 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
         }
         // two chains of products.  (fp32: the tensor core cuts its sums off where it adds to them, 2^-23 of the sum each time and always
         // towards 0, so a word's products are summed by themselves and the low-order halves' apart.)
-        float sb[4] = {0.f, 0.f, 0.f, 0.f};
+        float sb[L][4];
 #pragma unroll
-        for (int f = 0; f < 4; ++f) sc[n][f] = 0.f;
+        for (int q = 0; q < L; ++q)
+#pragma unroll
+          for (int f = 0; f < 4; ++f) sb[q][f] = sc[q][n][f] = 0.f;
 #pragma unroll
         for (int w = 0; w < 2 * KC; ++w) {
           uint32_t x[2][4];
@@ -486,81 +507,99 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
             float hi[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-              mma_m16n8k16_f16(hi, x[0][2 * s], x[1][2 * s], x[0][2 * s + 1], x[1][2 * s + 1], qh[2 * w + s][0], qh[2 * w + s][1]);
-              mma_m16n8k16_f16(sb, x[0][2 * s], x[1][2 * s], x[0][2 * s + 1], x[1][2 * s + 1], ql[2 * w + s][0], ql[2 * w + s][1]);
+              mma_m16n8k16_f16(hi, x[0][2 * s], x[1][2 * s], x[0][2 * s + 1], x[1][2 * s + 1], qh[0][2 * w + s][0], qh[0][2 * w + s][1]);
+              mma_m16n8k16_f16(sb[0], x[0][2 * s], x[1][2 * s], x[0][2 * s + 1], x[1][2 * s + 1], ql[2 * w + s][0], ql[2 * w + s][1]);
             }
 #pragma unroll
-            for (int f = 0; f < 4; ++f) sc[n][f] += hi[f];
+            for (int f = 0; f < 4; ++f) sc[0][n][f] += hi[f];
           } else {
-            mma_m16n8k16_f16(sc[n], x[0][0], x[1][0], x[0][1], x[1][1], qh[2 * w][0], qh[2 * w][1]);
-            mma_m16n8k16_f16(sb, x[0][2], x[1][2], x[0][3], x[1][3], qh[2 * w + 1][0], qh[2 * w + 1][1]);
+#pragma unroll
+            for (int q = 0; q < L; ++q) {
+              mma_m16n8k16_f16(sc[q][n], x[0][0], x[1][0], x[0][1], x[1][1], qh[q][2 * w][0], qh[q][2 * w][1]);
+              mma_m16n8k16_f16(sb[q], x[0][2], x[1][2], x[0][3], x[1][3], qh[q][2 * w + 1][0], qh[q][2 * w + 1][1]);
+            }
           }
         }
 #pragma unroll
-        for (int f = 0; f < 4; ++f) sc[n][f] += sb[f];
+        for (int q = 0; q < L; ++q)
+#pragma unroll
+          for (int f = 0; f < 4; ++f) sc[q][n][f] += sb[q][f];
       }
 
-      // ---- probabilities as operands (ph[n][t]: query row r, tokens 8 t + 2 c, + 1), the reference moved if needed
-      float most[2] = {-INFINITY, -INFINITY};
+      // ---- probabilities as operands (ph[tile][n][t]: query row r, tokens 8 t + 2 c, + 1), the references moved if needed
+      float most[L][2];
+      bool above = false;
 #pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        if (plain) {
+      for (int q = 0; q < L; ++q) {
+        most[q][0] = most[q][1] = -INFINITY;
 #pragma unroll
-          for (int i = 0; i < 4; i += 3 - E) sc[n][i] = fmaf(sc[n][i], c_row[i & 1], -m_ref[i & 1]);
-        } else {
+        for (int n = 0; n < NB; ++n) {
+          if (plain) {
 #pragma unroll
-          for (int i = 0; i < 4; i += 3 - E) sc[n][i] = score(sc[n][i] * c_row[i & 1], i & 1, tok0[n] + 8 * (i >> 1) + r) - m_ref[i & 1];
+            for (int i = 0; i < 4; i += 3 - E) sc[q][n][i] = fmaf(sc[q][n][i], c_row[q][i & 1], -m_ref[q][i & 1]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; i += 3 - E)
+              sc[q][n][i] = score(sc[q][n][i] * c_row[q][i & 1], pos[q][i & 1], slope2[q][i & 1], tok0[n] + 8 * (i >> 1) + r) - m_ref[q][i & 1];
+          }
+          if (MASKED) {
+#pragma unroll
+            for (int i = 0; i < 4; i += 3 - E)
+              if (!seen(tok0[n] + 8 * (i >> 1) + r, pos[q][i & 1])) sc[q][n][i] = -INFINITY;
+          }
+#pragma unroll
+          for (int e = 0; e < E; ++e) most[q][e] = fmaxf(most[q][e], fmaxf(sc[q][n][e], sc[q][n][2 + e]));
         }
-        if (MASKED) {
 #pragma unroll
-          for (int i = 0; i < 4; i += 3 - E)
-            if (!seen(tok0[n] + 8 * (i >> 1) + r, i & 1)) sc[n][i] = -INFINITY;
-        }
-#pragma unroll
-        for (int e = 0; e < E; ++e) most[e] = fmaxf(most[e], fmaxf(sc[n][e], sc[n][2 + e]));
+        for (int e = 0; e < E; ++e) above |= most[q][e] > grow[q][e];
       }
-      if (__any_sync(0xffffffffu, most[0] > grow[0] || (E == 2 && most[1] > grow[1]))) {
-        float alpha[2] = {1.f, 1.f};
+      if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          float mx = most[e];
+        for (int q = 0; q < L; ++q) {
+          float alpha[2] = {1.f, 1.f};
 #pragma unroll
-          for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-          mx -= kFqBelow;
-          const bool first = grow[e] != kFqGrow;         // nothing seen so far: sum and output are still 0
-          if (mx > (first ? -INFINITY : 0.f)) {
-            if (!first) alpha[e] = exp2_approx(-mx);
-            grow[e] = kFqGrow;
-            m_ref[e] += mx;
-            l_run[e] *= alpha[e];
+          for (int e = 0; e < E; ++e) {
+            float mx = most[q][e];
 #pragma unroll
-            for (int n = 0; n < NB; ++n) {
-              sc[n][e] -= mx;
-              sc[n][2 + e] -= mx;
+            for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+            mx -= kFqBelow;
+            const bool first = grow[q][e] != kFqGrow;    // nothing seen so far: sum and output are still 0
+            if (mx > (first ? -INFINITY : 0.f)) {
+              if (!first) alpha[e] = exp2_approx(-mx);
+              grow[q][e] = kFqGrow;
+              m_ref[q][e] += mx;
+              l_run[q][e] *= alpha[e];
+#pragma unroll
+              for (int n = 0; n < NB; ++n) {
+                sc[q][n][e] -= mx;
+                sc[q][n][2 + e] -= mx;
+              }
             }
           }
-        }
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+          for (int m = 0; m < MT; ++m)
 #pragma unroll
-          for (int f = 0; f < 4; f += 3 - E) o[m][f] *= alpha[f & 1];
-      }
-      uint32_t ph[NB][2], pl[NB][2];
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        float p[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < 4; i += 3 - E) {
-          p[i] = exp2_approx(sc[n][i]);
-          l_run[i & 1] += p[i];
-        }
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const HalfPair w = split_pair<kF32>(p[2 * t], p[2 * t + 1]);
-          ph[n][t] = movm(w.hi);
-          if (kF32) pl[n][t] = movm(w.lo);
+            for (int f = 0; f < 4; f += 3 - E) o[q][m][f] *= alpha[f & 1];
         }
       }
+      uint32_t ph[L][NB][2], pl[NB][2];
+#pragma unroll
+      for (int q = 0; q < L; ++q)
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          float p[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < 4; i += 3 - E) {
+            p[i] = exp2_approx(sc[q][n][i]);
+            l_run[q][i & 1] += p[i];
+          }
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const HalfPair w = split_pair<kF32>(p[2 * t], p[2 * t + 1]);
+            ph[q][n][t] = movm(w.hi);
+            if (kF32) pl[n][t] = movm(w.lo);
+          }
+        }
 
       // ---- output (fp32: the step's products are summed by themselves, as above)
       float step_o[kF32 ? MT : 1][4];
@@ -596,18 +635,20 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
             }
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float (&acc)[4] = kF32 ? step_o[kF32 ? 4 * w + i : 0] : o[4 * w + i];
-            mma_m16n8k16_f16(acc, x[0][i], y[0][i], x[1][i], y[1][i], ph[n][0], ph[n][1]);
-            if (kF32) mma_m16n8k16_f16(acc, x[0][i], y[0][i], x[1][i], y[1][i], pl[n][0], pl[n][1]);
-          }
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int q = 0; q < L; ++q) {
+              float (&acc)[4] = kF32 ? step_o[kF32 ? 4 * w + i : 0] : o[q][4 * w + i];
+              mma_m16n8k16_f16(acc, x[0][i], y[0][i], x[1][i], y[1][i], ph[q][n][0], ph[q][n][1]);
+              if (kF32) mma_m16n8k16_f16(acc, x[0][i], y[0][i], x[1][i], y[1][i], pl[n][0], pl[n][1]);
+            }
         }
       }
       if (kF32) {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-          for (int f = 0; f < 4; ++f) o[m][f] += step_o[kF32 ? m : 0][f];
+          for (int f = 0; f < 4; ++f) o[0][m][f] += step_o[kF32 ? m : 0][f];
       }
     };
 #pragma unroll 1
@@ -624,10 +665,14 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
         masked = (blk0 + (step + 1) * NB) * kQuantBlock - 1 > pos_first || step * NB + 1 >= nb;
       }
       const uint32_t src = ring + take * fq_stage_bytes(D);
+      const std::integral_constant<int, 1> one;
       if (spread) {
-        if (masked) attend(std::true_type(), std::true_type(), step, src); else attend(std::false_type(), std::true_type(), step, src);
-      } else {
-        if (masked) attend(std::true_type(), std::false_type(), step, src); else attend(std::false_type(), std::false_type(), step, src);
+        if (masked) attend(std::true_type(), std::true_type(), one, step, src); else attend(std::false_type(), std::true_type(), one, step, src);
+      } else if (!two_tiles) {
+        if (masked) attend(std::true_type(), std::false_type(), one, step, src); else attend(std::false_type(), std::false_type(), one, step, src);
+      } else if constexpr (Q == 2) {
+        const std::integral_constant<int, 2> two;
+        if (masked) attend(std::true_type(), std::false_type(), two, step, src); else attend(std::false_type(), std::false_type(), two, step, src);
       }
       __syncwarp();                                // (all lanes have read the stage: it may be overwritten)
       if (++take == kFqStages) {
@@ -654,28 +699,32 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
 
     // ---- the segment's result
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
-      for (int w = 4; w < 32; w <<= 1) l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], w);
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int w = 4; w < 32; w <<= 1) l_run[q][e] += __shfl_xor_sync(0xffffffffu, l_run[q][e], w);
     const bool starts = blk0 == 0, ends = seg_end == item_end;
     if (starts && ends) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int qrow = tile * kFqRows + row_of[e];
-        if (row_of[e] < kFqRows && qrow < n_rows) {
-          const float inv = l_run[e] == 0.f ? 0.f : out_scale / l_run[e];
-          float v[NT];
+      for (int q = 0; q < Q; ++q)
 #pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            v[2 * m] = o[m][e] * inv;
-            v[2 * m + 1] = o[m][2 + e] * inv;
+        for (int e = 0; e < 2; ++e) {
+          const int qrow = row0 + row_of[q][e];
+          if (row_of[q][e] >= 0 && qrow < n_rows) {
+            const float inv = l_run[q][e] == 0.f ? 0.f : out_scale / l_run[q][e];
+            float v[NT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+              v[2 * m] = o[q][m][e] * inv;
+              v[2 * m + 1] = o[q][m][2 + e] * inv;
+            }
+            T* dst = static_cast<T*>(a.out) +
+                     ((long long)(first_token + (qrow >> a.group_shift)) * a.n_q_heads + h * a.group + (qrow & (a.group - 1))) * D + NT * r;
+#pragma unroll
+            for (int f = 0; f < NT; f += Vec16<T>::N) store16<T>(dst + f, v + f);
           }
-          T* dst = static_cast<T*>(a.out) +
-                   ((long long)(first_token + (qrow >> a.group_shift)) * a.n_q_heads + h * a.group + (qrow & (a.group - 1))) * D + NT * r;
-#pragma unroll
-          for (int f = 0; f < NT; f += Vec16<T>::N) store16<T>(dst + f, v + f);
         }
-      }
     } else {
       const int at = 2 * warp + (starts ? 1 : 0);
       if (lane == 0) {
@@ -688,19 +737,23 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
       float* dst = seg_rows(at);
       if (r == 0) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          if (row_of[e] == kFqRows) continue;
-          sm.m[at][row_of[e]] = l_run[e] == 0.f ? -INFINITY : m_ref[e];
-          sm.l[at][row_of[e]] = l_run[e];
-        }
+        for (int q = 0; q < Q; ++q)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            if (row_of[q][e] < 0) continue;
+            sm.m[at][row_of[q][e]] = l_run[q][e] == 0.f ? -INFINITY : m_ref[q][e];
+            sm.l[at][row_of[q][e]] = l_run[q][e];
+          }
       }
       __syncwarp();                               // (the rows of the second kind lie over the ring)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        if (row_of[e] == kFqRows) continue;
+      for (int q = 0; q < Q; ++q)
 #pragma unroll
-        for (int m = 0; m < MT; ++m) *reinterpret_cast<float2*>(dst + row_of[e] * D + NT * r + 2 * m) = make_float2(o[m][e], o[m][2 + e]);
-      }
+        for (int e = 0; e < 2; ++e) {
+          if (row_of[q][e] < 0) continue;
+#pragma unroll
+          for (int m = 0; m < MT; ++m) *reinterpret_cast<float2*>(dst + row_of[q][e] * D + NT * r + 2 * m) = make_float2(o[q][m][e], o[q][m][2 + e]);
+        }
     }
     u = seg_end;
   }
@@ -708,48 +761,50 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
   // ---- segments of one item side by side in this CTA: combine them; what is still cut goes to the workspace.  A warp per query
   //      row; lane k looks at segment k.
   __syncthreads();
-  if (warp >= kFqRows) return;
-  const FqWork<D> ws(a.ws);
+  const FqWork<kRows> ws(a.ws);
   constexpr int E = D / 32;
   static_assert(2 * kFqWarps <= 32, "a lane per segment");
   const bool is_seg = lane < 2 * kFqWarps && sm.seg[lane < 2 * kFqWarps ? lane : 0].valid;
   const unsigned long long my_item = is_seg ? sm.seg[lane].item : ~0ull;
-  const float my_m = is_seg ? sm.m[lane][warp] : -INFINITY, my_l = is_seg ? sm.l[lane][warp] : 0.f;
-  uint32_t todo = __ballot_sync(0xffffffffu, is_seg);
-  while (todo) {
-    const int i = __ffs(todo) - 1;
-    const uint32_t mine = __ballot_sync(0xffffffffu, my_item == __shfl_sync(0xffffffffu, my_item, i)) & todo;
-    todo &= ~mine;
-    const QaSeg& first = sm.seg[i];
-    const bool starts = first.starts, ends = sm.seg[31 - __clz(mine)].ends;
-    const bool in = (mine >> lane) & 1;
-    const float m = warp_max(in ? my_m : -INFINITY);
-    // (a row that has seen nothing has the sum 0 -- or NaN)
-    const float w = !in || my_l == 0.f ? 0.f : exp2_approx(my_m - m);
-    const float l = warp_sum(in ? w * my_l : 0.f);
-    float acc[E] = {};
-    for (uint32_t left = mine; left; left &= left - 1) {
-      const int k = __ffs(left) - 1;
-      const float wk = __shfl_sync(0xffffffffu, w, k);
-      const float* o = seg_rows(k) + warp * D + lane * E;
+#pragma unroll 1
+  for (int row = warp; row < kRows; row += kFqWarps) {
+    const float my_m = is_seg ? sm.m[lane][row] : -INFINITY, my_l = is_seg ? sm.l[lane][row] : 0.f;
+    uint32_t todo = __ballot_sync(0xffffffffu, is_seg);
+    while (todo) {
+      const int i = __ffs(todo) - 1;
+      const uint32_t mine = __ballot_sync(0xffffffffu, my_item == __shfl_sync(0xffffffffu, my_item, i)) & todo;
+      todo &= ~mine;
+      const QaSeg& first = sm.seg[i];
+      const bool starts = first.starts, ends = sm.seg[31 - __clz(mine)].ends;
+      const bool in = (mine >> lane) & 1;
+      const float m = warp_max(in ? my_m : -INFINITY);
+      // (a row that has seen nothing has the sum 0 -- or NaN)
+      const float w = !in || my_l == 0.f ? 0.f : exp2_approx(my_m - m);
+      const float l = warp_sum(in ? w * my_l : 0.f);
+      float acc[E] = {};
+      for (uint32_t left = mine; left; left &= left - 1) {
+        const int k = __ffs(left) - 1;
+        const float wk = __shfl_sync(0xffffffffu, w, k);
+        const float* o = seg_rows(k) + row * D + lane * E;
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] += wk * o[e];
-    }
-    if (starts && ends) {
-      const int4 s = plan.info_of(first.b);
-      const int qrow = first.tile * kFqRows + warp;
-      if (qrow < s.w * a.group) {
-        const float inv = l == 0.f ? 0.f : out_scale / l;
-        T* dst = static_cast<T*>(a.out) +
-                 ((long long)(s.z + (qrow >> a.group_shift)) * a.n_q_heads + first.h * a.group + (qrow & (a.group - 1))) * D + lane * E;
-#pragma unroll
-        for (int e = 0; e < E; ++e) dst[e] = from_f32<T>(acc[e] * inv);
+        for (int e = 0; e < E; ++e) acc[e] += wk * o[e];
       }
-    } else {
-      const long long p = ((long long)blockIdx.x * 2 + (starts ? 1 : 0)) * kFqRows + warp;
-      if (lane == 0) ws.ml[p] = make_float2(m, l);
+      if (starts && ends) {
+        const int4 s = plan.info_of(first.b);
+        const int qrow = first.tile * kRows + row;
+        if (qrow < s.w * a.group) {
+          const float inv = l == 0.f ? 0.f : out_scale / l;
+          T* dst = static_cast<T*>(a.out) +
+                   ((long long)(s.z + (qrow >> a.group_shift)) * a.n_q_heads + first.h * a.group + (qrow & (a.group - 1))) * D + lane * E;
 #pragma unroll
-      for (int e = 0; e < E; ++e) ws.o[p * D + lane * E + e] = acc[e];
+          for (int e = 0; e < E; ++e) dst[e] = from_f32<T>(acc[e] * inv);
+        }
+      } else {
+        const long long p = ((long long)blockIdx.x * 2 + (starts ? 1 : 0)) * kRows + row;
+        if (lane == 0) ws.ml[p] = make_float2(m, l);
+#pragma unroll
+        for (int e = 0; e < E; ++e) ws.o[p * D + lane * E + e] = acc[e];
+      }
     }
   }
 }
@@ -757,13 +812,14 @@ __global__ void __launch_bounds__(FqShape<D>::kThreads, 1) fp4_attn_kernel(const
 // Joins the items that shares cut: block g the one whose first block of keys is in CTA g and that goes on in the next ones.  Also zeroes
 // the rows of unusable sequences (tokens).  Launched while the first kernel runs, it works out what it has to join and waits for that
 // one's end.
-template <typename T, int D, bool LIST>
-__global__ void __launch_bounds__(kFqMergeThreads) fp4_merge_kernel(const __grid_constant__ Fp4AttnArgs a) {
+template <typename T, int D, bool LIST, int Q>
+__global__ void __launch_bounds__(FqShape<D, Q>::kRows * 32) fp4_merge_kernel(const __grid_constant__ Fp4AttnArgs a) {
   constexpr int E = D / 32;
-  __shared__ FqPlanShared<kFqMergeThreads> shared;
+  constexpr int kRows = FqShape<D, Q>::kRows, kThreads = kRows * 32;       // a warp per query row
+  __shared__ FqPlanShared<kThreads> shared;
   const int tid = threadIdx.x, lane = tid & 31, row = tid >> 5;
-  const FqWork<D> ws(a.ws);
-  FqPlan<LIST, kFqMergeThreads> plan(a, shared, gridDim.x, 2 * FqShape<D>::kWarps, false);
+  const FqWork<kRows> ws(a.ws);
+  FqPlan<LIST, kThreads, kRows> plan(a, shared, gridDim.x, 2 * FqShape<D, Q>::kWarps, false);
   const unsigned long long from = plan.share * blockIdx.x, behind = from + plan.share;      // the units of CTA g
   int n_parts = 0;
   FqItem it = {};
@@ -780,12 +836,12 @@ __global__ void __launch_bounds__(kFqMergeThreads) fp4_merge_kernel(const __grid
     if (s.error && s.n > 0) {
       T* dst = static_cast<T*>(a.out) + (long long)s.first * a.n_q_heads * D;
       const long long n = (long long)s.n * a.n_q_heads * D;
-      for (long long i = tid; i < n; i += kFqMergeThreads) dst[i] = from_f32<T>(0.f);
+      for (long long i = tid; i < n; i += kThreads) dst[i] = from_f32<T>(0.f);
     }
   }
   const float out_scale = a.out_scale;
   if (n_parts == 0) return;
-  const auto part = [&](int p) -> long long { return ((long long)(blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * kFqRows + row; };
+  const auto part = [&](int p) -> long long { return ((long long)(blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * kRows + row; };
   const int4 s = plan.info;
   float m = -INFINITY;
   for (int p = lane; p < n_parts; p += 32) m = fmaxf(m, ws.ml[part(p)].x);
@@ -800,7 +856,7 @@ __global__ void __launch_bounds__(kFqMergeThreads) fp4_merge_kernel(const __grid
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] += w * o[e];
   }
-  const int qrow = it.tile * kFqRows + row;
+  const int qrow = it.tile * kRows + row;
   if (qrow >= s.w * a.group) return;
   const float inv = l == 0.f ? 0.f : out_scale / l;
   T* dst = static_cast<T*>(a.out) +
@@ -809,28 +865,33 @@ __global__ void __launch_bounds__(kFqMergeThreads) fp4_merge_kernel(const __grid
   for (int e = 0; e < E; ++e) dst[e] = from_f32<T>(acc[e] * inv);
 }
 
-template <typename T, int D, bool LIST>
+template <typename T, int D, bool LIST, int Q>
 cudaError_t launch(const Fp4AttnArgs& a, int sm_count, cudaStream_t stream) {
-  constexpr size_t smem = fq_ring_bytes<D>() + sizeof(FqSmem<D>);
-  static_assert(kFqStages * fq_stage_bytes(D) >= kFqRows * D * 4, "a segment's rows fit over a warp's ring");
+  constexpr size_t smem = fq_ring_bytes<D, Q>() + sizeof(FqSmem<D, Q>);
+  static_assert(kFqStages * fq_stage_bytes(D) >= FqShape<D, Q>::kRows * D * 4, "a segment's rows fit over a warp's ring");
   static_assert(smem <= 227 * 1024, "shared memory of one CTA");
   static std::atomic<unsigned long long> done{0};
-  cudaError_t e = allow_smem(fp4_attn_kernel<T, D, LIST>, smem, &done);
+  cudaError_t e = allow_smem(fp4_attn_kernel<T, D, LIST, Q>, smem, &done);
   if (e != cudaSuccess) return e;
   const int grid = sm_count < kFqMaxCtas ? sm_count : kFqMaxCtas;
-  if ((e = launch_early(fp4_attn_kernel<T, D, LIST>, dim3(grid), FqShape<D>::kThreads, smem, stream, a)) != cudaSuccess) return e;
-  return launch_early(fp4_merge_kernel<T, D, LIST>, dim3(grid), kFqMergeThreads, 0, stream, a);
+  if ((e = launch_early(fp4_attn_kernel<T, D, LIST, Q>, dim3(grid), FqShape<D, Q>::kThreads, smem, stream, a)) != cudaSuccess) return e;
+  return launch_early(fp4_merge_kernel<T, D, LIST, Q>, dim3(grid), FqShape<D, Q>::kRows * 32, 0, stream, a);
 }
 
 template <typename T, int D>
 cudaError_t launch_l(const Fp4AttnArgs& a, int sm_count, cudaStream_t stream) {
-  return a.t.seqs ? launch<T, D, true>(a, sm_count, stream) : launch<T, D, false>(a, sm_count, stream);
+  if (a.t.seqs) return launch<T, D, true, 1>(a, sm_count, stream);
+  // sequences may have more rows than a tile: items of two
+  if constexpr (sizeof(T) == 2) {
+    if (a.max_new > kFqTile >> a.group_shift) return launch<T, D, false, 2>(a, sm_count, stream);
+  }
+  return launch<T, D, false, 1>(a, sm_count, stream);
 }
 
 }  // namespace
 
 uint64_t fp4_attn_workspace_bytes(int head_dim) {
-  const uint64_t n = (uint64_t)kFqMaxCtas * 2 * kFqRows * (sizeof(float2) + (uint64_t)head_dim * sizeof(float));
+  const uint64_t n = (uint64_t)kFqMaxCtas * 2 * 2 * kFqTile * (sizeof(float2) + (uint64_t)head_dim * sizeof(float));
   return (n + 255) / 256 * 256;
 }
 
