@@ -560,7 +560,8 @@ typedef struct {
  *    rounded to the storage type in between), and, unless q is NULL, queries ([n_tokens] rows of n_q_heads x head_dim) are turned
  *    into q_out, which is q itself (same stride) or does not overlap the inputs; skipped tokens' queries too.
  *  - with bounds in the cache, those of every page that gets a token are worked out anew from its keys, rows 0 up to the last one
- *    that this call writes (a sequence's tokens come in order of position, each call beginning where the cache ends or before).
+ *    that this call writes (a sequence's tokens come one after the other in order of position, tokens without a row anywhere among
+ *    them, each call beginning where the cache ends or before).
  *  - a pool row may appear once per call.
  * Rows are 16-byte aligned (EINVAL); n_tokens at most 2^27. */
 int echokv_fourbit_append(const echokv_config* cfg, const echokv_fourbit_cache* cache, const echokv_rotation* rotation, const void* q,

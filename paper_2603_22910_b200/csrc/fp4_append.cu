@@ -235,13 +235,30 @@ __global__ void __launch_bounds__(kFaThreads, 4) fp4_append_kernel(const __grid_
   }
 }
 
-// Bounds of the pages that the call touched: a block looks at `chunk` tokens (32; 1 of a decode step) for the last ones of their pages; a warp
+// Bounds of the pages that the call touched: a block looks at `chunk` tokens (31; 1 of a decode step) for the last ones of their pages; a warp
 // takes such a page for one head.  It brings the keys of 64 tokens to shared memory at a time, all on their way at once (what the first kernel
 // wrote comes from the second level cache), then goes through them in a short loop, a lane with 8 features of every second
 // (fourth) token, so that little is left to join at the end.  (A kernel like this one runs its code once: what is unrolled is fetched
 // for nothing.  Loads to registers, which the compiler put next to their uses: 20 to 36 us after 34.5 thousand tokens, now 10.)
 constexpr int kFbWarps = 8;
 constexpr int kFbBlocks = 4;                       // of 16 tokens, at a time
+
+// The row of the first token from i on that has one (-1: none), by a whole warp: there may be many without one (a padded step), so 256
+// are looked at at once.
+__device__ __noinline__ long long next_row(const int64_t* slot_map, long long i, int n_tokens, int page_shift, long long n_pages) {
+  const int lane = threadIdx.x & 31;
+  for (; i < n_tokens; i += 256) {
+    long long row[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) row[e] = i + 32 * e + lane < n_tokens ? slot_map[i + 32 * e + lane] : -1;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t placed = __ballot_sync(0xffffffffu, row[e] >= 0 && (row[e] >> page_shift) < n_pages);
+      if (placed) return __shfl_sync(0xffffffffu, row[e], __ffs(placed) - 1);
+    }
+  }
+  return -1;
+}
 
 template <int D>
 __global__ void __launch_bounds__(kFbWarps * 32) fp4_bounds_kernel(const __grid_constant__ Fp4AppendArgs a, int chunk) {
@@ -259,14 +276,16 @@ __global__ void __launch_bounds__(kFbWarps * 32) fp4_bounds_kernel(const __grid_
   };
   // (a block of one token looks at those behind it with its other lanes)
   const long long i = (long long)blockIdx.x * chunk + lane, mine = row_of(i);
-  // the next token that has a row, if one of this page can come
-  const uint32_t later = __ballot_sync(0xffffffffu, mine >= 0) & ~(1u << lane | ((1u << lane) - 1));
+  // the next token that has a row: one of the next lanes', and for the last of those looked for behind them (where its page has room)
+  const uint32_t placed = __ballot_sync(0xffffffffu, mine >= 0), later = placed & ~(1u << lane | ((1u << lane) - 1));
   long long next = __shfl_sync(0xffffffffu, mine, later ? __ffs(later) - 1 : lane);
-  if (!later) {
-    next = -1;
-    if (mine >= 0 && lane < chunk) {
-      const int left = g.page_tokens - 1 - (int)(mine & (g.page_tokens - 1));
-      for (int j = 32 - lane; j <= left && next < 0 && i + j < a.n_tokens; ++j) next = row_of(i + j);
+  if (!later) next = -1;
+  const int end = 31 - __clz(placed);
+  if (placed != 0 && end < chunk && (long long)blockIdx.x * chunk + 32 < a.n_tokens) {
+    const long long row = __shfl_sync(0xffffffffu, mine, end);
+    if ((row & (g.page_tokens - 1)) != g.page_tokens - 1) {
+      const long long n = next_row(a.slot_map, (long long)blockIdx.x * chunk + 32, a.n_tokens, g.page_shift, g.n_pages);
+      if (lane == end) next = n;
     }
   }
   const bool last = mine >= 0 && lane < chunk && (next < 0 || (next >> g.page_shift) != (mine >> g.page_shift));
@@ -404,10 +423,10 @@ cudaError_t launch_append(const Fp4AppendArgs& a, int sm_count, cudaStream_t str
   const int per_block = a.n_tokens <= 4 * sm_count ? 1 : kFaTokens;
   cudaError_t e = launch_early(fp4_append_kernel<T, D>, dim3((unsigned)((a.n_tokens + per_block - 1) / per_block)), kFaThreads, 0, stream, a, per_block);
   if (e != cudaSuccess || a.g.bounds == nullptr) return e;
-  // (many tokens: 32 to a block, most of which are not the last ones of their pages, and the heads over several blocks if these are
-  // few; a decode step: a block for each token)
-  const int chunk = a.n_tokens <= 4 * sm_count ? 1 : 32, blocks = (a.n_tokens + chunk - 1) / chunk;
-  const int y = chunk == 1 || blocks >= sm_count ? 1 : min((32 * a.g.n_kv_heads + kFbWarps - 1) / kFbWarps, (2 * sm_count + blocks - 1) / blocks);
+  // (many tokens: 31 to a block, whose lanes then see the one behind them, most of which are not the last ones of their pages, and the
+  // heads over several blocks if these are few; a decode step: a block for each token)
+  const int chunk = a.n_tokens <= 4 * sm_count ? 1 : 31, blocks = (a.n_tokens + chunk - 1) / chunk;
+  const int y = chunk == 1 || blocks >= sm_count ? 1 : min((31 * a.g.n_kv_heads + kFbWarps - 1) / kFbWarps, (2 * sm_count + blocks - 1) / blocks);
   return launch_early(fp4_bounds_kernel<D>, dim3(blocks, y), kFbWarps * 32, 0, stream, a, chunk);
 }
 

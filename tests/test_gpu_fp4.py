@@ -200,6 +200,29 @@ def test_append_skips_tokens_without_a_row_and_reports_bad_ones():
         assert st.item() == binding.ECHOKV_EBADPAGE and (kk == 0).all() and (vv == 0).all()
 
 
+@pytest.mark.parametrize("gap,behind", [(5, 0), (16, 3), (40, 600), (300, 0), (700, 1), (1000, 5000)])
+@pytest.mark.parametrize("page", [16, 64])
+def test_bounds_see_every_row_however_many_tokens_without_one_lie_between(page, gap, behind):
+    cfg = config(n_q=4, n_kv=2, d=64, page=page, batch=2, pages=8, n_pages=16)
+    p = Program(cfg, seed=gap + behind)
+    n = 2 * page + 5
+    plan = p.plan([n])
+    k, v = p.rows(n, 2, 0.1), p.rows(n, 2)
+    k[n - 1] *= 100                               # (each page's last row is the one that its bounds come from)
+    k[page - 1] *= 50
+    rows = plan.slot_map.cpu().numpy()
+    at = [0, 1, 2, page - 1, page, 2 * page - 1, 2 * page, 2 * page + 2]       # gaps in front of these, and tokens without a row at the end
+    seen = np.full(n + gap * len(at) + behind, -1, np.int64)
+    places = np.arange(n) + gap * np.searchsorted(at, np.arange(n), side="right")
+    seen[places] = rows
+    kk, vv = (torch.full((len(seen), 2, 64), NAN, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    kk[places.tolist()], vv[places.tolist()] = k, v
+    p.cache.append(kk, vv, dev(seen, torch.int64), status=p.status)
+    p.note([n], k.float().cpu().numpy(), v.float().cpu().numpy())
+    p.check_cache()
+    assert p.status.item() == 0
+
+
 def test_queries_of_skipped_tokens_are_turned_and_a_cache_without_bounds_works():
     cfg = config(n_q=4, n_kv=2, d=64, page=16, batch=1, pages=4, n_pages=4)
     cache = binding.Fp4Cache(cfg, selection=False)
@@ -352,6 +375,36 @@ def test_many_sequences(B):
     for b in [b for b in (0, 1, 31, 32, B // 2, B - 2, B - 1) if new[b]]:
         ref, size = R.attend(f64(q[at[b]:at[b + 1]]), p.k[b], p.v[b], 0.125)
         assert (np.abs(f64(out[at[b]:at[b + 1]]) - ref) <= F.tolerance(ref, size, p.lens[b], EPS["bf16"], True)).all(), b
+
+
+@pytest.mark.parametrize("d,n_q,n_kv,page", [(128, 8, 2, 16), (64, 8, 1, 32), (128, 4, 4, 64), (64, 4, 4, 16)])
+def test_items_of_two_tiles(d, n_q, n_kv, page):
+    """9 to 16 query rows of an item, one tile and a last one of a few rows, items cut anywhere; row counts up to where chunks begin."""
+    g = n_q // n_kv
+    new = [n for n in (1, 2, 3, 4, 5, 7, 9, 12, 15, 16, 17, 31, 60) if n * g < CHUNK_ROWS]
+    B = len(new)
+    p = Program(config(n_q=n_q, n_kv=n_kv, d=d, page=page, batch=B, pages=2048 // page, n_pages=B * 2048 // page), seed=d + n_q)
+    p.step([int(x) for x in p.rng.integers(0, 1800, B)])
+    p.step(new)
+    q = p.rows(sum(new), n_q, 2.5)
+    for opts in ({}, dict(softcap=20.0, slopes=True, prefix=True)):
+        kw = options(opts, n_q, [x // 2 for x in p.lens])
+        out = p.attend(new, q, **dict(kw))
+        p.check_attention(new, q, out, **kw)
+        assert torch.equal(out, p.attend(new, q, **dict(kw)))
+    assert p.status.item() == 0
+
+
+@pytest.mark.parametrize("B,d", [(33, 128), (300, 128), (700, 64)])
+def test_many_sequences_with_drafts(B, d):
+    p = Program(config(n_q=8, n_kv=2, d=d, page=16, batch=B, pages=6, n_pages=6 * B), seed=B)
+    p.step([int(x) for x in p.rng.integers(0, 80, B)])
+    new = [int(x) for x in p.rng.integers(0, 6, B)]
+    p.step(new)
+    q = p.rows(sum(new), 8, 2.0)
+    out = p.attend(new, q)
+    assert p.status.item() == 0
+    p.check_attention(new, q, out)
 
 
 def test_rows_of_bad_sequences_are_zero_and_other_rows_stay():
