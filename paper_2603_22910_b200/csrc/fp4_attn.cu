@@ -132,7 +132,7 @@ struct FqPlan {
   int4 mine;                                      // (few) of this lane's owner
   unsigned long long mine_pre, total, share;
   // found: the owner of a unit, the first unit of it
-  int b;
+  int b = -1;
   unsigned long long base;
   int4 info;
 
@@ -181,7 +181,7 @@ struct FqPlan {
     if (few) return make_int4(__shfl_sync(0xffffffffu, mine.x, k), __shfl_sync(0xffffffffu, mine.y, k), __shfl_sync(0xffffffffu, mine.z, k), __shfl_sync(0xffffffffu, mine.w, k));
     return per == 1 ? sm.info[k] : owner_info<LIST>(a, k, false, without);
   }
-  // the owner of unit u < total, by a whole warp: the last one whose units begin at or before it
+  // the owner of unit u < total, by a whole warp: the last one whose units begin at or before it (units are asked for in order)
   __device__ __forceinline__ void locate(unsigned long long u) {
     const int lane = threadIdx.x & 31;
     if (few) {
@@ -191,11 +191,14 @@ struct FqPlan {
       return;
     }
     static_assert(THREADS <= 1024, "a lane per run of 32 prefixes");
-    const int run = __popc(__ballot_sync(0xffffffffu, lane < THREADS / 32 && sm.pre[lane * 32 < THREADS ? lane * 32 : 0] <= u)) - 1;
-    const int at = run * 32 + __popc(__ballot_sync(0xffffffffu, sm.pre[run * 32 + lane] <= u)) - 1;
-    b = at * per;
-    base = sm.pre[at];
-    info = info_of(b);
+    // (with runs of owners: on from the last one found, whose units end where the next unit begins)
+    if (per == 1 || b < 0) {
+      const int run = __popc(__ballot_sync(0xffffffffu, lane < THREADS / 32 && sm.pre[lane * 32 < THREADS ? lane * 32 : 0] <= u)) - 1;
+      const int at = run * 32 + __popc(__ballot_sync(0xffffffffu, sm.pre[run * 32 + lane] <= u)) - 1;
+      b = at * per;
+      base = sm.pre[at];
+      info = info_of(b);
+    }
     for (unsigned long long n = units_of<LIST, ROWS>(a, info); base + n <= u; n = units_of<LIST, ROWS>(a, info)) {
       base += n;
       info = info_of(++b);
