@@ -6,7 +6,7 @@
 // pages on the M rows and the query rows on N, exact in 32 bits, so that equal pages are equal and the choice does not depend on
 // the order of anything.  A block takes one KV head of one token, or of up to 8 neighbours of one sequence where there are tokens enough
 // for all SMs (a page's bounds are then read once for them).  A warp takes 16 pages at a time, whose bounds its lanes have asked for
-// four steps before (two, where the keys of many tokens leave no room), each the pieces that it will use itself, and writes their scores, as whole numbers in the order of the
+// two or four steps before, each the pieces that it will use itself, and writes their scores, as whole numbers in the order of the
 // floats, in the pages' order to shared memory.  The n_select largest are then found by counting eight bits at a time from the
 // top of what the keys differ in, and copied in order: what comes out is ascending, and of equal scores the first pages stay.
 // When the buffer is full it is cut down to n_select in the same way, so that a sequence may have any number of pages.  Few tokens over
@@ -525,34 +525,46 @@ template <typename T, int D>
 cudaError_t launch(const Fp4SelectArgs& a, int sm_count, cudaStream_t stream) {
   const int K = a.t.n_select;
   const long long heads = (long long)a.n_tokens * a.g.n_kv_heads;
-  // tokens of a block: as many as leave a block for every SM; with few tokens the pages of one may be in parts
-  int tile_tokens = 1;
-  while (tile_tokens < kFsMaxTokens && heads >= 2ll * tile_tokens * sm_count) tile_tokens *= 2;
-  int parts = 1;
+  constexpr size_t kRoom = 227 * 1024;
+  int tile_tokens = 1, parts = 1;
+  const auto capacity = [&] { return capacity_of(tile_tokens, K, kFsStep, (a.g.max_pages + parts - 1) / parts + 2 * kFsStep); };
+  const auto smem_of = [&](int depth) {
+    const int rows = (tile_tokens * a.group + 7) & ~7;
+    return (size_t)kFsWarps * depth * fs_stage_bytes(D) + (size_t)rows * (2 * D + 4) + tile_tokens * (sizeof(FsGroup) + 4ull * (capacity() + K));
+  };
+  const auto two_fit = [&] { return smem_of(2) <= kRoom / 2 - 1024; };       // on an SM, with two steps under way
+  // Tokens of a block: up to how many a sequence has on average, as many as leave a block for every SM; not 8 where two blocks of 4 fit
+  // on an SM and of 8 do not (4096 tokens of 1250 pages: 990 and 1390 us; where neither do, 256 tokens of 3750 pages, 291 and 260).
+  // With few tokens the pages of one may be in parts.
+  while (tile_tokens < kFsMaxTokens && (long long)tile_tokens * a.B < a.n_tokens && heads >= 2ll * tile_tokens * sm_count) {
+    const bool two = two_fit();
+    tile_tokens *= 2;
+    if (tile_tokens == kFsMaxTokens && two && !two_fit()) {
+      tile_tokens /= 2;
+      break;
+    }
+  }
   if (tile_tokens == 1) {
     const long long room = sm_count < kFsMaxParts ? sm_count : kFsMaxParts;
     const long long most = (a.g.max_pages + kFsMinPages - 1) / kFsMinPages;
     parts = (int)(room / heads < most ? room / heads : most);
     if (parts < 1) parts = 1;
   }
-  const int capacity = capacity_of(tile_tokens, K, kFsStep, (a.g.max_pages + parts - 1) / parts + 2 * kFsStep);
-  const auto smem_of = [&](int depth) {
-    const int rows = (tile_tokens * a.group + 7) & ~7;
-    return (size_t)kFsWarps * depth * fs_stage_bytes(D) + (size_t)rows * (2 * D + 4) + tile_tokens * (sizeof(FsGroup) + 4ull * (capacity + K));
-  };
-  constexpr size_t kRoom = 227 * 1024;
+  // Four steps under way, or two and two blocks to an SM where there are blocks for it (of 160 blocks 27 us with four and 31 with two, of 192
+  // 36 and 31, of 320 84 and 64)
+  const bool shared_sm = 4 * heads > 5ll * tile_tokens * sm_count && two_fit();
   static_assert(kFsWarps * 2 * fs_stage_bytes(128) + kFsMaxTokens * 8 * 260 + kFsMaxTokens * sizeof(FsGroup) + kFsEntries * 4 +
                 kFsMaxTokens * (32 + ECHOKV_FOURBIT_MAX_SELECT) * 4 <= kRoom, "shared memory of one CTA, however many tokens and pages");
   const dim3 grid((unsigned)heads, parts);
   cudaError_t e;
-  if (smem_of(4) <= kRoom) {
+  if (smem_of(4) <= kRoom && !shared_sm) {
     static std::atomic<unsigned long long> done{0};
     if ((e = allow_smem(fp4_select_kernel<T, D, 4>, kRoom, &done)) != cudaSuccess) return e;
-    e = launch_early(fp4_select_kernel<T, D, 4>, grid, kFsThreads, smem_of(4), stream, a, tile_tokens, capacity);
+    e = launch_early(fp4_select_kernel<T, D, 4>, grid, kFsThreads, smem_of(4), stream, a, tile_tokens, capacity());
   } else {
     static std::atomic<unsigned long long> done{0};
     if ((e = allow_smem(fp4_select_kernel<T, D, 2>, kRoom, &done)) != cudaSuccess) return e;
-    e = launch_early(fp4_select_kernel<T, D, 2>, grid, kFsThreads, smem_of(2), stream, a, tile_tokens, capacity);
+    e = launch_early(fp4_select_kernel<T, D, 2>, grid, kFsThreads, smem_of(2), stream, a, tile_tokens, capacity());
   }
   if (e != cudaSuccess || parts == 1) return e;
   const int merge_capacity = capacity_of(1, K, K, (long long)parts * K);
