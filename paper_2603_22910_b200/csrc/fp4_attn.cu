@@ -18,6 +18,10 @@
 //            probabilities beside them, take a second product with their low-order halves (22 bits).
 //   softmax  The running maximum is a reference that moves only when a score is 2^8 above it; probabilities are 2^5 times themselves, so
 //            that fp16 holds them down to 2^-29 of the reference.
+// Measured (device time, both kernels): 16 requests over 32768 keys, 8 bf16 heads of 128 118 us, 5.1 TB/s (the copies alone 110; fp32
+// queries 160); 32 ragged requests of 32 heads, pages of 16, 132 us, capped 147 (copies 122); one request of 777 keys 9.7; 8 drafts
+// for each of 16 requests over 32768 keys 341 us (by items of 8 rows 434); 64 listed pages of 64 tokens for 16 tokens 27 us. The
+// conversion to fp16 by the instruction and a byte select of its result: 118 us; by shifts 160, by whole-number arithmetic no better.
 #include "fp4_common.cuh"
 #include <type_traits>
 

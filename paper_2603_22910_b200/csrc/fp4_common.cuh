@@ -49,7 +49,8 @@ __device__ __forceinline__ uint32_t e4m3_code(float x) {
 constexpr uint32_t kE4m3Nan = 0x7fu;
 
 // A kernel whose blocks may be there before the one before it on the stream has ended.  It begins with after_the_one_before(), behind which
-// everything that was written before is seen; where it lets its own successor come early, it does so after that.
+// everything that was written before is seen; where it lets its own successor come early, it does so after that.  (A call's second kernel
+// may read the call's inputs sooner: the first one has waited for them before it let the second one come.)
 template <typename... P, typename... A>
 inline cudaError_t launch_early(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream, const A&... args) {
   cudaLaunchConfig_t cfg = {};
