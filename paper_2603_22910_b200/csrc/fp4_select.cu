@@ -6,7 +6,7 @@
 // pages on the M rows and the query rows on N, exact in 32 bits, so that equal pages are equal and the choice does not depend on
 // the order of anything.  A block takes one KV head of one token, or of up to 8 neighbours of one sequence where there are tokens enough
 // for all SMs (a page's bounds are then read once for them).  A warp takes 16 pages at a time, whose bounds its lanes have asked for
-// two or four steps before, each the pieces that it will use itself, and writes their scores, as whole numbers in the order of the
+// two steps before, each the pieces that it will use itself, and writes their scores, as whole numbers in the order of the
 // floats, in the pages' order to shared memory.  The n_select largest are then found by counting eight bits at a time from the
 // top of what the keys differ in, and copied in order: what comes out is ascending, and of equal scores the first pages stay.
 // When the buffer is full it is cut down to n_select in the same way, so that a sequence may have any number of pages.  Few tokens over
@@ -20,13 +20,14 @@ namespace echokv {
 
 namespace {
 
-constexpr int kFsWarps = 8;
-constexpr int kFsThreads = kFsWarps * 32;
-constexpr int kFsStep = kFsWarps * 16;             // pages that a block takes at once
+constexpr int kFsMaxWarps = 16;                    // of a block: 16, or 8 where two blocks share an SM or there is no room for more
+constexpr int kFsDepth = 2;                        // steps under way
+__host__ __device__ constexpr int fs_step(int warps) { return warps * 16; }        // pages that a block takes at once
 constexpr int kFsEntries = 16384;                  // keys of a block, of all its tokens
 constexpr int kFsMaxTokens = 8;                    // tokens of a block: each has room for 2048 keys, ECHOKV_FOURBIT_MAX_SELECT and a step
 constexpr int kFsMaxParts = 320;                   // (token, head, part of the pages) with a place in the workspace
 constexpr int kFsMinPages = 512;                   // pages of a part at least
+constexpr size_t kFsRoom = 227 * 1024;             // shared memory of a CTA
 constexpr uint32_t kFsAlways = 0xffffffffu;        // key of a page that is taken in any case (0: of one behind the token's own)
 
 struct FsPart {
@@ -43,7 +44,7 @@ struct FsPart {
 // of the warps that choose for one token
 struct FsGroup {
   uint32_t hist[256];
-  uint32_t red[kFsWarps][4], side[kFsWarps][2];
+  uint32_t red[kFsMaxWarps][4], side[kFsMaxWarps][2];
   uint32_t bin, want, whole;
 };
 
@@ -268,8 +269,9 @@ __device__ __forceinline__ void write_all(const Fp4SelectArgs& a, int token, int
 // bytes of a step's bounds for one warp: 16 pages, a lane's pieces [piece][lane] and scales [2][lane]
 __host__ __device__ constexpr int fs_stage_bytes(int d) { return 16 * 2 * d + 2 * 32 * 4; }
 
-template <typename T, int D, int kFsDepth>
-__global__ void __launch_bounds__(kFsThreads, 2) fp4_select_kernel(const __grid_constant__ Fp4SelectArgs a, int tile_tokens, int capacity) {
+template <typename T, int D, int kFsWarps>
+__global__ void __launch_bounds__(kFsWarps * 32, kFsWarps == 8 ? 2 : 1) fp4_select_kernel(const __grid_constant__ Fp4SelectArgs a, int tile_tokens, int capacity) {
+  constexpr int kFsThreads = kFsWarps * 32, kFsStep = fs_step(kFsWarps);
   constexpr int W = D / 64;                        // 16-byte pieces of a lane: features 64 i + 16 c and on
   extern __shared__ __align__(16) unsigned char fs_raw[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
@@ -482,8 +484,8 @@ __global__ void __launch_bounds__(kFsThreads, 2) fp4_select_kernel(const __grid_
 }
 
 // Chooses among what the parts of one token and head chose (each of them ascending, and so all of them one after the other).
-__global__ void __launch_bounds__(kFsWarps * 32) fp4_select_merge_kernel(const __grid_constant__ Fp4SelectArgs a, int parts, int capacity) {
-  constexpr int kThreads = kFsWarps * 32;
+__global__ void __launch_bounds__(kFsMaxWarps * 32) fp4_select_merge_kernel(const __grid_constant__ Fp4SelectArgs a, int parts, int capacity) {
+  constexpr int kThreads = kFsMaxWarps * 32;
   extern __shared__ __align__(16) unsigned char fs_raw[];
   __shared__ FsGroup sm;
   const int tid = threadIdx.x, warp = tid >> 5, H = a.g.n_kv_heads, K = a.t.n_select, token = blockIdx.x / H, h = blockIdx.x % H;
@@ -501,7 +503,7 @@ __global__ void __launch_bounds__(kFsWarps * 32) fp4_select_merge_kernel(const _
     const int slot = blockIdx.x * parts + p, m = ws.counts[slot];
     if (n + m > capacity) {
       __syncthreads();
-      cut_down(key, pages, n, K, sm, warp, kFsWarps, 1);
+      cut_down(key, pages, n, K, sm, warp, kFsMaxWarps, 1);
       n = K;
     }
     for (int j = tid; j < m; j += kThreads) {
@@ -511,30 +513,36 @@ __global__ void __launch_bounds__(kFsWarps * 32) fp4_select_merge_kernel(const _
     n += m;
   }
   __syncthreads();
-  const FsChoice f = choose(key, n, K, sm, warp, kFsWarps, 1);
+  const FsChoice f = choose(key, n, K, sm, warp, kFsMaxWarps, 1);
   int32_t* out = a.out + ((long long)token * H + h) * K;
-  const int m = chosen(f, key, n, K, sm, warp, kFsWarps, 1, [&](int at, int i) { out[at] = (int32_t)page[i]; });
+  const int m = chosen(f, key, n, K, sm, warp, kFsMaxWarps, 1, [&](int at, int i) { out[at] = (int32_t)page[i]; });
   for (int j = m + tid; j < K; j += kThreads) out[j] = -1;
 }
 
 int capacity_of(int tokens, int K, int step, long long wanted) {
   long long c = wanted < kFsEntries / tokens ? wanted : kFsEntries / tokens;
-  const long long least = K + step;                // (1152 at most: 8 tokens have 2048 entries each)
+  const long long least = K + step;                // (1280 at most: 8 tokens have 2048 entries each)
   return (int)((c > least ? c : least) + 31) / 32 * 32;
+}
+
+template <typename T, int D, int W>
+cudaError_t launch_of(const Fp4SelectArgs& a, dim3 grid, size_t smem, int tile_tokens, int capacity, cudaStream_t stream) {
+  static std::atomic<unsigned long long> done{0};
+  const cudaError_t e = allow_smem(fp4_select_kernel<T, D, W>, kFsRoom, &done);
+  return e != cudaSuccess ? e : launch_early(fp4_select_kernel<T, D, W>, grid, W * 32, smem, stream, a, tile_tokens, capacity);
 }
 
 template <typename T, int D>
 cudaError_t launch(const Fp4SelectArgs& a, int sm_count, cudaStream_t stream) {
   const int K = a.t.n_select;
   const long long heads = (long long)a.n_tokens * a.g.n_kv_heads;
-  constexpr size_t kRoom = 227 * 1024;
   int tile_tokens = 1, parts = 1;
-  const auto capacity = [&] { return capacity_of(tile_tokens, K, kFsStep, (a.g.max_pages + parts - 1) / parts + 2 * kFsStep); };
-  const auto smem_of = [&](int depth) {
+  const auto capacity = [&](int warps) { return capacity_of(tile_tokens, K, fs_step(warps), (a.g.max_pages + parts - 1) / parts + 2 * fs_step(warps)); };
+  const auto smem_of = [&](int warps) {
     const int rows = (tile_tokens * a.group + 7) & ~7;
-    return (size_t)kFsWarps * depth * fs_stage_bytes(D) + (size_t)rows * (2 * D + 4) + tile_tokens * (sizeof(FsGroup) + 4ull * (capacity() + K));
+    return (size_t)warps * kFsDepth * fs_stage_bytes(D) + (size_t)rows * (2 * D + 4) + tile_tokens * (sizeof(FsGroup) + 4ull * (capacity(warps) + K));
   };
-  const auto two_fit = [&] { return smem_of(2) <= kRoom / 2 - 1024; };       // on an SM, with two steps under way
+  const auto two_fit = [&] { return smem_of(8) <= kFsRoom / 2 - 1024; };     // on an SM
   // Tokens of a block: up to how many a sequence has on average, as many as leave a block for every SM; not 8 where two blocks of 4 fit
   // on an SM and of 8 do not (4096 tokens of 1250 pages: 990 and 1390 us; where neither do, 256 tokens of 3750 pages, 291 and 260).
   // With few tokens the pages of one may be in parts.
@@ -552,27 +560,20 @@ cudaError_t launch(const Fp4SelectArgs& a, int sm_count, cudaStream_t stream) {
     parts = (int)(room / heads < most ? room / heads : most);
     if (parts < 1) parts = 1;
   }
-  // Four steps under way, or two and two blocks to an SM where there are blocks for it (of 160 blocks 27 us with four and 31 with two, of 192
-  // 36 and 31, of 320 84 and 64)
+  static_assert(8 * kFsDepth * fs_stage_bytes(128) + kFsMaxTokens * 8 * 260 + kFsMaxTokens * sizeof(FsGroup) + kFsEntries * 4 +
+                kFsMaxTokens * (32 + ECHOKV_FOURBIT_MAX_SELECT) * 4 <= kFsRoom, "shared memory of one CTA, however many tokens and pages");
+  // 16 warps, or two blocks of 8 to an SM where there are blocks for it (128 blocks: 15.5 us with 16 warps, 17 with 8, of 192 32 and 32, of
+  // 320 70 and 64, of 512 95 and 71; 18 parts of a million keys 55 and 71)
   const bool shared_sm = 4 * heads > 5ll * tile_tokens * sm_count && two_fit();
-  static_assert(kFsWarps * 2 * fs_stage_bytes(128) + kFsMaxTokens * 8 * 260 + kFsMaxTokens * sizeof(FsGroup) + kFsEntries * 4 +
-                kFsMaxTokens * (32 + ECHOKV_FOURBIT_MAX_SELECT) * 4 <= kRoom, "shared memory of one CTA, however many tokens and pages");
+  const int warps = !shared_sm && smem_of(16) <= kFsRoom ? 16 : 8;
   const dim3 grid((unsigned)heads, parts);
-  cudaError_t e;
-  if (smem_of(4) <= kRoom && !shared_sm) {
-    static std::atomic<unsigned long long> done{0};
-    if ((e = allow_smem(fp4_select_kernel<T, D, 4>, kRoom, &done)) != cudaSuccess) return e;
-    e = launch_early(fp4_select_kernel<T, D, 4>, grid, kFsThreads, smem_of(4), stream, a, tile_tokens, capacity());
-  } else {
-    static std::atomic<unsigned long long> done{0};
-    if ((e = allow_smem(fp4_select_kernel<T, D, 2>, kRoom, &done)) != cudaSuccess) return e;
-    e = launch_early(fp4_select_kernel<T, D, 2>, grid, kFsThreads, smem_of(2), stream, a, tile_tokens, capacity());
-  }
+  cudaError_t e = warps == 16 ? launch_of<T, D, 16>(a, grid, smem_of(16), tile_tokens, capacity(16), stream)
+                              : launch_of<T, D, 8>(a, grid, smem_of(8), tile_tokens, capacity(8), stream);
   if (e != cudaSuccess || parts == 1) return e;
   const int merge_capacity = capacity_of(1, K, K, (long long)parts * K);
   static std::atomic<unsigned long long> done_merge{0};
   if ((e = allow_smem(fp4_select_merge_kernel, kFsEntries * 8 + 32 * 8, &done_merge)) != cudaSuccess) return e;
-  return launch_early(fp4_select_merge_kernel, dim3((unsigned)heads), kFsThreads, (size_t)merge_capacity * 8, stream, a, parts, merge_capacity);
+  return launch_early(fp4_select_merge_kernel, dim3((unsigned)heads), kFsMaxWarps * 32, (size_t)merge_capacity * 8, stream, a, parts, merge_capacity);
 }
 
 }  // namespace
