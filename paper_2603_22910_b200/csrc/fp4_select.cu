@@ -11,9 +11,9 @@
 // top of what the keys differ in, and copied in order: what comes out is ascending, and of equal scores the first pages stay.
 // When the buffer is full it is cut down to n_select in the same way, so that a sequence may have any number of pages.  Few tokens over
 // long caches are split along the pages; a second kernel then chooses among what the parts chose.
-// The bound is reading the bounds, 2 d + 4 bytes a page and head.  Measured (8 heads of 128): 64 of 1024 pages for 16 tokens 17 us,
-// of which reading takes 8, scores 4, the choice 5; one token among 62500 pages, in 18 parts, 71 us; 64 decode tokens among 1875 pages
-// each 71 us, 3.5 TB/s; 4096 tokens of 4 prompts among 1250 pages 990 us.
+// The bound is reading the bounds, 2 d + 4 bytes a page and head.  Measured (8 heads of 128): 64 of 1024 pages for 16 tokens 15.5
+// us, about 5 each for start, reading with scores, and the choice; one token among 62500 pages, in 18 parts, 55 us; 64 decode tokens
+// among 1875 pages each 71 us, 3.5 TB/s; 256 tokens of 4 requests among 3750 pages 194 us, 4096 of 4 prompts among 1250 pages 987.
 #include "fp4_common.cuh"
 
 namespace echokv {
@@ -544,7 +544,7 @@ cudaError_t launch(const Fp4SelectArgs& a, int sm_count, cudaStream_t stream) {
   };
   const auto two_fit = [&] { return smem_of(8) <= kFsRoom / 2 - 1024; };     // on an SM
   // Tokens of a block: up to how many a sequence has on average, as many as leave a block for every SM; not 8 where two blocks of 4 fit
-  // on an SM and of 8 do not (4096 tokens of 1250 pages: 990 and 1390 us; where neither do, 256 tokens of 3750 pages, 291 and 260).
+  // on an SM and of 8 do not (4096 tokens of 1250 pages: 987 and 1053 us; where neither do, 256 tokens of 3750 pages, 282 and 194).
   // With few tokens the pages of one may be in parts.
   while (tile_tokens < kFsMaxTokens && (long long)tile_tokens * a.B < a.n_tokens && heads >= 2ll * tile_tokens * sm_count) {
     const bool two = two_fit();
