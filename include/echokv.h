@@ -465,7 +465,8 @@ int echokv_quant_append(const echokv_config* cfg, const echokv_quant_cache* cach
 /* What is done to the scores x = softmax_scale q . k before the softmax; zeros / NULL = nothing.  In this order:
  *     softcap > 0:   x = softcap * tanh(x / softcap)            (at least 1e-30, EINVAL)
  *     alibi_slopes:  x = x - alibi_slopes[h] * |p - t|      (p, t: positions of the query and the key)
- *     mask:          key t is seen if t <= p or t < prefix_lens[b]  (a prefix whose tokens see each other)        */
+ *     mask:          key t is seen if t <= p or t < prefix_lens[b]  (a prefix whose tokens see each other; it may be longer than what
+ *                    is in the cache so far, of which there are dev_seq_lens[b] keys)                             */
 typedef struct {
   float softcap;
   int32_t reserved;

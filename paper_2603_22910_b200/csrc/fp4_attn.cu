@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(FqShape<D, Q>::kThreads, 1) fp4_attn_kernel(co
           if (kF32) ql[ks][f] = p.lo;
         }
     }
-    const int prefix = !LIST && a.prefix ? a.prefix[b] : 0;
+    const int prefix = !LIST && a.prefix ? min(a.prefix[b], len) : 0;          // (a prefix that comes in pieces is longer than what is there)
     int pos[Q][2], row_of[Q][2];                  // (row_of: -1 where the column is nobody's)
     float slope2[Q][2];
 #pragma unroll
