@@ -559,7 +559,8 @@ typedef struct {
  * pool row dev_slot_map[i] (echokv_plan_tokens').  A token with slot -1 is skipped; a bad slot -> device status EBADPAGE, skipped.
  *  - rotation: NULL = none.  Otherwise keys are turned to dev_positions (int32 [n_axes][n_tokens]) in fp32 on their way (not
  *    rounded to the storage type in between), and, unless q is NULL, queries ([n_tokens] rows of n_q_heads x head_dim) are turned
- *    into q_out, which is q itself (same stride) or does not overlap the inputs; skipped tokens' queries too.
+ *    into q_out, which is q itself (same stride) or does not overlap it, and in either case no other input (EINVAL; it may lie between
+ *    their rows, as the queries of a fused projection do); skipped tokens' queries too.
  *  - with bounds in the cache, those of every page that gets a token are worked out anew from its keys, rows 0 up to the last one
  *    that this call writes (a sequence's tokens come one after the other in order of position, tokens without a row anywhere among
  *    them, each call beginning where the cache ends or before).

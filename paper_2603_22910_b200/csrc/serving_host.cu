@@ -111,6 +111,24 @@ bool rows_meet(const void* rows, long long stride, long long width, long long n,
   return i < n && i * stride < from + size;
 }
 
+// do two sets of n rows (widths and strides in bytes; the rows of a set are apart) share a byte?  Slices of one buffer may lie between each
+// other's rows.
+bool rows_cross(const void* a, long long a_stride, long long a_width, const void* b, long long b_stride, long long b_width, long long n) {
+  if (a_stride == b_stride) {
+    // rows i of a and i + k of b: apart + k stride lies between -b_width and a_width
+    const long long apart = (long long)(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a)), low = -b_width - apart;
+    long long k = (low < 0 ? -((-low + a_stride - 1) / a_stride) : low / a_stride) + 1;        // the first one above the lower end
+    if (k < 1 - n) k = 1 - n;
+    return k < n && apart + k * a_stride < a_width;
+  }
+  if (a_stride > b_stride) return rows_cross(b, b_stride, b_width, a, a_stride, a_width, n);
+  // (fewer rows of b lie beside all of a: those are looked at one by one)
+  const long long apart = (long long)(reinterpret_cast<uintptr_t>(a) - reinterpret_cast<uintptr_t>(b)), end = apart + (n - 1) * a_stride + a_width;
+  for (long long j = apart < b_width ? 0 : (apart - b_width) / b_stride + 1; j < n && j * b_stride < end; ++j)
+    if (rows_meet(a, a_stride, a_width, n, static_cast<const char*>(b) + j * b_stride, b_width)) return true;
+  return false;
+}
+
 // frequencies of each position axis (none given: one axis has them all)
 bool sections_ok(int half, int n_axes, const int32_t* sections) {
   if (!sections) return n_axes == 1;
@@ -438,6 +456,13 @@ int echokv_fourbit_append(const echokv_config* cfg, const echokv_fourbit_cache* 
     const int q_width = cfg->n_q_heads * d;
     if (!rows_ok(q, q_stride, q_width, elem) || !rows_ok(q_out, q_out_stride, q_width, elem)) return ECHOKV_EINVAL;
     if (q == q_out && q_stride != q_out_stride) return ECHOKV_EINVAL;
+    const auto over = [&](const void* in, int64_t stride, int in_width) {
+      return rows_cross(q_out, q_out_stride * elem, (long long)q_width * elem, in, stride * elem, (long long)in_width * elem, n_tokens);
+    };
+    if ((q != q_out && over(q, q_stride, q_width)) || over(k_new, k_stride, width) || over(v_new, v_stride, width)) return ECHOKV_EINVAL;
+    if (rows_meet(q_out, q_out_stride * elem, (long long)q_width * elem, n_tokens, dev_positions, 4ll * rotation->n_axes * n_tokens) ||
+        rows_meet(q_out, q_out_stride * elem, (long long)q_width * elem, n_tokens, dev_slot_map, 8ll * n_tokens))
+      return ECHOKV_EINVAL;
   }
   a.q = q; a.q_out = q_out; a.q_stride = q_stride; a.q_out_stride = q_out_stride;
   a.x[0] = k_new; a.x[1] = v_new;

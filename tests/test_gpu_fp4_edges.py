@@ -1,8 +1,11 @@
 """The 4-bit cache's operators where a call is unlike the common ones."""
+import numpy as np
 import pytest
+import torch
 
+from paper_2603_22910_b200 import binding
 from tests.test_gpu_fp4 import Program
-from tests.test_gpu_serving import config
+from tests.test_gpu_serving import config, dev
 
 pytestmark = pytest.mark.gpu
 PREFIXES = [lambda n: n, lambda n: n + 1, lambda n: -(-n // 16) * 16, lambda n: n + 1000, lambda n: 1 << 30, lambda n: (1 << 31) - 1]
@@ -28,3 +31,38 @@ def test_a_prefix_longer_than_the_sequence(stale, dtype, d, page, n_q, n_kv, bef
         at = [prefix(n) for n in p.lens]
         p.check_attention(new, q, p.attend(new, q, prefix=at), prefix=at, only=True)
     assert p.status.item() == 0
+
+
+def test_queries_turned_into_any_place_that_overlaps_no_input():
+    """Queries, keys, values and turned queries anywhere in one buffer: between each other's rows is fine, a shared element is refused."""
+    cfg = config(n_q=2, n_kv=1, d=64, page=16, batch=1, pages=4, n_pages=4)
+    cache, rng = binding.Fp4Cache(cfg, selection=False), np.random.default_rng(23)
+    r, counts = binding.Rotation(cfg, 1e4), [0, 0, 0]
+    for _ in range(1500):
+        T = int(rng.integers(1, 7))
+        strides = [128 + 8 * int(x) for x in rng.integers(0, 70, 4)] if rng.random() < 0.6 else [128 + 8 * int(rng.integers(0, 70))] * 4
+        at = [8 * int(x) for x in rng.integers(0, rng.choice([60, 300, 900]), 4)]
+        if rng.random() < 0.3:
+            at[3], strides[3] = at[0], strides[0]                              # in place
+        shape = [(T, h, 64) for h in (2, 1, 1, 2)]
+        hold = torch.tensor(rng.standard_normal(12000), device="cuda").bfloat16()
+        q, k, v, out = (hold.as_strided(s, (n, 64, 1), a) for s, n, a in zip(shape, strides, at))
+        used = [{a + i * n + j for i in range(T) for j in range(s[1] * 64)} for s, n, a in zip(shape, strides, at)]
+        same = at[0] == at[3] and (strides[0] == strides[3] or T == 1)
+        shared = (used[3] & used[0] and not same) or used[3] & (used[1] | used[2])
+        pos, rows = dev(rng.integers(0, 5000, T)), dev(rng.permutation(64)[:T], torch.int64)
+        before = hold.clone()
+        if shared:
+            with pytest.raises(binding.EchoKVError) as e:
+                cache.append(k, v, rows, q=q, rotation=r, positions=pos, q_out=out)
+            assert e.value.status == binding.ECHOKV_EINVAL and torch.equal(hold, before)
+            counts[0] += 1
+            continue
+        want = cache.append(k.clone(), v.clone(), rows, q=q.clone(), rotation=r, positions=pos)
+        held = cache.read(rows)
+        cache.append(k, v, rows, q=q, rotation=r, positions=pos, q_out=out)
+        assert torch.equal(out, want) and all(torch.equal(x, y) for x, y in zip(cache.read(rows), held))
+        out.copy_(before.as_strided(shape[3], (strides[3], 64, 1), at[3]))
+        assert torch.equal(hold, before)                                       # nothing else was written
+        counts[1 + same] += 1
+    assert min(counts) > 100
