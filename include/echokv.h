@@ -488,6 +488,7 @@ typedef struct {
  * A sequence with a bad slot, a length beyond its capacity or shorter than its new tokens, or more than max_new new
  * tokens: zeros and the device status (EBADPAGE, EBADLENGTH); offsets that decrease or pass n_tokens: EBADLENGTH, nothing is
  * written for that sequence.  A page id outside the pool: EBADPAGE, the output of its sequence is unspecified.
+ * A query row with an infinity or NaN: NaN (infinite scores under a cap are the cap).
  * Scores and sums are fp32; codes enter the products exactly; bf16 queries as fp16 (exact around each row's power of two) with
  * probabilities rounded to fp16 (one below 2^-24 of its row's largest may count as 0 beside it), fp32 queries and their
  * probabilities as pairs of fp16 (22 bits).  For a bf16 sequence

@@ -370,16 +370,15 @@ __global__ void __launch_bounds__(FqShape<D, Q>::kThreads, 1) fp4_attn_kernel(co
 
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-      // (magnitudes compare as integers; an infinity or NaN gives the factor 1 and goes on through the products)
+      // (magnitudes compare as integers, an infinity or NaN above everything finite)
       uint32_t bits = 0;
 #pragma unroll
       for (int x = 0; x < KS; ++x) bits = qv[q][x].top(bits);
       bits = Quad<T>::top_bits(bits);
       bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 1));
       bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 2));
-      const float top = __uint_as_float(bits);
       float back;
-      const float up = scale_up_to_half(top, &back);
+      const float up = query_scale(__uint_as_float(bits), a.softcap > 0.f, &back);
 #pragma unroll
       for (int e = 0; e < 2; ++e)
         c_row[q][e] = __shfl_sync(0xffffffffu, back, 4 * (2 * c + e)) * a.scale * (a.softcap > 0.f ? 1.f : kLog2e);
@@ -389,7 +388,7 @@ __global__ void __launch_bounds__(FqShape<D, Q>::kThreads, 1) fp4_attn_kernel(co
         for (int f = 0; f < 2; ++f) {
           const HalfPair p = split_pair<kF32>(qv[q][ks].get(2 * f) * up, qv[q][ks].get(2 * f + 1) * up);
           qh[q][ks][f] = p.hi;
-          if (kF32) ql[ks][f] = p.lo;
+          if (kF32) ql[ks][f] = bits < 0x7f800000u ? p.lo : 0u;      // (an infinity less itself)
         }
     }
     const int prefix = !LIST && a.prefix ? min(a.prefix[b], len) : 0;          // (a prefix that comes in pieces is longer than what is there)

@@ -262,17 +262,18 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
     };
     for (int j = 0; j < min(kQaStages, n_codes); ++j) issue(j);
 
+    bool q_finite;                                 // row r is
     {
-      // (magnitudes compare as integers; an infinity or NaN gives the factor 1 and goes on through the products)
+      // (magnitudes compare as integers, an infinity or NaN above everything finite)
       uint32_t bits = 0;
 #pragma unroll
       for (int x = 0; x < KS; ++x) bits = qv[x].top(bits);
       bits = Quad<T>::top_bits(bits);
       bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 1));
       bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 2));
-      const float top = __uint_as_float(bits);
+      q_finite = bits < 0x7f800000u;
       float back;
-      const float up = scale_up_to_half(top, &back);
+      const float up = query_scale(__uint_as_float(bits), a.softcap > 0.f, &back);
 #pragma unroll
       for (int e = 0; e < 2; ++e)
         c_row[e] = __shfl_sync(0xffffffffu, back, 4 * (2 * c + e)) * a.scale * (a.softcap > 0.f ? 1.f : kLog2e);
@@ -282,7 +283,7 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
         for (int f = 0; f < 2; ++f) {
           const HalfPair p = split_pair<kF32>(qv[ks].get(2 * f) * up, qv[ks].get(2 * f + 1) * up);
           qh[ks][f] = p.hi;
-          if (kF32) ql[ks][f] = p.lo;
+          if (kF32) ql[ks][f] = q_finite ? p.lo : 0u;      // (an infinity less itself)
         }
     }
     const int prefix = a.prefix ? a.prefix[b] : 0;
@@ -483,7 +484,8 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
           }
           mma_m16n8k16_f16(sc, p[0].hi, p[1].hi, p[2].hi, p[3].hi, qh[x][0], qh[x][1]);
           mma_m16n8k16_f16(sc, p[0].hi, p[1].hi, p[2].hi, p[3].hi, ql[x][0], ql[x][1]);
-          mma_m16n8k16_f16(sc, p[0].lo, p[1].lo, p[2].lo, p[3].lo, qh[x][0], qh[x][1]);
+          // (an infinity has its sign from the keys' high-order halves)
+          mma_m16n8k16_f16(sc, p[0].lo, p[1].lo, p[2].lo, p[3].lo, q_finite ? qh[x][0] : 0u, q_finite ? qh[x][1] : 0u);
         }
         f_row[0] = k_ok ? c_row[0] : __uint_as_float(0x7fc00000u);
         f_row[1] = k_ok ? c_row[1] : __uint_as_float(0x7fc00000u);
@@ -526,7 +528,10 @@ __global__ void __launch_bounds__(kQaThreads, 1) quant_attn_kernel(const __grid_
         for (int t = 0; t < 4; ++t)
 #pragma unroll
           for (int x = 0; x < NT / 4; ++x) v_bad = zero_fma_bf16x2(vq[t][x].w.x, zero_fma_bf16x2(vq[t][x].w.y, v_bad));
-        f_row[0] = f_row[1] = __any_sync(0xffffffffu, (k_bad & 0x7fff7fffu) != 0) ? __uint_as_float(0x7fc00000u) : a.scale * (a.softcap > 0.f ? 1.f : kLog2e);
+        const bool k_ok = !__any_sync(0xffffffffu, (k_bad & 0x7fff7fffu) != 0);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)                  // (the row's inverse power has no part here, but a NaN instead of it)
+          f_row[e] = k_ok && c_row[e] == c_row[e] ? a.scale * (a.softcap > 0.f ? 1.f : kLog2e) : __uint_as_float(0x7fc00000u);
         if (__any_sync(0xffffffffu, (v_bad & 0x7fff7fffu) != 0)) v_mul = __uint_as_float(0x7fc00000u);
       }
       if (v_mul != v_mul) {

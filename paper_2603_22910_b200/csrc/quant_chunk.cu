@@ -963,7 +963,7 @@ __global__ void __launch_bounds__(kCkThreads, 1) quant_chunk_kernel(const __grid
           top = __vmaxu2(__vmaxu2(top, __vmaxu2(v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu)), __vmaxu2(v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu));
       }
       float c_row;
-      const float up = scale_up_to_half(__uint_as_float(max(top & 0xffff0000u, top << 16)), &c_row);
+      const float up = query_scale(__uint_as_float(max(top & 0xffff0000u, top << 16)), a.softcap > 0.f, &c_row);
 #pragma unroll 1
       for (int p = 0; p < D / 8; p += 4) {
         uint4 v[4];

@@ -154,4 +154,14 @@ __device__ __forceinline__ float scale_up_to_half(float m, float* inverse) {
   return __uint_as_float((uint32_t)(127 + k) << 23);
 }
 
+// The same for a query row (m: its largest magnitude).  A row with an infinity or NaN has scores of which none is finite, so its
+// output is NaN: the inverse is NaN, for a row of which all scores are -inf would seem to see no key.  A cap makes infinite scores
+// finite: the power then takes the row's finite elements out of the way (below 2^2, so that no sum of them matters beside an infinity).
+__device__ __forceinline__ float query_scale(float m, bool capped, float* inverse) {
+  const float up = scale_up_to_half(m, inverse);
+  if (__float_as_uint(m) < 0x7f800000u) return up;
+  *inverse = capped ? 1.f : __uint_as_float(0x7fc00000u);
+  return 0x1p-126f;
+}
+
 }  // namespace echokv

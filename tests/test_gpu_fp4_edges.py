@@ -4,10 +4,13 @@ import pytest
 import torch
 
 from paper_2603_22910_b200 import binding
+from tests import fp4_ref as F
+from tests import serving_ref as R
 from tests.test_gpu_fp4 import Program
-from tests.test_gpu_serving import config, dev
+from tests.test_gpu_serving import DT, EPS, config, dev, f64
 
 pytestmark = pytest.mark.gpu
+NAN, INF = float("nan"), float("inf")
 PREFIXES = [lambda n: n, lambda n: n + 1, lambda n: -(-n // 16) * 16, lambda n: n + 1000, lambda n: 1 << 30, lambda n: (1 << 31) - 1]
 
 
@@ -66,3 +69,39 @@ def test_queries_turned_into_any_place_that_overlaps_no_input():
         assert torch.equal(hold, before)                                       # nothing else was written
         counts[1 + same] += 1
     assert min(counts) > 100
+
+
+@pytest.mark.parametrize("softcap", [0.0, 5.0])
+@pytest.mark.parametrize("dtype,new", [("bf16", [1, 1, 2]), ("fp32", [1, 1, 2]), ("bf16", [3, 1, 20]), ("bf16", [1, 500, 1])])
+def test_queries_that_are_not_finite(dtype, new, softcap):
+    """A query row with an infinity or NaN has scores of which none is an ordinary number: its output is NaN, also where every key that
+    it sees scores -inf; a cap makes infinite scores finite.  Other rows are left alone."""
+    n_q = n_kv = 4
+    p = Program(config(n_q=n_q, n_kv=n_kv, d=64, page=16, batch=3, pages=64, n_pages=192, dtype=dtype), seed=17)
+    T = sum(new)
+    size = torch.tensor(p.rng.uniform(1.0, 1.5, (T, n_kv, 64)), device="cuda").to(DT[dtype][1])         # (no code of it is 0)
+    k = torch.where(torch.arange(n_kv, device="cuda")[:, None] % 2 == 0, -size, size)
+    p.step(new, k=k)
+    q = p.rows(T, n_q)
+    first = np.concatenate([[0], np.cumsum(new)[:-1]]).tolist()
+    q[first[0], :, 5], q[first[1], :2, 9], q[first[2], 1, 63], q[first[2], 2, 0] = INF, -INF, NAN, INF
+    q[first[2], 2, 7] = -1e6                                               # (beyond fp16's range beside the infinity)
+    out = f64(p.attend(new, q, softcap=softcap))
+    seqs, pos = p.tokens(new)
+    pages = np.arange(-(-max(new) // 16))
+    pages = np.broadcast_to(np.where(pages <= pos[:, None, None] // 16, pages, -1), (T, n_kv, len(pages))).copy()
+    some = f64(p.cache.sparse_attention(q, p.table, dev(seqs), dev(pos), dev(pages), seq_slots=dev(p.slots), softcap=softcap, status=p.status))
+    assert np.array_equal(np.isnan(some), np.isnan(out))
+    pages[:] = -1
+    none = p.cache.sparse_attention(q, p.table, dev(seqs), dev(pos), dev(pages), seq_slots=dev(p.slots), softcap=softcap)
+    assert (none == 0).all()                                                   # (a token that has no key)
+    for b, n in enumerate(new):
+        with np.errstate(invalid="ignore"):
+            ref, s = R.attend(f64(q[first[b]:first[b] + n]), p.k[b], p.v[b], 0.125, softcap, only=sorted({0, n // 2, n - 1}))
+        for i in sorted({0, n // 2, n - 1}):
+            got = out[first[b] + i]
+            assert np.array_equal(np.isnan(got), np.isnan(ref[i])), (b, i)
+            fine = ~np.isnan(ref[i]).any(-1) & np.isfinite(f64(q[first[b] + i])).all(-1)
+            tol = F.tolerance(ref[i:i + 1], s[i:i + 1], n, EPS[dtype], dtype == "bf16", n >= 64, softcap)[0]
+            assert (np.abs(got - ref[i]) <= tol)[fine].all(), (b, i)
+    assert p.status.item() == 0
