@@ -581,7 +581,7 @@ int echokv_fourbit_read(const echokv_config* cfg, const echokv_fourbit_cache* ca
 /* echokv_quant_attention over this cache: the same arguments, options, masks, statuses and rules for out and workspace
  * (echokv_fourbit_sizes.workspace_bytes).  The cache's values enter the products exactly; bf16 queries as fp16 (exact around each row's
  * power of two) with probabilities rounded to fp16 (one below 2^-29 of its row's largest may count as 0; in chunks 2^-24), fp32 queries
- * and their probabilities as pairs of fp16 (22 bits). */
+ * and their probabilities as pairs of fp16 (22 bits, of a probability down to 2^-42 of its row's largest). */
 int echokv_fourbit_attention(const echokv_config* cfg, const echokv_fourbit_cache* cache, const echokv_score_options* options, const void* q,
                          int64_t q_stride, void* out, const int32_t* dev_block_table, const int32_t* dev_seq_slots,
                          const int32_t* dev_seq_lens, const int32_t* dev_cu_tokens, int B, int n_tokens, int max_new, void* workspace,

@@ -17,7 +17,7 @@
 //            e2m1 x e4m3 has 6 bits and lies between 2^-10 and 2688: it is an fp16 exactly.  fp32 queries, and the
 //            probabilities beside them, take a second product with their low-order halves (22 bits).
 //   softmax  The running maximum is a reference that moves only when a score is 2^8 above it; probabilities are 2^5 times themselves, so
-//            that fp16 holds them down to 2^-29 of the reference.
+//            that fp16 holds them down to 2^-29 of the largest (with a second half, in fp32, to 2^-42).
 // Measured (device time, both kernels): 16 requests over 32768 keys, 8 bf16 heads of 128 118 us, 5.1 TB/s (the copies alone 110; fp32
 // queries 160); 32 ragged requests of 32 heads, pages of 16, 132 us, capped 147 (copies 122); one request of 777 keys 9.7; 8 drafts
 // for each of 16 requests over 32768 keys 341 us (by items of 8 rows 434); 64 listed pages of 64 tokens for 16 tokens 27 us. The
@@ -44,6 +44,8 @@ constexpr int kFqMaxCtas = 512;
 constexpr int kFqItemCost = 6;                    // what an item costs beside its blocks (queries, first copies, result), in blocks
 constexpr float kFqBelow = 5.f;                   // the reference stands 2^5 below the largest score it was taken from,
 constexpr float kFqGrow = 8.f + kFqBelow;         // and moves when a score is 2^13 above it (probabilities up to there fit fp16)
+constexpr float kFqLowUp = 8192.f;                // (fp32) low-order halves of probabilities, 2^2 at most, are held 2^13 times themselves: down
+                                                  // to 2^-42 of the largest, so that many small ones count beside a large one
 constexpr int kFqNowhere = 0x40000000;            // the first token of a block that nobody sees
 
 __host__ __device__ constexpr int fq_stage_bytes(int D) { return 2 * fp4_block_bytes(D); }
@@ -601,60 +603,68 @@ __global__ void __launch_bounds__(FqShape<D, Q>::kThreads, 1) fp4_attn_kernel(co
           }
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
-            const HalfPair w = split_pair<kF32>(p[2 * t], p[2 * t + 1]);
+            const HalfPair w = split_pair<kF32>(p[2 * t], p[2 * t + 1], kFqLowUp);
             ph[q][n][t] = movm(w.hi);
             if (kF32) pl[n][t] = movm(w.lo);
           }
         }
 
-      // ---- output (fp32: the step's products are summed by themselves, as above)
-      float step_o[kF32 ? MT : 1][4];
-      if (kF32) {
+      // ---- output
+      // (behind the sequence's end there may be anything: a NaN times a probability of 0)
+      if (MASKED) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-          for (int f = 0; f < 4; ++f) step_o[kF32 ? m : 0][f] = 0.f;
-      }
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        // (behind the sequence's end there may be anything: a NaN times a probability of 0)
-        if (MASKED) {
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             const int tok = tok0[n] + 8 * t + 2 * c;
             if (tok >= len) vs[n][t] = 0u;
             else if (tok + 1 >= len) vs[n][t] &= 0xffffu;
           }
+      }
+      // word w of block n's codes -> operands: features 2 i and 2 i + 1, a byte for both tokens
+      const auto values = [&](int n, int w, uint32_t (&x)[2][4], uint32_t (&y)[2][4]) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          e2m1_bytes(fp4_zip(vt[n][t][0][w], vt[n][t][1][w] << 4), x[t]);
+          e2m1_bytes(fp4_zip(vt[n][t][0][w] >> 4, vt[n][t][1][w]), y[t]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            x[t][i] = fp4_mul(x[t][i], vs[n][t]);
+            y[t][i] = fp4_mul(y[t][i], vs[n][t]);
+          }
         }
+      };
+      if constexpr (kF32) {
+        // (a step's products are summed by themselves, as above, those with the probabilities' low-order halves around their own power)
 #pragma unroll
         for (int w = 0; w < D / 64; ++w) {
-          uint32_t x[2][4], y[2][4];
+          uint32_t x[NB][2][4], y[NB][2][4];
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            // features 2 i and 2 i + 1, a byte for both tokens
-            e2m1_bytes(fp4_zip(vt[n][t][0][w], vt[n][t][1][w] << 4), x[t]);
-            e2m1_bytes(fp4_zip(vt[n][t][0][w] >> 4, vt[n][t][1][w]), y[t]);
+          for (int n = 0; n < NB; ++n) values(n, w, x[n], y[n]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              x[t][i] = fp4_mul(x[t][i], vs[n][t]);
-              y[t][i] = fp4_mul(y[t][i], vs[n][t]);
+          for (int i = 0; i < 4; ++i) {
+            float hi[4] = {0.f, 0.f, 0.f, 0.f}, lo[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+              mma_m16n8k16_f16(hi, x[n][0][i], y[n][0][i], x[n][1][i], y[n][1][i], ph[0][n][0], ph[0][n][1]);
+              mma_m16n8k16_f16(lo, x[n][0][i], y[n][0][i], x[n][1][i], y[n][1][i], pl[n][0], pl[n][1]);
             }
+#pragma unroll
+            for (int f = 0; f < 4; ++f) o[0][4 * w + i][f] += fmaf(lo[f], 1.f / kFqLowUp, hi[f]);
           }
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int q = 0; q < L; ++q) {
-              float (&acc)[4] = kF32 ? step_o[kF32 ? 4 * w + i : 0] : o[q][4 * w + i];
-              mma_m16n8k16_f16(acc, x[0][i], y[0][i], x[1][i], y[1][i], ph[q][n][0], ph[q][n][1]);
-              if (kF32) mma_m16n8k16_f16(acc, x[0][i], y[0][i], x[1][i], y[1][i], pl[n][0], pl[n][1]);
-            }
         }
-      }
-      if (kF32) {
+      } else {
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
-          for (int f = 0; f < 4; ++f) o[0][m][f] += step_o[kF32 ? m : 0][f];
+          for (int w = 0; w < D / 64; ++w) {
+            uint32_t x[2][4], y[2][4];
+            values(n, w, x, y);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int q = 0; q < L; ++q) mma_m16n8k16_f16(o[q][4 * w + i], x[0][i], y[0][i], x[1][i], y[1][i], ph[q][n][0], ph[q][n][1]);
+          }
       }
     };
 #pragma unroll 1

@@ -86,18 +86,18 @@ struct Quad<float> {
   }
   __device__ __forceinline__ static uint32_t top_bits(uint32_t t) { return t; }
 };
-// fp16 operands of x * up: the rounded pair and what it leaves
+// fp16 operands of a pair: the rounded one and what it leaves, times low_up (a power of two)
 struct HalfPair {
   uint32_t hi, lo;
 };
 template <bool LOW>
-__device__ __forceinline__ HalfPair split_pair(float x0, float x1) {
+__device__ __forceinline__ HalfPair split_pair(float x0, float x1, float low_up = 1.f) {
   HalfPair p;
   p.hi = h2(x0, x1);
   p.lo = 0u;
   if (LOW) {
     const float2 w = h2_float(p.hi);
-    p.lo = h2(x0 - w.x, x1 - w.y);
+    p.lo = h2((x0 - w.x) * low_up, (x1 - w.y) * low_up);
   }
   return p;
 }

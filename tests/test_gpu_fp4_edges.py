@@ -105,3 +105,31 @@ def test_queries_that_are_not_finite(dtype, new, softcap):
             tol = F.tolerance(ref[i:i + 1], s[i:i + 1], n, EPS[dtype], dtype == "bf16", n >= 64, softcap)[0]
             assert (np.abs(got - ref[i]) <= tol)[fine].all(), (b, i)
     assert p.status.item() == 0
+
+
+@pytest.mark.parametrize("d,at", [(64, "first"), (128, "last")])
+def test_many_small_probabilities_beside_one_large_one_in_fp32(d, at):
+    """One key holds nearly everything and 32767 others 2^-e of it each: their sum is part of the result.  Every sequence is the same
+    pages, with queries that give e from 20 to 44; there is an item for every warp, so that one pass over the keys holds them all.
+
+    Keys and queries have one feature: a score is one product.  In base-2 units it is below 2^6 and off by less than 2^-18 of that in fp32
+    steps and 22-bit operands: 2^-12 of a small weight.  Sums of 32768 / 16 parts in fp32: 2^11 2^-24 = 2^-13, twice.  A probability
+    has 22 bits, or is off by at most 2^-43 of the largest."""
+    L, B = 32768, 1776
+    cfg = config(n_q=1, n_kv=1, d=d, page=128, batch=B, pages=L // 128, n_pages=L // 128, dtype="fp32")
+    cache = binding.Fp4Cache(cfg, selection=False)
+    k, v = np.zeros((L, 1, d), np.float32), np.full((L, 1, d), 6.0, np.float32)
+    v[:, 0, 1::2] = -3.0
+    big = 0 if at == "first" else L - 1
+    k[big, 0, 0], v[big] = 6.0, 0.0
+    cache.append(dev(k, torch.float32), dev(v, torch.float32), dev(np.arange(L), torch.int64))
+    table = dev(np.tile(np.arange(L // 128), (B, 1)))
+    e = np.linspace(20, 44, B)
+    q = np.zeros((B, 1, d), np.float32)
+    q[:, 0, 0] = e * np.log(2.0) * np.sqrt(d) / 6.0
+    out = f64(cache.attention(dev(q, torch.float32), table, dev([L] * B)))
+    w = np.exp(-q[:, :, :1].astype(np.float64) * 6.0 / np.sqrt(d))                             # of a small one
+    ref = (L - 1) * w / (1 + (L - 1) * w) * v[L // 2].astype(np.float64)
+    tol = np.abs(ref) * (2.0 ** -12 + 2.0 ** -12) + L * 2.0 ** -43 * 6.0
+    err = np.abs(out - ref)
+    assert (err <= tol).all(), (float(e[np.argmax((err / tol).max((1, 2)))]), float((err / tol).max()))
