@@ -596,6 +596,8 @@ int echokv_fourbit_attention(const echokv_config* cfg, const echokv_fourbit_cach
  * with top and low the page's bounds, s_q = a * (1 / 127) limited to 2^-60 .. 2^100, a the largest magnitude of the query
  * row, code = round(q * (1 / s_q)); the sum is exact, the products are fp32.  A page whose scale is NaN counts as the largest finite
  * score; a query row with an infinity or NaN as a row of zeros.
+ * B: the number of sequences, whose ids lie below it.  Neighbouring tokens of a sequence are taken together, up to n_tokens / B of them, so
+ * a B far above the number of sequences that the tokens are of costs time (one above n_tokens says nothing and is not looked at).
  * n_first >= 0, n_recent >= 1, n_first + n_recent <= n_select <= ECHOKV_FOURBIT_MAX_SELECT (EINVAL).  Tokens with sequence -1: -1 entries.
  * A bad sequence, slot or page -> EBADPAGE, position -> EBADLENGTH: -1 entries (a bad page id: unspecified pages, all of them < p + 1). */
 int echokv_fourbit_select(const echokv_config* cfg, const echokv_fourbit_cache* cache, const void* q, int64_t q_stride,

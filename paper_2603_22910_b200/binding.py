@@ -838,16 +838,17 @@ class Fp4Cache:
                "echokv_fourbit_attention")
         return out
 
-    def _batch(self, seq_slots):
-        return self.cfg.max_batch if seq_slots is None else seq_slots.shape[0]
+    def _batch(self, n_seqs, seq_slots):
+        return n_seqs if n_seqs is not None else self.cfg.max_batch if seq_slots is None else seq_slots.shape[0]
 
     def select_pages(self, q, block_table, token_seqs, positions, n_select: int, n_first: int = 1, n_recent: int = 1, seq_slots=None,
-                     out=None, status=None, stream=None):
+                     out=None, status=None, stream=None, n_seqs: int | None = None):
         """The n_select pages of its sequence that each token reads, per KV head: int32 [T][n_kv_heads][n_select], ascending, -1 behind
         the last one -- the first n_first, the last n_recent, and those with the largest scores (see echokv.h).  token_seqs, positions:
-        plan_tokens'."""
+        plan_tokens'.  n_seqs: how many sequences the tokens are of, all ids below it (None: as many as seq_slots has, or max_batch);
+        a prompt's tokens are taken together, as many as there are to a sequence, so a bound far above it costs time."""
         import torch
-        cfg, T, B = self.cfg, q.shape[0], self._batch(seq_slots)
+        cfg, T, B = self.cfg, q.shape[0], self._batch(n_seqs, seq_slots)
         if self.bounds is None:
             raise ValueError("select_pages: a cache made without selection has no bounds")
         qp, qs = _rows(q, T, cfg.n_q_heads, cfg.head_dim, self.tdtype, "q", cfg.device)
@@ -866,11 +867,12 @@ class Fp4Cache:
         return out
 
     def sparse_attention(self, q, block_table, token_seqs, positions, pages, seq_slots=None, softcap: float = 0.0, alibi_slopes=None,
-                         out=None, status=None, stream=None):
+                         out=None, status=None, stream=None, n_seqs: int | None = None):
         """q [T][n_q_heads][d]: every token attends the pages that pages [T][n_kv_heads][n_select] lists of its sequence (select_pages', or
-        any others), keys up to its own position.  Rows of tokens with sequence -1 stay as they are (in a new tensor: anything)."""
+        any others), keys up to its own position.  Rows of tokens with sequence -1 stay as they are (in a new tensor: anything).  n_seqs: as
+        for select_pages."""
         import torch
-        cfg, T, B = self.cfg, q.shape[0], self._batch(seq_slots)
+        cfg, T, B = self.cfg, q.shape[0], self._batch(n_seqs, seq_slots)
         if pages.dim() != 3 or pages.shape[0] != T or pages.shape[1] != cfg.n_kv_heads:
             raise ValueError("pages: [%d tokens][%d][n_select] is needed" % (T, cfg.n_kv_heads))
         qp, qs, out, op = self._queries(q, out, stream)

@@ -543,8 +543,9 @@ cudaError_t launch(const Fp4SelectArgs& a, int sm_count, cudaStream_t stream) {
     return (size_t)warps * kFsDepth * fs_stage_bytes(D) + (size_t)rows * (2 * D + 4) + tile_tokens * (sizeof(FsGroup) + 4ull * (capacity(warps) + K));
   };
   const auto two_fit = [&] { return smem_of(8) <= kFsRoom / 2 - 1024; };     // on an SM
-  // Tokens of a block: up to how many a sequence has on average (where B is the batch and not only a bound), as many as leave a block for every SM; not 8 where two blocks of 4 fit
-  // on an SM and of 8 do not (4096 tokens of 1250 pages: 987 and 1053 us; where neither do, 256 tokens of 3750 pages, 282 and 194).
+  // Tokens of a block: up to how many a sequence has on average, if there are B of them (more than tokens: B is a bound that says nothing),
+  // as many as leave a block for every SM; not 8 where two blocks of 4 fit on an SM and of 8 do not (4096 tokens of 1250 pages: 987 and
+  // 1053 us; where neither do, 256 tokens of 3750 pages, 282 and 194).
   // With few tokens the pages of one may be in parts.
   while (tile_tokens < kFsMaxTokens && (a.B > a.n_tokens || (long long)tile_tokens * a.B < a.n_tokens) && heads >= 2ll * tile_tokens * sm_count) {
     const bool two = two_fit();

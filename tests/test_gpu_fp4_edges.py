@@ -6,7 +6,7 @@ import torch
 from paper_2603_22910_b200 import binding
 from tests import fp4_ref as F
 from tests import serving_ref as R
-from tests.test_gpu_fp4 import Program
+from tests.test_gpu_fp4 import Program, check_select
 from tests.test_gpu_serving import DT, EPS, config, dev, f64
 
 pytestmark = pytest.mark.gpu
@@ -133,3 +133,25 @@ def test_many_small_probabilities_beside_one_large_one_in_fp32(d, at):
     tol = np.abs(ref) * (2.0 ** -12 + 2.0 ** -12) + L * 2.0 ** -43 * 6.0
     err = np.abs(out - ref)
     assert (err <= tol).all(), (float(e[np.argmax((err / tol).max((1, 2)))]), float((err / tol).max()))
+
+
+@pytest.mark.parametrize("T", [1, 40, 600])
+def test_the_number_of_sequences_changes_no_choice(T):
+    """However many sequences a call says that there are, and so however many tokens a block takes."""
+    cfg = config(n_q=8, n_kv=8, d=64, page=16, batch=300, pages=64, n_pages=200)
+    p = Program(cfg, seed=24)
+    p.step([T + 300, 70])
+    p.step([0, 1])
+    seqs, pos = (dev(np.append(x, [y, -1])) for x, y in zip(p.tokens([T, 1]), (5, 3)))       # then one of a sequence beyond some counts, one of none
+    q, slots = p.rows(T + 3, 8, 2.0), dev(p.slots)
+    want = p.cache.select_pages(q[:T + 1], p.table, seqs[:T + 1], pos[:T + 1], 6, seq_slots=slots[:2], status=p.status)
+    check_select(p, [T, 1], q, want, 6, 1, 1)
+    some = p.cache.sparse_attention(q[:T + 1], p.table, seqs[:T + 1], pos[:T + 1], want, seq_slots=slots[:2], status=p.status)
+    for n in (2, 3, 5, 6, 30, 300):
+        status = dev([0])
+        got = p.cache.select_pages(q, p.table, seqs, pos, 6, seq_slots=slots, status=status, n_seqs=n)
+        assert torch.equal(got[:T + 1], want) and (got[T + 2] == -1).all()
+        assert status.item() == (binding.ECHOKV_EBADPAGE if n <= 5 else 0) and (n > 5 or (got[T + 1] == -1).all())
+        out = p.cache.sparse_attention(q[:T + 1], p.table, seqs[:T + 1], pos[:T + 1], want, seq_slots=slots, status=p.status, n_seqs=n)
+        assert torch.equal(out, some)
+    assert p.status.item() == 0
