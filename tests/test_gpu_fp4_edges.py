@@ -6,7 +6,7 @@ import torch
 from paper_2603_22910_b200 import binding
 from tests import fp4_ref as F
 from tests import serving_ref as R
-from tests.test_gpu_fp4 import Program, check_select
+from tests.test_gpu_fp4 import Program, check_select, check_sparse
 from tests.test_gpu_serving import DT, EPS, config, dev, f64
 
 pytestmark = pytest.mark.gpu
@@ -155,3 +155,105 @@ def test_the_number_of_sequences_changes_no_choice(T):
         out = p.cache.sparse_attention(q[:T + 1], p.table, seqs[:T + 1], pos[:T + 1], want, seq_slots=slots, status=p.status, n_seqs=n)
         assert torch.equal(out, some)
     assert p.status.item() == 0
+
+
+def wide(x, extra=32):
+    """x [T][heads][d] as a slice of rows that are `extra` heads longer, what is around it NaN."""
+    T, heads, d = x.shape
+    rows = torch.full((T, (heads + extra) * d), NAN, dtype=x.dtype, device=x.device)
+    y = rows[:, 8 * d:(8 + heads) * d].view(T, heads, d)
+    y.copy_(x)
+    return y
+
+
+@pytest.mark.parametrize("dtype,d,page,n_q,n_kv,before,new", [
+    ("bf16", 128, 16, 8, 2, [30, 0, 200], [1, 1, 1]), ("fp32", 64, 32, 4, 4, [90, 5], [3, 9]), ("bf16", 64, 64, 16, 8, [100, 0], [40, 130]),
+    ("bf16", 128, 16, 32, 8, [333], [300]), ("bf16", 128, 64, 8, 1, [700], [1])])
+def test_queries_inside_a_wider_tensor_and_results_in_place(dtype, d, page, n_q, n_kv, before, new):
+    """The fused projection's queries give what dense ones give, bit for bit, and so does every call that writes over its queries."""
+    B = len(new)
+    p = Program(config(n_q=n_q, n_kv=n_kv, d=d, page=page, batch=B, pages=1024 // page, n_pages=B * 1024 // page, dtype=dtype), seed=19)
+    p.step(before)
+    p.step(new)
+    q = p.rows(sum(new), n_q, 2.0)
+    inside, slots = wide(q), dev(p.slots)
+    seqs, pos = (dev(x) for x in p.tokens(new))
+    assert len(q) == 1 or inside.stride(0) == (n_q + 32) * d
+    assert torch.equal(p.attend(new, inside), p.attend(new, q))
+    pages = p.cache.select_pages(q, p.table, seqs, pos, 5, seq_slots=slots)
+    check_select(p, new, q, pages, 5, 1, 1)
+    assert torch.equal(p.cache.select_pages(inside, p.table, seqs, pos, 5, seq_slots=slots), pages)
+    some = p.cache.sparse_attention(q, p.table, seqs, pos, pages, seq_slots=slots)
+    check_sparse(p, *p.tokens(new), q, pages.cpu().numpy(), some)
+    assert torch.equal(p.cache.sparse_attention(inside, p.table, seqs, pos, pages, seq_slots=slots), some)
+    over = q.clone()
+    assert p.cache.sparse_attention(over, p.table, seqs, pos, pages, seq_slots=slots, out=over) is over and torch.equal(over, some)
+    want, over = p.attend(new, q), q.clone()
+    assert p.attend(new, over, out=over) is over and torch.equal(over, want)
+    assert p.status.item() == 0
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", [1, 1]), ("fp32", [2, 5]), ("bf16", [200, 90])])
+def test_the_callers_softmax_scale(dtype, new):
+    p = Program(config(n_q=8, n_kv=2, d=64, page=16, batch=2, pages=32, n_pages=64, dtype=dtype, softmax_scale=0.37), seed=20)
+    p.step([40, 3])
+    p.step(new)
+    q = p.rows(sum(new), 8)
+    out, (seqs, pos), at = p.attend(new, q), p.tokens(new), 0
+    pages = np.arange(-(-max(p.lens) // 16))
+    pages = np.broadcast_to(np.where(pages[None, None] <= pos[:, None, None] // 16, pages, -1), (len(pos), 2, len(pages)))
+    some = p.cache.sparse_attention(q, p.table, dev(seqs), dev(pos), dev(pages.copy()), seq_slots=dev(p.slots), status=p.status)
+    for b, n in enumerate(new):
+        rows = sorted({0, n // 2, n - 1})
+        ref, size = R.attend(f64(q[at:at + n]), p.k[b], p.v[b], 0.37, only=rows)
+        for got, chunk in ((out, dtype == "bf16" and 4 * n >= 64), (some, False)):
+            tol = F.tolerance(ref, size, p.lens[b], EPS[dtype], dtype == "bf16", chunk)
+            assert (np.abs(f64(got[at:at + n]) - ref)[rows] <= tol[rows]).all(), b
+        at += n
+    assert p.status.item() == 0
+
+
+def test_a_graph_whose_streams_fork_and_join():
+    """Kernels that may come before the one ahead of them has ended, behind and before events of other streams, in a graph and outside."""
+    cfg = config(n_q=8, n_kv=2, d=128, page=16, batch=2, pages=64, n_pages=128)
+    a, b = Program(cfg, seed=21), Program(cfg, seed=22)
+    for p in (a, b):
+        p.step([500, 90])
+    q, slots, lens = a.rows(2, 8), [dev(p.slots) for p in (a, b)], dev([501, 91])
+    seqs, pos = dev([0, 1]), dev([500, 90])
+    k, v = torch.zeros(2, 2, 128, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 2, 128, dtype=torch.bfloat16, device="cuda")
+    plans = [p.plan([1, 1]) for p in (a, b)]
+    out = [torch.zeros(2, 8, 128, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+
+    def branch(i, p):
+        p.cache.append(k, v, plans[i].slot_map, status=p.status)
+        p.cache.attention(q, p.table, lens, seq_slots=slots[i], out=out[i], status=p.status)
+        pages = p.cache.select_pages(q, p.table, seqs, pos, 6, seq_slots=slots[i], status=p.status)
+        p.cache.sparse_attention(q, p.table, seqs, pos, pages, seq_slots=slots[i], out=out[2 + i], status=p.status)
+
+    def step(main, other):
+        other.wait_stream(main)
+        with torch.cuda.stream(other):
+            branch(1, b)
+        branch(0, a)
+        main.wait_stream(other)
+        return a.cache.attention(out[1], a.table, lens, seq_slots=slots[0])                  # (behind the other stream's last kernel)
+    other, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=stream):
+        last = step(stream, other)
+    for i in range(10):
+        k.copy_(a.rows(2, 2))
+        v.copy_(a.rows(2, 2))
+        graph.replay()
+        got = [x.clone() for x in out] + [last.clone()]
+        for x in out:
+            x.zero_()
+        again = step(torch.cuda.current_stream(), other)
+        assert all(torch.equal(x, y) for x, y in zip(got, out + [again])), i
+    for i, p in enumerate((a, b)):
+        p.note([1, 1], k.float().cpu().numpy(), v.float().cpu().numpy())
+        p.check_cache()
+        p.check_attention([1, 1], q, got[i])
+    assert a.status.item() == 0 and b.status.item() == 0
