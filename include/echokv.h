@@ -491,7 +491,7 @@ typedef struct {
  * A query row with an infinity or NaN: NaN (infinite scores under a cap are the cap).
  * Scores and sums are fp32; codes enter the products exactly; bf16 queries as fp16 (exact around each row's power of two) with
  * probabilities rounded to fp16 (one below 2^-24 of its row's largest may count as 0 beside it), fp32 queries and their
- * probabilities as pairs of fp16 (22 bits).  For a bf16 sequence
+ * probabilities as pairs of fp16 (22 bits; a probability below 2^-29 of its row's largest may count as 0).  For a bf16 sequence
  * with 64 query rows per KV head or more (its new tokens times n_q_heads / n_kv_heads) the values and their scales may be
  * rounded to fp16 as well, and a key or value of the open block that is 2^-28 of that block's largest loses bits (such
  * sequences run on the tcgen05 kernel where that is the faster one, by their lengths). */
@@ -549,7 +549,8 @@ typedef struct {
 /* Sizes implied by a config.  Pure host arithmetic, no CUDA call. */
 int echokv_query_fourbit_sizes(const echokv_config* cfg, echokv_fourbit_sizes* out);
 
-/* A rotation as echokv_rotate's arguments describe it (rot_dim: 0 = head_dim, otherwise a multiple of 16). */
+/* A rotation as echokv_rotate's arguments describe it (rot_dim: 0 = head_dim, otherwise a multiple of 16, in fp32 too, where echokv_rotate
+ * takes multiples of 8: for those, that call and an append without a rotation). */
 typedef struct {
   double theta;                /* >= 1 */
   const int32_t* sections;     /* host [n_axes], or NULL with one axis */
@@ -594,8 +595,9 @@ int echokv_fourbit_attention(const echokv_config* cfg, const echokv_fourbit_cach
  * score, of equal ones the first.  The score of a page is the largest over the query heads that share the KV head of
  *     (s_q * scale) * sum_c (code_c > 0 ? code_c * top_c : code_c * low_c)      (an upper bound of q . k, in 8 bits)
  * with top and low the page's bounds, s_q = a * (1 / 127) limited to 2^-60 .. 2^100, a the largest magnitude of the query
- * row, code = round(q * (1 / s_q)); the sum is exact, the products are fp32.  A page whose scale is NaN counts as the largest finite
- * score; a query row with an infinity or NaN as a row of zeros.
+ * row, code = round(q * (1 / s_q)); the sum is exact, the products are fp32.  (Both sides are rounded to the nearest
+ * of 127 steps, so a page's score may lie below q . k of its best key, by head_dim / 126 of the product of the row's and the page's
+ * largest magnitudes at most.)  A page whose scale is NaN counts as the largest finite score; a query row with an infinity or NaN as a row of zeros.
  * B: the number of sequences, whose ids lie below it.  Neighbouring tokens of a sequence are taken together, up to n_tokens / B of them, so
  * a B far above the number of sequences that the tokens are of costs time (one above n_tokens says nothing and is not looked at).
  * n_first >= 0, n_recent >= 1, n_first + n_recent <= n_select <= ECHOKV_FOURBIT_MAX_SELECT (EINVAL).  Tokens with sequence -1: -1 entries.

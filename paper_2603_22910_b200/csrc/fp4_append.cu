@@ -239,7 +239,8 @@ __global__ void __launch_bounds__(kFaThreads, 4) fp4_append_kernel(const __grid_
 // takes such a page for one head.  It brings the keys of 64 tokens to shared memory at a time, all on their way at once (what the first kernel
 // wrote comes from the second level cache), then goes through them in a short loop, a lane with 8 features of every second
 // (fourth) token, so that little is left to join at the end.  (A kernel like this one runs its code once: what is unrolled is fetched
-// for nothing.  Loads to registers, which the compiler put next to their uses: 20 to 36 us after 34.5 thousand tokens, now 10.)
+// for nothing.  Loads to registers, which the compiler put next to their uses: 20 to 36 us after 34.5 thousand tokens, now 15 behind the
+// kernel before it; 16.5 by itself.)
 constexpr int kFbWarps = 8;
 constexpr int kFbBlocks = 4;                       // of 16 tokens, at a time
 

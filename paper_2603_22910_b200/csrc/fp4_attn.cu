@@ -19,7 +19,7 @@
 //   softmax  The running maximum is a reference that moves only when a score is 2^8 above it; probabilities are 2^5 times themselves, so
 //            that fp16 holds them down to 2^-29 of the largest (with a second half, in fp32, to 2^-42).
 // Measured (device time, both kernels): 16 requests over 32768 keys, 8 bf16 heads of 128 118 us, 5.1 TB/s (the copies alone 110; fp32
-// queries 160); 32 ragged requests of 32 heads, pages of 16, 132 us, capped 147 (copies 122); one request of 777 keys 9.7; 8 drafts
+// queries 158); 32 ragged requests of 32 heads, pages of 16, 132 us, capped 147 (copies 122); one request of 777 keys 9.7; 8 drafts
 // for each of 16 requests over 32768 keys 341 us (by items of 8 rows 434); 64 listed pages of 64 tokens for 16 tokens 27 us. The
 // conversion to fp16 by the instruction and a byte select of its result: 118 us; by shifts 160, by whole-number arithmetic no better.
 #include "fp4_common.cuh"
@@ -32,7 +32,9 @@ namespace echokv {
 namespace {
 
 // Q tiles of 8 query rows make up an item: 1, or 2 where a call may have more rows than one tile has (their values are then converted once).
-// (Heads of 128, one tile: 12 warps 119.5 us for 16 x 32768 keys, 14 134, 16 121; of 64, 16 x 8192 keys of 32 heads: 12 89, 16 79.)
+// (Heads of 128, one tile: 12 warps 119.5 us for 16 x 32768 keys, 14 134, 16 121; of 64, 16 x 8192 keys of 32 heads: 12 89, 16 79.
+// A call's max_new decides for all of its rows: the single tokens of that batch take 118 us in a call of theirs, 138 to 140 where another
+// sequence may have 3 tokens and more, 144 beside chunks.)
 template <int D, int Q>
 struct FqShape {
   static constexpr int kWarps = Q == 2 ? (D == 128 ? 8 : 12) : D == 128 ? 12 : 16, kThreads = kWarps * 32;

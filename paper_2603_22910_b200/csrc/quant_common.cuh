@@ -73,7 +73,8 @@ __device__ __forceinline__ bool take_chunks(const QuantAttnArgs& a, int sm_count
     by_rows += sums[w][0];
     by_chunks += sums[w][1];
   }
-  // 4 bits: by rows 22 us + 46 to 54 ns (heads of 64: 26 to 30) for every unit, by chunks 27 us + 0.25 us for every 16 keys of an item.
+  // 4 bits: by rows 22 us + 46 to 54 ns (heads of 64: 26 to 30) for every unit, by chunks 27 us + 0.25 us for every 16 keys of an item; the
+  // rule takes the upper ends, so between them it says chunks.
   // (Rows and chunks, heads of 128: one sequence over 8192 keys, 16 tokens 32.5 and 36.9 us, 32 tokens 42 and 38, 128 tokens 103 and
   // 46; 64 sequences over 1024, 16 tokens 119 and 104.  Heads of 64: over 8192 keys, 16 tokens 28 and 34, 64 tokens 46 and 37.)
   if (a.format == kFp4) return (a.g.head_dim == 128 ? 54 : 30) * by_rows > 5000ull * sm_count + 250 * by_chunks;

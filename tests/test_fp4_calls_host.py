@@ -1,7 +1,9 @@
 """Calls of the 4-bit cache's entry points that are refused before any CUDA call, or that the binding passes on, without a GPU."""
+import numpy as np
 import pytest
 
 from paper_2603_22910_b200 import binding, build
+from tests import fp4_ref as F
 from tests.test_fp4_host import BF, EINVAL, I32, append_call, fake_cache, rotation
 from tests.test_serving_host import NoStream, OnGpu, P1
 
@@ -41,3 +43,23 @@ def test_the_number_of_sequences_is_passed_on(monkeypatch):
         assert calls["echokv_fourbit_sparse_attention"][11:14] == (16, B, 6)
     with pytest.raises(ValueError, match="seq_slots"):
         cache.select_pages(q, table, ids, ids, 16, out=pages, stream=NoStream(), n_seqs=4, seq_slots=slots)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_how_far_a_pages_score_may_lie_below_its_best_key(d):
+    """q . k <= sum_c max(q_c top_c, q_c low_c), of which each factor is rounded to the nearest of 127 steps of its largest magnitude: a term is
+    off by a_q a_k (1 / 127 + 1 / (2 127)^2) at most, less than 1 / 126 of that, d of them in all (fp32 products: 2^-22 of the score)."""
+    rng = np.random.default_rng(d)
+    below = 0
+    for i in range(200):
+        k, q = rng.standard_normal((16, d)) * rng.uniform(0.1, 3, d), rng.standard_normal(d).astype(np.float32)
+        if i % 3 == 0:
+            k, q = k[:1], np.sign(q) * (1 + 0.49 / 127) * (np.arange(d) > 0) + (np.arange(d) == 0) * np.float32(127)      # one key, rounded down nearly everywhere
+        b, scale = F.bounds(k)
+        s_q = np.abs(q).max() / 127
+        code = np.rint(q / s_q)
+        score = s_q * float(scale) * np.maximum(code * b[0], code * b[1].astype(float)).sum()
+        best = (k @ q).max()
+        below += score < best
+        assert score >= best * (1 - 2.0 ** -22) - d / 126 * np.abs(q).max() * np.abs(k).max()
+    assert below > 0
